@@ -17,350 +17,13 @@
 // scoring pass leaves the float32 logits behind, which one pass over them turns into dz; in a workspace without room
 // for them, for narrow heads (and for blocks of rows whose logits spread too far for E) dz is recomputed tile by tile from H, W and lse.
 // The float32 path, for small shapes, carries its sums in float64 (umas_f32.h).
-#include <math.h>
-
-#include <algorithm>
 #include <mutex>
 
-#include "umas_common.h"
 #include "umas_f32.h"
-#include "umas_mfma.h"
-#include "umas_plan.h"
-#include "umas_surrogate.h"
+#include "umas_gradients.h"
 
 namespace umas {
 namespace {
-
-using Cfg = TileCfg<256, 256, 2, 4>;   // 8 wavefronts, two per SIMD: one issues memory operations while the other feeds the matrix pipe
-using Ring = Ring2Cfg<Cfg>;
-constexpr int kLogitLds = Ring::LDS_BYTES;
-constexpr int kGM = 4, kGN = 8;          // tile group resident on one XCD
-constexpr int kTilesPerWg = 4;           // logit tiles a workgroup computes one after the other (short K: launch gaps and store drain overlap)
-constexpr int kRowBlock = 256;
-constexpr float kNegInf = -INFINITY;
-constexpr float kMasked = -1e30f;        // stands for a logit that does not exist (vocabulary tail)
-
-__device__ __forceinline__ uint16_t f2bf(float x) {
-  return __builtin_bit_cast(uint16_t, static_cast<__bf16>(x));
-}
-// two floats rounded to bf16 in one word (first in the low half): one conversion instruction
-__device__ __forceinline__ uint32_t pack_bf16x2(float lo, float hi) {
-  typedef float f32x2 __attribute__((ext_vector_type(2)));
-  typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
-  return __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2{lo, hi}, bf16x2));
-}
-__device__ __forceinline__ float bf2f(uint16_t b) { return __uint_as_float(static_cast<uint32_t>(b) << 16); }
-
-// Online-softmax partial: m = max z, s = sum exp(z - m), t = sum exp(z - m) z.
-struct Part {
-  float m, s, t;
-};
-__device__ __forceinline__ Part part_merge(Part x, Part y) {
-  if (x.m == kNegInf) return y;
-  if (y.m == kNegInf) return x;
-  const float M = fmaxf(x.m, y.m);
-  const float ex = __expf(x.m - M), ey = __expf(y.m - M);
-  return Part{M, fmaf(x.s, ex, y.s * ey), fmaf(x.t, ex, y.t * ey)};   // written out: the same rounding in every kernel
-}
-
-// ------------------------------------------------------------------ small helpers
-__global__ void __launch_bounds__(256) k_clear(ClearArgs A) {
-  clear_words(A, static_cast<int64_t>(blockIdx.x) * blockDim.x + threadIdx.x, static_cast<int64_t>(gridDim.x) * blockDim.x);
-}
-
-// bytes are a multiple of 4 for every buffer cleared here
-hipError_t clear_bytes(hipStream_t st, void* a, size_t bytes_a, void* b = nullptr, size_t bytes_b = 0, void* c = nullptr, size_t bytes_c = 0) {
-  const ClearArgs A{{static_cast<uint32_t*>(a), static_cast<uint32_t*>(b), static_cast<uint32_t*>(c)},
-                    {static_cast<int64_t>(bytes_a / 4), static_cast<int64_t>(bytes_b / 4), static_cast<int64_t>(bytes_c / 4)}};
-  int64_t most = 0;
-  for (int k = 0; k < 3; ++k) most = A.p[k] ? std::max(most, A.words[k]) : most;
-  if (most == 0) return hipSuccess;
-  hipLaunchKernelGGL(k_clear, dim3(static_cast<unsigned>(std::min<int64_t>(most / 256 + 1, 65536))), dim3(256), 0, st, A);
-  const hipError_t e = hipGetLastError();
-  if (e == hipSuccess && g_prof_on) prof_kernel("k_clear", st);
-  return e;
-}
-
-// Where every weight is read by one tile only (one column tile) and W is larger than the memory-side cache, it is read past it: 203
-// rows of 3584 against 152 064, keeping 300 -> 270 us, 100 and 200 rows of 2048 against 151 936, scoring 153 -> 143 and 187 -> 182.
-// A smaller W may still lie there from the call before (250 rows of 1024 against 30 001, 61 MB: 28 us, past the cache 31), and
-// the better part of one that is a little larger: scoring 256 rows through the cache and past it on two cards, W of 257 MiB 102 and 114, 109 and
-// 116 us (d = 2048), 87 and 96, 89 and 96 (4096), 272 MiB 108 and 116, 119 and 117, 288 MiB 115 and 117, 123 and 119, 312 MiB 117
-// and 117, 125 and 120.  dH, which reads its other operand several times meanwhile, has its line at 256 MiB (update of 256 rows
-// of 1024, 264 MiB: 370 and 343, 384 and 358).
-constexpr int64_t kLogitsOnceBytes = int64_t{300} << 20, kDhOnceBytes = int64_t{256} << 20;
-__device__ __forceinline__ bool beyond_cache(int d, int V, int64_t bytes) { return static_cast<int64_t>(V) * d * 2 > bytes; }
-
-// Logit tile Z[v, n] = W[m0 + v, :] . H[row(n0 + n), :] for a 256x256 block of (vocabulary, selected rows),
-// row(n) = rowsel[sel0 + n] or sel0 + n.  Rows past V and past n_lim are clamped to valid ones; the
-// callers mask what comes out of them.
-template <class C>
-__device__ __forceinline__ void logit_tile(const uint16_t* __restrict__ W, const uint16_t* __restrict__ H, int d, int V,
-                                           const int32_t* __restrict__ rowsel, int64_t sel0, int64_t n_lim, int m0,
-                                           int64_t n0, bool w_once, uint16_t* lds, floatx4 (&acc)[C::MI][C::NI]) {
-#pragma unroll
-  for (int i = 0; i < C::MI; ++i)
-#pragma unroll
-    for (int j = 0; j < C::NI; ++j) acc[i][j] = floatx4{0.f, 0.f, 0.f, 0.f};
-  using R = Ring2Cfg<C>;
-  const uint32_t kofs = ring2_kofs();
-  uint32_t oa[R::NA], ob[R::NB];
-#pragma unroll
-  for (int i = 0; i < R::NA; ++i) oa[i] = (static_cast<uint32_t>(min(ring2_row<C>(i), V - 1 - m0)) * d + kofs) * 2u;
-#pragma unroll
-  for (int i = 0; i < R::NB; ++i) {
-    const int64_t n = sel0 + min(n0 + ring2_row<C>(i), n_lim - 1);
-    ob[i] = (static_cast<uint32_t>(rowsel ? rowsel[n] : n) * d + kofs) * 2u;   // host checks n_rows*d*2 < 2^32
-  }
-  const __amdgpu_buffer_rsrc_t ra = make_rsrc(W + static_cast<int64_t>(m0) * d), rb = make_rsrc(H);
-  if (d % C::BK != 0) mfma_mainloop_ring2<C, true, kCached>(ra, oa, rb, ob, d, lds, acc);
-  else if (w_once) mfma_mainloop_ring2<C, false, kStream>(ra, oa, rb, ob, d, lds, acc);
-  else mfma_mainloop_ring2<C, false, kCached>(ra, oa, rb, ob, d, lds, acc);
-}
-
-// ------------------------------------------------------------------ bf16: logit tiles -> partials
-// A = W (vocabulary rows on the M side, so one lane sees many vocabulary entries of one token),
-// B = rows c0 .. c0 + mc - 1 of the selection.  partial[tile_m][n] = (m, s, t, taken logit or 0).
-//
-// The keeping variant serves the backward pass when the dense part of dz is a row factor times the softmax
-// (no entropy bonus): it also writes E[n, v] = bf16(exp(z[n, v] - c_n)) to the chunk buffer [mcp, Vp], c_n a
-// per-row reference known before the pass (the taken token's logit), so that dz = (a_n exp(c_n - lse_n)) E
-// needs no second pass over the logits: the row factor is applied where dH is written and folded into the
-// copy of H that dW reads.  A block of 256 rows in which some logit exceeds its reference by more than kKeepMaxGap
-// (E could overflow) is flagged and gets its dz from the recomputing kernel instead.
-constexpr float kKeepMaxGap = 50.f;
-// The [rows, vocabulary] operand of the backward (E, or dz on the recomputing path) lies in blocks of 256 rows x 256
-// vocabulary entries, 128 KB each, row-major inside, vocabulary blocks of one block row next to each other: what a
-// gradient tile reads per K step is then one run of memory (32 KB of consecutive rows for dW, four steps per block
-// for dH) instead of 256 or 64 pieces a row pitch of 300 KB apart.
-constexpr int64_t kBlkElems = 256 * 256;
-__host__ __device__ __forceinline__ int64_t blk_offset(int64_t row_blk, int64_t voc_blk, int64_t tiles_v) {
-  return (row_blk * tiles_v + voc_blk) * kBlkElems;
-}
-template <class C>
-struct Stage {                                                                  // every wavefront stages its block: WTN rows x WTM vocabulary entries
-  static constexpr int kPitch = C::WTM * 2 + 16;                                // one staged row of bf16, 16-byte aligned
-  static constexpr int kBytes = C::WM * C::WN * C::WTN * kPitch;
-};
-constexpr int kStagePitch = Stage<Cfg>::kPitch;
-constexpr int kLogitPitch = Cfg::WTM * 4 + 16;                                  // one staged row of logits: 128 floats
-static_assert(kLogitLds <= 160 * 1024, "LDS of one CU");
-
-enum class Leave { kNothing, kNumerators, kLogits };   // what a scoring pass leaves behind for the backward
-struct KeepArgs {
-  const float* cref;   // [n_pad] reference per selected row, NaN for rows without a valid id
-  uint16_t* E;         // [mcp, Vp]
-  int64_t Vp;
-  int32_t* flags;      // per block of 256 selected rows
-  const int32_t* cidx; // per block of 256 selected rows: its place among the chunk's live blocks, -1 for a dead one
-  float* Z;            // Leave::kLogits: the logits, in blocks of 256 x 256 floats in the place and order of the operand's blocks
-};
-
-template <Leave LEAVE, class C>
-__device__ __forceinline__ void score_tile(const uint16_t* __restrict__ W, const uint16_t* __restrict__ H, int d, int V,
-                                           const int32_t* __restrict__ rowsel, int64_t c0, int64_t mc,
-                                           const int32_t* __restrict__ ids, int tile_m, int tile_n, bool w_once,
-                                           float4* __restrict__ partial, int64_t n_pad, const KeepArgs& keep,
-                                           uint16_t* lds) {
-  constexpr bool KEEP = LEAVE == Leave::kNumerators;
-  static_assert(LEAVE != Leave::kLogits || (C::BM == 256 && C::WTM == Cfg::WTM), "logits are kept in rows of 128 of a block's 256 entries");
-  static_assert(256 % C::BM == 0 && 256 % C::BN == 0, "numerators are kept inside a block");
-  constexpr int kPitch = Stage<C>::kPitch;
-  constexpr int kLds = C::T == Cfg::T ? kLogitLds : Ring2Cfg<C>::LDS_BYTES;   // halves of a tile use the whole one's buffers
-  static_assert(Ring2Cfg<C>::LDS_BYTES <= kLds, "the main loop's stages fit");
-  static_assert((LEAVE == Leave::kNothing ? 0 : Stage<C>::kBytes) + (C::WM * C::BN * 3 + C::BN) * 4 <= kLds, "staging and the partials fit the tile buffers");
-  static_assert(LEAVE != Leave::kLogits || 16 * kLogitPitch <= C::WTN * kPitch, "sixteen rows of logits fit a wavefront's stage");
-  const int m0 = tile_m * C::BM;
-  const int64_t n0 = static_cast<int64_t>(tile_n) * C::BN;   // chunk-relative
-  floatx4 acc[C::MI][C::NI];
-  // (a tile that lies past V as a whole, the second half of a block that is kept, reads the last entry)
-  logit_tile<C>(W, H, d, V, rowsel, c0, mc, min(m0, V - 1), n0, w_once, lds, acc);
-
-  // epilogue: the tile buffers are free now.  A lane holds, for each of its NI columns (selected rows), the
-  // vocabulary entries vbase + 16 i + r (i < MI, r < 4); the four lanes l, l + 16, l + 32, l + 48 share a column.
-  float* s_part = reinterpret_cast<float*>(reinterpret_cast<char*>(lds) + (LEAVE == Leave::kNothing ? 0 : Stage<C>::kBytes));   // [WM][BN][3], behind the staging area
-  float* s_zy = s_part + C::WM * C::BN * 3;               // [BN]
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int wm = wave / C::WN;
-  char* stage = reinterpret_cast<char*>(lds) + wave * (LEAVE == Leave::kLogits ? 16 * kLogitPitch : C::WTN * kPitch);
-  if (threadIdx.x < C::BN) s_zy[threadIdx.x] = 0.f;
-  __syncthreads();                                        // every wavefront has left the main loop's LDS reads
-  const int vbase = m0 + wm * C::WTM + (lane >> 4) * 4;   // vocabulary id of element (i = 0, r = 0)
-  const bool tail = m0 + C::BM > V;
-  if (tail) {   // vocabulary ids past V: a large negative logit whose exponential is 0 and whose products stay finite
-#pragma unroll
-    for (int i = 0; i < C::MI; ++i)
-#pragma unroll
-      for (int j = 0; j < C::NI; ++j)
-#pragma unroll
-        for (int r = 0; r < 4; ++r)
-          if (vbase + i * 16 + r >= V) acc[i][j][r] = kMasked;
-  }
-  constexpr float kLog2e = 1.44269504088896341f;
-  bool over = false;
-  // a block of rows none of which has a gradient (all advantages 0) keeps nothing: the backward never looks at it
-  const int64_t row_blk = (c0 + n0) >> 8;
-  const int out_blk = KEEP ? keep.cidx[row_blk] : -1;
-  const bool keeping = KEEP && out_blk >= 0;
-#pragma unroll
-  for (int j = 0; j < C::NI; ++j) {
-    const int col = acc_col<C>(j);
-    const int64_t n = n0 + col;
-    // exponentials of this lane's entries of column j relative to m (log2 domain), their sum s and sum of e z; the
-    // keeping variant stages them as bf16 in this wavefront's LDS region, stored in full lines below
-    float m = kMasked, s = 0.f, t = 0.f;
-    auto column = [&](float ref, auto premultiplied) {
-      const float r2 = ref * kLog2e;
-      s = 0.f;
-      t = 0.f;
-#pragma unroll
-      for (int i = 0; i < C::MI; ++i) {
-        float e[4];
-#pragma unroll
-        for (int r = 0; r < 4; ++r) {
-          const float z = acc[i][j][r];
-          // without a reference from outside: z - m first, exact 0 where a lane holds nothing but vocabulary tail
-          e[r] = decltype(premultiplied)::value ? __builtin_amdgcn_exp2f(fmaf(z, kLog2e, -r2)) : __builtin_amdgcn_exp2f((z - ref) * kLog2e);
-          s += e[r];
-          t = fmaf(e[r], z, t);
-        }
-        if (keeping) {
-          const uint32_t p01 = pack_bf16x2(e[0], e[1]), p23 = pack_bf16x2(e[2], e[3]);
-          *reinterpret_cast<uint2*>(stage + (j * 16 + (lane & 15)) * kPitch + (i * 16 + (lane >> 4) * 4) * 2) =
-              make_uint2(p01, p23);
-        }
-      }
-    };
-    auto lane_max = [&]() {
-      float mx = kMasked;
-#pragma unroll
-      for (int i = 0; i < C::MI; ++i)
-#pragma unroll
-        for (int r = 0; r < 4; ++r) mx = fmaxf(mx, acc[i][j][r]);
-      return mx;
-    };
-    if (keeping) {
-      // The keeping variant sums relative to the row's reference c_n instead of the lane's maximum (any reference
-      // serves the merge as long as nothing overflows), so the exponentials it sums are the numerators it keeps,
-      // and it does not look for the maximum first: a sum beyond 32 e^kKeepMaxGap (or not a number: rows without
-      // a valid id have the reference NaN) shows afterwards that some logit may lie more than kKeepMaxGap above
-      // c_n.  Only then is the column done again the long way, relative to the lane's maximum: a lane whose maximum
-      // does lie that far above c_n flags the block (its dz is recomputed later); rows without a valid id flag
-      // nothing, their row factor is 0.
-      const float c = n < mc ? keep.cref[c0 + n] : 1e30f;   // rows past the chunk: every exponential is 0, E = 0
-      m = c;
-      column(c, std::true_type{});
-      constexpr float kSumLimit = 1.6e23f;                   // 32 e^50 = 1.66e23
-      if (!(s < kSumLimit)) {
-        m = lane_max();
-        const float gap = m - c;
-        over |= gap > kKeepMaxGap;
-        if (gap <= kKeepMaxGap) m = c;                       // many large terms, none too large: c serves after all
-        else if (m == kMasked) m = 0.f;                     // nothing but vocabulary tail in this lane: exponentials 0 as well
-        column(m, std::true_type{});
-      }
-    } else {
-      m = lane_max();
-      column(m, std::false_type{});
-    }
-    if (LEAVE == Leave::kLogits) {
-      // sixteen rows of 128 logits through the wavefront's part of LDS, so that a store covers 512 bytes of two rows
-#pragma unroll
-      for (int i = 0; i < C::MI; ++i)
-        *reinterpret_cast<floatx4*>(stage + (lane & 15) * kLogitPitch + (i * 16 + (lane >> 4) * 4) * 4) = acc[i][j];
-      __builtin_amdgcn_wave_barrier();
-      float* out = keep.Z + blk_offset(n0 >> 8, tile_m, keep.Vp >> 8) + ((n0 & 255) + wave % C::WN * C::WTN + j * 16 + (lane >> 5)) * 256 + wm * C::WTM + (lane & 31) * 4;
-#pragma unroll
-      for (int q = 0; q < 8; ++q)
-        if (n0 + wave % C::WN * C::WTN + j * 16 + q * 2 + (lane >> 5) < mc)   // rows past the chunk: nobody reads them
-          __builtin_nontemporal_store(*reinterpret_cast<const floatx4*>(stage + (q * 2 + (lane >> 5)) * kLogitPitch + (lane & 31) * 16),
-                                      reinterpret_cast<floatx4*>(out + q * 512));
-      __builtin_amdgcn_wave_barrier();
-    }
-    Part p{m, s, t};
-#pragma unroll
-    for (int o = 16; o < kWave; o <<= 1) {
-      const Part q{__shfl_xor(p.m, o, kWave), __shfl_xor(p.s, o, kWave), __shfl_xor(p.t, o, kWave)};
-      p = part_merge(p, q);
-    }
-    if (lane < 16) {
-      float* dst = s_part + (wm * C::BN + col) * 3;
-      dst[0] = p.m; dst[1] = p.s; dst[2] = p.t;
-    }
-    if (!KEEP && n < mc) {                                  // the keeping variant got the taken logits beforehand
-      const int y = ids[rowsel ? rowsel[c0 + n] : c0 + n];
-      const int rel = y - vbase;                           // offset from this lane's first element
-      if (y >= 0 && y < V && rel >= 0 && rel < C::WTM && (rel & 12) == 0) {
-        float zy = 0.f;
-#pragma unroll
-        for (int i = 0; i < C::MI; ++i)
-#pragma unroll
-          for (int r = 0; r < 4; ++r)
-            if (i * 16 + r == rel) zy = acc[i][j][r];
-        s_zy[col] = zy;
-      }
-    }
-  }
-  if (keeping) {
-    if (over) keep.flags[row_blk] = 1;
-    // the staged block goes out 16 bytes per lane: one instruction covers 4 rows x 256 contiguous bytes (of 64 entries a row, 8 x 128)
-    constexpr int kLanes = C::WTM / 8, kRows = kWave / kLanes;
-    const int wn = wave % C::WN;
-    uint16_t* out = keep.E + blk_offset(out_blk, m0 >> 8, keep.Vp >> 8) + ((n0 & 255) + wn * C::WTN) * 256 + (m0 & 255) + wm * C::WTM + lane % kLanes * 8;
-#pragma unroll 8
-    for (int i = 0; i < C::WTN / kRows; ++i) {
-      const int row = i * kRows + lane / kLanes;
-      const uint4 v = *reinterpret_cast<const uint4*>(stage + row * kPitch + lane % kLanes * 16);
-      typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
-      __builtin_nontemporal_store(u32x4{v.x, v.y, v.z, v.w}, reinterpret_cast<u32x4*>(out + row * 256));
-    }
-  }
-  __syncthreads();
-  if (threadIdx.x < C::BN) {
-    const int col = threadIdx.x;
-    Part p{kNegInf, 0.f, 0.f};
-#pragma unroll
-    for (int w = 0; w < C::WM; ++w) {
-      const float* src = s_part + (w * C::BN + col) * 3;
-      p = part_merge(p, Part{src[0], src[1], src[2]});
-    }
-    if (c0 + n0 + col < n_pad) partial[static_cast<int64_t>(tile_m) * n_pad + c0 + n0 + col] = make_float4(p.m, p.s, p.t, s_zy[col]);
-  }
-  __syncthreads();                              // the LDS is the next tile's again
-}
-
-// The tiles of a workgroup.  With few column tiles a workgroup has one tile, and the last round of compute units is often nearly empty: the tiles of
-// one that is at most half full are cut into two of 128 rows of the selection.  594 tiles on 256 compute units, 256 rows: 2048 columns 190 -> 173 us, 3584
-// 283 -> 270; 150 rows 188 -> 170 and 271 -> 262; the update of 203 rows of 3584 1037 -> 1022, with an entropy bonus 1056 -> 1026, 100 rows of 2048 609 ->
-// 584.  (Up to 128 rows all tiles cut, whose other halves have no rows: 100 rows with a bonus 611, of 3584 957 -> 1036.)  Up to eight column tiles, beyond which
-// a workgroup has several: 300, 1000 and 2000 rows of 1536 against 33 001 86.7 -> 76.6, 126.5 -> 114.9 and 204.9 -> 193.5, of 1024 against 100 001
-// 130.1 -> 119.9, 217.8 -> 208.5 and 389.7 -> 382.4, of 2048 against 151 936 294.2 -> 276.9, 553.2 -> 547.4 and 1014 -> 1023, 900 of 3584 918 -> 900; where
-// the last round is fuller nothing changes.
-using HalfCfg = TileCfg<256, 128, 2, 4>;                 // the lanes of a row as in a whole tile: the same bits
-template <Leave LEAVE, class C>
-__device__ __forceinline__ void score_tiles(const uint16_t* __restrict__ W, const uint16_t* __restrict__ H, int d, int V,
-                                            const int32_t* __restrict__ rowsel, int64_t c0, int64_t mc,
-                                            const int32_t* __restrict__ ids, int tiles_m, int tiles_n, int panel,
-                                            float4* __restrict__ partial, int64_t n_pad, const KeepArgs& keep,
-                                            uint16_t* lds, int halved = 0) {
-  const bool w_once = tiles_n == 1 && beyond_cache(d, V, kLogitsOnceBytes);
-  if constexpr (C::BM == 256 && C::BN == 256) {
-    if (halved > 0) {                             // the last `halved` tiles of every XCD
-      const int per_xcd = (tiles_m * tiles_n + 7) / 8, xcd = static_cast<int>(blockIdx.x & 7), w = static_cast<int>(blockIdx.x >> 3), whole = per_xcd - halved;
-      if (w >= whole) {
-        const int in_xcd = whole + (w - whole) / 2, t = xcd * per_xcd + in_xcd, tile_m = t / tiles_n, half = t % tiles_n * 2 + ((w - whole) & 1);
-        if (in_xcd < per_xcd && tile_m < tiles_m && half * HalfCfg::BN < mc)
-          score_tile<LEAVE, HalfCfg>(W, H, d, V, rowsel, c0, mc, ids, tile_m, half, false, partial, n_pad, keep, lds);
-        return;
-      }
-    }
-  }
-  for (int it = 0; it < kTilesPerWg; ++it) {     // a workgroup walks the same place of kTilesPerWg consecutive tile groups
-    int tile_m, tile_n;
-    if (!tile_coords<kGM, kGN>(tiles_m, tiles_n, panel, &tile_m, &tile_n, it, kTilesPerWg)) continue;
-    score_tile<LEAVE, C>(W, H, d, V, rowsel, c0, mc, ids, tile_m, tile_n, w_once, partial, n_pad, keep, lds);
-  }
-}
 
 // (kernel templates whose bodies use buffer resources do not get their host stubs emitted: plain kernels)
 __global__ void __launch_bounds__(Cfg::T)
@@ -370,11 +33,6 @@ k_score_tiles(const uint16_t* __restrict__ W, const uint16_t* __restrict__ H, in
   __shared__ __attribute__((aligned(16))) uint16_t lds[kLogitLds / 2];
   score_tiles<Leave::kNothing, Cfg>(W, H, d, V, rowsel, 0, n_sel, ids, tiles_m, tiles_n, panel, partial, n_pad, KeepArgs{}, lds, halved);
 }
-// Up to 128 selected rows: half-size tiles with a pipeline of their own, two workgroups to a compute unit, so that one
-// fills its stages while the other multiplies (64 rows of 2048 / 3584 against 151 936: 156 / 215 us against 182 / 274 with
-// the large tiles; 128x256 and 256x128 tiles 213 / 347 and 167 / 234).
-using NarrowCfg = TileCfg<128, 128, 2, 2>;
-constexpr int kNarrowLds = Ring2Cfg<NarrowCfg>::LDS_BYTES;
 __global__ void __launch_bounds__(NarrowCfg::T)
 k_score_narrow(const uint16_t* __restrict__ W, const uint16_t* __restrict__ H, int d, int V,
                const int32_t* __restrict__ rowsel, int64_t n_sel, const int32_t* __restrict__ ids,
@@ -421,9 +79,6 @@ k_score_logits(const uint16_t* __restrict__ W, const uint16_t* __restrict__ H, i
 // compute unit; partials [workgroup][row].
 // 24 rows of 2048 (3584) against 151 936: 256x256 tiles 183 (279) us, this kernel 117 (199) us = 5.3 (5.5) TB/s of W; 64
 // rows of 2048 182 -> 122 us.
-constexpr int kFewWaves = 8, kFewT = kFewWaves * kWave;
-inline int few_pieces(int d) { return static_cast<int>(cdiv(d, kFewWaves * 64)); }   // PPW
-inline int few_rows(int d) { return few_pieces(d) <= 4 ? 64 : few_pieces(d) <= 8 ? 32 : 0; }   // what the registers hold
 template <int NI, int PPW>
 __global__ void __launch_bounds__(kFewT)
 k_score_few(const uint16_t* __restrict__ W, const uint16_t* __restrict__ H, int d, int V, const int32_t* __restrict__ rowsel, int n_sel,
@@ -535,60 +190,6 @@ k_score_few(const uint16_t* __restrict__ W, const uint16_t* __restrict__ H, int 
   }
 }
 
-// Merge the per-tile partials of each selected row; compact results and optional scatter.  Eight lanes of a wavefront
-// share a row (lane = 8 * part + row within the group of 8 rows, so a load covers whole 128-byte lines), four loads in
-// flight each.  Where there are few rows the four wavefronts of the workgroup share the group's tiles as well (SPLIT):
-// 24 rows of 594 tiles 41 -> 7 us, 16 100 rows 53 -> 36; with enough rows to fill the chip the extra merge only costs
-// (39 000 rows, 373 MB: 82 us split, 69 not).
-constexpr int64_t kFinSplitRows = 20000;
-// Row n's parts merged; true in the thread that has the result (SPLIT: one of the first eight of the workgroup).
-template <bool SPLIT>
-__device__ __forceinline__ bool merge_parts(const float4* __restrict__ partial, int tiles_m, int64_t n_pad, int64_t n, bool live, Part& p, float& zy) {
-  __shared__ float4 s_part[4][8];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  constexpr int kParts = SPLIT ? 32 : 8;
-  p = Part{kNegInf, 0.f, 0.f};
-  zy = 0.f;
-  if (live) {
-    for (int t0 = SPLIT ? threadIdx.x >> 3 : lane >> 3; t0 < tiles_m; t0 += 4 * kParts) {
-      float4 q[4];
-#pragma unroll
-      for (int k = 0; k < 4; ++k)
-        q[k] = t0 + k * kParts < tiles_m ? partial[static_cast<int64_t>(t0 + k * kParts) * n_pad + n] : make_float4(kNegInf, 0.f, 0.f, 0.f);
-#pragma unroll
-      for (int k = 0; k < 4; ++k) {
-        p = part_merge(p, Part{q[k].x, q[k].y, q[k].z});
-        zy += q[k].w;
-      }
-    }
-  }
-#pragma unroll
-  for (int o = 8; o < kWave; o <<= 1) {
-    const Part q{__shfl_xor(p.m, o, kWave), __shfl_xor(p.s, o, kWave), __shfl_xor(p.t, o, kWave)};
-    p = part_merge(p, q);
-    zy += __shfl_xor(zy, o, kWave);
-  }
-  if constexpr (SPLIT) {
-    if (lane < 8) s_part[wave][lane] = make_float4(p.m, p.s, p.t, zy);
-    __syncthreads();
-    if (wave == 0) {
-#pragma unroll
-      for (int k = 1; k < 4; ++k) {
-        const float4 q = s_part[k][lane & 7];
-        p = part_merge(p, Part{q.x, q.y, q.z});
-        zy += q.w;
-      }
-    }
-  }
-  return lane < 8 && live && (!SPLIT || wave == 0);
-}
-struct RowScore {
-  float logp, lse, entropy;
-};
-__device__ __forceinline__ RowScore row_score(const Part& p, float zy, bool ok) {
-  const float l = p.m + logf(p.s);
-  return RowScore{ok ? zy - l : 0.f, l, ok ? l - p.t / p.s : 0.f};
-}
 template <bool SPLIT>
 __global__ void __launch_bounds__(256)
 k_score_finalize(const float4* __restrict__ partial, int tiles_m, int64_t n_pad, int64_t n_begin,
@@ -709,116 +310,6 @@ __device__ __forceinline__ void ppo_stats_by_row(int k, const Surrogate& S, int6
   stats[k] = loss_stats(sum, k, entropy_coef, norm_rows);
 }
 
-// ------------------------------------------------------------------ bf16: blocks of rows that have a gradient
-// A selected row whose advantage is 0 has g = 0 and (without an entropy bonus or a KL term) no gradient at all; group-normalised
-// outcome rewards make whole trajectory groups such rows.  The keeping pass therefore works on the chunk's live blocks
-// of 256 selected rows only: E and the scaled copy of H hold them packed, dH has as many row tiles and dW as many K
-// steps as there are, and everything that depends on their number is worked out on the device.
-struct LiveInfo {
-  int32_t n_live;        // live blocks of the chunk
-  int32_t k_rows;        // rows of the packed operands that exist (the chunk's last block may be partly filled)
-  XcdShares dw;          // dW tiles per XCD (see share_dw)
-  int32_t next[8];       // per XCD: next place of its sequence of tiles, counted up by the workgroups of k_gemm_dh_dw
-};
-// Shares of the dW tiles per XCD for k_gemm_dh_dw: every XCD first works through its eighth of the dH tiles (contiguous
-// ranges, slice after slice; a tile costs about Vp / slices of K), then dW tiles (k_len of K each) go to the XCDs so that all
-// finish as evenly as possible.  Shares are whole groups where there are many: an XCD's workgroups that work on parts of two
-// groups at a time read a third more through its L2 (39 000 rows of 2048: 6 % of the step).
-constexpr int64_t kTileOverheadK = 768;   // what a tile costs besides its K steps (first loads, epilogue), as a length of K
-__device__ __forceinline__ int share_unit(int tiles, int slices) { return slices == 1 && tiles >= 8 * kGM * kGN ? kGM * kGN : 1; }
-__device__ __forceinline__ int dh_first(int tiles_dh, int slices, int xcd) {
-  const int unit = share_unit(tiles_dh, slices), units = (tiles_dh + unit - 1) / unit;
-  return min(static_cast<int>(static_cast<int64_t>(units) * xcd / 8) * unit, tiles_dh);
-}
-// K of the dW tiles: whole steps of 64 rows.  (With whole blocks of 256, and dH tiles that read and
-// multiply the rows that are not there as well: both products of 30 / 100 rows of 3584 672 us, now 612 / 620; update of 300 / 550 rows of 2048 976 / 1327,
-// now 890 / 1252.)
-__device__ __forceinline__ int dw_k(int k_rows) { return (k_rows + 63) / 64 * 64; }
-// Called by one wavefront; lane x of every eight works for XCD x (all eights do the same).  (One thread walking the eight XCDs took 20 us.)
-__device__ void share_dw(int tiles_r, int tiles_v, int tiles_d, int64_t Vp, int slices, int64_t k_len, XcdShares* out) {
-  const int x = threadIdx.x & 7;
-  auto sum8 = [](int64_t v) {
-#pragma unroll
-    for (int o = 4; o > 0; o >>= 1) v += static_cast<int64_t>(__shfl_xor(static_cast<long long>(v), o, kWave));
-    return v;
-  };
-  const int tiles_dh = tiles_r * tiles_d * slices;
-  const int64_t load = (dh_first(tiles_dh, slices, x + 1) - dh_first(tiles_dh, slices, x)) * (Vp / slices + kTileOverheadK);
-  const int tiles_dw = tiles_v * tiles_d, unit = share_unit(tiles_dw, 1);
-  const int64_t units = (tiles_dw + unit - 1) / unit;
-  k_len *= unit;
-  int64_t cnt;
-  if (k_len <= 0 || units == 0) {                      // nothing to even out
-    cnt = units / 8 + (x < units % 8 ? 1 : 0);
-  } else {
-    // the level up to which the XCDs would be filled if units could be cut: those that stand above it as they are take nothing ...
-    // (a search for it among whole numbers took 23 rounds: k_live_scan 9.6 us, now 5.1)
-    double level = 0.0;
-    bool takes = true;
-    for (int round = 0; round < 8; ++round) {
-      level = static_cast<double>(units * k_len + sum8(takes ? load : 0)) / static_cast<double>(sum8(takes ? 1 : 0));
-      const bool above = takes && static_cast<double>(load) >= level;
-      if (!__any(above)) break;
-      takes = takes && !above;
-    }
-    cnt = takes ? static_cast<int64_t>((level - static_cast<double>(load)) / static_cast<double>(k_len)) : 0;
-    // ... and of the few units that are left every one goes where it is done first (or comes, by rounding, from where it would be last)
-    for (int64_t left = units - sum8(cnt); left != 0; left -= left > 0 ? 1 : -1) {
-      const int64_t end = left > 0 ? -(load + cnt * k_len) : cnt > 0 ? load + cnt * k_len : INT64_MIN;
-      int64_t best = end;
-#pragma unroll
-      for (int o = 4; o > 0; o >>= 1) best = max(best, static_cast<int64_t>(__shfl_xor(static_cast<long long>(best), o, kWave)));
-      if (x == __ffsll(static_cast<long long>(__ballot(end == best))) - 1) cnt += left > 0 ? 1 : -1;
-    }
-  }
-  int first = static_cast<int>(cnt);                   // inclusive prefix sums: where the next XCD's units start
-#pragma unroll
-  for (int o = 1; o < 8; o <<= 1) {
-    const int t = __shfl_up(first, o, kWave);
-    if (x >= o) first += t;
-  }
-  if (threadIdx.x == 0) out->first[0] = 0;
-  if (threadIdx.x < 8) out->first[x + 1] = static_cast<int>(min(static_cast<int64_t>(first) * unit, static_cast<int64_t>(tiles_dw)));
-}
-// Packs the live blocks of a chunk, blk0 its first block; one workgroup, thread t has block t and knows if it is live.
-struct LiveArgs {
-  int blk0, nblk;
-  int64_t rows;
-  int all_live, tiles_v, tiles_d;
-  int64_t Vp;
-  int slices;
-  const int32_t* blk_live;
-  int32_t *blk_cidx, *blk_orig;
-  LiveInfo* info;
-};
-__device__ __forceinline__ void live_scan(const LiveArgs& A, int live) {
-  __shared__ int smem[32];
-  __shared__ int s_last_live;
-  const int t = threadIdx.x;
-  int total;
-  const int pos = block_excl_scan<int>(live, smem, &total);
-  if (t < A.nblk) {
-    A.blk_cidx[A.blk0 + t] = live ? pos : -1;
-    if (live) A.blk_orig[A.blk0 + pos] = t;
-  }
-  if (t == A.nblk - 1) s_last_live = live;
-  __syncthreads();
-  const int64_t last_rows = A.rows - static_cast<int64_t>(A.nblk - 1) * 256;   // rows of the chunk's last block
-  const int k_rows = static_cast<int>(s_last_live ? static_cast<int64_t>(total - 1) * 256 + last_rows : static_cast<int64_t>(total) * 256);
-  if (t == 0) {
-    A.info->n_live = total;
-    A.info->k_rows = k_rows;
-  }
-  if (t < 8) A.info->next[t] = 0;
-  if (t < kWave) share_dw(total, A.tiles_v, A.tiles_d, A.Vp, A.slices, total > 0 ? dw_k(k_rows) + kTileOverheadK : 0, &A.info->dw);
-}
-// One launch per chunk (all blocks live with all_live).
-__global__ void __launch_bounds__(512)
-k_live_scan(LiveArgs A) {
-  const int t = threadIdx.x;
-  live_scan(A, t < A.nblk && (A.all_live || A.blk_live[A.blk0 + t]));
-}
-
 // What opens the keeping update, in one launch: the first nblk workgroups mark the live blocks of 256 selected rows and
 // clear their flags, the others take the rows' references and clear what the call defines everywhere (logp_new when rows
 // are left out, dH), each its share.  Up to kFewBlocks blocks in one chunk the first workgroup alone marks them and packs them as well, under the
@@ -844,12 +335,6 @@ struct OpenArgs {
   LiveArgs live;
 };
 // ------------------------------------------------------------------ bf16: row references and row factors of the keeping pass
-__device__ __forceinline__ void bf16x8_to_f32(const uint4 v, float (&o)[8]) {
-  o[0] = __uint_as_float(v.x << 16); o[1] = __uint_as_float(v.x & 0xffff0000u);
-  o[2] = __uint_as_float(v.y << 16); o[3] = __uint_as_float(v.y & 0xffff0000u);
-  o[4] = __uint_as_float(v.z << 16); o[5] = __uint_as_float(v.z & 0xffff0000u);
-  o[6] = __uint_as_float(v.w << 16); o[7] = __uint_as_float(v.w & 0xffff0000u);
-}
 __global__ void __launch_bounds__(256)
 k_update_open(OpenArgs A) {
   if (A.pack && blockIdx.x == 0) {
@@ -1017,87 +502,6 @@ k_rows_few(RowsArgs A) {
   }
 }
 
-// ------------------------------------------------------------------ bf16: dz tiles into the chunk buffer
-// For blocks of rows whose numerators do not serve, and with an entropy bonus for narrow heads and in a small workspace (16 100 rows of 2048 in 2 GB,
-// chunks of 3300: 31.3 ms; chunks of logits of half that many rows would add to dW twice as often).  Same tile product as k_score_tiles; the epilogue forms the dense part of dz = g (onehot - softmax),
-// -g exp(z - lse), plus the entropy bonus's term when its coefficient is not 0, and writes it as bf16 to
-// dZ [mcp, Vp].  Rows past the chunk and vocabulary ids past V get 0.  The one-hot part g at v = y is a single term per row and is added in
-// float32 where dH and dW are written, so that it never meets the bf16 rounding of the dense part.
-// CLEAR: the taken token's entry of every row is left at 0 (see k_ppo_rows); the others leave that to who goes over the rows afterwards.
-template <bool CLEAR>
-__device__ __forceinline__ void dz_tile(int tile_m, int tile_n, const uint16_t* __restrict__ W, const uint16_t* __restrict__ H,
-                                        int d, int V, const int32_t* __restrict__ rowsel, int64_t c0, int64_t mc, const int32_t* __restrict__ ids,
-                                        const float* __restrict__ lse_c, const float* __restrict__ a_c,
-                                        const float* __restrict__ kz_c, uint16_t* __restrict__ dZ, int64_t Vp, int out_blk,
-                                        uint16_t* lds) {
-  using C = Cfg;
-  const int m0 = tile_m * C::BM;
-  const int64_t n0 = static_cast<int64_t>(tile_n) * C::BN;   // chunk-relative
-  floatx4 acc[C::MI][C::NI];
-  logit_tile<C>(W, H, d, V, rowsel, c0, mc, m0, n0, false, lds, acc);
-
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int wm = wave / C::WN;
-  const int vbase = m0 + wm * C::WTM + (lane >> 4) * 4;
-  const bool tail = m0 + C::BM > V;
-  // each wavefront stages its 64 (rows) x 128 (vocabulary) block; the 272-byte pitch keeps 16-byte alignment
-  char* stage = reinterpret_cast<char*>(lds) + wave * (C::WTN * kStagePitch);
-  __syncthreads();                              // every wavefront has left the main loop's LDS reads
-  if (tail) {                                   // vocabulary ids past V: the exponential below is 0, the factor next to it finite
-#pragma unroll
-    for (int i = 0; i < C::MI; ++i)
-#pragma unroll
-      for (int j = 0; j < C::NI; ++j)
-#pragma unroll
-        for (int r = 0; r < 4; ++r)
-          if (vbase + i * 16 + r >= V) acc[i][j][r] = kMasked;
-  }
-#pragma unroll
-  for (int j = 0; j < C::NI; ++j) {
-    const int64_t n = n0 + acc_col<C>(j);
-    // dz = p (a + kz z) with p = exp(z - lse), a = -g + k (entropy - lse), kz = k = entropy_coef / n_sel: the
-    // dense part of g (onehot - p) plus the entropy bonus's k p (log p + entropy).  Rows past the chunk: p = 0.
-    float l2 = 1e30f, a = 0.f, kz = 0.f;
-    if (n < mc) {
-      l2 = lse_c[c0 + n] * 1.44269504088896341f;
-      a = a_c[c0 + n];
-      kz = kz_c[c0 + n];
-    }
-#pragma unroll
-    for (int i = 0; i < C::MI; ++i) {
-      float dz[4];
-#pragma unroll
-      for (int r = 0; r < 4; ++r) {
-        const float z = acc[i][j][r];
-        dz[r] = __builtin_amdgcn_exp2f(fmaf(z, 1.44269504088896341f, -l2)) * fmaf(kz, z, a);
-      }
-      const uint32_t p01 = pack_bf16x2(dz[0], dz[1]), p23 = pack_bf16x2(dz[2], dz[3]);
-      // staged in this wavefront's LDS region, stored in full lines below
-      *reinterpret_cast<uint2*>(stage + (j * 16 + (lane & 15)) * kStagePitch + (i * 16 + (lane >> 4) * 4) * 2) =
-          make_uint2(p01, p23);
-    }
-  }
-  const int wn = wave % C::WN;
-  if constexpr (CLEAR) {                        // a lane per staged row (every entry compared above: 60 bytes of scratch a lane, like this 20; with no block flagged 6.9 us and 6.55)
-    static_assert(C::WTN == kWave, "a row a lane");
-    __builtin_amdgcn_wave_barrier();
-    const int64_t n = n0 + wn * C::WTN + lane;
-    const int y = (n < mc ? ids[rowsel ? rowsel[c0 + n] : c0 + n] : -1) - (m0 + wm * C::WTM);
-    const uint16_t none = 0;
-    if (y >= 0 && y < C::WTM) __builtin_memcpy(stage + lane * kStagePitch + y * 2, &none, 2);
-    __builtin_amdgcn_wave_barrier();
-  }
-  // the staged block goes out 16 bytes per lane: one instruction covers 4 rows x 256 contiguous bytes
-  uint16_t* out = dZ + blk_offset(out_blk, tile_m, Vp >> 8) + (wn * C::WTN) * 256 + wm * C::WTM + (lane & 15) * 8;
-#pragma unroll 8
-  for (int i = 0; i < C::WTN / 4; ++i) {
-    const int row = i * 4 + (lane >> 4);
-    const uint4 v = *reinterpret_cast<const uint4*>(stage + row * kStagePitch + (lane & 15) * 16);
-    typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
-    __builtin_nontemporal_store(u32x4{v.x, v.y, v.z, v.w}, reinterpret_cast<u32x4*>(out + row * 256));
-  }
-  __syncthreads();                              // the LDS is the next tile's again
-}
 __global__ void __launch_bounds__(Cfg::T)
 k_dz_tiles(const uint16_t* __restrict__ W, const uint16_t* __restrict__ H, int d, int V,
            const int32_t* __restrict__ rowsel, int64_t c0, int64_t mc,
@@ -1107,12 +511,11 @@ k_dz_tiles(const uint16_t* __restrict__ W, const uint16_t* __restrict__ H, int d
   for (int it = 0; it < kTilesPerWg; ++it) {     // a workgroup walks the same place of kTilesPerWg consecutive tile groups
     int tile_m, tile_n;
     if (!tile_coords<kGM, kGN>(tiles_m, tiles_n, panel, &tile_m, &tile_n, it, kTilesPerWg)) continue;
-    dz_tile<false>(tile_m, tile_n, W, H, d, V, rowsel, c0, mc, nullptr, lse_c, a_c, kz_c, dZ, Vp, tile_n, lds);
+    dz_tile(tile_m, tile_n, W, H, d, V, rowsel, c0, mc, LeaveRows{}, lse_c, a_c, kz_c, dZ, Vp, tile_n, lds);
   }
 }
 // The same tiles for the blocks of 256 rows that the keeping scoring pass has flagged, and only those: a fixed,
 // small grid walks (flagged block, vocabulary tile) pairs, so that the usual case of no flag costs next to nothing.
-constexpr int kFlaggedGrid = 256;
 __global__ void __launch_bounds__(Cfg::T)
 k_dz_flagged(const uint16_t* __restrict__ W, const uint16_t* __restrict__ H, int d, int V,
              const int32_t* __restrict__ rowsel, int64_t c0, int64_t mc, const int32_t* __restrict__ ids,
@@ -1124,7 +527,7 @@ k_dz_flagged(const uint16_t* __restrict__ W, const uint16_t* __restrict__ H, int
     const int out_blk = cidx[(c0 >> 8) + tile_n];
     if (!flags[(c0 >> 8) + tile_n] || out_blk < 0) continue;        // the same for every thread of the grid
     for (int tile_m = blockIdx.x; tile_m < tiles_m; tile_m += gridDim.x)
-      dz_tile<true>(tile_m, tile_n, W, H, d, V, rowsel, c0, mc, ids, lse_c, a_c, kz_c, dZ, Vp, out_blk, lds);
+      dz_tile(tile_m, tile_n, W, H, d, V, rowsel, c0, mc, ClearTaken{rowsel, ids}, lse_c, a_c, kz_c, dZ, Vp, out_blk, lds);
   }
 }
 
@@ -1197,391 +600,13 @@ k_dz_rows(const uint16_t* __restrict__ H, int d, int V, const int32_t* __restric
   for (int k = lane; k < d / 8; k += kWave) reinterpret_cast<uint4*>(Hs + (static_cast<int64_t>(k >> 5) * mcp + m) * 256)[k & 31] = h[k];
 }
 
-// ------------------------------------------------------------------ bf16: the two gradient products
-// dH = dZ W: A = dZ [mcp, Vp] (or the kept numerators E) is K-contiguous (K = vocabulary), B = W [V, d] is K-major and is read as it lies.
-//   dH[rowsel[c0 + m], j] = bf16(sc[m] C[m, j] + g[m] W[y[m], j]) for m < mc (sc: the keeping pass's row factor, else 1)
-// dW = dZ^T H: K = rows of the chunk; A = dZ [mcp, Vp] and B = the selected rows of H, copied (and scaled), are both K-major.
-//   dW[v, j] (+)= C[v, j]
-// (kernel templates whose bodies use buffer resources do not get their host stubs emitted: plain kernels)
-template <class C>
-__device__ __forceinline__ void zero_acc(floatx4 (&acc)[C::MI][C::NI]) {
-#pragma unroll
-  for (int i = 0; i < C::MI; ++i)
-#pragma unroll
-    for (int j = 0; j < C::NI; ++j) acc[i][j] = floatx4{0.f, 0.f, 0.f, 0.f};
-}
-// K-contiguous operand tile: block row `row_blk` of the blocked [rows, vocabulary] operand from vocabulary block `voc_blk` on, of which the
-// first `rows` rows are wanted: a pass of loads behind them takes the lines of the first one again, which are on their way to this
-// compute unit anyhow (the last row for all of them made one line hot: 203 rows of 2048 613 -> 650 us); K runs over the vocabulary, four steps of 64 per block
-template <class C>
-__device__ __forceinline__ KContig blocked_rows_tile(const uint16_t* X, int blk_pitch, int64_t tiles_v, int64_t row_blk, int voc_blk, int rows) {
-  KContig c;
-  c.rsrc = make_rsrc(X + blk_offset(row_blk, voc_blk, tiles_v) * blk_pitch);
-  c.hi_bytes = static_cast<uint32_t>(kBlkElems * 2 * blk_pitch - 4 * 128);        // from the fourth step of a block to the next block
-  const int tid = tile_thread();
-  const uint32_t kofs = ring2_kofs(tid);
-#pragma unroll
-  for (int i = 0; i < 4; ++i) c.off[i] = (static_cast<uint32_t>(ring2_row<C>(ring2_row<C>(i, 0) < rows ? i : 0, tid)) * 256u + kofs) * 2u;
-  return c;
-}
-
-// A tile's accumulators go out as float32 rows, `ld` floats apart from `out` on (or are added to what is there); rows and cols
-// of them exist, cols a multiple of 4.  A 16x16 block's registers cover 64 bytes of four rows each; stored like that, half a
-// line at a time, they kept the dW tiles of short selections waiting (725 rows of 2048 against 151 936: both products 2.1
-// ms, through LDS 1.3 ms).  Every wavefront turns its 128 x 64 block through its own part of LDS, 32 rows at a time, and
-// stores 256 bytes of four rows.  In a tile that exists as a whole nothing depends on the row: what is there already is
-// under way during the turn, and a piece's LDS reads and stores go out together (waiting for each of 32 pieces by itself:
-// both products of 725 rows of 2048 that add to dW 1155 us, together 1020; 64 rows without adding 459 and 443).  With `past` what is there is read
-// past the caches, which leaves them to the operands (see past_caches).  Such a piece is addressed by 32-bit offsets from the wavefront's first row; rows farther apart than
-// kPieceLd take the way of the tiles that end early, with 64-bit addresses.
-constexpr int kTurnBytes = 32 * 64 * 4;                              // 32 rows of 64 floats per wavefront
-constexpr int64_t kPieceLd = int64_t{1} << 22;                       // floats
-static_assert(((Cfg::WTM - 1) * kPieceLd + Cfg::WTN) * 4 < int64_t{1} << 31, "the last row of a wavefront's block is in reach");
-static_assert(Cfg::WTN == 64 && Cfg::WM * Cfg::WN == 8 && 8 * kTurnBytes <= 2 * Cfg::BM * 128, "the turn fits two stages of an operand");
-// 32 rows (blocks 2 h and 2 h + 1) of a wavefront's accumulators into its part of LDS, and four columns of four rows (4 i + lane /
-// 16) back.  The 16-byte unit u of row r lies in unit u ^ 4 ((r >> 2) & 3): neither side meets a bank twice.
-__device__ __forceinline__ void turn_in(const floatx4 (&acc)[Cfg::MI][Cfg::NI], int h, char* turn, int lane) {
-#pragma unroll
-  for (int bj = 0; bj < Cfg::NI; ++bj)
-#pragma unroll
-    for (int bi = 0; bi < 2; ++bi)
-#pragma unroll
-      for (int r = 0; r < 4; ++r)
-        *reinterpret_cast<float*>(turn + (bi * 16 + (lane >> 4) * 4 + r) * 256 + (((bj * 4 + ((lane >> 2) & 3)) ^ (4 * (lane >> 4))) * 16) + (lane & 3) * 4) =
-            acc[h * 2 + bi][bj][r];
-  __builtin_amdgcn_wave_barrier();
-}
-__device__ __forceinline__ floatx4 turn_out(const char* turn, int i, int lane) {
-  return *reinterpret_cast<const floatx4*>(turn + (i * 4 + (lane >> 4)) * 256 + (((lane & 15) ^ (4 * (i & 3))) * 16));
-}
-// dW that is added to is read past the caches (two updates of which the second adds, 203 rows of 2048 1454 -> 1380 us, 300 1950 -> 1885, 725 rows four times 5.82 ->
-// 5.73 ms) unless its rows start in the middle of 64 bytes: then every piece of a row shares lines with its neighbours, which read them once more.  Four updates of 200
-// rows of 2048 against 115 915, first of all through the caches, past them: 2056 columns 1943.6 and 2199.1 us (both products), 3592 against 60 001 1777.9 and
-// 2136.5, but 2064 1861.1 and 1930.8 in an update of 2966.7 and 2806.  A dW that the memory-side cache holds is read past the others all the same: eight of 367 rows
-// of 1096 against 50 001 (209 MiB) 2461 us and 2383.
-__device__ __forceinline__ bool past_caches(int d, int V) { return d % 16 == 0 || !beyond_cache(d, V, int64_t{128} << 20); }   // twice that in dW
-// `turn` is the wavefront's own part of LDS
-template <class C>
-__device__ __forceinline__ void store_acc_f32(const floatx4 (&acc)[C::MI][C::NI], char* turn, float* out, int64_t ld, int64_t rows, int cols,
-                                              int accumulate, bool past) {
-  static_assert(C::WTM == Cfg::WTM && C::WTN == Cfg::WTN, "the turn is written for these");
-  typedef float f32x4_a4 __attribute__((ext_vector_type(4), aligned(4)));   // dW has the alignment of a float
-  const int tid = tile_thread(), lane = tid & 63, wave = tid >> 6;
-  const int r0 = wave / C::WN * C::WTM, c0 = wave % C::WN * C::WTN + (lane & 15) * 4;
-  const bool whole = rows >= C::BM && cols >= C::BN && ld <= kPieceLd;   // the same for every thread
-  float* const dst = out + (r0 + (lane >> 4)) * ld + c0;
-  constexpr int kPieces = C::MI / 2;
-  // Each case is a run of its own: with the branches inside, the waits cannot tell what is under way and are for everything, the stores of
-  // the piece before included.
-  auto pieces = [&](auto add, auto past) {
-    constexpr bool kAdd = decltype(add)::value;
-    constexpr int kRead = decltype(past)::value ? kStream : kCached;
-    // (one offset a lane and one a piece: 32 addresses of 64 bits would be a quarter of the registers)
-    typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
-    const int w_row = __builtin_amdgcn_readfirstlane(r0), w_col = __builtin_amdgcn_readfirstlane(wave) % C::WN * C::WTN;
-    const __amdgpu_buffer_rsrc_t rsrc = make_rsrc(out + w_row * ld + w_col);
-    const int at = static_cast<int>((lane >> 4) * ld + (lane & 15) * 4) * 4, step = static_cast<int>(ld) * 16;   // four rows
-    floatx4 have[8];                                                 // what is there already, a piece ahead
-    auto fetch = [&](int h) {
-#pragma unroll
-      for (int i = 0; i < 8; ++i)
-        have[i] = __builtin_bit_cast(floatx4, __builtin_amdgcn_raw_buffer_load_b128(rsrc, at, (h * 8 + i) * step, kRead));
-    };
-    if constexpr (kAdd) fetch(0);
-#pragma unroll
-    for (int h = 0; h < kPieces; ++h) {
-      turn_in(acc, h, turn, lane);
-      floatx4 x[8];
-#pragma unroll
-      for (int i = 0; i < 8; ++i) x[i] = turn_out(turn, i, lane);
-      if constexpr (kAdd) {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) x[i] += have[i];
-        if (h + 1 < kPieces) fetch(h + 1);
-      }
-#pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, x[i]), rsrc, at, (h * 8 + i) * step, kStream);
-      }
-      __builtin_amdgcn_wave_barrier();
-    }
-  };
-  if (whole && accumulate && past) {
-    pieces(std::true_type(), std::true_type());
-  } else if (whole && accumulate) {
-    pieces(std::true_type(), std::false_type());
-  } else if (whole) {
-    pieces(std::false_type(), std::false_type());
-  } else {
-#pragma unroll
-    for (int h = 0; h < kPieces; ++h) {
-      turn_in(acc, h, turn, lane);
-#pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        const floatx4 x = turn_out(turn, i, lane);
-        if (r0 + h * 32 + i * 4 + (lane >> 4) < rows && c0 < cols) {
-          f32x4_a4* const at = reinterpret_cast<f32x4_a4*>(dst + (h * 32 + i * 4) * ld);
-          *at = accumulate ? x + *at : x;
-        }
-      }
-      __builtin_amdgcn_wave_barrier();
-    }
-  }
-}
-typedef uint32_t u32x2_a2 __attribute__((ext_vector_type(2), aligned(2)));     // dH has the alignment of its entries
-// What the sliced products leave behind: partial sums in blocks of 256 x 256 floats [slice][row tile][column tile].
-struct DhSlices {
-  int n;                // slices of the vocabulary (1: the tiles write dH themselves)
-  int voc_blks;         // vocabulary blocks of 256 per slice (the last slice may have fewer)
-  float* part;
-};
-// tile_m counts the chunk's live blocks of rows, of m_rows rows, nobody looks at those behind; orig_blk is the block's place in the chunk
-__device__ __forceinline__ void dh_tile(int tile_m, int m_rows, int orig_blk, int tile_n, int slice, const DhSlices& sl, int tiles_r, int tiles_d,
-                                        const uint16_t* __restrict__ dZ, int blk_pitch, int64_t Vp,
-                                        const uint16_t* __restrict__ W, int d, int V, uint16_t* __restrict__ dH,
-                                        const int32_t* __restrict__ rowsel, int64_t c0, int64_t rows,
-                                        const int32_t* __restrict__ ids, const float* __restrict__ g_c,
-                                        const float* __restrict__ sc, bool w_once, uint16_t* lds) {
-  using C = Cfg;
-  const int64_t m0 = static_cast<int64_t>(orig_blk) * C::BM;
-  const int n0 = tile_n * C::BN;
-  const int voc_blk = slice * sl.voc_blks, tiles_v = static_cast<int>(Vp >> 8);
-  const int k_len = min(sl.voc_blks, tiles_v - voc_blk) * 256;       // a multiple of 256, at least 256
-  const KContig ca = blocked_rows_tile<C>(dZ, blk_pitch, tiles_v, tile_m, voc_blk, m_rows);
-  KMajor kb;
-  kb.base = reinterpret_cast<const char*>(W + static_cast<int64_t>(voc_blk) * 256 * d + n0);
-  kb.ld_bytes = static_cast<int64_t>(d) * 2;
-  kb.hi_bytes = 0;
-  kb.k_rows = V - voc_blk * 256;                                     // dz is zero for vocabulary ids past V
-  kb.n_units = min(32, (d - n0) / 8);
-  floatx4 acc[C::MI][C::NI];
-  zero_acc<C>(acc);
-  // the third LDS stage goes to W: every group of row tiles streams all of it (twice the bytes of the [rows, V] operand).  With one
-  // row tile W is read once: past the caches where it is larger than they are, so that the operand, which every column tile
-  // reads, stays there (both products of 203 rows of 3584 762 -> 707 us, of 60 rows of 2048 449 -> 384; with up to four row tiles
-  // 725 rows that add to dW gain 1.7 %, 1000 rows lose 1 to 3).
-  // Up to half a tile of rows is multiplied by half of the wavefronts only, which halves the time of the matrix cores: every SIMD has one of either
-  // half.  (With the same loop for all numbers of rows 203 and 725 rows take 0.4 % longer.)
-  if (m_rows <= C::WTM && w_once) mfma_mainloop_mixed<C, false, true, 2, true, true>(ca, KMajor{}, KContig{}, kb, k_len, lds, acc, m_rows);
-  else if (m_rows <= C::WTM) mfma_mainloop_mixed<C, false, true, 2, false, true>(ca, KMajor{}, KContig{}, kb, k_len, lds, acc, m_rows);
-  else if (w_once) mfma_mainloop_mixed<C, false, true, 2, true>(ca, KMajor{}, KContig{}, kb, k_len, lds, acc);
-  else mfma_mainloop_mixed<C, false, true, 2>(ca, KMajor{}, KContig{}, kb, k_len, lds, acc);
-  if (sl.n > 1) {
-    float* out = sl.part + ((static_cast<int64_t>(slice) * tiles_r + tile_m) * tiles_d + tile_n) * (C::BM * C::BN);
-    store_acc_f32<C>(acc, reinterpret_cast<char*>(lds) + (tile_thread() >> 6) * kTurnBytes, out, C::BN, C::BM, C::BN, 0, false);
-    return;
-  }
-  // dH rows leave like the float32 ones: 32 rows at a time through LDS, 128 bytes of four rows to a store, the row numbers,
-  // factors and rows of W of a piece fetched together.  (One 2-byte entry after the other, each with its own chain of loads:
-  // both products of 39 000 rows of 2048 37.43 ms, like this 37.16, 12 000 rows 11.48 and 11.37.)
-  const int tid = tile_thread(), lane = tid & 63, wave = tid >> 6;
-  char* turn = reinterpret_cast<char*>(lds) + wave * kTurnBytes;
-  const int64_t r0 = m0 + wave / C::WN * C::WTM + (lane >> 4);
-  const int j = n0 + wave % C::WN * C::WTN + (lane & 15) * 4, jw = min(j, d - 4);   // d is a multiple of 8: four columns are all inside or all outside
-#pragma unroll
-  for (int h = 0; h < C::MI / 2; ++h) {
-    int64_t row[8];
-    float g[8], f[8];
-    uint2 w[8];
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      const int64_t n = c0 + min(r0 + h * 32 + i * 4, rows - 1);
-      row[i] = rowsel ? rowsel[n] : n;
-      g[i] = g_c[n];
-      f[i] = sc ? sc[n] : 1.f;
-    }
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {                                    // g = 0 for invalid ids
-      const int64_t id = g[i] != 0.f ? ids[row[i]] : 0;
-      w[i] = *reinterpret_cast<const uint2*>(W + id * d + jw);
-    }
-    turn_in(acc, h, turn, lane);
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      floatx4 v = turn_out(turn, i, lane);
-#pragma unroll
-      for (int k = 0; k < 4; ++k) {
-        v[k] = sc ? f[i] * v[k] : v[k];
-        const uint32_t wk = k < 2 ? w[i].x : w[i].y;
-        if (g[i] != 0.f) v[k] += g[i] * __uint_as_float(k & 1 ? wk & 0xffff0000u : wk << 16);
-      }
-      if (r0 + h * 32 + i * 4 < rows && j < d)
-        *reinterpret_cast<u32x2_a2*>(dH + row[i] * d + j) = u32x2_a2{pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3])};
-    }
-    __builtin_amdgcn_wave_barrier();
-  }
-}
-// Hs: the rows of H that go with the rows of dZ (scaled by the keeping pass), in column blocks [d / 256][mcp][256] so that a
-// tile's k-rows are one run of memory
-// k_len: rows of the packed [rows, V] operand, whole steps of 64 (0 when no block is live); rows: those that exist
-__device__ __forceinline__ void dw_tile(int tile_m, int tile_n, const uint16_t* __restrict__ dZ, int blk_pitch, int64_t mcp, int64_t Vp,
-                                        const uint16_t* __restrict__ Hs, int d, int V, int k_len, int rows, float* __restrict__ dW,
-                                        int accumulate, uint16_t* lds) {
-  using C = Cfg;
-  const int64_t m0 = static_cast<int64_t>(tile_m) * C::BM;
-  const int n0 = tile_n * C::BN;
-  KMajor ka;                                                         // blocked dZ: k = row of the chunk, entries = vocabulary
-  ka.base = reinterpret_cast<const char*>(dZ + blk_offset(0, tile_m, Vp >> 8) * blk_pitch);
-  ka.ld_bytes = 512;
-  ka.hi_bytes = (Vp >> 8) * kBlkElems * 2 * blk_pitch - 256 * 512;               // from the last row of a block to the block below
-  ka.k_rows = k_len;
-  ka.n_units = 32;
-  KMajor kb;                                                         // rows of H: k = row of the chunk, entries = hidden columns
-  kb.base = reinterpret_cast<const char*>(Hs + static_cast<int64_t>(tile_n) * mcp * 256);
-  kb.ld_bytes = 512;
-  kb.hi_bytes = 0;
-  kb.k_rows = rows;                                                  // dz is zero for rows past the chunk
-  kb.n_units = min(32, (d - n0) / 8);
-  floatx4 acc[C::MI][C::NI];
-  zero_acc<C>(acc);
-  if (k_len > 0) mfma_mainloop_mixed<C, true, true, 1>(KContig{}, ka, KContig{}, kb, k_len, lds, acc);
-  store_acc_f32<C>(acc, reinterpret_cast<char*>(lds) + (tile_thread() >> 6) * kTurnBytes, dW + m0 * d + n0, d, V - m0, d - n0, accumulate, past_caches(d, V));   // d is a multiple of 8
-}
-
-// dW of at most 256 rows.  A tile of 256 x 256 that a compute unit works on alone is products, then stores, and the next tile's first loads wait for these
-// stores (a wavefront's memory operations are counted in order): 203 rows of 3584 against 152 064 485 us, of which the products alone are 235 and the
-// stores of 2.2 GB 396 (5.5 TB/s, as much as a kernel that only stores such tiles reaches).  Here tiles of 256 x 128 have two workgroups to
-// a compute unit, so that one multiplies while the other stores, and a workgroup of its own each, which ends without waiting for its stores: 400
-// to 430 us.  K is walked in steps of 32 rows through three LDS stages of 24 KB, loaded two steps ahead, the fragments half a step ahead (read when they are
-// wanted: updates of 100 and 203 rows 1 % slower).  (Stored through the caches: 1075 us for
-// the update in place of 972.)
-using ShortCfg = TileCfg<256, 128, 2, 2>;
-constexpr int kShortA = 32 * 512, kShortStage = kShortA + 32 * 256, kShortLds = 3 * kShortStage;
-static_assert(2 * kShortLds <= 160 * 1024 && 3 * kTurnBytes <= kShortStage, "two workgroups to a compute unit; the turns of three wavefronts fit a stage");
-constexpr int kShortGM = 4, kShortGN = 16;               // tiles that the 64 workgroups of an XCD work on together
+// (the bodies and what bounds them: umas_gradients.h)
 __global__ void __launch_bounds__(ShortCfg::T, 2)
 k_dw_short(const uint16_t* __restrict__ dZ, int blk_pitch, int64_t Vp, int64_t mcp, const uint16_t* __restrict__ Hs, int d, int V, int tiles_v,
            int tiles_n, const LiveInfo* __restrict__ info, float* __restrict__ dW, int accumulate) {
-  using C = ShortCfg;
   __shared__ __attribute__((aligned(16))) char lds[kShortLds];
-  const int total = tiles_v * tiles_n, per = (total + 7) / 8, t = static_cast<int>(blockIdx.x & 7) * per + static_cast<int>(blockIdx.x >> 3);
-  if (static_cast<int>(blockIdx.x >> 3) >= per || t >= total) return;
-  int tile_m, tile_n;
-  tile_of_groups<kShortGM, kShortGN>(t, tiles_v, tiles_n, &tile_m, &tile_n);
-  const int k_rows = info->k_rows, nsub = (k_rows + 31) / 32;
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int wm = wave / C::WN, wn = wave % C::WN;
-  const char* const a0 = reinterpret_cast<const char*>(dZ + blk_offset(0, tile_m, Vp >> 8) * blk_pitch);
-  const int64_t blk_row = (Vp >> 8) * kBlkElems * 2 * blk_pitch;                                     // from a block of rows to the next
-  const char* const b0 = reinterpret_cast<const char*>(Hs + (static_cast<int64_t>(tile_n >> 1) * mcp) * 256 + (tile_n & 1) * 128);
-  // loads (K-major operands as in mfma_mainloop_mixed): one fills two k-rows of A, four of B
-  const int ka = 2 * wave + (lane >> 5), kb = 4 * wave + (lane >> 4);                                // + 8 p; + 16 p
-  const uint32_t ua = static_cast<uint32_t>((lane & 31) ^ (4 * (ka & 3))), ub = static_cast<uint32_t>((lane & 15) ^ (4 * (kb & 3)) ^ (2 * ((kb >> 3) & 1)));
-  auto load = [&](int sub) {
-    char* const st = lds + sub % 3 * kShortStage;
-    const int k0 = sub * 32;
-    const __amdgpu_buffer_rsrc_t ra = make_rsrc(a0 + (k0 >> 8) * blk_row + (k0 & 255) * 512), rb = make_rsrc(b0 + static_cast<int64_t>(k0) * 512);
-#pragma unroll
-    for (int p = 0; p < 4; ++p)
-      __builtin_amdgcn_raw_ptr_buffer_load_lds(ra, reinterpret_cast<uint32_t*>(st + (8 * p + 2 * wave) * 512), 16,
-                                               static_cast<uint32_t>(8 * p + ka) * 512u + (ua ^ (2u * (p & 1))) * 16u, 0, 0, kCached);
-#pragma unroll
-    for (int p = 0; p < 2; ++p)                            // dz is zero for rows that do not exist: the last one in their place
-      __builtin_amdgcn_raw_ptr_buffer_load_lds(rb, reinterpret_cast<uint32_t*>(st + kShortA + (16 * p + 4 * wave) * 256), 16,
-                                               static_cast<uint32_t>(min(16 * p + kb, k_rows - 1 - k0)) * 512u + ub * 16u, 0, 0, kCached);
-  };
-  // fragments through the transposing reads
-  const uint32_t lds0 = static_cast<uint32_t>(reinterpret_cast<uintptr_t>((__attribute__((address_space(3))) char*)(lds)));
-  const int tq = lane & 3, tj = (lane >> 2) & 3, tg = lane >> 4;
-  uint32_t tra[C::MI], trb[C::NI];
-#pragma unroll
-  for (int i = 0; i < C::MI; ++i)
-    tra[i] = lds0 + (tg * 8 + tj) * 512 + (tq & 1) * 8 + (((wm * (C::WTM / 8) + i * 2 + (tq >> 1)) ^ (4 * tj) ^ (2 * (tg & 1))) * 16);
-#pragma unroll
-  for (int j = 0; j < C::NI; ++j)
-    trb[j] = lds0 + kShortA + (tg * 8 + tj) * 256 + (tq & 1) * 8 + (((wn * (C::WTN / 8) + j * 2 + (tq >> 1)) ^ (4 * tj) ^ (2 * (tg & 1))) * 16);
-  typedef short short8v __attribute__((ext_vector_type(8)));
-  constexpr int HA = C::MI / 2;
-  bf16x8 af[2][HA], bfr[2][C::NI];
-  auto read = [&](uint32_t addr, auto row_c) {
-    short4v lo, hi;
-    asm volatile("ds_read_b64_tr_b16 %0, %1" : "=v"(lo) : "v"(addr));
-    asm volatile("ds_read_b64_tr_b16 %0, %1 offset:%2" : "=v"(hi) : "v"(addr), "n"(4 * decltype(row_c)::value));
-    const short8v v = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
-    return __builtin_bit_cast(bf16x8, v);
-  };
-  using RowA = std::integral_constant<int, 512>;
-  using RowB = std::integral_constant<int, 256>;
-  auto read_a = [&](int h, uint32_t st) {
-#pragma unroll
-    for (int i = 0; i < HA; ++i) af[h][i] = read(tra[h * HA + i] + st, RowA{});
-  };
-  auto read_b = [&](int buf, uint32_t st) {
-#pragma unroll
-    for (int j = 0; j < C::NI; ++j) bfr[buf][j] = read(trb[j] + st, RowB{});
-  };
-  auto wait_a = [&](int h) {
-#pragma unroll
-    for (int i = 0; i < HA; ++i) asm volatile("s_waitcnt lgkmcnt(0)" : "+v"(af[h][i]));
-  };
-  auto wait_b = [&](int buf) {
-#pragma unroll
-    for (int j = 0; j < C::NI; ++j) asm volatile("s_waitcnt lgkmcnt(0)" : "+v"(bfr[buf][j]));
-  };
-  floatx4 acc[C::MI][C::NI];
-  zero_acc<C>(acc);
-  auto mfmas = [&](int h, int buf) {
-#pragma unroll
-    for (int i = 0; i < HA; ++i)
-#pragma unroll
-      for (int jj = 0; jj < C::NI; ++jj) {
-        const int j = i & 1 ? C::NI - 1 - jj : jj;
-        acc[h * HA + i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(af[h][i], bfr[buf][j], acc[h * HA + i][j], 0, 0, 0);
-      }
-  };
-  auto stage = [&](int sub) { return static_cast<uint32_t>(sub % 3 * kShortStage); };
-  // One step: the second half of its A fragments is read under the products of the first, the next step's B and first half under those of the
-  // second.  The barrier in between: the next step's loads have landed, and everybody has read this step's stage, which is loaded again.
-  auto step = [&](int sub, auto buf_c) {
-    constexpr int buf = decltype(buf_c)::value;
-    wait_b(buf);
-    wait_a(0);
-    read_a(1, stage(sub));
-    mfmas(0, buf);
-    __builtin_amdgcn_sched_barrier(0);
-    wait_a(1);
-    if (sub + 1 < nsub) {
-      if (sub + 2 < nsub) __builtin_amdgcn_s_waitcnt(0x0F70 | 6); else __builtin_amdgcn_s_waitcnt(0x0F70);
-      __builtin_amdgcn_s_barrier();
-      __builtin_amdgcn_sched_barrier(0);
-      if (sub + 3 < nsub) load(sub + 3);
-      read_b(buf ^ 1, stage(sub + 1));
-      read_a(0, stage(sub + 1));
-    }
-    mfmas(1, buf);
-    __builtin_amdgcn_sched_barrier(0);
-  };
-  if (nsub > 0) {
-    load(0);
-    if (nsub > 1) load(1);
-    if (nsub > 2) load(2);
-    if (nsub > 2) __builtin_amdgcn_s_waitcnt(0x0F70 | 12); else if (nsub > 1) __builtin_amdgcn_s_waitcnt(0x0F70 | 6); else __builtin_amdgcn_s_waitcnt(0x0F70);
-    __builtin_amdgcn_s_barrier();
-    __builtin_amdgcn_sched_barrier(0);
-    read_b(0, 0);
-    read_a(0, 0);
-    for (int sub = 0; sub < nsub; sub += 2) {
-      step(sub, std::integral_constant<int, 0>());
-      if (sub + 1 < nsub) step(sub + 1, std::integral_constant<int, 1>());
-    }
-  }
-  // the turns lie in the two stages that nobody reads any more and no load is under way to
-  char* const turn = lds + (nsub + (wave == 3 ? 1 : 0)) % 3 * kShortStage + (wave == 3 ? 0 : wave) * kTurnBytes;
-  const int64_t m0 = static_cast<int64_t>(tile_m) * C::BM;
-  const int n0 = tile_n * C::BN;
-  store_acc_f32<C>(acc, turn, dW + m0 * d + n0, d, V - m0, d - n0, accumulate, past_caches(d, V));
+  dw_short<float>(dZ, blk_pitch, Vp, mcp, Hs, d, V, tiles_v, tiles_n, info, dW, accumulate, lds);
 }
-// Both products in one launch, in groups of 4 x 8 tiles that are worked on together on one XCD.  Every XCD owns a contiguous
-// range of the dH tiles (slice after slice, so that its workgroups share a slice of both operands) and behind it the share
-// of the dW tiles that evens out the sum (share_dw): dH tiles are long (K = vocabulary, or a slice of it) and few, on their
-// own they leave a fifth of the last round idle; they go first and the many short dW tiles fill up.  (Sliced dH tiles and
-// dW tiles taking turns instead: +-1 % at 725 rows, 8 % slower at 203.)
-// One workgroup per compute unit stays for the whole launch and takes the next place of its XCD's sequence whenever it is done
-// (the number of the next place is fetched a tile ahead): a workgroup per tile paid for its start at every tile, of which short
-// selections have many short ones, and workgroups without a tile (groups cut off by the edge, places kept free because
-// the shares are known on the device only) waited for a whole compute unit like the others.  A workgroup whose sequence is at
-// its end goes on with the one that has most left.  203 rows of 3584 1316 -> 845 us, 64 rows of 2048 841 -> 455, 725 rows
-// 1098 -> 930, 2000 rows of 3584 3.93 -> 3.52 ms, 39 000 rows of 2048 37.5 -> 36.5 ms.
 __global__ void __launch_bounds__(Cfg::T)
 k_gemm_dh_dw(const uint16_t* __restrict__ dZ, int blk_pitch, int64_t Vp, int64_t mcp, const uint16_t* __restrict__ W,
              const uint16_t* __restrict__ Hs, int d, int V, int tiles_v,
@@ -1590,88 +615,7 @@ k_gemm_dh_dw(const uint16_t* __restrict__ dZ, int blk_pitch, int64_t Vp, int64_t
              int64_t c0, int64_t rows, const int32_t* __restrict__ ids, const float* __restrict__ g_c,
              const float* __restrict__ sc) {
   __shared__ __attribute__((aligned(16))) uint16_t lds[MixedLdsBytes<Cfg>::value / 2];
-  const int n_live = info->n_live;                     // live blocks of rows: dH row tiles, dW K blocks
-  const int k_rows = info->k_rows, tiles_mn = n_live * tiles_d, tiles_dh = tiles_mn * sl.n;
-  // whose sequence of tiles the workgroup takes from, and the sequence: dH tiles, then dW tiles
-  int xcd = static_cast<int>(blockIdx.x & 7), first_dh, n_dh, first_dw, n_all;
-  auto sequence = [&]() {
-    first_dh = dh_first(tiles_dh, sl.n, xcd);
-    n_dh = dh_first(tiles_dh, sl.n, xcd + 1) - first_dh;
-    first_dw = info->dw.first[xcd];
-    n_all = n_dh + info->dw.first[xcd + 1] - first_dw;
-  };
-  sequence();
-  volatile int* const word = reinterpret_cast<volatile int*>(lds);   // wavefront 0's own at the end of a tile
-  int taken = threadIdx.x == 0 ? atomicAdd(&info->next[xcd], 1) : 0;
-  for (;;) {
-    if (threadIdx.x == 0) *word = taken;
-    __syncthreads();
-    int seq = __builtin_amdgcn_readfirstlane(*word);
-    __syncthreads();
-    while (seq >= n_all) {                               // the sequence is at its end: on with the one that has most left
-      if (threadIdx.x < kWave) {
-        const int x = threadIdx.x & 7;
-        const int length = dh_first(tiles_dh, sl.n, x + 1) - dh_first(tiles_dh, sl.n, x) + info->dw.first[x + 1] - info->dw.first[x];
-        const int left = length - __hip_atomic_load(&info->next[x], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-        int most = left;
-#pragma unroll
-        for (int o = 4; o > 0; o >>= 1) most = max(most, __shfl_xor(most, o, kWave));
-        if (most > 0) xcd = __ffsll(static_cast<long long>(__ballot(left == most))) - 1;
-        if (threadIdx.x == 0) {
-          word[0] = most > 0 ? atomicAdd(&info->next[xcd], 1) : -1;
-          word[1] = xcd;
-        }
-      }
-      __syncthreads();
-      seq = __builtin_amdgcn_readfirstlane(word[0]);
-      xcd = __builtin_amdgcn_readfirstlane(word[1]);
-      __syncthreads();
-      if (seq < 0) return;
-      sequence();
-    }
-    if (threadIdx.x == 0) taken = atomicAdd(&info->next[xcd], 1);
-    int tile_m, tile_n;
-    if (seq < n_dh) {
-      const int t = first_dh + seq, slice = t / tiles_mn;
-      tile_of_groups<kGM, kGN>(t - slice * tiles_mn, n_live, tiles_d, &tile_m, &tile_n);
-      dh_tile(tile_m, min(k_rows - tile_m * 256, 256), blk_orig[(c0 >> 8) + tile_m], tile_n, slice, sl, tiles_r, tiles_d, dZ, blk_pitch, Vp, W, d, V, dH, rowsel, c0, rows, ids, g_c, sc, n_live == 1 && beyond_cache(d, V, kDhOnceBytes), lds);
-    } else {
-      tile_of_groups<kGM, kGN>(first_dw + seq - n_dh, tiles_v, tiles_d, &tile_m, &tile_n);
-      dw_tile(tile_m, tile_n, dZ, blk_pitch, mcp, Vp, Hs, d, V, dw_k(k_rows), k_rows, dW, accumulate, lds);
-    }
-  }
-}
-
-// The slices' partial sums of dH added up in slice order, with what the tile epilogue does otherwise: row factor, one-hot
-// part, bf16 row through the selection.  One workgroup per (row of the live blocks, 1024 columns), four columns a thread.
-__device__ __forceinline__ void
-dh_reduce(int live_row, int piece, const DhSlices& sl, int tiles_r, int tiles_d, const uint16_t* __restrict__ W, int d, const LiveInfo* __restrict__ info,
-          const int32_t* __restrict__ blk_orig, uint16_t* __restrict__ dH, const int32_t* __restrict__ rowsel, int64_t c0,
-          int64_t rows, const int32_t* __restrict__ ids, const float* __restrict__ g_c, const float* __restrict__ sc) {
-  const int tile_m = live_row >> 8, r = live_row & 255;
-  if (tile_m >= info->n_live) return;
-  const int64_t m = static_cast<int64_t>(blk_orig[(c0 >> 8) + tile_m]) * 256 + r;
-  const int j = (piece * 256 + static_cast<int>(threadIdx.x)) * 4;
-  if (m >= rows || j >= d) return;
-  const float* src = sl.part + (static_cast<int64_t>(tile_m) * tiles_d + (j >> 8)) * 65536 + r * 256 + (j & 255);
-  const int64_t stride = static_cast<int64_t>(tiles_r) * tiles_d * 65536;
-  float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
-  for (int k0 = 0; k0 < sl.n; k0 += 8) {                             // eight slices in flight
-    float4 v[8];
-#pragma unroll
-    for (int q = 0; q < 8; ++q) v[q] = k0 + q < sl.n ? *reinterpret_cast<const float4*>(src + (k0 + q) * stride) : make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll
-    for (int q = 0; q < 8; ++q) { s.x += v[q].x; s.y += v[q].y; s.z += v[q].z; s.w += v[q].w; }
-  }
-  const int64_t row = rowsel ? rowsel[c0 + m] : c0 + m;
-  const float f = sc ? sc[c0 + m] : 1.f, g = g_c[c0 + m];
-  s.x *= f; s.y *= f; s.z *= f; s.w *= f;
-  if (g != 0.f) {                                                    // g = 0 for invalid ids
-    const uint2 w = *reinterpret_cast<const uint2*>(W + static_cast<int64_t>(ids[row]) * d + j);
-    s.x += g * __uint_as_float(w.x << 16); s.y += g * __uint_as_float(w.x & 0xffff0000u);
-    s.z += g * __uint_as_float(w.y << 16); s.w += g * __uint_as_float(w.y & 0xffff0000u);
-  }
-  *reinterpret_cast<u32x2_a2*>(dH + row * d + j) = u32x2_a2{pack_bf16x2(s.x, s.y), pack_bf16x2(s.z, s.w)};
+  gemm_dh_dw<true, float>(dZ, blk_pitch, Vp, mcp, W, Hs, d, V, tiles_v, tiles_d, sl, tiles_r, info, blk_orig, dH, dW, accumulate, rowsel, c0, rows, ids, g_c, sc, lds);
 }
 
 // One-hot part of dW: dW[y_n, :] += g_n h_n for every selected row, in float32.  Rows that took the same token add
@@ -1840,19 +784,11 @@ k_update_close(CloseArgs A) {
     return;
   }
   i -= A.n_stats;
-  dh_reduce(i % A.reduce_rows, i / A.reduce_rows, A.sl, A.tiles_r, A.tiles_d, A.W, A.d, A.info, A.blk_orig, A.dH, A.rowsel, A.c0, A.rows,
+  dh_reduce<true>(i % A.reduce_rows, i / A.reduce_rows, A.sl, A.tiles_r, A.tiles_d, A.W, A.d, A.info, A.blk_orig, A.dH, A.rowsel, A.c0, A.rows,
             A.ids, A.g_c, A.sc);
 }
 
 // ------------------------------------------------------------------ host side
-constexpr int64_t kF32ChunkRows = 4096;
-constexpr double kF32MaxWork = 137438953472.0;   // 2^37 multiply-adds per product
-// A chunk of more rows is no faster: 73 728 rows of 2048 in one chunk 108.6 ms, in two 105.8; 122 880 of 3584 in one 326 ms, in two
-// 320.7, in three 315; 163 840 in two 432, in three 427.
-constexpr int64_t kMaxChunkRows = 1 << 16;
-
-int64_t round_up(int64_t x, int64_t a) { return (x + a - 1) / a * a; }
-
 struct ScoreWs {
   float4* partial;   // [tiles_m][n_pad]
   float* logp_c;
@@ -1889,16 +825,6 @@ struct PpoWs {
   char* chunk;       // rest of the workspace: dZ (or E) [mcp, Vp], then the scaled copy of the chunk's rows of H
   size_t fixed_bytes;
 };
-// bytes one chunk of mc rows needs
-size_t chunk_bytes(int64_t mc, int d, int V, umas_dtype dt) {
-  if (dt == UMAS_F32) return align_up(static_cast<size_t>(mc) * V * sizeof(float));
-  const int64_t Vp = round_up(V, 256), mcp = round_up(mc, 256);
-  return align_up(static_cast<size_t>(mcp) * Vp * 2) + align_up(static_cast<size_t>(mcp) * round_up(d, 256) * 2);
-}
-// bytes one chunk of mc rows needs whose float32 logits are kept in place of the operand (entropy bonus)
-size_t logit_chunk_bytes(int64_t mc, int d, int V) {
-  return chunk_bytes(mc, d, V, UMAS_BF16) + static_cast<size_t>(round_up(mc, 256)) * round_up(V, 256) * 2;
-}
 // The float32 update keeps the logits (float64) of all its rows where that is no more than 1 GiB.  Storing and reading them costs the same
 // at every hidden size, a second product costs by it: below 64 columns up to 128 MiB, which the memory-side cache holds together with
 // dz, below 32 up to 32 MiB.  Update on new rows, computed twice / kept: 500 rows of 8 against 8000 (30 MiB) 179 / 180 us, 2000 (122) 278 /
@@ -1915,12 +841,6 @@ size_t f32_part_bytes(int64_t n_sel, int V) { return align_up(static_cast<size_t
 bool f32_few_launches(int64_t n_sel, int d, int V, size_t room) {
   const size_t z = n_sel <= kF32ChunkRows ? f32_logit_bytes(n_sel, d, V) : 0;
   return z > 0 && chunk_bytes(n_sel, d, V, UMAS_F32) + z + f32_part_bytes(n_sel, V) <= room;
-}
-// partial sums of as many slices as are wanted
-size_t full_part_bytes(int64_t n_sel, int64_t chunk_rows, int d, int V) {
-  if (!slices_dh(n_sel, chunk_rows, d)) return 0;
-  const int tiles_r = static_cast<int>(cdiv(chunk_rows, 256)), tiles_d = (d + 255) / 256;
-  return dh_part_bytes(plan_dh(tiles_r, tiles_d, (V + 255) / 256, SIZE_MAX), tiles_r, tiles_d);
 }
 // The update with an entropy bonus keeps the logits of a chunk in float32 instead of computing them a second time where the
 // workspace has room for chunks that are not small: the whole selection, or chunks whose dH tiles are whole ones (the same bits
@@ -1970,49 +890,11 @@ size_t carve_ppo(Carver& c, PpoWs& w, int64_t n_sel, int d, int V, umas_dtype dt
   return c.off;
 }
 
-umas_status check_model_args(const void* H, const void* W, umas_dtype dt, int64_t n_rows, int d, int V,
-                             const int32_t* ids, const int32_t* rowsel, int64_t n_sel) {
-  UMAS_REQUIRE(dt == UMAS_F32 || dt == UMAS_BF16, UMAS_EDTYPE, "dtype=%d is neither F32 nor BF16", static_cast<int>(dt));
-  UMAS_REQUIRE(n_rows >= 0 && n_sel >= 0, UMAS_EINVAL, "negative row count");
-  UMAS_REQUIRE(d >= 1 && V >= 1, UMAS_ESHAPE, "d=%d and V=%d must be positive", d, V);
-  UMAS_REQUIRE(dt != UMAS_BF16 || d % 8 == 0, UMAS_ESHAPE, "bf16 needs d %% 8 == 0 (d=%d)", d);
-  UMAS_REQUIRE(dt != UMAS_F32 || d <= 8192, UMAS_ESHAPE, "the float32 path supports d <= 8192 (d=%d)", d);
-  // the float32 path sums in float64: small shapes only
-  UMAS_REQUIRE(dt != UMAS_F32 || static_cast<double>(n_sel) * V * d <= kF32MaxWork, UMAS_ESHAPE,
-               "the float32 path is for small shapes: n_sel * V * d = %.3g exceeds %.3g; use bf16",
-               static_cast<double>(n_sel) * V * d, kF32MaxWork);
-  UMAS_REQUIRE(dt != UMAS_BF16 || static_cast<uint64_t>(n_rows) * d * 2 < (1ull << 32), UMAS_ESHAPE,
-               "bf16 H must be smaller than 4 GiB (32-bit buffer offsets): n_rows=%lld d=%d",
-               static_cast<long long>(n_rows), d);
-  UMAS_REQUIRE(dt != UMAS_BF16 || static_cast<uint64_t>(std::min(V, 256)) * d * 2 < (1ull << 32), UMAS_ESHAPE,
-               "256 rows of a bf16 W must be smaller than 4 GiB (32-bit buffer offsets): V=%d d=%d", V, d);
-  UMAS_REQUIRE(rowsel || n_sel == n_rows, UMAS_EINVAL, "rowsel is NULL but n_sel != n_rows");
-  UMAS_REQUIRE(n_sel <= n_rows, UMAS_EINVAL, "n_sel=%lld exceeds n_rows=%lld", static_cast<long long>(n_sel),
-               static_cast<long long>(n_rows));
-  UMAS_REQUIRE((H && ids) || n_rows == 0, UMAS_EINVAL, "H and ids must not be NULL");
-  UMAS_REQUIRE(W, UMAS_EINVAL, "W must not be NULL");
-  UMAS_REQUIRE(reinterpret_cast<uintptr_t>(H) % 16 == 0 && reinterpret_cast<uintptr_t>(W) % 16 == 0, UMAS_EINVAL,
-               "H and W must be 16-byte aligned");
-  return UMAS_OK;
-}
-
-umas_status check_ws(void* ws, size_t have, size_t need) {
-  UMAS_REQUIRE(ws && reinterpret_cast<uintptr_t>(ws) % kAlign == 0 && have >= need, UMAS_EWORKSPACE,
-               "workspace must be 256-byte aligned and hold %zu bytes (got %zu)", need, have);
-  return UMAS_OK;
-}
-
 // Four workgroups per compute unit, at most one wavefront per row: 203 rows of 3584 145 -> 29 us, 725 rows of 2048 88 ->
 // 25 us, 39 000 rows (307 groups, three workgroups each) 203 -> 195 us; twice and four times as many are no faster.
 dim3 onehot_grid(int64_t n_sel) {
   const unsigned groups = cdiv(n_sel, kOneHotRows);
   return dim3(groups, std::min(std::max(1024 / groups, 1u), static_cast<unsigned>(kOneHotRows / 4)));
-}
-int device_cus() {
-  int dev = 0, n_cu = 0;
-  if (hipGetDevice(&dev) != hipSuccess || hipDeviceGetAttribute(&n_cu, hipDeviceAttributeMultiprocessorCount, dev) != hipSuccess || n_cu < 1)
-    n_cu = 64;
-  return n_cu;
 }
 template <int PPW, class... Args>
 void launch_score_few_ppw(int ni, unsigned grid, hipStream_t st, Args... args) {
@@ -2040,27 +922,6 @@ template <class... Args>
 void launch_finalize(int64_t rows, int64_t n_sel, hipStream_t st, Args... args) {
   if (n_sel < kFinSplitRows) hipLaunchKernelGGL(k_score_finalize<true>, dim3(cdiv(rows, 8)), dim3(256), 0, st, args...);
   else hipLaunchKernelGGL(k_score_finalize<false>, dim3(cdiv(rows, 32)), dim3(256), 0, st, args...);
-}
-
-// Row tiles that the logit kernels work through together (see tile_coords): an XCD reads all rows of H once for every four
-// vocabulary tiles, all XCDs at about the same time, so a panel that stays in the memory-side cache (256 MB) comes from HBM once
-// instead of nineteen times.  40 960 rows of 3584 (293 MB), score: all rows 33.4 ms, panels of at most 40 / 64 / 96 / 128 / 160
-// MiB 31.5 / 30.6 / 30.7 / 30.5 / 30.7; 24 576 rows kept 20.6 -> 19.3 ms; 40 960 rows of 2048 (168 MB) 18.2 either way.
-constexpr int64_t kPanelBytes = int64_t{128} << 20;
-int row_panel(int tiles_n, int d) {
-  const int most = std::max(static_cast<int>(kPanelBytes / (static_cast<int64_t>(Cfg::BN) * d * 2)) / kGN * kGN, kGN);
-  const int panels = (tiles_n + most - 1) / most;
-  return ((tiles_n + panels - 1) / panels + kGN - 1) / kGN * kGN;
-}
-
-// Tiles of every XCD that are cut in two (see score_tiles): those of the last round of compute units where it is at most half full.
-int halved_tiles(int tiles_m, int tiles_n) {
-  if (tiles_n > kGN) return 0;
-  const int per_xcd = static_cast<int>(cdiv(static_cast<size_t>(tiles_m) * tiles_n, 8)), cus = std::max(device_cus() / 8, 1), rest = per_xcd % cus;
-  return rest * 2 <= cus ? rest : 0;
-}
-dim3 score_grid(int tiles_m, int tiles_n, int panel, int halved) {
-  return dim3(tile_grid<kGM, kGN>(tiles_m, tiles_n, panel, kTilesPerWg) + 8 * static_cast<unsigned>(halved));
 }
 
 // Forward scoring of the selected rows into compact arrays and/or scattered outputs.  float32: `room` holds statistics of
