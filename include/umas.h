@@ -413,6 +413,82 @@ umas_status umas_ready_batch_packed(const umas_streams* streams, int32_t n_model
                                     int64_t* mb_off, int32_t* n_parts, void* workspace, size_t workspace_bytes,
                                     void* hip_stream);
 
+/* ---------------------------------------------------------------------------------------------
+ * Teaching a head from targets: what a worker group does to a model before and beside the policy update (a supervised
+ * warm start, an auxiliary supervised term, one role's model taught by another's).  H, W, rowsel, n_sel, dtype and their
+ * limits are those of umas_policy_logprobs; logits are never written out as such.
+ *
+ * Cross entropy of given tokens and its gradient:
+ *   z = W h_i, lse_i = log sum_v exp z_v;  l_i = lse_i - z_{ids[i]} + z_coef lse_i^2;  loss = sum_i w_i l_i / norm
+ *   g_i = w_i / norm;  dz_iv = g_i ((1 + 2 z_coef lse_i) softmax(z_i)_v - 1[v = ids[i]]);  dH = dz W;  dW = dz^T H
+ * with norm = norm_rows, or n_sel where that is 0 (rows without a target count in it: the token mean over the selection).
+ *   ids        DEVICE int32 [n_rows]; a row whose id is outside [0,V) (-100, say) is ignored: it adds nothing to any sum
+ *              but the count of ignored rows and has no gradient, whatever its row of H holds
+ *   weight     DEVICE float [n_rows] or NULL (= 1); a weight of 0 takes a row out of loss and gradients the same way
+ *   tok_role   DEVICE int32 [n_rows] or NULL with n_roles = 0
+ *   z_coef     >= 0, the penalty that keeps logsumexps near 0
+ *   stats      DEVICE umas_target_stats [1 + n_roles]
+ *   logp       DEVICE float [n_rows] or NULL: log-prob of the row's token, 0 on rows that are not selected or ignored
+ *   dH         DEVICE [n_rows, d] in the dtype of H; rows not selected or ignored are set to 0
+ *   dW         DEVICE [V, d] of the type dW_type: UMAS_F32, or for a bf16 head UMAS_BF16 (16-byte aligned; float32 sums
+ *              rounded once).  accumulate_dW = 0 overwrites, 1 adds: to float32 exactly as the policy update does, to bf16
+ *              with a rounding per call.  UMAS_NO_DW with dW = NULL: the head is frozen, the product is left out.
+ * The bf16 call keeps one bf16 number per (row, vocabulary entry) of a chunk of rows in its workspace, as the policy update
+ * does (softmax numerators, not logits), and runs in as few chunks as the workspace allows: of 256 rows in the smallest size, of up
+ * to 65536 in the full one.  A dW of bf16 that comes from several chunks is summed in float32 in the workspace. */
+typedef struct umas_target_stats {
+  float loss;              /* row 0: sum of w_i l_i over norm; roles: over the role's rows */
+  float weight_mean;       /* of the selected rows, 0 for ignored ones */
+  float entropy_mean;      /* of the head, over the rows that are not ignored */
+  float lse_mean;          /* ... its logsumexp */
+  int64_t n_scored;        /* selected rows */
+  int64_t n_ignored;       /* ... that have no target */
+} umas_target_stats;
+enum { UMAS_NO_DW = -1 };
+enum { UMAS_MAX_TOP = 64 };
+size_t umas_cross_entropy_workspace_bytes_min(int64_t n_sel, int32_t d, int32_t V, umas_dtype dtype, int32_t dW_type);
+size_t umas_cross_entropy_workspace_bytes(int64_t n_sel, int32_t d, int32_t V, umas_dtype dtype, int32_t dW_type);
+umas_status umas_cross_entropy_fwd_bwd(const void* H, const void* W, umas_dtype dtype, int64_t n_rows, int32_t d, int32_t V,
+                                       const int32_t* ids, const int32_t* rowsel, int64_t n_sel, const float* weight,
+                                       const int32_t* tok_role, int32_t n_roles, float z_coef, int32_t accumulate_dW,
+                                       int64_t norm_rows, umas_target_stats* stats, float* logp, void* dH, void* dW,
+                                       int32_t dW_type, void* workspace, size_t workspace_bytes, void* hip_stream);
+
+/* The k largest logits of a head: what a teacher hands to umas_distill_fwd_bwd, and the candidates of a next token.  For each
+ * selected row, z = W h_i (float accumulate):
+ *   top_ids     DEVICE int32 [n_rows, k]: tokens in falling order of their logits, equal logits in rising order of tokens
+ *   top_logits  DEVICE float [n_rows, k]: their logits
+ *   lse         DEVICE float [n_rows]: log sum_v exp z_v over the whole vocabulary
+ * 1 <= k <= UMAS_MAX_TOP.  Logits of -infinity and those that are not a number are not listed; places left over (they, or
+ * V < k) hold token -1 and logit -infinity.  Rows that are not selected get tokens of -1, logits and logsumexp of 0.  H, W,
+ * rowsel, n_sel, dtype and their limits as in umas_policy_logprobs.  The workspace bounds what is kept of the logits on the way;
+ * the results do not depend on it. */
+size_t umas_top_logits_workspace_bytes_min(int64_t n_sel, int32_t d, int32_t V, int32_t k, umas_dtype dtype);
+size_t umas_top_logits_workspace_bytes(int64_t n_sel, int32_t d, int32_t V, int32_t k, umas_dtype dtype);
+umas_status umas_top_logits(const void* H, const void* W, umas_dtype dtype, int64_t n_rows, int32_t d, int32_t V,
+                            const int32_t* rowsel, int64_t n_sel, int32_t k, int32_t* top_ids, float* top_logits, float* lse,
+                            void* workspace, size_t workspace_bytes, void* hip_stream);
+
+/* Distillation from a teacher's k largest logits and its gradient.  The teacher's distribution over its k places, t_j:
+ * with teacher_lse = NULL the softmax of the k logits; else exp(top_logits_j - teacher_lse_i), the teacher's own
+ * probabilities, what it gives to other tokens teaching nothing (T_i = sum_j t_j <= 1):
+ *   kl_i = sum_j t_j (log t_j - log softmax(z_i)_{v_j});  loss = sum_i w_i kl_i / norm
+ *   dz_iv = g_i (T_i softmax(z_i)_v - sum_{j: v_j = v} t_j)
+ *   top_ids     DEVICE int32 [n_rows, k], 1 <= k <= UMAS_MAX_TOP, as umas_top_logits writes them or any others; places whose token is
+ *               outside [0,V), whose logit is -infinity or not a number do not count; a row without any is ignored.  A token
+ *               in several places counts with all of them.
+ *   top_logits  DEVICE float [n_rows, k]
+ *   teacher_lse DEVICE float [n_rows] or NULL
+ *   kl          DEVICE float [n_rows] or NULL, 0 on rows that are not selected or ignored
+ * The rest as in umas_cross_entropy_fwd_bwd. */
+size_t umas_distill_workspace_bytes_min(int64_t n_sel, int32_t d, int32_t V, int32_t k, umas_dtype dtype, int32_t dW_type);
+size_t umas_distill_workspace_bytes(int64_t n_sel, int32_t d, int32_t V, int32_t k, umas_dtype dtype, int32_t dW_type);
+umas_status umas_distill_fwd_bwd(const void* H, const void* W, umas_dtype dtype, int64_t n_rows, int32_t d, int32_t V,
+                                 const int32_t* top_ids, const float* top_logits, int32_t k, const float* teacher_lse,
+                                 const int32_t* rowsel, int64_t n_sel, const float* weight, const int32_t* tok_role,
+                                 int32_t n_roles, int32_t accumulate_dW, int64_t norm_rows, umas_target_stats* stats, float* kl,
+                                 void* dH, void* dW, int32_t dW_type, void* workspace, size_t workspace_bytes, void* hip_stream);
+
 /* Kernel timing aid for benchmarks (not part of the method).  While enabled, every kernel launch
  * of the library is followed by a HIP event on its stream and the time between consecutive events
  * of one call is booked to the kernel launched in between.  umas_profile_enable(on) discards earlier

@@ -600,3 +600,93 @@ def ready_batch_packed(streams, traj_turn_off, traj_keep, traj_order, max_rows):
         off[m, :] = len(out)
         off[m, :len(starts)] = starts
     return np.array(out, dtype=np.int32), off, n_parts
+
+
+# --------------------------------------------------------------------------------------
+# Teaching a head from targets: largest logits, cross entropy, distillation.  Written from the definitions; sums in float64.
+# --------------------------------------------------------------------------------------
+def top_logits(H, W, k, rowsel=None):
+    """Tokens of the k largest logits of every selected row, falling, equal ones in rising order of tokens, their logits and the row's logsumexp.
+    Logits that are -infinity or no number are not listed: token -1, logit -infinity.  Other rows: -1, 0, 0."""
+    n = H.shape[0]
+    rows = np.arange(n) if rowsel is None else np.asarray(rowsel, dtype=np.int64)
+    W64 = np.asarray(W, dtype=np.float64)
+    ids, top, lse = np.full((n, k), -1, np.int64), np.zeros((n, k)), np.zeros(n)
+    for i in rows:
+        z = W64 @ np.asarray(H[i], dtype=np.float64)
+        m = z.max()
+        lse[i] = m + np.log(np.exp(z - m).sum())
+        listed = [v for v in sorted(range(len(z)), key=lambda v: (-z[v], v)) if z[v] > -np.inf][:k]
+        ids[i, :len(listed)] = listed
+        top[i] = -np.inf
+        top[i, :len(listed)] = z[listed]
+    return ids, top, lse
+
+
+def teacher_masses(top_ids, top_logits_, teacher_lse, V):
+    """What every place of a row teaches: softmax of the places that count, or with the teacher's logsumexp its own probabilities; 0 for a place whose
+    token does not exist or whose logit is -infinity or no number."""
+    t = np.zeros(np.shape(top_ids))
+    for i in range(len(t)):
+        have = [j for j in range(t.shape[1]) if 0 <= top_ids[i, j] < V and top_logits_[i, j] > -np.inf]
+        if not have:
+            continue
+        l = np.asarray(top_logits_[i, have], np.float64)
+        if teacher_lse is None:
+            e = np.exp(l - l.max())
+            t[i, have] = e / e.sum()
+        else:
+            t[i, have] = np.exp(l - np.float64(teacher_lse[i]))
+    return t
+
+
+def teach(H, W, ids, masses, rowsel=None, weight=None, z_coef=0.0, norm_rows=0, entropy_part=True):
+    """Weighted mean over the selected rows (or over norm_rows) of sum_j t_j ([log t_j] - log p_{ids_j}) + z_coef lse^2, the bracket with entropy_part
+    (distillation) only, and its gradient.  A row without mass or of weight 0 adds nothing and has no gradient.
+    Returns a dict: loss; row (without the weight and the penalty); dz [len(rows), V], dH [n, d], dW [V, d]; w, mass, lse, entropy of the rows."""
+    n, d = H.shape
+    V = W.shape[0]
+    rows = np.arange(n) if rowsel is None else np.asarray(rowsel, dtype=np.int64)
+    W64 = np.asarray(W, dtype=np.float64)
+    norm = norm_rows if norm_rows else max(len(rows), 1)
+    row, dz, dH = np.zeros(n), np.zeros((len(rows), V)), np.zeros((n, d))
+    dW = np.zeros((V, d))
+    w_used, mass, lses, ents, loss = np.zeros(len(rows)), np.zeros(len(rows)), np.zeros(len(rows)), np.zeros(len(rows)), 0.0
+    for q, i in enumerate(rows):
+        t = np.asarray(masses[i], np.float64)
+        mass[q] = t.sum()
+        if not mass[q] > 0:
+            continue
+        z = W64 @ np.asarray(H[i], dtype=np.float64)
+        m = z.max()
+        lse = m + np.log(np.exp(z - m).sum())
+        lp = z - lse
+        p = np.exp(lp)
+        w_used[q] = 1.0 if weight is None else weight[i]
+        lses[q], ents[q] = lse, -(p * lp).sum()
+        have = t > 0
+        v = np.asarray(ids[i])[have]
+        row[i] = (t[have] * ((np.log(t[have]) if entropy_part else 0.0) - lp[v])).sum()
+        if w_used[q] == 0:
+            continue
+        g = w_used[q] / norm
+        loss += g * (row[i] + z_coef * lse * lse)
+        dz[q] = g * (mass[q] + 2 * z_coef * lse) * p
+        np.subtract.at(dz[q], v, g * t[have])
+        dH[i] = dz[q] @ W64
+        dW += np.outer(dz[q], np.asarray(H[i], np.float64))
+    return dict(loss=loss, row=row, dz=dz, dH=dH, dW=dW, w=w_used, mass=mass, lse=lses, entropy=ents, rows=rows)
+
+
+def cross_entropy(H, W, ids, rowsel=None, weight=None, z_coef=0.0, norm_rows=0):
+    """teach with one target of mass 1 a row; ids outside [0, V) are ignored.  row is the token's log-prob."""
+    ids = np.asarray(ids)
+    ok = (ids >= 0) & (ids < W.shape[0])
+    r = teach(H, W, np.where(ok, ids, 0)[:, None], ok[:, None].astype(np.float64), rowsel, weight, z_coef, norm_rows, entropy_part=False)
+    r["row"] = -r["row"]
+    return r
+
+
+def distill(H, W, top_ids, top_logits_, teacher_lse=None, rowsel=None, weight=None, norm_rows=0):
+    """teach with the teacher's masses; row is the divergence."""
+    return teach(H, W, top_ids, teacher_masses(top_ids, top_logits_, teacher_lse, W.shape[0]), rowsel, weight, 0.0, norm_rows)

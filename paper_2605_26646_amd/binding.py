@@ -136,6 +136,24 @@ def load_library():
     lib.umas_policy_logprobs_static.argtypes = [C.c_void_p, C.c_void_p, C.c_int, C.c_int64, C.c_int32, C.c_int32,
                                                 C.c_void_p, C.c_void_p, C.c_int64, C.c_void_p, C.c_void_p, C.c_void_p,
                                                 C.c_void_p]
+    for name, places in (("cross_entropy", []), ("distill", [C.c_int32])):
+        for which in ("_min", ""):
+            f = getattr(lib, f"umas_{name}_workspace_bytes{which}")
+            f.restype, f.argtypes = C.c_size_t, [C.c_int64, C.c_int32, C.c_int32, *places, C.c_int, C.c_int32]
+    lib.umas_cross_entropy_fwd_bwd.restype = C.c_int
+    lib.umas_cross_entropy_fwd_bwd.argtypes = [C.c_void_p, C.c_void_p, C.c_int, C.c_int64, C.c_int32, C.c_int32, C.c_void_p, C.c_void_p, C.c_int64,
+                                               C.c_void_p, C.c_void_p, C.c_int32, C.c_float, C.c_int32, C.c_int64, C.c_void_p, C.c_void_p, C.c_void_p,
+                                               C.c_void_p, C.c_int32, C.c_void_p, C.c_size_t, C.c_void_p]
+    lib.umas_distill_fwd_bwd.restype = C.c_int
+    lib.umas_distill_fwd_bwd.argtypes = [C.c_void_p, C.c_void_p, C.c_int, C.c_int64, C.c_int32, C.c_int32, C.c_void_p, C.c_void_p, C.c_int32, C.c_void_p,
+                                         C.c_void_p, C.c_int64, C.c_void_p, C.c_void_p, C.c_int32, C.c_int32, C.c_int64, C.c_void_p, C.c_void_p,
+                                         C.c_void_p, C.c_void_p, C.c_int32, C.c_void_p, C.c_size_t, C.c_void_p]
+    for which in ("_min", ""):
+        f = getattr(lib, f"umas_top_logits_workspace_bytes{which}")
+        f.restype, f.argtypes = C.c_size_t, [C.c_int64, C.c_int32, C.c_int32, C.c_int32, C.c_int]
+    lib.umas_top_logits.restype = C.c_int
+    lib.umas_top_logits.argtypes = [C.c_void_p, C.c_void_p, C.c_int, C.c_int64, C.c_int32, C.c_int32, C.c_void_p, C.c_int64, C.c_int32, C.c_void_p,
+                                    C.c_void_p, C.c_void_p, C.c_void_p, C.c_size_t, C.c_void_p]
     lib.umas_values.restype = C.c_int
     lib.umas_values.argtypes = [C.c_void_p, C.c_void_p, C.c_float, C.c_int, C.c_int64, C.c_int32, C.c_void_p, C.c_int64,
                                 C.c_void_p, C.c_void_p]
@@ -264,6 +282,41 @@ def umas_ppo_loss_fwd_bwd(H, W, ids, rowsel, logp_old, adv, tok_role, n_roles, c
     _check_rows(rowsel, H)
     return _done(_native().ppo_loss(H, W, ids, rowsel, logp_old, adv, tok_role, n_roles, clip_eps, entropy_coef, dual_clip, accumulate_dW,
                                     norm_rows, logp_ref, kl_coef, dW, dH, logp_new, stats, workspace, _stream()))
+
+
+TARGET_STATS_DTYPE = np.dtype([("loss", "<f4"), ("weight_mean", "<f4"), ("entropy_mean", "<f4"), ("lse_mean", "<f4"),
+                               ("n_scored", "<i8"), ("n_ignored", "<i8")])
+MAX_TOP = 64
+
+
+def umas_top_logits(H, W, k, rowsel=None, *, ids=None, logits=None, lse=None, workspace=None):
+    """The k largest logits of every selected row: (ids int32 [n, k], logits float32 [n, k], lse float32 [n]), falling, equal
+    logits in rising order of tokens; rows that are not selected get -1, 0 and 0."""
+    _check_rows(rowsel, H)
+    return _done(_native().top_logits(H, W, k, rowsel, ids, logits, lse, workspace, _stream()))
+
+
+def umas_cross_entropy_fwd_bwd(H, W, ids, rowsel=None, weight=None, tok_role=None, n_roles=0, *, z_coef=0.0, train_head=True,
+                               accumulate_dW=False, norm_rows=0, dW=None, dH=None, logp=None, stats=None, workspace=None):
+    """Returns (stats, log-prob of every row's token, dH, dW).  dW has the type of W unless one of float32 is passed; train_head=False
+    leaves it out (None)."""
+    _check_rows(rowsel, H)
+    return _done(_native().cross_entropy(H, W, ids, rowsel, z_coef, weight, tok_role, n_roles, train_head, accumulate_dW, norm_rows, dW, dH, logp,
+                                         stats, workspace, _stream()))
+
+
+def umas_distill_fwd_bwd(H, W, top_ids, top_logits, teacher_lse=None, rowsel=None, weight=None, tok_role=None, n_roles=0, *, train_head=True,
+                         accumulate_dW=False, norm_rows=0, dW=None, dH=None, kl=None, stats=None, workspace=None):
+    """Returns (stats, divergence of every row, dH, dW); top_ids, top_logits [n, k] and teacher_lse [n] as umas_top_logits leaves them for
+    the teacher's hidden states and head, teacher_lse=None renormalises over the k places."""
+    _check_rows(rowsel, H)
+    return _done(_native().distill(H, W, top_ids, top_logits, teacher_lse, rowsel, weight, tok_role, n_roles, train_head, accumulate_dW, norm_rows, dW,
+                                   dH, kl, stats, workspace, _stream()))
+
+
+def read_target_stats(stats: torch.Tensor) -> np.ndarray:
+    """Copy the device umas_target_stats array to a numpy structured array (synchronises)."""
+    return stats.cpu().numpy().view(TARGET_STATS_DTYPE)
 
 
 VALUE_STATS_DTYPE = np.dtype([("loss", "<f4"), ("clip_frac", "<f4"), ("value_mean", "<f4"), ("reserved", "<f4"),

@@ -17,6 +17,7 @@
 #include "umas_surrogate.h"
 
 namespace umas {
+namespace {
 namespace f32 {
 
 typedef double double4v __attribute__((ext_vector_type(4)));
@@ -134,6 +135,7 @@ struct ScoreOut {
   double* rest_c;                            // compact arrays (NULL: none): sum of the probabilities of the tokens not taken
   float *logp_c, *lse_c, *ent_c;
   float *logp, *lse, *entropy;               // scattered (NULL: none)
+  double* lse64_c = nullptr;                 // compact, not rounded
 };
 struct Scores {
   bool ok;                                   // the token id exists
@@ -152,11 +154,13 @@ __device__ __forceinline__ void write_scores(const Stat& a, int64_t n, int64_t r
     o.logp_c[n] = s.lp; o.lse_c[n] = s.lse; o.ent_c[n] = s.en;
     o.rest_c[n] = s.rest;
   }
+  if (o.lse64_c) o.lse64_c[n] = a.m + log(a.s);
   if (o.logp) o.logp[row] = s.lp;
   if (o.lse) o.lse[row] = s.lse;
   if (o.entropy) o.entropy[row] = s.en;
 }
 
+// (ids may be NULL where nobody asks for the taken token's log-prob: token 0 stands for it.)
 // A workgroup takes 32 rows and every splits-th block of 128 vocabulary entries, 32 to a wavefront; a lane holds 8
 // entries of each of two rows.  With NB = 1 it is half as many of both: four times as many workgroups, a quarter as many products in each,
 // for updates that are few tiles altogether (see update).  Without `part` (one workgroup per row block) the scores are final, else the statistics go to
@@ -184,7 +188,7 @@ k_score_f32(const float* __restrict__ W, const float* __restrict__ H, int d, int
   for (int j = 0; j < NB; ++j) {
     const int64_t n = min(n0 + blk_index(j), n_sel - 1), row = rowsel ? rowsel[n] : n;
     h.p[j] = H + row * d;
-    y[j] = ids[row];
+    y[j] = ids ? ids[row] : 0;
   }
   Stat st[NB];
 #pragma unroll
@@ -241,7 +245,7 @@ k_score_f32(const float* __restrict__ W, const float* __restrict__ H, int d, int
     return;
   }
   const int64_t row = rowsel ? rowsel[n] : n;
-  write_scores(a, n, row, ids[row], V, out);
+  write_scores(a, n, row, ids ? ids[row] : 0, V, out);
 }
 // One workgroup per row, every thread walks the vocabulary entries tid, tid + 256, ...: one launch and no room needed.
 template <bool KEEP_Z>
@@ -253,7 +257,7 @@ k_score_f32_row(const float* __restrict__ W, const float* __restrict__ H, int d,
   const int64_t n = blockIdx.x, row = rowsel ? rowsel[n] : n;
   for (int k = threadIdx.x; k < d; k += 256) s_h[k] = H[row * d + k];
   __syncthreads();
-  const int y = ids[row];
+  const int y = ids ? ids[row] : 0;
   Stat a = empty_stat();
   for (int v = threadIdx.x; v < V; v += 256) {
     const float* w = W + static_cast<int64_t>(v) * d;
@@ -283,7 +287,7 @@ k_score_f32_merge(const Stat* __restrict__ part, int splits, int V, const int32_
   for (int o = 1; o < kWave; o <<= 1) a = merge(a, shfl_xor(a, o));
   if (lane != 0) return;
   const int64_t row = rowsel ? rowsel[n] : n;
-  write_scores(a, n, row, ids[row], V, out);
+  write_scores(a, n, row, ids ? ids[row] : 0, V, out);
 }
 
 // ------------------------------------------------------------------ backward
@@ -432,6 +436,7 @@ struct GradArgs {
   int rows, accumulate;
   float *dH, *dW;
   int n_dh, n_dw, dw_first;                  // tiles; the longer ones go first
+  const float* h_rows = nullptr;             // the rows of H that dW reads, of the chunk, next to each other (NULL: H through the selection)
 };
 // The statistics of the rows, in the gradients' launch: a workgroup for the model and one for each role.
 struct StatArgs {
@@ -486,11 +491,11 @@ __device__ __forceinline__ void dw_tile(const GradArgs& A, int tile, double* s_a
   a.ld = A.V;
   a.map = nullptr;
   b.ld = A.d;
-  b.map = A.rowsel ? A.rowsel + A.c0 : nullptr;
+  b.map = A.rowsel && !A.h_rows ? A.rowsel + A.c0 : nullptr;
 #pragma unroll
   for (int i = 0; i < T::NB; ++i) {
     a.p[i] = A.dz + min(v0 + blk_index(i), A.V - 1);
-    b.p[i] = (A.rowsel ? A.H : A.H + A.c0 * A.d) + min(j0 + blk_index(i), A.d - 1);
+    b.p[i] = (A.h_rows ? A.h_rows : A.rowsel ? A.H : A.H + A.c0 * A.d) + min(j0 + blk_index(i), A.d - 1);
   }
   gradient_tile<SIZE>(a, b, A.rows, s_acc, [&](int r, int c, double x) {
     const int v = v0 + r, j = j0 + c;
@@ -612,6 +617,7 @@ inline void launch_gradients(GradArgs A, const StatArgs& T, hipStream_t st) {
       default: return go(k_gradients_f32<2, 2>);
     }
   };
+  if (!A.dW) return launch(n_dh, 0, T);      // a frozen head
   const int64_t n_w = static_cast<int64_t>(A.V) * A.d;
   if (A.dW + n_w <= A.W || A.W + n_w <= A.dW) return launch(n_dh, n_dw, T);
   launch(n_dh, 0, StatArgs{});               // dW lies over the weights, which dH has to have read by then
@@ -665,4 +671,5 @@ inline umas_status update(const UpdateArgs& A, hipStream_t st) {
 }
 
 }  // namespace f32
+}  // namespace
 }  // namespace umas

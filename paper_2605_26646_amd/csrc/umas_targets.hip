@@ -1,0 +1,920 @@
+// Teaching a head from targets: softmax cross entropy of given tokens and distillation from a teacher's largest logits, each with its gradient to hidden
+// states and head.
+//
+// Both are one computation with k targets a row (cross entropy: one, of mass 1).  For a selected row i with z = W h_i, lse = log sum_v exp z_v, targets
+// (v_j, t_j) of mass T = sum t_j and weight w_i, over norm rows:
+//   cross entropy  l_i = lse - z_y + c lse^2          distillation  l_i = sum_j t_j (log t_j - z_{v_j} + lse)
+//   loss = sum_i w_i l_i / norm,  g = w_i / norm,  dz_v = g (a' p_v - t_v),  p = softmax(z),  a' = T + 2 c lse,  dH = dz W,  dW = dz^T H
+// The dense part of dz is a row factor times the softmax, so one product of logits serves both directions, as in the policy update: the scoring pass
+// leaves E = bf16(exp(z - r_i)) behind, r_i the largest logit among the row's targets, which a gather of k dot products finds beforehand and which is
+// never far above the row's logsumexp.  What is left is f = g a' exp(r - lse) as a row factor (folded into dH's rows and into the copy of H that dW reads)
+// and k entries a row, which are written over their numerators before the gradient products:
+//   E[i, v_j] = bf16((a' p - t) / (a' exp(r - lse))) = bf16(exp(lse - r) (p - t / a'))
+// so the sparse part costs k two-byte stores a row and no pass of its own over dH or dW.
+#include "umas_f32.h"
+#include "umas_gradients.h"
+
+namespace umas {
+namespace {
+
+// What a row is taught.
+struct Targets {
+  const int32_t* ids;      // [n_rows][k]; a place whose token does not exist does not count
+  const float* logits;     // [n_rows][k] the teacher's, NULL: cross entropy, mass 1 for the one token
+  const float* lse;        // [n_rows] the teacher's, NULL: the k places are all there is
+  int k;
+};
+struct Teach {
+  Targets t;
+  const int32_t* rowsel;
+  int64_t n_sel;
+  int V, d;
+  const float* weight;     // [n_rows] or NULL: 1
+  float norm, z_coef;
+};
+__device__ __forceinline__ float exp_of(float x) { return expf(x); }
+__device__ __forceinline__ double exp_of(double x) { return exp(x); }
+// A lane's target of a row, its mass (0: does not count) and the mass of the row; every lane of a wavefront calls it.  Real: float or, where sums
+// are in float64, double.
+template <class Real>
+struct Place {
+  int id;
+  Real t, mass;
+};
+template <class Real>
+__device__ __forceinline__ Place<Real> place_of(const Targets& T, int V, int64_t row) {
+  const int lane = threadIdx.x & 63;
+  const bool in = lane < T.k;
+  const int id = in ? T.ids[row * T.k + lane] : -1;
+  bool have = id >= 0 && id < V;
+  Real t;
+  if (!T.logits) {
+    t = have ? Real(1) : Real(0);
+  } else {
+    const float l = have ? T.logits[row * T.k + lane] : -INFINITY;
+    have = have && l > -INFINITY;                            // no number: does not count
+    const float m = wave_max(have ? l : -INFINITY);
+    t = have ? exp_of(Real(l) - Real(m)) : Real(0);
+    if (T.lse) t = have ? t * exp_of(Real(m) - Real(T.lse[row])) : Real(0);
+    else { const Real s = wave_sum(t); t = have ? t / s : Real(0); }
+  }
+  return Place<Real>{id, t, wave_sum(t)};
+}
+// Mass of the lane's token over all places that name it.
+template <class Real>
+__device__ __forceinline__ Real mass_of_token(int k, int id, Real t) {
+  Real s = 0;
+  for (int j = 0; j < k; ++j) {
+    const Real tj = __shfl(t, j, kWave);
+    if (__shfl(id, j, kWave) == id) s += tj;
+  }
+  return s;
+}
+// g of the row: 0 where nothing is taught
+__device__ __forceinline__ float row_weight(const Teach& A, int64_t row, bool taught) { return taught ? (A.weight ? A.weight[row] : 1.f) : 0.f; }
+// A factor of 0 in the dense part (a mass of 0 is no target, but a negative logsumexp with the penalty can come to it) would divide the sparse one: kept
+// off it by what is below the rounding of either.
+template <class Real>
+__device__ __forceinline__ Real dense_factor(Real mass, float z_coef, Real lse) {
+  const Real a = z_coef != 0.f ? mass + 2 * Real(z_coef) * lse : mass;
+  return fabs(a) < Real(1e-10) ? Real(1e-10) : a;
+}
+
+// ------------------------------------------------------------------ what a call leaves per row, compact, in selection order
+struct RowArrays {
+  float* lse;
+  float* ent;
+  float* l;                // the row's loss without its weight
+  float* w;                // its weight, 0 where nothing is taught
+  float* a;                // g a' for the blocks that are computed once more
+  float* zero;             // zeros
+  float* cref;             // r
+  float* sc;               // f
+  float* zt;               // [n_sel][k] logits of the targets
+  float* tt;               // [n_sel][k] their masses, all places of a token added up
+  float* mass;
+};
+struct OpenArgs {
+  Teach A;
+  const uint16_t *H, *W;
+  RowArrays R;
+  int32_t* flags;
+  int n_flags;
+  LiveArgs live;           // of the first chunk
+  uint32_t* dH;            // cleared, with the row outputs, where rows are left out; else NULL
+  int64_t dh_words;
+  float* row_out;
+  int64_t n_rows;
+};
+// One wavefront per selected row: the targets' masses, their logits (dot products of float32 sums), the row's reference.  The first workgroup clears
+// the flags and lays out the chunk, others clear what the call defines everywhere.
+constexpr int kAtOnce = 4;   // targets whose rows of W are under way together
+__global__ void __launch_bounds__(256)
+k_target_open(OpenArgs O) {
+  if (blockIdx.x == 0) {
+    for (int i = threadIdx.x; i < O.n_flags; i += 256) O.flags[i] = 0;
+    live_scan(O.live, static_cast<int>(threadIdx.x) < O.live.nblk);
+    return;
+  }
+  const Teach& A = O.A;
+  const int64_t blk = static_cast<int64_t>(blockIdx.x) - 1, nb = static_cast<int64_t>(gridDim.x) - 1;
+  if (O.dH) {
+    const int64_t stride = nb * 256;
+    for (int64_t i = blk * 256 + threadIdx.x; i < O.dh_words; i += stride) O.dH[i] = 0u;
+    for (int64_t i = blk * 256 + threadIdx.x; i < O.n_rows; i += stride) O.row_out[i] = 0.f;
+  }
+  const int lane = threadIdx.x & 63, k = A.t.k;
+  for (int64_t n = blk * 4 + threadIdx.x / kWave; n < A.n_sel; n += nb * 4) {
+    const int64_t row = A.rowsel ? A.rowsel[n] : n;
+    const Place<float> P = place_of<float>(A.t, A.V, row);
+    const uint4* h = reinterpret_cast<const uint4*>(O.H + row * A.d);
+    float z = 0.f;
+    unsigned long long left = __ballot(P.t != 0.f);          // NaN counts
+    while (left) {
+      int j[kAtOnce];
+      const uint4* w[kAtOnce];
+      float s[kAtOnce];
+#pragma unroll
+      for (int b = 0; b < kAtOnce; ++b) {
+        j[b] = left ? __ffsll(static_cast<long long>(left)) - 1 : j[b - (b > 0)];
+        left &= left - 1;
+        w[b] = reinterpret_cast<const uint4*>(O.W + static_cast<int64_t>(__shfl(P.id, j[b], kWave)) * A.d);
+        s[b] = 0.f;
+      }
+      for (int c = lane; c < A.d / 8; c += kWave) {
+        float x[8];
+        bf16x8_to_f32(h[c], x);
+#pragma unroll
+        for (int b = 0; b < kAtOnce; ++b) {
+          float y[8];
+          bf16x8_to_f32(w[b][c], y);
+#pragma unroll
+          for (int q = 0; q < 8; ++q) s[b] = fmaf(x[q], y[q], s[b]);
+        }
+      }
+#pragma unroll
+      for (int b = 0; b < kAtOnce; ++b) {
+        const float sum = wave_sum(s[b]);
+        if (lane == j[b]) z = sum;
+      }
+    }
+    const bool taught = P.mass > 0.f || P.mass != P.mass;
+    const float top = wave_max(P.t != 0.f ? z : -INFINITY), ts = mass_of_token(k, P.id, P.t);
+    if (lane < k) {
+      O.R.zt[n * k + lane] = z;
+      O.R.tt[n * k + lane] = P.t != 0.f ? ts : 0.f;
+    }
+    if (lane == 0) {
+      O.R.cref[n] = taught ? top : 1e30f;                    // every numerator of a row that teaches nothing is 0
+      O.R.w[n] = row_weight(A, row, taught);
+      O.R.mass[n] = P.mass;
+      O.R.zero[n] = 0.f;
+    }
+  }
+}
+
+// ------------------------------------------------------------------ bf16: scores that keep the numerators
+__global__ void __launch_bounds__(Cfg::T)
+k_target_tiles(const uint16_t* __restrict__ W, const uint16_t* __restrict__ H, int d, int V, const int32_t* __restrict__ rowsel, int64_t c0, int64_t mc,
+               int tiles_m, int tiles_n, int panel, int halved, float4* __restrict__ partial, int64_t n_pad, const float* __restrict__ cref,
+               uint16_t* __restrict__ E, int64_t Vp, int32_t* __restrict__ flags, const int32_t* __restrict__ cidx) {
+  __shared__ __attribute__((aligned(16))) uint16_t lds[kLogitLds / 2];
+  score_tiles<Leave::kNumerators, Cfg>(W, H, d, V, rowsel, c0, mc, nullptr, tiles_m, tiles_n, panel, partial, n_pad, KeepArgs{cref, E, Vp, flags, cidx, nullptr}, lds, halved);
+}
+__global__ void __launch_bounds__(NarrowCfg::T)
+k_target_narrow(const uint16_t* __restrict__ W, const uint16_t* __restrict__ H, int d, int V, const int32_t* __restrict__ rowsel, int64_t n_sel,
+                int tiles_m, float4* __restrict__ partial, int64_t n_pad, const float* __restrict__ cref, uint16_t* __restrict__ E, int64_t Vp,
+                int32_t* __restrict__ flags, const int32_t* __restrict__ cidx) {
+  __shared__ __attribute__((aligned(16))) uint16_t lds[kNarrowLds / 2];
+  score_tiles<Leave::kNumerators, NarrowCfg>(W, H, d, V, rowsel, 0, n_sel, nullptr, tiles_m, 1, kGN, partial, n_pad, KeepArgs{cref, E, Vp, flags, cidx, nullptr}, lds);
+}
+
+// ------------------------------------------------------------------ bf16: rows
+// Eight rows to a workgroup: their parts merged, then a wavefront to a row: its loss and factor, its k entries of the operand, its scaled copy of H.
+struct RowsArgs {
+  Teach A;
+  const uint16_t* H;
+  RowArrays R;
+  const float4* partial;
+  int tiles_m;
+  int64_t n_pad, c0, rows;
+  const int32_t *flags, *cidx;
+  uint16_t* E;
+  int64_t tiles_v;
+  uint16_t* Hs;            // NULL: dW is not wanted
+  int64_t mcp;
+  float* row_out;
+};
+// (a' p - t) / (a' exp(r - lse)); p near 1 is taken as 1 + expm1, so that a confident row's difference keeps its digits
+__device__ __forceinline__ float target_entry(float z, float lse, float r, float t, float a) {
+  const float lp = z - lse, q = t / a;
+  return __expf(lse - r) * (lp > -0.7f ? expm1f(lp) + (1.f - q) : __expf(lp) - q);
+}
+__device__ __forceinline__ bool is_finite(float x) { return fabsf(x) < INFINITY; }
+__global__ void __launch_bounds__(256)
+k_target_rows(RowsArgs O) {
+  __shared__ float s_lse[8], s_ent[8], s_sum[8];
+  const Teach& A = O.A;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, k = A.t.k;
+  const int64_t m0 = static_cast<int64_t>(blockIdx.x) * 8;
+  {
+    const int64_t m = m0 + (lane & 7);
+    Part p;
+    float none;
+    if (merge_parts<true>(O.partial, O.tiles_m, O.n_pad, O.c0 + m, m < O.rows, p, none)) {
+      s_lse[lane] = p.m + logf(p.s);
+      s_ent[lane] = s_lse[lane] - p.t / p.s;
+      s_sum[lane] = p.s;
+    }
+  }
+  __syncthreads();
+  for (int q = wave; q < 8; q += 4) {
+    const int64_t m = m0 + q, n = O.c0 + m;
+    if (m >= O.rows) break;
+    const int64_t row = A.rowsel ? A.rowsel[n] : n;
+    const int blk = O.cidx[n >> 8], flag = O.flags[n >> 8];
+    const float w = O.R.w[n], mass = O.R.mass[n], r = O.R.cref[n];
+    const bool in = lane < k, taught = r < 1e30f || r != r;
+    const int id = in ? A.t.ids[row * k + lane] : -1;
+    const float z = in ? O.R.zt[n * k + lane] : 0.f, ts = in ? O.R.tt[n * k + lane] : 0.f;
+    const float lse = s_lse[q], g = w / A.norm, a = dense_factor(mass, A.z_coef, lse);
+    float l = 0.f, out = 0.f, f = 0.f;
+    if (taught) {
+      if (!A.t.logits) {
+        out = __shfl(z, 0, kWave) - lse;
+        l = A.z_coef != 0.f ? fmaf(A.z_coef * lse, lse, -out) : -out;
+      } else {
+        const Place<float> P = place_of<float>(A.t, A.V, row);
+        out = l = wave_sum(P.t != 0.f ? P.t * (logf(P.t) - (z - lse)) : 0.f);
+      }
+      f = g != 0.f ? (flag ? 1.f : g * a * __expf(r - lse)) : 0.f;
+    }
+    // The row's entries are rounded to bf16.  dH's row factor is taken as what makes them, times it, what they were (least squares; one target: exactly), as
+    // they and not the dense part make most of the row's dH: 60 rows of 2048 with ten targets dH off by 0.0028 of its norm without it, its own rounding
+    // being 0.0017.  (Not so dW's, where a dense entry of few rows stands by itself and would carry the shift.)
+    const bool put = f != 0.f && !flag && ts != 0.f;
+    const float e = put ? target_entry(z, lse, r, ts, a) : 0.f, most = wave_max(fabsf(e));
+    const uint16_t rounded = f2bf(e);
+    float shift = 1.f;
+    if (most > 0.f) {
+      const float x = e / most, y = bf2f(rounded) / most, xy = wave_sum(x * y), yy = wave_sum(y * y);
+      if (yy > 0.f) shift = xy / yy;
+    }
+    if (lane == 0) {
+      O.R.lse[n] = taught ? lse : 0.f;
+      O.R.ent[n] = taught ? s_ent[q] : 0.f;
+      O.R.l[n] = l;
+      O.R.a[n] = g != 0.f ? g * a : 0.f;
+      O.R.sc[n] = f * shift;
+      if (O.row_out) O.row_out[row] = out;
+    }
+    uint16_t* const Erow = O.E + blk_offset(blk, 0, O.tiles_v) + (m & 255) * 256;
+    if (f != 0.f) {
+      if (put) Erow[static_cast<int64_t>(id >> 8) * kBlkElems + (id & 255)] = rounded;
+    } else if (!is_finite(s_sum[q]) || (taught && !is_finite(lse))) {
+      // a row that teaches nothing may hold anything: its numerators must not be multiplied; the last row's stand in those behind it as well
+      const int64_t rows = m == O.rows - 1 ? (m & ~int64_t{63}) + 64 - m : 1;
+      for (int64_t i = 0; i < rows; ++i)
+        for (int64_t vb = 0; vb < O.tiles_v; ++vb) *reinterpret_cast<uint2*>(Erow + i * 256 + vb * kBlkElems + lane * 4) = make_uint2(0u, 0u);
+    }
+    if (O.Hs) {
+      const int64_t mp = static_cast<int64_t>(blk) * 256 + (m & 255);
+      const uint4* h = reinterpret_cast<const uint4*>(O.H + row * A.d);
+      for (int c = lane; c < A.d / 8; c += kWave) {
+        float x[8];
+        bf16x8_to_f32(h[c], x);
+        uint4 v = make_uint4(0u, 0u, 0u, 0u);
+        if (f != 0.f) v = make_uint4(pack_bf16x2(x[0] * f, x[1] * f), pack_bf16x2(x[2] * f, x[3] * f), pack_bf16x2(x[4] * f, x[5] * f), pack_bf16x2(x[6] * f, x[7] * f));
+        reinterpret_cast<uint4*>(O.Hs + (static_cast<int64_t>(c >> 5) * O.mcp + mp) * 256)[c & 31] = v;
+      }
+    }
+  }
+}
+// Blocks in which some logit lies far above its row's reference: dz is computed once more, its k entries on the way out.
+struct PutTargets {
+  const int32_t *rowsel, *ids;
+  int k;
+  const float *zt, *tt, *lse, *a, *w;
+  float norm;
+  __device__ __forceinline__ void operator()(char* staged, int64_t n, int v0, int width) const {
+    const float g = n < 0 ? 0.f : w[n] / norm;
+    if (g == 0.f) {                                          // whatever its logits are
+      for (int i = 0; i < width * 2; i += 4) *reinterpret_cast<uint32_t*>(staged + i) = 0u;
+      return;
+    }
+    const int32_t* id = ids + (rowsel ? rowsel[n] : n) * k;
+    for (int j = 0; j < k; ++j) {
+      const int v = id[j] - v0;
+      const float t = tt[n * k + j];
+      if (v < 0 || v >= width || t == 0.f) continue;
+      const uint16_t e = f2bf(fmaf(a[n], __expf(zt[n * k + j] - lse[n]), -g * t));
+      __builtin_memcpy(staged + v * 2, &e, 2);
+    }
+  }
+};
+__global__ void __launch_bounds__(Cfg::T)
+k_target_flagged(const uint16_t* __restrict__ W, const uint16_t* __restrict__ H, int d, int V, const int32_t* __restrict__ rowsel, int64_t c0, int64_t mc,
+                 const float* __restrict__ zero, PutTargets put, int tiles_m, int tiles_n, uint16_t* __restrict__ dZ, int64_t Vp,
+                 const int32_t* __restrict__ flags, const int32_t* __restrict__ cidx) {
+  __shared__ __attribute__((aligned(16))) uint16_t lds[kLogitLds / 2];
+  for (int tile_n = 0; tile_n < tiles_n; ++tile_n) {
+    const int out_blk = cidx[(c0 >> 8) + tile_n];
+    if (!flags[(c0 >> 8) + tile_n]) continue;                // the same for every thread of the grid
+    for (int tile_m = blockIdx.x; tile_m < tiles_m; tile_m += gridDim.x)
+      dz_tile(tile_m, tile_n, W, H, d, V, rowsel, c0, mc, put, put.lse, put.a, zero, dZ, Vp, out_blk, lds);
+  }
+}
+
+// ------------------------------------------------------------------ bf16: the two gradient products (umas_gradients.h)
+struct GradientArgs {
+  const uint16_t* E;
+  int64_t Vp, mcp;
+  const uint16_t *W, *Hs;
+  int d, V, tiles_v, tiles_d;
+  DhSlices sl;
+  int tiles_r;
+  LiveInfo* info;
+  const int32_t* blk_orig;
+  uint16_t* dH;
+  int accumulate;
+  const int32_t* rowsel;
+  int64_t c0, rows;
+  const float* sc;
+};
+__global__ void __launch_bounds__(Cfg::T)
+k_target_gemm(GradientArgs G, float* __restrict__ dW) {
+  __shared__ __attribute__((aligned(16))) uint16_t lds[MixedLdsBytes<Cfg>::value / 2];
+  gemm_dh_dw<false, float>(G.E, 1, G.Vp, G.mcp, G.W, G.Hs, G.d, G.V, G.tiles_v, G.tiles_d, G.sl, G.tiles_r, G.info, G.blk_orig, G.dH, dW, G.accumulate,
+                           G.rowsel, G.c0, G.rows, nullptr, nullptr, G.sc, lds);
+}
+__global__ void __launch_bounds__(Cfg::T)
+k_target_gemm_bf16(GradientArgs G, uint16_t* __restrict__ dW) {
+  __shared__ __attribute__((aligned(16))) uint16_t lds[MixedLdsBytes<Cfg>::value / 2];
+  gemm_dh_dw<false, uint16_t>(G.E, 1, G.Vp, G.mcp, G.W, G.Hs, G.d, G.V, G.tiles_v, G.tiles_d, G.sl, G.tiles_r, G.info, G.blk_orig, G.dH, dW, G.accumulate,
+                              G.rowsel, G.c0, G.rows, nullptr, nullptr, G.sc, lds);
+}
+__global__ void __launch_bounds__(ShortCfg::T, 2)
+k_target_dw_short(GradientArgs G, int tiles_n, float* __restrict__ dW) {
+  __shared__ __attribute__((aligned(16))) char lds[kShortLds];
+  dw_short<float>(G.E, 1, G.Vp, G.mcp, G.Hs, G.d, G.V, G.tiles_v, tiles_n, G.info, dW, G.accumulate, lds);
+}
+__global__ void __launch_bounds__(ShortCfg::T, 2)
+k_target_dw_short_bf16(GradientArgs G, int tiles_n, uint16_t* __restrict__ dW) {
+  __shared__ __attribute__((aligned(16))) char lds[kShortLds];
+  dw_short<uint16_t>(G.E, 1, G.Vp, G.mcp, G.Hs, G.d, G.V, G.tiles_v, tiles_n, G.info, dW, G.accumulate, lds);
+}
+// dW of bf16 from the float32 sums of several chunks: rounded once
+__global__ void __launch_bounds__(256)
+k_target_round(const float* __restrict__ sums, uint16_t* __restrict__ dW, int64_t n8, int accumulate) {
+  for (int64_t i = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x; i < n8; i += static_cast<int64_t>(gridDim.x) * 256) {
+    float4 lo = reinterpret_cast<const float4*>(sums)[2 * i], hi = reinterpret_cast<const float4*>(sums)[2 * i + 1];
+    uint4* const at = reinterpret_cast<uint4*>(dW) + i;
+    if (accumulate) {
+      float x[8];
+      bf16x8_to_f32(*at, x);
+      lo.x += x[0]; lo.y += x[1]; lo.z += x[2]; lo.w += x[3];
+      hi.x += x[4]; hi.y += x[5]; hi.z += x[6]; hi.w += x[7];
+    }
+    *at = make_uint4(pack_bf16x2(lo.x, lo.y), pack_bf16x2(lo.z, lo.w), pack_bf16x2(hi.x, hi.y), pack_bf16x2(hi.z, hi.w));
+  }
+}
+
+// ------------------------------------------------------------------ statistics and what closes a call
+struct StatArgs {
+  int64_t n_sel;
+  const int32_t *rowsel, *role;
+  const float *l, *w, *ent, *lse, *mass;
+  float norm;
+  umas_target_stats* stats;
+};
+constexpr int kCloseT = 256;
+// the model's record (k = 0) or a role's, a workgroup to each; sums in float64, in an order that does not depend on scheduling
+__device__ __forceinline__ void target_stats(const StatArgs& S, int k) {
+  __shared__ double smem[32];
+  double v[6] = {}, sum[6];
+  for (int64_t n = threadIdx.x; n < S.n_sel; n += kCloseT) {
+    if (k > 0 && S.role[S.rowsel ? S.rowsel[n] : n] != k - 1) continue;
+    const bool taught = S.mass[n] != 0.f;
+    const float w = S.w[n];
+    v[0] += w != 0.f ? static_cast<double>(w) * static_cast<double>(S.l[n]) : 0.0;
+    v[1] += static_cast<double>(w);
+    v[2] += taught ? static_cast<double>(S.ent[n]) : 0.0;
+    v[3] += taught ? static_cast<double>(S.lse[n]) : 0.0;
+    v[4] += 1.0;
+    v[5] += taught ? 0.0 : 1.0;
+  }
+#pragma unroll
+  for (int j = 0; j < 6; ++j) sum[j] = block_sum<double>(v[j], smem);
+  if (threadIdx.x != 0) return;
+  const double taught = sum[4] - sum[5];
+  umas_target_stats s;
+  s.loss = sum[4] > 0 ? static_cast<float>(sum[0] / (k == 0 ? static_cast<double>(S.norm) : sum[4])) : 0.f;
+  s.weight_mean = sum[4] > 0 ? static_cast<float>(sum[1] / sum[4]) : 0.f;
+  s.entropy_mean = taught > 0 ? static_cast<float>(sum[2] / taught) : 0.f;
+  s.lse_mean = taught > 0 ? static_cast<float>(sum[3] / taught) : 0.f;
+  s.n_scored = static_cast<int64_t>(sum[4]);
+  s.n_ignored = static_cast<int64_t>(sum[5]);
+  S.stats[k] = s;
+}
+struct CloseArgs {
+  StatArgs stats;
+  unsigned n_stats, reduce_rows;          // workgroups; 0: none
+  DhSlices sl;
+  int tiles_r, tiles_d, d;
+  const LiveInfo* info;
+  const int32_t* blk_orig;
+  uint16_t* dH;
+  const int32_t* rowsel;
+  int64_t c0, rows;
+  const float* sc;
+};
+__global__ void __launch_bounds__(kCloseT)
+k_target_close(CloseArgs C) {
+  unsigned i = blockIdx.x;
+  if (i < C.n_stats) {
+    target_stats(C.stats, static_cast<int>(i));
+    return;
+  }
+  i -= C.n_stats;
+  dh_reduce<false>(i % C.reduce_rows, i / C.reduce_rows, C.sl, C.tiles_r, C.tiles_d, nullptr, C.d, C.info, C.blk_orig, C.dH, C.rowsel, C.c0, C.rows, nullptr,
+                   nullptr, C.sc);
+}
+
+// ------------------------------------------------------------------ float32, sums in float64
+struct OpenArgsF32 {
+  Teach A;
+  const float *H, *W;
+  RowArrays R;
+  double *zt, *tt, *mass;
+  float* h_rows;                          // [n_sel][d]: the rows that teach, zeros for the others, whatever they hold; NULL: no dW
+  uint32_t *dH, *row_out;
+  int64_t dh_words, n_rows;
+};
+__global__ void __launch_bounds__(256)
+k_target_open_f32(OpenArgsF32 O) {
+  const Teach& A = O.A;
+  if (O.dH) {
+    const int64_t stride = static_cast<int64_t>(gridDim.x) * 256;
+    for (int64_t i = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x; i < O.dh_words; i += stride) O.dH[i] = 0u;
+    for (int64_t i = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x; i < O.n_rows; i += stride) O.row_out[i] = 0u;
+  }
+  const int lane = threadIdx.x & 63, k = A.t.k;
+  const int64_t n = static_cast<int64_t>(blockIdx.x) * 4 + threadIdx.x / kWave;
+  if (n >= A.n_sel) return;
+  const int64_t row = A.rowsel ? A.rowsel[n] : n;
+  const Place<double> P = place_of<double>(A.t, A.V, row);
+  double z = 0.0;
+  for (unsigned long long left = __ballot(P.t != 0.0); left; left &= left - 1) {
+    const int j = __ffsll(static_cast<long long>(left)) - 1;
+    const float* w = O.W + static_cast<int64_t>(__shfl(P.id, j, kWave)) * A.d;
+    double s = 0.0;
+    for (int c = lane; c < A.d; c += kWave) s = fma(static_cast<double>(O.H[row * A.d + c]), static_cast<double>(w[c]), s);
+    s = wave_sum(s);
+    if (lane == j) z = s;
+  }
+  const double ts = mass_of_token(k, P.id, P.t);
+  const float weight = row_weight(A, row, P.mass != 0.0);
+  if (O.h_rows)
+    for (int c = lane; c < A.d; c += kWave) O.h_rows[n * A.d + c] = weight != 0.f ? O.H[row * A.d + c] : 0.f;
+  if (lane < k) {
+    O.zt[n * k + lane] = z;
+    O.tt[n * k + lane] = P.t != 0.0 ? ts : 0.0;
+  }
+  if (lane == 0) {
+    O.R.w[n] = weight;
+    O.R.mass[n] = static_cast<float>(P.mass);
+    O.mass[n] = P.mass;
+  }
+}
+struct DzArgsF32 {
+  Teach A;
+  const float *H, *W;
+  RowArrays R;
+  const double *z, *zt, *tt, *mass, *lse; // z: kept logits [n_sel][V] or NULL
+  int64_t c0, rows;
+  int per_wg;
+  float *dz, *row_out;
+};
+// What a row's dz is made of; every lane gets the same.
+struct RowF32 {
+  double lse, g, a;                       // dz = a exp(z - lse) - g t
+};
+__device__ __forceinline__ RowF32 row_f32(const DzArgsF32& D, int64_t n) {
+  const float w = D.R.w[n];
+  const double lse = D.lse[n], g = static_cast<double>(w) / static_cast<double>(D.A.norm);
+  return RowF32{lse, g, g * dense_factor(D.mass[n], D.A.z_coef, lse)};
+}
+__device__ __forceinline__ void finish_row_f32(const DzArgsF32& D, int64_t n) {   // one wavefront: the row's loss
+  const int lane = threadIdx.x & 63, k = D.A.t.k;
+  const int64_t row = D.A.rowsel ? D.A.rowsel[n] : n;
+  const double lse = D.lse[n], z = lane < k ? D.zt[n * k + lane] : 0.0;
+  double l = 0.0, out = 0.0;
+  const bool taught = D.mass[n] != 0.0;
+  if (taught && !D.A.t.logits) {
+    out = __shfl(z, 0, kWave) - lse;
+    l = -out + static_cast<double>(D.A.z_coef) * lse * lse;
+  } else if (taught) {
+    const Place<double> P = place_of<double>(D.A.t, D.A.V, row);
+    out = l = wave_sum(P.t != 0.0 ? P.t * (log(P.t) - (z - lse)) : 0.0);
+  }
+  if (lane == 0) {
+    D.R.l[n] = static_cast<float>(l);
+    if (D.row_out) D.row_out[row] = static_cast<float>(out);
+  }
+}
+__device__ __forceinline__ void put_targets_f32(const DzArgsF32& D, int64_t n, const RowF32& r, int v0, int v1, int j) {
+  const int k = D.A.t.k, id = D.A.t.ids[(D.A.rowsel ? D.A.rowsel[n] : n) * k + j];
+  const double t = D.tt[n * k + j];
+  if (id < v0 || id >= v1 || !(t != 0.0) || r.g == 0.0) return;
+  D.dz[(n - D.c0) * D.A.V + id] = static_cast<float>(r.a * exp(D.zt[n * k + j] - r.lse) - r.g * t);
+}
+// From kept logits: a workgroup to a row and a part of the vocabulary.
+__global__ void __launch_bounds__(256)
+k_target_dz_kept_f32(DzArgsF32 D) {
+  const int64_t m = blockIdx.y, n = D.c0 + m;
+  const int V = D.A.V, v0 = blockIdx.x * D.per_wg, v1 = min(v0 + D.per_wg, V);
+  if (blockIdx.x == 0 && threadIdx.x < kWave) finish_row_f32(D, n);
+  const RowF32 r = row_f32(D, n);
+  for (int v = v0 + threadIdx.x; v < v1; v += 256) D.dz[m * V + v] = r.g != 0.0 ? static_cast<float>(r.a * exp(D.z[n * V + v] - r.lse)) : 0.f;
+  __syncthreads();
+  if (static_cast<int>(threadIdx.x) < D.A.t.k) put_targets_f32(D, n, r, v0, v1, threadIdx.x);
+}
+// Computed once more: tiles as in the scores.
+__global__ void __launch_bounds__(f32::kWaves* kWave)
+k_target_dz_f32(DzArgsF32 D) {
+  using namespace f32;
+  const int wave = threadIdx.x >> 6, V = D.A.V, d = D.A.d;
+  const int64_t n0 = static_cast<int64_t>(blockIdx.y) * kTile, vb = static_cast<int64_t>(blockIdx.x) * kVocBlock;
+  if (blockIdx.x == 0)
+    for (int64_t m = n0 + wave; m < min(n0 + kTile, D.rows); m += kWaves) finish_row_f32(D, D.c0 + m);
+  if (vb + wave * kTile < V) {
+    const int v0 = static_cast<int>(vb) + wave * kTile;
+    Rows<2> h, w;
+    h.vec = w.vec = d % 4 == 0;
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const int64_t n = D.c0 + min(n0 + blk_index(i), D.rows - 1);
+      h.p[i] = D.H + (D.A.rowsel ? D.A.rowsel[n] : n) * static_cast<int64_t>(d);
+      w.p[i] = D.W + static_cast<int64_t>(min(v0 + blk_index(i), V - 1)) * d;
+    }
+    double4v acc[2][2];
+    zero<2>(acc);
+    product<2>(h, w, 0, d, d, acc);
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        const int64_t m = n0 + blk_row(i, r);
+        if (m >= D.rows) continue;
+        const RowF32 x = row_f32(D, D.c0 + m);
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+          const int v = v0 + blk_index(j);
+          if (v < V) D.dz[m * V + v] = x.g != 0.0 ? static_cast<float>(x.a * exp(acc[i][j][r] - x.lse)) : 0.f;
+        }
+      }
+  }
+  __syncthreads();
+  const int k = D.A.t.k;
+  for (int i = threadIdx.x; i < kTile * k; i += kWaves * kWave) {
+    const int64_t m = n0 + i / k;
+    if (m < D.rows) put_targets_f32(D, D.c0 + m, row_f32(D, D.c0 + m), static_cast<int>(vb), static_cast<int>(min<int64_t>(vb + kVocBlock, V)), i % k);
+  }
+}
+
+// ------------------------------------------------------------------ host side
+struct Ws {
+  float4* partial;
+  RowArrays R;
+  int32_t *flags, *blk_cidx, *blk_orig;
+  LiveInfo* live;
+  double *zt, *tt, *mass, *rest, *lse64;  // float32
+  float *logp_c, *h_rows;
+  char* chunk;
+  size_t fixed_bytes;
+};
+void carve(Carver& c, Ws& w, int64_t n_sel, int d, int V, int k, umas_dtype dt) {
+  const int64_t n_pad = round_up(n_sel > 0 ? n_sel : 1, Cfg::BN), tiles_m = (V + Cfg::BM - 1) / Cfg::BM;
+  const bool bf = dt == UMAS_BF16;
+  w = Ws{};
+  if (bf) w.partial = c.take<float4>(static_cast<size_t>(tiles_m) * n_pad);
+  for (float** p : {&w.R.lse, &w.R.ent, &w.R.l, &w.R.w, &w.R.a, &w.R.zero, &w.R.cref, &w.R.sc, &w.R.mass}) *p = c.take<float>(n_pad);
+  if (bf) {
+    w.R.zt = c.take<float>(static_cast<size_t>(n_pad) * k);
+    w.R.tt = c.take<float>(static_cast<size_t>(n_pad) * k);
+    w.flags = c.take<int32_t>(cdiv(n_pad, 256));
+    w.blk_cidx = c.take<int32_t>(cdiv(n_pad, 256));
+    w.blk_orig = c.take<int32_t>(cdiv(n_pad, 256));
+    w.live = c.take<LiveInfo>(1);
+  } else {
+    w.zt = c.take<double>(static_cast<size_t>(n_pad) * k);
+    w.tt = c.take<double>(static_cast<size_t>(n_pad) * k);
+    w.mass = c.take<double>(n_pad);
+    w.rest = c.take<double>(n_pad);
+    w.lse64 = c.take<double>(n_pad);
+    w.logp_c = c.take<float>(n_pad);
+    w.h_rows = c.take<float>(static_cast<size_t>(n_pad) * d);
+  }
+  w.chunk = c.base ? c.base + c.off : nullptr;
+  w.fixed_bytes = c.off;
+}
+// float32 sums of dW where it is bf16 and comes from several chunks
+size_t sum_bytes(int d, int V, int dW_type) { return dW_type == UMAS_BF16 ? align_up(static_cast<size_t>(V) * d * sizeof(float)) : 0; }
+size_t kept_f32_bytes(int64_t n_sel, int V) {
+  const double b = static_cast<double>(n_sel) * V * sizeof(double);
+  return b <= 1073741824.0 ? align_up(static_cast<size_t>(n_sel) * V * sizeof(double)) : 0;
+}
+bool sizes_ok(int64_t n_sel, int d, int V, int k, int dW_type) {
+  return n_sel >= 0 && d >= 1 && V >= 1 && k >= 1 && k <= UMAS_MAX_TOP && dW_type >= UMAS_NO_DW && dW_type <= UMAS_BF16;
+}
+size_t least_bytes(int64_t n_sel, int d, int V, int k, umas_dtype dt, int dW_type) {
+  if (!sizes_ok(n_sel, d, V, k, dW_type)) return 0;
+  Carver c(nullptr);
+  Ws w;
+  carve(c, w, n_sel, d, V, k, dt);
+  const int64_t all = std::max<int64_t>(n_sel, 1), mc = std::min<int64_t>(all, 256);
+  const size_t chunked = chunk_bytes(mc, d, V, dt) + (n_sel > 256 ? sum_bytes(d, V, dW_type) : 0);
+  // the sums of chunks can take more than one chunk of all rows
+  return c.off + (all <= (dt == UMAS_F32 ? kF32ChunkRows : kMaxChunkRows) ? std::min(chunked, chunk_bytes(all, d, V, dt)) : chunked);
+}
+size_t full_bytes(int64_t n_sel, int d, int V, int k, umas_dtype dt, int dW_type) {
+  if (!sizes_ok(n_sel, d, V, k, dW_type)) return 0;
+  Carver c(nullptr);
+  Ws w;
+  carve(c, w, n_sel, d, V, k, dt);
+  int64_t mc = std::max<int64_t>(n_sel, 1);
+  const int64_t cap = dt == UMAS_F32 ? kF32ChunkRows : kMaxChunkRows;
+  size_t sums = 0;
+  if (mc > cap) {
+    const int64_t nchunk = (mc + cap - 1) / cap;
+    mc = round_up((mc + nchunk - 1) / nchunk, 256);
+    sums = sum_bytes(d, V, dW_type);
+  }
+  if (dt == UMAS_F32) return c.off + chunk_bytes(mc, d, V, dt) + kept_f32_bytes(n_sel, V) + align_up(f32::score_room(n_sel, V));
+  return c.off + chunk_bytes(mc, d, V, dt) + full_part_bytes(n_sel, mc, d, V) + sums;
+}
+
+struct Call {
+  const void *H, *W;
+  umas_dtype dt;
+  int64_t n_rows;
+  int32_t d, V;
+  Targets t;
+  const int32_t* rowsel;
+  int64_t n_sel;
+  const float* weight;
+  const int32_t* tok_role;
+  int32_t n_roles;
+  float z_coef;
+  int32_t accumulate_dW;
+  int64_t norm_rows;
+  umas_target_stats* stats;
+  float* row_out;
+  void *dH, *dW;
+  int32_t dW_type;
+  void* workspace;
+  size_t workspace_bytes;
+  hipStream_t st;
+};
+umas_status check_call(const Call& a) {
+  umas_status s = check_model_args(a.H, a.W, a.dt, a.n_rows, a.d, a.V, a.t.ids, a.rowsel, a.n_sel);
+  if (s != UMAS_OK) return s;
+  UMAS_REQUIRE(a.t.k >= 1 && a.t.k <= UMAS_MAX_TOP, UMAS_ESHAPE, "k=%d outside [1,%d]", a.t.k, UMAS_MAX_TOP);
+  UMAS_REQUIRE(a.dH || a.n_rows == 0, UMAS_EINVAL, "dH must not be NULL");
+  UMAS_REQUIRE(a.stats, UMAS_EINVAL, "stats must not be NULL");
+  UMAS_REQUIRE(a.n_roles >= 0 && a.n_roles <= UMAS_MAX_ROLES, UMAS_ESHAPE, "n_roles=%d outside [0,%d]", a.n_roles, UMAS_MAX_ROLES);
+  UMAS_REQUIRE(a.tok_role || a.n_roles == 0, UMAS_EINVAL, "tok_role is NULL but n_roles > 0");
+  UMAS_REQUIRE(a.dW_type == UMAS_F32 || (a.dW_type == UMAS_BF16 && a.dt == UMAS_BF16) || a.dW_type == UMAS_NO_DW, UMAS_EDTYPE,
+               "dW_type=%d: float32, the type of the head, or none", a.dW_type);
+  UMAS_REQUIRE((a.dW != nullptr) == (a.dW_type != UMAS_NO_DW), UMAS_EINVAL, "dW must be NULL with UMAS_NO_DW and only then");
+  UMAS_REQUIRE(a.dW_type != UMAS_BF16 || reinterpret_cast<uintptr_t>(a.dW) % 16 == 0, UMAS_EINVAL, "a dW of bf16 must be 16-byte aligned");
+  UMAS_REQUIRE(a.z_coef >= 0.f && a.z_coef < INFINITY, UMAS_EINVAL, "z_coef=%g must be finite and not negative", static_cast<double>(a.z_coef));
+  UMAS_REQUIRE(a.n_sel < (1LL << 31), UMAS_ESHAPE, "at most 2^31-1 selected rows");
+  UMAS_REQUIRE(a.norm_rows == 0 || a.norm_rows >= a.n_sel, UMAS_EINVAL, "norm_rows=%lld must be 0 or at least n_sel=%lld",
+               static_cast<long long>(a.norm_rows), static_cast<long long>(a.n_sel));
+  return check_ws(a.workspace, a.workspace_bytes, least_bytes(a.n_sel, a.d, a.V, a.t.k, a.dt, a.dW_type));
+}
+StatArgs stat_args(const Call& a, const Ws& w, float norm) {
+  return StatArgs{a.n_sel, a.rowsel, a.tok_role, w.R.l, w.R.w, w.R.ent, w.R.lse, w.R.mass, norm, a.stats};
+}
+
+umas_status run_f32(const Call& a, const Ws& w, const Teach& A) {
+  hipStream_t st = a.st;
+  const float *H = static_cast<const float*>(a.H), *W = static_cast<const float*>(a.W);
+  const size_t room = a.workspace_bytes - w.fixed_bytes;
+  const int64_t n = a.n_sel, cap = std::min<int64_t>(n, kF32ChunkRows);
+  int64_t mc = cap;
+  if (chunk_bytes(mc, a.d, a.V, UMAS_F32) > room) mc = std::max<int64_t>(static_cast<int64_t>(room / chunk_bytes(256, a.d, a.V, UMAS_F32)) * 256, 256);
+  mc = std::min(mc, n);
+  const size_t z_at = chunk_bytes(mc, a.d, a.V, UMAS_F32), z_bytes = kept_f32_bytes(n, a.V);
+  double* const z = z_bytes > 0 && z_at + z_bytes <= room ? reinterpret_cast<double*>(w.chunk + z_at) : nullptr;
+  hipLaunchKernelGGL(k_target_open_f32, dim3(cdiv(n, 4)), dim3(256), 0, st,
+                     OpenArgsF32{A, H, W, w.R, w.zt, w.tt, w.mass, a.dW ? w.h_rows : nullptr, a.rowsel ? static_cast<uint32_t*>(a.dH) : nullptr, reinterpret_cast<uint32_t*>(a.row_out),
+                                 a.n_rows * a.d, a.row_out ? a.n_rows : 0});
+  UMAS_LAUNCHED("k_target_open_f32");
+  char* const parts = z ? w.chunk + z_at + z_bytes : w.chunk;
+  umas_status s = f32::score(W, H, a.d, a.V, a.rowsel, n, nullptr, parts, room - static_cast<size_t>(parts - w.chunk),
+                             f32::ScoreOut{z, w.rest, w.logp_c, w.R.lse, w.R.ent, nullptr, nullptr, nullptr, w.lse64}, st);
+  if (s != UMAS_OK) return s;
+  for (int64_t c0 = 0; c0 < n; c0 += mc) {
+    const int64_t rows = std::min(mc, n - c0);
+    DzArgsF32 D{A, H, W, w.R, z, w.zt, w.tt, w.mass, w.lse64, c0, rows, 0, reinterpret_cast<float*>(w.chunk), a.row_out};
+    if (z) {
+      const unsigned wgs = cdiv(2048, static_cast<size_t>(rows)), most = cdiv(a.V, 1024);
+      D.per_wg = static_cast<int>(cdiv(most, std::min(wgs, most))) * 1024;
+      hipLaunchKernelGGL(k_target_dz_kept_f32, dim3(cdiv(a.V, D.per_wg), static_cast<unsigned>(rows)), dim3(256), 0, st, D);
+      UMAS_LAUNCHED("k_target_dz_kept_f32");
+    } else {
+      hipLaunchKernelGGL(k_target_dz_f32, dim3(cdiv(a.V, f32::kVocBlock), cdiv(rows, f32::kTile)), dim3(f32::kWaves * kWave), 0, st, D);
+      UMAS_LAUNCHED("k_target_dz_f32");
+    }
+    f32::launch_gradients(f32::GradArgs{D.dz, W, H, a.d, a.V, a.rowsel, c0, static_cast<int>(rows), a.accumulate_dW || c0 > 0 ? 1 : 0,
+                                        static_cast<float*>(a.dH), static_cast<float*>(a.dW), 0, 0, 0, w.h_rows + c0 * a.d}, f32::StatArgs{}, st);
+    UMAS_LAUNCHED("k_target_gradients_f32");
+  }
+  CloseArgs C{};
+  C.stats = stat_args(a, w, A.norm);
+  C.n_stats = 1 + a.n_roles;
+  hipLaunchKernelGGL(k_target_close, dim3(C.n_stats), dim3(kCloseT), 0, st, C);
+  UMAS_LAUNCHED("k_target_close");
+  return UMAS_OK;
+}
+
+umas_status run_bf16(const Call& a, const Ws& w, const Teach& A) {
+  hipStream_t st = a.st;
+  const uint16_t *H = static_cast<const uint16_t*>(a.H), *W = static_cast<const uint16_t*>(a.W);
+  const int64_t n_sel = a.n_sel, Vp = round_up(a.V, 256);
+  const int d = a.d, V = a.V, tiles_v = static_cast<int>(Vp / 256), tiles_d = (d + 255) / 256;
+  size_t room = a.workspace_bytes - w.fixed_bytes;
+  // chunks of rows as the workspace allows; a dW of bf16 that comes from several has its sums in front of them
+  int64_t mc = std::min(n_sel, kMaxChunkRows);
+  const bool chunked = n_sel > kMaxChunkRows || chunk_bytes(mc, d, V, UMAS_BF16) > room;
+  float* sums = nullptr;
+  char* chunk = w.chunk;
+  if (chunked && a.dW_type == UMAS_BF16) {
+    sums = reinterpret_cast<float*>(chunk);
+    chunk += sum_bytes(d, V, UMAS_BF16);
+    room -= sum_bytes(d, V, UMAS_BF16);
+  }
+  if (chunked) {
+    if (chunk_bytes(mc, d, V, UMAS_BF16) > room) mc = std::max<int64_t>(static_cast<int64_t>(room / chunk_bytes(256, d, V, UMAS_BF16)), 1) * 256;
+    const int64_t nchunk = (n_sel + mc - 1) / mc;
+    mc = std::min(mc, round_up((n_sel + nchunk - 1) / nchunk, 256));
+  }
+  UMAS_REQUIRE(chunk_bytes(std::min(mc, n_sel), d, V, UMAS_BF16) <= room, UMAS_EWORKSPACE, "workspace cannot hold one chunk of %lld rows", static_cast<long long>(mc));
+  const bool no_dw = a.dW_type == UMAS_NO_DW;
+  auto plan = [&](int64_t rows, DhSlices* sl) {             // as in the policy update: partial sums behind the chunk's operands or in the place of the scores' parts
+    const size_t used = chunk_bytes(rows, d, V, UMAS_BF16), behind = room > used ? room - used : 0;
+    const size_t front = static_cast<size_t>(reinterpret_cast<char*>(w.R.lse) - reinterpret_cast<char*>(w.partial));
+    const size_t have = slices_dh(n_sel, mc, d) ? std::max(behind, front) : 0;
+    const GradPlan p = no_dw ? GradPlan{plan_dh((rows + 255) / 256, tiles_d, tiles_v, have, true), false} : plan_gradients(n_sel, rows, d, V, have);
+    *sl = DhSlices{p.dh.slices, p.dh.voc_blks, behind > front ? reinterpret_cast<float*>(chunk + used) : reinterpret_cast<float*>(w.partial)};
+    return p.dw_apart;
+  };
+  auto live_args = [&](int64_t c0, int64_t rows, int slices, bool dw_apart) {
+    return LiveArgs{static_cast<int>(c0 >> 8), static_cast<int>(cdiv(rows, 256)), rows, 1, dw_apart || no_dw ? 0 : tiles_v, tiles_d, Vp, slices, nullptr,
+                    w.blk_cidx, w.blk_orig, w.live};
+  };
+  for (int64_t c0 = 0; c0 < n_sel; c0 += mc) {
+    const int64_t rows = std::min(mc, n_sel - c0), mcp = round_up(rows, 256);
+    const int tiles_r = static_cast<int>(mcp / 256), panel = row_panel(tiles_r, d), halved = halved_tiles(tiles_v, tiles_r);
+    uint16_t* const E = reinterpret_cast<uint16_t*>(chunk);
+    uint16_t* const Hs = no_dw ? nullptr : reinterpret_cast<uint16_t*>(chunk + align_up(static_cast<size_t>(mcp) * Vp * 2));
+    DhSlices sl;
+    const bool dw_apart = plan(rows, &sl);
+    const LiveArgs live = live_args(c0, rows, sl.n, dw_apart);
+    if (c0 == 0) {
+      const OpenArgs O{A, H, W, w.R, w.flags, static_cast<int>(cdiv(n_sel, 256)), live, a.rowsel ? static_cast<uint32_t*>(a.dH) : nullptr,
+                       a.n_rows * static_cast<int64_t>(d) / 2, a.row_out, a.row_out ? a.n_rows : 0};
+      hipLaunchKernelGGL(k_target_open, dim3(1 + std::min<unsigned>(std::max<unsigned>(cdiv(n_sel, 4), a.rowsel ? 1024 : 1), 8192)), dim3(256), 0, st, O);
+      UMAS_LAUNCHED("k_target_open");
+    } else {
+      hipLaunchKernelGGL(k_live_scan, dim3(1), dim3(512), 0, st, live);
+      UMAS_LAUNCHED("k_live_scan");
+    }
+    const bool narrow = n_sel <= NarrowCfg::BN;
+    const int64_t n_pad = round_up(n_sel, narrow ? NarrowCfg::BN : Cfg::BN);
+    const int tiles_m = narrow ? static_cast<int>(Vp / NarrowCfg::BM) : tiles_v;
+    if (narrow)
+      hipLaunchKernelGGL(k_target_narrow, dim3(tile_grid<kGM, kGN>(tiles_m, 1, kGN, kTilesPerWg)), dim3(NarrowCfg::T), 0, st, W, H, d, V, a.rowsel, rows,
+                         tiles_m, w.partial, n_pad, w.R.cref, E, Vp, w.flags, w.blk_cidx);
+    else
+      hipLaunchKernelGGL(k_target_tiles, score_grid(tiles_v, tiles_r, panel, halved), dim3(Cfg::T), 0, st, W, H, d, V, a.rowsel, c0, rows, tiles_v, tiles_r,
+                         panel, halved, w.partial, n_pad, w.R.cref, E, Vp, w.flags, w.blk_cidx);
+    UMAS_LAUNCHED(narrow ? "k_target_narrow" : "k_target_tiles");
+    hipLaunchKernelGGL(k_target_rows, dim3(cdiv(rows, 8)), dim3(256), 0, st,
+                       RowsArgs{A, H, w.R, w.partial, tiles_m, n_pad, c0, rows, w.flags, w.blk_cidx, E, tiles_v, Hs, mcp, a.row_out});
+    UMAS_LAUNCHED("k_target_rows");
+    const PutTargets put{a.rowsel, a.t.ids, a.t.k, w.R.zt, w.R.tt, w.R.lse, w.R.a, w.R.w, A.norm};
+    hipLaunchKernelGGL(k_target_flagged, dim3(kFlaggedGrid), dim3(Cfg::T), 0, st, W, H, d, V, a.rowsel, c0, rows, w.R.zero, put, tiles_v, tiles_r, E, Vp,
+                       w.flags, w.blk_cidx);
+    UMAS_LAUNCHED("k_target_flagged");
+    const int add = c0 > 0 || (a.accumulate_dW && !sums) ? 1 : 0;
+    const GradientArgs G{E, Vp, mcp, W, Hs, d, V, tiles_v, tiles_d, sl, tiles_r, w.live, w.blk_orig, static_cast<uint16_t*>(a.dH), add, a.rowsel, c0, rows, w.R.sc};
+    const unsigned grid = static_cast<unsigned>(round_up(device_cus(), 8));
+    if (sums || a.dW_type == UMAS_F32) hipLaunchKernelGGL(k_target_gemm, dim3(grid), dim3(Cfg::T), 0, st, G, sums ? sums : static_cast<float*>(a.dW));
+    else hipLaunchKernelGGL(k_target_gemm_bf16, dim3(grid), dim3(Cfg::T), 0, st, G, static_cast<uint16_t*>(a.dW));
+    UMAS_LAUNCHED("k_target_gemm");
+    if (dw_apart) {
+      const int tiles_n = (d + ShortCfg::BN - 1) / ShortCfg::BN;
+      const dim3 g2(static_cast<unsigned>(round_up(static_cast<int64_t>(tiles_v) * tiles_n, 8)));
+      if (sums || a.dW_type == UMAS_F32) hipLaunchKernelGGL(k_target_dw_short, g2, dim3(ShortCfg::T), 0, st, G, tiles_n, sums ? sums : static_cast<float*>(a.dW));
+      else hipLaunchKernelGGL(k_target_dw_short_bf16, g2, dim3(ShortCfg::T), 0, st, G, tiles_n, static_cast<uint16_t*>(a.dW));
+      UMAS_LAUNCHED("k_target_dw_short");
+    }
+    CloseArgs C{};
+    if (c0 + rows >= n_sel) {
+      C.stats = stat_args(a, w, A.norm);
+      C.n_stats = 1 + a.n_roles;
+    }
+    unsigned wgs = C.n_stats;
+    if (sl.n > 1) {
+      C.reduce_rows = static_cast<unsigned>(mcp);
+      C.sl = sl;
+      C.tiles_r = tiles_r;
+      C.tiles_d = tiles_d;
+      C.d = d;
+      C.info = w.live;
+      C.blk_orig = w.blk_orig;
+      C.dH = static_cast<uint16_t*>(a.dH);
+      C.rowsel = a.rowsel;
+      C.c0 = c0;
+      C.rows = rows;
+      C.sc = w.R.sc;
+      wgs += C.reduce_rows * cdiv(d, 1024);
+    }
+    if (wgs) {
+      hipLaunchKernelGGL(k_target_close, dim3(wgs), dim3(kCloseT), 0, st, C);
+      UMAS_LAUNCHED("k_target_close");
+    }
+  }
+  if (sums) {
+    const int64_t n8 = static_cast<int64_t>(V) * d / 8;
+    hipLaunchKernelGGL(k_target_round, dim3(static_cast<unsigned>(std::min<int64_t>((n8 + 255) / 256, 8192))), dim3(256), 0, st, sums,
+                       static_cast<uint16_t*>(a.dW), n8, a.accumulate_dW ? 1 : 0);
+    UMAS_LAUNCHED("k_target_round");
+  }
+  return UMAS_OK;
+}
+
+umas_status run(const Call& a) {
+  umas_status s = check_call(a);
+  if (s != UMAS_OK) return s;
+  hipStream_t st = a.st;
+  prof_mark(st);
+  Carver c(a.workspace);
+  Ws w;
+  carve(c, w, a.n_sel, a.d, a.V, a.t.k, a.dt);
+  const float norm = static_cast<float>(a.norm_rows > 0 ? a.norm_rows : a.n_sel > 0 ? a.n_sel : 1);
+  const Teach A{a.t, a.rowsel, a.n_sel, a.V, a.d, a.weight, norm, a.z_coef};
+  if (a.n_sel == 0) {
+    const size_t esz = a.dt == UMAS_BF16 ? 2 : 4, dw = static_cast<size_t>(a.V) * a.d * (a.dW_type == UMAS_BF16 ? 2 : 4);
+    UMAS_HIP(clear_bytes(st, a.n_rows > 0 ? a.dH : nullptr, static_cast<size_t>(a.n_rows) * a.d * esz, a.row_out, static_cast<size_t>(a.n_rows) * 4,
+                         a.accumulate_dW ? nullptr : a.dW, dw));
+    CloseArgs C{};
+    C.stats = stat_args(a, w, norm);
+    C.n_stats = 1 + a.n_roles;
+    hipLaunchKernelGGL(k_target_close, dim3(C.n_stats), dim3(kCloseT), 0, st, C);
+    UMAS_LAUNCHED("k_target_close");
+    return UMAS_OK;
+  }
+  return a.dt == UMAS_F32 ? run_f32(a, w, A) : run_bf16(a, w, A);
+}
+
+}  // namespace
+}  // namespace umas
+
+using namespace umas;
+
+extern "C" size_t umas_cross_entropy_workspace_bytes_min(int64_t n_sel, int32_t d, int32_t V, umas_dtype dtype, int32_t dW_type) {
+  return least_bytes(n_sel, d, V, 1, dtype, dW_type);
+}
+extern "C" size_t umas_cross_entropy_workspace_bytes(int64_t n_sel, int32_t d, int32_t V, umas_dtype dtype, int32_t dW_type) {
+  return full_bytes(n_sel, d, V, 1, dtype, dW_type);
+}
+extern "C" size_t umas_distill_workspace_bytes_min(int64_t n_sel, int32_t d, int32_t V, int32_t k, umas_dtype dtype, int32_t dW_type) {
+  return least_bytes(n_sel, d, V, k, dtype, dW_type);
+}
+extern "C" size_t umas_distill_workspace_bytes(int64_t n_sel, int32_t d, int32_t V, int32_t k, umas_dtype dtype, int32_t dW_type) {
+  return full_bytes(n_sel, d, V, k, dtype, dW_type);
+}
+
+extern "C" umas_status umas_cross_entropy_fwd_bwd(const void* H, const void* W, umas_dtype dtype, int64_t n_rows, int32_t d, int32_t V, const int32_t* ids,
+                                                  const int32_t* rowsel, int64_t n_sel, const float* weight, const int32_t* tok_role, int32_t n_roles,
+                                                  float z_coef, int32_t accumulate_dW, int64_t norm_rows, umas_target_stats* stats, float* logp, void* dH,
+                                                  void* dW, int32_t dW_type, void* workspace, size_t workspace_bytes, void* hip_stream) {
+  return run(Call{H, W, dtype, n_rows, d, V, Targets{ids, nullptr, nullptr, 1}, rowsel, n_sel, weight, tok_role, n_roles, z_coef,
+                  accumulate_dW, norm_rows, stats, logp, dH, dW, dW_type, workspace, workspace_bytes, static_cast<hipStream_t>(hip_stream)});
+}
+
+extern "C" umas_status umas_distill_fwd_bwd(const void* H, const void* W, umas_dtype dtype, int64_t n_rows, int32_t d, int32_t V, const int32_t* top_ids,
+                                            const float* top_logits, int32_t k, const float* teacher_lse, const int32_t* rowsel, int64_t n_sel,
+                                            const float* weight, const int32_t* tok_role, int32_t n_roles, int32_t accumulate_dW, int64_t norm_rows,
+                                            umas_target_stats* stats, float* kl, void* dH, void* dW, int32_t dW_type, void* workspace,
+                                            size_t workspace_bytes, void* hip_stream) {
+  UMAS_REQUIRE(top_logits || n_rows == 0, UMAS_EINVAL, "top_logits must not be NULL");
+  static const float none = 0.f;           // no rows: anything but NULL, which stands for cross entropy
+  return run(Call{H, W, dtype, n_rows, d, V, Targets{top_ids, top_logits ? top_logits : &none, teacher_lse, k}, rowsel, n_sel, weight,
+                  tok_role, n_roles, 0.f, accumulate_dW, norm_rows, stats, kl, dH, dW, dW_type, workspace, workspace_bytes,
+                  static_cast<hipStream_t>(hip_stream)});
+}

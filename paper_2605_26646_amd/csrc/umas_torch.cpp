@@ -103,6 +103,26 @@ struct Selection {                                        // None: all rows; an 
   void point(void* otherwise, PyObject* o) { if (o != Py_None && !p) p = static_cast<const int32_t*>(otherwise); }
 };
 
+// The calls that list logits and teach targets read and write [n, k] arrays: types, shapes and layout are looked at here, where a wrong one would be read
+// out of bounds.
+void same_head(const Rows& H, const at::Tensor& W) {
+  if (W.dim() == 2 && W.size(1) == H.d && W.scalar_type() == H.t.scalar_type() && H.t.is_contiguous() && W.is_contiguous()) return;
+  PyErr_SetString(PyExc_ValueError, "H [n, d] and W [V, d] must be contiguous and of one type and width");
+  throw Failed();
+}
+const at::Tensor& targets(PyObject* o, at::ScalarType type, int64_t n, int64_t k, const char* name) {
+  const at::Tensor& t = tensor(o);
+  if (t.scalar_type() != type) {
+    PyErr_Format(PyExc_TypeError, "%s must be %s", name, type == at::kInt ? "int32" : "float32");
+    throw Failed();
+  }
+  if (t.numel() != n * k || t.dim() == 0 || t.size(0) != n || !t.is_contiguous()) {
+    PyErr_Format(PyExc_ValueError, "%s must be contiguous and hold %lld values for each of the %lld rows of H", name, static_cast<long long>(k), static_cast<long long>(n));
+    throw Failed();
+  }
+  return t;
+}
+
 PyObject* ascontiguousarray = nullptr;                    // numpy's
 // A host array of the ABI's type: the object's own memory where it has that type, is contiguous and lies at a multiple of the type's
 // size, else numpy's copy.
@@ -370,6 +390,104 @@ PyObject* ppo_loss(PyObject* const* a) {
   return pack({stats.object(), logp_new.object(), dH.object(), dW.object()});
 }
 
+PyObject* top_logits(PyObject* const* a) {                // H, W, k, rowsel, ids, logits, lse, workspace, stream
+  const Rows H(a[0]);
+  const at::Tensor& W = tensor(a[1]);
+  const int32_t V = static_cast<int32_t>(W.size(0)), k = integer32(a[2]);
+  Selection sel(a[3], H.n);
+  const at::Device dev = H.t.device();
+  const umas_dtype dt = static_cast<umas_dtype>(H.dt);
+  const int64_t places = std::max(k, 0);
+  const Output ids(a[4], [&] { return fresh({H.n, places}, at::kInt, dev); });
+  const Output logits(a[5], [&] { return fresh({H.n, places}, at::kFloat, dev); });
+  const Output lse(a[6], [&] { return fresh({H.n}, at::kFloat, dev); });
+  const Output ws(a[7], [&] { return workspace(umas_top_logits_workspace_bytes(sel.n, H.d, V, k, dt), dev); });
+  sel.point(ws.t.data_ptr(), a[3]);
+  void* const st = stream_of(a[8]);
+  same_head(H, W);
+  UMAS_CALL(umas_top_logits(H.t.data_ptr(), W.data_ptr(), dt, H.n, H.d, V, sel.p, sel.n, k, ptr<int32_t>(ids.t), ptr<float>(logits.t), ptr<float>(lse.t),
+                            ws.t.data_ptr(), ws.t.numel(), st));
+  return pack({ids.object(), logits.object(), lse.object()});
+}
+
+// What cross entropy and distillation have in common; `o` from weight on: weight, tok_role, n_roles, train_head, accumulate_dW, norm_rows, dW, dH, row_out,
+// stats, workspace, stream.
+struct Taught {
+  const Rows H;
+  const at::Tensor& W;
+  const int32_t V;
+  Selection sel;
+  const at::Device dev;
+  const umas_dtype dt;
+  const float* weight;
+  const int32_t *role, n_roles;
+  const bool head;
+  const int32_t accumulate;
+  const int64_t norm_rows;
+  at::Tensor dW;
+  PyObject* dW_given;
+  const Output dH, row_out, stats;
+  int32_t dW_type;
+  void* const st;
+  Taught(PyObject* h, PyObject* w, PyObject* rowsel, PyObject* const* o)
+      : H(h), W(tensor(w)), V(static_cast<int32_t>(W.size(0))), sel(rowsel, H.n), dev(H.t.device()), dt(static_cast<umas_dtype>(H.dt)),
+        weight(ptr_or_null<const float>(o[0])), role(ptr_or_null<const int32_t>(o[1])), n_roles(integer32(o[2])), head(truth(o[3])), accumulate(truth(o[4])),
+        norm_rows(as_int(o[5])), dW_given(o[6] == Py_None ? nullptr : o[6]), dH(o[7], [&] { return at::empty_like(H.t); }),
+        row_out(o[8], [&] { return fresh({H.n}, at::kFloat, dev); }),
+        stats(o[9], [&] { return fresh({(1 + static_cast<int64_t>(std::max(n_roles, 0))) * static_cast<int64_t>(sizeof(umas_target_stats))}, at::kByte, dev); }),
+        dW_type(UMAS_NO_DW), st(stream_of(o[11])) {
+    same_head(H, W);
+    if (!head) return;
+    dW = dW_given ? tensor(dW_given) : at::empty_like(W);
+    if (dW.scalar_type() != at::kFloat && dW.scalar_type() != W.scalar_type()) {
+      PyErr_SetString(PyExc_TypeError, "dW must be float32 or of the type of W");
+      throw Failed();
+    }
+    if (dW.numel() != W.numel() || !dW.is_contiguous()) {
+      PyErr_SetString(PyExc_ValueError, "dW must be contiguous and of the shape of W");
+      throw Failed();
+    }
+    dW_type = dW.scalar_type() == at::kFloat ? UMAS_F32 : UMAS_BF16;
+  }
+  PyObject* results() const {
+    PyObject* w = Py_None;
+    if (head && !dW_given) w = wrap(dW);
+    else {
+      if (head) w = dW_given;
+      Py_INCREF(w);
+    }
+    return pack({stats.object(), row_out.object(), dH.object(), w});
+  }
+};
+
+PyObject* cross_entropy(PyObject* const* a) {
+  // H, W, ids, rowsel, z_coef, weight, tok_role, n_roles, train_head, accumulate_dW, norm_rows, dW, dH, logp, stats, workspace, stream
+  Taught T(a[0], a[1], a[3], a + 5);
+  const at::Tensor& ids = targets(a[2], at::kInt, T.H.n, 1, "ids");
+  const float z_coef = real(a[4]);
+  const Output ws(a[15], [&] { return workspace(umas_cross_entropy_workspace_bytes(T.sel.n, T.H.d, T.V, T.dt, T.dW_type), T.dev); });
+  T.sel.point(ws.t.data_ptr(), a[3]);
+  UMAS_CALL(umas_cross_entropy_fwd_bwd(T.H.t.data_ptr(), T.W.data_ptr(), T.dt, T.H.n, T.H.d, T.V, ptr<int32_t>(ids), T.sel.p, T.sel.n, T.weight, T.role,
+                                       T.n_roles, z_coef, T.accumulate, T.norm_rows, ptr<umas_target_stats>(T.stats.t), ptr<float>(T.row_out.t),
+                                       T.dH.t.data_ptr(), T.head ? T.dW.data_ptr() : nullptr, T.dW_type, ws.t.data_ptr(), ws.t.numel(), T.st));
+  return T.results();
+}
+
+PyObject* distill(PyObject* const* a) {
+  // H, W, top_ids, top_logits, teacher_lse, rowsel, weight, tok_role, n_roles, train_head, accumulate_dW, norm_rows, dW, dH, kl, stats, workspace, stream
+  Taught T(a[0], a[1], a[5], a + 6);
+  const int64_t k = tensor(a[2]).dim() == 2 ? tensor(a[2]).size(1) : 0;
+  const at::Tensor &ids = targets(a[2], at::kInt, T.H.n, k, "top_ids"), &logits = targets(a[3], at::kFloat, T.H.n, k, "top_logits");
+  const float* const lse = a[4] == Py_None ? nullptr : ptr<const float>(targets(a[4], at::kFloat, T.H.n, 1, "teacher_lse"));
+  const int32_t places = static_cast<int32_t>(std::min<int64_t>(k, 1 << 30));
+  const Output ws(a[16], [&] { return workspace(umas_distill_workspace_bytes(T.sel.n, T.H.d, T.V, places, T.dt, T.dW_type), T.dev); });
+  T.sel.point(ws.t.data_ptr(), a[5]);
+  UMAS_CALL(umas_distill_fwd_bwd(T.H.t.data_ptr(), T.W.data_ptr(), T.dt, T.H.n, T.H.d, T.V, ptr<int32_t>(ids), ptr<float>(logits), places, lse, T.sel.p,
+                                 T.sel.n, T.weight, T.role, T.n_roles, T.accumulate, T.norm_rows, ptr<umas_target_stats>(T.stats.t), ptr<float>(T.row_out.t),
+                                 T.dH.t.data_ptr(), T.head ? T.dW.data_ptr() : nullptr, T.dW_type, ws.t.data_ptr(), ws.t.numel(), T.st));
+  return T.results();
+}
+
 PyObject* values(PyObject* const* a) {                    // H, w, bias, rowsel, value, stream
   const Rows H(a[0]);
   const at::Tensor& w = tensor(a[1]);
@@ -492,7 +610,8 @@ PyObject* entry(PyObject*, PyObject* const* args, Py_ssize_t n) {
 }
 #define ENTRY(name, f, n) {name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)(void)>(&entry<f, n>)), METH_FASTCALL, nullptr}
 PyMethodDef g_methods[] = {ENTRY("assign", assign, 19), ENTRY("advantages", advantages, 7), ENTRY("policy_logprobs", policy_logprobs, 7),
-                           ENTRY("policy_logprobs_static", policy_logprobs_static, 8), ENTRY("ppo_loss", ppo_loss, 21), ENTRY("values", values, 6),
+                           ENTRY("policy_logprobs_static", policy_logprobs_static, 8), ENTRY("ppo_loss", ppo_loss, 21), ENTRY("top_logits", top_logits, 9),
+                           ENTRY("cross_entropy", cross_entropy, 17), ENTRY("distill", distill, 18), ENTRY("values", values, 6),
                            ENTRY("value_loss", value_loss, 19), ENTRY("kl_rewards", kl_rewards, 7), ENTRY("whiten", whiten, 9),
                            ENTRY("ready_batch", ready_batch, 7), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef g_module = {PyModuleDef_HEAD_INIT, "_umas_torch", nullptr, -1, g_methods, nullptr, nullptr, nullptr, nullptr};
