@@ -1,7 +1,12 @@
 // The k largest logits of a head and its logsumexp, for selected rows.
 //
+// The logits of a row fall into groups, those that one lane of the product holds (32 of a tile of 256 x 256, 16 of a small one, a place of every block of 16 in
+// a workgroup's part of the vocabulary with few rows).  The product leaves the groups' maxima, the tiles' sums of exponentials and the logits themselves,
+// group by group.  Who is among the k largest lies in a group whose maximum is among the k largest maxima, so a row's selection reads the maxima,
+// takes a bound that at least k of them reach, and then only the groups that reach it: k of thousands, give or take a few, whatever the logits are.
+//
 // A logit and its token make one 64-bit key whose order is that of the result: the logit's bits, turned so that they order as whole numbers, above the
-// complement of the token.  A wavefront keeps the 64 largest keys it has seen, one to a lane in falling order, and looks only at logits that reach its
+// complement of the token.  A wavefront keeps the 64 largest keys it has seen, one to a lane in falling order, and takes only keys beyond its
 // k-th: those collect in LDS until there are 64, are sorted (21 exchanges) and merged with what is there (7).
 #include "umas_f32.h"
 #include "umas_logits.h"
@@ -44,30 +49,32 @@ __device__ __forceinline__ TopKey merged(TopKey x, TopKey y) {
 }
 struct WaveTop {
   TopKey list = 0;
-  float least = -INFINITY;                                   // logits below it are not among the k largest
+  TopKey least = 0;                                          // keys up to it are not among the k largest (known from outside, or of the list)
   int waiting = 0;
-  TopKey* buf;                                                // [128] in LDS, this wavefront's
+  TopKey* buf;                                               // [128] in LDS, this wavefront's
   int k;
   __device__ __forceinline__ void take(TopKey x) {
     list = merged(list, sorted_desc(x));
-    least = logit_of(__shfl(list, k - 1, kWave));
+    const TopKey kth = __shfl(list, k - 1, kWave);
+    least = least > kth ? least : kth;
   }
   // one logit a lane
   __device__ __forceinline__ void offer(float z, int id, bool have) {
-    const bool in = have && z >= least && z > -INFINITY;
+    const TopKey x = have && z > -INFINITY ? key_of(z, id) : 0;
+    const bool in = x > least;
     const unsigned long long m = __ballot(in);
     if (!m) return;
     const int lane = threadIdx.x & 63;
-    if (in) buf[waiting + __popcll(m & ((1ull << lane) - 1))] = key_of(z, id);
+    if (in) buf[waiting + __popcll(m & ((1ull << lane) - 1))] = x;
     waiting += __popcll(m);
     __builtin_amdgcn_wave_barrier();
     if (waiting < kWave) return;
-    const TopKey x = buf[lane], rest = buf[kWave + lane];
+    const TopKey y = buf[lane], rest = buf[kWave + lane];
     __builtin_amdgcn_wave_barrier();
     waiting -= kWave;
     if (lane < waiting) buf[lane] = rest;
     __builtin_amdgcn_wave_barrier();
-    take(x);
+    take(y);
   }
   __device__ __forceinline__ void finish() {
     if (!waiting) return;
@@ -89,21 +96,33 @@ __device__ __forceinline__ TopKey merge_waves(TopKey list, TopKey (*s_list)[kWav
   return list;
 }
 
-// ------------------------------------------------------------------ bf16: logit tiles that are kept, with (max, sum exp) of their rows
+// ------------------------------------------------------------------ bf16: logits in groups
+// What a product leaves of its rows: per row and tile (of the vocabulary) G group maxima and a sum of exponentials relative to the largest of them, and the
+// logits.  Entries that do not exist hold kMasked.
+struct Groups {
+  float* max;              // [rows][tiles][G]
+  float* sum;              // [rows][tiles]
+  float* z;                // [rows][tiles][G][E], of the kernel for few rows [rows][tiles][E][G]
+  int tiles;
+};
+constexpr int kGroups = 8;                                   // of a tile: four lane groups, two wavefronts along the vocabulary
 template <class C>
+constexpr int kEntries = C::MI * 4;
+template <class C, bool ALL>
 __device__ __forceinline__ void top_tile(const uint16_t* __restrict__ W, const uint16_t* __restrict__ H, int d, int V, const int32_t* __restrict__ rowsel,
-                                         int64_t c0, int64_t mc, int tile_m, int tile_n, bool w_once, float2* __restrict__ partial, int64_t n_pad,
-                                         float* __restrict__ Z, int64_t tiles_v, uint16_t* lds) {
-  constexpr int kPitch = C::WTM * 4 + 16;                    // a staged row of logits
-  constexpr int kStage = 16 * kPitch;                        // sixteen of them, a wavefront's
-  static_assert(C::WM * C::WN * kStage + C::WM * C::BN * 8 <= Ring2Cfg<C>::LDS_BYTES, "staging and the partials fit the tile buffers");
+                                         int64_t c0, int64_t mc, int tile_m, int tile_n, bool w_once, const Groups& out, const float* __restrict__ bound,
+                                         uint16_t* lds) {
+  // a wavefront's part of LDS for sixteen rows on their way out: rows of its half of the tile, 16 bytes more to a group and to a row (banks)
+  constexpr int kGroupPitch = kEntries<C> * 4 + 16, kRowPitch = 4 * kGroupPitch + 16, kStage = 16 * kRowPitch;
+  static_assert(C::WM == 2 && C::BN * (kGroups + 2) * 4 + C::WM * C::WN * kStage <= Ring2Cfg<C>::LDS_BYTES, "maxima, sums and stages fit the tile buffers");
   const int m0 = tile_m * C::BM;
   const int64_t n0 = static_cast<int64_t>(tile_n) * C::BN;
   floatx4 acc[C::MI][C::NI];
   logit_tile<C>(W, H, d, V, rowsel, c0, mc, m0, n0, w_once, lds, acc);
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, wm = wave / C::WN, wn = wave % C::WN;
-  char* const stage = reinterpret_cast<char*>(lds) + wave * kStage;
-  float2* const s_part = reinterpret_cast<float2*>(reinterpret_cast<char*>(lds) + C::WM * C::WN * kStage);
+  float* const s_max = reinterpret_cast<float*>(lds);        // [BN][8]
+  float* const s_sum = s_max + C::BN * kGroups;              // [2][BN]
+  char* const stage = reinterpret_cast<char*>(s_sum + 2 * C::BN) + wave * kStage;
   __syncthreads();
   const int vbase = m0 + wm * C::WTM + (lane >> 4) * 4;
   if (m0 + C::BM > V) {
@@ -115,95 +134,372 @@ __device__ __forceinline__ void top_tile(const uint16_t* __restrict__ W, const u
         for (int r = 0; r < 4; ++r)
           if (vbase + i * 16 + r >= V) acc[i][j][r] = kMasked;
   }
+  constexpr float kLog2e = 1.44269504088896341f;
+  const int group = wm * 4 + (lane >> 4);
 #pragma unroll
   for (int j = 0; j < C::NI; ++j) {
     const int col = wn * C::WTN + j * 16 + (lane & 15);
-    float m = kMasked, s = 0.f;
+    float m = acc[0][j][0];
 #pragma unroll
     for (int i = 0; i < C::MI; ++i)
 #pragma unroll
       for (int r = 0; r < 4; ++r) m = fmaxf(m, acc[i][j][r]);
+    float most = fmaxf(m, kMasked);                          // of the column's four lanes
+    most = fmaxf(most, __shfl_xor(most, 16, kWave));
+    most = fmaxf(most, __shfl_xor(most, 32, kWave));
+    float s = 0.f;
 #pragma unroll
     for (int i = 0; i < C::MI; ++i)
 #pragma unroll
-      for (int r = 0; r < 4; ++r) s += __builtin_amdgcn_exp2f((acc[i][j][r] - m) * 1.44269504088896341f);
+      for (int r = 0; r < 4; ++r) s += __builtin_amdgcn_exp2f((acc[i][j][r] - most) * kLog2e);
+    s += __shfl_xor(s, 16, kWave);
+    s += __shfl_xor(s, 32, kWave);
+    s_max[col * kGroups + group] = m;
+    if (lane < 16) s_sum[wm * C::BN + col] = s;
+    if constexpr (!ALL) {                                    // only groups that reach a bound that k logits are known to reach
+      if (n0 + col < mc && m >= bound[n0 + col]) {
+        floatx4* const z = reinterpret_cast<floatx4*>(out.z + (((n0 + col) * out.tiles + tile_m) * kGroups + group) * kEntries<C>);
 #pragma unroll
-    for (int o = 16; o < kWave; o <<= 1) {
-      const float m2 = __shfl_xor(m, o, kWave), s2 = __shfl_xor(s, o, kWave), M = fmaxf(m, m2);
-      s = s * __expf(m - M) + s2 * __expf(m2 - M);
-      m = M;
+        for (int i = 0; i < C::MI; ++i) z[i] = acc[i][j];
+      }
+    } else {
+      char* const mine = stage + (lane & 15) * kRowPitch + (lane >> 4) * kGroupPitch;
+#pragma unroll
+      for (int i = 0; i < C::MI; ++i) *reinterpret_cast<floatx4*>(mine + i * 16) = acc[i][j];
+      __builtin_amdgcn_wave_barrier();
+      constexpr int kLanes = C::WTM / 4, kRows = kWave / kLanes, kPerGroup = kLanes / 4;   // lanes to a row, rows to a store, lanes to a group
+      const int64_t r0 = n0 + wn * C::WTN + j * 16 + lane / kLanes;
+      const int q = lane % kLanes;
+#pragma unroll
+      for (int i = 0; i < 16 / kRows; ++i)
+        if (r0 + i * kRows < mc)
+          *reinterpret_cast<floatx4*>(out.z + (((r0 + i * kRows) * out.tiles + tile_m) * kGroups + wm * 4) * kEntries<C> + q * 4) =
+              *reinterpret_cast<const floatx4*>(stage + (i * kRows + lane / kLanes) * kRowPitch + q / kPerGroup * kGroupPitch + q % kPerGroup * 16);
+      __builtin_amdgcn_wave_barrier();
     }
-    if (lane < 16) s_part[wm * C::BN + col] = make_float2(m, s);
-    // sixteen rows through the wavefront's part of LDS: a store covers whole lines
-#pragma unroll
-    for (int i = 0; i < C::MI; ++i) *reinterpret_cast<floatx4*>(stage + (lane & 15) * kPitch + (i * 16 + (lane >> 4) * 4) * 4) = acc[i][j];
-    __builtin_amdgcn_wave_barrier();
-    constexpr int kLanes = C::WTM / 4, kRows = kWave / kLanes;
-    const int64_t r0 = n0 + wn * C::WTN + j * 16 + lane / kLanes;
-    float* const out = Z + ((r0 >> 8) * tiles_v + (m0 >> 8)) * kBlkElems + (r0 & 255) * 256 + (m0 & 255) + wm * C::WTM + lane % kLanes * 4;
-#pragma unroll
-    for (int q = 0; q < 16 / kRows; ++q)
-      if (r0 + q * kRows < mc) *reinterpret_cast<floatx4*>(out + q * kRows * 256) = *reinterpret_cast<const floatx4*>(stage + (q * kRows + lane / kLanes) * kPitch + lane % kLanes * 16);
-    __builtin_amdgcn_wave_barrier();
   }
   __syncthreads();
-  if (threadIdx.x < C::BN) {
-    float2 p = s_part[threadIdx.x];
-#pragma unroll
-    for (int w = 1; w < C::WM; ++w) {
-      const float2 q = s_part[w * C::BN + threadIdx.x];
-      const float M = fmaxf(p.x, q.x);
-      p = make_float2(M, p.y * __expf(p.x - M) + q.y * __expf(q.x - M));
-    }
-    partial[static_cast<int64_t>(tile_m) * n_pad + n0 + threadIdx.x] = p;
+  if (threadIdx.x < C::BN && n0 + threadIdx.x < mc) {
+    const int col = threadIdx.x;
+    const floatx4 a = reinterpret_cast<const floatx4*>(s_max)[col * 2], b = reinterpret_cast<const floatx4*>(s_max)[col * 2 + 1];
+    const float ma = fmaxf(fmaxf(fmaxf(a[0], a[1]), fmaxf(a[2], a[3])), kMasked), mb = fmaxf(fmaxf(fmaxf(b[0], b[1]), fmaxf(b[2], b[3])), kMasked);
+    const float m = fmaxf(ma, mb);
+    const int64_t at = (n0 + col) * out.tiles + tile_m;
+    reinterpret_cast<floatx4*>(out.max)[at * 2] = a;
+    reinterpret_cast<floatx4*>(out.max)[at * 2 + 1] = b;
+    out.sum[at] = s_sum[col] * __expf(ma - m) + s_sum[C::BN + col] * __expf(mb - m);
   }
   __syncthreads();
 }
-template <class C>
+template <class C, bool ALL>
 __device__ __forceinline__ void top_tiles(const uint16_t* __restrict__ W, const uint16_t* __restrict__ H, int d, int V, const int32_t* __restrict__ rowsel,
-                                          int64_t c0, int64_t mc, int tiles_m, int tiles_n, int panel, float2* __restrict__ partial, int64_t n_pad,
-                                          float* __restrict__ Z, int64_t tiles_v, uint16_t* lds) {
+                                          int64_t c0, int64_t mc, int first, int tiles_m, int tiles_n, int panel, const Groups& out,
+                                          const float* __restrict__ bound, uint16_t* lds) {
   const bool w_once = tiles_n == 1 && beyond_cache(d, V, kLogitsOnceBytes);
   for (int it = 0; it < kTilesPerWg; ++it) {
     int tile_m, tile_n;
     if (!tile_coords<kGM, kGN>(tiles_m, tiles_n, panel, &tile_m, &tile_n, it, kTilesPerWg)) continue;
-    top_tile<C>(W, H, d, V, rowsel, c0, mc, tile_m, tile_n, w_once, partial, n_pad, Z, tiles_v, lds);
+    top_tile<C, ALL>(W, H, d, V, rowsel, c0, mc, first + tile_m, tile_n, w_once, out, bound, lds);
   }
 }
 __global__ void __launch_bounds__(Cfg::T)
 k_top_tiles(const uint16_t* __restrict__ W, const uint16_t* __restrict__ H, int d, int V, const int32_t* __restrict__ rowsel, int64_t c0, int64_t mc,
-            int tiles_m, int tiles_n, int panel, float2* __restrict__ partial, int64_t n_pad, float* __restrict__ Z, int64_t tiles_v) {
+            int tiles_m, int tiles_n, int panel, Groups out) {
   __shared__ __attribute__((aligned(16))) uint16_t lds[kLogitLds / 2];
-  top_tiles<Cfg>(W, H, d, V, rowsel, c0, mc, tiles_m, tiles_n, panel, partial, n_pad, Z, tiles_v, lds);
+  top_tiles<Cfg, true>(W, H, d, V, rowsel, c0, mc, 0, tiles_m, tiles_n, panel, out, nullptr, lds);
+}
+__global__ void __launch_bounds__(Cfg::T)
+k_top_tiles_bound(const uint16_t* __restrict__ W, const uint16_t* __restrict__ H, int d, int V, const int32_t* __restrict__ rowsel, int64_t c0, int64_t mc,
+                  int first, int tiles_m, int tiles_n, int panel, Groups out, const float* __restrict__ bound) {
+  __shared__ __attribute__((aligned(16))) uint16_t lds[kLogitLds / 2];
+  top_tiles<Cfg, false>(W, H, d, V, rowsel, c0, mc, first, tiles_m, tiles_n, panel, out, bound, lds);
 }
 __global__ void __launch_bounds__(NarrowCfg::T)
-k_top_narrow(const uint16_t* __restrict__ W, const uint16_t* __restrict__ H, int d, int V, const int32_t* __restrict__ rowsel, int64_t c0, int64_t mc,
-             int tiles_m, float2* __restrict__ partial, int64_t n_pad, float* __restrict__ Z, int64_t tiles_v) {
+k_top_narrow(const uint16_t* __restrict__ W, const uint16_t* __restrict__ H, int d, int V, const int32_t* __restrict__ rowsel, int64_t c0, int64_t mc, Groups out) {
   __shared__ __attribute__((aligned(16))) uint16_t lds[kNarrowLds / 2];
-  top_tiles<NarrowCfg>(W, H, d, V, rowsel, c0, mc, tiles_m, 1, kGN, partial, n_pad, Z, tiles_v, lds);
+  top_tiles<NarrowCfg, true>(W, H, d, V, rowsel, c0, mc, 0, out.tiles, 1, kGN, out, nullptr, lds);
+}
+
+// A few rows: W streams past rows that stay in registers (the loop and what bounds it: k_score_few).  A thread has one place of every block of 16 entries of its
+// workgroup's part of the vocabulary: its group.  The logits are summed over the wavefronts in a fixed order; they collect in LDS, 64 KB of them, and leave
+// together: memory operations are counted in order, and a store in every step has the loads of W behind it wait for it (one row of 2048 129 us in place
+// of 110, 24 rows of 3584 247 in place of 199).
+constexpr int kFewGroups = 16, kFewMostTiles = 512;
+template <int NI, int PPW>
+__global__ void __launch_bounds__(kFewT)
+k_top_few(const uint16_t* __restrict__ W, const uint16_t* __restrict__ H, int d, int V, const int32_t* __restrict__ rowsel, int n_sel, int per, Groups out) {
+  constexpr int MB = PPW <= 4 && NI <= 2 ? 2 : 1;            // blocks of 16 vocabulary entries per step
+  constexpr int NL = (NI + 1) / 2;                           // logits per thread and block
+  constexpr int kHold = 64 / NI, kHoldPitch = kHold * 16 + 16;   // blocks that collect, floats of a row of them (16 more: banks)
+  __shared__ __attribute__((aligned(16))) float s_z[2][kFewWaves][MB][NI][16][16];   // [.][wavefront][block][.][row][entry]
+  __shared__ __attribute__((aligned(16))) float s_out[NI * 16 * kHoldPitch];
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int piece = (lane >> 4) * 8;
+  bf16x8 hf[PPW][2][NI];
+#pragma unroll
+  for (int p = 0; p < PPW; ++p)
+#pragma unroll
+    for (int q = 0; q < 2; ++q)
+#pragma unroll
+      for (int j = 0; j < NI; ++j) {
+        const int n = min(j * 16 + (lane & 15), n_sel - 1), k = (p * kFewWaves + wave) * 64 + q * 32 + piece;
+        const int64_t row = rowsel ? rowsel[n] : n;
+        const uint4 v = k < d ? *reinterpret_cast<const uint4*>(H + row * d + k) : make_uint4(0u, 0u, 0u, 0u);
+        hf[p][q][j] = __builtin_bit_cast(bf16x8, v);
+      }
+  const int blocks = (V + 15) / 16;
+  const int b0 = static_cast<int>(blockIdx.x) * per, b1 = min(b0 + per, blocks);
+  uint4 w[MB][PPW][2];
+  bool past[2];                                              // the last piece's columns that do not exist
+#pragma unroll
+  for (int q = 0; q < 2; ++q) past[q] = ((PPW - 1) * kFewWaves + wave) * 64 + q * 32 + piece >= d;
+  auto load = [&](int b, int p, int q, int i) {              // past the hidden size: some entry of the row, cleared where it is used
+    const int v = min((b + i) * 16 + (lane & 15), V - 1), k = min((p * kFewWaves + wave) * 64 + q * 32 + piece, d - 8);
+    w[i][p][q] = *reinterpret_cast<const uint4*>(W + static_cast<int64_t>(v) * d + k);
+  };
+  if (b0 < b1)
+#pragma unroll
+    for (int i = 0; i < MB; ++i)
+#pragma unroll
+      for (int p = 0; p < PPW; ++p) { load(b0, p, 0, i); load(b0, p, 1, i); }
+  const bool mine = tid < NI * 256;
+  const int my_n = (tid >> 4) & 15, my_v = tid & 15;
+  float m[NL], s[NL];
+#pragma unroll
+  for (int l = 0; l < NL; ++l) {
+    m[l] = kMasked;
+    s[l] = 0.f;
+  }
+  int first = b0;                                            // of the blocks that collect
+  auto leave = [&](int end) {                                // a wavefront to a row
+    __syncthreads();
+    for (int n = wave; n < n_sel; n += kFewWaves) {
+      float* const z = out.z + ((static_cast<int64_t>(n) * out.tiles + blockIdx.x) * per + first - b0) * kFewGroups;
+      for (int c = lane * 4; c < (end - first) * 16; c += kWave * 4)
+        *reinterpret_cast<floatx4*>(z + c) = *reinterpret_cast<const floatx4*>(s_out + n * kHoldPitch + c);
+    }
+    __syncthreads();
+    first = end;
+  };
+  int buf = 0;
+  for (int b = b0; b < b1; b += MB, buf ^= 1) {
+    floatx4 acc[MB][NI];
+#pragma unroll
+    for (int i = 0; i < MB; ++i)
+#pragma unroll
+      for (int j = 0; j < NI; ++j) acc[i][j] = floatx4{0.f, 0.f, 0.f, 0.f};
+    const int nb = b + MB < b1 ? b + MB : b;                 // past the range: loaded again, not used
+#pragma unroll
+    for (int i = 0; i < MB; ++i)
+#pragma unroll
+      for (int p = 0; p < PPW; ++p)
+#pragma unroll
+        for (int q = 0; q < 2; ++q) {
+          const bf16x8 a = __builtin_bit_cast(bf16x8, p == PPW - 1 && past[q] ? make_uint4(0u, 0u, 0u, 0u) : w[i][p][q]);
+#pragma unroll
+          for (int j = 0; j < NI; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, hf[p][q][j], acc[i][j], 0, 0, 0);
+          load(nb, p, q, i);
+        }
+#pragma unroll
+    for (int i = 0; i < MB; ++i)
+#pragma unroll
+      for (int j = 0; j < NI; ++j) *reinterpret_cast<floatx4*>(&s_z[buf][wave][i][j][lane & 15][(lane >> 4) * 4]) = acc[i][j];
+    __syncthreads();
+    if (mine) {
+#pragma unroll
+      for (int i = 0; i < MB; ++i)
+#pragma unroll
+        for (int l = 0; l < NL; ++l) {
+          float z = 0.f;
+#pragma unroll
+          for (int k = 0; k < kFewWaves; ++k) z += s_z[buf][k][i][2 * l + (tid >> 8)][my_n][my_v];
+          if ((b + i) * 16 + my_v >= V || b + i >= b1) z = kMasked;
+          s_out[((2 * l + (tid >> 8)) * 16 + my_n) * kHoldPitch + (b + i - first) * 16 + my_v] = z;
+          const float gap = z - m[l], e = __expf(-fabsf(gap));  // one exponential: of the smaller relative to the larger
+          s[l] = gap > 0.f ? fmaf(s[l], e, 1.f) : s[l] + e;
+          m[l] = fmaxf(m[l], z);
+        }
+    }
+    if (b + MB - first == kHold) leave(b + MB);
+  }
+  if (first < b1) leave(min(b0 + per, (b1 - first + MB - 1) / MB * MB + first));
+#pragma unroll
+  for (int l = 0; l < NL; ++l) {
+    float most = m[l];                                       // of the row's sixteen threads, which are neighbours
+#pragma unroll
+    for (int o = 1; o < 16; o <<= 1) most = fmaxf(most, __shfl_xor(most, o, kWave));
+    float sum = s[l] * __expf(m[l] - most);
+#pragma unroll
+    for (int o = 1; o < 16; o <<= 1) sum += __shfl_xor(sum, o, kWave);
+    const int n = (2 * l + (tid >> 8)) * 16 + my_n;
+    if (!mine || n >= n_sel) continue;
+    const int64_t at = static_cast<int64_t>(n) * out.tiles + blockIdx.x;
+    out.max[at * kFewGroups + my_v] = m[l];
+    if (my_v == 0) out.sum[at] = sum;
+  }
 }
 
 // ------------------------------------------------------------------ selection
-// Logits of row m (of the chunk), four next to each other from v on; those past V are not looked at.
-struct Blocked {                                             // float32 in blocks of 256 x 256
-  const float* Z;
-  int64_t tiles_v;
-  __device__ __forceinline__ float4 load(int64_t m, int v, int) const {
-    return *reinterpret_cast<const float4*>(Z + ((m >> 8) * tiles_v + (v >> 8)) * kBlkElems + (m & 255) * 256 + (v & 255));
-  }
+// Where a group's entries lie in the vocabulary, and how many there are.
+template <class C>
+struct TileGroups {
+  static constexpr int G = kGroups;
+  __device__ __forceinline__ int entries() const { return kEntries<C>; }
+  __device__ __forceinline__ int token(int tile, int g, int e) const { return tile * C::BM + (g >> 2) * C::WTM + (e >> 2) * 16 + (g & 3) * 4 + (e & 3); }
+  __device__ __forceinline__ int64_t place(int tile, int g, int e) const { return (static_cast<int64_t>(tile) * G + g) * kEntries<C> + e; }
 };
-struct Doubles {                                             // float64 [rows][V]
-  const double* Z;
-  __device__ __forceinline__ float4 load(int64_t m, int v, int V) const {
-    const double* p = Z + m * V + v;
-    return make_float4(static_cast<float>(p[0]), v + 1 < V ? static_cast<float>(p[1]) : 0.f, v + 2 < V ? static_cast<float>(p[2]) : 0.f,
-                       v + 3 < V ? static_cast<float>(p[3]) : 0.f);
-  }
+struct FewGroups {
+  static constexpr int G = kFewGroups;
+  int per;
+  __device__ __forceinline__ int entries() const { return per; }
+  __device__ __forceinline__ int token(int tile, int g, int e) const { return (tile * per + e) * 16 + g; }
+  __device__ __forceinline__ int64_t place(int tile, int g, int e) const { return token(tile, g, e); }
 };
-// A workgroup goes over a part of a row's vocabulary, its wavefronts 256 entries at a time in turn: list[row][part] gets the 64 largest keys.
-template <class Logits>
+__device__ __forceinline__ float exchange(float x, int j, bool larger) {
+  const float y = __shfl_xor(x, j, kWave);
+  return larger ? fmaxf(x, y) : fminf(x, y);
+}
+struct TopOut {
+  const int32_t* rowsel;
+  int64_t c0;
+  int k;
+  int32_t* ids;
+  float *logits, *lse;
+};
+__device__ __forceinline__ void write_top(const TopOut& O, int64_t row, TopKey list) {   // wavefront 0
+  const int lane = threadIdx.x & 63;
+  if (lane >= O.k) return;
+  O.ids[row * O.k + lane] = token_of(list);
+  O.logits[row * O.k + lane] = logit_of(list);
+}
+// A bound that at least k logits of a row reach: the threads of a workgroup take the maximum over the row's tiles in turn, and the k-th largest of these
+// 256 numbers is it (k at most 64; with random logits 74 groups of thousands reach the 64th).  `lm`, `ls`: the wavefront's part of the logsumexp.
+template <int G>
+__device__ __forceinline__ void load_maxima(const float* __restrict__ maxima, int t, float (&x)[G]) {
+#pragma unroll
+  for (int g = 0; g < G; g += 4) {
+    const floatx4 v = *reinterpret_cast<const floatx4*>(maxima + static_cast<int64_t>(t) * G + g);
+    x[g] = v[0]; x[g + 1] = v[1]; x[g + 2] = v[2]; x[g + 3] = v[3];
+  }
+}
+template <int G>
+__device__ __forceinline__ float row_bound(const float* __restrict__ maxima, const float* __restrict__ sums, int tiles, int k, float (*s_top)[kWave], float& lm, float& ls) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  float x = -INFINITY;
+  lm = kMasked;
+  ls = 0.f;
+  for (int t = threadIdx.x; t < tiles; t += kSelectT) {
+    float g_max[G];
+    load_maxima<G>(maxima, t, g_max);
+    float tm = g_max[0];
+#pragma unroll
+    for (int g = 1; g < G; ++g) tm = fmaxf(tm, g_max[g]);
+    x = fmaxf(x, tm);
+    if (sums) {
+      tm = fmaxf(tm, kMasked);
+      const float s = sums[t], M = fmaxf(lm, tm);
+      ls = ls * __expf(lm - M) + s * __expf(tm - M);
+      lm = M;
+    }
+  }
+  // the wavefront's 64 maxima, falling; then everybody merges the four lists
+#pragma unroll
+  for (int q = 2; q <= kWave; q <<= 1)
+#pragma unroll
+    for (int j = q >> 1; j > 0; j >>= 1) x = exchange(x, j, ((lane & j) == 0) == ((lane & q) == 0));
+  s_top[wave][lane] = x;
+  __syncthreads();
+  x = s_top[0][lane];
+#pragma unroll
+  for (int w = 1; w < kSelectWaves; ++w) {
+    x = fmaxf(x, s_top[w][63 - lane]);
+#pragma unroll
+    for (int j = kWave / 2; j > 0; j >>= 1) x = exchange(x, j, (lane & j) == 0);
+  }
+  return __shfl(x, k - 1, kWave);
+}
 __global__ void __launch_bounds__(kSelectT)
-k_top_select(Logits L, int V, int k, int parts, int per, TopKey* __restrict__ lists) {
+k_top_bound(Groups A, int tiles, int k, float* __restrict__ bound) {   // of a row's first tiles
+  __shared__ float s_top[kSelectWaves][kWave];
+  float lm, ls;
+  const int64_t m = blockIdx.x;
+  const float b = row_bound<kGroups>(A.max + m * A.tiles * kGroups, nullptr, tiles, k, s_top, lm, ls);
+  if (threadIdx.x == 0) bound[m] = b;
+}
+// A workgroup to a row: the groups that reach its bound are listed, and the wavefronts go through their entries.  The row's logsumexp comes from the tiles'
+// sums on the way.
+constexpr int kAtOnce = 4;                                   // loads of entries under way
+template <class Map>
+__global__ void __launch_bounds__(kSelectT)
+k_top_row(Groups A, Map map, int V, TopOut O) {
+  __shared__ TopKey s_buf[kSelectWaves][2 * kWave];
+  __shared__ TopKey s_list[kSelectWaves][kWave];
+  __shared__ float s_top[kSelectWaves][kWave], s_m[kSelectWaves], s_s[kSelectWaves];
+  __shared__ int s_group[kSelectT * Map::G];
+  __shared__ int s_n;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int64_t m = blockIdx.x, n = O.c0 + m, row = O.rowsel ? O.rowsel[n] : n;
+  const float* const maxima = A.max + m * A.tiles * Map::G;
+  if (threadIdx.x == 0) s_n = 0;
+  float lm, ls;
+  const float bound = row_bound<Map::G>(maxima, A.sum + m * A.tiles, A.tiles, O.k, s_top, lm, ls);
+  {
+    const float M = wave_max(lm), sum = wave_sum(ls * __expf(lm - M));
+    if (lane == 0) { s_m[wave] = M; s_s[wave] = sum; }
+  }
+  WaveTop top;
+  top.buf = s_buf[wave];
+  top.k = O.k;
+  top.least = bound > -INFINITY ? key_of(bound, -1) : 0;     // below every logit of that size
+  const int E = map.entries();
+  const int side = E <= 16 ? 16 : E <= 32 ? 32 : 64, at_once = kWave / side;   // lanes to a group, groups to a load
+  const int sub = lane / side, e0 = lane % side;
+  const float* const z = A.z + m * A.tiles * Map::G * E;
+  for (int t0 = 0; t0 < A.tiles; t0 += kSelectT) {
+    const int t = t0 + threadIdx.x;
+    if (t < A.tiles) {
+      float g_max[Map::G];
+      load_maxima<Map::G>(maxima, t, g_max);
+#pragma unroll
+      for (int g = 0; g < Map::G; ++g)
+        if (g_max[g] >= bound && g_max[g] > -INFINITY) s_group[atomicAdd(&s_n, 1)] = t * Map::G + g;
+    }
+    __syncthreads();
+    const int count = s_n;
+    for (int i = wave * at_once; i < count; i += kSelectWaves * at_once * kAtOnce)
+      for (int f = 0; f < E; f += side) {
+        float v[kAtOnce];
+        int id[kAtOnce];
+#pragma unroll
+        for (int b = 0; b < kAtOnce; ++b) {
+          const int q = i + b * kSelectWaves * at_once + sub, e = f + e0, g = q < count ? s_group[q] : 0;
+          id[b] = q < count && e < E ? map.token(g / Map::G, g % Map::G, e) : V;
+          v[b] = id[b] < V ? z[map.place(g / Map::G, g % Map::G, e)] : 0.f;
+        }
+#pragma unroll
+        for (int b = 0; b < kAtOnce; ++b) top.offer(v[b], id[b], id[b] < V);
+      }
+    __syncthreads();
+    if (threadIdx.x == 0) s_n = 0;
+    __syncthreads();
+  }
+  top.finish();
+  const TopKey list = merge_waves(top.list, s_list);
+  if (wave == 0) write_top(O, row, list);
+  if (threadIdx.x != 0) return;
+  float M = s_m[0], sum = s_s[0];
+  for (int w = 1; w < kSelectWaves; ++w) {
+    const float X = fmaxf(M, s_m[w]);
+    sum = sum * __expf(M - X) + s_s[w] * __expf(s_m[w] - X);
+    M = X;
+  }
+  O.lse[row] = M + logf(sum);
+}
+
+// float32: float64 logits [rows][V].  A workgroup goes over a part of a row's vocabulary, its wavefronts 256 entries at a time in turn: list[row][part] gets the 64
+// largest keys.
+__global__ void __launch_bounds__(kSelectT)
+k_top_select(const double* __restrict__ Z, int V, int k, int parts, int per, TopKey* __restrict__ lists) {
   __shared__ TopKey s_buf[kSelectWaves][2 * kWave];
   __shared__ TopKey s_list[kSelectWaves][kWave];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
@@ -213,59 +509,25 @@ k_top_select(Logits L, int V, int k, int parts, int per, TopKey* __restrict__ li
   top.buf = s_buf[wave];
   top.k = k;
   for (int b = v0 + wave * 256; b < v1; b += kSelectWaves * 256) {
-    const int v = b + lane * 4;
-    const float4 z = v < v1 ? L.load(m, v, V) : make_float4(0.f, 0.f, 0.f, 0.f);
-    top.offer(z.x, v, v < v1);
-    top.offer(z.y, v + 1, v + 1 < v1);
-    top.offer(z.z, v + 2, v + 2 < v1);
-    top.offer(z.w, v + 3, v + 3 < v1);
+    float z[4];
+#pragma unroll
+    for (int q = 0; q < 4; ++q) z[q] = b + q * 64 + lane < v1 ? static_cast<float>(Z[m * V + b + q * 64 + lane]) : 0.f;
+#pragma unroll
+    for (int q = 0; q < 4; ++q) top.offer(z[q], b + q * 64 + lane, b + q * 64 + lane < v1);
   }
   top.finish();
   const TopKey all = merge_waves(top.list, s_list);
   if (wave == 0) lists[(m * parts + part) * kWave + lane] = all;
 }
-// A workgroup merges a row's lists and, where there are parts of its softmax, its logsumexp; writes the results.
-struct TopOut {
-  const int32_t* rowsel;
-  int64_t c0;
-  int k;
-  int32_t* ids;
-  float *logits, *lse;
-};
 __global__ void __launch_bounds__(kSelectT)
-k_top_merge(const TopKey* __restrict__ lists, int parts, const float2* __restrict__ partial, int tiles_m, int64_t n_pad, TopOut O) {
+k_top_merge(const TopKey* __restrict__ lists, int parts, TopOut O) {
   __shared__ TopKey s_list[kSelectWaves][kWave];
-  __shared__ float s_m[kSelectWaves], s_s[kSelectWaves];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int64_t m = blockIdx.x, n = O.c0 + m, row = O.rowsel ? O.rowsel[n] : n;
   TopKey list = 0;
   for (int p = wave; p < parts; p += kSelectWaves) list = merged(list, lists[(m * parts + p) * kWave + lane]);
   list = merge_waves(list, s_list);
-  if (wave == 0 && lane < O.k) {
-    O.ids[row * O.k + lane] = token_of(list);
-    O.logits[row * O.k + lane] = logit_of(list);
-  }
-  if (!partial) return;
-  float mx = -INFINITY, s = 0.f;
-  for (int t = threadIdx.x; t < tiles_m; t += kSelectT) {
-    const float2 p = partial[static_cast<int64_t>(t) * n_pad + m];
-    const float M = fmaxf(mx, p.x);
-    s = s * __expf(mx - M) + p.y * __expf(p.x - M);
-    mx = M;
-  }
-  const float M = wave_max(mx);
-  s = wave_sum(mx == -INFINITY ? 0.f : s * __expf(mx - M));
-  if (lane == 0) { s_m[wave] = M; s_s[wave] = s; }
-  __syncthreads();
-  if (threadIdx.x != 0) return;
-  float a = s_m[0], b = s_s[0];
-  for (int w = 1; w < kSelectWaves; ++w) {
-    if (s_m[w] == -INFINITY) continue;
-    const float X = fmaxf(a, s_m[w]);
-    b = b * __expf(a - X) + s_s[w] * __expf(s_m[w] - X);
-    a = X;
-  }
-  O.lse[row] = a + logf(b);
+  if (wave == 0) write_top(O, row, list);
 }
 // what the call defines on rows that are not selected
 __global__ void __launch_bounds__(256)
@@ -280,31 +542,68 @@ constexpr int64_t kTopChunkRows = 4096;
 // workgroups to a row: as many as fill the chip, 256 entries to a wavefront at the least
 constexpr int64_t kSelectLists = 2048;
 int select_parts(int64_t rows, int V) { return static_cast<int>(std::min<int64_t>(std::max<int64_t>(kSelectLists / rows, 1), cdiv(V, kSelectWaves * 256))); }
+template <int PPW, class... Args>
+void launch_top_few_ppw(int ni, unsigned grid, hipStream_t st, Args... args) {
+  if constexpr (PPW <= 4)
+    if (ni > 2) { hipLaunchKernelGGL((k_top_few<4, PPW>), dim3(grid), dim3(kFewT), 0, st, args...); return; }
+  if (ni <= 1) hipLaunchKernelGGL((k_top_few<1, PPW>), dim3(grid), dim3(kFewT), 0, st, args...);
+  else hipLaunchKernelGGL((k_top_few<2, PPW>), dim3(grid), dim3(kFewT), 0, st, args...);
+}
+template <class... Args>
+void launch_top_few(int ppw, Args... args) {
+  switch (ppw) {
+    case 1: return launch_top_few_ppw<1>(args...);
+    case 2: return launch_top_few_ppw<2>(args...);
+    case 3: return launch_top_few_ppw<3>(args...);
+    case 4: return launch_top_few_ppw<4>(args...);
+    case 5: return launch_top_few_ppw<5>(args...);
+    case 6: return launch_top_few_ppw<6>(args...);
+    case 7: return launch_top_few_ppw<7>(args...);
+    default: return launch_top_few_ppw<8>(args...);
+  }
+}
 struct TopWs {
-  TopKey* lists;
-  float2* partial;
-  void* z;
-  char* room;                                                // float32: for the scores' parts
-  size_t bytes, room_bytes;
+  TopKey* lists;                                             // float32
+  double* z64;
+  char* room;                                                // ... for the scores' parts
+  size_t room_bytes;
+  Groups groups;                                             // bf16
+  float* bound;
+  size_t bytes;
 };
-void carve(Carver& c, TopWs& w, int64_t rows, int V, umas_dtype dt) {
-  const int64_t pad = round_up(rows, 256), Vp = round_up(V, 256);
+// Tiles of the vocabulary whose logits are all kept: they give the bound that leaves most of the others unwritten.  With n entries in them a group of E = 32 among
+// the others reaches the bound with a probability of about E k / n, and stores 16 bytes at a time, which costs about three times what the rows of whole tiles do:
+// n^2 = 3 E k V; then whole rounds of compute units.
+int first_tiles(int tiles, int tiles_n, int k) {
+  const double n = sqrt(3.0 * kEntries<Cfg> * k * (static_cast<double>(tiles) * 256.0));
+  const int round = static_cast<int>(cdiv(std::max(device_cus(), 1), tiles_n));
+  const int first = static_cast<int>(round_up(static_cast<int64_t>(n / 256.0) + 1, round));
+  return first * 2 > tiles ? tiles : first;
+}
+// blocks of 16 entries to a workgroup of the kernel for few rows
+int few_per(int V, int tiles) { return static_cast<int>(round_up(cdiv(cdiv(V, 16), tiles), 2)); }   // steps of two blocks end in them
+void carve(Carver& c, TopWs& w, int64_t rows, int d, int V, umas_dtype dt) {
   w = TopWs{};
-  w.lists = c.take<TopKey>(static_cast<size_t>(std::max(rows, kSelectLists)) * kWave);
   if (dt == UMAS_BF16) {
-    w.partial = c.take<float2>(static_cast<size_t>(Vp / 128) * pad);
-    w.z = c.take<float>(static_cast<size_t>(pad) * Vp);
+    // as many groups and entries as any of the kernels has: tiles of 256 or 128 entries, up to kFewMostTiles workgroups whose parts end unevenly
+    const bool few = rows <= few_rows(d);
+    const int64_t tiles = few ? kFewMostTiles : round_up(V, 256) / 128, groups = few ? int64_t{kFewMostTiles} * kFewGroups : tiles * kGroups;
+    w.groups.max = c.take<float>(static_cast<size_t>(rows) * groups);
+    w.groups.sum = c.take<float>(static_cast<size_t>(rows) * tiles);
+    w.bound = c.take<float>(rows);
+    w.groups.z = c.take<float>(static_cast<size_t>(rows) * (round_up(V, 256) + (few ? 3 * kFewMostTiles * kFewGroups : 0)));
   } else {
-    w.z = c.take<double>(static_cast<size_t>(rows) * V);
+    w.lists = c.take<TopKey>(static_cast<size_t>(std::max(rows, kSelectLists)) * kWave);
+    w.z64 = c.take<double>(static_cast<size_t>(rows) * V);
     w.room_bytes = align_up(f32::score_room(rows, V));
     w.room = c.take<char>(w.room_bytes);
   }
   w.bytes = c.off;
 }
-size_t top_bytes(int64_t n_sel, int64_t cap, int V, umas_dtype dt) {
+size_t top_bytes(int64_t n_sel, int64_t cap, int d, int V, umas_dtype dt) {
   Carver c(nullptr);
   TopWs w;
-  carve(c, w, std::min(std::max<int64_t>(n_sel, 1), cap), V, dt);
+  carve(c, w, std::min(std::max<int64_t>(n_sel, 1), cap), d, V, dt);
   return w.bytes;
 }
 
@@ -315,11 +614,11 @@ using namespace umas;
 
 extern "C" size_t umas_top_logits_workspace_bytes_min(int64_t n_sel, int32_t d, int32_t V, int32_t k, umas_dtype dtype) {
   if (n_sel < 0 || d < 1 || V < 1 || k < 1 || k > UMAS_MAX_TOP) return 0;
-  return top_bytes(n_sel, 256, V, dtype);
+  return top_bytes(n_sel, 256, d, V, dtype);
 }
 extern "C" size_t umas_top_logits_workspace_bytes(int64_t n_sel, int32_t d, int32_t V, int32_t k, umas_dtype dtype) {
   if (n_sel < 0 || d < 1 || V < 1 || k < 1 || k > UMAS_MAX_TOP) return 0;
-  return top_bytes(n_sel, kTopChunkRows, V, dtype);
+  return top_bytes(n_sel, kTopChunkRows, d, V, dtype);
 }
 
 extern "C" umas_status umas_top_logits(const void* H, const void* W, umas_dtype dtype, int64_t n_rows, int32_t d, int32_t V, const int32_t* rowsel,
@@ -340,44 +639,56 @@ extern "C" umas_status umas_top_logits(const void* H, const void* W, umas_dtype 
   }
   if (n_sel == 0) return UMAS_OK;
   int64_t cap = std::min(n_sel, kTopChunkRows);
-  while (cap > 256 && top_bytes(n_sel, cap, V, dtype) > workspace_bytes) cap = std::max<int64_t>(round_up(cap / 2, 256), 256);
+  while (cap > 256 && top_bytes(n_sel, cap, d, V, dtype) > workspace_bytes) cap = std::max<int64_t>(round_up(cap / 2, 256), 256);
   Carver c(workspace);
   TopWs w;
-  carve(c, w, cap, V, dtype);
+  carve(c, w, cap, d, V, dtype);
   for (int64_t c0 = 0; c0 < n_sel; c0 += cap) {
-    const int64_t rows = std::min(cap, n_sel - c0), tiles_v = round_up(V, 256) / 256;
-    int tiles_m = static_cast<int>(tiles_v);
-    int64_t n_pad = round_up(rows, 256);
-    const int parts = select_parts(rows, V), per = static_cast<int>(round_up(cdiv(V, parts), 256));
-    const dim3 select(static_cast<unsigned>(rows), parts);
+    const int64_t rows = std::min(cap, n_sel - c0);
+    const TopOut O{rowsel, c0, k, top_ids, top_logits, lse};
+    const dim3 grid(static_cast<unsigned>(rows));
     if (dtype == UMAS_BF16) {
       const uint16_t *Wb = static_cast<const uint16_t*>(W), *Hb = static_cast<const uint16_t*>(H);
-      float* const Z = static_cast<float*>(w.z);
-      if (rows <= NarrowCfg::BN) {
-        tiles_m = (V + NarrowCfg::BM - 1) / NarrowCfg::BM;
-        n_pad = NarrowCfg::BN;
-        hipLaunchKernelGGL(k_top_narrow, dim3(tile_grid<kGM, kGN>(tiles_m, 1, kGN, kTilesPerWg)), dim3(NarrowCfg::T), 0, st, Wb, Hb, d, V, rowsel, c0, rows, tiles_m,
-                           w.partial, n_pad, Z, tiles_v);
+      Groups A = w.groups;
+      if (cap <= few_rows(d)) {                              // one chunk
+        A.tiles = std::min(std::min(device_cus(), kFewMostTiles), static_cast<int>(cdiv(V, 16)));
+        const int per = few_per(V, A.tiles);
+        launch_top_few(few_pieces(d), rows <= 16 ? 1 : rows <= 32 ? 2 : 4, A.tiles, st, Wb, Hb, d, V, rowsel, static_cast<int>(rows), per, A);
+        UMAS_LAUNCHED("k_top_few");
+        hipLaunchKernelGGL(k_top_row<FewGroups>, grid, dim3(kSelectT), 0, st, A, FewGroups{per}, V, O);
+      } else if (rows <= NarrowCfg::BN) {
+        A.tiles = static_cast<int>(cdiv(V, NarrowCfg::BM));
+        hipLaunchKernelGGL(k_top_narrow, dim3(tile_grid<kGM, kGN>(A.tiles, 1, kGN, kTilesPerWg)), dim3(NarrowCfg::T), 0, st, Wb, Hb, d, V, rowsel, c0, rows, A);
         UMAS_LAUNCHED("k_top_narrow");
+        hipLaunchKernelGGL(k_top_row<TileGroups<NarrowCfg>>, grid, dim3(kSelectT), 0, st, A, TileGroups<NarrowCfg>{}, V, O);
       } else {
-        const int tiles_n = static_cast<int>(n_pad / 256), panel = row_panel(tiles_n, d);
-        hipLaunchKernelGGL(k_top_tiles, score_grid(tiles_m, tiles_n, panel, 0), dim3(Cfg::T), 0, st, Wb, Hb, d, V, rowsel, c0, rows, tiles_m, tiles_n, panel,
-                           w.partial, n_pad, Z, tiles_v);
+        A.tiles = static_cast<int>(cdiv(V, Cfg::BM));
+        const int tiles_n = static_cast<int>(cdiv(rows, Cfg::BN)), panel = row_panel(tiles_n, d);
+        const int first = first_tiles(A.tiles, tiles_n, k);
+        hipLaunchKernelGGL(k_top_tiles, score_grid(first, tiles_n, panel, 0), dim3(Cfg::T), 0, st, Wb, Hb, d, V, rowsel, c0, rows, first, tiles_n, panel, A);
         UMAS_LAUNCHED("k_top_tiles");
+        if (first < A.tiles) {
+          hipLaunchKernelGGL(k_top_bound, grid, dim3(kSelectT), 0, st, A, first, k, w.bound);
+          UMAS_LAUNCHED("k_top_bound");
+          const int rest = A.tiles - first;
+          hipLaunchKernelGGL(k_top_tiles_bound, score_grid(rest, tiles_n, panel, 0), dim3(Cfg::T), 0, st, Wb, Hb, d, V, rowsel, c0, rows, first, rest, tiles_n, panel,
+                             A, w.bound);
+          UMAS_LAUNCHED("k_top_tiles_bound");
+        }
+        hipLaunchKernelGGL(k_top_row<TileGroups<Cfg>>, grid, dim3(kSelectT), 0, st, A, TileGroups<Cfg>{}, V, O);
       }
-      hipLaunchKernelGGL(k_top_select<Blocked>, select, dim3(kSelectT), 0, st, Blocked{Z, tiles_v}, V, k, parts, per, w.lists);
+      UMAS_LAUNCHED("k_top_row");
     } else {
+      const int parts = select_parts(rows, V), per = static_cast<int>(round_up(cdiv(V, parts), 256));
       const float* Hf = static_cast<const float*>(H) + (rowsel ? 0 : c0 * d);
-      double* const Z = static_cast<double*>(w.z);
       s = f32::score(static_cast<const float*>(W), Hf, d, V, rowsel ? rowsel + c0 : nullptr, rows, nullptr, w.room, w.room_bytes,
-                     f32::ScoreOut{Z, nullptr, nullptr, nullptr, nullptr, nullptr, rowsel ? lse : lse + c0, nullptr}, st);
+                     f32::ScoreOut{w.z64, nullptr, nullptr, nullptr, nullptr, nullptr, rowsel ? lse : lse + c0, nullptr}, st);
       if (s != UMAS_OK) return s;
-      hipLaunchKernelGGL(k_top_select<Doubles>, select, dim3(kSelectT), 0, st, Doubles{Z}, V, k, parts, per, w.lists);
+      hipLaunchKernelGGL(k_top_select, dim3(static_cast<unsigned>(rows), parts), dim3(kSelectT), 0, st, w.z64, V, k, parts, per, w.lists);
+      UMAS_LAUNCHED("k_top_select");
+      hipLaunchKernelGGL(k_top_merge, grid, dim3(kSelectT), 0, st, w.lists, parts, O);
+      UMAS_LAUNCHED("k_top_merge");
     }
-    UMAS_LAUNCHED("k_top_select");
-    hipLaunchKernelGGL(k_top_merge, dim3(static_cast<unsigned>(rows)), dim3(kSelectT), 0, st, w.lists, parts, dtype == UMAS_BF16 ? w.partial : nullptr, tiles_m, n_pad,
-                       TopOut{rowsel, c0, k, top_ids, top_logits, lse});
-    UMAS_LAUNCHED("k_top_merge");
   }
   return UMAS_OK;
 }
