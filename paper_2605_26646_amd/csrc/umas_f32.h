@@ -135,7 +135,6 @@ struct ScoreOut {
   double* rest_c;                            // compact arrays (NULL: none): sum of the probabilities of the tokens not taken
   float *logp_c, *lse_c, *ent_c;
   float *logp, *lse, *entropy;               // scattered (NULL: none)
-  double* lse64_c = nullptr;                 // compact, not rounded
 };
 struct Scores {
   bool ok;                                   // the token id exists
@@ -154,7 +153,6 @@ __device__ __forceinline__ void write_scores(const Stat& a, int64_t n, int64_t r
     o.logp_c[n] = s.lp; o.lse_c[n] = s.lse; o.ent_c[n] = s.en;
     o.rest_c[n] = s.rest;
   }
-  if (o.lse64_c) o.lse64_c[n] = a.m + log(a.s);
   if (o.logp) o.logp[row] = s.lp;
   if (o.lse) o.lse[row] = s.lse;
   if (o.entropy) o.entropy[row] = s.en;

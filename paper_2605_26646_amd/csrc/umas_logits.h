@@ -127,7 +127,8 @@ struct Stage {                                                                  
   static constexpr int kBytes = C::WM * C::WN * C::WTN * kPitch;
 };
 constexpr int kStagePitch = Stage<Cfg>::kPitch;
-constexpr int kLogitPitch = Cfg::WTM * 4 + 16;                                  // one staged row of logits: 128 floats
+template <class C>
+constexpr int kLogitPitch = C::WTM * 4 + 16;                                    // one staged row of logits: 128 (64) floats
 static_assert(kLogitLds <= 160 * 1024, "LDS of one CU");
 
 enum class Leave { kNothing, kNumerators, kLogits };   // what a scoring pass leaves behind for the backward
@@ -147,13 +148,12 @@ __device__ __forceinline__ void score_tile(const uint16_t* __restrict__ W, const
                                            float4* __restrict__ partial, int64_t n_pad, const KeepArgs& keep,
                                            uint16_t* lds) {
   constexpr bool KEEP = LEAVE == Leave::kNumerators;
-  static_assert(LEAVE != Leave::kLogits || (C::BM == 256 && C::WTM == Cfg::WTM), "logits are kept in rows of 128 of a block's 256 entries");
   static_assert(256 % C::BM == 0 && 256 % C::BN == 0, "numerators are kept inside a block");
   constexpr int kPitch = Stage<C>::kPitch;
   constexpr int kLds = C::T == Cfg::T ? kLogitLds : Ring2Cfg<C>::LDS_BYTES;   // halves of a tile use the whole one's buffers
   static_assert(Ring2Cfg<C>::LDS_BYTES <= kLds, "the main loop's stages fit");
   static_assert((LEAVE == Leave::kNothing ? 0 : Stage<C>::kBytes) + (C::WM * C::BN * 3 + C::BN) * 4 <= kLds, "staging and the partials fit the tile buffers");
-  static_assert(LEAVE != Leave::kLogits || 16 * kLogitPitch <= C::WTN * kPitch, "sixteen rows of logits fit a wavefront's stage");
+  static_assert(LEAVE != Leave::kLogits || 16 * kLogitPitch<C> <= C::WTN * kPitch, "sixteen rows of logits fit a wavefront's stage");
   const int m0 = tile_m * C::BM;
   const int64_t n0 = static_cast<int64_t>(tile_n) * C::BN;   // chunk-relative
   floatx4 acc[C::MI][C::NI];
@@ -166,7 +166,7 @@ __device__ __forceinline__ void score_tile(const uint16_t* __restrict__ W, const
   float* s_zy = s_part + C::WM * C::BN * 3;               // [BN]
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int wm = wave / C::WN;
-  char* stage = reinterpret_cast<char*>(lds) + wave * (LEAVE == Leave::kLogits ? 16 * kLogitPitch : C::WTN * kPitch);
+  char* stage = reinterpret_cast<char*>(lds) + wave * (LEAVE == Leave::kLogits ? 16 * kLogitPitch<C> : C::WTN * kPitch);
   if (threadIdx.x < C::BN) s_zy[threadIdx.x] = 0.f;
   __syncthreads();                                        // every wavefront has left the main loop's LDS reads
   const int vbase = m0 + wm * C::WTM + (lane >> 4) * 4;   // vocabulary id of element (i = 0, r = 0)
@@ -248,17 +248,19 @@ __device__ __forceinline__ void score_tile(const uint16_t* __restrict__ W, const
       column(m, std::false_type{});
     }
     if (LEAVE == Leave::kLogits) {
-      // sixteen rows of 128 logits through the wavefront's part of LDS, so that a store covers 512 bytes of two rows
+      // sixteen rows of 128 (64) logits through the wavefront's part of LDS, so that a store covers 512 (256) bytes of two (four) rows
 #pragma unroll
       for (int i = 0; i < C::MI; ++i)
-        *reinterpret_cast<floatx4*>(stage + (lane & 15) * kLogitPitch + (i * 16 + (lane >> 4) * 4) * 4) = acc[i][j];
+        *reinterpret_cast<floatx4*>(stage + (lane & 15) * kLogitPitch<C> + (i * 16 + (lane >> 4) * 4) * 4) = acc[i][j];
       __builtin_amdgcn_wave_barrier();
-      float* out = keep.Z + blk_offset(n0 >> 8, tile_m, keep.Vp >> 8) + ((n0 & 255) + wave % C::WN * C::WTN + j * 16 + (lane >> 5)) * 256 + wm * C::WTM + (lane & 31) * 4;
+      constexpr int kLanes = C::WTM / 4, kRows = kWave / kLanes;
+      float* out = keep.Z + blk_offset(n0 >> 8, m0 >> 8, keep.Vp >> 8) + ((n0 & 255) + wave % C::WN * C::WTN + j * 16 + lane / kLanes) * 256 + (m0 & 255) +
+                   wm * C::WTM + lane % kLanes * 4;
 #pragma unroll
-      for (int q = 0; q < 8; ++q)
-        if (n0 + wave % C::WN * C::WTN + j * 16 + q * 2 + (lane >> 5) < mc)   // rows past the chunk: nobody reads them
-          __builtin_nontemporal_store(*reinterpret_cast<const floatx4*>(stage + (q * 2 + (lane >> 5)) * kLogitPitch + (lane & 31) * 16),
-                                      reinterpret_cast<floatx4*>(out + q * 512));
+      for (int q = 0; q < 16 / kRows; ++q)
+        if (n0 + wave % C::WN * C::WTN + j * 16 + q * kRows + lane / kLanes < mc)   // rows past the chunk: nobody reads them
+          __builtin_nontemporal_store(*reinterpret_cast<const floatx4*>(stage + (q * kRows + lane / kLanes) * kLogitPitch<C> + lane % kLanes * 16),
+                                      reinterpret_cast<floatx4*>(out + q * kRows * 256));
       __builtin_amdgcn_wave_barrier();
     }
     Part p{m, s, t};

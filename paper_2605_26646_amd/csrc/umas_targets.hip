@@ -90,6 +90,7 @@ struct RowArrays {
   float* zero;             // zeros
   float* cref;             // r
   float* sc;               // f
+  uint16_t* entries;       // [n_sel][k] (up to kFewTaught rows)
   float* zt;               // [n_sel][k] logits of the targets
   float* tt;               // [n_sel][k] their masses, all places of a token added up
   float* mass;
@@ -173,6 +174,60 @@ k_target_open(OpenArgs O) {
   }
 }
 
+// ------------------------------------------------------------------ statistics
+struct StatArgs {
+  int64_t n_sel;
+  const int32_t *rowsel, *role;
+  const float *l, *w, *ent, *lse, *mass;
+  float norm;
+  umas_target_stats* stats;
+};
+// The model's record (k = 0) or a role's, a workgroup of T threads to each, next to others that do something else; sums in float64, in an order that does
+// not depend on scheduling.
+template <int T>
+__device__ __forceinline__ void target_stats(const StatArgs& S, int k, double* smem) {
+  constexpr int kRows = 4;                                   // loads of as many rows are under way
+  double v[6] = {}, sum[6];
+  for (int64_t n0 = threadIdx.x; n0 < S.n_sel; n0 += kRows * T) {
+    float l[kRows], w[kRows], ent[kRows], lse[kRows], mass[kRows];
+    bool in[kRows];
+#pragma unroll
+    for (int q = 0; q < kRows; ++q) {
+      const int64_t n = n0 + q * T, at = n < S.n_sel ? n : n0;
+      l[q] = S.l[at]; w[q] = S.w[at]; ent[q] = S.ent[at]; lse[q] = S.lse[at]; mass[q] = S.mass[at];
+      in[q] = n < S.n_sel && (k == 0 || S.role[S.rowsel ? S.rowsel[at] : at] == k - 1);
+    }
+#pragma unroll
+    for (int q = 0; q < kRows; ++q) {
+      if (!in[q]) continue;
+      const bool taught = mass[q] != 0.f;
+      v[0] += w[q] != 0.f ? static_cast<double>(w[q]) * static_cast<double>(l[q]) : 0.0;
+      v[1] += static_cast<double>(w[q]);
+      v[2] += taught ? static_cast<double>(ent[q]) : 0.0;
+      v[3] += taught ? static_cast<double>(lse[q]) : 0.0;
+      v[4] += 1.0;
+      v[5] += taught ? 0.0 : 1.0;
+    }
+  }
+#pragma unroll
+  for (int j = 0; j < 6; ++j) sum[j] = block_sum<double>(v[j], smem);
+  if (threadIdx.x != 0) return;
+  const double taught = sum[4] - sum[5];
+  umas_target_stats s;
+  s.loss = sum[4] > 0 ? static_cast<float>(sum[0] / (k == 0 ? static_cast<double>(S.norm) : sum[4])) : 0.f;
+  s.weight_mean = sum[4] > 0 ? static_cast<float>(sum[1] / sum[4]) : 0.f;
+  s.entropy_mean = taught > 0 ? static_cast<float>(sum[2] / taught) : 0.f;
+  s.lse_mean = taught > 0 ? static_cast<float>(sum[3] / taught) : 0.f;
+  s.n_scored = static_cast<int64_t>(sum[4]);
+  s.n_ignored = static_cast<int64_t>(sum[5]);
+  S.stats[k] = s;
+}
+__global__ void __launch_bounds__(256)
+k_target_stats(StatArgs S) {
+  __shared__ double smem[32];
+  target_stats<256>(S, static_cast<int>(blockIdx.x), smem);
+}
+
 // ------------------------------------------------------------------ bf16: scores that keep the numerators
 __global__ void __launch_bounds__(Cfg::T)
 k_target_tiles(const uint16_t* __restrict__ W, const uint16_t* __restrict__ H, int d, int V, const int32_t* __restrict__ rowsel, int64_t c0, int64_t mc,
@@ -181,14 +236,6 @@ k_target_tiles(const uint16_t* __restrict__ W, const uint16_t* __restrict__ H, i
   __shared__ __attribute__((aligned(16))) uint16_t lds[kLogitLds / 2];
   score_tiles<Leave::kNumerators, Cfg>(W, H, d, V, rowsel, c0, mc, nullptr, tiles_m, tiles_n, panel, partial, n_pad, KeepArgs{cref, E, Vp, flags, cidx, nullptr}, lds, halved);
 }
-__global__ void __launch_bounds__(NarrowCfg::T)
-k_target_narrow(const uint16_t* __restrict__ W, const uint16_t* __restrict__ H, int d, int V, const int32_t* __restrict__ rowsel, int64_t n_sel,
-                int tiles_m, float4* __restrict__ partial, int64_t n_pad, const float* __restrict__ cref, uint16_t* __restrict__ E, int64_t Vp,
-                int32_t* __restrict__ flags, const int32_t* __restrict__ cidx) {
-  __shared__ __attribute__((aligned(16))) uint16_t lds[kNarrowLds / 2];
-  score_tiles<Leave::kNumerators, NarrowCfg>(W, H, d, V, rowsel, 0, n_sel, nullptr, tiles_m, 1, kGN, partial, n_pad, KeepArgs{cref, E, Vp, flags, cidx, nullptr}, lds);
-}
-
 // ------------------------------------------------------------------ bf16: rows
 // Eight rows to a workgroup: their parts merged, then a wavefront to a row: its loss and factor, its k entries of the operand, its scaled copy of H.
 struct RowsArgs {
@@ -290,6 +337,154 @@ k_target_rows(RowsArgs O) {
     }
   }
 }
+// ------------------------------------------------------------------ bf16: one block of rows
+// Up to 256 rows the scores leave their logits in float32 instead: 6 bytes a logit more to write and read, of which there are few here, in place of the
+// gather, the references and what they may not serve for.  The operand is then made from the logits, D = bf16(dz / (g a' x)), with f = g a' x as the row factor: x, near
+// 1, is what makes the row's largest target entry, rounded, exact.  It costs the others no second rounding here, so that dW has it as well.  (Few rows are where
+// it shows: a row of dW is one row's entry times its hidden state.)
+constexpr uint16_t kNoEntry = 0xFFFF;                        // a place that does not count
+__global__ void __launch_bounds__(Cfg::T)
+k_target_logits(const uint16_t* __restrict__ W, const uint16_t* __restrict__ H, int d, int V, const int32_t* __restrict__ rowsel, int64_t n_sel,
+                const int32_t* __restrict__ ids, int tiles_m, int halved, float4* __restrict__ partial, int64_t n_pad, float* __restrict__ Z, int64_t Vp) {
+  __shared__ __attribute__((aligned(16))) uint16_t lds[kLogitLds / 2];
+  score_tiles<Leave::kLogits, Cfg>(W, H, d, V, rowsel, 0, n_sel, ids, tiles_m, 1, kGN, partial, n_pad, KeepArgs{nullptr, nullptr, Vp, nullptr, nullptr, Z}, lds, halved);
+}
+__global__ void __launch_bounds__(NarrowCfg::T)
+k_target_logits_narrow(const uint16_t* __restrict__ W, const uint16_t* __restrict__ H, int d, int V, const int32_t* __restrict__ rowsel, int64_t n_sel,
+                       const int32_t* __restrict__ ids, int tiles_m, float4* __restrict__ partial, int64_t n_pad, float* __restrict__ Z, int64_t Vp) {
+  __shared__ __attribute__((aligned(16))) uint16_t lds[kNarrowLds / 2];
+  score_tiles<Leave::kLogits, NarrowCfg>(W, H, d, V, rowsel, 0, n_sel, ids, tiles_m, 1, kGN, partial, n_pad, KeepArgs{nullptr, nullptr, Vp, nullptr, nullptr, Z}, lds);
+}
+// The first workgroup lays the block out, `clearing` of them clear what the call defines everywhere, the others do eight rows each.
+struct FewArgs {
+  Teach A;
+  const uint16_t* H;
+  RowArrays R;
+  float* x;                // [rows] 1 / x; 0 for a row without a gradient
+  uint16_t* entries;       // [rows][k] the targets' entries of the operand
+  const float4* partial;
+  int tiles_m;
+  int64_t n_pad;
+  const float* Z;
+  uint16_t* Hs;
+  int64_t mcp;
+  float* row_out;
+  LiveArgs live;
+  unsigned clearing;
+  uint32_t* dH;
+  int64_t dh_words, n_rows;
+};
+__global__ void __launch_bounds__(256)
+k_target_few(FewArgs F) {
+  __shared__ float s_lse[8], s_ent[8];
+  const Teach& A = F.A;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, k = A.t.k;
+  if (blockIdx.x == 0) {
+    live_scan(F.live, static_cast<int>(threadIdx.x) < F.live.nblk);
+    return;
+  }
+  if (blockIdx.x <= F.clearing) {
+    const int64_t stride = static_cast<int64_t>(F.clearing) * 256, i0 = static_cast<int64_t>(blockIdx.x - 1) * 256 + threadIdx.x;
+    for (int64_t i = i0; i < F.dh_words; i += stride) F.dH[i] = 0u;
+    if (F.row_out)
+      for (int64_t i = i0; i < F.n_rows; i += stride) F.row_out[i] = 0.f;
+    return;
+  }
+  const int64_t m0 = (static_cast<int64_t>(blockIdx.x) - 1 - F.clearing) * 8;
+  {
+    const int64_t m = m0 + (lane & 7);
+    Part p;
+    float none;
+    if (merge_parts<true>(F.partial, F.tiles_m, F.n_pad, m, m < A.n_sel, p, none)) {
+      s_lse[lane] = p.m + logf(p.s);
+      s_ent[lane] = s_lse[lane] - p.t / p.s;
+    }
+  }
+  __syncthreads();
+  for (int q = wave; q < 8; q += 4) {
+    const int64_t n = m0 + q;
+    if (n >= A.n_sel) break;
+    const int64_t row = A.rowsel ? A.rowsel[n] : n;
+    const Place<float> P = place_of<float>(A.t, A.V, row);
+    const bool taught = P.mass != 0.f;                       // (a mass that is no number is the caller's)
+    const float w = row_weight(A, row, taught), g = w / A.norm, lse = s_lse[q], a = dense_factor(P.mass, A.z_coef, lse), ts = mass_of_token(k, P.id, P.t);
+    const float z = P.t != 0.f ? F.Z[blk_offset(0, P.id >> 8, 0) + n * 256 + (P.id & 255)] : 0.f;
+    float l = 0.f, out = 0.f;
+    if (taught) {
+      if (!A.t.logits) {
+        out = __shfl(z, 0, kWave) - lse;
+        l = A.z_coef != 0.f ? fmaf(A.z_coef * lse, lse, -out) : -out;
+      } else {
+        out = l = wave_sum(P.t != 0.f ? P.t * (logf(P.t) - (z - lse)) : 0.f);
+      }
+    }
+    const float e = g != 0.f && P.t != 0.f ? target_entry(z, lse, lse, ts, a) : 0.f, most = wave_max(fabsf(e));
+    const float x = most > 0.f ? most / bf2f(f2bf(most)) : 1.f;
+    const float f = g != 0.f ? g * a * x : 0.f;
+    if (lane < k) F.entries[n * k + lane] = P.t != 0.f ? f2bf(e / x) : kNoEntry;
+    if (lane == 0) {
+      F.R.lse[n] = taught ? lse : 0.f;
+      F.R.ent[n] = taught ? s_ent[q] : 0.f;
+      F.R.l[n] = l;
+      F.R.w[n] = w;
+      F.R.mass[n] = P.mass;
+      F.R.sc[n] = f;
+      F.x[n] = f != 0.f ? 1.f / x : 0.f;
+      F.R.a[n] = out;                                        // to row_out by who comes next: others clear it now
+    }
+    if (!F.Hs) continue;
+    const uint4* h = reinterpret_cast<const uint4*>(F.H + row * A.d);
+    for (int c = lane; c < A.d / 8; c += kWave) {
+      float v[8];
+      bf16x8_to_f32(h[c], v);
+      uint4 o = make_uint4(0u, 0u, 0u, 0u);
+      if (f != 0.f) o = make_uint4(pack_bf16x2(v[0] * f, v[1] * f), pack_bf16x2(v[2] * f, v[3] * f), pack_bf16x2(v[4] * f, v[5] * f), pack_bf16x2(v[6] * f, v[7] * f));
+      reinterpret_cast<uint4*>(F.Hs + (static_cast<int64_t>(c >> 5) * F.mcp + n) * 256)[c & 31] = o;
+    }
+  }
+}
+// 32 rows of a block of 256 entries to a workgroup; rows up to the next multiple of 64 are zeros.
+constexpr int kTurnedRows = 32;
+__global__ void __launch_bounds__(256)
+k_target_turn(const float* __restrict__ Z, const float* __restrict__ lse, const float* __restrict__ inv_x, const uint16_t* __restrict__ entries, Targets T,
+              const int32_t* __restrict__ rowsel, int64_t n_sel, uint16_t* __restrict__ D, const float* __restrict__ out, float* __restrict__ row_out, int tiles_v, StatArgs S) {
+  if (static_cast<int>(blockIdx.x) >= tiles_v) {             // the statistics
+    __shared__ double smem[32];
+    if (blockIdx.y == 0) target_stats<256>(S, static_cast<int>(blockIdx.x) - tiles_v, smem);
+    return;
+  }
+  if (blockIdx.x == 0 && row_out && threadIdx.x < kTurnedRows) {
+    const int64_t n = static_cast<int64_t>(blockIdx.y) * kTurnedRows + threadIdx.x;
+    if (n < n_sel) row_out[rowsel ? rowsel[n] : n] = out[n];
+  }
+  const int64_t at = static_cast<int64_t>(blockIdx.x) * kBlkElems;
+  const int r = static_cast<int>(blockIdx.y) * kTurnedRows + (threadIdx.x >> 3), c = (threadIdx.x & 7) * 8;
+  const float inv = r < n_sel ? inv_x[r] : 0.f, l2 = r < n_sel ? lse[r] * 1.44269504088896341f : 0.f;
+  float4 z[4][2];
+  if (inv != 0.f)
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+      for (int q = 0; q < 2; ++q) z[i][q] = *reinterpret_cast<const float4*>(Z + at + r * 256 + i * 64 + c + q * 4);
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    uint4 o = make_uint4(0u, 0u, 0u, 0u);
+    if (inv != 0.f) {
+      auto p = [&](float x) { return __builtin_amdgcn_exp2f(fmaf(x, 1.44269504088896341f, -l2)) * inv; };
+      o = make_uint4(pack_bf16x2(p(z[i][0].x), p(z[i][0].y)), pack_bf16x2(p(z[i][0].z), p(z[i][0].w)), pack_bf16x2(p(z[i][1].x), p(z[i][1].y)),
+                     pack_bf16x2(p(z[i][1].z), p(z[i][1].w)));
+    }
+    *reinterpret_cast<uint4*>(D + at + r * 256 + i * 64 + c) = o;
+  }
+  __syncthreads();
+  for (int i = threadIdx.x; i < kTurnedRows * T.k; i += 256) {
+    const int64_t n = static_cast<int64_t>(blockIdx.y) * kTurnedRows + i / T.k;
+    if (n >= n_sel || inv_x[n] == 0.f) continue;
+    const int id = T.ids[(rowsel ? rowsel[n] : n) * T.k + i % T.k];
+    const uint16_t e = entries[n * T.k + i % T.k];
+    if (e != kNoEntry && id >> 8 == static_cast<int>(blockIdx.x)) D[at + n * 256 + (id & 255)] = e;
+  }
+}
 // Blocks in which some logit lies far above its row's reference: dz is computed once more, its k entries on the way out.
 struct PutTargets {
   const int32_t *rowsel, *ids;
@@ -315,12 +510,16 @@ struct PutTargets {
 __global__ void __launch_bounds__(Cfg::T)
 k_target_flagged(const uint16_t* __restrict__ W, const uint16_t* __restrict__ H, int d, int V, const int32_t* __restrict__ rowsel, int64_t c0, int64_t mc,
                  const float* __restrict__ zero, PutTargets put, int tiles_m, int tiles_n, uint16_t* __restrict__ dZ, int64_t Vp,
-                 const int32_t* __restrict__ flags, const int32_t* __restrict__ cidx) {
+                 const int32_t* __restrict__ flags, const int32_t* __restrict__ cidx, StatArgs S) {
   __shared__ __attribute__((aligned(16))) uint16_t lds[kLogitLds / 2];
+  if (blockIdx.x >= kFlaggedGrid) {                          // the statistics, behind the last chunk's rows
+    target_stats<Cfg::T>(S, static_cast<int>(blockIdx.x) - kFlaggedGrid, reinterpret_cast<double*>(lds));
+    return;
+  }
   for (int tile_n = 0; tile_n < tiles_n; ++tile_n) {
     const int out_blk = cidx[(c0 >> 8) + tile_n];
     if (!flags[(c0 >> 8) + tile_n]) continue;                // the same for every thread of the grid
-    for (int tile_m = blockIdx.x; tile_m < tiles_m; tile_m += gridDim.x)
+    for (int tile_m = blockIdx.x; tile_m < tiles_m; tile_m += kFlaggedGrid)
       dz_tile(tile_m, tile_n, W, H, d, V, rowsel, c0, mc, put, put.lse, put.a, zero, dZ, Vp, out_blk, lds);
   }
 }
@@ -379,46 +578,9 @@ k_target_round(const float* __restrict__ sums, uint16_t* __restrict__ dW, int64_
   }
 }
 
-// ------------------------------------------------------------------ statistics and what closes a call
-struct StatArgs {
-  int64_t n_sel;
-  const int32_t *rowsel, *role;
-  const float *l, *w, *ent, *lse, *mass;
-  float norm;
-  umas_target_stats* stats;
-};
-constexpr int kCloseT = 256;
-// the model's record (k = 0) or a role's, a workgroup to each; sums in float64, in an order that does not depend on scheduling
-__device__ __forceinline__ void target_stats(const StatArgs& S, int k) {
-  __shared__ double smem[32];
-  double v[6] = {}, sum[6];
-  for (int64_t n = threadIdx.x; n < S.n_sel; n += kCloseT) {
-    if (k > 0 && S.role[S.rowsel ? S.rowsel[n] : n] != k - 1) continue;
-    const bool taught = S.mass[n] != 0.f;
-    const float w = S.w[n];
-    v[0] += w != 0.f ? static_cast<double>(w) * static_cast<double>(S.l[n]) : 0.0;
-    v[1] += static_cast<double>(w);
-    v[2] += taught ? static_cast<double>(S.ent[n]) : 0.0;
-    v[3] += taught ? static_cast<double>(S.lse[n]) : 0.0;
-    v[4] += 1.0;
-    v[5] += taught ? 0.0 : 1.0;
-  }
-#pragma unroll
-  for (int j = 0; j < 6; ++j) sum[j] = block_sum<double>(v[j], smem);
-  if (threadIdx.x != 0) return;
-  const double taught = sum[4] - sum[5];
-  umas_target_stats s;
-  s.loss = sum[4] > 0 ? static_cast<float>(sum[0] / (k == 0 ? static_cast<double>(S.norm) : sum[4])) : 0.f;
-  s.weight_mean = sum[4] > 0 ? static_cast<float>(sum[1] / sum[4]) : 0.f;
-  s.entropy_mean = taught > 0 ? static_cast<float>(sum[2] / taught) : 0.f;
-  s.lse_mean = taught > 0 ? static_cast<float>(sum[3] / taught) : 0.f;
-  s.n_scored = static_cast<int64_t>(sum[4]);
-  s.n_ignored = static_cast<int64_t>(sum[5]);
-  S.stats[k] = s;
-}
-struct CloseArgs {
-  StatArgs stats;
-  unsigned n_stats, reduce_rows;          // workgroups; 0: none
+// The sum of the slices of dH.
+struct ReduceArgs {
+  unsigned rows_pad;
   DhSlices sl;
   int tiles_r, tiles_d, d;
   const LiveInfo* info;
@@ -428,158 +590,69 @@ struct CloseArgs {
   int64_t c0, rows;
   const float* sc;
 };
-__global__ void __launch_bounds__(kCloseT)
-k_target_close(CloseArgs C) {
-  unsigned i = blockIdx.x;
-  if (i < C.n_stats) {
-    target_stats(C.stats, static_cast<int>(i));
-    return;
-  }
-  i -= C.n_stats;
-  dh_reduce<false>(i % C.reduce_rows, i / C.reduce_rows, C.sl, C.tiles_r, C.tiles_d, nullptr, C.d, C.info, C.blk_orig, C.dH, C.rowsel, C.c0, C.rows, nullptr,
-                   nullptr, C.sc);
+__global__ void __launch_bounds__(256)
+k_target_reduce(ReduceArgs C) {
+  dh_reduce<false>(blockIdx.x % C.rows_pad, blockIdx.x / C.rows_pad, C.sl, C.tiles_r, C.tiles_d, nullptr, C.d, C.info, C.blk_orig, C.dH, C.rowsel, C.c0, C.rows,
+                   nullptr, nullptr, C.sc);
 }
 
 // ------------------------------------------------------------------ float32, sums in float64
-struct OpenArgsF32 {
-  Teach A;
-  const float *H, *W;
-  RowArrays R;
-  double *zt, *tt, *mass;
-  float* h_rows;                          // [n_sel][d]: the rows that teach, zeros for the others, whatever they hold; NULL: no dW
-  uint32_t *dH, *row_out;
-  int64_t dh_words, n_rows;
-};
-__global__ void __launch_bounds__(256)
-k_target_open_f32(OpenArgsF32 O) {
-  const Teach& A = O.A;
-  if (O.dH) {
-    const int64_t stride = static_cast<int64_t>(gridDim.x) * 256;
-    for (int64_t i = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x; i < O.dh_words; i += stride) O.dH[i] = 0u;
-    for (int64_t i = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x; i < O.n_rows; i += stride) O.row_out[i] = 0u;
-  }
-  const int lane = threadIdx.x & 63, k = A.t.k;
-  const int64_t n = static_cast<int64_t>(blockIdx.x) * 4 + threadIdx.x / kWave;
-  if (n >= A.n_sel) return;
-  const int64_t row = A.rowsel ? A.rowsel[n] : n;
-  const Place<double> P = place_of<double>(A.t, A.V, row);
-  double z = 0.0;
-  for (unsigned long long left = __ballot(P.t != 0.0); left; left &= left - 1) {
-    const int j = __ffsll(static_cast<long long>(left)) - 1;
-    const float* w = O.W + static_cast<int64_t>(__shfl(P.id, j, kWave)) * A.d;
-    double s = 0.0;
-    for (int c = lane; c < A.d; c += kWave) s = fma(static_cast<double>(O.H[row * A.d + c]), static_cast<double>(w[c]), s);
-    s = wave_sum(s);
-    if (lane == j) z = s;
-  }
-  const double ts = mass_of_token(k, P.id, P.t);
-  const float weight = row_weight(A, row, P.mass != 0.0);
-  if (O.h_rows)
-    for (int c = lane; c < A.d; c += kWave) O.h_rows[n * A.d + c] = weight != 0.f ? O.H[row * A.d + c] : 0.f;
-  if (lane < k) {
-    O.zt[n * k + lane] = z;
-    O.tt[n * k + lane] = P.t != 0.0 ? ts : 0.0;
-  }
-  if (lane == 0) {
-    O.R.w[n] = weight;
-    O.R.mass[n] = static_cast<float>(P.mass);
-    O.mass[n] = P.mass;
-  }
-}
+// The scores keep the float64 logits of a chunk of rows (see k_score_f32) and leave the statistics of parts of the vocabulary; then a workgroup of a row and part
+// of the vocabulary merges the row's parts and takes its targets for itself, and turns its share of the logits into dz, the first one of the row leaving what else
+// there is to say of it; then the gradient products, of rows of H that are zeros where nothing is taught.
 struct DzArgsF32 {
   Teach A;
-  const float *H, *W;
+  const float* H;
   RowArrays R;
-  const double *z, *zt, *tt, *mass, *lse; // z: kept logits [n_sel][V] or NULL
+  const double* z;                        // [rows][V], of the chunk
+  const f32::Stat* part;
+  int splits;
   int64_t c0, rows;
   int per_wg;
-  float *dz, *row_out;
+  float *dz, *h_rows, *row_out;           // h_rows: of the chunk, NULL: no dW
 };
-// What a row's dz is made of; every lane gets the same.
-struct RowF32 {
-  double lse, g, a;                       // dz = a exp(z - lse) - g t
-};
-__device__ __forceinline__ RowF32 row_f32(const DzArgsF32& D, int64_t n) {
-  const float w = D.R.w[n];
-  const double lse = D.lse[n], g = static_cast<double>(w) / static_cast<double>(D.A.norm);
-  return RowF32{lse, g, g * dense_factor(D.mass[n], D.A.z_coef, lse)};
-}
-__device__ __forceinline__ void finish_row_f32(const DzArgsF32& D, int64_t n) {   // one wavefront: the row's loss
-  const int lane = threadIdx.x & 63, k = D.A.t.k;
-  const int64_t row = D.A.rowsel ? D.A.rowsel[n] : n;
-  const double lse = D.lse[n], z = lane < k ? D.zt[n * k + lane] : 0.0;
+__global__ void __launch_bounds__(256)
+k_target_dz_f32(DzArgsF32 D) {
+  const Teach& A = D.A;
+  const int lane = threadIdx.x & 63, k = A.t.k, V = A.V;
+  const int64_t m = blockIdx.y, n = D.c0 + m, row = A.rowsel ? A.rowsel[n] : n;
+  f32::Stat a = f32::empty_stat();
+  for (int p = lane; p < D.splits; p += kWave) a = f32::merge(a, D.part[p * D.rows + m]);
+  if (a.s == 0.0) a = f32::Stat{-INFINITY, 0.0, 0.0, 0.0, 0.0};
+  const double most = wave_max(a.m), e = a.s == 0.0 ? 0.0 : exp(a.m - most), s = wave_sum(a.s * e);
+  const double lse = most + log(s), ent = lse - wave_sum(a.t * e) / s;
+  const Place<double> P = place_of<double>(A.t, V, row);
+  const bool taught = P.mass != 0.0;
+  const float w = row_weight(A, row, taught);
+  const double g = static_cast<double>(w) / static_cast<double>(A.norm), f = g * dense_factor(P.mass, A.z_coef, lse);
+  const double ts = mass_of_token(k, P.id, P.t), z = P.t != 0.0 ? D.z[m * V + P.id] : 0.0;
+  const int v0 = blockIdx.x * D.per_wg, v1 = min(v0 + D.per_wg, V);
+  for (int vb = v0; vb < v1; vb += 1024)
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      const int v = vb + q * 256 + threadIdx.x;
+      if (v < v1) D.dz[m * V + v] = g != 0.0 ? static_cast<float>(f * exp(D.z[m * V + v] - lse)) : 0.f;
+    }
+  __syncthreads();
+  if (threadIdx.x < kWave && P.t != 0.0 && g != 0.0 && P.id >= v0 && P.id < v1) D.dz[m * V + P.id] = static_cast<float>(f * exp(z - lse) - g * ts);
+  if (blockIdx.x != 0) return;
+  if (D.h_rows)
+    for (int c = threadIdx.x; c < A.d; c += 256) D.h_rows[m * A.d + c] = w != 0.f ? D.H[row * A.d + c] : 0.f;
+  if (threadIdx.x >= kWave) return;
   double l = 0.0, out = 0.0;
-  const bool taught = D.mass[n] != 0.0;
-  if (taught && !D.A.t.logits) {
+  if (taught && !A.t.logits) {
     out = __shfl(z, 0, kWave) - lse;
-    l = -out + static_cast<double>(D.A.z_coef) * lse * lse;
+    l = -out + static_cast<double>(A.z_coef) * lse * lse;
   } else if (taught) {
-    const Place<double> P = place_of<double>(D.A.t, D.A.V, row);
     out = l = wave_sum(P.t != 0.0 ? P.t * (log(P.t) - (z - lse)) : 0.0);
   }
-  if (lane == 0) {
-    D.R.l[n] = static_cast<float>(l);
-    if (D.row_out) D.row_out[row] = static_cast<float>(out);
-  }
-}
-__device__ __forceinline__ void put_targets_f32(const DzArgsF32& D, int64_t n, const RowF32& r, int v0, int v1, int j) {
-  const int k = D.A.t.k, id = D.A.t.ids[(D.A.rowsel ? D.A.rowsel[n] : n) * k + j];
-  const double t = D.tt[n * k + j];
-  if (id < v0 || id >= v1 || !(t != 0.0) || r.g == 0.0) return;
-  D.dz[(n - D.c0) * D.A.V + id] = static_cast<float>(r.a * exp(D.zt[n * k + j] - r.lse) - r.g * t);
-}
-// From kept logits: a workgroup to a row and a part of the vocabulary.
-__global__ void __launch_bounds__(256)
-k_target_dz_kept_f32(DzArgsF32 D) {
-  const int64_t m = blockIdx.y, n = D.c0 + m;
-  const int V = D.A.V, v0 = blockIdx.x * D.per_wg, v1 = min(v0 + D.per_wg, V);
-  if (blockIdx.x == 0 && threadIdx.x < kWave) finish_row_f32(D, n);
-  const RowF32 r = row_f32(D, n);
-  for (int v = v0 + threadIdx.x; v < v1; v += 256) D.dz[m * V + v] = r.g != 0.0 ? static_cast<float>(r.a * exp(D.z[n * V + v] - r.lse)) : 0.f;
-  __syncthreads();
-  if (static_cast<int>(threadIdx.x) < D.A.t.k) put_targets_f32(D, n, r, v0, v1, threadIdx.x);
-}
-// Computed once more: tiles as in the scores.
-__global__ void __launch_bounds__(f32::kWaves* kWave)
-k_target_dz_f32(DzArgsF32 D) {
-  using namespace f32;
-  const int wave = threadIdx.x >> 6, V = D.A.V, d = D.A.d;
-  const int64_t n0 = static_cast<int64_t>(blockIdx.y) * kTile, vb = static_cast<int64_t>(blockIdx.x) * kVocBlock;
-  if (blockIdx.x == 0)
-    for (int64_t m = n0 + wave; m < min(n0 + kTile, D.rows); m += kWaves) finish_row_f32(D, D.c0 + m);
-  if (vb + wave * kTile < V) {
-    const int v0 = static_cast<int>(vb) + wave * kTile;
-    Rows<2> h, w;
-    h.vec = w.vec = d % 4 == 0;
-#pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      const int64_t n = D.c0 + min(n0 + blk_index(i), D.rows - 1);
-      h.p[i] = D.H + (D.A.rowsel ? D.A.rowsel[n] : n) * static_cast<int64_t>(d);
-      w.p[i] = D.W + static_cast<int64_t>(min(v0 + blk_index(i), V - 1)) * d;
-    }
-    double4v acc[2][2];
-    zero<2>(acc);
-    product<2>(h, w, 0, d, d, acc);
-#pragma unroll
-    for (int i = 0; i < 2; ++i)
-#pragma unroll
-      for (int r = 0; r < 4; ++r) {
-        const int64_t m = n0 + blk_row(i, r);
-        if (m >= D.rows) continue;
-        const RowF32 x = row_f32(D, D.c0 + m);
-#pragma unroll
-        for (int j = 0; j < 2; ++j) {
-          const int v = v0 + blk_index(j);
-          if (v < V) D.dz[m * V + v] = x.g != 0.0 ? static_cast<float>(x.a * exp(acc[i][j][r] - x.lse)) : 0.f;
-        }
-      }
-  }
-  __syncthreads();
-  const int k = D.A.t.k;
-  for (int i = threadIdx.x; i < kTile * k; i += kWaves * kWave) {
-    const int64_t m = n0 + i / k;
-    if (m < D.rows) put_targets_f32(D, D.c0 + m, row_f32(D, D.c0 + m), static_cast<int>(vb), static_cast<int>(min<int64_t>(vb + kVocBlock, V)), i % k);
-  }
+  if (lane != 0) return;
+  D.R.l[n] = static_cast<float>(l);
+  D.R.w[n] = w;
+  D.R.mass[n] = static_cast<float>(P.mass);
+  D.R.lse[n] = taught ? static_cast<float>(lse) : 0.f;
+  D.R.ent[n] = taught ? static_cast<float>(ent) : 0.f;
+  if (D.row_out) D.row_out[row] = static_cast<float>(out);
 }
 
 // ------------------------------------------------------------------ host side
@@ -588,8 +661,6 @@ struct Ws {
   RowArrays R;
   int32_t *flags, *blk_cidx, *blk_orig;
   LiveInfo* live;
-  double *zt, *tt, *mass, *rest, *lse64;  // float32
-  float *logp_c, *h_rows;
   char* chunk;
   size_t fixed_bytes;
 };
@@ -602,27 +673,29 @@ void carve(Carver& c, Ws& w, int64_t n_sel, int d, int V, int k, umas_dtype dt) 
   if (bf) {
     w.R.zt = c.take<float>(static_cast<size_t>(n_pad) * k);
     w.R.tt = c.take<float>(static_cast<size_t>(n_pad) * k);
+    w.R.entries = reinterpret_cast<uint16_t*>(w.R.tt);       // one or the other
     w.flags = c.take<int32_t>(cdiv(n_pad, 256));
     w.blk_cidx = c.take<int32_t>(cdiv(n_pad, 256));
     w.blk_orig = c.take<int32_t>(cdiv(n_pad, 256));
     w.live = c.take<LiveInfo>(1);
-  } else {
-    w.zt = c.take<double>(static_cast<size_t>(n_pad) * k);
-    w.tt = c.take<double>(static_cast<size_t>(n_pad) * k);
-    w.mass = c.take<double>(n_pad);
-    w.rest = c.take<double>(n_pad);
-    w.lse64 = c.take<double>(n_pad);
-    w.logp_c = c.take<float>(n_pad);
-    w.h_rows = c.take<float>(static_cast<size_t>(n_pad) * d);
   }
   w.chunk = c.base ? c.base + c.off : nullptr;
   w.fixed_bytes = c.off;
 }
+// A block of rows keeps its float32 logits; dH's partial sums take their place later.
+constexpr int64_t kFewTaught = 256;
+size_t few_bytes(int64_t n_sel, int V, umas_dtype dt) { return dt == UMAS_BF16 && n_sel <= kFewTaught ? static_cast<size_t>(256) * round_up(V, 256) * sizeof(float) : 0; }
 // float32 sums of dW where it is bf16 and comes from several chunks
 size_t sum_bytes(int d, int V, int dW_type) { return dW_type == UMAS_BF16 ? align_up(static_cast<size_t>(V) * d * sizeof(float)) : 0; }
-size_t kept_f32_bytes(int64_t n_sel, int V) {
-  const double b = static_cast<double>(n_sel) * V * sizeof(double);
-  return b <= 1073741824.0 ? align_up(static_cast<size_t>(n_sel) * V * sizeof(double)) : 0;
+// float32: a chunk's dz, its rows of H, its float64 logits and the statistics of their parts.  256 MiB of logits to a chunk, what the memory-side cache holds,
+// is as many as it takes to fill the chip.
+size_t f32_bytes(int64_t mc, int d, int V) {
+  return align_up(static_cast<size_t>(mc) * V * sizeof(float)) + align_up(static_cast<size_t>(mc) * d * sizeof(float)) +
+         align_up(static_cast<size_t>(mc) * V * sizeof(double)) + align_up(static_cast<size_t>(f32::part_plan(mc, V).splits) * mc * sizeof(f32::Stat));
+}
+int64_t f32_rows(int64_t n_sel, int V) {
+  const int64_t fit = static_cast<int64_t>((size_t{256} << 20) / (static_cast<size_t>(V) * sizeof(double)));
+  return std::min(std::max<int64_t>(n_sel, 1), std::min(std::max<int64_t>(fit, 256), kF32ChunkRows));
 }
 bool sizes_ok(int64_t n_sel, int d, int V, int k, int dW_type) {
   return n_sel >= 0 && d >= 1 && V >= 1 && k >= 1 && k <= UMAS_MAX_TOP && dW_type >= UMAS_NO_DW && dW_type <= UMAS_BF16;
@@ -633,25 +706,25 @@ size_t least_bytes(int64_t n_sel, int d, int V, int k, umas_dtype dt, int dW_typ
   Ws w;
   carve(c, w, n_sel, d, V, k, dt);
   const int64_t all = std::max<int64_t>(n_sel, 1), mc = std::min<int64_t>(all, 256);
+  if (dt == UMAS_F32) return c.off + f32_bytes(std::min<int64_t>(all, 32), d, V);
   const size_t chunked = chunk_bytes(mc, d, V, dt) + (n_sel > 256 ? sum_bytes(d, V, dW_type) : 0);
   // the sums of chunks can take more than one chunk of all rows
-  return c.off + (all <= (dt == UMAS_F32 ? kF32ChunkRows : kMaxChunkRows) ? std::min(chunked, chunk_bytes(all, d, V, dt)) : chunked);
+  return c.off + (all <= kMaxChunkRows ? std::min(chunked, chunk_bytes(all, d, V, dt)) : chunked) + few_bytes(all, V, dt);
 }
 size_t full_bytes(int64_t n_sel, int d, int V, int k, umas_dtype dt, int dW_type) {
   if (!sizes_ok(n_sel, d, V, k, dW_type)) return 0;
   Carver c(nullptr);
   Ws w;
   carve(c, w, n_sel, d, V, k, dt);
+  if (dt == UMAS_F32) return c.off + f32_bytes(f32_rows(n_sel, V), d, V);
   int64_t mc = std::max<int64_t>(n_sel, 1);
-  const int64_t cap = dt == UMAS_F32 ? kF32ChunkRows : kMaxChunkRows;
   size_t sums = 0;
-  if (mc > cap) {
-    const int64_t nchunk = (mc + cap - 1) / cap;
+  if (mc > kMaxChunkRows) {
+    const int64_t nchunk = (mc + kMaxChunkRows - 1) / kMaxChunkRows;
     mc = round_up((mc + nchunk - 1) / nchunk, 256);
     sums = sum_bytes(d, V, dW_type);
   }
-  if (dt == UMAS_F32) return c.off + chunk_bytes(mc, d, V, dt) + kept_f32_bytes(n_sel, V) + align_up(f32::score_room(n_sel, V));
-  return c.off + chunk_bytes(mc, d, V, dt) + full_part_bytes(n_sel, mc, d, V) + sums;
+  return c.off + chunk_bytes(mc, d, V, dt) + std::max(full_part_bytes(n_sel, mc, d, V), few_bytes(mc, V, dt)) + sums;
 }
 
 struct Call {
@@ -702,41 +775,45 @@ umas_status run_f32(const Call& a, const Ws& w, const Teach& A) {
   hipStream_t st = a.st;
   const float *H = static_cast<const float*>(a.H), *W = static_cast<const float*>(a.W);
   const size_t room = a.workspace_bytes - w.fixed_bytes;
-  const int64_t n = a.n_sel, cap = std::min<int64_t>(n, kF32ChunkRows);
-  int64_t mc = cap;
-  if (chunk_bytes(mc, a.d, a.V, UMAS_F32) > room) mc = std::max<int64_t>(static_cast<int64_t>(room / chunk_bytes(256, a.d, a.V, UMAS_F32)) * 256, 256);
-  mc = std::min(mc, n);
-  const size_t z_at = chunk_bytes(mc, a.d, a.V, UMAS_F32), z_bytes = kept_f32_bytes(n, a.V);
-  double* const z = z_bytes > 0 && z_at + z_bytes <= room ? reinterpret_cast<double*>(w.chunk + z_at) : nullptr;
-  hipLaunchKernelGGL(k_target_open_f32, dim3(cdiv(n, 4)), dim3(256), 0, st,
-                     OpenArgsF32{A, H, W, w.R, w.zt, w.tt, w.mass, a.dW ? w.h_rows : nullptr, a.rowsel ? static_cast<uint32_t*>(a.dH) : nullptr, reinterpret_cast<uint32_t*>(a.row_out),
-                                 a.n_rows * a.d, a.row_out ? a.n_rows : 0});
-  UMAS_LAUNCHED("k_target_open_f32");
-  char* const parts = z ? w.chunk + z_at + z_bytes : w.chunk;
-  umas_status s = f32::score(W, H, a.d, a.V, a.rowsel, n, nullptr, parts, room - static_cast<size_t>(parts - w.chunk),
-                             f32::ScoreOut{z, w.rest, w.logp_c, w.R.lse, w.R.ent, nullptr, nullptr, nullptr, w.lse64}, st);
-  if (s != UMAS_OK) return s;
+  const int64_t n = a.n_sel;
+  int64_t mc = f32_rows(n, a.V);
+  while (mc > 32 && f32_bytes(mc, a.d, a.V) > room) mc = std::max<int64_t>(mc / 2, 32);
+  const f32::PartPlan plan = f32::part_plan(mc, a.V);   // of every chunk
   for (int64_t c0 = 0; c0 < n; c0 += mc) {
     const int64_t rows = std::min(mc, n - c0);
-    DzArgsF32 D{A, H, W, w.R, z, w.zt, w.tt, w.mass, w.lse64, c0, rows, 0, reinterpret_cast<float*>(w.chunk), a.row_out};
-    if (z) {
-      const unsigned wgs = cdiv(2048, static_cast<size_t>(rows)), most = cdiv(a.V, 1024);
-      D.per_wg = static_cast<int>(cdiv(most, std::min(wgs, most))) * 1024;
-      hipLaunchKernelGGL(k_target_dz_kept_f32, dim3(cdiv(a.V, D.per_wg), static_cast<unsigned>(rows)), dim3(256), 0, st, D);
-      UMAS_LAUNCHED("k_target_dz_kept_f32");
-    } else {
-      hipLaunchKernelGGL(k_target_dz_f32, dim3(cdiv(a.V, f32::kVocBlock), cdiv(rows, f32::kTile)), dim3(f32::kWaves * kWave), 0, st, D);
-      UMAS_LAUNCHED("k_target_dz_f32");
+    Carver c(w.chunk);
+    float* const dz = c.take<float>(static_cast<size_t>(rows) * a.V);
+    float* const h_rows = c.take<float>(static_cast<size_t>(rows) * a.d);
+    double* const z = c.take<double>(static_cast<size_t>(rows) * a.V);
+    f32::Stat* const part = c.take<f32::Stat>(static_cast<size_t>(plan.splits) * rows);
+    ClearArgs clear{};
+    unsigned n_clear = 0;                    // in rows of the grid
+    if (a.rowsel && c0 == 0) {
+      clear = ClearArgs{{reinterpret_cast<uint32_t*>(a.row_out), static_cast<uint32_t*>(a.dH), nullptr}, {a.n_rows, a.n_rows * a.d, 0}};
+      const unsigned wg = cdiv(static_cast<size_t>(a.n_rows) * a.d, 2048);
+      n_clear = cdiv(std::min(wg, 1024u), cdiv(rows, plan.side));
     }
-    f32::launch_gradients(f32::GradArgs{D.dz, W, H, a.d, a.V, a.rowsel, c0, static_cast<int>(rows), a.accumulate_dW || c0 > 0 ? 1 : 0,
-                                        static_cast<float*>(a.dH), static_cast<float*>(a.dW), 0, 0, 0, w.h_rows + c0 * a.d}, f32::StatArgs{}, st);
+    const f32::ScoreOut out{z, nullptr, nullptr, nullptr, nullptr, nullptr, nullptr, nullptr};
+    const float* const Hc = a.rowsel ? H : H + c0 * a.d;
+    const dim3 grid(cdiv(rows, plan.side), plan.splits + n_clear);
+    auto score = [&](auto kernel) {
+      hipLaunchKernelGGL(kernel, grid, dim3(f32::kWaves * kWave), 0, st, W, Hc, a.d, a.V, a.rowsel ? a.rowsel + c0 : nullptr, rows, nullptr, part, out, plan.splits,
+                         clear);
+    };
+    if (plan.side == f32::kTile) score(f32::k_score_f32<true, 2>);
+    else score(f32::k_score_f32<true, 1>);
+    UMAS_LAUNCHED("k_score_f32");
+    const unsigned wgs = cdiv(2048, static_cast<size_t>(rows)), most = cdiv(a.V, 1024);      // eight workgroups to a compute unit
+    const int per_wg = static_cast<int>(cdiv(most, std::min(wgs, most))) * 1024;
+    hipLaunchKernelGGL(k_target_dz_f32, dim3(cdiv(a.V, per_wg), static_cast<unsigned>(rows)), dim3(256), 0, st,
+                       DzArgsF32{A, H, w.R, z, part, plan.splits, c0, rows, per_wg, dz, a.dW ? h_rows : nullptr, a.row_out});
+    UMAS_LAUNCHED("k_target_dz_f32");
+    f32::launch_gradients(f32::GradArgs{dz, W, H, a.d, a.V, a.rowsel, c0, static_cast<int>(rows), a.accumulate_dW || c0 > 0 ? 1 : 0,
+                                        static_cast<float*>(a.dH), static_cast<float*>(a.dW), 0, 0, 0, h_rows}, f32::StatArgs{}, st);
     UMAS_LAUNCHED("k_target_gradients_f32");
   }
-  CloseArgs C{};
-  C.stats = stat_args(a, w, A.norm);
-  C.n_stats = 1 + a.n_roles;
-  hipLaunchKernelGGL(k_target_close, dim3(C.n_stats), dim3(kCloseT), 0, st, C);
-  UMAS_LAUNCHED("k_target_close");
+  hipLaunchKernelGGL(k_target_stats, dim3(1 + a.n_roles), dim3(256), 0, st, stat_args(a, w, A.norm));
+  UMAS_LAUNCHED("k_target_stats");
   return UMAS_OK;
 }
 
@@ -763,6 +840,7 @@ umas_status run_bf16(const Call& a, const Ws& w, const Teach& A) {
   }
   UMAS_REQUIRE(chunk_bytes(std::min(mc, n_sel), d, V, UMAS_BF16) <= room, UMAS_EWORKSPACE, "workspace cannot hold one chunk of %lld rows", static_cast<long long>(mc));
   const bool no_dw = a.dW_type == UMAS_NO_DW;
+  const StatArgs stats = stat_args(a, w, A.norm);
   auto plan = [&](int64_t rows, DhSlices* sl) {             // as in the policy update: partial sums behind the chunk's operands or in the place of the scores' parts
     const size_t used = chunk_bytes(rows, d, V, UMAS_BF16), behind = room > used ? room - used : 0;
     const size_t front = static_cast<size_t>(reinterpret_cast<char*>(w.R.lse) - reinterpret_cast<char*>(w.partial));
@@ -783,7 +861,28 @@ umas_status run_bf16(const Call& a, const Ws& w, const Teach& A) {
     DhSlices sl;
     const bool dw_apart = plan(rows, &sl);
     const LiveArgs live = live_args(c0, rows, sl.n, dw_apart);
-    if (c0 == 0) {
+    const bool few = n_sel <= kFewTaught;
+    const bool narrow = n_sel <= NarrowCfg::BN;
+    const int64_t n_pad = round_up(n_sel, narrow ? NarrowCfg::BN : Cfg::BN);
+    const int tiles_m = narrow ? static_cast<int>(Vp / NarrowCfg::BM) : tiles_v;
+    if (few) {
+      float* const Z = reinterpret_cast<float*>(chunk + chunk_bytes(rows, d, V, UMAS_BF16));
+      if (narrow)
+        hipLaunchKernelGGL(k_target_logits_narrow, dim3(tile_grid<kGM, kGN>(tiles_m, 1, kGN, kTilesPerWg)), dim3(NarrowCfg::T), 0, st, W, H, d, V, a.rowsel, n_sel,
+                           a.t.ids, tiles_m, w.partial, n_pad, Z, Vp);
+      else
+        hipLaunchKernelGGL(k_target_logits, score_grid(tiles_v, 1, kGN, halved), dim3(Cfg::T), 0, st, W, H, d, V, a.rowsel, n_sel, a.t.ids, tiles_v, halved, w.partial,
+                           n_pad, Z, Vp);
+      UMAS_LAUNCHED(narrow ? "k_target_logits_narrow" : "k_target_logits");
+      const unsigned clearing = a.rowsel ? 256 : 0;
+      hipLaunchKernelGGL(k_target_few, dim3(1 + clearing + cdiv(n_sel, 8)), dim3(256), 0, st,
+                         FewArgs{A, H, w.R, w.R.cref, w.R.entries, w.partial, tiles_m, n_pad, Z, Hs, mcp, a.row_out, live, clearing, static_cast<uint32_t*>(a.dH),
+                                 a.n_rows * static_cast<int64_t>(d) / 2, a.n_rows});
+      UMAS_LAUNCHED("k_target_few");
+      hipLaunchKernelGGL(k_target_turn, dim3(tiles_v + 1 + a.n_roles, static_cast<unsigned>(round_up(n_sel, 64) / kTurnedRows)), dim3(256), 0, st, Z, w.R.lse, w.R.cref, w.R.entries, A.t,
+                         a.rowsel, n_sel, E, w.R.a, a.row_out, tiles_v, stats);
+      UMAS_LAUNCHED("k_target_turn");
+    } else if (c0 == 0) {
       const OpenArgs O{A, H, W, w.R, w.flags, static_cast<int>(cdiv(n_sel, 256)), live, a.rowsel ? static_cast<uint32_t*>(a.dH) : nullptr,
                        a.n_rows * static_cast<int64_t>(d) / 2, a.row_out, a.row_out ? a.n_rows : 0};
       hipLaunchKernelGGL(k_target_open, dim3(1 + std::min<unsigned>(std::max<unsigned>(cdiv(n_sel, 4), a.rowsel ? 1024 : 1), 8192)), dim3(256), 0, st, O);
@@ -792,23 +891,18 @@ umas_status run_bf16(const Call& a, const Ws& w, const Teach& A) {
       hipLaunchKernelGGL(k_live_scan, dim3(1), dim3(512), 0, st, live);
       UMAS_LAUNCHED("k_live_scan");
     }
-    const bool narrow = n_sel <= NarrowCfg::BN;
-    const int64_t n_pad = round_up(n_sel, narrow ? NarrowCfg::BN : Cfg::BN);
-    const int tiles_m = narrow ? static_cast<int>(Vp / NarrowCfg::BM) : tiles_v;
-    if (narrow)
-      hipLaunchKernelGGL(k_target_narrow, dim3(tile_grid<kGM, kGN>(tiles_m, 1, kGN, kTilesPerWg)), dim3(NarrowCfg::T), 0, st, W, H, d, V, a.rowsel, rows,
-                         tiles_m, w.partial, n_pad, w.R.cref, E, Vp, w.flags, w.blk_cidx);
-    else
+    if (!few) {
       hipLaunchKernelGGL(k_target_tiles, score_grid(tiles_v, tiles_r, panel, halved), dim3(Cfg::T), 0, st, W, H, d, V, a.rowsel, c0, rows, tiles_v, tiles_r,
                          panel, halved, w.partial, n_pad, w.R.cref, E, Vp, w.flags, w.blk_cidx);
-    UMAS_LAUNCHED(narrow ? "k_target_narrow" : "k_target_tiles");
-    hipLaunchKernelGGL(k_target_rows, dim3(cdiv(rows, 8)), dim3(256), 0, st,
-                       RowsArgs{A, H, w.R, w.partial, tiles_m, n_pad, c0, rows, w.flags, w.blk_cidx, E, tiles_v, Hs, mcp, a.row_out});
-    UMAS_LAUNCHED("k_target_rows");
-    const PutTargets put{a.rowsel, a.t.ids, a.t.k, w.R.zt, w.R.tt, w.R.lse, w.R.a, w.R.w, A.norm};
-    hipLaunchKernelGGL(k_target_flagged, dim3(kFlaggedGrid), dim3(Cfg::T), 0, st, W, H, d, V, a.rowsel, c0, rows, w.R.zero, put, tiles_v, tiles_r, E, Vp,
-                       w.flags, w.blk_cidx);
-    UMAS_LAUNCHED("k_target_flagged");
+      UMAS_LAUNCHED("k_target_tiles");
+      hipLaunchKernelGGL(k_target_rows, dim3(cdiv(rows, 8)), dim3(256), 0, st,
+                         RowsArgs{A, H, w.R, w.partial, tiles_m, n_pad, c0, rows, w.flags, w.blk_cidx, E, tiles_v, Hs, mcp, a.row_out});
+      UMAS_LAUNCHED("k_target_rows");
+      const PutTargets put{a.rowsel, a.t.ids, a.t.k, w.R.zt, w.R.tt, w.R.lse, w.R.a, w.R.w, A.norm};
+      hipLaunchKernelGGL(k_target_flagged, dim3(kFlaggedGrid + (c0 + rows >= n_sel ? 1 + a.n_roles : 0)), dim3(Cfg::T), 0, st, W, H, d, V, a.rowsel, c0, rows, w.R.zero, put, tiles_v, tiles_r, E, Vp,
+                         w.flags, w.blk_cidx, stats);
+      UMAS_LAUNCHED("k_target_flagged");
+    }
     const int add = c0 > 0 || (a.accumulate_dW && !sums) ? 1 : 0;
     const GradientArgs G{E, Vp, mcp, W, Hs, d, V, tiles_v, tiles_d, sl, tiles_r, w.live, w.blk_orig, static_cast<uint16_t*>(a.dH), add, a.rowsel, c0, rows, w.R.sc};
     const unsigned grid = static_cast<unsigned>(round_up(device_cus(), 8));
@@ -822,30 +916,10 @@ umas_status run_bf16(const Call& a, const Ws& w, const Teach& A) {
       else hipLaunchKernelGGL(k_target_dw_short_bf16, g2, dim3(ShortCfg::T), 0, st, G, tiles_n, static_cast<uint16_t*>(a.dW));
       UMAS_LAUNCHED("k_target_dw_short");
     }
-    CloseArgs C{};
-    if (c0 + rows >= n_sel) {
-      C.stats = stat_args(a, w, A.norm);
-      C.n_stats = 1 + a.n_roles;
-    }
-    unsigned wgs = C.n_stats;
     if (sl.n > 1) {
-      C.reduce_rows = static_cast<unsigned>(mcp);
-      C.sl = sl;
-      C.tiles_r = tiles_r;
-      C.tiles_d = tiles_d;
-      C.d = d;
-      C.info = w.live;
-      C.blk_orig = w.blk_orig;
-      C.dH = static_cast<uint16_t*>(a.dH);
-      C.rowsel = a.rowsel;
-      C.c0 = c0;
-      C.rows = rows;
-      C.sc = w.R.sc;
-      wgs += C.reduce_rows * cdiv(d, 1024);
-    }
-    if (wgs) {
-      hipLaunchKernelGGL(k_target_close, dim3(wgs), dim3(kCloseT), 0, st, C);
-      UMAS_LAUNCHED("k_target_close");
+      hipLaunchKernelGGL(k_target_reduce, dim3(static_cast<unsigned>(mcp) * cdiv(d, 1024)), dim3(256), 0, st,
+                         ReduceArgs{static_cast<unsigned>(mcp), sl, tiles_r, tiles_d, d, w.live, w.blk_orig, static_cast<uint16_t*>(a.dH), a.rowsel, c0, rows, w.R.sc});
+      UMAS_LAUNCHED("k_target_reduce");
     }
   }
   if (sums) {
@@ -871,11 +945,8 @@ umas_status run(const Call& a) {
     const size_t esz = a.dt == UMAS_BF16 ? 2 : 4, dw = static_cast<size_t>(a.V) * a.d * (a.dW_type == UMAS_BF16 ? 2 : 4);
     UMAS_HIP(clear_bytes(st, a.n_rows > 0 ? a.dH : nullptr, static_cast<size_t>(a.n_rows) * a.d * esz, a.row_out, static_cast<size_t>(a.n_rows) * 4,
                          a.accumulate_dW ? nullptr : a.dW, dw));
-    CloseArgs C{};
-    C.stats = stat_args(a, w, norm);
-    C.n_stats = 1 + a.n_roles;
-    hipLaunchKernelGGL(k_target_close, dim3(C.n_stats), dim3(kCloseT), 0, st, C);
-    UMAS_LAUNCHED("k_target_close");
+    hipLaunchKernelGGL(k_target_stats, dim3(1 + a.n_roles), dim3(256), 0, st, stat_args(a, w, norm));
+    UMAS_LAUNCHED("k_target_stats");
     return UMAS_OK;
   }
   return a.dt == UMAS_F32 ? run_f32(a, w, A) : run_bf16(a, w, A);
