@@ -724,7 +724,9 @@ size_t full_bytes(int64_t n_sel, int d, int V, int k, umas_dtype dt, int dW_type
     mc = round_up((mc + nchunk - 1) / nchunk, 256);
     sums = sum_bytes(d, V, dW_type);
   }
-  return c.off + chunk_bytes(mc, d, V, dt) + std::max(full_part_bytes(n_sel, mc, d, V), few_bytes(mc, V, dt)) + sums;
+  // (a frozen head: room for what plan_dh_alone may want, up to four rounds of pieces)
+  const size_t parts = dW_type == UMAS_NO_DW ? std::min<size_t>(static_cast<size_t>(dh_tiles(mc, d)) * cdiv(V, 256), 1024) * (256 * 256 * sizeof(float)) : full_part_bytes(n_sel, mc, d, V);
+  return c.off + chunk_bytes(mc, d, V, dt) + std::max(parts, few_bytes(mc, V, dt)) + sums;
 }
 
 struct Call {
@@ -844,8 +846,9 @@ umas_status run_bf16(const Call& a, const Ws& w, const Teach& A) {
   auto plan = [&](int64_t rows, DhSlices* sl) {             // as in the policy update: partial sums behind the chunk's operands or in the place of the scores' parts
     const size_t used = chunk_bytes(rows, d, V, UMAS_BF16), behind = room > used ? room - used : 0;
     const size_t front = static_cast<size_t>(reinterpret_cast<char*>(w.R.lse) - reinterpret_cast<char*>(w.partial));
-    const size_t have = slices_dh(n_sel, mc, d) ? std::max(behind, front) : 0;
-    const GradPlan p = no_dw ? GradPlan{plan_dh((rows + 255) / 256, tiles_d, tiles_v, have, true), false} : plan_gradients(n_sel, rows, d, V, have);
+    const size_t have = std::max(behind, front);
+    const GradPlan p = no_dw ? GradPlan{plan_dh_alone(static_cast<int64_t>(cdiv(rows, 256)) * tiles_d, tiles_v, device_cus(), have), false}
+                             : plan_gradients(n_sel, rows, d, V, slices_dh(n_sel, mc, d) ? have : 0);
     *sl = DhSlices{p.dh.slices, p.dh.voc_blks, behind > front ? reinterpret_cast<float*>(chunk + used) : reinterpret_cast<float*>(w.partial)};
     return p.dw_apart;
   };

@@ -194,7 +194,17 @@ __device__ __forceinline__ void top_tile(const uint16_t* __restrict__ W, const u
 template <class C, bool ALL>
 __device__ __forceinline__ void top_tiles(const uint16_t* __restrict__ W, const uint16_t* __restrict__ H, int d, int V, const int32_t* __restrict__ rowsel,
                                           int64_t c0, int64_t mc, int first, int tiles_m, int tiles_n, int panel, const Groups& out,
-                                          const float* __restrict__ bound, uint16_t* lds) {
+                                          const float* __restrict__ bound, uint16_t* lds, int halved = 0) {
+  if constexpr (C::BM == 256 && C::BN == 256) {
+    if (halved > 0) {                                        // the last tiles of every XCD in two halves of 128 rows (see score_tiles)
+      const int per_xcd = (tiles_m * tiles_n + 7) / 8, xcd = static_cast<int>(blockIdx.x & 7), w = static_cast<int>(blockIdx.x >> 3), whole = per_xcd - halved;
+      if (w >= whole) {
+        const int in_xcd = whole + (w - whole) / 2, t = xcd * per_xcd + in_xcd, tile_m = t / tiles_n, half = t % tiles_n * 2 + ((w - whole) & 1);
+        if (in_xcd < per_xcd && tile_m < tiles_m && half * HalfCfg::BN < mc) top_tile<HalfCfg, ALL>(W, H, d, V, rowsel, c0, mc, first + tile_m, half, false, out, bound, lds);
+        return;
+      }
+    }
+  }
   const bool w_once = tiles_n == 1 && beyond_cache(d, V, kLogitsOnceBytes);
   for (int it = 0; it < kTilesPerWg; ++it) {
     int tile_m, tile_n;
@@ -204,15 +214,15 @@ __device__ __forceinline__ void top_tiles(const uint16_t* __restrict__ W, const 
 }
 __global__ void __launch_bounds__(Cfg::T)
 k_top_tiles(const uint16_t* __restrict__ W, const uint16_t* __restrict__ H, int d, int V, const int32_t* __restrict__ rowsel, int64_t c0, int64_t mc,
-            int tiles_m, int tiles_n, int panel, Groups out) {
+            int tiles_m, int tiles_n, int panel, int halved, Groups out) {
   __shared__ __attribute__((aligned(16))) uint16_t lds[kLogitLds / 2];
-  top_tiles<Cfg, true>(W, H, d, V, rowsel, c0, mc, 0, tiles_m, tiles_n, panel, out, nullptr, lds);
+  top_tiles<Cfg, true>(W, H, d, V, rowsel, c0, mc, 0, tiles_m, tiles_n, panel, out, nullptr, lds, halved);
 }
 __global__ void __launch_bounds__(Cfg::T)
 k_top_tiles_bound(const uint16_t* __restrict__ W, const uint16_t* __restrict__ H, int d, int V, const int32_t* __restrict__ rowsel, int64_t c0, int64_t mc,
-                  int first, int tiles_m, int tiles_n, int panel, Groups out, const float* __restrict__ bound) {
+                  int first, int tiles_m, int tiles_n, int panel, int halved, Groups out, const float* __restrict__ bound) {
   __shared__ __attribute__((aligned(16))) uint16_t lds[kLogitLds / 2];
-  top_tiles<Cfg, false>(W, H, d, V, rowsel, c0, mc, first, tiles_m, tiles_n, panel, out, bound, lds);
+  top_tiles<Cfg, false>(W, H, d, V, rowsel, c0, mc, first, tiles_m, tiles_n, panel, out, bound, lds, halved);
 }
 __global__ void __launch_bounds__(NarrowCfg::T)
 k_top_narrow(const uint16_t* __restrict__ W, const uint16_t* __restrict__ H, int d, int V, const int32_t* __restrict__ rowsel, int64_t c0, int64_t mc, Groups out) {
@@ -665,14 +675,15 @@ extern "C" umas_status umas_top_logits(const void* H, const void* W, umas_dtype 
         A.tiles = static_cast<int>(cdiv(V, Cfg::BM));
         const int tiles_n = static_cast<int>(cdiv(rows, Cfg::BN)), panel = row_panel(tiles_n, d);
         const int first = first_tiles(A.tiles, tiles_n, k);
-        hipLaunchKernelGGL(k_top_tiles, score_grid(first, tiles_n, panel, 0), dim3(Cfg::T), 0, st, Wb, Hb, d, V, rowsel, c0, rows, first, tiles_n, panel, A);
+        const int halved = halved_tiles(first, tiles_n);
+        hipLaunchKernelGGL(k_top_tiles, score_grid(first, tiles_n, panel, halved), dim3(Cfg::T), 0, st, Wb, Hb, d, V, rowsel, c0, rows, first, tiles_n, panel, halved, A);
         UMAS_LAUNCHED("k_top_tiles");
         if (first < A.tiles) {
           hipLaunchKernelGGL(k_top_bound, grid, dim3(kSelectT), 0, st, A, first, k, w.bound);
           UMAS_LAUNCHED("k_top_bound");
-          const int rest = A.tiles - first;
-          hipLaunchKernelGGL(k_top_tiles_bound, score_grid(rest, tiles_n, panel, 0), dim3(Cfg::T), 0, st, Wb, Hb, d, V, rowsel, c0, rows, first, rest, tiles_n, panel,
-                             A, w.bound);
+          const int rest = A.tiles - first, halved = halved_tiles(rest, tiles_n);
+          hipLaunchKernelGGL(k_top_tiles_bound, score_grid(rest, tiles_n, panel, halved), dim3(Cfg::T), 0, st, Wb, Hb, d, V, rowsel, c0, rows, first, rest, tiles_n, panel,
+                             halved, A, w.bound);
           UMAS_LAUNCHED("k_top_tiles_bound");
         }
         hipLaunchKernelGGL(k_top_row<TileGroups<Cfg>>, grid, dim3(kSelectT), 0, st, A, TileGroups<Cfg>{}, V, O);
