@@ -64,7 +64,8 @@ inline GradPlan plan_gradients(int64_t n_sel, int64_t rows, int d, int V, size_t
 }
 
 // dH of a frozen head: no dW fills a last round, so the slices are chosen for it, in microseconds: rounds of pieces on `cus` compute units, a piece its steps of 64 (1.6 each
-// of 256 x 256) and what a tile costs besides (twelve steps), and the partial sums' way to memory and back (0.1 a piece).
+// of 256 x 256) and what a tile costs besides (twelve steps), and 0.4 for a piece's partial sums: their way to memory and back is a third of it, the rest what they push out of the caches (2900 rows of 1536 in 504
+// pieces instead of 216: the product 829 -> 787 us, the sum 16 -> 29, the next call's scores 808 -> 832).
 inline DhPlan plan_dh_alone(int64_t tiles, int tiles_v, int cus, size_t room) {
   DhPlan best{1, tiles_v};
   double least = 0.0;
@@ -72,7 +73,7 @@ inline DhPlan plan_dh_alone(int64_t tiles, int tiles_v, int cus, size_t room) {
     const int blks = (tiles_v + want - 1) / want, slices = (tiles_v + blks - 1) / blks;
     const int64_t pieces = tiles * slices;
     if (slices > 1 && static_cast<size_t>(pieces) * (256 * 256 * sizeof(float)) > room) break;
-    const double us = static_cast<double>((pieces + cus - 1) / cus) * (blks * 4 + 12) * 1.6 + (slices > 1 ? pieces * 0.1 : 0.0);
+    const double us = static_cast<double>((pieces + cus - 1) / cus) * (blks * 4 + 12) * 1.6 + (slices > 1 ? pieces * 0.4 : 0.0);
     if (want == 1 || us < least) {
       best = DhPlan{slices, blks};
       least = us;

@@ -12,6 +12,7 @@
 //   E[i, v_j] = bf16((a' p - t) / (a' exp(r - lse))) = bf16(exp(lse - r) (p - t / a'))
 // so the sparse part costs k two-byte stores a row and no pass of its own over dH or dW.
 #include "umas_f32.h"
+#include "umas_few.h"
 #include "umas_gradients.h"
 
 namespace umas {
@@ -355,6 +356,20 @@ k_target_logits_narrow(const uint16_t* __restrict__ W, const uint16_t* __restric
   __shared__ __attribute__((aligned(16))) uint16_t lds[kNarrowLds / 2];
   score_tiles<Leave::kLogits, NarrowCfg>(W, H, d, V, rowsel, 0, n_sel, ids, tiles_m, 1, kGN, partial, n_pad, KeepArgs{nullptr, nullptr, Vp, nullptr, nullptr, Z}, lds);
 }
+template <int NI, int PPW>
+__global__ void __launch_bounds__(kFewT)
+k_target_logits_few(const uint16_t* __restrict__ W, const uint16_t* __restrict__ H, int d, int V, const int32_t* __restrict__ rowsel, int n_sel, int per,
+                    float4* __restrict__ partial, int64_t n_pad, float* __restrict__ Z, int64_t stride) {
+  few_logits<NI, PPW, true>(W, H, d, V, rowsel, n_sel, per, Z, stride, [&](int n, int place, float, float most, float s, float t) {
+    if (place == 0) partial[static_cast<int64_t>(blockIdx.x) * n_pad + n] = make_float4(most, s, t, 0.f);
+  });
+}
+// Where the block's logits lie: rows of `stride`, or (0) blocks of 256 x 256.
+struct KeptLogits {
+  const float* z;
+  int64_t stride;
+  __device__ __forceinline__ const float* at(int64_t n, int blk, int c) const { return z + (stride ? n * stride + blk * 256 : blk * kBlkElems + n * 256) + c; }
+};
 // The first workgroup lays the block out, `clearing` of them clear what the call defines everywhere, the others do eight rows each.
 struct FewArgs {
   Teach A;
@@ -365,7 +380,7 @@ struct FewArgs {
   const float4* partial;
   int tiles_m;
   int64_t n_pad;
-  const float* Z;
+  KeptLogits Z;
   uint16_t* Hs;
   int64_t mcp;
   float* row_out;
@@ -408,7 +423,7 @@ k_target_few(FewArgs F) {
     const Place<float> P = place_of<float>(A.t, A.V, row);
     const bool taught = P.mass != 0.f;                       // (a mass that is no number is the caller's)
     const float w = row_weight(A, row, taught), g = w / A.norm, lse = s_lse[q], a = dense_factor(P.mass, A.z_coef, lse), ts = mass_of_token(k, P.id, P.t);
-    const float z = P.t != 0.f ? F.Z[blk_offset(0, P.id >> 8, 0) + n * 256 + (P.id & 255)] : 0.f;
+    const float z = P.t != 0.f ? *F.Z.at(n, P.id >> 8, P.id & 255) : 0.f;
     float l = 0.f, out = 0.f;
     if (taught) {
       if (!A.t.logits) {
@@ -446,7 +461,7 @@ k_target_few(FewArgs F) {
 // 32 rows of a block of 256 entries to a workgroup; rows up to the next multiple of 64 are zeros.
 constexpr int kTurnedRows = 32;
 __global__ void __launch_bounds__(256)
-k_target_turn(const float* __restrict__ Z, const float* __restrict__ lse, const float* __restrict__ inv_x, const uint16_t* __restrict__ entries, Targets T,
+k_target_turn(KeptLogits Z, int V, const float* __restrict__ lse, const float* __restrict__ inv_x, const uint16_t* __restrict__ entries, Targets T,
               const int32_t* __restrict__ rowsel, int64_t n_sel, uint16_t* __restrict__ D, const float* __restrict__ out, float* __restrict__ row_out, int tiles_v, StatArgs S) {
   if (static_cast<int>(blockIdx.x) >= tiles_v) {             // the statistics
     __shared__ double smem[32];
@@ -465,14 +480,15 @@ k_target_turn(const float* __restrict__ Z, const float* __restrict__ lse, const 
 #pragma unroll
     for (int i = 0; i < 4; ++i)
 #pragma unroll
-      for (int q = 0; q < 2; ++q) z[i][q] = *reinterpret_cast<const float4*>(Z + at + r * 256 + i * 64 + c + q * 4);
+      for (int q = 0; q < 2; ++q) z[i][q] = *reinterpret_cast<const float4*>(Z.at(r, blockIdx.x, i * 64 + c + q * 4));
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
     uint4 o = make_uint4(0u, 0u, 0u, 0u);
     if (inv != 0.f) {
-      auto p = [&](float x) { return __builtin_amdgcn_exp2f(fmaf(x, 1.44269504088896341f, -l2)) * inv; };
-      o = make_uint4(pack_bf16x2(p(z[i][0].x), p(z[i][0].y)), pack_bf16x2(p(z[i][0].z), p(z[i][0].w)), pack_bf16x2(p(z[i][1].x), p(z[i][1].y)),
-                     pack_bf16x2(p(z[i][1].z), p(z[i][1].w)));
+      const int left = V - static_cast<int>(blockIdx.x) * 256 - i * 64 - c;   // entries from V on: 0, whatever lies there
+      auto p = [&](float x, int e) { return e < left ? __builtin_amdgcn_exp2f(fmaf(x, 1.44269504088896341f, -l2)) * inv : 0.f; };
+      o = make_uint4(pack_bf16x2(p(z[i][0].x, 0), p(z[i][0].y, 1)), pack_bf16x2(p(z[i][0].z, 2), p(z[i][0].w, 3)), pack_bf16x2(p(z[i][1].x, 4), p(z[i][1].y, 5)),
+                     pack_bf16x2(p(z[i][1].z, 6), p(z[i][1].w, 7)));
     }
     *reinterpret_cast<uint4*>(D + at + r * 256 + i * 64 + c) = o;
   }
@@ -668,7 +684,7 @@ void carve(Carver& c, Ws& w, int64_t n_sel, int d, int V, int k, umas_dtype dt) 
   const int64_t n_pad = round_up(n_sel > 0 ? n_sel : 1, Cfg::BN), tiles_m = (V + Cfg::BM - 1) / Cfg::BM;
   const bool bf = dt == UMAS_BF16;
   w = Ws{};
-  if (bf) w.partial = c.take<float4>(static_cast<size_t>(tiles_m) * n_pad);
+  if (bf) w.partial = c.take<float4>(std::max(static_cast<size_t>(tiles_m) * n_pad, n_sel <= 64 ? static_cast<size_t>(kFewMostTiles) * 64 : 0));
   for (float** p : {&w.R.lse, &w.R.ent, &w.R.l, &w.R.w, &w.R.a, &w.R.zero, &w.R.cref, &w.R.sc, &w.R.mass}) *p = c.take<float>(n_pad);
   if (bf) {
     w.R.zt = c.take<float>(static_cast<size_t>(n_pad) * k);
@@ -684,7 +700,7 @@ void carve(Carver& c, Ws& w, int64_t n_sel, int d, int V, int k, umas_dtype dt) 
 }
 // A block of rows keeps its float32 logits; dH's partial sums take their place later.
 constexpr int64_t kFewTaught = 256;
-size_t few_bytes(int64_t n_sel, int V, umas_dtype dt) { return dt == UMAS_BF16 && n_sel <= kFewTaught ? static_cast<size_t>(256) * round_up(V, 256) * sizeof(float) : 0; }
+size_t few_bytes(int64_t n_sel, int V, umas_dtype dt) { return dt == UMAS_BF16 && n_sel <= kFewTaught ? std::max(static_cast<size_t>(256) * round_up(V, 256), few_floats(64, V) + 256) * sizeof(float) : 0; }
 // float32 sums of dW where it is bf16 and comes from several chunks
 size_t sum_bytes(int d, int V, int dW_type) { return dW_type == UMAS_BF16 ? align_up(static_cast<size_t>(V) * d * sizeof(float)) : 0; }
 // float32: a chunk's dz, its rows of H, its float64 logits and the statistics of their parts.  256 MiB of logits to a chunk, what the memory-side cache holds,
@@ -866,23 +882,36 @@ umas_status run_bf16(const Call& a, const Ws& w, const Teach& A) {
     const LiveArgs live = live_args(c0, rows, sl.n, dw_apart);
     const bool few = n_sel <= kFewTaught;
     const bool narrow = n_sel <= NarrowCfg::BN;
-    const int64_t n_pad = round_up(n_sel, narrow ? NarrowCfg::BN : Cfg::BN);
-    const int tiles_m = narrow ? static_cast<int>(Vp / NarrowCfg::BM) : tiles_v;
+    const int64_t n_pad = n_sel <= few_rows(d) ? 64 : round_up(n_sel, narrow ? NarrowCfg::BN : Cfg::BN);
     if (few) {
       float* const Z = reinterpret_cast<float*>(chunk + chunk_bytes(rows, d, V, UMAS_BF16));
-      if (narrow)
-        hipLaunchKernelGGL(k_target_logits_narrow, dim3(tile_grid<kGM, kGN>(tiles_m, 1, kGN, kTilesPerWg)), dim3(NarrowCfg::T), 0, st, W, H, d, V, a.rowsel, n_sel,
-                           a.t.ids, tiles_m, w.partial, n_pad, Z, Vp);
-      else
+      KeptLogits kept{Z, 0};
+      int parts = tiles_v;
+      if (n_sel <= few_rows(d)) {
+        parts = few_workgroups(V);
+        const int per = few_per(V, parts);
+        kept.stride = static_cast<int64_t>(parts) * per * 16;
+        with_few(d, n_sel, [&](auto ni, auto ppw) {
+          hipLaunchKernelGGL((k_target_logits_few<decltype(ni)::value, decltype(ppw)::value>), dim3(parts), dim3(kFewT), 0, st, W, H, d, V, a.rowsel,
+                             static_cast<int>(n_sel), per, w.partial, n_pad, Z, kept.stride);
+        });
+        UMAS_LAUNCHED("k_target_logits_few");
+      } else if (narrow) {
+        parts = static_cast<int>(Vp / NarrowCfg::BM);
+        hipLaunchKernelGGL(k_target_logits_narrow, dim3(tile_grid<kGM, kGN>(parts, 1, kGN, kTilesPerWg)), dim3(NarrowCfg::T), 0, st, W, H, d, V, a.rowsel, n_sel,
+                           a.t.ids, parts, w.partial, n_pad, Z, Vp);
+        UMAS_LAUNCHED("k_target_logits_narrow");
+      } else {
         hipLaunchKernelGGL(k_target_logits, score_grid(tiles_v, 1, kGN, halved), dim3(Cfg::T), 0, st, W, H, d, V, a.rowsel, n_sel, a.t.ids, tiles_v, halved, w.partial,
                            n_pad, Z, Vp);
-      UMAS_LAUNCHED(narrow ? "k_target_logits_narrow" : "k_target_logits");
+        UMAS_LAUNCHED("k_target_logits");
+      }
       const unsigned clearing = a.rowsel ? 256 : 0;
       hipLaunchKernelGGL(k_target_few, dim3(1 + clearing + cdiv(n_sel, 8)), dim3(256), 0, st,
-                         FewArgs{A, H, w.R, w.R.cref, w.R.entries, w.partial, tiles_m, n_pad, Z, Hs, mcp, a.row_out, live, clearing, static_cast<uint32_t*>(a.dH),
+                         FewArgs{A, H, w.R, w.R.cref, w.R.entries, w.partial, parts, n_pad, kept, Hs, mcp, a.row_out, live, clearing, static_cast<uint32_t*>(a.dH),
                                  a.n_rows * static_cast<int64_t>(d) / 2, a.n_rows});
       UMAS_LAUNCHED("k_target_few");
-      hipLaunchKernelGGL(k_target_turn, dim3(tiles_v + 1 + a.n_roles, static_cast<unsigned>(round_up(n_sel, 64) / kTurnedRows)), dim3(256), 0, st, Z, w.R.lse, w.R.cref, w.R.entries, A.t,
+      hipLaunchKernelGGL(k_target_turn, dim3(tiles_v + 1 + a.n_roles, static_cast<unsigned>(round_up(n_sel, 64) / kTurnedRows)), dim3(256), 0, st, kept, V, w.R.lse, w.R.cref, w.R.entries, A.t,
                          a.rowsel, n_sel, E, w.R.a, a.row_out, tiles_v, stats);
       UMAS_LAUNCHED("k_target_turn");
     } else if (c0 == 0) {
@@ -899,7 +928,7 @@ umas_status run_bf16(const Call& a, const Ws& w, const Teach& A) {
                          panel, halved, w.partial, n_pad, w.R.cref, E, Vp, w.flags, w.blk_cidx);
       UMAS_LAUNCHED("k_target_tiles");
       hipLaunchKernelGGL(k_target_rows, dim3(cdiv(rows, 8)), dim3(256), 0, st,
-                         RowsArgs{A, H, w.R, w.partial, tiles_m, n_pad, c0, rows, w.flags, w.blk_cidx, E, tiles_v, Hs, mcp, a.row_out});
+                         RowsArgs{A, H, w.R, w.partial, tiles_v, n_pad, c0, rows, w.flags, w.blk_cidx, E, tiles_v, Hs, mcp, a.row_out});
       UMAS_LAUNCHED("k_target_rows");
       const PutTargets put{a.rowsel, a.t.ids, a.t.k, w.R.zt, w.R.tt, w.R.lse, w.R.a, w.R.w, A.norm};
       hipLaunchKernelGGL(k_target_flagged, dim3(kFlaggedGrid + (c0 + rows >= n_sel ? 1 + a.n_roles : 0)), dim3(Cfg::T), 0, st, W, H, d, V, a.rowsel, c0, rows, w.R.zero, put, tiles_v, tiles_r, E, Vp,

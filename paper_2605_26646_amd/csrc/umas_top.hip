@@ -9,7 +9,7 @@
 // complement of the token.  A wavefront keeps the 64 largest keys it has seen, one to a lane in falling order, and takes only keys beyond its
 // k-th: those collect in LDS until there are 64, are sorted (21 exchanges) and merged with what is there (7).
 #include "umas_f32.h"
-#include "umas_logits.h"
+#include "umas_few.h"
 
 namespace umas {
 namespace {
@@ -230,123 +230,16 @@ k_top_narrow(const uint16_t* __restrict__ W, const uint16_t* __restrict__ H, int
   top_tiles<NarrowCfg, true>(W, H, d, V, rowsel, c0, mc, 0, out.tiles, 1, kGN, out, nullptr, lds);
 }
 
-// A few rows: W streams past rows that stay in registers (the loop and what bounds it: k_score_few).  A thread has one place of every block of 16 entries of its
-// workgroup's part of the vocabulary: its group.  The logits are summed over the wavefronts in a fixed order; they collect in LDS, 64 KB of them, and leave
-// together: memory operations are counted in order, and a store in every step has the loads of W behind it wait for it (one row of 2048 129 us in place
-// of 110, 24 rows of 3584 247 in place of 199).
-constexpr int kFewGroups = 16, kFewMostTiles = 512;
+// A few rows (umas_few.h): a thread's place of every block of 16 entries of its workgroup's part of the vocabulary is a group.
+constexpr int kFewGroups = 16;
 template <int NI, int PPW>
 __global__ void __launch_bounds__(kFewT)
 k_top_few(const uint16_t* __restrict__ W, const uint16_t* __restrict__ H, int d, int V, const int32_t* __restrict__ rowsel, int n_sel, int per, Groups out) {
-  constexpr int MB = PPW <= 4 && NI <= 2 ? 2 : 1;            // blocks of 16 vocabulary entries per step
-  constexpr int NL = (NI + 1) / 2;                           // logits per thread and block
-  constexpr int kHold = 64 / NI, kHoldPitch = kHold * 16 + 16;   // blocks that collect, floats of a row of them (16 more: banks)
-  __shared__ __attribute__((aligned(16))) float s_z[2][kFewWaves][MB][NI][16][16];   // [.][wavefront][block][.][row][entry]
-  __shared__ __attribute__((aligned(16))) float s_out[NI * 16 * kHoldPitch];
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  const int piece = (lane >> 4) * 8;
-  bf16x8 hf[PPW][2][NI];
-#pragma unroll
-  for (int p = 0; p < PPW; ++p)
-#pragma unroll
-    for (int q = 0; q < 2; ++q)
-#pragma unroll
-      for (int j = 0; j < NI; ++j) {
-        const int n = min(j * 16 + (lane & 15), n_sel - 1), k = (p * kFewWaves + wave) * 64 + q * 32 + piece;
-        const int64_t row = rowsel ? rowsel[n] : n;
-        const uint4 v = k < d ? *reinterpret_cast<const uint4*>(H + row * d + k) : make_uint4(0u, 0u, 0u, 0u);
-        hf[p][q][j] = __builtin_bit_cast(bf16x8, v);
-      }
-  const int blocks = (V + 15) / 16;
-  const int b0 = static_cast<int>(blockIdx.x) * per, b1 = min(b0 + per, blocks);
-  uint4 w[MB][PPW][2];
-  bool past[2];                                              // the last piece's columns that do not exist
-#pragma unroll
-  for (int q = 0; q < 2; ++q) past[q] = ((PPW - 1) * kFewWaves + wave) * 64 + q * 32 + piece >= d;
-  auto load = [&](int b, int p, int q, int i) {              // past the hidden size: some entry of the row, cleared where it is used
-    const int v = min((b + i) * 16 + (lane & 15), V - 1), k = min((p * kFewWaves + wave) * 64 + q * 32 + piece, d - 8);
-    w[i][p][q] = *reinterpret_cast<const uint4*>(W + static_cast<int64_t>(v) * d + k);
-  };
-  if (b0 < b1)
-#pragma unroll
-    for (int i = 0; i < MB; ++i)
-#pragma unroll
-      for (int p = 0; p < PPW; ++p) { load(b0, p, 0, i); load(b0, p, 1, i); }
-  const bool mine = tid < NI * 256;
-  const int my_n = (tid >> 4) & 15, my_v = tid & 15;
-  float m[NL], s[NL];
-#pragma unroll
-  for (int l = 0; l < NL; ++l) {
-    m[l] = kMasked;
-    s[l] = 0.f;
-  }
-  int first = b0;                                            // of the blocks that collect
-  auto leave = [&](int end) {                                // a wavefront to a row
-    __syncthreads();
-    for (int n = wave; n < n_sel; n += kFewWaves) {
-      float* const z = out.z + ((static_cast<int64_t>(n) * out.tiles + blockIdx.x) * per + first - b0) * kFewGroups;
-      for (int c = lane * 4; c < (end - first) * 16; c += kWave * 4)
-        *reinterpret_cast<floatx4*>(z + c) = *reinterpret_cast<const floatx4*>(s_out + n * kHoldPitch + c);
-    }
-    __syncthreads();
-    first = end;
-  };
-  int buf = 0;
-  for (int b = b0; b < b1; b += MB, buf ^= 1) {
-    floatx4 acc[MB][NI];
-#pragma unroll
-    for (int i = 0; i < MB; ++i)
-#pragma unroll
-      for (int j = 0; j < NI; ++j) acc[i][j] = floatx4{0.f, 0.f, 0.f, 0.f};
-    const int nb = b + MB < b1 ? b + MB : b;                 // past the range: loaded again, not used
-#pragma unroll
-    for (int i = 0; i < MB; ++i)
-#pragma unroll
-      for (int p = 0; p < PPW; ++p)
-#pragma unroll
-        for (int q = 0; q < 2; ++q) {
-          const bf16x8 a = __builtin_bit_cast(bf16x8, p == PPW - 1 && past[q] ? make_uint4(0u, 0u, 0u, 0u) : w[i][p][q]);
-#pragma unroll
-          for (int j = 0; j < NI; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, hf[p][q][j], acc[i][j], 0, 0, 0);
-          load(nb, p, q, i);
-        }
-#pragma unroll
-    for (int i = 0; i < MB; ++i)
-#pragma unroll
-      for (int j = 0; j < NI; ++j) *reinterpret_cast<floatx4*>(&s_z[buf][wave][i][j][lane & 15][(lane >> 4) * 4]) = acc[i][j];
-    __syncthreads();
-    if (mine) {
-#pragma unroll
-      for (int i = 0; i < MB; ++i)
-#pragma unroll
-        for (int l = 0; l < NL; ++l) {
-          float z = 0.f;
-#pragma unroll
-          for (int k = 0; k < kFewWaves; ++k) z += s_z[buf][k][i][2 * l + (tid >> 8)][my_n][my_v];
-          if ((b + i) * 16 + my_v >= V || b + i >= b1) z = kMasked;
-          s_out[((2 * l + (tid >> 8)) * 16 + my_n) * kHoldPitch + (b + i - first) * 16 + my_v] = z;
-          const float gap = z - m[l], e = __expf(-fabsf(gap));  // one exponential: of the smaller relative to the larger
-          s[l] = gap > 0.f ? fmaf(s[l], e, 1.f) : s[l] + e;
-          m[l] = fmaxf(m[l], z);
-        }
-    }
-    if (b + MB - first == kHold) leave(b + MB);
-  }
-  if (first < b1) leave(min(b0 + per, (b1 - first + MB - 1) / MB * MB + first));
-#pragma unroll
-  for (int l = 0; l < NL; ++l) {
-    float most = m[l];                                       // of the row's sixteen threads, which are neighbours
-#pragma unroll
-    for (int o = 1; o < 16; o <<= 1) most = fmaxf(most, __shfl_xor(most, o, kWave));
-    float sum = s[l] * __expf(m[l] - most);
-#pragma unroll
-    for (int o = 1; o < 16; o <<= 1) sum += __shfl_xor(sum, o, kWave);
-    const int n = (2 * l + (tid >> 8)) * 16 + my_n;
-    if (!mine || n >= n_sel) continue;
+  few_logits<NI, PPW, false>(W, H, d, V, rowsel, n_sel, per, out.z, static_cast<int64_t>(out.tiles) * kFewGroups * per, [&](int n, int place, float m, float most, float sum, float) {
     const int64_t at = static_cast<int64_t>(n) * out.tiles + blockIdx.x;
-    out.max[at * kFewGroups + my_v] = m[l];
-    if (my_v == 0) out.sum[at] = sum;
-  }
+    out.max[at * kFewGroups + place] = m;
+    if (place == 0) out.sum[at] = sum;
+  });
 }
 
 // ------------------------------------------------------------------ selection
@@ -552,26 +445,6 @@ constexpr int64_t kTopChunkRows = 4096;
 // workgroups to a row: as many as fill the chip, 256 entries to a wavefront at the least
 constexpr int64_t kSelectLists = 2048;
 int select_parts(int64_t rows, int V) { return static_cast<int>(std::min<int64_t>(std::max<int64_t>(kSelectLists / rows, 1), cdiv(V, kSelectWaves * 256))); }
-template <int PPW, class... Args>
-void launch_top_few_ppw(int ni, unsigned grid, hipStream_t st, Args... args) {
-  if constexpr (PPW <= 4)
-    if (ni > 2) { hipLaunchKernelGGL((k_top_few<4, PPW>), dim3(grid), dim3(kFewT), 0, st, args...); return; }
-  if (ni <= 1) hipLaunchKernelGGL((k_top_few<1, PPW>), dim3(grid), dim3(kFewT), 0, st, args...);
-  else hipLaunchKernelGGL((k_top_few<2, PPW>), dim3(grid), dim3(kFewT), 0, st, args...);
-}
-template <class... Args>
-void launch_top_few(int ppw, Args... args) {
-  switch (ppw) {
-    case 1: return launch_top_few_ppw<1>(args...);
-    case 2: return launch_top_few_ppw<2>(args...);
-    case 3: return launch_top_few_ppw<3>(args...);
-    case 4: return launch_top_few_ppw<4>(args...);
-    case 5: return launch_top_few_ppw<5>(args...);
-    case 6: return launch_top_few_ppw<6>(args...);
-    case 7: return launch_top_few_ppw<7>(args...);
-    default: return launch_top_few_ppw<8>(args...);
-  }
-}
 struct TopWs {
   TopKey* lists;                                             // float32
   double* z64;
@@ -590,8 +463,6 @@ int first_tiles(int tiles, int tiles_n, int k) {
   const int first = static_cast<int>(round_up(static_cast<int64_t>(n / 256.0) + 1, round));
   return first * 2 > tiles ? tiles : first;
 }
-// blocks of 16 entries to a workgroup of the kernel for few rows
-int few_per(int V, int tiles) { return static_cast<int>(round_up(cdiv(cdiv(V, 16), tiles), 2)); }   // steps of two blocks end in them
 void carve(Carver& c, TopWs& w, int64_t rows, int d, int V, umas_dtype dt) {
   w = TopWs{};
   if (dt == UMAS_BF16) {
@@ -601,7 +472,7 @@ void carve(Carver& c, TopWs& w, int64_t rows, int d, int V, umas_dtype dt) {
     w.groups.max = c.take<float>(static_cast<size_t>(rows) * groups);
     w.groups.sum = c.take<float>(static_cast<size_t>(rows) * tiles);
     w.bound = c.take<float>(rows);
-    w.groups.z = c.take<float>(static_cast<size_t>(rows) * (round_up(V, 256) + (few ? 3 * kFewMostTiles * kFewGroups : 0)));
+    w.groups.z = c.take<float>(few ? few_floats(rows, V) : static_cast<size_t>(rows) * round_up(V, 256));
   } else {
     w.lists = c.take<TopKey>(static_cast<size_t>(std::max(rows, kSelectLists)) * kWave);
     w.z64 = c.take<double>(static_cast<size_t>(rows) * V);
@@ -661,9 +532,11 @@ extern "C" umas_status umas_top_logits(const void* H, const void* W, umas_dtype 
       const uint16_t *Wb = static_cast<const uint16_t*>(W), *Hb = static_cast<const uint16_t*>(H);
       Groups A = w.groups;
       if (cap <= few_rows(d)) {                              // one chunk
-        A.tiles = std::min(std::min(device_cus(), kFewMostTiles), static_cast<int>(cdiv(V, 16)));
+        A.tiles = few_workgroups(V);
         const int per = few_per(V, A.tiles);
-        launch_top_few(few_pieces(d), rows <= 16 ? 1 : rows <= 32 ? 2 : 4, A.tiles, st, Wb, Hb, d, V, rowsel, static_cast<int>(rows), per, A);
+        with_few(d, rows, [&](auto ni, auto ppw) {
+          hipLaunchKernelGGL((k_top_few<decltype(ni)::value, decltype(ppw)::value>), dim3(A.tiles), dim3(kFewT), 0, st, Wb, Hb, d, V, rowsel, static_cast<int>(rows), per, A);
+        });
         UMAS_LAUNCHED("k_top_few");
         hipLaunchKernelGGL(k_top_row<FewGroups>, grid, dim3(kSelectT), 0, st, A, FewGroups{per}, V, O);
       } else if (rows <= NarrowCfg::BN) {
