@@ -107,8 +107,9 @@ struct OpenArgs {
   int64_t dh_words;
   float* row_out;
   int64_t n_rows;
+  int share;               // wavefronts to a row: 1 or 4
 };
-// One wavefront per selected row: the targets' masses, their logits (dot products of float32 sums), the row's reference.  The first workgroup clears
+// One wavefront (four) per selected row: the targets' masses, their logits (dot products of float32 sums), the row's reference.  The first workgroup clears
 // the flags and lays out the chunk, others clear what the call defines everywhere.
 constexpr int kAtOnce = 4;   // targets whose rows of W are under way together
 __global__ void __launch_bounds__(256)
@@ -125,13 +126,17 @@ k_target_open(OpenArgs O) {
     for (int64_t i = blk * 256 + threadIdx.x; i < O.dh_words; i += stride) O.dH[i] = 0u;
     for (int64_t i = blk * 256 + threadIdx.x; i < O.n_rows; i += stride) O.row_out[i] = 0.f;
   }
-  const int lane = threadIdx.x & 63, k = A.t.k;
-  for (int64_t n = blk * 4 + threadIdx.x / kWave; n < A.n_sel; n += nb * 4) {
+  // `share` wavefronts to a row: their numbers in the row, its targets dealt out among them
+  __shared__ float s_z[4][kWave];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, k = A.t.k, share = O.share, mine = wave % share;
+  for (int64_t n0 = blk * (4 / share); n0 < A.n_sel; n0 += nb * (4 / share)) {
+    const int64_t n = min(n0 + wave / share, A.n_sel - 1);
     const int64_t row = A.rowsel ? A.rowsel[n] : n;
     const Place<float> P = place_of<float>(A.t, A.V, row);
     const uint4* h = reinterpret_cast<const uint4*>(O.H + row * A.d);
     float z = 0.f;
-    unsigned long long left = __ballot(P.t != 0.f);          // NaN counts
+    const unsigned long long share_of = share == 4 ? 0x1111111111111111ull << mine : ~0ull;
+    unsigned long long left = __ballot(P.t != 0.f) & share_of;   // NaN counts
     while (left) {
       int j[kAtOnce];
       const uint4* w[kAtOnce];
@@ -159,6 +164,15 @@ k_target_open(OpenArgs O) {
         const float sum = wave_sum(s[b]);
         if (lane == j[b]) z = sum;
       }
+    }
+    if (share == 4) {
+      __syncthreads();                                       // (the row before)
+      s_z[wave][lane] = z;
+      __syncthreads();
+      z = s_z[lane & 3][lane];
+      if (wave != 0) continue;
+    } else if (n0 + wave >= A.n_sel) {
+      continue;
     }
     const bool taught = P.mass > 0.f || P.mass != P.mass;
     const float top = wave_max(P.t != 0.f ? z : -INFINITY), ts = mass_of_token(k, P.id, P.t);
@@ -238,7 +252,55 @@ k_target_tiles(const uint16_t* __restrict__ W, const uint16_t* __restrict__ H, i
   score_tiles<Leave::kNumerators, Cfg>(W, H, d, V, rowsel, c0, mc, nullptr, tiles_m, tiles_n, panel, partial, n_pad, KeepArgs{cref, E, Vp, flags, cidx, nullptr}, lds, halved);
 }
 // ------------------------------------------------------------------ bf16: rows
-// Eight rows to a workgroup: their parts merged, then a wavefront to a row: its loss and factor, its k entries of the operand, its scaled copy of H.
+// Eight rows to a workgroup, a wavefront to each, which asks for what it needs of its row; then all of them merge the rows' parts (a load covers the eight rows of
+// eight parts), and a wavefront goes on with its row: its loss and factor, its k entries of the operand, its scaled copy of H.
+constexpr int kRowsT = 512;
+struct MergedRows {
+  float lse[8], ent[8], sum[8];
+};
+__device__ __forceinline__ void merge_rows(const float4* __restrict__ partial, int parts, int64_t n_pad, int64_t n0, bool live, MergedRows& out) {
+  __shared__ float4 s_part[kRowsT / kWave][8];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  constexpr int kParts = kRowsT / 8;
+  Part p{kNegInf, 0.f, 0.f};
+  if (live)
+    for (int t0 = threadIdx.x >> 3; t0 < parts; t0 += 4 * kParts) {
+      float4 q[4];
+#pragma unroll
+      for (int k = 0; k < 4; ++k)
+        q[k] = t0 + k * kParts < parts ? partial[static_cast<int64_t>(t0 + k * kParts) * n_pad + n0 + (lane & 7)] : make_float4(kNegInf, 0.f, 0.f, 0.f);
+#pragma unroll
+      for (int k = 0; k < 4; ++k) p = part_merge(p, Part{q[k].x, q[k].y, q[k].z});
+    }
+#pragma unroll
+  for (int o = 8; o < kWave; o <<= 1) p = part_merge(p, Part{__shfl_xor(p.m, o, kWave), __shfl_xor(p.s, o, kWave), __shfl_xor(p.t, o, kWave)});
+  if (lane < 8) s_part[wave][lane] = make_float4(p.m, p.s, p.t, 0.f);
+  __syncthreads();
+  if (threadIdx.x < 8) {
+    p = Part{kNegInf, 0.f, 0.f};
+#pragma unroll
+    for (int w = 0; w < kRowsT / kWave; ++w) {
+      const float4 q = s_part[w][threadIdx.x];
+      p = part_merge(p, Part{q.x, q.y, q.z});
+    }
+    const float lse = p.m + logf(p.s);
+    out.lse[threadIdx.x] = lse;
+    out.ent[threadIdx.x] = lse - p.t / p.s;
+    out.sum[threadIdx.x] = p.s;
+  }
+  __syncthreads();
+}
+// one wavefront: bf16(f h) into the column blocks that dW reads; zeros, whatever h is, for f = 0
+__device__ __forceinline__ void copy_row(const uint16_t* __restrict__ H, int64_t row, int d, float f, uint16_t* __restrict__ Hs, int64_t mcp, int64_t mp) {
+  const uint4* h = reinterpret_cast<const uint4*>(H + row * d);
+  for (int c = threadIdx.x & 63; c < d / 8; c += kWave) {
+    float x[8];
+    bf16x8_to_f32(h[c], x);
+    uint4 v = make_uint4(0u, 0u, 0u, 0u);
+    if (f != 0.f) v = make_uint4(pack_bf16x2(x[0] * f, x[1] * f), pack_bf16x2(x[2] * f, x[3] * f), pack_bf16x2(x[4] * f, x[5] * f), pack_bf16x2(x[6] * f, x[7] * f));
+    reinterpret_cast<uint4*>(Hs + (static_cast<int64_t>(c >> 5) * mcp + mp) * 256)[c & 31] = v;
+  }
+}
 struct RowsArgs {
   Teach A;
   const uint16_t* H;
@@ -259,85 +321,62 @@ __device__ __forceinline__ float target_entry(float z, float lse, float r, float
   return __expf(lse - r) * (lp > -0.7f ? expm1f(lp) + (1.f - q) : __expf(lp) - q);
 }
 __device__ __forceinline__ bool is_finite(float x) { return fabsf(x) < INFINITY; }
-__global__ void __launch_bounds__(256)
+__global__ void __launch_bounds__(kRowsT)
 k_target_rows(RowsArgs O) {
-  __shared__ float s_lse[8], s_ent[8], s_sum[8];
+  __shared__ MergedRows s_rows;
   const Teach& A = O.A;
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, k = A.t.k;
-  const int64_t m0 = static_cast<int64_t>(blockIdx.x) * 8;
-  {
-    const int64_t m = m0 + (lane & 7);
-    Part p;
-    float none;
-    if (merge_parts<true>(O.partial, O.tiles_m, O.n_pad, O.c0 + m, m < O.rows, p, none)) {
-      s_lse[lane] = p.m + logf(p.s);
-      s_ent[lane] = s_lse[lane] - p.t / p.s;
-      s_sum[lane] = p.s;
+  const int lane = threadIdx.x & 63, q = threadIdx.x >> 6, k = A.t.k;
+  const int64_t m0 = static_cast<int64_t>(blockIdx.x) * 8, m = m0 + q, n = O.c0 + min(m, O.rows - 1);
+  const int64_t row = A.rowsel ? A.rowsel[n] : n;
+  const int blk = O.cidx[n >> 8], flag = O.flags[n >> 8];
+  const float w = O.R.w[n], mass = O.R.mass[n], r = O.R.cref[n];
+  const bool in = lane < k, taught = r < 1e30f || r != r;
+  const int id = in ? A.t.ids[row * k + lane] : -1;
+  const float z = in ? O.R.zt[n * k + lane] : 0.f, ts = in ? O.R.tt[n * k + lane] : 0.f, t = A.t.logits ? place_of<float>(A.t, A.V, row).t : 0.f;
+  merge_rows(O.partial, O.tiles_m, O.n_pad, O.c0 + m0, m0 + (lane & 7) < O.rows, s_rows);
+  if (m >= O.rows) return;
+  const float lse = s_rows.lse[q], g = w / A.norm, a = dense_factor(mass, A.z_coef, lse);
+  float l = 0.f, out = 0.f, f = 0.f;
+  if (taught) {
+    if (!A.t.logits) {
+      out = __shfl(z, 0, kWave) - lse;
+      l = A.z_coef != 0.f ? fmaf(A.z_coef * lse, lse, -out) : -out;
+    } else {
+      out = l = wave_sum(t != 0.f ? t * (logf(t) - (z - lse)) : 0.f);
     }
+    f = g != 0.f ? (flag ? 1.f : g * a * __expf(r - lse)) : 0.f;
   }
-  __syncthreads();
-  for (int q = wave; q < 8; q += 4) {
-    const int64_t m = m0 + q, n = O.c0 + m;
-    if (m >= O.rows) break;
-    const int64_t row = A.rowsel ? A.rowsel[n] : n;
-    const int blk = O.cidx[n >> 8], flag = O.flags[n >> 8];
-    const float w = O.R.w[n], mass = O.R.mass[n], r = O.R.cref[n];
-    const bool in = lane < k, taught = r < 1e30f || r != r;
-    const int id = in ? A.t.ids[row * k + lane] : -1;
-    const float z = in ? O.R.zt[n * k + lane] : 0.f, ts = in ? O.R.tt[n * k + lane] : 0.f;
-    const float lse = s_lse[q], g = w / A.norm, a = dense_factor(mass, A.z_coef, lse);
-    float l = 0.f, out = 0.f, f = 0.f;
-    if (taught) {
-      if (!A.t.logits) {
-        out = __shfl(z, 0, kWave) - lse;
-        l = A.z_coef != 0.f ? fmaf(A.z_coef * lse, lse, -out) : -out;
-      } else {
-        const Place<float> P = place_of<float>(A.t, A.V, row);
-        out = l = wave_sum(P.t != 0.f ? P.t * (logf(P.t) - (z - lse)) : 0.f);
-      }
-      f = g != 0.f ? (flag ? 1.f : g * a * __expf(r - lse)) : 0.f;
-    }
-    // The row's entries are rounded to bf16.  dH's row factor is taken as what makes them, times it, what they were (least squares; one target: exactly), as
-    // they and not the dense part make most of the row's dH: 60 rows of 2048 with ten targets dH off by 0.0028 of its norm without it, its own rounding
-    // being 0.0017.  (Not so dW's, where a dense entry of few rows stands by itself and would carry the shift.)
-    const bool put = f != 0.f && !flag && ts != 0.f;
-    const float e = put ? target_entry(z, lse, r, ts, a) : 0.f, most = wave_max(fabsf(e));
-    const uint16_t rounded = f2bf(e);
-    float shift = 1.f;
-    if (most > 0.f) {
-      const float x = e / most, y = bf2f(rounded) / most, xy = wave_sum(x * y), yy = wave_sum(y * y);
-      if (yy > 0.f) shift = xy / yy;
-    }
-    if (lane == 0) {
-      O.R.lse[n] = taught ? lse : 0.f;
-      O.R.ent[n] = taught ? s_ent[q] : 0.f;
-      O.R.l[n] = l;
-      O.R.a[n] = g != 0.f ? g * a : 0.f;
-      O.R.sc[n] = f * shift;
-      if (O.row_out) O.row_out[row] = out;
-    }
-    uint16_t* const Erow = O.E + blk_offset(blk, 0, O.tiles_v) + (m & 255) * 256;
-    if (f != 0.f) {
-      if (put) Erow[static_cast<int64_t>(id >> 8) * kBlkElems + (id & 255)] = rounded;
-    } else if (!is_finite(s_sum[q]) || (taught && !is_finite(lse))) {
-      // a row that teaches nothing may hold anything: its numerators must not be multiplied; the last row's stand in those behind it as well
-      const int64_t rows = m == O.rows - 1 ? (m & ~int64_t{63}) + 64 - m : 1;
-      for (int64_t i = 0; i < rows; ++i)
-        for (int64_t vb = 0; vb < O.tiles_v; ++vb) *reinterpret_cast<uint2*>(Erow + i * 256 + vb * kBlkElems + lane * 4) = make_uint2(0u, 0u);
-    }
-    if (O.Hs) {
-      const int64_t mp = static_cast<int64_t>(blk) * 256 + (m & 255);
-      const uint4* h = reinterpret_cast<const uint4*>(O.H + row * A.d);
-      for (int c = lane; c < A.d / 8; c += kWave) {
-        float x[8];
-        bf16x8_to_f32(h[c], x);
-        uint4 v = make_uint4(0u, 0u, 0u, 0u);
-        if (f != 0.f) v = make_uint4(pack_bf16x2(x[0] * f, x[1] * f), pack_bf16x2(x[2] * f, x[3] * f), pack_bf16x2(x[4] * f, x[5] * f), pack_bf16x2(x[6] * f, x[7] * f));
-        reinterpret_cast<uint4*>(O.Hs + (static_cast<int64_t>(c >> 5) * O.mcp + mp) * 256)[c & 31] = v;
-      }
-    }
+  // The row's entries are rounded to bf16.  dH's row factor is taken as what makes them, times it, what they were (least squares; one target: exactly), as
+  // they and not the dense part make most of the row's dH: 60 rows of 2048 with ten targets dH off by 0.0028 of its norm without it, its own rounding
+  // being 0.0017.  (Not so dW's, where a dense entry of few rows stands by itself and would carry the shift.)
+  const bool put = f != 0.f && !flag && ts != 0.f;
+  const float e = put ? target_entry(z, lse, r, ts, a) : 0.f, most = wave_max(fabsf(e));
+  const uint16_t rounded = f2bf(e);
+  float shift = 1.f;
+  if (most > 0.f) {
+    const float x = e / most, y = bf2f(rounded) / most, xy = wave_sum(x * y), yy = wave_sum(y * y);
+    if (yy > 0.f) shift = xy / yy;
   }
+  if (lane == 0) {
+    O.R.lse[n] = taught ? lse : 0.f;
+    O.R.ent[n] = taught ? s_rows.ent[q] : 0.f;
+    O.R.l[n] = l;
+    O.R.a[n] = g != 0.f ? g * a : 0.f;
+    O.R.sc[n] = f * shift;
+    if (O.row_out) O.row_out[row] = out;
+  }
+  uint16_t* const Erow = O.E + blk_offset(blk, 0, O.tiles_v) + (m & 255) * 256;
+  if (f != 0.f) {
+    if (put) Erow[static_cast<int64_t>(id >> 8) * kBlkElems + (id & 255)] = rounded;
+  } else if (!is_finite(s_rows.sum[q]) || (taught && !is_finite(lse))) {
+    // a row that teaches nothing may hold anything: its numerators must not be multiplied; the last row's stand in those behind it as well
+    const int64_t rows = m == O.rows - 1 ? (m & ~int64_t{63}) + 64 - m : 1;
+    for (int64_t i = 0; i < rows; ++i)
+      for (int64_t vb = 0; vb < O.tiles_v; ++vb) *reinterpret_cast<uint2*>(Erow + i * 256 + vb * kBlkElems + lane * 4) = make_uint2(0u, 0u);
+  }
+  if (O.Hs) copy_row(O.H, row, A.d, f, O.Hs, O.mcp, static_cast<int64_t>(blk) * 256 + (m & 255));
 }
+
 // ------------------------------------------------------------------ bf16: one block of rows
 // Up to 256 rows the scores leave their logits in float32 instead: 6 bytes a logit more to write and read, of which there are few here, in place of the
 // gather, the references and what they may not serve for.  The operand is then made from the logits, D = bf16(dz / (g a' x)), with f = g a' x as the row factor: x, near
@@ -389,74 +428,55 @@ struct FewArgs {
   uint32_t* dH;
   int64_t dh_words, n_rows;
 };
-__global__ void __launch_bounds__(256)
+__global__ void __launch_bounds__(kRowsT)
 k_target_few(FewArgs F) {
-  __shared__ float s_lse[8], s_ent[8];
+  __shared__ MergedRows s_rows;
   const Teach& A = F.A;
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, k = A.t.k;
+  const int lane = threadIdx.x & 63, q = threadIdx.x >> 6, k = A.t.k;
   if (blockIdx.x == 0) {
     live_scan(F.live, static_cast<int>(threadIdx.x) < F.live.nblk);
     return;
   }
   if (blockIdx.x <= F.clearing) {
-    const int64_t stride = static_cast<int64_t>(F.clearing) * 256, i0 = static_cast<int64_t>(blockIdx.x - 1) * 256 + threadIdx.x;
+    const int64_t stride = static_cast<int64_t>(F.clearing) * kRowsT, i0 = static_cast<int64_t>(blockIdx.x - 1) * kRowsT + threadIdx.x;
     for (int64_t i = i0; i < F.dh_words; i += stride) F.dH[i] = 0u;
     if (F.row_out)
       for (int64_t i = i0; i < F.n_rows; i += stride) F.row_out[i] = 0.f;
     return;
   }
-  const int64_t m0 = (static_cast<int64_t>(blockIdx.x) - 1 - F.clearing) * 8;
-  {
-    const int64_t m = m0 + (lane & 7);
-    Part p;
-    float none;
-    if (merge_parts<true>(F.partial, F.tiles_m, F.n_pad, m, m < A.n_sel, p, none)) {
-      s_lse[lane] = p.m + logf(p.s);
-      s_ent[lane] = s_lse[lane] - p.t / p.s;
+  const int64_t m0 = (static_cast<int64_t>(blockIdx.x) - 1 - F.clearing) * 8, n = min(m0 + q, A.n_sel - 1);
+  const int64_t row = A.rowsel ? A.rowsel[n] : n;
+  const Place<float> P = place_of<float>(A.t, A.V, row);
+  const bool taught = P.mass != 0.f;                         // (a mass that is no number is the caller's)
+  const float w = row_weight(A, row, taught), g = w / A.norm, ts = mass_of_token(k, P.id, P.t);
+  const float z = P.t != 0.f ? *F.Z.at(n, P.id >> 8, P.id & 255) : 0.f;
+  merge_rows(F.partial, F.tiles_m, F.n_pad, m0, m0 + (lane & 7) < A.n_sel, s_rows);
+  if (m0 + q >= A.n_sel) return;
+  const float lse = s_rows.lse[q], a = dense_factor(P.mass, A.z_coef, lse);
+  float l = 0.f, out = 0.f;
+  if (taught) {
+    if (!A.t.logits) {
+      out = __shfl(z, 0, kWave) - lse;
+      l = A.z_coef != 0.f ? fmaf(A.z_coef * lse, lse, -out) : -out;
+    } else {
+      out = l = wave_sum(P.t != 0.f ? P.t * (logf(P.t) - (z - lse)) : 0.f);
     }
   }
-  __syncthreads();
-  for (int q = wave; q < 8; q += 4) {
-    const int64_t n = m0 + q;
-    if (n >= A.n_sel) break;
-    const int64_t row = A.rowsel ? A.rowsel[n] : n;
-    const Place<float> P = place_of<float>(A.t, A.V, row);
-    const bool taught = P.mass != 0.f;                       // (a mass that is no number is the caller's)
-    const float w = row_weight(A, row, taught), g = w / A.norm, lse = s_lse[q], a = dense_factor(P.mass, A.z_coef, lse), ts = mass_of_token(k, P.id, P.t);
-    const float z = P.t != 0.f ? *F.Z.at(n, P.id >> 8, P.id & 255) : 0.f;
-    float l = 0.f, out = 0.f;
-    if (taught) {
-      if (!A.t.logits) {
-        out = __shfl(z, 0, kWave) - lse;
-        l = A.z_coef != 0.f ? fmaf(A.z_coef * lse, lse, -out) : -out;
-      } else {
-        out = l = wave_sum(P.t != 0.f ? P.t * (logf(P.t) - (z - lse)) : 0.f);
-      }
-    }
-    const float e = g != 0.f && P.t != 0.f ? target_entry(z, lse, lse, ts, a) : 0.f, most = wave_max(fabsf(e));
-    const float x = most > 0.f ? most / bf2f(f2bf(most)) : 1.f;
-    const float f = g != 0.f ? g * a * x : 0.f;
-    if (lane < k) F.entries[n * k + lane] = P.t != 0.f ? f2bf(e / x) : kNoEntry;
-    if (lane == 0) {
-      F.R.lse[n] = taught ? lse : 0.f;
-      F.R.ent[n] = taught ? s_ent[q] : 0.f;
-      F.R.l[n] = l;
-      F.R.w[n] = w;
-      F.R.mass[n] = P.mass;
-      F.R.sc[n] = f;
-      F.x[n] = f != 0.f ? 1.f / x : 0.f;
-      F.R.a[n] = out;                                        // to row_out by who comes next: others clear it now
-    }
-    if (!F.Hs) continue;
-    const uint4* h = reinterpret_cast<const uint4*>(F.H + row * A.d);
-    for (int c = lane; c < A.d / 8; c += kWave) {
-      float v[8];
-      bf16x8_to_f32(h[c], v);
-      uint4 o = make_uint4(0u, 0u, 0u, 0u);
-      if (f != 0.f) o = make_uint4(pack_bf16x2(v[0] * f, v[1] * f), pack_bf16x2(v[2] * f, v[3] * f), pack_bf16x2(v[4] * f, v[5] * f), pack_bf16x2(v[6] * f, v[7] * f));
-      reinterpret_cast<uint4*>(F.Hs + (static_cast<int64_t>(c >> 5) * F.mcp + n) * 256)[c & 31] = o;
-    }
+  const float e = g != 0.f && P.t != 0.f ? target_entry(z, lse, lse, ts, a) : 0.f, most = wave_max(fabsf(e));
+  const float x = most > 0.f ? most / bf2f(f2bf(most)) : 1.f;
+  const float f = g != 0.f ? g * a * x : 0.f;
+  if (lane < k) F.entries[n * k + lane] = P.t != 0.f ? f2bf(e / x) : kNoEntry;
+  if (lane == 0) {
+    F.R.lse[n] = taught ? lse : 0.f;
+    F.R.ent[n] = taught ? s_rows.ent[q] : 0.f;
+    F.R.l[n] = l;
+    F.R.w[n] = w;
+    F.R.mass[n] = P.mass;
+    F.R.sc[n] = f;
+    F.x[n] = f != 0.f ? 1.f / x : 0.f;
+    F.R.a[n] = out;                                          // to row_out by who comes next: others clear it now
   }
+  if (F.Hs) copy_row(F.H, row, A.d, f, F.Hs, F.mcp, n);
 }
 // 32 rows of a block of 256 entries to a workgroup; rows up to the next multiple of 64 are zeros.
 constexpr int kTurnedRows = 32;
@@ -906,8 +926,8 @@ umas_status run_bf16(const Call& a, const Ws& w, const Teach& A) {
                            n_pad, Z, Vp);
         UMAS_LAUNCHED("k_target_logits");
       }
-      const unsigned clearing = a.rowsel ? 256 : 0;
-      hipLaunchKernelGGL(k_target_few, dim3(1 + clearing + cdiv(n_sel, 8)), dim3(256), 0, st,
+      const unsigned clearing = a.rowsel ? 128 : 0;
+      hipLaunchKernelGGL(k_target_few, dim3(1 + clearing + cdiv(n_sel, 8)), dim3(kRowsT), 0, st,
                          FewArgs{A, H, w.R, w.R.cref, w.R.entries, w.partial, parts, n_pad, kept, Hs, mcp, a.row_out, live, clearing, static_cast<uint32_t*>(a.dH),
                                  a.n_rows * static_cast<int64_t>(d) / 2, a.n_rows});
       UMAS_LAUNCHED("k_target_few");
@@ -915,9 +935,10 @@ umas_status run_bf16(const Call& a, const Ws& w, const Teach& A) {
                          a.rowsel, n_sel, E, w.R.a, a.row_out, tiles_v, stats);
       UMAS_LAUNCHED("k_target_turn");
     } else if (c0 == 0) {
+      const int share = a.t.k > 4 ? 4 : 1;
       const OpenArgs O{A, H, W, w.R, w.flags, static_cast<int>(cdiv(n_sel, 256)), live, a.rowsel ? static_cast<uint32_t*>(a.dH) : nullptr,
-                       a.n_rows * static_cast<int64_t>(d) / 2, a.row_out, a.row_out ? a.n_rows : 0};
-      hipLaunchKernelGGL(k_target_open, dim3(1 + std::min<unsigned>(std::max<unsigned>(cdiv(n_sel, 4), a.rowsel ? 1024 : 1), 8192)), dim3(256), 0, st, O);
+                       a.n_rows * static_cast<int64_t>(d) / 2, a.row_out, a.row_out ? a.n_rows : 0, share};
+      hipLaunchKernelGGL(k_target_open, dim3(1 + std::min<unsigned>(std::max<unsigned>(cdiv(n_sel, 4 / share), a.rowsel ? 1024 : 1), 8192)), dim3(256), 0, st, O);
       UMAS_LAUNCHED("k_target_open");
     } else {
       hipLaunchKernelGGL(k_live_scan, dim3(1), dim3(512), 0, st, live);
@@ -927,7 +948,7 @@ umas_status run_bf16(const Call& a, const Ws& w, const Teach& A) {
       hipLaunchKernelGGL(k_target_tiles, score_grid(tiles_v, tiles_r, panel, halved), dim3(Cfg::T), 0, st, W, H, d, V, a.rowsel, c0, rows, tiles_v, tiles_r,
                          panel, halved, w.partial, n_pad, w.R.cref, E, Vp, w.flags, w.blk_cidx);
       UMAS_LAUNCHED("k_target_tiles");
-      hipLaunchKernelGGL(k_target_rows, dim3(cdiv(rows, 8)), dim3(256), 0, st,
+      hipLaunchKernelGGL(k_target_rows, dim3(cdiv(rows, 8)), dim3(kRowsT), 0, st,
                          RowsArgs{A, H, w.R, w.partial, tiles_v, n_pad, c0, rows, w.flags, w.blk_cidx, E, tiles_v, Hs, mcp, a.row_out});
       UMAS_LAUNCHED("k_target_rows");
       const PutTargets put{a.rowsel, a.t.ids, a.t.k, w.R.zt, w.R.tt, w.R.lse, w.R.a, w.R.w, A.norm};
