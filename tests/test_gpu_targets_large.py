@@ -1,0 +1,137 @@
+"""Largest logits, cross entropy and distillation where sizes pass a limit: arrays of more than 4 GiB, more rows than one chunk holds.
+
+The reference is float64 on the device, one part of the vocabulary after the other.  Bars: gradients 1e-2 of the largest entry (bf16, as everywhere), log-probs, divergences and
+logsumexps 1e-5 (1 + largest magnitude) + 8 * 2^-24 * largest logit, as for the small sizes.  Selections compare exactly on inputs whose products and sums are exact in float32."""
+import pytest
+import torch
+
+import paper_2605_26646_amd as umas
+
+pytestmark = pytest.mark.gpu
+
+
+def grid(*shape, seed, scale):
+    """Few distinct values, so that float32 sums of products are exact."""
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    out = torch.empty(shape, dtype=torch.bfloat16, device="cuda")
+    for a in range(0, shape[0], 1 << 16):
+        part = out[a:a + (1 << 16)]
+        part.copy_(torch.randint(-8, 9, part.shape, device="cuda", generator=g) * scale)
+    return out
+
+
+def parts_of(V, n):
+    step = max(256, (1 << 28) // max(n, 1) // 8)
+    return [(a, min(a + step, V)) for a in range(0, V, step)]
+
+
+def logits64(H, W, a, b):
+    return H.double() @ W[a:b].double().T
+
+
+def lse64(H, W):
+    out = None
+    for a, b in parts_of(len(W), max(len(H), W.shape[1])):
+        l = torch.logsumexp(logits64(H, W, a, b), 1)
+        out = l if out is None else torch.logaddexp(out, l)
+    return out
+
+
+def taught64(H, W, ids, masses, norm, tokens):
+    """lse, logits of the targets, dH of all rows and dW of the tokens; ids, masses [n, k], everything has a target."""
+    lse, n, V = lse64(H, W), len(H), len(W)
+    zt = torch.stack([(H.double() * W[ids[:, j]].double()).sum(1) for j in range(ids.shape[1])], 1)
+    dH, dW = torch.zeros(H.shape, dtype=torch.float64, device="cuda"), torch.zeros(len(tokens), H.shape[1], dtype=torch.float64, device="cuda")
+    total = masses.sum(1, keepdim=True)
+    for a, b in parts_of(V, max(n, W.shape[1])):
+        dz = (logits64(H, W, a, b) - lse[:, None]).exp() * total
+        for j in range(ids.shape[1]):
+            q = ((ids[:, j] >= a) & (ids[:, j] < b)).nonzero()[:, 0]
+            dz[q, ids[q, j] - a] -= masses[q, j]
+        dz /= norm
+        dH += dz @ W[a:b].double()
+        here = ((tokens >= a) & (tokens < b)).nonzero()[:, 0]
+        dW[here] = dz[:, tokens[here] - a].T @ H.double()
+    return lse, zt, dH, dW
+
+
+def close(got, want, bar, what):
+    scale = float(want.abs().max())
+    assert float((got.double() - want).abs().max()) <= bar * scale, what
+
+
+def check(n, d, V, k, seed, dW=None, rows=None):
+    """Distillation over k targets (cross entropy: 1) at once for all rows or a selection."""
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    H, W = grid(n, d, seed=seed, scale=1 / 8), grid(V, d, seed=seed + 1, scale=1 / 64)
+    ids = torch.randint(0, V, (n, k), device="cuda", generator=g)
+    ids[:: 7, 0] = V - 1                                       # the far end
+    sel = None if rows is None else rows.int()
+    if k == 1:
+        stats, row, dH, dW = umas.umas_cross_entropy_fwd_bwd(H, W, ids[:, 0].int(), sel, dW=dW)
+        masses = torch.ones(n, 1, dtype=torch.float64, device="cuda")
+    else:
+        l = torch.randn(n, k, device="cuda", generator=g)
+        stats, row, dH, dW = umas.umas_distill_fwd_bwd(H, W, ids.int(), l, None, sel, dW=dW)
+        masses = torch.softmax(l.double(), 1)
+    if rows is not None:
+        idle = torch.ones(n, dtype=torch.bool, device="cuda")
+        idle[rows] = False
+        assert not row[idle].any() and not dH[idle].any()
+        H, ids, masses, row, dH = H[rows], ids[rows], masses[rows], row[rows], dH[rows]
+    tokens = torch.cat([torch.tensor([0, 1, V // 2, V - 2, V - 1], device="cuda"), ids[:20].reshape(-1)]).unique()
+    lse, zt, dH_o, dW_o = taught64(H, W, ids, masses, len(H), tokens)
+    want = zt[:, 0] - lse if k == 1 else (masses * (masses.log() - zt + lse[:, None])).sum(1)
+    tol = 1e-5 * (1 + float(want.abs().max())) + 8 * 2.0 ** -24 * float(zt.abs().max() + lse.abs().max())
+    assert float((row.double() - want).abs().max()) <= tol
+    s = umas.read_target_stats(stats)
+    assert abs(float(s["loss"][0]) - float(want.mean()) * (-1 if k == 1 else 1)) <= tol and int(s["n_scored"][0]) == len(H)
+    close(dH, dH_o, 1e-2, "dH")
+    close(dW[tokens], dW_o, 1e-2, "dW")
+
+
+@pytest.mark.parametrize("k", [1, 8])
+def test_numerators_of_more_than_4_gib(k):
+    check(20000, 64, 120001, k, 3)
+
+
+@pytest.mark.parametrize("k,dW", [(1, "bf16"), (4, "float32")])
+def test_more_rows_than_a_chunk_holds(k, dW):
+    check(66000, 64, 1200, k, 5, dW=torch.full((1200, 64), float("nan"), device="cuda") if dW == "float32" else None)
+
+
+@pytest.mark.parametrize("n,d,V", [(3, 4096, 540001), (100, 8192, 270001), (300, 4096, 540001)])
+def test_a_head_of_more_than_4_gib(n, d, V):
+    check(n, d, V, 4, 7)
+
+
+def test_hidden_states_of_almost_4_gib():
+    n, d, V = (1 << 31) // 2048 - 1, 2048, 3000
+    rows = torch.cat([torch.arange(3, device="cuda"), n - 1 - torch.arange(320, device="cuda")])
+    check(n, d, V, 1, 9, rows=rows)
+
+
+@pytest.mark.parametrize("n,d,V,k", [(3, 4096, 540001, 50), (300, 4096, 540001, 64), (9000, 64, 5001, 64)])
+def test_largest_logits(n, d, V, k):
+    H, W = grid(n, d, seed=11, scale=1 / 8), grid(V, d, seed=12, scale=1 / 64)
+    ids, top, lse = umas.umas_top_logits(H, W, k)
+    best = None
+    for a, b in parts_of(V, max(n, d)):                        # a key of logit and token: products are multiples of 1/512
+        key = (logits64(H, W, a, b) * 512).round().long() * 2 ** 20 + torch.arange(2 ** 20 - 1 - a, 2 ** 20 - 1 - b, -1, device="cuda")
+        best = (key if best is None else torch.cat([best, key], 1)).topk(k, dim=1).values
+    assert torch.equal(ids.long(), 2 ** 20 - 1 - (best & (2 ** 20 - 1)))
+    assert torch.equal(top.double(), (best >> 20).double() / 512)
+    want = lse64(H, W)
+    assert float((lse - want).abs().max()) <= 1e-5 * (1 + float(want.abs().max()))
+
+
+def test_largest_logits_of_hidden_states_of_almost_4_gib():
+    n, d, V, k = (1 << 31) // 2048 - 1, 2048, 3000, 4
+    H, W = grid(n, d, seed=13, scale=1 / 8), grid(V, d, seed=14, scale=1 / 64)
+    rows = n - 1 - torch.arange(40, device="cuda")
+    ids, top, lse = umas.umas_top_logits(H, W, k, rows.int())
+    z = logits64(H[rows], W, 0, V)
+    key = (z * 512).round().long() * 2 ** 20 + torch.arange(2 ** 20 - 1, 2 ** 20 - 1 - V, -1, device="cuda")
+    best = key.topk(k, dim=1).values
+    assert torch.equal(ids[rows].long(), 2 ** 20 - 1 - (best & (2 ** 20 - 1)))
+    assert (ids[:n - 40] == -1).all() and not top[:n - 40].any() and not lse[:n - 40].any()
