@@ -10,6 +10,12 @@
  *   umas_policy_logprobs       LM-head scoring: log-prob of the taken token, logsumexp, entropy
  *   umas_ppo_loss_fwd_bwd      scoring + clipped surrogate + backward to hidden states and weights
  *
+ * Around them, further down: the critic, shaping of rewards and advantages, ready batches; and what teaches a head from targets:
+ *
+ *   umas_top_logits            the k largest logits of a head: a teacher's, or a next token's candidates
+ *   umas_cross_entropy_fwd_bwd, umas_distill_fwd_bwd
+ *                              loss and gradients towards given tokens, or towards a teacher's largest logits
+ *
  * Conventions
  *   - THIN metadata (graph, reward scalars) are HOST pointers, caller-owned, read during the
  *     call only (the paper's controller keeps exactly this: role ids, routing ids, reward
@@ -416,7 +422,7 @@ umas_status umas_ready_batch_packed(const umas_streams* streams, int32_t n_model
 /* ---------------------------------------------------------------------------------------------
  * Teaching a head from targets: what a worker group does to a model before and beside the policy update (a supervised
  * warm start, an auxiliary supervised term, one role's model taught by another's).  H, W, rowsel, n_sel, dtype and their
- * limits are those of umas_policy_logprobs; logits are never written out as such.
+ * limits are those of umas_policy_logprobs.
  *
  * Cross entropy of given tokens and its gradient:
  *   z = W h_i, lse_i = log sum_v exp z_v;  l_i = lse_i - z_{ids[i]} + z_coef lse_i^2;  loss = sum_i w_i l_i / norm
@@ -434,8 +440,9 @@ umas_status umas_ready_batch_packed(const umas_streams* streams, int32_t n_model
  *              rounded once).  accumulate_dW = 0 overwrites, 1 adds: to float32 exactly as the policy update does, to bf16
  *              with a rounding per call.  UMAS_NO_DW with dW = NULL: the head is frozen, the product is left out.
  * The bf16 call keeps one bf16 number per (row, vocabulary entry) of a chunk of rows in its workspace, as the policy update
- * does (softmax numerators, not logits), and runs in as few chunks as the workspace allows: of 256 rows in the smallest size, of up
- * to 65536 in the full one.  A dW of bf16 that comes from several chunks is summed in float32 in the workspace. */
+ * does (softmax numerators; the logits in float32 beside them where there are at most 256 selected rows), and runs in as few chunks
+ * as the workspace allows: of 256 rows in the smallest size, of up to 65536 in the full one; float32 calls of 32 rows and up.  A dW of
+ * bf16 that comes from several chunks is summed in float32 in the workspace. */
 typedef struct umas_target_stats {
   float loss;              /* row 0: sum of w_i l_i over norm; roles: over the role's rows */
   float weight_mean;       /* of the selected rows, 0 for ignored ones */
@@ -461,8 +468,8 @@ umas_status umas_cross_entropy_fwd_bwd(const void* H, const void* W, umas_dtype 
  *   lse         DEVICE float [n_rows]: log sum_v exp z_v over the whole vocabulary
  * 1 <= k <= UMAS_MAX_TOP.  Logits of -infinity and those that are not a number are not listed; places left over (they, or
  * V < k) hold token -1 and logit -infinity.  Rows that are not selected get tokens of -1, logits and logsumexp of 0.  H, W,
- * rowsel, n_sel, dtype and their limits as in umas_policy_logprobs.  The workspace bounds what is kept of the logits on the way;
- * the results do not depend on it. */
+ * rowsel, n_sel, dtype and their limits as in umas_policy_logprobs.  The workspace bounds of how many rows logits are kept on the
+ * way, at least 256; the results do not depend on it. */
 size_t umas_top_logits_workspace_bytes_min(int64_t n_sel, int32_t d, int32_t V, int32_t k, umas_dtype dtype);
 size_t umas_top_logits_workspace_bytes(int64_t n_sel, int32_t d, int32_t V, int32_t k, umas_dtype dtype);
 umas_status umas_top_logits(const void* H, const void* W, umas_dtype dtype, int64_t n_rows, int32_t d, int32_t V,

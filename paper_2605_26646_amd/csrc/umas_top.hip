@@ -8,6 +8,9 @@
 // A logit and its token make one 64-bit key whose order is that of the result: the logit's bits, turned so that they order as whole numbers, above the
 // complement of the token.  A wavefront keeps the 64 largest keys it has seen, one to a lane in falling order, and takes only keys beyond its
 // k-th: those collect in LDS until there are 64, are sorted (21 exchanges) and merged with what is there (7).
+//
+// What bounds it: up to 128 rows reading W (one row of 2048 against 151 936 107 us, 5.8 TB/s; 24 rows of 3584 against 152 064 209 us, 5.2 TB/s; 128 rows of 2048 166 us), then
+// the product (8192 rows of 2048 with 64 places 3.82 ms, 1.33 PFLOP/s, of 3.97; 777 rows of 1544 against 50 001 185 us, whole rounds of tiles of 52 to 58 us, of 205).
 #include "umas_f32.h"
 #include "umas_few.h"
 
@@ -196,7 +199,8 @@ __device__ __forceinline__ void top_tiles(const uint16_t* __restrict__ W, const 
                                           int64_t c0, int64_t mc, int first, int tiles_m, int tiles_n, int panel, const Groups& out,
                                           const float* __restrict__ bound, uint16_t* lds, int halved = 0) {
   if constexpr (C::BM == 256 && C::BN == 256) {
-    if (halved > 0) {                                        // the last tiles of every XCD in two halves of 128 rows (see score_tiles)
+    // the last tiles of every XCD in two halves of 128 rows (see score_tiles): 129 rows of 3584 291 -> 265 us, 1000 of 2048 554 -> 543, 777 of 1544 222 -> 215, else +- 1 %
+    if (halved > 0) {
       const int per_xcd = (tiles_m * tiles_n + 7) / 8, xcd = static_cast<int>(blockIdx.x & 7), w = static_cast<int>(blockIdx.x >> 3), whole = per_xcd - halved;
       if (w >= whole) {
         const int in_xcd = whole + (w - whole) / 2, t = xcd * per_xcd + in_xcd, tile_m = t / tiles_n, half = t % tiles_n * 2 + ((w - whole) & 1);
@@ -276,7 +280,7 @@ __device__ __forceinline__ void write_top(const TopOut& O, int64_t row, TopKey l
   O.logits[row * O.k + lane] = logit_of(list);
 }
 // A bound that at least k logits of a row reach: the threads of a workgroup take the maximum over the row's tiles in turn, and the k-th largest of these
-// 256 numbers is it (k at most 64; with random logits 74 groups of thousands reach the 64th).  `lm`, `ls`: the wavefront's part of the logsumexp.
+// 256 numbers is it (k at most 64; with random logits 74 groups of thousands reach the 64th).  By itself, for what is left unwritten, 7 us, 4096 rows 14.  `lm`, `ls`: the wavefront's part of the logsumexp.
 template <int G>
 __device__ __forceinline__ void load_maxima(const float* __restrict__ maxima, int t, float (&x)[G]) {
 #pragma unroll
@@ -330,7 +334,7 @@ k_top_bound(Groups A, int tiles, int k, float* __restrict__ bound) {   // of a r
   if (threadIdx.x == 0) bound[m] = b;
 }
 // A workgroup to a row: the groups that reach its bound are listed, and the wavefronts go through their entries.  The row's logsumexp comes from the tiles'
-// sums on the way.
+// sums on the way.  13 us for one row, a chain of reads and exchanges; 8192 rows with 64 places 117 us.
 constexpr int kAtOnce = 4;                                   // loads of entries under way
 template <class Map>
 __global__ void __launch_bounds__(kSelectT)
@@ -456,7 +460,8 @@ struct TopWs {
 };
 // Tiles of the vocabulary whose logits are all kept: they give the bound that leaves most of the others unwritten.  With n entries in them a group of E = 32 among
 // the others reaches the bound with a probability of about E k / n, and stores 16 bytes at a time, which costs about three times what the rows of whole tiles do:
-// n^2 = 3 E k V; then whole rounds of compute units.
+// n^2 = 3 E k V; then whole rounds of compute units.  With the bound and all logits written: 8192 rows of 2048 against 151 936, 64 places 4.19 and 4.75 ms, 1000 rows, one place
+// 543 and 617 us, 300 rows, 32 places 321 and 335, 777 rows of 1544 against 50 001 215 and 227, 2000 rows of 1024 against 32 000 160 and 170, 129 rows of 3584 265 and 282.
 int first_tiles(int tiles, int tiles_n, int k) {
   const double n = sqrt(3.0 * kEntries<Cfg> * k * (static_cast<double>(tiles) * 256.0));
   const int round = static_cast<int>(cdiv(std::max(device_cus(), 1), tiles_n));
