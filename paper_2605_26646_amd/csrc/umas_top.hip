@@ -29,27 +29,52 @@ __device__ __forceinline__ float logit_of(TopKey k) {
 }
 __device__ __forceinline__ int token_of(TopKey k) { return k ? static_cast<int>(0xFFFFFFFFu - static_cast<uint32_t>(k)) : -1; }
 
-__device__ __forceinline__ TopKey exchange(TopKey x, int j, bool larger) {
-  const TopKey y = __shfl_xor(x, j, kWave);
-  return (x > y) == larger ? x : y;
-}
-__device__ __forceinline__ TopKey sorted_desc(TopKey x) {
+// The value of lane ^ J, J a power of two or 63: moves of the vector unit.  (Through LDS, which a __shfl_xor is, an exchange waits for a round trip of it.)
+template <int CTRL>
+__device__ __forceinline__ uint32_t dpp(uint32_t x) { return static_cast<uint32_t>(__builtin_amdgcn_update_dpp(0, static_cast<int>(x), CTRL, 0xF, 0xF, true)); }
+template <int J>
+__device__ __forceinline__ uint32_t lane_xor(uint32_t x) {
   const int lane = threadIdx.x & 63;
-#pragma unroll
-  for (int k = 2; k <= kWave; k <<= 1)
-#pragma unroll
-    for (int j = k >> 1; j > 0; j >>= 1) x = exchange(x, j, ((lane & j) == 0) == ((lane & k) == 0));
-  return x;
+  if constexpr (J == 1) return dpp<0xB1>(x);
+  else if constexpr (J == 2) return dpp<0x4E>(x);
+  else if constexpr (J == 4) return dpp<0x1B>(dpp<0x141>(x));   // ^ 7, ^ 3
+  else if constexpr (J == 8) return dpp<0x128>(x);
+  else if constexpr (J == 16) {
+    const auto r = __builtin_amdgcn_permlane16_swap(x, x, false, false);   // of every two groups of sixteen: twice the first, twice the second
+    return lane & 16 ? r[0] : r[1];
+  } else if constexpr (J == 32) {
+    const auto r = __builtin_amdgcn_permlane32_swap(x, x, false, false);
+    return lane & 32 ? r[0] : r[1];
+  } else {
+    static_assert(J == 63, "");
+    return lane_xor<32>(lane_xor<16>(dpp<0x140>(x)));
+  }
+}
+template <int J>
+__device__ __forceinline__ float lane_xor(float x) { return __uint_as_float(lane_xor<J>(__float_as_uint(x))); }
+template <int J>
+__device__ __forceinline__ TopKey lane_xor(TopKey x) {
+  return static_cast<TopKey>(lane_xor<J>(static_cast<uint32_t>(x >> 32))) << 32 | lane_xor<J>(static_cast<uint32_t>(x));
+}
+__device__ __forceinline__ TopKey either(bool larger, TopKey x, TopKey y) { return (x > y) == larger ? x : y; }
+__device__ __forceinline__ float either(bool larger, float x, float y) { return larger ? fmaxf(x, y) : fminf(x, y); }
+// A list of 64, one to a lane, that falls and then rises, or the like of it in runs of 2 J: falling in runs of K, rising in every second of them.
+template <int K, int J = K / 2, class T>
+__device__ __forceinline__ T order_runs(T x) {
+  const int lane = threadIdx.x & 63;
+  x = either(((lane & J) == 0) == ((lane & K) == 0), x, lane_xor<J>(x));
+  if constexpr (J > 1) return order_runs<K, J / 2>(x);
+  else return x;
+}
+template <int K = 2, class T>
+__device__ __forceinline__ T sorted_desc(T x) {
+  x = order_runs<K>(x);
+  if constexpr (K < kWave) return sorted_desc<K * 2>(x);
+  else return x;
 }
 // The 64 largest of two falling lists, falling.
-__device__ __forceinline__ TopKey merged(TopKey x, TopKey y) {
-  const int lane = threadIdx.x & 63;
-  const TopKey r = __shfl(y, 63 - lane, kWave);
-  x = x > r ? x : r;
-#pragma unroll
-  for (int j = kWave / 2; j > 0; j >>= 1) x = exchange(x, j, (lane & j) == 0);
-  return x;
-}
+template <class T>
+__device__ __forceinline__ T merged(T x, T y) { return order_runs<kWave>(either(true, x, lane_xor<63>(y))); }
 struct WaveTop {
   TopKey list = 0;
   TopKey least = 0;                                          // keys up to it are not among the k largest (known from outside, or of the list)
@@ -262,10 +287,6 @@ struct FewGroups {
   __device__ __forceinline__ int token(int tile, int g, int e) const { return (tile * per + e) * 16 + g; }
   __device__ __forceinline__ int64_t place(int tile, int g, int e) const { return token(tile, g, e); }
 };
-__device__ __forceinline__ float exchange(float x, int j, bool larger) {
-  const float y = __shfl_xor(x, j, kWave);
-  return larger ? fmaxf(x, y) : fminf(x, y);
-}
 struct TopOut {
   const int32_t* rowsel;
   int64_t c0;
@@ -310,19 +331,12 @@ __device__ __forceinline__ float row_bound(const float* __restrict__ maxima, con
     }
   }
   // the wavefront's 64 maxima, falling; then everybody merges the four lists
-#pragma unroll
-  for (int q = 2; q <= kWave; q <<= 1)
-#pragma unroll
-    for (int j = q >> 1; j > 0; j >>= 1) x = exchange(x, j, ((lane & j) == 0) == ((lane & q) == 0));
+  x = sorted_desc(x);
   s_top[wave][lane] = x;
   __syncthreads();
   x = s_top[0][lane];
 #pragma unroll
-  for (int w = 1; w < kSelectWaves; ++w) {
-    x = fmaxf(x, s_top[w][63 - lane]);
-#pragma unroll
-    for (int j = kWave / 2; j > 0; j >>= 1) x = exchange(x, j, (lane & j) == 0);
-  }
+  for (int w = 1; w < kSelectWaves; ++w) x = merged(x, s_top[w][lane]);
   return __shfl(x, k - 1, kWave);
 }
 __global__ void __launch_bounds__(kSelectT)
