@@ -353,7 +353,7 @@ k_top_bound(Groups A, int tiles, int k, float* __restrict__ bound) {   // of a r
   if (threadIdx.x == 0) bound[m] = b;
 }
 // A workgroup to a row: the groups that reach its bound are listed, and the wavefronts go through their entries.  The row's logsumexp comes from the tiles'
-// sums on the way.  13 us for one row, a chain of reads and exchanges; 8192 rows with 64 places 117 us.
+// sums on the way.  12 us for one row, a chain of reads and exchanges (through LDS 13); 8192 rows with 64 places 114 us.
 constexpr int kAtOnce = 4;                                   // loads of entries under way
 template <class Map>
 __global__ void __launch_bounds__(kSelectT)
