@@ -226,11 +226,10 @@ __device__ __forceinline__ void zero_acc(floatx4 (&acc)[C::MI][C::NI]) {
 // first `rows` rows are wanted: a pass of loads behind them takes the lines of the first one again, which are on their way to this
 // compute unit anyhow (the last row for all of them made one line hot: 203 rows of 2048 613 -> 650 us); K runs over the vocabulary, four steps of 64 per block
 template <class C>
-__device__ __forceinline__ KContig blocked_rows_tile(const uint16_t* X, int blk_pitch, int64_t tiles_v, int64_t row_blk, int voc_blk, int rows) {
+__device__ __forceinline__ KContig blocked_rows_tile(const uint16_t* X, int blk_pitch, int64_t tiles_v, int64_t row_blk, int voc_blk, int rows, int tid) {
   KContig c;
   c.rsrc = make_rsrc(X + blk_offset(row_blk, voc_blk, tiles_v) * blk_pitch);
   c.hi_bytes = static_cast<uint32_t>(kBlkElems * 2 * blk_pitch - 4 * 128);        // from the fourth step of a block to the next block
-  const int tid = tile_thread();
   const uint32_t kofs = ring2_kofs(tid);
 #pragma unroll
   for (int i = 0; i < 4; ++i) c.off[i] = (static_cast<uint32_t>(ring2_row<C>(ring2_row<C>(i, 0) < rows ? i : 0, tid)) * 256u + kofs) * 2u;
@@ -274,11 +273,11 @@ __device__ __forceinline__ floatx4 turn_out(const char* turn, int i, int lane) {
 __device__ __forceinline__ bool past_caches(int d, int V) { return d % 16 == 0 || !beyond_cache(d, V, int64_t{128} << 20); }   // twice that in dW
 // `turn` is the wavefront's own part of LDS
 template <class C>
-__device__ __forceinline__ void store_acc_f32(const floatx4 (&acc)[C::MI][C::NI], char* turn, float* out, int64_t ld, int64_t rows, int cols,
+__device__ __forceinline__ void store_acc_f32(const floatx4 (&acc)[C::MI][C::NI], int tid, char* turn, float* out, int64_t ld, int64_t rows, int cols,
                                               int accumulate, bool past) {
   static_assert(C::WTM == Cfg::WTM && C::WTN == Cfg::WTN, "the turn is written for these");
   typedef float f32x4_a4 __attribute__((ext_vector_type(4), aligned(4)));   // dW has the alignment of a float
-  const int tid = tile_thread(), lane = tid & 63, wave = tid >> 6;
+  const int lane = tid & 63, wave = tid >> 6;
   const int r0 = wave / C::WN * C::WTM, c0 = wave % C::WN * C::WTN + (lane & 15) * 4;
   const bool whole = rows >= C::BM && cols >= C::BN && ld <= kPieceLd;   // the same for every thread
   float* const dst = out + (r0 + (lane >> 4)) * ld + c0;
@@ -343,9 +342,9 @@ __device__ __forceinline__ void store_acc_f32(const floatx4 (&acc)[C::MI][C::NI]
 // The same into rows of bf16: eight columns of eight rows to a store, 128 bytes a row.  Sums are rounded once; what is added to was rounded by
 // whoever wrote it.  The rows are 16-byte aligned.
 template <class C>
-__device__ __forceinline__ void store_acc_bf16(const floatx4 (&acc)[C::MI][C::NI], char* turn, uint16_t* out, int64_t ld, int64_t rows, int cols, int accumulate) {
+__device__ __forceinline__ void store_acc_bf16(const floatx4 (&acc)[C::MI][C::NI], int tid, char* turn, uint16_t* out, int64_t ld, int64_t rows, int cols, int accumulate) {
   static_assert(C::WTM == Cfg::WTM && C::WTN == Cfg::WTN, "the turn is written for these");
-  const int tid = tile_thread(), lane = tid & 63, wave = tid >> 6;
+  const int lane = tid & 63, wave = tid >> 6;
   const int r0 = wave / C::WN * C::WTM + (lane >> 3), c0 = wave % C::WN * C::WTN + (lane & 7) * 8;
   typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 #pragma unroll
@@ -371,12 +370,12 @@ __device__ __forceinline__ void store_acc_bf16(const floatx4 (&acc)[C::MI][C::NI
   }
 }
 template <class C>
-__device__ __forceinline__ void store_dw(const floatx4 (&acc)[C::MI][C::NI], char* turn, float* out, int64_t ld, int64_t rows, int cols, int accumulate, bool past) {
-  store_acc_f32<C>(acc, turn, out, ld, rows, cols, accumulate, past);
+__device__ __forceinline__ void store_dw(const floatx4 (&acc)[C::MI][C::NI], int tid, char* turn, float* out, int64_t ld, int64_t rows, int cols, int accumulate, bool past) {
+  store_acc_f32<C>(acc, tid, turn, out, ld, rows, cols, accumulate, past);
 }
 template <class C>
-__device__ __forceinline__ void store_dw(const floatx4 (&acc)[C::MI][C::NI], char* turn, uint16_t* out, int64_t ld, int64_t rows, int cols, int accumulate, bool) {
-  store_acc_bf16<C>(acc, turn, out, ld, rows, cols, accumulate);
+__device__ __forceinline__ void store_dw(const floatx4 (&acc)[C::MI][C::NI], int tid, char* turn, uint16_t* out, int64_t ld, int64_t rows, int cols, int accumulate, bool) {
+  store_acc_bf16<C>(acc, tid, turn, out, ld, rows, cols, accumulate);
 }
 typedef uint32_t u32x2_a2 __attribute__((ext_vector_type(2), aligned(2)));     // dH has the alignment of its entries
 // What the sliced products leave behind: partial sums in blocks of 256 x 256 floats [slice][row tile][column tile].
@@ -399,7 +398,8 @@ __device__ __forceinline__ void dh_tile(int tile_m, int m_rows, int orig_blk, in
   const int n0 = tile_n * C::BN;
   const int voc_blk = slice * sl.voc_blks, tiles_v = static_cast<int>(Vp >> 8);
   const int k_len = min(sl.voc_blks, tiles_v - voc_blk) * 256;       // a multiple of 256, at least 256
-  const KContig ca = blocked_rows_tile<C>(dZ, blk_pitch, tiles_v, tile_m, voc_blk, m_rows);
+  int tid = cut_thread<C>(m_rows, d - n0);
+  const KContig ca = blocked_rows_tile<C>(dZ, blk_pitch, tiles_v, tile_m, voc_blk, m_rows, tid);
   KMajor kb;
   kb.base = reinterpret_cast<const char*>(W + static_cast<int64_t>(voc_blk) * 256 * d + n0);
   kb.ld_bytes = static_cast<int64_t>(d) * 2;
@@ -412,21 +412,23 @@ __device__ __forceinline__ void dh_tile(int tile_m, int m_rows, int orig_blk, in
   // row tile W is read once: past the caches where it is larger than they are, so that the operand, which every column tile
   // reads, stays there (both products of 203 rows of 3584 762 -> 707 us, of 60 rows of 2048 449 -> 384; with up to four row tiles
   // 725 rows that add to dW gain 1.7 %, 1000 rows lose 1 to 3).
-  // Up to half a tile of rows is multiplied by half of the wavefronts only, which halves the time of the matrix cores: every SIMD has one of either
+  // Up to half a tile of rows or columns is multiplied by half of the wavefronts only, which halves the time of the matrix cores: every SIMD has one of either
   // half.  (With the same loop for all numbers of rows 203 and 725 rows take 0.4 % longer.)
-  if (m_rows <= C::WTM && w_once) mfma_mainloop_mixed<C, false, true, 2, true, true>(ca, KMajor{}, KContig{}, kb, k_len, lds, acc, m_rows);
-  else if (m_rows <= C::WTM) mfma_mainloop_mixed<C, false, true, 2, false, true>(ca, KMajor{}, KContig{}, kb, k_len, lds, acc, m_rows);
-  else if (w_once) mfma_mainloop_mixed<C, false, true, 2, true>(ca, KMajor{}, KContig{}, kb, k_len, lds, acc);
-  else mfma_mainloop_mixed<C, false, true, 2>(ca, KMajor{}, KContig{}, kb, k_len, lds, acc);
+  const bool cut = m_rows <= C::WTM || d - n0 <= C::BN / 2;
+  if (cut && w_once) mfma_mainloop_mixed<C, false, true, 2, true, true>(ca, KMajor{}, KContig{}, kb, k_len, lds, acc, tid, m_rows, d - n0);
+  else if (cut) mfma_mainloop_mixed<C, false, true, 2, false, true>(ca, KMajor{}, KContig{}, kb, k_len, lds, acc, tid, m_rows, d - n0);
+  else if (w_once) mfma_mainloop_mixed<C, false, true, 2, true>(ca, KMajor{}, KContig{}, kb, k_len, lds, acc, tid);
+  else mfma_mainloop_mixed<C, false, true, 2>(ca, KMajor{}, KContig{}, kb, k_len, lds, acc, tid);
+  tid = cut_thread<C>(m_rows, d - n0);
   if (sl.n > 1) {
     float* out = sl.part + ((static_cast<int64_t>(slice) * tiles_r + tile_m) * tiles_d + tile_n) * (C::BM * C::BN);
-    store_acc_f32<C>(acc, reinterpret_cast<char*>(lds) + (tile_thread() >> 6) * kTurnBytes, out, C::BN, C::BM, C::BN, 0, false);
+    store_acc_f32<C>(acc, tid, reinterpret_cast<char*>(lds) + (tid >> 6) * kTurnBytes, out, C::BN, C::BM, C::BN, 0, false);
     return;
   }
   // dH rows leave like the float32 ones: 32 rows at a time through LDS, 128 bytes of four rows to a store, the row numbers,
   // factors and rows of W of a piece fetched together.  (One 2-byte entry after the other, each with its own chain of loads:
   // both products of 39 000 rows of 2048 37.43 ms, like this 37.16, 12 000 rows 11.48 and 11.37.)
-  const int tid = tile_thread(), lane = tid & 63, wave = tid >> 6;
+  const int lane = tid & 63, wave = tid >> 6;
   char* turn = reinterpret_cast<char*>(lds) + wave * kTurnBytes;
   const int64_t r0 = m0 + wave / C::WN * C::WTM + (lane >> 4);
   const int j = n0 + wave % C::WN * C::WTN + (lane & 15) * 4, jw = min(j, d - 4);   // d is a multiple of 8: four columns are all inside or all outside
@@ -492,8 +494,11 @@ __device__ __forceinline__ void dw_tile(int tile_m, int tile_n, const uint16_t* 
   kb.n_units = min(32, (d - n0) / 8);
   floatx4 acc[C::MI][C::NI];
   zero_acc<C>(acc);
-  if (k_len > 0) mfma_mainloop_mixed<C, true, true, 1>(KContig{}, ka, KContig{}, kb, k_len, lds, acc);
-  store_dw<C>(acc, reinterpret_cast<char*>(lds) + (tile_thread() >> 6) * kTurnBytes, dW + m0 * d + n0, d, V - m0, d - n0, accumulate, past_caches(d, V));   // d is a multiple of 8
+  int tid = cut_thread<C>(C::BM, d - n0);
+  if (k_len > 0 && d - n0 <= C::BN / 2) mfma_mainloop_mixed<C, true, true, 1, false, true>(KContig{}, ka, KContig{}, kb, k_len, lds, acc, tid, C::BM, d - n0);
+  else if (k_len > 0) mfma_mainloop_mixed<C, true, true, 1>(KContig{}, ka, KContig{}, kb, k_len, lds, acc, tid);
+  tid = cut_thread<C>(C::BM, d - n0);
+  store_dw<C>(acc, tid, reinterpret_cast<char*>(lds) + (tid >> 6) * kTurnBytes, dW + m0 * d + n0, d, V - m0, d - n0, accumulate, past_caches(d, V));   // d is a multiple of 8
 }
 
 // dW of at most 256 rows.  A tile of 256 x 256 that a compute unit works on alone is products, then stores, and the next tile's first loads wait for these
@@ -626,7 +631,7 @@ __device__ __forceinline__ void dw_short(const uint16_t* __restrict__ dZ, int bl
   char* const turn = lds + (nsub + (wave == 3 ? 1 : 0)) % 3 * kShortStage + (wave == 3 ? 0 : wave) * kTurnBytes;
   const int64_t m0 = static_cast<int64_t>(tile_m) * C::BM;
   const int n0 = tile_n * C::BN;
-  store_dw<C>(acc, turn, dW + m0 * d + n0, d, V - m0, d - n0, accumulate, past_caches(d, V));
+  store_dw<C>(acc, tile_thread(), turn, dW + m0 * d + n0, d, V - m0, d - n0, accumulate, past_caches(d, V));
 }
 // Both products in one launch, in groups of 4 x 8 tiles that are worked on together on one XCD.  Every XCD owns a contiguous
 // range of the dH tiles (slice after slice, so that its workgroups share a slice of both operands) and behind it the share

@@ -34,8 +34,10 @@ struct TileCfg {
 
 // The thread's number as a value that the compiler takes for a new one every time: what a tile derives from it (addresses of
 // loads and fragments, dozens of registers for each kind of tile) is then not kept over a loop of tiles.
-__device__ __forceinline__ int tile_thread() {
+// `swapped`: with wavefronts 2, 3 and 4, 5 in each other's place, so that those of the right half of a tile of 256 x 256 are 4 to 7, one on every SIMD.
+__device__ __forceinline__ int tile_thread(bool swapped = false) {
   int t = threadIdx.x;
+  if (swapped) t = (t & ~0x180) | (t & 0x80) << 1 | (t & 0x100) >> 1;
   asm volatile("" : "+v"(t));
   return t;
 }
@@ -244,15 +246,17 @@ struct KContig {                // an operand tile stored K-contiguous: per-slot
   uint32_t hi_bytes;            // added once more per 256 k (an operand stored in blocks of 256 columns), else 0
 };
 
-// B_STREAM: operand B is read once, past the caches.  CUT: only m_rows rows of the tile are looked at; a wavefront whose sub-tile has none of
-// them loads for the others and multiplies nothing.
+// B_STREAM: operand B is read once, past the caches.  CUT: only m_rows rows and n_cols columns of the tile are looked at; a wavefront whose sub-tile has none of
+// them loads for the others and multiplies nothing.  Half a tile of either takes half the time of the matrix cores if it is one wavefront of every SIMD that does: `tid`, the
+// number of the thread in the tile, sees to that (cut_thread).
+template <class C>
+__device__ __forceinline__ int cut_thread(int m_rows, int n_cols) { return tile_thread(m_rows > C::WTM && n_cols <= C::BN / 2); }
 template <class C, bool ATR, bool BTR, int AHEAD, bool B_STREAM = false, bool CUT = false>
 __device__ __forceinline__ void mfma_mainloop_mixed(const KContig& ca, const KMajor& ka, const KContig& cb, const KMajor& kb,
-                                                    int K, uint16_t* lds, floatx4 (&acc)[C::MI][C::NI], int m_rows = C::BM) {
+                                                    int K, uint16_t* lds, floatx4 (&acc)[C::MI][C::NI], int tid, int m_rows = C::BM, int n_cols = C::BN) {
   using R = Ring2Cfg<C>;
   static_assert(C::BM == 256 && C::BN == 256 && C::T == 512 && R::NA == 4 && R::NB == 4, "written for 256x256 tiles, 8 wavefronts");
   constexpr int HA = C::MI / 2;                      // A blocks of one half of the wavefront's sub-tile
-  const int tid = tile_thread();
   const int lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int wm = wave / C::WN, wn = wave % C::WN;
@@ -412,7 +416,7 @@ __device__ __forceinline__ void mfma_mainloop_mixed(const KContig& ca, const KMa
   __builtin_amdgcn_s_barrier();
   auto next3 = [](int i) { return i == 2 ? 0 : i + 1; };
   int ia = 0, ib = 0;                                // stages of the current step
-  if (CUT && wm * C::WTM >= m_rows) {                // the loads and barriers of the loop below
+  if (CUT && (wm * C::WTM >= m_rows || wn * C::WTN >= n_cols)) {   // the loads and barriers of the loop below
     for (int j = 0; j < nsub; ++j) {
       const int ia1 = AHEAD == 1 ? next3(ia) : (ia ^ 1), ib1 = AHEAD == 2 ? next3(ib) : (ib ^ 1);
       if (AHEAD == 1) {
