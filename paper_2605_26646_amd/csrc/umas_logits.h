@@ -164,7 +164,8 @@ __device__ __forceinline__ void score_tile(const uint16_t* __restrict__ W, const
   // vocabulary entries vbase + 16 i + r (i < MI, r < 4); the four lanes l, l + 16, l + 32, l + 48 share a column.
   float* s_part = reinterpret_cast<float*>(reinterpret_cast<char*>(lds) + (LEAVE == Leave::kNothing ? 0 : Stage<C>::kBytes));   // [WM][BN][3], behind the staging area
   float* s_zy = s_part + C::WM * C::BN * 3;               // [BN]
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  // (the thread's own number instead kept what two kinds of tile derive from it in registers: logits of 203 rows of 3584 with 252 bytes of scratch a lane 327 us, now 277)
+  const int tid = tile_thread(), lane = tid & 63, wave = tid >> 6;
   const int wm = wave / C::WN;
   char* stage = reinterpret_cast<char*>(lds) + wave * (LEAVE == Leave::kLogits ? 16 * kLogitPitch<C> : C::WTN * kPitch);
   if (threadIdx.x < C::BN) s_zy[threadIdx.x] = 0.f;
@@ -323,13 +324,42 @@ __device__ __forceinline__ void score_tile(const uint16_t* __restrict__ W, const
 // 130.1 -> 119.9, 217.8 -> 208.5 and 389.7 -> 382.4, of 2048 against 151 936 294.2 -> 276.9, 553.2 -> 547.4 and 1014 -> 1023, 900 of 3584 918 -> 900; where
 // the last round is fuller nothing changes.
 using HalfCfg = TileCfg<256, 128, 2, 4>;                 // the lanes of a row as in a whole tile: the same bits
-template <Leave LEAVE, class C>
+// So is a tile whose rows end in its first half: 300 rows of 2048 against 151 936 265 -> 250 us, 600 371 -> 357, 4200 of 3584 3454 -> 3376, 262 of 1664 against 63 167 88 -> 81.
+enum class HalfTile { kNone, kWhole, kHalf };
+// The tile of a workgroup, `it` of its kTilesPerWg, of the `mc` rows; a half's number counts halves.
+__device__ __forceinline__ HalfTile half_tile(int tiles_m, int tiles_n, int panel, int halved, int it, int64_t mc, int* tile_m, int* tile_n) {
+  if (halved > 0) {                               // the last `halved` tiles of every XCD
+    const int per_xcd = (tiles_m * tiles_n + 7) / 8, xcd = static_cast<int>(blockIdx.x & 7), w = static_cast<int>(blockIdx.x >> 3), whole = per_xcd - halved;
+    if (w >= whole) {
+      const int in_xcd = whole + (w - whole) / 2, t = xcd * per_xcd + in_xcd;
+      *tile_m = t / tiles_n;
+      *tile_n = t % tiles_n * 2 + ((w - whole) & 1);
+      return it == 0 && in_xcd < per_xcd && *tile_m < tiles_m && *tile_n * HalfCfg::BN < mc ? HalfTile::kHalf : HalfTile::kNone;
+    }
+  }
+  if (!tile_coords<kGM, kGN>(tiles_m, tiles_n, panel, tile_m, tile_n, it, kTilesPerWg)) return HalfTile::kNone;
+  if (*tile_n == 0 || mc - static_cast<int64_t>(*tile_n) * Cfg::BN > HalfCfg::BN) return HalfTile::kWhole;   // (a single row tile reads W once: whole)
+  *tile_n *= 2;
+  return HalfTile::kHalf;
+}
+// ENDS: with halves where the rows end in the first half of a tile.  (A loop of its own, which costs whole tiles 0.8 %: 16 384 rows of 2048 7.82 -> 7.88 ms.)
+template <Leave LEAVE, class C, bool ENDS = false>
 __device__ __forceinline__ void score_tiles(const uint16_t* __restrict__ W, const uint16_t* __restrict__ H, int d, int V,
                                             const int32_t* __restrict__ rowsel, int64_t c0, int64_t mc,
                                             const int32_t* __restrict__ ids, int tiles_m, int tiles_n, int panel,
                                             float4* __restrict__ partial, int64_t n_pad, const KeepArgs& keep,
                                             uint16_t* lds, int halved = 0) {
   const bool w_once = tiles_n == 1 && beyond_cache(d, V, kLogitsOnceBytes);
+  if constexpr (ENDS) {
+    for (int it = 0; it < kTilesPerWg; ++it) {
+      int tile_m, tile_n;
+      const HalfTile h = half_tile(tiles_m, tiles_n, panel, halved, it, mc, &tile_m, &tile_n);
+      if (h == HalfTile::kNone) continue;
+      if (h == HalfTile::kHalf) score_tile<LEAVE, HalfCfg>(W, H, d, V, rowsel, c0, mc, ids, tile_m, tile_n, false, partial, n_pad, keep, lds);
+      else score_tile<LEAVE, C>(W, H, d, V, rowsel, c0, mc, ids, tile_m, tile_n, w_once, partial, n_pad, keep, lds);
+    }
+    return;
+  }
   if constexpr (C::BM == 256 && C::BN == 256) {
     if (halved > 0) {                             // the last `halved` tiles of every XCD
       const int per_xcd = (tiles_m * tiles_n + 7) / 8, xcd = static_cast<int>(blockIdx.x & 7), w = static_cast<int>(blockIdx.x >> 3), whole = per_xcd - halved;

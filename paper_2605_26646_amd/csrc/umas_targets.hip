@@ -14,7 +14,7 @@
 //
 // What bounds it: the products.  16 384 rows of 2048 against 151 936: the scores 7.85 ms (1.30 PFLOP/s), both gradients 14.9 ms (1.36 PFLOP/s), all else 0.13 ms;
 // 4096 rows 2.06 and 3.80 ms and 0.21 (64 targets a row).  Fewer rows are bound by W and dW, which have to be read twice and written: 203 rows of 3584 against
-// 152 064, 3.3 GB and 1.0 TFLOP of whole blocks: 0.98 ms.
+// 152 064, 3.3 GB and 1.0 TFLOP of whole blocks: 0.94 ms.
 //
 // Roundings to bf16: an entry of E (relative error up to 2^-9; the sum of exponentials and the logsumexp are float32 and do not see it), the scaled
 // copy of H, and the results.  A row of dW that a single row of H makes carries all three: 270 to 2000 rows dW is off by 0.0024 to 0.0028 of its norm, where
@@ -260,6 +260,14 @@ k_target_tiles(const uint16_t* __restrict__ W, const uint16_t* __restrict__ H, i
   __shared__ __attribute__((aligned(16))) uint16_t lds[kLogitLds / 2];
   score_tiles<Leave::kNumerators, Cfg>(W, H, d, V, rowsel, c0, mc, nullptr, tiles_m, tiles_n, panel, partial, n_pad, KeepArgs{cref, E, Vp, flags, cidx, nullptr}, lds, halved);
 }
+// ... where the rows end in the first half of a tile of 256
+__global__ void __launch_bounds__(Cfg::T)
+k_target_tiles_end(const uint16_t* __restrict__ W, const uint16_t* __restrict__ H, int d, int V, const int32_t* __restrict__ rowsel, int64_t c0, int64_t mc,
+                   int tiles_m, int tiles_n, int panel, int halved, float4* __restrict__ partial, int64_t n_pad, const float* __restrict__ cref,
+                   uint16_t* __restrict__ E, int64_t Vp, int32_t* __restrict__ flags, const int32_t* __restrict__ cidx) {
+  __shared__ __attribute__((aligned(16))) uint16_t lds[kLogitLds / 2];
+  score_tiles<Leave::kNumerators, Cfg, true>(W, H, d, V, rowsel, c0, mc, nullptr, tiles_m, tiles_n, panel, partial, n_pad, KeepArgs{cref, E, Vp, flags, cidx, nullptr}, lds, halved);
+}
 // ------------------------------------------------------------------ bf16: rows
 // Eight rows to a workgroup, a wavefront to each, which asks for what it needs of its row; then all of them merge the rows' parts (a load covers the eight rows of
 // eight parts), and a wavefront goes on with its row: its loss and factor, its k entries of the operand, its scaled copy of H.  Bound by the parts (16 bytes a row and tile) and
@@ -391,7 +399,7 @@ k_target_rows(RowsArgs O) {
 // Up to 256 rows the scores leave their logits in float32 instead: 6 bytes a logit more to write and read, of which there are few here, in place of the
 // gather, the references and what they may not serve for.  The operand is then made from the logits, D = bf16(dz / (g a' x)), with f = g a' x as the row factor: x, near
 // 1, is what makes the row's largest target entry, rounded, exact.  It costs the others no second rounding here, so that dW has it as well.  (Few rows are where
-// it shows: a row of dW is one row's entry times its hidden state.  203 rows of 3584 dW off by 0.0023 of its norm, by the way of more rows 0.0027, for 979 us in place of
+// it shows: a row of dW is one row's entry times its hidden state.  203 rows of 3584 dW off by 0.0023 of its norm, by the way of more rows 0.0027, for 940 us in place of
 // 909; from a whole block on the logits would cost more than that.)
 constexpr uint16_t kNoEntry = 0xFFFF;                        // a place that does not count
 __global__ void __launch_bounds__(Cfg::T)
@@ -958,7 +966,9 @@ umas_status run_bf16(const Call& a, const Ws& w, const Teach& A) {
       UMAS_LAUNCHED("k_live_scan");
     }
     if (!few) {
-      hipLaunchKernelGGL(k_target_tiles, score_grid(tiles_v, tiles_r, panel, halved), dim3(Cfg::T), 0, st, W, H, d, V, a.rowsel, c0, rows, tiles_v, tiles_r,
+      // (half a tile less of 17 is 2 %, of 64 what the other loop costs)
+      const bool ends = rows % Cfg::BN != 0 && rows % Cfg::BN <= HalfCfg::BN && tiles_r <= 32;
+      hipLaunchKernelGGL(ends ? k_target_tiles_end : k_target_tiles, score_grid(tiles_v, tiles_r, panel, halved), dim3(Cfg::T), 0, st, W, H, d, V, a.rowsel, c0, rows, tiles_v, tiles_r,
                          panel, halved, w.partial, n_pad, w.R.cref, E, Vp, w.flags, w.blk_cidx);
       UMAS_LAUNCHED("k_target_tiles");
       hipLaunchKernelGGL(k_target_rows, dim3(cdiv(rows, 8)), dim3(kRowsT), 0, st,

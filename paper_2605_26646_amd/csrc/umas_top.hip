@@ -223,22 +223,19 @@ template <class C, bool ALL>
 __device__ __forceinline__ void top_tiles(const uint16_t* __restrict__ W, const uint16_t* __restrict__ H, int d, int V, const int32_t* __restrict__ rowsel,
                                           int64_t c0, int64_t mc, int first, int tiles_m, int tiles_n, int panel, const Groups& out,
                                           const float* __restrict__ bound, uint16_t* lds, int halved = 0) {
-  if constexpr (C::BM == 256 && C::BN == 256) {
-    // the last tiles of every XCD in two halves of 128 rows (see score_tiles): 129 rows of 3584 291 -> 265 us, 1000 of 2048 554 -> 543, 777 of 1544 222 -> 215, else +- 1 %
-    if (halved > 0) {
-      const int per_xcd = (tiles_m * tiles_n + 7) / 8, xcd = static_cast<int>(blockIdx.x & 7), w = static_cast<int>(blockIdx.x >> 3), whole = per_xcd - halved;
-      if (w >= whole) {
-        const int in_xcd = whole + (w - whole) / 2, t = xcd * per_xcd + in_xcd, tile_m = t / tiles_n, half = t % tiles_n * 2 + ((w - whole) & 1);
-        if (in_xcd < per_xcd && tile_m < tiles_m && half * HalfCfg::BN < mc) top_tile<HalfCfg, ALL>(W, H, d, V, rowsel, c0, mc, first + tile_m, half, false, out, bound, lds);
-        return;
-      }
-    }
-  }
   const bool w_once = tiles_n == 1 && beyond_cache(d, V, kLogitsOnceBytes);
   for (int it = 0; it < kTilesPerWg; ++it) {
     int tile_m, tile_n;
-    if (!tile_coords<kGM, kGN>(tiles_m, tiles_n, panel, &tile_m, &tile_n, it, kTilesPerWg)) continue;
-    top_tile<C, ALL>(W, H, d, V, rowsel, c0, mc, first + tile_m, tile_n, w_once, out, bound, lds);
+    // halves as in score_tiles: of the last round 129 rows of 3584 291 -> 265 us, 1000 of 2048 554 -> 543, 777 of 1544 222 -> 215, else +- 1 %; at the end of the
+    // rows 300 of 2048 319 -> 290, 600 of 3584 681 -> 645, 2100 of 2048 1188 -> 1120
+    if constexpr (C::BM == 256 && C::BN == 256) {
+      const HalfTile h = half_tile(tiles_m, tiles_n, panel, halved, it, mc, &tile_m, &tile_n);
+      if (h == HalfTile::kNone) continue;
+      if (h == HalfTile::kHalf) top_tile<HalfCfg, ALL>(W, H, d, V, rowsel, c0, mc, first + tile_m, tile_n, false, out, bound, lds);
+      else top_tile<C, ALL>(W, H, d, V, rowsel, c0, mc, first + tile_m, tile_n, w_once, out, bound, lds);
+    } else {
+      if (tile_coords<kGM, kGN>(tiles_m, tiles_n, panel, &tile_m, &tile_n, it, kTilesPerWg)) top_tile<C, ALL>(W, H, d, V, rowsel, c0, mc, first + tile_m, tile_n, w_once, out, bound, lds);
+    }
   }
 }
 __global__ void __launch_bounds__(Cfg::T)
