@@ -339,43 +339,54 @@ __device__ __forceinline__ void store_acc_f32(const floatx4 (&acc)[C::MI][C::NI]
     }
   }
 }
+// More rows, whose products are longer than the stores, lose more by what the stores push out of the caches (455 rows of 2680 242 -> 252 us the pass).
+__device__ __forceinline__ bool store_lines(int d, int rows) { return d % 64 == 0 || rows > 256; }
 // The same into rows of bf16: eight columns of eight rows to a store, 128 bytes a row.  Sums are rounded once; what is added to was rounded by
-// whoever wrote it.  The rows are 16-byte aligned.
+// whoever wrote it.  The rows are 16-byte aligned.  `whole_lines`: stores past the caches, which is what pays where a piece of a row is lines of its own.  (Where rows start anywhere in a
+// line, neighbours share one, and the caches put it together: both products of 31 rows of 2456 against 56 239 184 us, through the caches 120, dW of 200 of 3592 against 120 001
+// 427 and 318; what they push out of the caches costs the next call's logits 30 to 45.)
 template <class C>
-__device__ __forceinline__ void store_acc_bf16(const floatx4 (&acc)[C::MI][C::NI], int tid, char* turn, uint16_t* out, int64_t ld, int64_t rows, int cols, int accumulate) {
+__device__ __forceinline__ void store_acc_bf16(const floatx4 (&acc)[C::MI][C::NI], int tid, char* turn, uint16_t* out, int64_t ld, int64_t rows, int cols, int accumulate,
+                                               bool whole_lines) {
   static_assert(C::WTM == Cfg::WTM && C::WTN == Cfg::WTN, "the turn is written for these");
-  const int lane = tid & 63, wave = tid >> 6;
-  const int r0 = wave / C::WN * C::WTM + (lane >> 3), c0 = wave % C::WN * C::WTN + (lane & 7) * 8;
+  const int lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int w_row = wave / C::WN * C::WTM, c0 = wave % C::WN * C::WTN + (lane & 7) * 8;
   typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+  // (a store's policy is part of the instruction)
+  auto pieces = [&](auto stream) {
+    constexpr int kWrite = decltype(stream)::value ? kStream : kCached;
 #pragma unroll
-  for (int h = 0; h < C::MI / 2; ++h) {
-    turn_in(acc, h, turn, lane);
+    for (int h = 0; h < C::MI / 2; ++h) {
+      turn_in(acc, h, turn, lane);
+      const __amdgpu_buffer_rsrc_t rsrc = make_rsrc(out + (w_row + h * 32) * ld);   // 32 rows are in reach of 32 bits
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const int r = i * 8 + (lane >> 3), unit = (lane & 7) * 2, turned = 4 * ((r >> 2) & 3);
-      floatx4 lo = *reinterpret_cast<const floatx4*>(turn + r * 256 + (unit ^ turned) * 16);
-      floatx4 hi = *reinterpret_cast<const floatx4*>(turn + r * 256 + ((unit + 1) ^ turned) * 16);
-      if (r0 + h * 32 + i * 8 < rows && c0 < cols) {                 // d is a multiple of 8: eight columns are all inside or all outside
-        uint16_t* const at = out + (r0 + h * 32 + i * 8) * ld + c0;
-        if (accumulate) {
-          const u32x4 x = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(at));
-          lo += floatx4{__uint_as_float(x[0] << 16), __uint_as_float(x[0] & 0xffff0000u), __uint_as_float(x[1] << 16), __uint_as_float(x[1] & 0xffff0000u)};
-          hi += floatx4{__uint_as_float(x[2] << 16), __uint_as_float(x[2] & 0xffff0000u), __uint_as_float(x[3] << 16), __uint_as_float(x[3] & 0xffff0000u)};
+      for (int i = 0; i < 4; ++i) {
+        const int r = i * 8 + (lane >> 3), unit = (lane & 7) * 2, turned = 4 * ((r >> 2) & 3);
+        floatx4 lo = *reinterpret_cast<const floatx4*>(turn + r * 256 + (unit ^ turned) * 16);
+        floatx4 hi = *reinterpret_cast<const floatx4*>(turn + r * 256 + ((unit + 1) ^ turned) * 16);
+        if (w_row + h * 32 + r < rows && c0 < cols) {                // d is a multiple of 8: eight columns are all inside or all outside
+          const int at = (r * static_cast<int>(ld) + c0) * 2;
+          if (accumulate) {
+            const u32x4 x = __builtin_amdgcn_raw_buffer_load_b128(rsrc, at, 0, kStream);
+            lo += floatx4{__uint_as_float(x[0] << 16), __uint_as_float(x[0] & 0xffff0000u), __uint_as_float(x[1] << 16), __uint_as_float(x[1] & 0xffff0000u)};
+            hi += floatx4{__uint_as_float(x[2] << 16), __uint_as_float(x[2] & 0xffff0000u), __uint_as_float(x[3] << 16), __uint_as_float(x[3] & 0xffff0000u)};
+          }
+          __builtin_amdgcn_raw_buffer_store_b128(u32x4{pack_bf16x2(lo[0], lo[1]), pack_bf16x2(lo[2], lo[3]), pack_bf16x2(hi[0], hi[1]), pack_bf16x2(hi[2], hi[3])}, rsrc, at, 0, kWrite);
         }
-        __builtin_nontemporal_store(u32x4{pack_bf16x2(lo[0], lo[1]), pack_bf16x2(lo[2], lo[3]), pack_bf16x2(hi[0], hi[1]), pack_bf16x2(hi[2], hi[3])},
-                                    reinterpret_cast<u32x4*>(at));
       }
+      __builtin_amdgcn_wave_barrier();
     }
-    __builtin_amdgcn_wave_barrier();
-  }
+  };
+  if (whole_lines) pieces(std::true_type());
+  else pieces(std::false_type());
 }
 template <class C>
-__device__ __forceinline__ void store_dw(const floatx4 (&acc)[C::MI][C::NI], int tid, char* turn, float* out, int64_t ld, int64_t rows, int cols, int accumulate, bool past) {
+__device__ __forceinline__ void store_dw(const floatx4 (&acc)[C::MI][C::NI], int tid, char* turn, float* out, int64_t ld, int64_t rows, int cols, int accumulate, bool past, bool) {
   store_acc_f32<C>(acc, tid, turn, out, ld, rows, cols, accumulate, past);
 }
 template <class C>
-__device__ __forceinline__ void store_dw(const floatx4 (&acc)[C::MI][C::NI], int tid, char* turn, uint16_t* out, int64_t ld, int64_t rows, int cols, int accumulate, bool) {
-  store_acc_bf16<C>(acc, tid, turn, out, ld, rows, cols, accumulate);
+__device__ __forceinline__ void store_dw(const floatx4 (&acc)[C::MI][C::NI], int tid, char* turn, uint16_t* out, int64_t ld, int64_t rows, int cols, int accumulate, bool, bool whole_lines) {
+  store_acc_bf16<C>(acc, tid, turn, out, ld, rows, cols, accumulate, whole_lines);
 }
 typedef uint32_t u32x2_a2 __attribute__((ext_vector_type(2), aligned(2)));     // dH has the alignment of its entries
 // What the sliced products leave behind: partial sums in blocks of 256 x 256 floats [slice][row tile][column tile].
@@ -498,7 +509,7 @@ __device__ __forceinline__ void dw_tile(int tile_m, int tile_n, const uint16_t* 
   if (k_len > 0 && d - n0 <= C::BN / 2) mfma_mainloop_mixed<C, true, true, 1, false, true>(KContig{}, ka, KContig{}, kb, k_len, lds, acc, tid, C::BM, d - n0);
   else if (k_len > 0) mfma_mainloop_mixed<C, true, true, 1>(KContig{}, ka, KContig{}, kb, k_len, lds, acc, tid);
   tid = cut_thread<C>(C::BM, d - n0);
-  store_dw<C>(acc, tid, reinterpret_cast<char*>(lds) + (tid >> 6) * kTurnBytes, dW + m0 * d + n0, d, V - m0, d - n0, accumulate, past_caches(d, V));   // d is a multiple of 8
+  store_dw<C>(acc, tid, reinterpret_cast<char*>(lds) + (tid >> 6) * kTurnBytes, dW + m0 * d + n0, d, V - m0, d - n0, accumulate, past_caches(d, V), store_lines(d, rows));   // d is a multiple of 8
 }
 
 // dW of at most 256 rows.  A tile of 256 x 256 that a compute unit works on alone is products, then stores, and the next tile's first loads wait for these
@@ -631,7 +642,7 @@ __device__ __forceinline__ void dw_short(const uint16_t* __restrict__ dZ, int bl
   char* const turn = lds + (nsub + (wave == 3 ? 1 : 0)) % 3 * kShortStage + (wave == 3 ? 0 : wave) * kTurnBytes;
   const int64_t m0 = static_cast<int64_t>(tile_m) * C::BM;
   const int n0 = tile_n * C::BN;
-  store_dw<C>(acc, tile_thread(), turn, dW + m0 * d + n0, d, V - m0, d - n0, accumulate, past_caches(d, V));
+  store_dw<C>(acc, tile_thread(), turn, dW + m0 * d + n0, d, V - m0, d - n0, accumulate, past_caches(d, V), store_lines(d, k_rows));
 }
 // Both products in one launch, in groups of 4 x 8 tiles that are worked on together on one XCD.  Every XCD owns a contiguous
 // range of the dH tiles (slice after slice, so that its workgroups share a slice of both operands) and behind it the share
