@@ -390,6 +390,21 @@ PyObject* ppo_loss(PyObject* const* a) {
   return pack({stats.object(), logp_new.object(), dH.object(), dW.object()});
 }
 
+// (the checks of the two calls below and their kin, see same_head)
+const at::Tensor* targets_or_null(PyObject* o, at::ScalarType type, int64_t n, const char* name) { return o == Py_None ? nullptr : &targets(o, type, n, 1, name); }
+void whole_selection(PyObject* o) {
+  if (o == Py_None) return;
+  const at::Tensor& t = tensor(o);
+  if (t.scalar_type() == at::kInt && t.is_contiguous()) return;
+  PyErr_SetString(PyExc_TypeError, "rowsel must be contiguous and int32");
+  throw Failed();
+}
+void room(const Output& out, at::ScalarType type, int64_t n, const char* name) {
+  if (!out.given || (out.t.scalar_type() == type && out.t.numel() == n && out.t.is_contiguous())) return;
+  PyErr_Format(PyExc_ValueError, "%s must be contiguous, %s and hold %lld values", name, c10::toString(type), static_cast<long long>(n));
+  throw Failed();
+}
+
 PyObject* top_logits(PyObject* const* a) {                // H, W, k, rowsel, ids, logits, lse, workspace, stream
   const Rows H(a[0]);
   const at::Tensor& W = tensor(a[1]);
@@ -405,6 +420,10 @@ PyObject* top_logits(PyObject* const* a) {                // H, W, k, rowsel, id
   sel.point(ws.t.data_ptr(), a[3]);
   void* const st = stream_of(a[8]);
   same_head(H, W);
+  whole_selection(a[3]);
+  room(ids, at::kInt, H.n * places, "ids");
+  room(logits, at::kFloat, H.n * places, "logits");
+  room(lse, at::kFloat, H.n, "lse");
   UMAS_CALL(umas_top_logits(H.t.data_ptr(), W.data_ptr(), dt, H.n, H.d, V, sel.p, sel.n, k, ptr<int32_t>(ids.t), ptr<float>(logits.t), ptr<float>(lse.t),
                             ws.t.data_ptr(), ws.t.numel(), st));
   return pack({ids.object(), logits.object(), lse.object()});
@@ -437,6 +456,16 @@ struct Taught {
         stats(o[9], [&] { return fresh({(1 + static_cast<int64_t>(std::max(n_roles, 0))) * static_cast<int64_t>(sizeof(umas_target_stats))}, at::kByte, dev); }),
         dW_type(UMAS_NO_DW), st(stream_of(o[11])) {
     same_head(H, W);
+    whole_selection(rowsel);
+    targets_or_null(o[0], at::kFloat, H.n, "weight");
+    targets_or_null(o[1], at::kInt, H.n, "tok_role");
+    room(dH, H.t.scalar_type(), H.t.numel(), "dH");
+    room(row_out, at::kFloat, H.n, "the output of every row");
+    room(stats, at::kByte, (1 + static_cast<int64_t>(std::max(n_roles, 0))) * static_cast<int64_t>(sizeof(umas_target_stats)), "stats");
+    if (head && accumulate && !dW_given) {
+      PyErr_SetString(PyExc_ValueError, "accumulate_dW needs the dW to add to");
+      throw Failed();
+    }
     if (!head) return;
     dW = dW_given ? tensor(dW_given) : at::empty_like(W);
     if (dW.scalar_type() != at::kFloat && dW.scalar_type() != W.scalar_type()) {

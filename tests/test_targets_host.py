@@ -2,8 +2,10 @@
 import os
 
 import pytest
+import torch
 
 import paper_2605_26646_amd as umas
+from paper_2605_26646_amd import binding
 
 F32, BF16, NO_DW = 0, 1, -1
 
@@ -93,3 +95,66 @@ def test_arguments_of_the_taught_head(lib, call, kw, code, needle):
 def test_arguments_of_their_own(lib, call, kw, code, needle):
     status, message = call(lib, **kw)
     assert status == code and needle in message, message
+
+
+# ------------------------------------------------------------------------------------------------ the binding's own checks, on host tensors
+def tensors(**kw):
+    n, d, V, k = 6, 16, 40, 3
+    a = dict(H=torch.zeros(n, d, dtype=torch.bfloat16), W=torch.zeros(V, d, dtype=torch.bfloat16), ids=torch.zeros(n, dtype=torch.int32),
+             top_ids=torch.zeros(n, k, dtype=torch.int32), top_logits=torch.zeros(n, k), lse=None, rowsel=None, z_coef=0.0, weight=None, tok_role=None, n_roles=0,
+             train_head=True, accumulate_dW=False, norm_rows=0, dW=None, dH=None, row=None, stats=None, workspace=torch.empty(0, dtype=torch.uint8))
+    return {**a, **kw}
+
+
+def native_ce(a):
+    return binding._native().cross_entropy(a["H"], a["W"], a["ids"], a["rowsel"], a["z_coef"], a["weight"], a["tok_role"], a["n_roles"], a["train_head"], a["accumulate_dW"],
+                                           a["norm_rows"], a["dW"], a["dH"], a["row"], a["stats"], a["workspace"], 0)
+
+
+def native_distill(a):
+    return binding._native().distill(a["H"], a["W"], a["top_ids"], a["top_logits"], a["lse"], a["rowsel"], a["weight"], a["tok_role"], a["n_roles"], a["train_head"],
+                                     a["accumulate_dW"], a["norm_rows"], a["dW"], a["dH"], a["row"], a["stats"], a["workspace"], 0)
+
+
+F, I, B = torch.float32, torch.int32, torch.bfloat16
+WRONG = [(dict(W=torch.zeros(40, 24, dtype=B)), ValueError), (dict(W=torch.zeros(40, 16)), ValueError), (dict(W=torch.zeros(16, 40, dtype=B).T), ValueError),
+         (dict(H=torch.zeros(6, 32, dtype=B)[:, ::2]), ValueError), (dict(rowsel=torch.zeros(3, dtype=torch.int64)), TypeError), (dict(rowsel=torch.zeros(6, dtype=I)[::2]), TypeError),
+         (dict(weight=torch.zeros(5)), ValueError), (dict(weight=torch.zeros(6, dtype=torch.float64)), TypeError), (dict(tok_role=torch.zeros(7, dtype=I), n_roles=2), ValueError),
+         (dict(tok_role=torch.zeros(6), n_roles=2), TypeError), (dict(dH=torch.zeros(6, 16)), ValueError), (dict(dH=torch.zeros(5, 16, dtype=B)), ValueError),
+         (dict(row=torch.zeros(5)), ValueError), (dict(row=torch.zeros(6, dtype=B)), ValueError), (dict(stats=torch.zeros(31, dtype=torch.uint8)), ValueError),
+         (dict(stats=torch.zeros(32, dtype=torch.uint8), n_roles=1, tok_role=torch.zeros(6, dtype=I)), ValueError), (dict(accumulate_dW=True), ValueError),
+         (dict(dW=torch.zeros(40, 16, dtype=torch.float64)), TypeError), (dict(dW=torch.zeros(39, 16)), ValueError), (dict(dW=torch.zeros(16, 40).T), ValueError)]
+
+
+@pytest.mark.parametrize("call", [native_ce, native_distill])
+@pytest.mark.parametrize("kw,kind", WRONG)
+def test_tensors_that_do_not_fit(lib, call, kw, kind):
+    with pytest.raises(kind):
+        call(tensors(**kw))
+
+
+@pytest.mark.parametrize("call,kw,kind", [(native_ce, dict(ids=torch.zeros(6, dtype=torch.int64)), TypeError), (native_ce, dict(ids=torch.zeros(5, dtype=I)), ValueError),
+                                          (native_distill, dict(top_ids=torch.zeros(6, 3, dtype=torch.int64)), TypeError), (native_distill, dict(top_logits=torch.zeros(6, 2)), ValueError),
+                                          (native_distill, dict(top_logits=torch.zeros(3, 6).T), ValueError), (native_distill, dict(lse=torch.zeros(5)), ValueError)])
+def test_targets_that_do_not_fit(lib, call, kw, kind):
+    with pytest.raises(kind):
+        call(tensors(**kw))
+
+
+@pytest.mark.parametrize("call", [native_ce, native_distill])
+def test_what_fits_gets_as_far_as_the_workspace(lib, call):
+    for kw in (dict(), dict(train_head=False), dict(dW=torch.zeros(40, 16)), dict(dW=torch.zeros(40, 16, dtype=B), accumulate_dW=True),
+               dict(weight=torch.zeros(6), tok_role=torch.zeros(6, dtype=I), n_roles=2, rowsel=torch.zeros(4, dtype=I), dH=torch.zeros(6, 16, dtype=B), row=torch.zeros(6),
+                    stats=torch.zeros(96, dtype=torch.uint8))):
+        assert call(tensors(**kw)) == -4 and "workspace" in lib.umas_last_error().decode()
+
+
+@pytest.mark.parametrize("kw,kind", [(dict(W=torch.zeros(40, 24, dtype=B)), ValueError), (dict(rowsel=torch.zeros(3, dtype=torch.int64)), TypeError),
+                                     (dict(ids=torch.zeros(6, 3, dtype=torch.int64)), ValueError), (dict(ids=torch.zeros(6, 2, dtype=I)), ValueError),
+                                     (dict(logits=torch.zeros(6, 4)), ValueError), (dict(lse=torch.zeros(5)), ValueError)])
+def test_outputs_of_the_largest_logits_that_do_not_fit(lib, kw, kind):
+    a = {**dict(H=torch.zeros(6, 16, dtype=B), W=torch.zeros(40, 16, dtype=B), rowsel=None, ids=None, logits=None, lse=None, ws=torch.empty(0, dtype=torch.uint8)), **kw}
+    call = lambda a: binding._native().top_logits(a["H"], a["W"], 3, a["rowsel"], a["ids"], a["logits"], a["lse"], a["ws"], 0)
+    with pytest.raises(kind):
+        call(a)
+    assert call({**a, **dict(W=torch.zeros(40, 16, dtype=B), rowsel=None, ids=None, logits=None, lse=None)}) == -4
