@@ -135,3 +135,26 @@ def test_largest_logits_of_hidden_states_of_almost_4_gib():
     best = key.topk(k, dim=1).values
     assert torch.equal(ids[rows].long(), 2 ** 20 - 1 - (best & (2 ** 20 - 1)))
     assert (ids[:n - 40] == -1).all() and not top[:n - 40].any() and not lse[:n - 40].any()
+
+
+@pytest.mark.parametrize("n,d,V,k,dW_type", [(203, 2056, 140001, 4, torch.bfloat16), (150, 4096, 70003, 1, torch.bfloat16), (250, 2056, 140001, 1, torch.float32), (100, 3584, 100001, 4, torch.bfloat16)])
+@pytest.mark.parametrize("add", [False, True])
+def test_a_large_dW_of_one_block_of_rows(n, d, V, k, dW_type, add):
+    """dW in a launch of its own: rows of whole lines and others, written and added to."""
+    g = torch.Generator(device="cuda").manual_seed(21)
+    H, W = grid(n, d, seed=22, scale=1 / 8), grid(V, d, seed=23, scale=1 / 64)
+    ids = torch.randint(0, V, (n, k), device="cuda", generator=g)
+    l = torch.randn(n, k, device="cuda", generator=g)
+    tokens = torch.cat([torch.tensor([0, 1, V // 2, V - 2, V - 1], device="cuda"), ids[:40].reshape(-1)]).unique()
+    dW = torch.full((V, d), float("nan"), dtype=dW_type, device="cuda")
+    before = 0.0
+    if add:
+        for a in range(0, V, 1 << 16):
+            dW[a:a + (1 << 16)] = torch.randn(min(1 << 16, V - a), d, device="cuda", generator=g).mul_(0.01).to(dW_type)
+        before = dW[tokens].double()
+    _, kl, dH, got = umas.umas_distill_fwd_bwd(H, W, ids.int(), l, dW=dW, accumulate_dW=add)
+    masses = torch.softmax(l.double(), 1)
+    lse, zt, dH_o, dW_o = taught64(H, W, ids, masses, n, tokens)
+    assert got is dW and bool(torch.isfinite(got).all())
+    close(dH, dH_o, 1e-2, "dH")
+    close(got[tokens], dW_o + before, 1e-2, "dW")
