@@ -324,9 +324,11 @@ __device__ __forceinline__ void score_tile(const uint16_t* __restrict__ W, const
 // 130.1 -> 119.9, 217.8 -> 208.5 and 389.7 -> 382.4, of 2048 against 151 936 294.2 -> 276.9, 553.2 -> 547.4 and 1014 -> 1023, 900 of 3584 918 -> 900; where
 // the last round is fuller nothing changes.
 using HalfCfg = TileCfg<256, 128, 2, 4>;                 // the lanes of a row as in a whole tile: the same bits
+using HalfNarrowCfg = TileCfg<128, 64, 2, 2>;            // of a NarrowCfg
 // So is a tile whose rows end in its first half: 300 rows of 2048 against 151 936 265 -> 250 us, 600 371 -> 357, 4200 of 3584 3454 -> 3376, 262 of 1664 against 63 167 88 -> 81.
 enum class HalfTile { kNone, kWhole, kHalf };
 // The tile of a workgroup, `it` of its kTilesPerWg, of the `mc` rows; a half's number counts halves.
+template <class Half>
 __device__ __forceinline__ HalfTile half_tile(int tiles_m, int tiles_n, int panel, int halved, int it, int64_t mc, int* tile_m, int* tile_n) {
   if (halved > 0) {                               // the last `halved` tiles of every XCD
     const int per_xcd = (tiles_m * tiles_n + 7) / 8, xcd = static_cast<int>(blockIdx.x & 7), w = static_cast<int>(blockIdx.x >> 3), whole = per_xcd - halved;
@@ -334,11 +336,11 @@ __device__ __forceinline__ HalfTile half_tile(int tiles_m, int tiles_n, int pane
       const int in_xcd = whole + (w - whole) / 2, t = xcd * per_xcd + in_xcd;
       *tile_m = t / tiles_n;
       *tile_n = t % tiles_n * 2 + ((w - whole) & 1);
-      return it == 0 && in_xcd < per_xcd && *tile_m < tiles_m && *tile_n * HalfCfg::BN < mc ? HalfTile::kHalf : HalfTile::kNone;
+      return it == 0 && in_xcd < per_xcd && *tile_m < tiles_m && *tile_n * Half::BN < mc ? HalfTile::kHalf : HalfTile::kNone;
     }
   }
   if (!tile_coords<kGM, kGN>(tiles_m, tiles_n, panel, tile_m, tile_n, it, kTilesPerWg)) return HalfTile::kNone;
-  if (*tile_n == 0 || mc - static_cast<int64_t>(*tile_n) * Cfg::BN > HalfCfg::BN) return HalfTile::kWhole;   // (a single row tile reads W once: whole)
+  if (*tile_n == 0 || mc - static_cast<int64_t>(*tile_n) * (2 * Half::BN) > Half::BN) return HalfTile::kWhole;   // (a single row tile reads W once: whole)
   *tile_n *= 2;
   return HalfTile::kHalf;
 }
@@ -351,11 +353,12 @@ __device__ __forceinline__ void score_tiles(const uint16_t* __restrict__ W, cons
                                             uint16_t* lds, int halved = 0) {
   const bool w_once = tiles_n == 1 && beyond_cache(d, V, kLogitsOnceBytes);
   if constexpr (ENDS) {
+    using Half = std::conditional_t<C::BN == HalfCfg::BN * 2, HalfCfg, HalfNarrowCfg>;
     for (int it = 0; it < kTilesPerWg; ++it) {
       int tile_m, tile_n;
-      const HalfTile h = half_tile(tiles_m, tiles_n, panel, halved, it, mc, &tile_m, &tile_n);
+      const HalfTile h = half_tile<Half>(tiles_m, tiles_n, panel, halved, it, mc, &tile_m, &tile_n);
       if (h == HalfTile::kNone) continue;
-      if (h == HalfTile::kHalf) score_tile<LEAVE, HalfCfg>(W, H, d, V, rowsel, c0, mc, ids, tile_m, tile_n, false, partial, n_pad, keep, lds);
+      if (h == HalfTile::kHalf) score_tile<LEAVE, Half>(W, H, d, V, rowsel, c0, mc, ids, tile_m, tile_n, false, partial, n_pad, keep, lds);
       else score_tile<LEAVE, C>(W, H, d, V, rowsel, c0, mc, ids, tile_m, tile_n, w_once, partial, n_pad, keep, lds);
     }
     return;
@@ -511,10 +514,10 @@ inline int row_panel(int tiles_n, int d) {
 }
 
 // Tiles of every XCD that are cut in two (see score_tiles): those of the last round of compute units where it is at most half full.
-inline int halved_tiles(int tiles_m, int tiles_n) {
+inline int halved_tiles(int tiles_m, int tiles_n, int per_cu = 1) {   // per_cu: workgroups to a compute unit
   if (tiles_n > kGN) return 0;
-  const int per_xcd = static_cast<int>(cdiv(static_cast<size_t>(tiles_m) * tiles_n, 8)), cus = std::max(device_cus() / 8, 1), rest = per_xcd % cus;
-  return rest * 2 <= cus ? rest : 0;
+  const int per_xcd = static_cast<int>(cdiv(static_cast<size_t>(tiles_m) * tiles_n, 8)), round = std::max(device_cus() / 8, 1) * per_cu, rest = per_xcd % round;
+  return rest * 2 <= round ? rest : 0;
 }
 inline dim3 score_grid(int tiles_m, int tiles_n, int panel, int halved) {
   return dim3(tile_grid<kGM, kGN>(tiles_m, tiles_n, panel, kTilesPerWg) + 8 * static_cast<unsigned>(halved));

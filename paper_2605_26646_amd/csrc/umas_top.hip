@@ -228,14 +228,11 @@ __device__ __forceinline__ void top_tiles(const uint16_t* __restrict__ W, const 
     int tile_m, tile_n;
     // halves as in score_tiles: of the last round 129 rows of 3584 291 -> 265 us, 1000 of 2048 554 -> 543, 777 of 1544 222 -> 215, else +- 1 %; at the end of the
     // rows 300 of 2048 319 -> 290, 600 of 3584 681 -> 645, 2100 of 2048 1188 -> 1120
-    if constexpr (C::BM == 256 && C::BN == 256) {
-      const HalfTile h = half_tile(tiles_m, tiles_n, panel, halved, it, mc, &tile_m, &tile_n);
-      if (h == HalfTile::kNone) continue;
-      if (h == HalfTile::kHalf) top_tile<HalfCfg, ALL>(W, H, d, V, rowsel, c0, mc, first + tile_m, tile_n, false, out, bound, lds);
-      else top_tile<C, ALL>(W, H, d, V, rowsel, c0, mc, first + tile_m, tile_n, w_once, out, bound, lds);
-    } else {
-      if (tile_coords<kGM, kGN>(tiles_m, tiles_n, panel, &tile_m, &tile_n, it, kTilesPerWg)) top_tile<C, ALL>(W, H, d, V, rowsel, c0, mc, first + tile_m, tile_n, w_once, out, bound, lds);
-    }
+    using Half = std::conditional_t<C::BN == HalfCfg::BN * 2, HalfCfg, HalfNarrowCfg>;
+    const HalfTile h = half_tile<Half>(tiles_m, tiles_n, panel, halved, it, mc, &tile_m, &tile_n);
+    if (h == HalfTile::kNone) continue;
+    if (h == HalfTile::kHalf) top_tile<Half, ALL>(W, H, d, V, rowsel, c0, mc, first + tile_m, tile_n, false, out, bound, lds);
+    else top_tile<C, ALL>(W, H, d, V, rowsel, c0, mc, first + tile_m, tile_n, w_once, out, bound, lds);
   }
 }
 __global__ void __launch_bounds__(Cfg::T)
@@ -251,9 +248,9 @@ k_top_tiles_bound(const uint16_t* __restrict__ W, const uint16_t* __restrict__ H
   top_tiles<Cfg, false>(W, H, d, V, rowsel, c0, mc, first, tiles_m, tiles_n, panel, out, bound, lds, halved);
 }
 __global__ void __launch_bounds__(NarrowCfg::T)
-k_top_narrow(const uint16_t* __restrict__ W, const uint16_t* __restrict__ H, int d, int V, const int32_t* __restrict__ rowsel, int64_t c0, int64_t mc, Groups out) {
+k_top_narrow(const uint16_t* __restrict__ W, const uint16_t* __restrict__ H, int d, int V, const int32_t* __restrict__ rowsel, int64_t c0, int64_t mc, int halved, Groups out) {
   __shared__ __attribute__((aligned(16))) uint16_t lds[kNarrowLds / 2];
-  top_tiles<NarrowCfg, true>(W, H, d, V, rowsel, c0, mc, 0, out.tiles, 1, kGN, out, nullptr, lds);
+  top_tiles<NarrowCfg, true>(W, H, d, V, rowsel, c0, mc, 0, out.tiles, 1, kGN, out, nullptr, lds, halved);
 }
 
 // A few rows (umas_few.h): a thread's place of every block of 16 entries of its workgroup's part of the vocabulary is a group.
@@ -562,7 +559,9 @@ extern "C" umas_status umas_top_logits(const void* H, const void* W, umas_dtype 
         hipLaunchKernelGGL(k_top_row<FewGroups>, grid, dim3(kSelectT), 0, st, A, FewGroups{per}, V, O);
       } else if (rows <= NarrowCfg::BN) {
         A.tiles = static_cast<int>(cdiv(V, NarrowCfg::BM));
-        hipLaunchKernelGGL(k_top_narrow, dim3(tile_grid<kGM, kGN>(A.tiles, 1, kGN, kTilesPerWg)), dim3(NarrowCfg::T), 0, st, Wb, Hb, d, V, rowsel, c0, rows, A);
+        // (100 rows of 1024 against 32 000 23 -> 19 us, 70 of 3584 against 152 064 229 -> 223, 128 of 2048 169 -> 163, 121 of 3584 equal)
+        const int halved = rows > HalfNarrowCfg::BN ? halved_tiles(A.tiles, 1, 2) : 0;
+        hipLaunchKernelGGL(k_top_narrow, score_grid(A.tiles, 1, kGN, halved), dim3(NarrowCfg::T), 0, st, Wb, Hb, d, V, rowsel, c0, rows, halved, A);
         UMAS_LAUNCHED("k_top_narrow");
         hipLaunchKernelGGL(k_top_row<TileGroups<NarrowCfg>>, grid, dim3(kSelectT), 0, st, A, TileGroups<NarrowCfg>{}, V, O);
       } else {
