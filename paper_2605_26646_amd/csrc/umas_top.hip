@@ -348,10 +348,12 @@ k_top_bound(Groups A, int tiles, int k, float* __restrict__ bound) {   // of a r
 }
 // A workgroup to a row: the groups that reach its bound are listed, and the wavefronts go through their entries.  The row's logsumexp comes from the tiles'
 // sums on the way.  12 us for one row, a chain of reads and exchanges (through LDS 13); 8192 rows with 64 places 114 us.
+// `written`: the bound below which k_top_tiles_bound left a group's logits unwritten (NULL: all are there).  The row's own can lie below it, as of few tiles it is one of groups
+// and of many one of tiles, of which the large logits may share one; k logits reach either, so the larger of the two serves and only what was written is read.
 constexpr int kAtOnce = 4;                                   // loads of entries under way
 template <class Map>
 __global__ void __launch_bounds__(kSelectT)
-k_top_row(Groups A, Map map, int V, TopOut O) {
+k_top_row(Groups A, Map map, int V, const float* __restrict__ written, TopOut O) {
   __shared__ TopKey s_buf[kSelectWaves][2 * kWave];
   __shared__ TopKey s_list[kSelectWaves][kWave];
   __shared__ float s_top[kSelectWaves][kWave], s_m[kSelectWaves], s_s[kSelectWaves];
@@ -362,7 +364,8 @@ k_top_row(Groups A, Map map, int V, TopOut O) {
   const float* const maxima = A.max + m * A.tiles * Map::G;
   if (threadIdx.x == 0) s_n = 0;
   float lm, ls;
-  const float bound = row_bound<Map::G>(maxima, A.sum + m * A.tiles, A.tiles, O.k, s_top, lm, ls);
+  float bound = row_bound<Map::G>(maxima, A.sum + m * A.tiles, A.tiles, O.k, s_top, lm, ls);
+  if (written) bound = fmaxf(bound, written[m]);
   {
     const float M = wave_max(lm), sum = wave_sum(ls * __expf(lm - M));
     if (lane == 0) { s_m[wave] = M; s_s[wave] = sum; }
@@ -556,14 +559,14 @@ extern "C" umas_status umas_top_logits(const void* H, const void* W, umas_dtype 
           hipLaunchKernelGGL((k_top_few<decltype(ni)::value, decltype(ppw)::value>), dim3(A.tiles), dim3(kFewT), 0, st, Wb, Hb, d, V, rowsel, static_cast<int>(rows), per, A);
         });
         UMAS_LAUNCHED("k_top_few");
-        hipLaunchKernelGGL(k_top_row<FewGroups>, grid, dim3(kSelectT), 0, st, A, FewGroups{per}, V, O);
+        hipLaunchKernelGGL(k_top_row<FewGroups>, grid, dim3(kSelectT), 0, st, A, FewGroups{per}, V, nullptr, O);
       } else if (rows <= NarrowCfg::BN) {
         A.tiles = static_cast<int>(cdiv(V, NarrowCfg::BM));
         // (100 rows of 1024 against 32 000 23 -> 19 us, 70 of 3584 against 152 064 229 -> 223, 128 of 2048 169 -> 163, 121 of 3584 equal)
         const int halved = rows > HalfNarrowCfg::BN ? halved_tiles(A.tiles, 1, 2) : 0;
         hipLaunchKernelGGL(k_top_narrow, score_grid(A.tiles, 1, kGN, halved), dim3(NarrowCfg::T), 0, st, Wb, Hb, d, V, rowsel, c0, rows, halved, A);
         UMAS_LAUNCHED("k_top_narrow");
-        hipLaunchKernelGGL(k_top_row<TileGroups<NarrowCfg>>, grid, dim3(kSelectT), 0, st, A, TileGroups<NarrowCfg>{}, V, O);
+        hipLaunchKernelGGL(k_top_row<TileGroups<NarrowCfg>>, grid, dim3(kSelectT), 0, st, A, TileGroups<NarrowCfg>{}, V, nullptr, O);
       } else {
         A.tiles = static_cast<int>(cdiv(V, Cfg::BM));
         const int tiles_n = static_cast<int>(cdiv(rows, Cfg::BN)), panel = row_panel(tiles_n, d);
@@ -579,7 +582,7 @@ extern "C" umas_status umas_top_logits(const void* H, const void* W, umas_dtype 
                              halved, A, w.bound);
           UMAS_LAUNCHED("k_top_tiles_bound");
         }
-        hipLaunchKernelGGL(k_top_row<TileGroups<Cfg>>, grid, dim3(kSelectT), 0, st, A, TileGroups<Cfg>{}, V, O);
+        hipLaunchKernelGGL(k_top_row<TileGroups<Cfg>>, grid, dim3(kSelectT), 0, st, A, TileGroups<Cfg>{}, V, first < A.tiles ? w.bound : nullptr, O);
       }
       UMAS_LAUNCHED("k_top_row");
     } else {

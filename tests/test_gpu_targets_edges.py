@@ -1,0 +1,41 @@
+"""Largest logits, cross entropy and distillation on inputs that show what a kernel assumes: large logits gathered in few tokens.  Inputs and tolerances as in
+test_gpu_targets."""
+import pytest
+import torch
+
+import paper_2605_26646_amd as umas
+
+pytestmark = pytest.mark.gpu
+
+
+# ------------------------------------------------------------------------------------------------ largest logits
+def largest64(H, W, k):
+    """Tokens and logits in float64, ties to the lowest token; logits are multiples of 1/256."""
+    ids, top, V = [], [], len(W)
+    for h in H.split(500):
+        z = h.double() @ W.double().T
+        key = (z * 256).round().long() * 2 ** 20 + torch.arange(V - 1, -1, -1, device="cuda")
+        ids.append(V - 1 - (key.topk(k, dim=1).values & (2 ** 20 - 1)))
+        top.append(z.gather(1, ids[-1]))
+    return torch.cat(ids), torch.cat(top)
+
+
+@pytest.mark.parametrize("kind", ["raised", "falling"])
+@pytest.mark.parametrize("n,V,k", [(1300, 151936, 8), (2100, 32001, 2), (2100, 32001, 20), (2100, 50001, 20), (4200, 32001, 8), (4200, 50001, 20), (4200, 50001, 2)])
+def test_large_logits_that_share_a_few_tiles(n, V, k, kind):
+    """Frequent tokens first, as in a trained head: the k largest lie in one tile or two, and single tokens behind them come close.  Whatever is not written
+    on the way holds a large number here, which must not be taken for a logit."""
+    g = torch.Generator(device="cuda").manual_seed(n + V + k)
+    d = 64
+    H = torch.randint(-4, 5, (n, d), device="cuda", generator=g, dtype=torch.float32).div_(4)
+    W = torch.randint(-8, 9, (V, d), device="cuda", generator=g, dtype=torch.float32).div_(64)
+    v = torch.arange(V, device="cuda")
+    H[:, 0] = 1
+    W[:, 0] = (v < 256) * 8.0 if kind == "raised" else torch.round(-(1.0 + v).log() * 16).div_(16)
+    H, W = H.bfloat16(), W.bfloat16()
+    want, top = largest64(H, W, k)
+    lib = umas.load_library()
+    for which in ("", "_min"):
+        bytes_ = getattr(lib, "umas_top_logits_workspace_bytes" + which)(n, d, V, k, 1)
+        got = umas.umas_top_logits(H, W, k, workspace=torch.full((bytes_,), 0x7F, dtype=torch.uint8, device="cuda"))
+        assert torch.equal(got[0].long(), want) and torch.equal(got[1].double(), top)
