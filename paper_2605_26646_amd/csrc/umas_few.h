@@ -1,6 +1,8 @@
 // Logits of a few rows (up to 32, 64 at d <= 2048) that are to be read again: the product is bound by reading W once.
 #pragma once
 
+#include <float.h>
+
 #include <type_traits>
 
 #include "umas_logits.h"
@@ -12,11 +14,14 @@ namespace {
 // workgroup's part of the vocabulary, `per` blocks.  The logits are summed over the wavefronts in a fixed order; they collect in LDS, 64 KB of them, and leave
 // together: memory operations are counted in order, and a store in every step has the loads of W behind it wait for it (one row of 2048 129 us in place
 // of 110, 24 rows of 3584 247 in place of 199).
-// Logit v of row n goes to Z[n * stride + v], up to the end of the workgroups' parts (kMasked from V on).  emit(n, place, m, most, s, t): the thread's maximum, and
+// Logit v of row n goes to Z[n * stride + v], up to the end of the workgroups' parts.  From V on lies what no logit is: -infinity, and a thread that has none emits the lowest
+// number, or with ENTROPY, where products with it have to stay finite, kMasked for both.
+// emit(n, place, m, most, s, t): the thread's maximum, and
 // for its row's part of the vocabulary the maximum, sum exp(z - most) and, with ENTROPY, sum exp(z - most) z.
 template <int NI, int PPW, bool ENTROPY, class Emit>
 __device__ __forceinline__ void few_logits(const uint16_t* __restrict__ W, const uint16_t* __restrict__ H, int d, int V, const int32_t* __restrict__ rowsel, int n_sel, int per,
                                            float* __restrict__ Z, int64_t stride, Emit emit) {
+  constexpr float kNone = ENTROPY ? kMasked : -INFINITY, kFirst = ENTROPY ? kMasked : -FLT_MAX;
   constexpr int MB = PPW <= 4 && NI <= 2 ? 2 : 1;            // blocks of 16 vocabulary entries per step
   constexpr int NL = (NI + 1) / 2;                           // logits per thread and block
   constexpr int kHold = 64 / NI, kHoldPitch = kHold * 16 + 16;   // blocks that collect, floats of a row of them (16 more: banks)
@@ -56,7 +61,7 @@ __device__ __forceinline__ void few_logits(const uint16_t* __restrict__ W, const
   float m[NL], s[NL], t[NL];
 #pragma unroll
   for (int l = 0; l < NL; ++l) {
-    m[l] = kMasked;
+    m[l] = kFirst;
     s[l] = t[l] = 0.f;
   }
   int first = b0;                                            // of the blocks that collect
@@ -102,7 +107,7 @@ __device__ __forceinline__ void few_logits(const uint16_t* __restrict__ W, const
           float z = 0.f;
 #pragma unroll
           for (int k = 0; k < kFewWaves; ++k) z += s_z[buf][k][i][2 * l + (tid >> 8)][my_n][my_v];
-          if ((b + i) * 16 + my_v >= V || b + i >= b1) z = kMasked;
+          if ((b + i) * 16 + my_v >= V || b + i >= b1) z = kNone;
           s_out[((2 * l + (tid >> 8)) * 16 + my_n) * kHoldPitch + (b + i - first) * 16 + my_v] = z;
           const float gap = z - m[l], e = __expf(-fabsf(gap));  // one exponential: of the smaller relative to the larger
           s[l] = gap > 0.f ? fmaf(s[l], e, 1.f) : s[l] + e;

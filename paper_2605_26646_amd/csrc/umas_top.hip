@@ -11,11 +11,17 @@
 //
 // What bounds it: up to 128 rows reading W (one row of 2048 against 151 936 107 us, 5.8 TB/s; 24 rows of 3584 against 152 064 209 us, 5.2 TB/s; 128 rows of 2048 166 us), then
 // the product (8192 rows of 2048 with 64 places 3.82 ms, 1.33 PFLOP/s, of 3.97; 777 rows of 1544 against 50 001 185 us, whole rounds of tiles of 52 to 58 us, of 205).
+#include <float.h>
+
 #include "umas_f32.h"
 #include "umas_few.h"
 
 namespace umas {
 namespace {
+
+// A logit may be any number, down to a type's lowest where a token is masked by it: entries that do not exist are -infinity here, whose exponential is 0, and
+// references of sums start at the lowest number, so that no difference is of infinities.
+constexpr float kLowest = -FLT_MAX;
 
 typedef unsigned long long TopKey;                            // 0: nothing
 __device__ __forceinline__ TopKey key_of(float z, int id) {   // z is a number above -infinity
@@ -126,7 +132,7 @@ __device__ __forceinline__ TopKey merge_waves(TopKey list, TopKey (*s_list)[kWav
 
 // ------------------------------------------------------------------ bf16: logits in groups
 // What a product leaves of its rows: per row and tile (of the vocabulary) G group maxima and a sum of exponentials relative to the largest of them, and the
-// logits.  Entries that do not exist hold kMasked.
+// logits.  Entries that do not exist hold -infinity; a group of few rows without a number has kLowest for a maximum.
 struct Groups {
   float* max;              // [rows][tiles][G]
   float* sum;              // [rows][tiles]
@@ -160,7 +166,7 @@ __device__ __forceinline__ void top_tile(const uint16_t* __restrict__ W, const u
       for (int j = 0; j < C::NI; ++j)
 #pragma unroll
         for (int r = 0; r < 4; ++r)
-          if (vbase + i * 16 + r >= V) acc[i][j][r] = kMasked;
+          if (vbase + i * 16 + r >= V) acc[i][j][r] = -INFINITY;
   }
   constexpr float kLog2e = 1.44269504088896341f;
   const int group = wm * 4 + (lane >> 4);
@@ -172,7 +178,7 @@ __device__ __forceinline__ void top_tile(const uint16_t* __restrict__ W, const u
     for (int i = 0; i < C::MI; ++i)
 #pragma unroll
       for (int r = 0; r < 4; ++r) m = fmaxf(m, acc[i][j][r]);
-    float most = fmaxf(m, kMasked);                          // of the column's four lanes
+    float most = fmaxf(m, kLowest);                          // of the column's four lanes
     most = fmaxf(most, __shfl_xor(most, 16, kWave));
     most = fmaxf(most, __shfl_xor(most, 32, kWave));
     float s = 0.f;
@@ -210,7 +216,7 @@ __device__ __forceinline__ void top_tile(const uint16_t* __restrict__ W, const u
   if (threadIdx.x < C::BN && n0 + threadIdx.x < mc) {
     const int col = threadIdx.x;
     const floatx4 a = reinterpret_cast<const floatx4*>(s_max)[col * 2], b = reinterpret_cast<const floatx4*>(s_max)[col * 2 + 1];
-    const float ma = fmaxf(fmaxf(fmaxf(a[0], a[1]), fmaxf(a[2], a[3])), kMasked), mb = fmaxf(fmaxf(fmaxf(b[0], b[1]), fmaxf(b[2], b[3])), kMasked);
+    const float ma = fmaxf(fmaxf(fmaxf(a[0], a[1]), fmaxf(a[2], a[3])), kLowest), mb = fmaxf(fmaxf(fmaxf(b[0], b[1]), fmaxf(b[2], b[3])), kLowest);
     const float m = fmaxf(ma, mb);
     const int64_t at = (n0 + col) * out.tiles + tile_m;
     reinterpret_cast<floatx4*>(out.max)[at * 2] = a;
@@ -308,7 +314,7 @@ template <int G>
 __device__ __forceinline__ float row_bound(const float* __restrict__ maxima, const float* __restrict__ sums, int tiles, int k, float (*s_top)[kWave], float& lm, float& ls) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   float x = -INFINITY;
-  lm = kMasked;
+  lm = kLowest;
   ls = 0.f;
   for (int t = threadIdx.x; t < tiles; t += kSelectT) {
     float g_max[G];
@@ -318,7 +324,7 @@ __device__ __forceinline__ float row_bound(const float* __restrict__ maxima, con
     for (int g = 1; g < G; ++g) tm = fmaxf(tm, g_max[g]);
     x = fmaxf(x, tm);
     if (sums) {
-      tm = fmaxf(tm, kMasked);
+      tm = fmaxf(tm, kLowest);
       const float s = sums[t], M = fmaxf(lm, tm);
       ls = ls * __expf(lm - M) + s * __expf(tm - M);
       lm = M;

@@ -1,9 +1,11 @@
-"""Largest logits, cross entropy and distillation on inputs that show what a kernel assumes: large logits gathered in few tokens.  Inputs and tolerances as in
-test_gpu_targets."""
+"""Largest logits, cross entropy and distillation on inputs that show what a kernel assumes: large logits gathered in few tokens, masks of a type's lowest value.  Inputs and
+tolerances as in test_gpu_targets."""
+import numpy as np
 import pytest
 import torch
 
 import paper_2605_26646_amd as umas
+from tests.test_gpu_targets import DT, arrays, cuda
 
 pytestmark = pytest.mark.gpu
 
@@ -39,3 +41,42 @@ def test_large_logits_that_share_a_few_tiles(n, V, k, kind):
         bytes_ = getattr(lib, "umas_top_logits_workspace_bytes" + which)(n, d, V, k, 1)
         got = umas.umas_top_logits(H, W, k, workspace=torch.full((bytes_,), 0x7F, dtype=torch.uint8, device="cuda"))
         assert torch.equal(got[0].long(), want) and torch.equal(got[1].double(), top)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("n,d", [(3, 64), (40, 64), (100, 64), (300, 64)])
+@pytest.mark.parametrize("V,k", [(700, 20), (1025, 12), (1025, 64), (3001, 64)])
+def test_tokens_masked_by_the_lowest_number(n, d, V, k, dtype):
+    """A mask of the type's lowest value in a column of its own: these logits are numbers, which come behind all others, in rising order of tokens.  In one row nothing
+    but masked tokens is left."""
+    H, W, Hd, Wd, rng = arrays(n + V + k, n, d, V, dtype, grid=True)
+    lowest = torch.finfo(torch.bfloat16).min
+    open_ = np.sort(rng.permutation(V)[:10])
+    masked = np.ones(V, bool)
+    masked[open_] = False
+    W[masked] = 0
+    W[:, :2] = 0
+    W[masked, 0], W[:, 1] = lowest, lowest
+    H[:, 0], H[:, 1] = 1, 0
+    empty = n // 2
+    H[empty] = 0
+    H[empty, 1] = 1
+    ids, top, lse = (x.cpu().numpy() for x in umas.umas_top_logits(cuda(H, np.float32).to(DT[dtype]), cuda(W, np.float32).to(DT[dtype]), k))
+    z = H @ W.T
+    for i in range(n):
+        want = np.lexsort((np.arange(V), -z[i]))[:k]
+        assert (ids[i] == want).all() and (top[i] == z[i][want].astype(np.float32)).all()
+        m = z[i].max()
+        want_lse = m + np.log(np.exp(z[i] - m).sum())
+        assert abs(lse[i] - want_lse) <= 1e-5 * (1 + abs(want_lse))
+
+
+@pytest.mark.parametrize("n", [3, 40, 100, 300])
+@pytest.mark.parametrize("V", [256, 300, 1025])
+def test_a_row_without_any_logit_has_no_mass(n, V):
+    """Every logit is -infinity: nothing is listed, and the sum of exponentials is 0."""
+    d = 64
+    H, W = torch.zeros(n, d, device="cuda"), torch.zeros(V, d, device="cuda")
+    H[:, 0], W[:, 0] = 1, -float("inf")
+    ids, top, lse = umas.umas_top_logits(H.bfloat16(), W.bfloat16(), 5)
+    assert (ids == -1).all() and (top == -float("inf")).all() and (lse == -float("inf")).all()
