@@ -348,7 +348,7 @@ k_target_rows(RowsArgs O) {
   const int64_t row = A.rowsel ? A.rowsel[n] : n;
   const int blk = O.cidx[n >> 8], flag = O.flags[n >> 8];
   const float w = O.R.w[n], mass = O.R.mass[n], r = O.R.cref[n];
-  const bool in = lane < k, taught = r < 1e30f || r != r;
+  const bool in = lane < k, taught = mass > 0.f || mass != mass;   // (not by r, which is what a target's logit happens to be, infinity among others)
   const int id = in ? A.t.ids[row * k + lane] : -1;
   const float z = in ? O.R.zt[n * k + lane] : 0.f, ts = in ? O.R.tt[n * k + lane] : 0.f, t = A.t.logits ? place_of<float>(A.t, A.V, row).t : 0.f;
   merge_rows(O.partial, O.tiles_m, O.n_pad, O.c0 + m0, m0 + (lane & 7) < O.rows, s_rows);

@@ -1,5 +1,5 @@
-"""Largest logits, cross entropy and distillation on inputs that show what a kernel assumes: large logits gathered in few tokens, masks of a type's lowest value.  Inputs and
-tolerances as in test_gpu_targets."""
+"""Largest logits, cross entropy and distillation on inputs that show what a kernel assumes: large logits gathered in few tokens, masks of a type's lowest value,
+infinities in rows that are taught.  Inputs and tolerances as in test_gpu_targets."""
 import numpy as np
 import pytest
 import torch
@@ -80,3 +80,42 @@ def test_a_row_without_any_logit_has_no_mass(n, V):
     H[:, 0], W[:, 0] = 1, -float("inf")
     ids, top, lse = umas.umas_top_logits(H.bfloat16(), W.bfloat16(), 5)
     assert (ids == -1).all() and (top == -float("inf")).all() and (lse == -float("inf")).all()
+
+
+# ------------------------------------------------------------------------------------------------ targets
+def teach(kind, Hd, Wd, ids, weight, n_roles=0, role=None):
+    w = None if weight is None else cuda(weight, np.float32)
+    r = None if role is None else cuda(role, np.int32)
+    if kind == "ce":
+        return umas.umas_cross_entropy_fwd_bwd(Hd, Wd, cuda(ids, np.int32), None, w, r, n_roles)
+    return umas.umas_distill_fwd_bwd(Hd, Wd, cuda(ids[:, None], np.int32), torch.zeros(len(ids), 1, device="cuda"), None, None, w, r, n_roles)
+
+
+@pytest.mark.parametrize("kind", ["ce", "distill"])
+@pytest.mark.parametrize("n,dtype", [(40, "bf16"), (200, "bf16"), (300, "bf16"), (40, "f32"), (300, "f32")])
+def test_an_overflow_in_a_taught_row_is_seen(n, dtype, kind):
+    """The row's logits are all +infinity: its loss is no number however many rows there are, and nothing takes it for a row that is ignored."""
+    H, W, Hd, Wd, rng = arrays(n, n, 64, 700, dtype)
+    ids = rng.integers(0, 700, n)
+    Wd[:, 0] = 1.0
+    Hd[n // 3, 0] = float("inf")
+    stats, row, dH, dW = teach(kind, Hd, Wd, ids, None)
+    s = umas.read_target_stats(stats)
+    assert not np.isfinite(s["loss"][0]) and s["n_ignored"][0] == 0
+    bad = ~torch.isfinite(row)
+    assert bad[n // 3] and int(bad.sum()) == 1
+    assert not torch.isfinite(dH[n // 3].float()).any()
+
+
+@pytest.mark.parametrize("n", [40, 300])
+def test_a_targets_logit_that_overflows_is_seen(n):
+    H, W, Hd, Wd, rng = arrays(n + 1, n, 64, 700, "bf16")
+    ids = rng.integers(1, 700, n)
+    bad, y = n // 3, 0
+    ids[bad] = y
+    Hd[:, 0], Wd[:, 0] = 0.0, 0.0
+    Hd[bad, 0], Wd[y, 0] = 2.0 ** 100, 2.0 ** 30
+    stats, logp, dH, dW = teach("ce", Hd, Wd, ids, None)
+    assert not np.isfinite(umas.read_target_stats(stats)["loss"][0])
+    no = ~torch.isfinite(logp)
+    assert no[bad] and int(no.sum()) == 1
