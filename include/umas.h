@@ -446,7 +446,8 @@ umas_status umas_ready_batch_packed(const umas_streams* streams, int32_t n_model
 typedef struct umas_target_stats {
   float loss;              /* row 0: sum of w_i l_i over norm; roles: over the role's rows */
   float weight_mean;       /* of the selected rows, 0 for ignored ones */
-  float entropy_mean;      /* of the head, over the rows that are not ignored */
+  float entropy_mean;      /* of the head, over the rows that are not ignored; rows of weight 0 whose entropy or logsumexp
+                            * is no number are left out */
   float lse_mean;          /* ... its logsumexp */
   int64_t n_scored;        /* selected rows */
   int64_t n_ignored;       /* ... that have no target */

@@ -211,7 +211,8 @@ struct StatArgs {
 template <int T>
 __device__ __forceinline__ void target_stats(const StatArgs& S, int k, double* smem) {
   constexpr int kRows = 4;                                   // loads of as many rows are under way
-  double v[6] = {}, sum[6];
+  constexpr int kSums = 7;
+  double v[kSums] = {}, sum[kSums];
   for (int64_t n0 = threadIdx.x; n0 < S.n_sel; n0 += kRows * T) {
     float l[kRows], w[kRows], ent[kRows], lse[kRows], mass[kRows];
     bool in[kRows];
@@ -224,24 +225,25 @@ __device__ __forceinline__ void target_stats(const StatArgs& S, int k, double* s
 #pragma unroll
     for (int q = 0; q < kRows; ++q) {
       if (!in[q]) continue;
-      const bool taught = mass[q] != 0.f;
+      // a row of weight 0 counts in the means of entropy and logsumexp while they are numbers: its hidden state may be anything
+      const bool taught = mass[q] != 0.f, counts = taught && (w[q] != 0.f || (fabsf(ent[q]) < INFINITY && fabsf(lse[q]) < INFINITY));
       v[0] += w[q] != 0.f ? static_cast<double>(w[q]) * static_cast<double>(l[q]) : 0.0;
       v[1] += static_cast<double>(w[q]);
-      v[2] += taught ? static_cast<double>(ent[q]) : 0.0;
-      v[3] += taught ? static_cast<double>(lse[q]) : 0.0;
+      v[2] += counts ? static_cast<double>(ent[q]) : 0.0;
+      v[3] += counts ? static_cast<double>(lse[q]) : 0.0;
       v[4] += 1.0;
       v[5] += taught ? 0.0 : 1.0;
+      v[6] += counts ? 1.0 : 0.0;
     }
   }
 #pragma unroll
-  for (int j = 0; j < 6; ++j) sum[j] = block_sum<double>(v[j], smem);
+  for (int j = 0; j < kSums; ++j) sum[j] = block_sum<double>(v[j], smem);
   if (threadIdx.x != 0) return;
-  const double taught = sum[4] - sum[5];
   umas_target_stats s;
   s.loss = sum[4] > 0 ? static_cast<float>(sum[0] / (k == 0 ? static_cast<double>(S.norm) : sum[4])) : 0.f;
   s.weight_mean = sum[4] > 0 ? static_cast<float>(sum[1] / sum[4]) : 0.f;
-  s.entropy_mean = taught > 0 ? static_cast<float>(sum[2] / taught) : 0.f;
-  s.lse_mean = taught > 0 ? static_cast<float>(sum[3] / taught) : 0.f;
+  s.entropy_mean = sum[6] > 0 ? static_cast<float>(sum[2] / sum[6]) : 0.f;
+  s.lse_mean = sum[6] > 0 ? static_cast<float>(sum[3] / sum[6]) : 0.f;
   s.n_scored = static_cast<int64_t>(sum[4]);
   s.n_ignored = static_cast<int64_t>(sum[5]);
   S.stats[k] = s;

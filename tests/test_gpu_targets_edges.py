@@ -1,10 +1,11 @@
 """Largest logits, cross entropy and distillation on inputs that show what a kernel assumes: large logits gathered in few tokens, masks of a type's lowest value,
-infinities in rows that are taught.  Inputs and tolerances as in test_gpu_targets."""
+infinities in rows that are taught, rows of weight 0.  Inputs and tolerances as in test_gpu_targets."""
 import numpy as np
 import pytest
 import torch
 
 import paper_2605_26646_amd as umas
+from oracle import umas_oracle as orc
 from tests.test_gpu_targets import DT, arrays, cuda
 
 pytestmark = pytest.mark.gpu
@@ -119,3 +120,34 @@ def test_a_targets_logit_that_overflows_is_seen(n):
     assert not np.isfinite(umas.read_target_stats(stats)["loss"][0])
     no = ~torch.isfinite(logp)
     assert no[bad] and int(no.sum()) == 1
+
+
+@pytest.mark.parametrize("kind", ["ce", "distill"])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("n", [40, 200, 600])
+def test_statistics_next_to_rows_of_weight_0_that_hold_anything(n, dtype, kind):
+    """Their entropies and logsumexps are no numbers and are left out; those of a row of weight 0 that are numbers count.  (Tolerances as in check_taught: 2^-24 of the
+    logits and of their squares.)"""
+    V = 700
+    H, W, Hd, Wd, rng = arrays(n + 2, n, 64, V, dtype)
+    ids, role = rng.integers(0, V, n), rng.integers(0, 2, n)
+    weight = np.ones(n, np.float32)
+    bad = np.array([3, n // 2, n - 2])
+    weight[bad], weight[7] = 0, 0
+    role[bad[0]] = 0
+    role[bad[1]] = 1
+    for i, x in zip(bad, (np.nan, np.inf, -np.inf)):
+        Hd[i] = x
+    clean = H.copy()
+    clean[bad] = 0
+    r = orc.cross_entropy(clean, W, ids, None, weight)
+    s = umas.read_target_stats(teach(kind, Hd, Wd, ids, weight, 2, role)[0])
+    good = np.ones(n, bool)
+    good[bad] = False
+    zl = np.abs(H @ W.T).max() + np.abs(r["lse"]).max()
+    for k in range(3):
+        q = good if k == 0 else good & (role == k - 1)
+        for name in ("entropy", "lse"):
+            want = r[name][q].mean()
+            assert abs(s[name + "_mean"][k] - want) <= 1e-5 * (1 + abs(want)) + (16 * 2.0 ** -24 * zl * (1 + zl) if name == "entropy" else 0)
+        assert s["n_scored"][k] == (n if k == 0 else (role == k - 1).sum()) and s["n_ignored"][k] == 0
