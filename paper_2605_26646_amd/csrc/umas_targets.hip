@@ -81,12 +81,13 @@ __device__ __forceinline__ Real mass_of_token(int k, int id, Real t) {
 }
 // g of the row: 0 where nothing is taught
 __device__ __forceinline__ float row_weight(const Teach& A, int64_t row, bool taught) { return taught ? (A.weight ? A.weight[row] : 1.f) : 0.f; }
-// A factor of 0 in the dense part (a mass of 0 is no target, but a negative logsumexp with the penalty can come to it) would divide the sparse one: kept
-// off it by what is below the rounding of either.
+// a', the factor of the dense part; the sparse part is divided by it, T / a'.  With the penalty it can come to 0 beside a mass that does not (a negative logsumexp):
+// then it is kept off 0 by what is below the rounding of either part.  Without, it is the mass, however little that is: a teacher may give e^-40 to its places.
 template <class Real>
-__device__ __forceinline__ Real dense_factor(Real mass, float z_coef, Real lse) {
-  const Real a = z_coef != 0.f ? mass + 2 * Real(z_coef) * lse : mass;
-  return fabs(a) < Real(1e-10) ? Real(1e-10) : a;
+__device__ __forceinline__ Real dense_factor(Real mass, float z_coef, Real lse) { return z_coef != 0.f ? mass + 2 * Real(z_coef) * lse : mass; }
+__device__ __forceinline__ float dense_divisor(float mass, float z_coef, float lse) {
+  const float a = dense_factor(mass, z_coef, lse);
+  return fabsf(a) < 1e-10f * mass ? 1e-10f * mass : a;
 }
 
 // ------------------------------------------------------------------ what a call leaves per row, compact, in selection order
@@ -355,7 +356,7 @@ k_target_rows(RowsArgs O) {
   const float z = in ? O.R.zt[n * k + lane] : 0.f, ts = in ? O.R.tt[n * k + lane] : 0.f, t = A.t.logits ? place_of<float>(A.t, A.V, row).t : 0.f;
   merge_rows(O.partial, O.tiles_m, O.n_pad, O.c0 + m0, m0 + (lane & 7) < O.rows, s_rows);
   if (m >= O.rows) return;
-  const float lse = s_rows.lse[q], g = w / A.norm, a = dense_factor(mass, A.z_coef, lse);
+  const float lse = s_rows.lse[q], g = w / A.norm, a = dense_divisor(mass, A.z_coef, lse);
   float l = 0.f, out = 0.f, f = 0.f;
   if (taught) {
     if (!A.t.logits) {
@@ -474,7 +475,7 @@ k_target_few(FewArgs F) {
   const float z = P.t != 0.f ? *F.Z.at(n, P.id >> 8, P.id & 255) : 0.f;
   merge_rows(F.partial, F.tiles_m, F.n_pad, m0, m0 + (lane & 7) < A.n_sel, s_rows);
   if (m0 + q >= A.n_sel) return;
-  const float lse = s_rows.lse[q], a = dense_factor(P.mass, A.z_coef, lse);
+  const float lse = s_rows.lse[q], a = dense_divisor(P.mass, A.z_coef, lse);
   float l = 0.f, out = 0.f;
   if (taught) {
     if (!A.t.logits) {

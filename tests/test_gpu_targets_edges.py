@@ -1,12 +1,12 @@
 """Largest logits, cross entropy and distillation on inputs that show what a kernel assumes: large logits gathered in few tokens, masks of a type's lowest value,
-infinities in rows that are taught, rows of weight 0.  Inputs and tolerances as in test_gpu_targets."""
+infinities in rows that are taught, rows of weight 0, teachers that give next to nothing to their places.  Inputs and tolerances as in test_gpu_targets."""
 import numpy as np
 import pytest
 import torch
 
 import paper_2605_26646_amd as umas
 from oracle import umas_oracle as orc
-from tests.test_gpu_targets import DT, arrays, cuda
+from tests.test_gpu_targets import DT, arrays, check_taught, cuda
 
 pytestmark = pytest.mark.gpu
 
@@ -151,3 +151,41 @@ def test_statistics_next_to_rows_of_weight_0_that_hold_anything(n, dtype, kind):
             want = r[name][q].mean()
             assert abs(s[name + "_mean"][k] - want) <= 1e-5 * (1 + abs(want)) + (16 * 2.0 ** -24 * zl * (1 + zl) if name == "entropy" else 0)
         assert s["n_scored"][k] == (n if k == 0 else (role == k - 1).sum()) and s["n_ignored"][k] == 0
+
+
+@pytest.mark.parametrize("dtype,dW_dtype", [("bf16", "bf16"), ("bf16", "f32"), ("f32", "f32")])
+@pytest.mark.parametrize("n", [30, 200, 300])
+@pytest.mark.parametrize("gap", [20.0, 28.0, 40.0])
+def test_a_teacher_that_gives_next_to_nothing_to_its_places(n, dtype, dW_dtype, gap):
+    """Masses of e^-20 and less: dz = g (T p - t) still sums to 0 over the vocabulary."""
+    d, V, k = 64, 300, 5
+    H, W, Hd, Wd, rng = arrays(int(n + gap), n, d, V, dtype, scale=2.0)
+    ids = np.stack([rng.permutation(V)[:k] for _ in range(n)])
+    l = rng.normal(size=(n, k)).astype(np.float32)
+    lse = (l.max(1) + gap).astype(np.float32)
+    masses = orc.teacher_masses(ids, l, lse, V)
+    r = orc.distill(H, W, ids, l, lse)
+    kw = {} if dW_dtype == dtype else dict(dW=torch.full((V, d), float("nan"), device="cuda"))
+    got = umas.umas_distill_fwd_bwd(Hd, Wd, cuda(ids, np.int32), cuda(l, np.float32), cuda(lse, np.float32), **kw)
+    check_taught(r, H, W, ids, masses, got, dtype, dW_dtype, np.zeros(n), 0, n, 0.0)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("n", [30, 300])
+def test_a_penalty_that_cancels_the_dense_part(n, dtype):
+    """1 + 2 c lse is 0, or as near as float32 comes: the one-hot part stands by itself.  Norm-wise bars: what is left of the dense part is rounding."""
+    V = 300
+    H, W, _, _, rng = arrays(n + 3, 1, 64, V, dtype)
+    H, W = np.repeat(H, n, 0), W.copy()
+    H[:, 0], W[:, 0] = 1.0, -12.0
+    ids = rng.integers(0, V, n)
+    z = H[0] @ W.T
+    lse = z.max() + np.log(np.exp(z - z.max()).sum())
+    assert lse < -2
+    c = float(np.float32(-0.5 / lse))
+    r = orc.cross_entropy(H, W, ids, z_coef=c)
+    stats, logp, dH, dW = umas.umas_cross_entropy_fwd_bwd(cuda(H, np.float32).to(DT[dtype]), cuda(W, np.float32).to(DT[dtype]), cuda(ids, np.int32), z_coef=c)
+    assert abs(umas.read_target_stats(stats)["loss"][0] - r["loss"]) <= 1e-5 * (1 + abs(r["loss"]))
+    for x, o in ((dH, r["dH"]), (dW, r["dW"])):
+        x = x.double().cpu().numpy()
+        assert np.isfinite(x).all() and np.linalg.norm(x - o) <= (1e-2 if dtype == "bf16" else 1e-5) * np.linalg.norm(o)
