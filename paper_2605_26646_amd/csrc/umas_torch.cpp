@@ -103,15 +103,30 @@ struct Selection {                                        // None: all rows; an 
   void point(void* otherwise, PyObject* o) { if (o != Py_None && !p) p = static_cast<const int32_t*>(otherwise); }
 };
 
-// The calls that list logits and teach targets read and write [n, k] arrays: types, shapes and layout are looked at here, where a wrong one would be read
+// A kernel gets addresses: an array in host memory would fault the GPU.  `dev` is where H lies; pinned host memory is in reach of a kernel as well.
+void in_reach(const at::Tensor& t, const at::Device& dev, const char* name) {
+  if (t.device() == dev || (t.is_cpu() && t.is_pinned())) return;
+  PyErr_Format(PyExc_ValueError, "%s must be on the device of H", name);
+  throw Failed();
+}
+// (H on the host goes with a workspace there; an empty one the library refuses itself, behind its own checks)
+void on_gpu(const at::Tensor& ws, const at::Device& dev) {
+  in_reach(ws, dev, "workspace");
+  if (ws.is_cuda() || ws.numel() == 0) return;
+  PyErr_SetString(PyExc_ValueError, "H and what goes with it must be on a GPU");
+  throw Failed();
+}
+// The calls that list logits and teach targets read and write [n, k] arrays: types, shapes, layout and device are looked at here, where a wrong one would be read
 // out of bounds.
 void same_head(const Rows& H, const at::Tensor& W) {
+  in_reach(W, H.t.device(), "W");
   if (W.dim() == 2 && W.size(1) == H.d && W.scalar_type() == H.t.scalar_type() && H.t.is_contiguous() && W.is_contiguous()) return;
   PyErr_SetString(PyExc_ValueError, "H [n, d] and W [V, d] must be contiguous and of one type and width");
   throw Failed();
 }
-const at::Tensor& targets(PyObject* o, at::ScalarType type, int64_t n, int64_t k, const char* name) {
+const at::Tensor& targets(PyObject* o, at::ScalarType type, int64_t n, int64_t k, const at::Device& dev, const char* name) {
   const at::Tensor& t = tensor(o);
+  in_reach(t, dev, name);
   if (t.scalar_type() != type) {
     PyErr_Format(PyExc_TypeError, "%s must be %s", name, type == at::kInt ? "int32" : "float32");
     throw Failed();
@@ -391,15 +406,19 @@ PyObject* ppo_loss(PyObject* const* a) {
 }
 
 // (the checks of the two calls below and their kin, see same_head)
-const at::Tensor* targets_or_null(PyObject* o, at::ScalarType type, int64_t n, const char* name) { return o == Py_None ? nullptr : &targets(o, type, n, 1, name); }
-void whole_selection(PyObject* o) {
+const at::Tensor* targets_or_null(PyObject* o, at::ScalarType type, int64_t n, const at::Device& dev, const char* name) {
+  return o == Py_None ? nullptr : &targets(o, type, n, 1, dev, name);
+}
+void whole_selection(PyObject* o, const at::Device& dev) {
   if (o == Py_None) return;
   const at::Tensor& t = tensor(o);
+  in_reach(t, dev, "rowsel");
   if (t.scalar_type() == at::kInt && t.is_contiguous()) return;
   PyErr_SetString(PyExc_TypeError, "rowsel must be contiguous and int32");
   throw Failed();
 }
-void room(const Output& out, at::ScalarType type, int64_t n, const char* name) {
+void room(const Output& out, at::ScalarType type, int64_t n, const at::Device& dev, const char* name) {
+  in_reach(out.t, dev, name);
   if (!out.given || (out.t.scalar_type() == type && out.t.numel() == n && out.t.is_contiguous())) return;
   PyErr_Format(PyExc_ValueError, "%s must be contiguous, %s and hold %lld values", name, c10::toString(type), static_cast<long long>(n));
   throw Failed();
@@ -420,10 +439,11 @@ PyObject* top_logits(PyObject* const* a) {                // H, W, k, rowsel, id
   sel.point(ws.t.data_ptr(), a[3]);
   void* const st = stream_of(a[8]);
   same_head(H, W);
-  whole_selection(a[3]);
-  room(ids, at::kInt, H.n * places, "ids");
-  room(logits, at::kFloat, H.n * places, "logits");
-  room(lse, at::kFloat, H.n, "lse");
+  whole_selection(a[3], dev);
+  room(ids, at::kInt, H.n * places, dev, "ids");
+  room(logits, at::kFloat, H.n * places, dev, "logits");
+  room(lse, at::kFloat, H.n, dev, "lse");
+  on_gpu(ws.t, dev);
   UMAS_CALL(umas_top_logits(H.t.data_ptr(), W.data_ptr(), dt, H.n, H.d, V, sel.p, sel.n, k, ptr<int32_t>(ids.t), ptr<float>(logits.t), ptr<float>(lse.t),
                             ws.t.data_ptr(), ws.t.numel(), st));
   return pack({ids.object(), logits.object(), lse.object()});
@@ -456,18 +476,19 @@ struct Taught {
         stats(o[9], [&] { return fresh({(1 + static_cast<int64_t>(std::max(n_roles, 0))) * static_cast<int64_t>(sizeof(umas_target_stats))}, at::kByte, dev); }),
         dW_type(UMAS_NO_DW), st(stream_of(o[11])) {
     same_head(H, W);
-    whole_selection(rowsel);
-    targets_or_null(o[0], at::kFloat, H.n, "weight");
-    targets_or_null(o[1], at::kInt, H.n, "tok_role");
-    room(dH, H.t.scalar_type(), H.t.numel(), "dH");
-    room(row_out, at::kFloat, H.n, "the output of every row");
-    room(stats, at::kByte, (1 + static_cast<int64_t>(std::max(n_roles, 0))) * static_cast<int64_t>(sizeof(umas_target_stats)), "stats");
+    whole_selection(rowsel, dev);
+    targets_or_null(o[0], at::kFloat, H.n, dev, "weight");
+    targets_or_null(o[1], at::kInt, H.n, dev, "tok_role");
+    room(dH, H.t.scalar_type(), H.t.numel(), dev, "dH");
+    room(row_out, at::kFloat, H.n, dev, "the output of every row");
+    room(stats, at::kByte, (1 + static_cast<int64_t>(std::max(n_roles, 0))) * static_cast<int64_t>(sizeof(umas_target_stats)), dev, "stats");
     if (head && accumulate && !dW_given) {
       PyErr_SetString(PyExc_ValueError, "accumulate_dW needs the dW to add to");
       throw Failed();
     }
     if (!head) return;
     dW = dW_given ? tensor(dW_given) : at::empty_like(W);
+    in_reach(dW, dev, "dW");
     if (dW.scalar_type() != at::kFloat && dW.scalar_type() != W.scalar_type()) {
       PyErr_SetString(PyExc_TypeError, "dW must be float32 or of the type of W");
       throw Failed();
@@ -492,9 +513,10 @@ struct Taught {
 PyObject* cross_entropy(PyObject* const* a) {
   // H, W, ids, rowsel, z_coef, weight, tok_role, n_roles, train_head, accumulate_dW, norm_rows, dW, dH, logp, stats, workspace, stream
   Taught T(a[0], a[1], a[3], a + 5);
-  const at::Tensor& ids = targets(a[2], at::kInt, T.H.n, 1, "ids");
+  const at::Tensor& ids = targets(a[2], at::kInt, T.H.n, 1, T.dev, "ids");
   const float z_coef = real(a[4]);
   const Output ws(a[15], [&] { return workspace(umas_cross_entropy_workspace_bytes(T.sel.n, T.H.d, T.V, T.dt, T.dW_type), T.dev); });
+  on_gpu(ws.t, T.dev);
   T.sel.point(ws.t.data_ptr(), a[3]);
   UMAS_CALL(umas_cross_entropy_fwd_bwd(T.H.t.data_ptr(), T.W.data_ptr(), T.dt, T.H.n, T.H.d, T.V, ptr<int32_t>(ids), T.sel.p, T.sel.n, T.weight, T.role,
                                        T.n_roles, z_coef, T.accumulate, T.norm_rows, ptr<umas_target_stats>(T.stats.t), ptr<float>(T.row_out.t),
@@ -506,10 +528,11 @@ PyObject* distill(PyObject* const* a) {
   // H, W, top_ids, top_logits, teacher_lse, rowsel, weight, tok_role, n_roles, train_head, accumulate_dW, norm_rows, dW, dH, kl, stats, workspace, stream
   Taught T(a[0], a[1], a[5], a + 6);
   const int64_t k = tensor(a[2]).dim() == 2 ? tensor(a[2]).size(1) : 0;
-  const at::Tensor &ids = targets(a[2], at::kInt, T.H.n, k, "top_ids"), &logits = targets(a[3], at::kFloat, T.H.n, k, "top_logits");
-  const float* const lse = a[4] == Py_None ? nullptr : ptr<const float>(targets(a[4], at::kFloat, T.H.n, 1, "teacher_lse"));
+  const at::Tensor &ids = targets(a[2], at::kInt, T.H.n, k, T.dev, "top_ids"), &logits = targets(a[3], at::kFloat, T.H.n, k, T.dev, "top_logits");
+  const float* const lse = a[4] == Py_None ? nullptr : ptr<const float>(targets(a[4], at::kFloat, T.H.n, 1, T.dev, "teacher_lse"));
   const int32_t places = static_cast<int32_t>(std::min<int64_t>(k, 1 << 30));
   const Output ws(a[16], [&] { return workspace(umas_distill_workspace_bytes(T.sel.n, T.H.d, T.V, places, T.dt, T.dW_type), T.dev); });
+  on_gpu(ws.t, T.dev);
   T.sel.point(ws.t.data_ptr(), a[5]);
   UMAS_CALL(umas_distill_fwd_bwd(T.H.t.data_ptr(), T.W.data_ptr(), T.dt, T.H.n, T.H.d, T.V, ptr<int32_t>(ids), ptr<float>(logits), places, lse, T.sel.p,
                                  T.sel.n, T.weight, T.role, T.n_roles, T.accumulate, T.norm_rows, ptr<umas_target_stats>(T.stats.t), ptr<float>(T.row_out.t),
