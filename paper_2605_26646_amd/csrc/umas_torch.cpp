@@ -67,6 +67,33 @@ T* ptr_or(const at::Tensor& t, void* otherwise) {
   T* p = ptr<T>(t);
   return p ? p : static_cast<T*>(otherwise);
 }
+// A kernel gets addresses: an array in host memory would fault the GPU.  `dev` is where the call's first array lies (H, the mask, the streams); pinned host memory is in
+// reach of a kernel as well.
+void in_reach(const at::Tensor& t, const at::Device& dev, const char* name) {
+  if (t.device() == dev || t.numel() == 0 || (t.is_cpu() && t.is_pinned())) return;
+  PyErr_Format(PyExc_ValueError, "%s is not on the device of the other arrays", name);
+  throw Failed();
+}
+struct Named {
+  PyObject* o;                                            // a tensor or None
+  const char* name;
+};
+void in_reach(std::initializer_list<Named> arrays, const at::Device& dev) {
+  for (const Named& a : arrays)
+    if (a.o != Py_None) in_reach(tensor(a.o), dev, a.name);
+}
+void on_gpu(const at::Device& dev) {
+  if (dev.is_cuda()) return;
+  PyErr_SetString(PyExc_ValueError, "H and what goes with it must be on a GPU");
+  throw Failed();
+}
+// (H on the host goes with a workspace there; an empty one the library refuses itself, behind its own checks)
+void on_gpu(const at::Tensor& ws, const at::Device& dev) {
+  in_reach(ws, dev, "workspace");
+  if (ws.numel() != 0) on_gpu(ws.device());
+}
+// Bytes of a workspace that the binding has made: none on the host, so that the library, whose checks of the call's host arrays come first, refuses.
+size_t bytes_of(const at::Tensor& ws) { return ws.is_cuda() ? static_cast<size_t>(ws.numel()) : 0; }
 int dtype_code(PyObject* o) {
   const at::Tensor& t = tensor(o);
   if (t.scalar_type() == at::kFloat) return UMAS_F32;
@@ -103,19 +130,6 @@ struct Selection {                                        // None: all rows; an 
   void point(void* otherwise, PyObject* o) { if (o != Py_None && !p) p = static_cast<const int32_t*>(otherwise); }
 };
 
-// A kernel gets addresses: an array in host memory would fault the GPU.  `dev` is where H lies; pinned host memory is in reach of a kernel as well.
-void in_reach(const at::Tensor& t, const at::Device& dev, const char* name) {
-  if (t.device() == dev || (t.is_cpu() && t.is_pinned())) return;
-  PyErr_Format(PyExc_ValueError, "%s must be on the device of H", name);
-  throw Failed();
-}
-// (H on the host goes with a workspace there; an empty one the library refuses itself, behind its own checks)
-void on_gpu(const at::Tensor& ws, const at::Device& dev) {
-  in_reach(ws, dev, "workspace");
-  if (ws.is_cuda() || ws.numel() == 0) return;
-  PyErr_SetString(PyExc_ValueError, "H and what goes with it must be on a GPU");
-  throw Failed();
-}
 // The calls that list logits and teach targets read and write [n, k] arrays: types, shapes, layout and device are looked at here, where a wrong one would be read
 // out of bounds.
 void same_head(const Rows& H, const at::Tensor& W) {
@@ -250,11 +264,12 @@ struct Ref {                                              // an owned reference
   ~Ref() { Py_DECREF(o); }
 };
 // the ABI's struct of a Streams object; the object keeps its tensors
-umas_streams streams_of(PyObject* o, void* otherwise) {
+umas_streams streams_of(PyObject* o, const at::Device& dev, void* otherwise) {
   umas_streams s;
   void** p = reinterpret_cast<void**>(&s);
   for (int i = 0; i < kStreamTensors; ++i) {
     const Ref t(PyObject_GetAttr(o, g_stream_names[i]));
+    in_reach(tensor(t.o), dev, kStreamNames[i]);
     p[i] = ptr_or<void>(tensor(t.o), otherwise);
   }
   return s;
@@ -315,7 +330,7 @@ PyObject* assign(PyObject* const* a) {
   const at::Tensor ws = workspace(umas_assign_workspace_bytes(&g), dev);
   umas_streams s;
   for (int i = 0; i < kStreamTensors; ++i) reinterpret_cast<void**>(&s)[i] = ptr_or<void>(out[i], ws.data_ptr());
-  UMAS_CALL(umas_assign_token_rewards(&g, &r, ptr_or<uint8_t>(mask, ws.data_ptr()), &s, ws.data_ptr(), ws.numel(), st));
+  UMAS_CALL(umas_assign_token_rewards(&g, &r, ptr_or<uint8_t>(mask, ws.data_ptr()), &s, ws.data_ptr(), bytes_of(ws), st));
   PyObject* res = PyTuple_New(3 + kStreamTensors);
   if (!res) return nullptr;
   PyTuple_SET_ITEM(res, 0, PyLong_FromLongLong(N));
@@ -332,10 +347,11 @@ PyObject* advantages(PyObject* const* a) {                // streams, value, gam
   const float gamma = real(a[2]), lam = real(a[3]), gamma_turn = real(a[4]);
   const int32_t seg = integer32(a[5]);
   const at::Tensor adv = fresh({N}, at::kFloat, dev), ret = fresh({N}, at::kFloat, dev), ws = workspace(umas_advantages_workspace_bytes(N), dev);
-  const umas_streams s = streams_of(a[0], ws.data_ptr());
+  const umas_streams s = streams_of(a[0], dev, ws.data_ptr());
+  in_reach({{a[1], "value"}}, dev);
   const float* value = ptr_or_null<const float>(a[1]);
   void* const st = stream_of(a[6]);
-  UMAS_CALL(umas_advantages(&s, N, U, value, gamma, lam, gamma_turn, seg, ptr<float>(adv), ptr<float>(ret), ws.data_ptr(), ws.numel(), st));
+  UMAS_CALL(umas_advantages(&s, N, U, value, gamma, lam, gamma_turn, seg, ptr<float>(adv), ptr<float>(ret), ws.data_ptr(), bytes_of(ws), st));
   return pack({wrap(adv), wrap(ret)});
 }
 
@@ -345,6 +361,8 @@ PyObject* policy_logprobs(PyObject* const* a) {           // H, W, ids, rowsel, 
   const int32_t V = static_cast<int32_t>(W.size(0));
   Selection sel(a[3], H.n);
   const at::Device dev = H.t.device();
+  on_gpu(dev);
+  in_reach({{a[1], "W"}, {a[2], "ids"}, {a[3], "rowsel"}, {a[5], "workspace"}}, dev);
   const at::Tensor logp = fresh({H.n}, at::kFloat, dev), lse = fresh({H.n}, at::kFloat, dev);
   const bool want = truth(a[4]);
   const at::Tensor entropy = want ? fresh({H.n}, at::kFloat, dev) : at::Tensor();
@@ -363,6 +381,8 @@ PyObject* policy_logprobs_static(PyObject* const* a) {    // H, W, ids, rowsel, 
   const Rows H(a[0]);
   const at::Tensor &W = tensor(a[1]), &ids = tensor(a[2]);
   const at::Device dev = H.t.device();
+  on_gpu(dev);
+  in_reach({{a[1], "W"}, {a[2], "ids"}, {a[3], "rowsel"}, {a[4], "logp"}, {a[5], "lse"}, {a[6], "entropy"}}, dev);
   auto row = [&] { return fresh({H.n}, at::kFloat, dev); };
   const Output logp(a[4], row), lse(a[5], row), entropy(a[6], row);
   Selection sel(a[3], H.n);
@@ -381,6 +401,9 @@ PyObject* ppo_loss(PyObject* const* a) {
   const int32_t V = static_cast<int32_t>(W.size(0)), n_roles = integer32(a[7]);
   Selection sel(a[3], H.n);
   const at::Device dev = H.t.device();
+  on_gpu(dev);
+  in_reach({{a[1], "W"}, {a[2], "ids"}, {a[3], "rowsel"}, {a[4], "logp_old"}, {a[5], "adv"}, {a[6], "tok_role"}, {a[13], "logp_ref"}, {a[15], "dW"}, {a[16], "dH"},
+            {a[17], "logp_new"}, {a[18], "stats"}, {a[19], "workspace"}}, dev);
   const umas_dtype dt = static_cast<umas_dtype>(H.dt);
   const Output dW(a[15], [&] { return fresh({W.size(0), H.d}, at::kFloat, dev); });
   const Output dH(a[16], [&] { return at::empty_like(H.t); });
@@ -543,6 +566,8 @@ PyObject* distill(PyObject* const* a) {
 PyObject* values(PyObject* const* a) {                    // H, w, bias, rowsel, value, stream
   const Rows H(a[0]);
   const at::Tensor& w = tensor(a[1]);
+  on_gpu(H.t.device());
+  in_reach({{a[1], "w"}, {a[3], "rowsel"}, {a[4], "value"}}, H.t.device());
   const Output value(a[4], [&] { return fresh({H.n}, at::kFloat, H.t.device()); });
   Selection sel(a[3], H.n);
   sel.point(w.data_ptr(), a[3]);
@@ -558,6 +583,9 @@ PyObject* value_loss(PyObject* const* a) {
   const Rows H(a[0]);
   const at::Tensor& w = tensor(a[1]);
   const at::Device dev = H.t.device();
+  on_gpu(dev);
+  in_reach({{a[1], "w"}, {a[3], "rowsel"}, {a[4], "value_old"}, {a[5], "ret"}, {a[6], "tok_role"}, {a[12], "dH"}, {a[13], "dw"}, {a[14], "db"}, {a[15], "value_new"}, {a[16], "stats"},
+            {a[17], "workspace"}}, dev);
   const umas_dtype dt = static_cast<umas_dtype>(H.dt);
   const int32_t n_roles = integer32(a[7]);
   Selection sel(a[3], H.n);
@@ -584,6 +612,7 @@ PyObject* kl_rewards(PyObject* const* a) {                // tok_reward, logp, l
   const at::Tensor& r = tensor(a[0]);
   const int64_t n = r.numel();
   const at::Device dev = r.device();
+  in_reach({{a[1], "logp"}, {a[2], "logp_ref"}, {a[3], "tok_mask"}, {a[5], "out"}}, dev);
   const Output out(a[5], [&] { return at::empty_like(r); });
   const at::Tensor kl = fresh({1}, at::kFloat, dev), ws = workspace(umas_kl_rewards_workspace_bytes(n), dev);
   auto at_ = [&](const at::Tensor& t) { return n ? t.data_ptr() : ws.data_ptr(); };
@@ -591,7 +620,7 @@ PyObject* kl_rewards(PyObject* const* a) {                // tok_reward, logp, l
   const float beta = real(a[4]);
   void* const st = stream_of(a[6]);
   UMAS_CALL(umas_kl_rewards(static_cast<float*>(at_(r)), static_cast<float*>(at_(logp)), static_cast<float*>(at_(ref)), static_cast<uint8_t*>(at_(mask)), n,
-                            beta, static_cast<float*>(at_(out.t)), ptr<float>(kl), ws.data_ptr(), ws.numel(), st));
+                            beta, static_cast<float*>(at_(out.t)), ptr<float>(kl), ws.data_ptr(), bytes_of(ws), st));
   return pack({out.object(), wrap(kl)});
 }
 
@@ -599,6 +628,7 @@ PyObject* whiten(PyObject* const* a) {                    // adv, tok_mask, tok_
   const at::Tensor& adv = tensor(a[0]);
   const int64_t n = adv.numel();
   const at::Device dev = adv.device();
+  in_reach({{a[1], "tok_mask"}, {a[2], "tok_role"}, {a[7], "out"}}, dev);
   I64_ARRAY(off, a[3]);
   const int32_t n_models = static_cast<int32_t>(off.len - 1), n_roles = integer32(a[4]), scope = integer32(a[5]);
   const Output out(a[7], [&] { return at::empty_like(adv); });
@@ -610,7 +640,7 @@ PyObject* whiten(PyObject* const* a) {                    // adv, tok_mask, tok_
   const int32_t* const role = static_cast<int32_t*>(at_(a[2]));
   float* const y = static_cast<float*>(n ? out.t.data_ptr() : ws.data_ptr());
   void* const st = stream_of(a[8]);
-  UMAS_CALL(umas_whiten_advantages(x, mask, role, off.as<int64_t>(), n_models, n_roles, n, scope, eps, y, ws.data_ptr(), ws.numel(), st));
+  UMAS_CALL(umas_whiten_advantages(x, mask, role, off.as<int64_t>(), n_models, n_roles, n, scope, eps, y, ws.data_ptr(), bytes_of(ws), st));
   return out.object();
 }
 
@@ -631,17 +661,17 @@ PyObject* ready_batch(PyObject* const* a) {               // streams, traj_turn_
   const at::Tensor off = fresh({M, (cut == 2 ? B : arg) + 1}, at::kLong, dev);
   const at::Tensor parts = cut == 2 ? fresh({M}, at::kInt, dev) : at::Tensor();
   const at::Tensor ws = workspace(umas_ready_batch_workspace_bytes(B, M), dev);
-  const umas_streams s = streams_of(a[0], ws.data_ptr());
+  const umas_streams s = streams_of(a[0], dev, ws.data_ptr());
   const int32_t* const t = tto.as<int32_t>();
   const uint8_t* const k = keep.as<uint8_t>();
   const int32_t* const o = order.as<int32_t>();
   void* const st = stream_of(a[6]);
   if (cut == 2) {
-    UMAS_CALL(umas_ready_batch_packed(&s, M, U, t, B, k, o, arg, ptr<int32_t>(rows), ptr<int64_t>(off), ptr<int32_t>(parts), ws.data_ptr(), ws.numel(), st));
+    UMAS_CALL(umas_ready_batch_packed(&s, M, U, t, B, k, o, arg, ptr<int32_t>(rows), ptr<int64_t>(off), ptr<int32_t>(parts), ws.data_ptr(), bytes_of(ws), st));
     return pack({wrap(rows), wrap(off), wrap(parts)});
   }
   const auto fn = cut == 1 ? umas_ready_batch_balanced : umas_ready_batch;
-  UMAS_CALL(fn(&s, M, U, t, B, k, o, static_cast<int32_t>(arg), ptr<int32_t>(rows), ptr<int64_t>(off), ws.data_ptr(), ws.numel(), st));
+  UMAS_CALL(fn(&s, M, U, t, B, k, o, static_cast<int32_t>(arg), ptr<int32_t>(rows), ptr<int64_t>(off), ws.data_ptr(), bytes_of(ws), st));
   return pack({wrap(rows), wrap(off)});
 }
 
