@@ -19,6 +19,8 @@
 // Roundings to bf16: an entry of E (relative error up to 2^-9; the sum of exponentials and the logsumexp are float32 and do not see it), the scaled
 // copy of H, and the results.  A row of dW that a single row of H makes carries all three: 270 to 2000 rows dW is off by 0.0024 to 0.0028 of its norm, where
 // rounding the result alone is 0.0017, 4096 rows 0.0024, up to 256 rows (two roundings, see below) 0.0021 to 0.0024.
+#include <float.h>
+
 #include "umas_f32.h"
 #include "umas_few.h"
 #include "umas_gradients.h"
@@ -341,7 +343,20 @@ __device__ __forceinline__ float target_entry(float z, float lse, float r, float
   const float lp = z - lse, q = t / a;
   return __expf(lse - r) * (lp > -0.7f ? expm1f(lp) + (1.f - q) : __expf(lp) - q);
 }
+// A row's entries are rounded to bf16.  dH's row factor is taken as what makes them, times it, what they were (least squares; one target: exactly), as
+// they and not the dense part make most of the row's dH: 60 rows of 2048 with ten targets dH off by 0.0028 of its norm without it, its own rounding
+// being 0.0017; with it 270 rows with eight targets 0.0019.  (Not so dW's, where a dense entry of few rows stands by itself and would carry the shift.)
+__device__ __forceinline__ float rounding_shift(float e, uint16_t rounded) {
+  const float most = wave_max(fabsf(e));
+  if (!(most > 0.f)) return 1.f;
+  const float x = e / most, y = bf2f(rounded) / most, xy = wave_sum(x * y), yy = wave_sum(y * y);
+  return yy > 0.f ? xy / yy : 1.f;
+}
 __device__ __forceinline__ bool is_finite(float x) { return fabsf(x) < INFINITY; }
+// sign and exponent of a number (of the smallest normal one for numbers below it); no number for infinities and no numbers
+__device__ __forceinline__ float power_below(float x) {
+  return fabsf(x) < FLT_MIN ? copysignf(FLT_MIN, x) : __uint_as_float(__float_as_uint(x) & 0xff800000u);
+}
 __global__ void __launch_bounds__(kRowsT)
 k_target_rows(RowsArgs O) {
   __shared__ MergedRows s_rows;
@@ -367,17 +382,10 @@ k_target_rows(RowsArgs O) {
     }
     f = g != 0.f ? (flag ? 1.f : g * a * __expf(r - lse)) : 0.f;
   }
-  // The row's entries are rounded to bf16.  dH's row factor is taken as what makes them, times it, what they were (least squares; one target: exactly), as
-  // they and not the dense part make most of the row's dH: 60 rows of 2048 with ten targets dH off by 0.0028 of its norm without it, its own rounding
-  // being 0.0017; with it 270 rows with eight targets 0.0019.  (Not so dW's, where a dense entry of few rows stands by itself and would carry the shift.)
   const bool put = f != 0.f && !flag && ts != 0.f;
-  const float e = put ? target_entry(z, lse, r, ts, a) : 0.f, most = wave_max(fabsf(e));
+  const float e = put ? target_entry(z, lse, r, ts, a) : 0.f;
   const uint16_t rounded = f2bf(e);
-  float shift = 1.f;
-  if (most > 0.f) {
-    const float x = e / most, y = bf2f(rounded) / most, xy = wave_sum(x * y), yy = wave_sum(y * y);
-    if (yy > 0.f) shift = xy / yy;
-  }
+  const float shift = rounding_shift(e, rounded);
   if (lane == 0) {
     O.R.lse[n] = taught ? lse : 0.f;
     O.R.ent[n] = taught ? s_rows.ent[q] : 0.f;
@@ -400,8 +408,8 @@ k_target_rows(RowsArgs O) {
 
 // ------------------------------------------------------------------ bf16: one block of rows
 // Up to 256 rows the scores leave their logits in float32 instead: 6 bytes a logit more to write and read, of which there are few here, in place of the
-// gather, the references and what they may not serve for.  The operand is then made from the logits, D = bf16(dz / (g a' x)), with f = g a' x as the row factor: x, near
-// 1, is what makes the row's largest target entry, rounded, exact.  It costs the others no second rounding here, so that dW has it as well.  (Few rows are where
+// gather, the references and what they may not serve for.  The operand is then made from the logits, D = bf16(dz / u), u the power of two below the row's factor g a': the copy of
+// H that dW reads is u h, which is exact, so that dW has the roundings of D and of the result.  (Few rows are where
 // it shows: a row of dW is one row's entry times its hidden state.  203 rows of 3584 dW off by 0.0023 of its norm, by the way of more rows 0.0027, for 940 us in place of
 // 909; from a whole block on the logits would cost more than that.)
 constexpr uint16_t kNoEntry = 0xFFFF;                        // a place that does not count
@@ -437,7 +445,7 @@ struct FewArgs {
   Teach A;
   const uint16_t* H;
   RowArrays R;
-  float* x;                // [rows] 1 / x; 0 for a row without a gradient
+  float* y;                // [rows] g a' over its power of two; 0 for a row without a gradient
   uint16_t* entries;       // [rows][k] the targets' entries of the operand
   const float4* partial;
   int tiles_m;
@@ -485,26 +493,27 @@ k_target_few(FewArgs F) {
       out = l = wave_sum(P.t != 0.f ? P.t * (logf(P.t) - (z - lse)) : 0.f);
     }
   }
-  const float e = g != 0.f && P.t != 0.f ? target_entry(z, lse, lse, ts, a) : 0.f, most = wave_max(fabsf(e));
-  const float x = most > 0.f ? most / bf2f(f2bf(most)) : 1.f;
-  const float f = g != 0.f ? g * a * x : 0.f;
-  if (lane < k) F.entries[n * k + lane] = P.t != 0.f ? f2bf(e / x) : kNoEntry;
+  const float f = g != 0.f ? g * a : 0.f, unit = f != 0.f ? power_below(f) : 0.f, y = f != 0.f ? f / unit : 0.f;
+  const float e = f != 0.f && P.t != 0.f ? y * target_entry(z, lse, lse, ts, a) : 0.f;
+  const uint16_t rounded = f2bf(e);
+  const float shift = rounding_shift(e, rounded);
+  if (lane < k) F.entries[n * k + lane] = P.t != 0.f ? rounded : kNoEntry;
   if (lane == 0) {
     F.R.lse[n] = taught ? lse : 0.f;
     F.R.ent[n] = taught ? s_rows.ent[q] : 0.f;
     F.R.l[n] = l;
     F.R.w[n] = w;
     F.R.mass[n] = P.mass;
-    F.R.sc[n] = f;
-    F.x[n] = f != 0.f ? 1.f / x : 0.f;
+    F.R.sc[n] = unit * shift;
+    F.y[n] = y;
     F.R.a[n] = out;                                          // to row_out by who comes next: others clear it now
   }
-  if (F.Hs) copy_row(F.H, row, A.d, f, F.Hs, F.mcp, n);
+  if (F.Hs) copy_row(F.H, row, A.d, unit, F.Hs, F.mcp, n);
 }
 // 32 rows of a block of 256 entries to a workgroup; rows up to the next multiple of 64 are zeros.  203 rows against 152 064 39 us for 191 MB (4.9 TB/s).
 constexpr int kTurnedRows = 32;
 __global__ void __launch_bounds__(256)
-k_target_turn(KeptLogits Z, int V, const float* __restrict__ lse, const float* __restrict__ inv_x, const uint16_t* __restrict__ entries, Targets T,
+k_target_turn(KeptLogits Z, int V, const float* __restrict__ lse, const float* __restrict__ scale, const uint16_t* __restrict__ entries, Targets T,
               const int32_t* __restrict__ rowsel, int64_t n_sel, uint16_t* __restrict__ D, const float* __restrict__ out, float* __restrict__ row_out, int tiles_v, StatArgs S) {
   if (static_cast<int>(blockIdx.x) >= tiles_v) {             // the statistics
     __shared__ double smem[32];
@@ -517,9 +526,9 @@ k_target_turn(KeptLogits Z, int V, const float* __restrict__ lse, const float* _
   }
   const int64_t at = static_cast<int64_t>(blockIdx.x) * kBlkElems;
   const int r = static_cast<int>(blockIdx.y) * kTurnedRows + (threadIdx.x >> 3), c = (threadIdx.x & 7) * 8;
-  const float inv = r < n_sel ? inv_x[r] : 0.f, l2 = r < n_sel ? lse[r] * 1.44269504088896341f : 0.f;
+  const float y = r < n_sel ? scale[r] : 0.f, l2 = r < n_sel ? lse[r] * 1.44269504088896341f : 0.f;
   float4 z[4][2];
-  if (inv != 0.f)
+  if (y != 0.f)
 #pragma unroll
     for (int i = 0; i < 4; ++i)
 #pragma unroll
@@ -527,9 +536,9 @@ k_target_turn(KeptLogits Z, int V, const float* __restrict__ lse, const float* _
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
     uint4 o = make_uint4(0u, 0u, 0u, 0u);
-    if (inv != 0.f) {
+    if (y != 0.f) {
       const int left = V - static_cast<int>(blockIdx.x) * 256 - i * 64 - c;   // entries from V on: 0, whatever lies there
-      auto p = [&](float x, int e) { return e < left ? __builtin_amdgcn_exp2f(fmaf(x, 1.44269504088896341f, -l2)) * inv : 0.f; };
+      auto p = [&](float x, int e) { return e < left ? __builtin_amdgcn_exp2f(fmaf(x, 1.44269504088896341f, -l2)) * y : 0.f; };
       o = make_uint4(pack_bf16x2(p(z[i][0].x, 0), p(z[i][0].y, 1)), pack_bf16x2(p(z[i][0].z, 2), p(z[i][0].w, 3)), pack_bf16x2(p(z[i][1].x, 4), p(z[i][1].y, 5)),
                      pack_bf16x2(p(z[i][1].z, 6), p(z[i][1].w, 7)));
     }
@@ -538,7 +547,7 @@ k_target_turn(KeptLogits Z, int V, const float* __restrict__ lse, const float* _
   __syncthreads();
   for (int i = threadIdx.x; i < kTurnedRows * T.k; i += 256) {
     const int64_t n = static_cast<int64_t>(blockIdx.y) * kTurnedRows + i / T.k;
-    if (n >= n_sel || inv_x[n] == 0.f) continue;
+    if (n >= n_sel || scale[n] == 0.f) continue;
     const int id = T.ids[(rowsel ? rowsel[n] : n) * T.k + i % T.k];
     const uint16_t e = entries[n * T.k + i % T.k];
     if (e != kNoEntry && id >> 8 == static_cast<int>(blockIdx.x)) D[at + n * 256 + (id & 255)] = e;

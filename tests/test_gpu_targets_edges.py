@@ -189,3 +189,20 @@ def test_a_penalty_that_cancels_the_dense_part(n, dtype):
     for x, o in ((dH, r["dH"]), (dW, r["dW"])):
         x = x.double().cpu().numpy()
         assert np.isfinite(x).all() and np.linalg.norm(x - o) <= (1e-2 if dtype == "bf16" else 1e-5) * np.linalg.norm(o)
+
+
+@pytest.mark.parametrize("n,dW_dtype", [(20, "bf16"), (64, "bf16"), (120, "bf16"), (200, "bf16"), (200, "f32")])
+def test_roundings_of_a_head_taught_by_few_rows(n, dW_dtype):
+    """Every target is a token of its own, so that a row of dW is one entry times one hidden state: up to 256 rows it carries the rounding of the entry and, in bf16, that of the result.  Independent
+    roundings add by their squares; one is what the exact dW is off by when it is rounded.  A tenth more is let pass."""
+    d, V, k = 256, 20001, 64
+    H, W, Hd, Wd, rng = arrays(n, n, d, V, "bf16")
+    ids = rng.permutation(V)[:n * k].reshape(n, k)
+    l = rng.normal(size=(n, k)).astype(np.float32) * 0.3          # no target much larger than the others
+    r = orc.distill(H, W, ids, l)
+    kw = {} if dW_dtype == "bf16" else dict(dW=torch.empty(V, d, device="cuda"))
+    _, _, dH, dW = umas.umas_distill_fwd_bwd(Hd, Wd, cuda(ids, np.int32), cuda(l, np.float32), **kw)
+    off = lambda x, o: np.linalg.norm(x.double().cpu().numpy() - o) / np.linalg.norm(o)  # noqa: E731
+    one = lambda o: off(torch.from_numpy(o).bfloat16(), o)  # noqa: E731
+    assert off(dW, r["dW"]) <= 1.1 * one(r["dW"]) * (2 ** 0.5 if dW_dtype == "bf16" else 1)
+    assert off(dH, r["dH"]) <= 1.1 * one(r["dH"]) * 2 ** 0.5
