@@ -206,3 +206,26 @@ def test_roundings_of_a_head_taught_by_few_rows(n, dW_dtype):
     one = lambda o: off(torch.from_numpy(o).bfloat16(), o)  # noqa: E731
     assert off(dW, r["dW"]) <= 1.1 * one(r["dW"]) * (2 ** 0.5 if dW_dtype == "bf16" else 1)
     assert off(dH, r["dH"]) <= 1.1 * one(r["dH"]) * 2 ** 0.5
+
+
+@pytest.mark.parametrize("kind", ["ce", "distill"])
+@pytest.mark.parametrize("n,dtype", [(3, "bf16"), (60, "bf16"), (100, "bf16"), (200, "bf16"), (300, "bf16"), (100, "f32")])
+def test_targets_beside_tokens_masked_by_the_lowest_number(n, dtype, kind):
+    """Tokens that a column of its own masks have no probability and no gradient; the others are what they are without them.  Norm-wise bars as everywhere."""
+    V, d = 1025, 64
+    H, W, _, _, rng = arrays(n + 4, n, d, V, dtype)
+    masked = rng.random(V) < 0.6
+    masked[[0, V - 1]] = False, True
+    open_ = np.flatnonzero(~masked)
+    W[masked], W[:, 0] = 0, 0
+    H[:, 0] = 1
+    ids = rng.choice(open_, n)
+    r = orc.cross_entropy(H, W[open_], np.searchsorted(open_, ids))
+    W[masked, 0] = torch.finfo(torch.bfloat16).min
+    stats, row, dH, dW = teach(kind, cuda(H, np.float32).to(DT[dtype]), cuda(W, np.float32).to(DT[dtype]), ids, None)
+    s = umas.read_target_stats(stats)
+    assert abs(s["loss"][0] - r["loss"]) <= 1e-5 * (1 + r["loss"]) and abs(s["entropy_mean"][0] - r["entropy"].mean()) <= 1e-4 * (1 + r["entropy"].mean())
+    assert not dW[torch.from_numpy(masked).cuda()].any()
+    tol = 1e-2 if dtype == "bf16" else 1e-5
+    for x, o in ((dH.double().cpu().numpy(), r["dH"]), (dW.double().cpu().numpy()[open_], r["dW"])):
+        assert np.isfinite(x).all() and np.linalg.norm(x - o) <= tol * np.linalg.norm(o)
