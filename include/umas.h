@@ -429,7 +429,9 @@ umas_status umas_ready_batch_packed(const umas_streams* streams, int32_t n_model
  *   g_i = w_i / norm;  dz_iv = g_i ((1 + 2 z_coef lse_i) softmax(z_i)_v - 1[v = ids[i]]);  dH = dz W;  dW = dz^T H
  * with norm = norm_rows, or n_sel where that is 0 (rows without a target count in it: the token mean over the selection).
  *   ids        DEVICE int32 [n_rows]; a row whose id is outside [0,V) (-100, say) is ignored: it adds nothing to any sum
- *              but the count of ignored rows and has no gradient, whatever its row of H holds
+ *              but the count of ignored rows and has no gradient, whatever its row of H holds.  Its logits and its share of the
+ *              products are computed all the same: where many rows are ignored, a rowsel of the others saves their time, and
+ *              makes the mean one over the rows that have a target
  *   weight     DEVICE float [n_rows] or NULL (= 1); a weight of 0 takes a row out of loss and gradients the same way
  *   tok_role   DEVICE int32 [n_rows] or NULL with n_roles = 0
  *   z_coef     >= 0, the penalty that keeps logsumexps near 0
@@ -439,6 +441,9 @@ umas_status umas_ready_batch_packed(const umas_streams* streams, int32_t n_model
  *   dW         DEVICE [V, d] of the type dW_type: UMAS_F32, or for a bf16 head UMAS_BF16 (16-byte aligned; float32 sums
  *              rounded once).  accumulate_dW = 0 overwrites, 1 adds: to float32 exactly as the policy update does, to bf16
  *              with a rounding per call.  UMAS_NO_DW with dW = NULL: the head is frozen, the product is left out.
+ * Roundings to bf16 of a bf16 head, besides those of dH and dW: the entries of dz that the products read, and with more than 256
+ * selected rows the copy of H, scaled by row, that dW's reads.  A dW whose rows come from single rows of H is then off by up to
+ * 0.0029 of its norm (0.0024 up to 256 rows), where rounding the exact one is 0.0017; dH by 0.0017 to 0.0021.
  * The bf16 call keeps one bf16 number per (row, vocabulary entry) of a chunk of rows in its workspace, as the policy update
  * does (softmax numerators; the logits in float32 beside them where there are at most 256 selected rows), and runs in as few chunks
  * as the workspace allows: of 256 rows in the smallest size, of up to 65536 in the full one; float32 calls of 32 rows and up.  A dW of
@@ -470,7 +475,7 @@ umas_status umas_cross_entropy_fwd_bwd(const void* H, const void* W, umas_dtype 
  * 1 <= k <= UMAS_MAX_TOP.  Logits of -infinity and those that are not a number are not listed; places left over (they, or
  * V < k) hold token -1 and logit -infinity.  Rows that are not selected get tokens of -1, logits and logsumexp of 0.  H, W,
  * rowsel, n_sel, dtype and their limits as in umas_policy_logprobs.  The workspace bounds of how many rows logits are kept on the
- * way, at least 256; the results do not depend on it. */
+ * way, at least 256; tokens and logits do not depend on it, the logsumexp by no more than the rounding of its float32 sums. */
 size_t umas_top_logits_workspace_bytes_min(int64_t n_sel, int32_t d, int32_t V, int32_t k, umas_dtype dtype);
 size_t umas_top_logits_workspace_bytes(int64_t n_sel, int32_t d, int32_t V, int32_t k, umas_dtype dtype);
 umas_status umas_top_logits(const void* H, const void* W, umas_dtype dtype, int64_t n_rows, int32_t d, int32_t V,
@@ -479,7 +484,9 @@ umas_status umas_top_logits(const void* H, const void* W, umas_dtype dtype, int6
 
 /* Distillation from a teacher's k largest logits and its gradient.  The teacher's distribution over its k places, t_j:
  * with teacher_lse = NULL the softmax of the k logits; else exp(top_logits_j - teacher_lse_i), the teacher's own
- * probabilities, what it gives to other tokens teaching nothing (T_i = sum_j t_j <= 1):
+ * probabilities, what it gives to other tokens teaching nothing (T_i = sum_j t_j <= 1; the row's share in loss and gradient is
+ * then T_i of what it would be renormalised, plus T_i log T_i in kl_i, which can be negative: the optimum is the same, no
+ * probability outside the k places):
  *   kl_i = sum_j t_j (log t_j - log softmax(z_i)_{v_j});  loss = sum_i w_i kl_i / norm
  *   dz_iv = g_i (T_i softmax(z_i)_v - sum_{j: v_j = v} t_j)
  *   top_ids     DEVICE int32 [n_rows, k], 1 <= k <= UMAS_MAX_TOP, as umas_top_logits writes them or any others; places whose token is

@@ -23,7 +23,8 @@ inline bool slices_dh(int64_t n_sel, int64_t chunk_rows, int d) { return dh_tile
 // and 1.6 GiB: 2048 columns 1.019, 1.012, 1.008, 0.994 (151 936 entries are 1.16), 2560 1.025, 1.039, 1.017, 0.976, 0.975, 0.957, 3584
 // 0.931, 0.920, 0.916, 0.940, 0.952, 0.966, 8192 0.981, 0.983, 0.988, 0.938, 0.949, 0.965.  65 to 128 rows, whose dH tiles are half as long: 2048 columns
 // 1.044, 1.031, 0.998, 1.009, 2560 1.052, 1.032, 1.018, 0.975, 1.000, 0.973, 3584 0.983, 0.970, 0.970, 0.954, 0.954, 0.977, 4096 above 1.25 GiB
-// 0.978, 4608 1.009, 8192 1.009 to 1.017, 16 384 1.02; 30 rows of 2048 508 and 517 us, 3072 722 and 731.  More than a block: 300 rows of 2048 876 and
+// 0.978, 4608 1.009, 8192 1.009 to 1.017, 16 384 1.02; 30 rows of 2048 508 and 517 us, 3072 722 and 731.  A dW of bf16 goes by the same line, in bytes of float32: one launch 0 to 7 % slower at 100 to 256 rows of 2560 to 8192 columns, 160 rows of 2048
+// equal.  More than a block: 300 rows of 2048 876 and
 // 922, 725 of 3584 2262 and 2258, 2500 6594 and 8070.
 constexpr int64_t kDwApartBytes = int64_t{1} << 30;
 inline bool dw_apart(int64_t n_sel, int d, int V) {
@@ -63,7 +64,7 @@ inline GradPlan plan_gradients(int64_t n_sel, int64_t rows, int d, int V, size_t
   return GradPlan{plan_dh(tiles_r, tiles_d, tiles_v, room), false};
 }
 
-// dH of a frozen head: no dW fills a last round, so the slices are chosen for it, in microseconds: rounds of pieces on `cus` compute units, a piece its steps of 64 (1.6 each
+// dH of a frozen head: no dW fills a last round, so the slices are chosen for it, in microseconds (costs measured on a head of 1536 columns and 100 279 entries, taken for all): rounds of pieces on `cus` compute units, a piece its steps of 64 (1.6 each
 // of 256 x 256) and what a tile costs besides (twelve steps), and 0.4 for a piece's partial sums: their way to memory and back is a third of it, the rest what they push out of the caches (2900 rows of 1536 in 504
 // pieces instead of 216: the product 829 -> 787 us, the sum 16 -> 29, the next call's scores 808 -> 832).
 inline DhPlan plan_dh_alone(int64_t tiles, int tiles_v, int cus, size_t room) {

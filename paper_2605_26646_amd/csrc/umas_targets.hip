@@ -12,13 +12,14 @@
 //   E[i, v_j] = bf16((a' p - t) / (a' exp(r - lse))) = bf16(exp(lse - r) (p - t / a'))
 // so the sparse part costs k two-byte stores a row and no pass of its own over dH or dW.
 //
-// What bounds it: the products.  16 384 rows of 2048 against 151 936: the scores 7.85 ms (1.30 PFLOP/s), both gradients 14.9 ms (1.36 PFLOP/s), all else 0.13 ms;
-// 4096 rows 2.06 and 3.80 ms and 0.21 (64 targets a row).  Fewer rows are bound by W and dW, which have to be read twice and written: 203 rows of 3584 against
+// What bounds it: the products.  16 384 rows of 2048 against 151 936: the scores 7.82 ms (1.30 PFLOP/s), both gradients 14.9 ms (1.37 PFLOP/s), all else 0.11 ms;
+// 4096 rows 2.02 and 3.81 ms and 0.20 (64 targets a row).  Fewer rows are bound by W and dW, which have to be read twice and written: 203 rows of 3584 against
 // 152 064, 3.3 GB and 1.0 TFLOP of whole blocks: 0.94 ms.
 //
-// Roundings to bf16: an entry of E (relative error up to 2^-9; the sum of exponentials and the logsumexp are float32 and do not see it), the scaled
-// copy of H, and the results.  A row of dW that a single row of H makes carries all three: 270 to 2000 rows dW is off by 0.0024 to 0.0028 of its norm, where
-// rounding the result alone is 0.0017, 4096 rows 0.0024, up to 256 rows (two roundings, see below) 0.0021 to 0.0024.
+// Roundings to bf16: an entry of E (relative error up to 2^-8; the sum of exponentials and the logsumexp are float32 and do not see it), the scaled
+// copy of H, and the results.  A row of dW that a single row of H makes carries all three: dW is off by 0.0024 to 0.0029 of its norm, where
+// rounding the result alone is 0.0017 (one target a row: 300 rows 0.0028, 1500 0.0024, 8192 0.0019; 64 targets: 2000 rows 0.0029, 4096 0.0027 to 0.0029, with 20 targets 0.0024).  Up to
+// 256 rows (two roundings, see below) 0.0022 to 0.0024.  dH, whose factor undoes what its targets' entries lost, 0.0017 (one target) to 0.0021.
 #include <float.h>
 
 #include "umas_f32.h"
@@ -121,8 +122,8 @@ struct OpenArgs {
   int share;               // wavefronts to a row: 1 or 4
 };
 // One wavefront (four) per selected row: the targets' masses, their logits (dot products of float32 sums), the row's reference.  The first workgroup clears
-// the flags and lays out the chunk, others clear what the call defines everywhere.  Bound by the rows of W: 4096 rows with 64 targets of 4 KB each 154 us (7.0 TB/s, a part of it
-// from the caches; a wavefront to a row, whose sixteen turns are one behind the other, 184).  16 384 rows with one target 36 us (a wavefront to a row).
+// the flags and lays out the chunk, others clear what the call defines everywhere.  Bound by the rows of W: 4096 rows with 64 targets of 4 KB each 150 us (7.2 TB/s, a part of it
+// from the caches; a wavefront to a row, whose sixteen turns are one behind the other, 184).  16 384 rows with one target 32 us (a wavefront to a row).
 constexpr int kAtOnce = 4;   // targets whose rows of W are under way together
 __global__ void __launch_bounds__(256)
 k_target_open(OpenArgs O) {
@@ -276,7 +277,7 @@ k_target_tiles_end(const uint16_t* __restrict__ W, const uint16_t* __restrict__ 
 // ------------------------------------------------------------------ bf16: rows
 // Eight rows to a workgroup, a wavefront to each, which asks for what it needs of its row; then all of them merge the rows' parts (a load covers the eight rows of
 // eight parts), and a wavefront goes on with its row: its loss and factor, its k entries of the operand, its scaled copy of H.  Bound by the parts (16 bytes a row and tile) and
-// the copy: 16 384 rows of 2048 against 151 936 60 us (4.8 TB/s), 4096 rows 26 (a workgroup of four wavefronts to four rows 66 and 30), 1111 rows of 1096 14 us, which is latency.
+// the copy: 16 384 rows of 2048 against 151 936 57 us (5.1 TB/s), 4096 rows 24 (a workgroup of four wavefronts to four rows 66 and 30), 1111 rows of 1096 10 us, which is latency.
 constexpr int kRowsT = 512;
 struct MergedRows {
   float lse[8], ent[8], sum[8];
@@ -409,8 +410,8 @@ k_target_rows(RowsArgs O) {
 // ------------------------------------------------------------------ bf16: one block of rows
 // Up to 256 rows the scores leave their logits in float32 instead: 6 bytes a logit more to write and read, of which there are few here, in place of the
 // gather, the references and what they may not serve for.  The operand is then made from the logits, D = bf16(dz / u), u the power of two below the row's factor g a': the copy of
-// H that dW reads is u h, which is exact, so that dW has the roundings of D and of the result.  (Few rows are where
-// it shows: a row of dW is one row's entry times its hidden state.  203 rows of 3584 dW off by 0.0023 of its norm, by the way of more rows 0.0027, for 940 us in place of
+// H that dW reads is u h, which is exact, so that dW has the roundings of D and of the result.  (Few rows are where it shows: a row of dW is one
+// row's entry times its hidden state.  203 rows of 3584 dW off by 0.0022 of its norm, by the way of more rows 0.0027, for 940 us in place of
 // 909; from a whole block on the logits would cost more than that.)
 constexpr uint16_t kNoEntry = 0xFFFF;                        // a place that does not count
 __global__ void __launch_bounds__(Cfg::T)
@@ -439,7 +440,7 @@ struct KeptLogits {
   int64_t stride;
   __device__ __forceinline__ const float* at(int64_t n, int blk, int c) const { return z + (stride ? n * stride + blk * 256 : blk * kBlkElems + n * 256) + c; }
 };
-// The first workgroup lays the block out, `clearing` of them clear what the call defines everywhere, the others do eight rows each.  13 to 15 us for 60 to 256 rows: a
+// The first workgroup lays the block out, `clearing` of them clear what the call defines everywhere, the others do eight rows each.  12 us for 60 to 256 rows: a
 // few dependent reads (rows one after the other in a workgroup of four wavefronts: 22).
 struct FewArgs {
   Teach A;
@@ -510,7 +511,7 @@ k_target_few(FewArgs F) {
   }
   if (F.Hs) copy_row(F.H, row, A.d, unit, F.Hs, F.mcp, n);
 }
-// 32 rows of a block of 256 entries to a workgroup; rows up to the next multiple of 64 are zeros.  203 rows against 152 064 39 us for 191 MB (4.9 TB/s).
+// 32 rows of a block of 256 entries to a workgroup; rows up to the next multiple of 64 are zeros.  203 rows against 152 064 35 us for 191 MB (5.4 TB/s).
 constexpr int kTurnedRows = 32;
 __global__ void __launch_bounds__(256)
 k_target_turn(KeptLogits Z, int V, const float* __restrict__ lse, const float* __restrict__ scale, const uint16_t* __restrict__ entries, Targets T,
@@ -553,7 +554,7 @@ k_target_turn(KeptLogits Z, int V, const float* __restrict__ lse, const float* _
     if (e != kNoEntry && id >> 8 == static_cast<int>(blockIdx.x)) D[at + n * 256 + (id & 255)] = e;
   }
 }
-// Blocks in which some logit lies far above its row's reference: dz is computed once more, its k entries on the way out.  Without any 12 us, in which the
+// Blocks in which some logit lies far above its row's reference: dz is computed once more, its k entries on the way out.  Without any 9 to 20 us, in which the
 // statistics are summed beside.
 struct PutTargets {
   const int32_t *rowsel, *ids;

@@ -9,8 +9,9 @@
 // complement of the token.  A wavefront keeps the 64 largest keys it has seen, one to a lane in falling order, and takes only keys beyond its
 // k-th: those collect in LDS until there are 64, are sorted (21 exchanges) and merged with what is there (7).
 //
-// What bounds it: up to 128 rows reading W (one row of 2048 against 151 936 107 us, 5.8 TB/s; 24 rows of 3584 against 152 064 209 us, 5.2 TB/s; 128 rows of 2048 166 us), then
-// the product (8192 rows of 2048 with 64 places 3.82 ms, 1.33 PFLOP/s, of 3.97; 777 rows of 1544 against 50 001 185 us, whole rounds of tiles of 52 to 58 us, of 205).
+// What bounds it: up to 128 rows reading W (one row of 2048 against 151 936 104 us, 6.0 TB/s; 24 rows of 3584 against 152 064 200 us, 5.5 TB/s; 128 rows of 2048, by tiles that fetch W
+// in pieces of 128 bytes, 160 us, 3.9 TB/s), then the product (8192 rows of 2048 with 64 places 3.72 ms, 1.37 PFLOP/s, of 3.84; 777 rows of 1544 against 50 001 174 us, whole rounds of
+// tiles of 52 us, of 185).
 #include <float.h>
 
 #include "umas_f32.h"
@@ -301,7 +302,7 @@ __device__ __forceinline__ void write_top(const TopOut& O, int64_t row, TopKey l
   O.logits[row * O.k + lane] = logit_of(list);
 }
 // A bound that at least k logits of a row reach: the threads of a workgroup take the maximum over the row's tiles in turn, and the k-th largest of these
-// 256 numbers is it (k at most 64; with random logits 74 groups of thousands reach the 64th).  By itself, for what is left unwritten, 7 us, 4096 rows 14.  `lm`, `ls`: the wavefront's part of the logsumexp.
+// 256 numbers is it (k at most 64; with random logits 74 groups of thousands reach the 64th).  By itself, for what is left unwritten, 5 us for 777 rows, 10 for 4096.  `lm`, `ls`: the wavefront's part of the logsumexp.
 template <int G>
 __device__ __forceinline__ void load_maxima(const float* __restrict__ maxima, int t, float (&x)[G]) {
 #pragma unroll
@@ -353,7 +354,7 @@ k_top_bound(Groups A, int tiles, int k, float* __restrict__ bound) {   // of a r
   if (threadIdx.x == 0) bound[m] = b;
 }
 // A workgroup to a row: the groups that reach its bound are listed, and the wavefronts go through their entries.  The row's logsumexp comes from the tiles'
-// sums on the way.  12 us for one row, a chain of reads and exchanges (through LDS 13); 8192 rows with 64 places 114 us.
+// sums on the way.  9 us for one row, a chain of reads and exchanges (through LDS one more); 8192 rows with 64 places 106 us.
 // `written`: the bound below which k_top_tiles_bound left a group's logits unwritten (NULL: all are there).  The row's own can lie below it, as of few tiles it is one of groups
 // and of many one of tiles, of which the large logits may share one; k logits reach either, so the larger of the two serves and only what was written is read.
 constexpr int kAtOnce = 4;                                   // loads of entries under way
