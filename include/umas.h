@@ -16,6 +16,14 @@
  *   umas_cross_entropy_fwd_bwd, umas_distill_fwd_bwd
  *                              loss and gradients towards given tokens, or towards a teacher's largest logits
  *
+ * and what stands directly in front of a head and behind it:
+ *
+ *   umas_rms_norm, umas_rms_norm_quantized, umas_rms_norm_bwd
+ *                              the norm that makes hidden states, with the residual's addition; an output in 8 bits; its gradients
+ *   umas_sample_logits, umas_sample_tokens
+ *                              the token that a model answers with, under temperature, top-k, min-p and top-p
+ *   umas_clip_gradients        the global norm of a list of gradients, and clipping
+ *
  * Conventions
  *   - THIN metadata (graph, reward scalars) are HOST pointers, caller-owned, read during the
  *     call only (the paper's controller keeps exactly this: role ids, routing ids, reward
@@ -503,6 +511,99 @@ umas_status umas_distill_fwd_bwd(const void* H, const void* W, umas_dtype dtype,
                                  const int32_t* rowsel, int64_t n_sel, const float* weight, const int32_t* tok_role,
                                  int32_t n_roles, int32_t accumulate_dW, int64_t norm_rows, umas_target_stats* stats, float* kl,
                                  void* dH, void* dW, int32_t dW_type, void* workspace, size_t workspace_bytes, void* hip_stream);
+
+/* ---------------------------------------------------------------------------------------------
+ * Around a head.
+ *
+ * Root-mean-square norm of x + residual:
+ *   s = x + residual, rounded to the type of x;  i = 1 / sqrt(mean_j s_j^2 + eps);  y_j = s_j i gain_j
+ *   x, residual  DEVICE [n_rows, d], residual may be NULL (s = x)
+ *   gain         DEVICE [d]
+ *   hidden       DEVICE [n_rows, d]: s, what goes on past the norm; NULL exactly where residual is.  It may be x or residual themselves.
+ *   y            DEVICE [n_rows, d]; may be x
+ *   inv_rms      DEVICE float [n_rows]: i, for the backward pass; may be NULL
+ * All arrays but inv_rms have the type dtype and are 16-byte aligned; 1 <= d <= 16384, a multiple of 8 for bf16.  Sums are float32.
+ *
+ * umas_rms_norm_quantized leaves y in 8 bits instead: q = y / scale in e4m3 (4 bits of exponent, 3 of mantissa, no infinities, largest 448), rounded to
+ * nearest, scale_i = max_j |y_ij| / 448 and 1 for a row of zeros; y is not rounded on the way.
+ *   q            DEVICE uint8 [n_rows, d], 16-byte aligned
+ *   scale        DEVICE float [n_rows]; of a row that holds something that is no number, or an infinity, scale and q are no numbers either
+ *
+ * Backward, a_j = dy_j gain_j:
+ *   dx_j = i (a_j - s_j i^2/d sum_k a_k s_k) + dhidden_j;  dgain_j = sum over rows of dy_j s_j i
+ * dx is the gradient of x and of residual alike.
+ *   dy           DEVICE [n_rows, d]; a row that is 0 throughout adds nothing, whatever the row of hidden holds: its dx is dhidden
+ *   hidden       DEVICE [n_rows, d], inv_rms DEVICE float [n_rows], as umas_rms_norm leaves them (hidden is x where there was no residual)
+ *   dhidden      DEVICE [n_rows, d] or NULL (0): the gradient that reaches s past the norm
+ *   dx           DEVICE [n_rows, d]; may be dy or dhidden
+ *   dgain        DEVICE float [d]; accumulate_dgain = 0 overwrites, 1 adds */
+umas_status umas_rms_norm(const void* x, const void* residual, const void* gain, umas_dtype dtype, int64_t n_rows, int32_t d, float eps,
+                          void* hidden, void* y, float* inv_rms, void* hip_stream);
+umas_status umas_rms_norm_quantized(const void* x, const void* residual, const void* gain, umas_dtype dtype, int64_t n_rows, int32_t d,
+                                    float eps, void* hidden, uint8_t* q, float* scale, float* inv_rms, void* hip_stream);
+size_t umas_rms_norm_workspace_bytes(int64_t n_rows, int32_t d);
+umas_status umas_rms_norm_bwd(const void* dy, const void* hidden, const void* gain, const float* inv_rms, const void* dhidden,
+                              umas_dtype dtype, int64_t n_rows, int32_t d, int32_t accumulate_dgain, void* dx, float* dgain,
+                              void* workspace, size_t workspace_bytes, void* hip_stream);
+
+/* The draw of a token for every row of logits z:
+ *   w_v = exp((z_v - max z) / temperature).  Tokens are taken in falling order of z, equal ones in rising order; kept are
+ *   the first top_k (0, or V and more: all); of these those with w_v >= min_p; of these the shortest run from the front whose mass
+ *   (sum of w) reaches top_p of the mass of them all (1: all).  The token is the first, in rising order, at which the running mass of
+ *   what is kept passes u times the kept mass.
+ * Logits of -infinity and those that are no number are never drawn and have no mass.  Masses are float64 or exact: tokens whose w is below 2^-39 to 2^-52
+ * (2^-44 at 151 936 tokens) count as 0 where a filter is on.  The same inputs give the same token, whatever the other rows and the workspace are.
+ *   logits       DEVICE [n_rows, V] of the type dtype, row i at logits + i * row_stride, row_stride >= V, aligned to its type
+ *   u            DEVICE float [n_rows], uniform on [0,1); below 0 or no number counts as 0, from 1 on the last kept token is drawn
+ *   ids          DEVICE int32 [n_rows]; -1 for a row that has nothing to draw from
+ *   logp         DEVICE float [n_rows] or NULL: log softmax(z)[id], what umas_policy_logprobs gives; 0 where id is -1
+ *   logq         DEVICE float [n_rows] or NULL: log-probability of the token under what it was drawn from; 0 where id is -1
+ * umas_sample_tokens takes the logits from a head, z = W h_i (float accumulate), for the selected rows; ids, logp and logq of other rows are -1, 0
+ * and 0.  H, W, rowsel, n_sel, dtype and their limits as in umas_policy_logprobs; u and the settings of a row lie at its number in [0, n_rows).
+ * The workspace bounds of how many rows logits are kept on the way, at least 256.  V <= UMAS_MAX_SAMPLE_V. */
+typedef struct umas_sampling {
+  double temperature;            /* >= 0; 0: the largest logit, of equal ones the lowest token (top_k, top_p and min_p change nothing then) */
+  double top_p;                  /* in [0,1] */
+  double min_p;                  /* in [0,1] */
+  int32_t top_k;                 /* >= 0 */
+  const float* temperature_of;   /* DEVICE [n_rows], one for each row in place of the number above, or NULL; a temperature that is not above 0 counts as 0 */
+  const float* top_p_of;         /* ... beyond 1 or no number: 1, below 0: 0 */
+  const float* min_p_of;         /* ... beyond 1: 1, below 0 or no number: 0 */
+  const int32_t* top_k_of;       /* ... below 0: 0 */
+} umas_sampling;
+enum { UMAS_MAX_SAMPLE_V = 1 << 22 };
+size_t umas_sample_logits_workspace_bytes(int64_t n_rows, int32_t V);
+umas_status umas_sample_logits(const void* logits, umas_dtype dtype, int64_t n_rows, int32_t V, int64_t row_stride, const float* u,
+                               const umas_sampling* sampling, int32_t* ids, float* logp, float* logq, void* workspace,
+                               size_t workspace_bytes, void* hip_stream);
+size_t umas_sample_tokens_workspace_bytes_min(int64_t n_sel, int32_t d, int32_t V, umas_dtype dtype);
+size_t umas_sample_tokens_workspace_bytes(int64_t n_sel, int32_t d, int32_t V, umas_dtype dtype);
+umas_status umas_sample_tokens(const void* H, const void* W, umas_dtype dtype, int64_t n_rows, int32_t d, int32_t V,
+                               const int32_t* rowsel, int64_t n_sel, const float* u, const umas_sampling* sampling, int32_t* ids,
+                               float* logp, float* logq, void* workspace, size_t workspace_bytes, void* hip_stream);
+
+/* The global norm of a list of gradients, and clipping:
+ *   N = sqrt(sum over all arrays of g^2);  c = max_norm / N where N > max_norm, else 1;  out = c g
+ * Squares are summed in float64.  A norm that is no finite number scales nothing (c = 1): n_not_finite says that the step is to be left out.
+ *   gradients  HOST [n], read inside the call: arrays of any size, each of its own type, aligned to that; out is grad (in place; with c = 1 nothing is
+ *              written) or another array of the same type and size.  No output may overlap anything else of the list (UMAS_EINVAL).
+ *   max_norm   > 0; infinity: the norm alone
+ *   stats      DEVICE umas_clip_stats
+ * The call may be recorded into a graph: the list travels with the launches. */
+typedef struct umas_gradient {
+  const void* grad;
+  void* out;
+  int64_t n;
+  int32_t dtype;                 /* umas_dtype */
+} umas_gradient;
+typedef struct umas_clip_stats {
+  float norm;
+  float scale;                   /* c */
+  int64_t n_not_finite;          /* numbers that are infinite or none */
+} umas_clip_stats;
+size_t umas_clip_workspace_bytes(int32_t n);
+umas_status umas_clip_gradients(const umas_gradient* gradients, int32_t n, double max_norm, umas_clip_stats* stats, void* workspace,
+                                size_t workspace_bytes, void* hip_stream);
 
 /* Kernel timing aid for benchmarks (not part of the method).  While enabled, every kernel launch
  * of the library is followed by a HIP event on its stream and the time between consecutive events

@@ -690,3 +690,71 @@ def cross_entropy(H, W, ids, rowsel=None, weight=None, z_coef=0.0, norm_rows=0):
 def distill(H, W, top_ids, top_logits_, teacher_lse=None, rowsel=None, weight=None, norm_rows=0):
     """teach with the teacher's masses; row is the divergence."""
     return teach(H, W, top_ids, teacher_masses(top_ids, top_logits_, teacher_lse, W.shape[0]), rowsel, weight, 0.0, norm_rows)
+
+
+# ------------------------------------------------------------------ around a head
+def rms_norm(s, gain, eps):
+    """(s / root mean square of each row, times gain; 1 / that root), of the sum as it is stored."""
+    s, gain = np.asarray(s, np.float64), np.asarray(gain, np.float64)
+    inv = np.array([1.0 / np.sqrt(sum(v * v for v in row) / len(row) + eps) for row in s])
+    return s * inv[:, None] * gain, inv
+
+
+def rms_norm_backward(dy, s, gain, inv, dhidden=None):
+    """Gradients by the sum (and so by both of its parts) and by gain; rows of dy that are 0 throughout add nothing."""
+    dy, s, gain, inv = (np.asarray(a, np.float64) for a in (dy, s, gain, inv))
+    dx, dgain = np.zeros(dy.shape), np.zeros(dy.shape[1])
+    for i in range(len(dy)):
+        if (dy[i] != 0).any():
+            a = dy[i] * gain
+            dx[i] = inv[i] * (a - s[i] * (inv[i] ** 2 * (a @ s[i]) / len(a)))
+            dgain += dy[i] * s[i] * inv[i]
+        if dhidden is not None:
+            dx[i] += np.asarray(dhidden[i], np.float64)
+    return dx, dgain
+
+
+def e4m3_values():
+    """The finite numbers of 8 bits with 4 of exponent (bias 7) and 3 of mantissa, by their bits 0 .. 126."""
+    out = []
+    for b in range(127):
+        e, m = b >> 3, b & 7
+        out.append(m * 2.0 ** -9 if e == 0 else (8 + m) * 2.0 ** (e - 10))
+    return np.array(out)
+
+
+def sample(z, u, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0):
+    """One row: (token, log softmax(z)[token], log-probability under what it was drawn from); (-1, 0, 0) where there is nothing to draw from."""
+    z = np.where(np.isnan(z), -np.inf, np.asarray(z, np.float64))
+    order = [v for v in sorted(range(len(z)), key=lambda v: (-z[v], v)) if z[v] > -np.inf]
+    if not order:
+        return -1, 0.0, 0.0
+    top = z[order[0]]
+
+    def away(v, t):                                            # exp of the difference to the largest; of infinities only equal ones count
+        return 1.0 if z[v] == top else np.exp((z[v] - top) / t)
+
+    softmax = np.array([away(v, 1.0) for v in order])
+    if not temperature > 0:
+        return order[0], -np.log(softmax.sum()), 0.0
+    kept = order[:top_k] if 0 < top_k < len(order) else order
+    w = np.array([away(v, temperature) for v in kept])
+    n = int((w >= min(max(min_p, 0.0), 1.0)).sum()) if min_p > 0 else len(w)
+    w = w[:n]
+    if top_p < 1:
+        ahead = np.concatenate([[0.0], np.cumsum(w)[:-1]])
+        n = max(1, int((ahead < top_p * w.sum()).sum()))
+        w = w[:n]
+    by_token = sorted(range(n), key=lambda j: kept[j])
+    run, target = np.cumsum([w[j] for j in by_token]), u * w.sum()
+    beyond = [j for j, r in zip(by_token, run) if r > target and w[j] > 0]
+    j = beyond[0] if beyond else max((j for j in by_token if w[j] > 0), key=lambda j: kept[j])
+    return kept[j], np.log(softmax[order.index(kept[j])] / softmax.sum()), np.log(w[j] / w.sum())
+
+
+def clip(gradients, max_norm):
+    """(norm of all arrays together, factor, count of numbers that are not finite, scaled arrays)."""
+    bad = sum(int((~np.isfinite(g)).sum()) for g in gradients)
+    norm = np.sqrt(sum(float((np.asarray(g, np.float64) ** 2).sum()) for g in gradients))
+    c = max_norm / norm if np.isfinite(norm) and norm > max_norm else 1.0
+    return norm, c, bad, [np.asarray(g, np.float64) * c for g in gradients]

@@ -41,6 +41,15 @@ _STREAM_FIELDS = ["model_tok_off", "perm", "tok_turn", "tok_role", "tok_mask", "
                   "model_rowsel_off", "turn_scalar", "turn_step", "tok_flags"]
 
 
+class _Sampling(C.Structure):
+    _fields_ = [("temperature", C.c_double), ("top_p", C.c_double), ("min_p", C.c_double), ("top_k", C.c_int32),
+                ("temperature_of", C.c_void_p), ("top_p_of", C.c_void_p), ("min_p_of", C.c_void_p), ("top_k_of", C.c_void_p)]
+
+
+class _Gradient(C.Structure):
+    _fields_ = [("grad", C.c_void_p), ("out", C.c_void_p), ("n", C.c_int64), ("dtype", C.c_int32)]
+
+
 class _Streams(C.Structure):
     _fields_ = [(name, C.c_void_p) for name in _STREAM_FIELDS]
 
@@ -154,6 +163,28 @@ def load_library():
     lib.umas_top_logits.restype = C.c_int
     lib.umas_top_logits.argtypes = [C.c_void_p, C.c_void_p, C.c_int, C.c_int64, C.c_int32, C.c_int32, C.c_void_p, C.c_int64, C.c_int32, C.c_void_p,
                                     C.c_void_p, C.c_void_p, C.c_void_p, C.c_size_t, C.c_void_p]
+    for name in ("umas_rms_norm", "umas_rms_norm_quantized"):
+        f = getattr(lib, name)
+        scale = [C.c_void_p] if name.endswith("quantized") else []
+        f.restype, f.argtypes = C.c_int, [C.c_void_p, C.c_void_p, C.c_void_p, C.c_int, C.c_int64, C.c_int32, C.c_float, C.c_void_p, C.c_void_p, *scale,
+                                          C.c_void_p, C.c_void_p]
+    lib.umas_rms_norm_workspace_bytes.restype, lib.umas_rms_norm_workspace_bytes.argtypes = C.c_size_t, [C.c_int64, C.c_int32]
+    lib.umas_rms_norm_bwd.restype = C.c_int
+    lib.umas_rms_norm_bwd.argtypes = [C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_int, C.c_int64, C.c_int32, C.c_int32, C.c_void_p,
+                                      C.c_void_p, C.c_void_p, C.c_size_t, C.c_void_p]
+    lib.umas_sample_logits_workspace_bytes.restype, lib.umas_sample_logits_workspace_bytes.argtypes = C.c_size_t, [C.c_int64, C.c_int32]
+    lib.umas_sample_logits.restype = C.c_int
+    lib.umas_sample_logits.argtypes = [C.c_void_p, C.c_int, C.c_int64, C.c_int32, C.c_int64, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p,
+                                       C.c_void_p, C.c_size_t, C.c_void_p]
+    for which in ("_min", ""):
+        f = getattr(lib, f"umas_sample_tokens_workspace_bytes{which}")
+        f.restype, f.argtypes = C.c_size_t, [C.c_int64, C.c_int32, C.c_int32, C.c_int]
+    lib.umas_sample_tokens.restype = C.c_int
+    lib.umas_sample_tokens.argtypes = [C.c_void_p, C.c_void_p, C.c_int, C.c_int64, C.c_int32, C.c_int32, C.c_void_p, C.c_int64, C.c_void_p, C.c_void_p,
+                                       C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_size_t, C.c_void_p]
+    lib.umas_clip_workspace_bytes.restype, lib.umas_clip_workspace_bytes.argtypes = C.c_size_t, [C.c_int32]
+    lib.umas_clip_gradients.restype = C.c_int
+    lib.umas_clip_gradients.argtypes = [C.c_void_p, C.c_int32, C.c_double, C.c_void_p, C.c_void_p, C.c_size_t, C.c_void_p]
     lib.umas_values.restype = C.c_int
     lib.umas_values.argtypes = [C.c_void_p, C.c_void_p, C.c_float, C.c_int, C.c_int64, C.c_int32, C.c_void_p, C.c_int64,
                                 C.c_void_p, C.c_void_p]
@@ -317,6 +348,48 @@ def umas_distill_fwd_bwd(H, W, top_ids, top_logits, teacher_lse=None, rowsel=Non
 def read_target_stats(stats: torch.Tensor) -> np.ndarray:
     """Copy the device umas_target_stats array to a numpy structured array (synchronises)."""
     return stats.cpu().numpy().view(TARGET_STATS_DTYPE)
+
+
+def umas_rms_norm(x, gain, residual=None, *, eps=1e-6, hidden=None, y=None, inv_rms=None):
+    """Returns (y, hidden, inv_rms): the norm of x + residual times gain, the sum itself (x where there is no residual) and 1 / its root mean
+    square.  x [n, d], gain [d]; hidden may be x or residual, y may be x."""
+    return _done(_native().rms_norm(x, gain, residual, eps, hidden, y, inv_rms, _stream()))
+
+
+def umas_rms_norm_quantized(x, gain, residual=None, *, eps=1e-6, hidden=None, q=None, scale=None, inv_rms=None):
+    """Returns (q float8_e4m3fn [n, d], scale float32 [n], hidden, inv_rms): as umas_rms_norm, q * scale in place of y."""
+    return _done(_native().rms_norm_quantized(x, gain, residual, eps, hidden, q, scale, inv_rms, _stream()))
+
+
+def umas_rms_norm_bwd(dy, hidden, gain, inv_rms, dhidden=None, *, accumulate_dgain=False, dx=None, dgain=None, workspace=None):
+    """Returns (dx, dgain float32 [d]); hidden and inv_rms as umas_rms_norm left them, dhidden the gradient that reaches hidden past the norm."""
+    return _done(_native().rms_norm_bwd(dy, hidden, gain, inv_rms, dhidden, accumulate_dgain, dx, dgain, workspace, _stream()))
+
+
+def umas_sample_logits(logits, u, *, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0, ids=None, logp=None, logq=None, workspace=None):
+    """A token for every row of logits [n, V] (rows may lie apart), by one uniform number a row: (ids int32 [n], log-prob of the softmax, log-prob
+    under what was drawn from).  Each setting is a number, or a tensor with one for each row (top_k int32, the others float32)."""
+    return _done(_native().sample_logits(logits, u, temperature, top_k, top_p, min_p, ids, logp, logq, workspace, _stream()))
+
+
+def umas_sample_tokens(H, W, u, rowsel=None, *, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0, ids=None, logp=None, logq=None, workspace=None):
+    """umas_sample_logits of H W^T for the selected rows; the others get -1, 0 and 0."""
+    _check_rows(rowsel, H)
+    return _done(_native().sample_tokens(H, W, u, rowsel, temperature, top_k, top_p, min_p, ids, logp, logq, workspace, _stream()))
+
+
+CLIP_STATS_DTYPE = np.dtype([("norm", "<f4"), ("scale", "<f4"), ("n_not_finite", "<i8")])
+
+
+def umas_clip_gradients(gradients, max_norm, *, out=None, stats=None, workspace=None):
+    """Scales the list of gradients to a global norm of at most max_norm, in place or into the tensors of `out`: (stats, list of what was
+    written).  Does not wait: read_clip_stats(stats) has the norm before, the factor and the count of numbers that are not finite."""
+    return _done(_native().clip_gradients(gradients, max_norm, out, stats, workspace, _stream()))
+
+
+def read_clip_stats(stats: torch.Tensor) -> np.ndarray:
+    """Copy the device umas_clip_stats to a numpy structured array (synchronises)."""
+    return stats.cpu().numpy().view(CLIP_STATS_DTYPE)
 
 
 VALUE_STATS_DTYPE = np.dtype([("loss", "<f4"), ("clip_frac", "<f4"), ("value_mean", "<f4"), ("reserved", "<f4"),

@@ -15,6 +15,7 @@
 
 #include <algorithm>
 #include <initializer_list>
+#include <vector>
 
 #include "../../include/umas.h"
 
@@ -563,6 +564,200 @@ PyObject* distill(PyObject* const* a) {
   return T.results();
 }
 
+// ------------------------------------------------------------------ around a head
+// An array that a call reads or writes: its type, length, layout and device are looked at before any address is taken.
+const at::Tensor& whole(const at::Tensor& t, at::ScalarType type, int64_t n, const at::Device& dev, const char* name) {
+  in_reach(t, dev, name);
+  if (t.scalar_type() == type && t.numel() == n && t.is_contiguous()) return t;
+  PyErr_Format(PyExc_ValueError, "%s must be contiguous, %s and hold %lld values", name, c10::toString(type), static_cast<long long>(n));
+  throw Failed();
+}
+const at::Tensor& whole(PyObject* o, at::ScalarType type, int64_t n, const at::Device& dev, const char* name) { return whole(tensor(o), type, n, dev, name); }
+void* whole_or_null(PyObject* o, at::ScalarType type, int64_t n, const at::Device& dev, const char* name) {
+  return o == Py_None ? nullptr : whole(o, type, n, dev, name).data_ptr();
+}
+void on_a_gpu(const at::Tensor& t, const char* name) {
+  if (t.is_cuda()) return;
+  PyErr_Format(PyExc_ValueError, "%s and what goes with it must be on a GPU", name);
+  throw Failed();
+}
+void same_address(const char* a, const at::Tensor& x, const char* b, const at::Tensor& y) {   // two outputs of a call
+  if (x.data_ptr() != y.data_ptr() || x.numel() == 0) return;
+  PyErr_Format(PyExc_ValueError, "%s and %s must be different arrays", a, b);
+  throw Failed();
+}
+// x, gain, residual, eps, hidden, then the output (y, or q and scale), inv_rms, stream
+template <bool QUANT>
+PyObject* norm(PyObject* const* a) {
+  const Rows x(a[0]);
+  const at::Device dev = x.t.device();
+  const at::ScalarType type = x.t.scalar_type(), out_type = QUANT ? at::kFloat8_e4m3fn : type;
+  const at::Tensor& gain = whole(a[1], type, x.d, dev, "gain");
+  whole(x.t, type, x.n * x.d, dev, "x");
+  const bool sum = a[2] != Py_None;
+  void* const residual = whole_or_null(a[2], type, x.n * x.d, dev, "residual");
+  const float eps = real(a[3]);
+  if (!sum && a[4] != Py_None) {
+    PyErr_SetString(PyExc_ValueError, "hidden is x itself where there is no residual");
+    throw Failed();
+  }
+  PyObject* const* const o = a + 5;                        // the output
+  const Output hidden(a[4], [&] { return sum ? at::empty_like(x.t) : at::Tensor(); });
+  const Output y(o[0], [&] { return fresh({x.n, x.d}, out_type, dev); });
+  const Output scale(QUANT ? o[1] : Py_None, [&] { return QUANT ? fresh({x.n}, at::kFloat, dev) : at::Tensor(); });
+  const Output inv_rms(o[QUANT ? 2 : 1], [&] { return fresh({x.n}, at::kFloat, dev); });
+  if (sum) whole(hidden.t, type, x.n * x.d, dev, "hidden");
+  whole(y.t, out_type, x.n * x.d, dev, QUANT ? "q" : "y");
+  whole(inv_rms.t, at::kFloat, x.n, dev, "inv_rms");
+  if (sum) same_address("hidden", hidden.t, "the output", y.t);
+  if constexpr (QUANT) whole(scale.t, at::kFloat, x.n, dev, "scale");
+  on_a_gpu(x.t, "x");
+  void* const st = stream_of(o[QUANT ? 3 : 2]);
+  const umas_dtype dt = static_cast<umas_dtype>(x.dt);
+  void* const h = sum ? hidden.t.data_ptr() : nullptr;
+  if constexpr (QUANT) {
+    UMAS_CALL(umas_rms_norm_quantized(x.t.data_ptr(), residual, gain.data_ptr(), dt, x.n, x.d, eps, h, static_cast<uint8_t*>(y.t.data_ptr()), ptr<float>(scale.t),
+                                      ptr<float>(inv_rms.t), st));
+  } else {
+    UMAS_CALL(umas_rms_norm(x.t.data_ptr(), residual, gain.data_ptr(), dt, x.n, x.d, eps, h, y.t.data_ptr(), ptr<float>(inv_rms.t), st));
+  }
+  PyObject* same = nullptr;
+  if (!sum) Py_INCREF(same = a[0]);
+  if constexpr (QUANT) return pack({y.object(), scale.object(), sum ? hidden.object() : same, inv_rms.object()});
+  else return pack({y.object(), sum ? hidden.object() : same, inv_rms.object()});
+}
+PyObject* rms_norm(PyObject* const* a) { return norm<false>(a); }
+PyObject* rms_norm_quantized(PyObject* const* a) { return norm<true>(a); }
+
+PyObject* rms_norm_bwd(PyObject* const* a) {              // dy, hidden, gain, inv_rms, dhidden, accumulate_dgain, dx, dgain, workspace, stream
+  const Rows dy(a[0]);
+  const at::Device dev = dy.t.device();
+  const at::ScalarType type = dy.t.scalar_type();
+  const int64_t all = dy.n * dy.d;
+  whole(dy.t, type, all, dev, "dy");
+  const at::Tensor &hidden = whole(a[1], type, all, dev, "hidden"), &gain = whole(a[2], type, dy.d, dev, "gain"), &inv_rms = whole(a[3], at::kFloat, dy.n, dev, "inv_rms");
+  void* const dhidden = whole_or_null(a[4], type, all, dev, "dhidden");
+  const int32_t accumulate = truth(a[5]);
+  if (accumulate && a[7] == Py_None) {
+    PyErr_SetString(PyExc_ValueError, "accumulate_dgain needs the dgain to add to");
+    throw Failed();
+  }
+  const Output dx(a[6], [&] { return at::empty_like(dy.t); });
+  const Output dgain(a[7], [&] { return fresh({dy.d}, at::kFloat, dev); });
+  const Output ws(a[8], [&] { return workspace(umas_rms_norm_workspace_bytes(dy.n, dy.d), dev); });
+  whole(dx.t, type, all, dev, "dx");
+  whole(dgain.t, at::kFloat, dy.d, dev, "dgain");
+  in_reach(ws.t, dev, "workspace");
+  on_a_gpu(dy.t, "dy");
+  void* const st = stream_of(a[9]);
+  UMAS_CALL(umas_rms_norm_bwd(dy.t.data_ptr(), hidden.data_ptr(), gain.data_ptr(), ptr<float>(inv_rms), dhidden, static_cast<umas_dtype>(dy.dt), dy.n, dy.d, accumulate,
+                              dx.t.data_ptr(), ptr<float>(dgain.t), ws.t.data_ptr(), ws.t.nbytes(), st));
+  return pack({dx.object(), dgain.object()});
+}
+
+// temperature, top_k, top_p, min_p: each a number or a tensor with one for each of n rows
+umas_sampling sampling_of(PyObject* const* a, int64_t n, const at::Device& dev) {
+  umas_sampling s{1.0, 1.0, 0.0, 0, nullptr, nullptr, nullptr, nullptr};
+  auto number = [&](PyObject* o, double* one, const float** each, const char* name) {
+    if (THPVariable_Check(o)) {
+      *each = ptr<const float>(whole(o, at::kFloat, n, dev, name));
+      return;
+    }
+    *one = PyFloat_AsDouble(o);
+    if (*one == -1.0 && PyErr_Occurred()) throw Failed();
+  };
+  number(a[0], &s.temperature, &s.temperature_of, "temperature");
+  number(a[2], &s.top_p, &s.top_p_of, "top_p");
+  number(a[3], &s.min_p, &s.min_p_of, "min_p");
+  if (THPVariable_Check(a[1])) s.top_k_of = ptr<const int32_t>(whole(a[1], at::kInt, n, dev, "top_k"));
+  else s.top_k = static_cast<int32_t>(std::max<int64_t>(std::min<int64_t>(as_int(a[1]), INT32_MAX), INT32_MIN));
+  return s;
+}
+struct DrawnOutputs {                                     // ids, logp, logq
+  const Output ids, logp, logq;
+  DrawnOutputs(PyObject* const* a, int64_t n, const at::Device& dev)
+      : ids(a[0], [&] { return fresh({n}, at::kInt, dev); }), logp(a[1], [&] { return fresh({n}, at::kFloat, dev); }), logq(a[2], [&] { return fresh({n}, at::kFloat, dev); }) {
+    whole(ids.t, at::kInt, n, dev, "ids");
+    whole(logp.t, at::kFloat, n, dev, "logp");
+    whole(logq.t, at::kFloat, n, dev, "logq");
+    same_address("logp", logp.t, "logq", logq.t);
+  }
+};
+PyObject* sample_logits(PyObject* const* a) {             // logits, u, temperature, top_k, top_p, min_p, ids, logp, logq, workspace, stream
+  const Rows z(a[0]);
+  const at::Device dev = z.t.device();
+  if (z.n > 0 && z.d > 0 && ((z.d > 1 && z.t.stride(1) != 1) || (z.n > 1 && z.t.stride(0) < z.d))) {
+    PyErr_SetString(PyExc_ValueError, "logits [n, V]: the numbers of a row must lie next to each other, the rows one behind the other");
+    throw Failed();
+  }
+  const at::Tensor& u = whole(a[1], at::kFloat, z.n, dev, "u");
+  const umas_sampling s = sampling_of(a + 2, z.n, dev);
+  const DrawnOutputs out(a + 6, z.n, dev);
+  const Output ws(a[9], [&] { return workspace(umas_sample_logits_workspace_bytes(z.n, z.d), dev); });
+  in_reach(ws.t, dev, "workspace");
+  on_a_gpu(z.t, "logits");
+  void* const st = stream_of(a[10]);
+  UMAS_CALL(umas_sample_logits(z.t.data_ptr(), static_cast<umas_dtype>(z.dt), z.n, z.d, z.n > 1 ? z.t.stride(0) : z.d, ptr<float>(u), &s, ptr<int32_t>(out.ids.t),
+                               ptr<float>(out.logp.t), ptr<float>(out.logq.t), ws.t.data_ptr(), ws.t.nbytes(), st));
+  return pack({out.ids.object(), out.logp.object(), out.logq.object()});
+}
+PyObject* sample_tokens(PyObject* const* a) {             // H, W, u, rowsel, temperature, top_k, top_p, min_p, ids, logp, logq, workspace, stream
+  const Rows H(a[0]);
+  const at::Tensor& W = tensor(a[1]);
+  const at::Device dev = H.t.device();
+  same_head(H, W);
+  const int32_t V = static_cast<int32_t>(W.size(0));
+  whole_selection(a[3], dev);
+  Selection sel(a[3], H.n);
+  const at::Tensor& u = whole(a[2], at::kFloat, H.n, dev, "u");
+  const umas_sampling s = sampling_of(a + 4, H.n, dev);
+  const DrawnOutputs out(a + 8, H.n, dev);
+  const umas_dtype dt = static_cast<umas_dtype>(H.dt);
+  const Output ws(a[11], [&] { return workspace(umas_sample_tokens_workspace_bytes(sel.n, H.d, V, dt), dev); });
+  in_reach(ws.t, dev, "workspace");
+  on_a_gpu(H.t, "H");
+  sel.point(ws.t.data_ptr(), a[3]);
+  void* const st = stream_of(a[12]);
+  UMAS_CALL(umas_sample_tokens(H.t.data_ptr(), W.data_ptr(), dt, H.n, H.d, V, sel.p, sel.n, ptr<float>(u), &s, ptr<int32_t>(out.ids.t), ptr<float>(out.logp.t),
+                               ptr<float>(out.logq.t), ws.t.data_ptr(), ws.t.nbytes(), st));
+  return pack({out.ids.object(), out.logp.object(), out.logq.object()});
+}
+
+PyObject* clip_gradients(PyObject* const* a) {            // gradients, max_norm, out, stats, workspace, stream
+  const Ref list(PySequence_Fast(a[0], "gradients must be a list of tensors"));
+  const Ref to(a[2] == Py_None ? (Py_INCREF(list.o), list.o) : PySequence_Fast(a[2], "out must be a list of tensors"));
+  const Py_ssize_t n = PySequence_Fast_GET_SIZE(list.o);
+  if (PySequence_Fast_GET_SIZE(to.o) != n) {
+    PyErr_SetString(PyExc_ValueError, "out must hold a tensor for every gradient");
+    throw Failed();
+  }
+  if (n == 0) {
+    PyErr_SetString(PyExc_ValueError, "gradients must hold a tensor");
+    throw Failed();
+  }
+  const at::Device dev = tensor(PySequence_Fast_GET_ITEM(list.o, 0)).device();
+  std::vector<umas_gradient> g(static_cast<size_t>(n));
+  for (Py_ssize_t i = 0; i < n; ++i) {
+    PyObject* const o = PySequence_Fast_GET_ITEM(list.o, i);
+    const int dt = dtype_code(o);
+    const at::Tensor &x = tensor(o), &y = tensor(PySequence_Fast_GET_ITEM(to.o, i));
+    whole(x, x.scalar_type(), x.numel(), dev, "a gradient");
+    whole(y, x.scalar_type(), x.numel(), dev, "an output of a gradient");
+    g[static_cast<size_t>(i)] = umas_gradient{x.data_ptr(), y.data_ptr(), x.numel(), dt};
+  }
+  const double max_norm = PyFloat_AsDouble(a[1]);
+  if (max_norm == -1.0 && PyErr_Occurred()) throw Failed();
+  const Output stats(a[3], [&] { return fresh({static_cast<int64_t>(sizeof(umas_clip_stats))}, at::kByte, dev); });
+  const Output ws(a[4], [&] { return workspace(umas_clip_workspace_bytes(static_cast<int32_t>(std::min<Py_ssize_t>(n, INT32_MAX))), dev); });
+  whole(stats.t, at::kByte, static_cast<int64_t>(sizeof(umas_clip_stats)), dev, "stats");
+  in_reach(ws.t, dev, "workspace");
+  on_a_gpu(tensor(PySequence_Fast_GET_ITEM(list.o, 0)), "gradients");
+  void* const st = stream_of(a[5]);
+  UMAS_CALL(umas_clip_gradients(g.data(), static_cast<int32_t>(n), max_norm, ptr<umas_clip_stats>(stats.t), ws.t.data_ptr(), ws.t.nbytes(), st));
+  PyObject* const written = PySequence_List(to.o);
+  return pack({stats.object(), written});
+}
+
 PyObject* values(PyObject* const* a) {                    // H, w, bias, rowsel, value, stream
   const Rows H(a[0]);
   const at::Tensor& w = tensor(a[1]);
@@ -693,7 +888,9 @@ PyObject* entry(PyObject*, PyObject* const* args, Py_ssize_t n) {
 #define ENTRY(name, f, n) {name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)(void)>(&entry<f, n>)), METH_FASTCALL, nullptr}
 PyMethodDef g_methods[] = {ENTRY("assign", assign, 19), ENTRY("advantages", advantages, 7), ENTRY("policy_logprobs", policy_logprobs, 7),
                            ENTRY("policy_logprobs_static", policy_logprobs_static, 8), ENTRY("ppo_loss", ppo_loss, 21), ENTRY("top_logits", top_logits, 9),
-                           ENTRY("cross_entropy", cross_entropy, 17), ENTRY("distill", distill, 18), ENTRY("values", values, 6),
+                           ENTRY("cross_entropy", cross_entropy, 17), ENTRY("distill", distill, 18), ENTRY("rms_norm", rms_norm, 8),
+                           ENTRY("rms_norm_quantized", rms_norm_quantized, 9), ENTRY("rms_norm_bwd", rms_norm_bwd, 10), ENTRY("sample_logits", sample_logits, 11),
+                           ENTRY("sample_tokens", sample_tokens, 13), ENTRY("clip_gradients", clip_gradients, 6), ENTRY("values", values, 6),
                            ENTRY("value_loss", value_loss, 19), ENTRY("kl_rewards", kl_rewards, 7), ENTRY("whiten", whiten, 9),
                            ENTRY("ready_batch", ready_batch, 7), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef g_module = {PyModuleDef_HEAD_INIT, "_umas_torch", nullptr, -1, g_methods, nullptr, nullptr, nullptr, nullptr};
