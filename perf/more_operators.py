@@ -216,7 +216,7 @@ def _run_own(s):
     if kind == "norm_bwd":
         dx, dgain = umas.umas_rms_norm_bwd(s["dy"], s["hidden"], s["gain"], s["inv_rms"], s["dhidden"])
         return {"dx": dx, "dgain": dgain}
-    stats = umas.umas_clip_gradients(s["grads"], s["max_norm"], out=s["out"])
+    stats, _ = umas.umas_clip_gradients(s["grads"], s["max_norm"], out=s["out"])
     return _clip_result(s, stats.view(torch.float32)[0])
 
 
