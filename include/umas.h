@@ -571,7 +571,7 @@ typedef struct umas_sampling {
   const float* min_p_of;         /* ... beyond 1: 1, below 0 or no number: 0 */
   const int32_t* top_k_of;       /* ... below 0: 0 */
 } umas_sampling;
-enum { UMAS_MAX_SAMPLE_V = 1 << 22 };
+enum { UMAS_MAX_SAMPLE_V = 1 << 20 };
 size_t umas_sample_logits_workspace_bytes(int64_t n_rows, int32_t V);
 umas_status umas_sample_logits(const void* logits, umas_dtype dtype, int64_t n_rows, int32_t V, int64_t row_stride, const float* u,
                                const umas_sampling* sampling, int32_t* ids, float* logp, float* logq, void* workspace,

@@ -276,19 +276,28 @@ k_norm_back(NormBackArgs A) {
     }
   }
 }
-// dg from the workgroups' shares: a workgroup to 64 columns.
-__global__ void __launch_bounds__(kNT)
+// dg from the workgroups' shares: a workgroup to 64 columns, its wavefronts every sixteenth share, eight loads of a thread under way (with four wavefronts and
+// one load after the other the 1024 shares of 2048 columns took 95 us).
+constexpr int kGainT = 1024;
+__global__ void __launch_bounds__(kGainT)
 k_norm_gain(const float* __restrict__ part, int parts, int d, int accumulate, float* __restrict__ dgain) {
-  __shared__ float s[kNT];
+  constexpr int kWaves = kGainT / kWave, kAtOnce = 8;
+  __shared__ float s[kGainT];
   const int col = blockIdx.x * kWave + (threadIdx.x & 63), w = threadIdx.x >> 6;
   float v = 0.f;
   if (col < d)
-    for (int p = w; p < parts; p += kNT / kWave) v += part[static_cast<int64_t>(p) * d + col];
+    for (int p = w; p < parts; p += kWaves * kAtOnce) {
+      float x[kAtOnce];
+#pragma unroll
+      for (int i = 0; i < kAtOnce; ++i) x[i] = p + i * kWaves < parts ? part[static_cast<int64_t>(p + i * kWaves) * d + col] : 0.f;
+#pragma unroll
+      for (int i = 0; i < kAtOnce; ++i) v += x[i];
+    }
   s[threadIdx.x] = v;
   __syncthreads();
   if (w != 0 || col >= d) return;
 #pragma unroll
-  for (int k = 1; k < kNT / kWave; ++k) v += s[k * kWave + threadIdx.x];
+  for (int k = 1; k < kWaves; ++k) v += s[k * kWave + threadIdx.x];
   dgain[col] = accumulate ? dgain[col] + v : v;
 }
 
@@ -395,7 +404,7 @@ extern "C" umas_status umas_rms_norm_bwd(const void* dy, const void* hidden, con
     else run(float{});
     UMAS_LAUNCHED("k_norm_back");
   }
-  hipLaunchKernelGGL(k_norm_gain, dim3(cdiv(d, kWave)), dim3(kNT), 0, st, static_cast<const float*>(workspace), parts, d, accumulate_dgain, dgain);
+  hipLaunchKernelGGL(k_norm_gain, dim3(cdiv(d, kWave)), dim3(kGainT), 0, st, static_cast<const float*>(workspace), parts, d, accumulate_dgain, dgain);
   UMAS_LAUNCHED("k_norm_gain");
   return UMAS_OK;
 }

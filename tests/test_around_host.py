@@ -33,7 +33,7 @@ def test_queries(lib):
         assert lib.umas_rms_norm_workspace_bytes(n, d) == 0
     assert 0 < lib.umas_sample_logits_workspace_bytes(1, 1) < lib.umas_sample_logits_workspace_bytes(64, 151936)
     assert lib.umas_sample_logits_workspace_bytes(5000, 3001) == lib.umas_sample_logits_workspace_bytes(1 << 40, 3001)
-    for n, V in ((-1, 64), (4, 0), (4, (1 << 22) + 1)):
+    for n, V in ((-1, 64), (4, 0), (4, (1 << 20) + 1)):
         assert lib.umas_sample_logits_workspace_bytes(n, V) == 0
         for w in ("_min", ""):
             assert getattr(lib, "umas_sample_tokens_workspace_bytes" + w)(n, 64, V, BF16) == 0
@@ -101,7 +101,7 @@ def call_tokens(lib, settings=None, **kw):
 
 @pytest.mark.parametrize("call", [call_logits, call_tokens])
 @pytest.mark.parametrize("kw,code,needle", [
-    (dict(dtype=7), -3, "dtype"), (dict(n=-1), -1, "negative"), (dict(V=0), -2, "positive"), (dict(V=(1 << 22) + 1, stride=1 << 23), -2, "exceeds"), (dict(u=None), -1, "u "),
+    (dict(dtype=7), -3, "dtype"), (dict(n=-1), -1, "negative"), (dict(V=0), -2, "positive"), (dict(V=(1 << 20) + 1, stride=1 << 21), -2, "exceeds"), (dict(u=None), -1, "u "),
     (dict(ids=None), -1, "ids"), (dict(sampling=None), -1, "sampling"), (dict(ws=None), -4, "workspace"), (dict(ws=264), -4, "256-byte"), (dict(ws_bytes=64), -4, "hold"),
     (dict(settings=dict(temperature=-0.1)), -1, "temperature"), (dict(settings=dict(temperature=math.nan)), -1, "temperature"), (dict(settings=dict(top_p=1.1)), -1, "top_p"),
     (dict(settings=dict(top_p=-0.1)), -1, "top_p"), (dict(settings=dict(top_p=math.nan)), -1, "top_p"), (dict(settings=dict(min_p=1.1)), -1, "min_p"),
