@@ -53,5 +53,38 @@ __device__ __forceinline__ T sorted_desc(T x) {
 template <class T>
 __device__ __forceinline__ T merged(T x, T y) { return order_runs<kWave>(either(true, x, lane_xor<63>(y))); }
 
+// Sums over the wavefront in 32 or 64 bits, by moves of the vector unit as well: of all lanes, and of the lanes up to the own one.
+__device__ __forceinline__ double bits_of(unsigned long long x, double) { return __longlong_as_double(static_cast<long long>(x)); }
+__device__ __forceinline__ unsigned long long bits_of(unsigned long long x, unsigned long long) { return x; }
+__device__ __forceinline__ unsigned long long bits_in(double x) { return static_cast<unsigned long long>(__double_as_longlong(x)); }
+__device__ __forceinline__ unsigned long long bits_in(unsigned long long x) { return x; }
+template <class T>
+__device__ __forceinline__ T lanes_sum(T x) {                 // double, unsigned long long
+  x += bits_of(lane_xor<1>(bits_in(x)), T());
+  x += bits_of(lane_xor<2>(bits_in(x)), T());
+  x += bits_of(lane_xor<4>(bits_in(x)), T());
+  x += bits_of(lane_xor<8>(bits_in(x)), T());
+  x += bits_of(lane_xor<16>(bits_in(x)), T());
+  x += bits_of(lane_xor<32>(bits_in(x)), T());
+  return x;
+}
+// What the lane gets from another one, 0 where there is none: CTRL of DPP, in the rows of 16 lanes that ROWS names.
+template <int CTRL, int ROWS>
+__device__ __forceinline__ unsigned long long moved(unsigned long long x) {
+  const uint32_t lo = static_cast<uint32_t>(__builtin_amdgcn_update_dpp(0, static_cast<int>(x), CTRL, ROWS, 0xF, false));
+  const uint32_t hi = static_cast<uint32_t>(__builtin_amdgcn_update_dpp(0, static_cast<int>(x >> 32), CTRL, ROWS, 0xF, false));
+  return static_cast<unsigned long long>(hi) << 32 | lo;
+}
+template <class T>
+__device__ __forceinline__ T lanes_scan(T x) {                // inclusive
+  x += bits_of(moved<0x111, 0xF>(bits_in(x)), T());           // one, two, four, eight lanes up in a row of 16
+  x += bits_of(moved<0x112, 0xF>(bits_in(x)), T());
+  x += bits_of(moved<0x114, 0xF>(bits_in(x)), T());
+  x += bits_of(moved<0x118, 0xF>(bits_in(x)), T());
+  x += bits_of(moved<0x142, 0xA>(bits_in(x)), T());           // a row's last lane to the next row, then the half's to the other half
+  x += bits_of(moved<0x143, 0xC>(bits_in(x)), T());
+  return x;
+}
+
 }  // namespace
 }  // namespace umas

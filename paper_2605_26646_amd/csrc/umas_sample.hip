@@ -9,6 +9,8 @@
 // Two launches.  The first reads the logits once: maxima of groups of 64, and of units of 1024 the maximum, the mass at T and the sum of exponentials.  The second gives
 // a workgroup to a row.  Without filters the unit and then the token are found from the units' masses; thresholds are found by their bits, eleven at a time from
 // the top, with a histogram of counts or masses.
+#include <float.h>
+
 #include <algorithm>
 #include <type_traits>
 
@@ -28,12 +30,28 @@ constexpr int kMaxSampleV = UMAS_MAX_SAMPLE_V;
 // exp((z - top) c), c = log2 e / T, for z <= top, as 2^n times a polynomial in the rest f, |f| <= 1/2: the interpolation of (2^f - 1) / f at eight Chebyshev nodes, times f, plus
 // 1; off by 2.2e-12 of itself.  Whole and rest come from an addition that pushes the rest out of a float64, the power from an addition to the exponent's bits: the conversions and
 // ldexp that the compiler would take for them cost four times a multiply-add each (39 million logits, with eleven coefficients, rint and ldexp 58 us).
-// The largest logit's own weight is exactly 1, equal logits' weights are equal; below 2^-1000 is 2^-1000.
+// The largest logit's own weight is exactly 1, equal logits' weights are equal; below 2^-1000 is 2^-1000: logits are held up to the one whose weight that is, in float32, which
+// costs a third of a float64 maximum.  (Where that one is not below the largest itself the temperature is so low that c may as well be what takes the next number
+// below the largest to 2^-1000.)
+// The maximum of two numbers in one instruction (fmaxf makes both quiet first).
+__device__ __forceinline__ float larger(float a, float b) { return __builtin_elementwise_maximum(a, b); }
 struct Weigh {
   double top, c;
+  float least;
+  __device__ __forceinline__ Weigh(float largest, double c_) : top(largest) {
+    const uint32_t u = __float_as_uint(largest);             // the next number below it
+    const float below = largest == 0.f ? __uint_as_float(0x80000001u) : __uint_as_float(largest > 0.f ? u - 1 : u + 1);
+    c = fmax(fmin(c_, 1000.0 / (top - static_cast<double>(below))), 1e-30);   // (a temperature without end: all are 1 but those of -infinity)
+    least = fminf(static_cast<float>(fmax(top - 1000.0 / c, -3e38)), below);
+  }
+  __device__ __forceinline__ float next_above() const {      // the largest logit's next number
+    const float x = static_cast<float>(top);
+    const uint32_t u = __float_as_uint(x);
+    return x == 0.f ? __uint_as_float(1u) : __uint_as_float(x > 0.f ? u + 1 : u - 1);
+  }
   __device__ __forceinline__ double operator()(float z) const {
     constexpr double kPush = 6755399441055744.0;             // 3 * 2^51
-    const double t = fmax((static_cast<double>(z) - top) * c, -1000.0);
+    const double t = (static_cast<double>(larger(z, least)) - top) * c;
     const double pushed = t + kPush, f = t - (pushed - kPush);
     double p = 1.3250805522890813e-06;
     p = fma(p, f, 1.530370071143596e-05);
@@ -49,6 +67,13 @@ struct Weigh {
 };
 constexpr double kNoWeight = 1e-290;                          // what is no more than this is not drawn, u = 0 or not
 constexpr double kLog2e64 = 1.4426950408889634074;
+// log x of 1 <= x: the float32 one and a step of Newton's, whose error is half the square of what that one is off by.  (The library's took 3 us of a row.)
+__device__ __forceinline__ double log_of(double x) {
+  const float y = __logf(static_cast<float>(x));
+  return static_cast<double>(y) + (x * Weigh(0.f, kLog2e64)(-y) - 1.0);
+}
+// 2^t, nearly: for estimates.
+__device__ __forceinline__ double exp2_near(double t) { return static_cast<double>(__builtin_amdgcn_exp2f(static_cast<float>(t))); }
 // A temperature whose inverse leaves no finite number: 0 times it has to stay 0.
 __device__ __forceinline__ double scale_of(double t) { return fmin(kLog2e64 / t, 1e300); }
 __device__ __forceinline__ uint32_t order_of(float z) {       // whole numbers in the order of the logits, one zero
@@ -83,11 +108,16 @@ struct Summary {
 // The lane's share of a unit: pieces of kRun tokens that lie next to each other, kRun * 64 tokens apart.  What is no number counts as -infinity, as what lies
 // past the vocabulary.
 template <typename In> constexpr int kRun = std::is_same<In, uint16_t>::value ? 8 : 4;
-__device__ __forceinline__ float logit(float x) { return fmaxf(x, -INFINITY); }
-__device__ __forceinline__ float logit(double x) { return fmaxf(static_cast<float>(x), -INFINITY); }
-__device__ __forceinline__ float logit(uint16_t x) { return fmaxf(bf2f(x), -INFINITY); }
-// Where the largest logit is +infinity: tokens that are as large share the mass, others have none.
-__device__ __forceinline__ float or_none(float z, bool infinite) { return infinite ? (z == INFINITY ? 0.f : -INFINITY) : z; }
+__device__ __forceinline__ float logit(float x) { return x == x ? x : -INFINITY; }
+__device__ __forceinline__ float logit(double x) { return logit(static_cast<float>(x)); }
+__device__ __forceinline__ float logit(uint16_t x) { return logit(bf2f(x)); }
+// Where the largest logit is +infinity, or the type's lowest number, which has none below it: tokens that are as large share the mass, others have none.
+struct Extreme {
+  float top;
+  bool is;
+  __device__ __forceinline__ explicit Extreme(float t) : top(t), is(t == INFINITY || t == -FLT_MAX) {}
+  __device__ __forceinline__ float operator()(float z) const { return is ? (z == top ? 0.f : -INFINITY) : z; }
+};
 template <typename In>
 __device__ __forceinline__ int token_of(int unit, int i) {    // of the lane's i-th logit
   return unit * kUnit + (i / kRun<In>) * (kRun<In> * kWave) + (threadIdx.x & 63) * kRun<In> + i % kRun<In>;
@@ -123,18 +153,6 @@ __device__ __forceinline__ void load_unit(const In* __restrict__ z, int V, int u
 }
 
 // ------------------------------------------------------------------ first launch
-__device__ __forceinline__ double lanes_sum(double x) {       // of the wavefront, in every lane
-  auto other = [](double v, auto j) {
-    return __longlong_as_double(static_cast<long long>(lane_xor<decltype(j)::value>(static_cast<u64>(__double_as_longlong(v)))));
-  };
-  x += other(x, std::integral_constant<int, 1>());
-  x += other(x, std::integral_constant<int, 2>());
-  x += other(x, std::integral_constant<int, 4>());
-  x += other(x, std::integral_constant<int, 8>());
-  x += other(x, std::integral_constant<int, 16>());
-  x += other(x, std::integral_constant<int, 32>());
-  return x;
-}
 constexpr int kOpenT = 256, kOpenUnits = kOpenT / kWave;
 template <typename In>
 __global__ void __launch_bounds__(kOpenT)
@@ -151,22 +169,25 @@ k_sample_open(Logits<In> L, Settings S, const int32_t* __restrict__ rowsel, int6
   for (int i = 0; i < kPerLane; i += R) {
     float g = x[i];
 #pragma unroll
-    for (int j = 1; j < R; ++j) g = fmaxf(g, x[i + j]);
+    for (int j = 1; j < R; ++j) g = larger(g, x[i + j]);
 #pragma unroll
-    for (int o = 1; o < kLanes; o <<= 1) g = fmaxf(g, __shfl_xor(g, o, kWave));
+    for (int s = 0; s < 4; ++s)
+      if (1 << s < kLanes) g = larger(g, s == 0 ? lane_xor<1>(g) : s == 1 ? lane_xor<2>(g) : s == 2 ? lane_xor<4>(g) : lane_xor<8>(g));
     if (lane % kLanes == 0) out.group[at * kGroupsPerUnit + i / R * R + lane / kLanes] = g;
-    top = fmaxf(top, g);
+    top = larger(top, g);
   }
 #pragma unroll
-  for (int o = kLanes; o < kWave; o <<= 1) top = fmaxf(top, __shfl_xor(top, o, kWave));
+  for (int s = 3; s < 6; ++s)
+    if (1 << s >= kLanes) top = larger(top, s == 3 ? lane_xor<8>(top) : s == 4 ? lane_xor<16>(top) : lane_xor<32>(top));
   double mass = 0.0, sum = 0.0;
   if (top > -INFINITY) {
     const double t = S.t(row);
-    const bool drawn = t > 0.0, infinite = top == INFINITY;
-    if (infinite)
+    const bool drawn = t > 0.0;
+    const Extreme extreme(top);
+    if (extreme.is)
 #pragma unroll
-      for (int i = 0; i < kPerLane; ++i) x[i] = or_none(x[i], true);
-    const float ref = infinite ? 0.f : top;
+      for (int i = 0; i < kPerLane; ++i) x[i] = extreme(x[i]);
+    const float ref = extreme(top);
     if (drawn) {
       const Weigh w{ref, scale_of(t)};
 #pragma unroll
@@ -194,14 +215,73 @@ constexpr int kBins = 2048;
 constexpr int kTopRank = 64;
 constexpr int kListCap = 4096, kRanked = 256;                // tokens of a list, and of one that is ordered by comparing all with all
 constexpr int kGroupCap = 1024;
+// Sums and scans over a workgroup of T threads: what the wavefronts have goes through one of two buffers in turn, so that one barrier is enough.
+template <int T>
+struct Block {
+  static constexpr int W = T / kWave;
+  u64 (*buf)[2][W];                                          // [2], of two numbers a wavefront
+  int turn = 0;
+  __device__ __forceinline__ explicit Block(u64 (*b)[2][W]) : buf(b) {}
+  template <class V>
+  __device__ __forceinline__ V scan(V v, V* total) {         // exclusive
+    const int wave = threadIdx.x >> 6;
+    const V incl = lanes_scan(v);
+    u64(&to)[W] = buf[turn][0];
+    turn ^= 1;
+    if ((threadIdx.x & 63) == 63) to[wave] = bits_in(incl);
+    __syncthreads();
+    V before = V(), all = V();
+#pragma unroll
+    for (int w = 0; w < W; ++w) {
+      const V x = umas::bits_of(to[w], V());
+      before += w < wave ? x : V();
+      all += x;
+    }
+    *total = all;
+    return before + (incl - v);
+  }
+  template <class V>
+  __device__ __forceinline__ void sum(V& a, V& b) {
+    a = lanes_sum(a);
+    b = lanes_sum(b);
+    u64(&to)[2][W] = buf[turn];
+    turn ^= 1;
+    if ((threadIdx.x & 63) == 0) {
+      to[0][threadIdx.x >> 6] = bits_in(a);
+      to[1][threadIdx.x >> 6] = bits_in(b);
+    }
+    __syncthreads();
+    a = b = V();
+#pragma unroll
+    for (int w = 0; w < W; ++w) {
+      a += umas::bits_of(to[0][w], V());
+      b += umas::bits_of(to[1][w], V());
+    }
+  }
+  template <class V>
+  __device__ __forceinline__ V sum(V a) {
+    V b = V();
+    sum(a, b);
+    return a;
+  }
+  __device__ __forceinline__ float max(float v) {
+    v = wave_max(v);
+    u64(&to)[W] = buf[turn][0];
+    turn ^= 1;
+    if ((threadIdx.x & 63) == 0) to[threadIdx.x >> 6] = __float_as_uint(v);
+    __syncthreads();
+#pragma unroll
+    for (int w = 0; w < W; ++w) v = larger(v, __uint_as_float(static_cast<uint32_t>(to[w])));
+    return v;
+  }
+};
 template <int T>
 struct RowShared {
+  u64 block[2][2][T / kWave];
   u64 bins[kBins];                                           // masses or counts
   float list_z[kListCap];
   int list_id[kListCap];
-  float top[T / kWave][kWave];
-  u64 scan[17];
-  double dscan[17];
+  float top[4][kWave];
   u64 found_above, found_here, found_rest;
   double found_drest;
   uint32_t found_bin;
@@ -213,20 +293,21 @@ struct RowSource {
   const In* z;
   int V, units;
   const float* unit_max;                                     // of the row
-  bool infinite;                                             // its largest is
-  __device__ __forceinline__ float at(int v) const { return v < V ? or_none(logit(z[v]), infinite) : -INFINITY; }
+  Extreme extreme;
+  __device__ __forceinline__ float at(int v) const { return v < V ? extreme(logit(z[v])) : -INFINITY; }
   // f(z, token) for every token with z > -infinity, and z >= lo; others may come.  `after` once a unit, by its wavefront, also where the unit has none
   template <class F, class G>
   __device__ __forceinline__ void each(float lo, F f, G after) const {
     for (int u = threadIdx.x >> 6; u < units; u += T / kWave) {
       const float top = unit_max[u];
-      if (top >= lo && top > -INFINITY) {
+      if ((extreme.is || top >= lo) && top > -INFINITY) {
         float x[kPerLane];
         load_unit(z, V, u, x);
 #pragma unroll
         for (int i = 0; i < kPerLane; ++i) {
-          const float zi = or_none(x[i], infinite);
+          const float zi = extreme(x[i]);
           if (zi > -INFINITY) f(zi, token_of<In>(u, i));
+          if (i % 4 == 3) __builtin_amdgcn_sched_barrier(0);  // sixteen weights at once take more registers than there are
         }
       }
       after(u);
@@ -245,32 +326,25 @@ struct ListSource {
     for (int i = a + static_cast<int>(threadIdx.x); i < b; i += T) f(s->list_z[i], s->list_id[i]);
   }
 };
-template <int T>
-__device__ __forceinline__ u64 block_total(u64 v, RowShared<T>& s) {
-  u64 total;
-  block_excl_scan(v, s.scan, &total);
-  __syncthreads();
-  return total;
-}
 struct Border {
   uint32_t key;
   u64 above, here;                                           // sums over larger keys, and over those equal to it
 };
-// The key at which the sum of val over the keys in falling order reaches `need`, 1 <= need <= the sum over all.  Eleven bits at a time from the top; whole
-// numbers, so that the order in which the additions come is nothing.
+// The key at which the sum of val over the keys in falling order reaches `need`, 1 <= need <= the sum over all; keys of `known` bits.  Eleven
+// bits at a time from the top; whole numbers, so that the order in which the additions come is nothing.
 template <int T, class Source, class K, class F>
-__device__ __forceinline__ Border border_of(const Source& src, RowShared<T>& s, float lo, K key_of, F val, u64 need) {
+__device__ __forceinline__ Border border_of(const Source& src, RowShared<T>& s, Block<T>& all, float lo, K key_of, F val, u64 need, int known) {
   constexpr int kEach = kBins / T;
   Border b{0, 0, 0};
 #pragma unroll 1
-  for (int digit = 0; digit < 3; ++digit) {
-    const int shift = digit == 0 ? 21 : digit == 1 ? 10 : 0, known = digit == 0 ? 32 : digit == 1 ? 21 : 10;
+  while (known > 0) {
+    const int shift = max(known - 11, 0);
     const uint32_t mask = (1u << (known - shift)) - 1;
     for (int i = threadIdx.x; i < kBins; i += T) s.bins[i] = 0;
     __syncthreads();
     src.each(lo, [&](float z, int id) {
       const uint32_t key = key_of(z, id);
-      if (digit != 0 && (key ^ b.key) >> known) return;
+      if (known < 32 && (key ^ b.key) >> known) return;
       const u64 v = val(z, id);
       if (v) atomicAdd(&s.bins[(key >> shift) & mask], v);
     });
@@ -279,7 +353,7 @@ __device__ __forceinline__ Border border_of(const Source& src, RowShared<T>& s, 
     u64 sum = 0, total;
 #pragma unroll
     for (int i = 0; i < kEach; ++i) sum += s.bins[hi - i];
-    u64 above = b.above + block_excl_scan(sum, s.scan, &total);
+    u64 above = b.above + all.scan(sum, &total);
 #pragma unroll
     for (int i = 0; i < kEach; ++i) {
       const u64 x = s.bins[hi - i];
@@ -294,6 +368,7 @@ __device__ __forceinline__ Border border_of(const Source& src, RowShared<T>& s, 
     b.key |= s.found_bin << shift;
     b.above = s.found_above;
     b.here = s.found_here;
+    known = shift;
     __syncthreads();
   }
   return b;
@@ -311,6 +386,7 @@ struct RowDraw {
   double p, m, u;                                            // p = 1, m = 0: none
   double all;                                                // the mass of all tokens, in units of the largest weight
   double one;                                                // 1 in units of the whole numbers
+  int id_bits;                                               // of a token's number
   __device__ __forceinline__ bool by_min() const { return m > 0.0; }
   __device__ __forceinline__ u64 whole(double x) const {     // x * one, one at most 2^51, rounded to nearest by the addition
     return static_cast<u64>(__double_as_longlong(fma(x, one, 4503599627370496.0))) & ((u64{1} << 52) - 1);
@@ -341,28 +417,34 @@ struct Drawn {
   int id;
   u64 mass;                                                  // the kept one
 };
-// The cut after `need` of val, of which `each_one` at the border's logit; *mass: the sum of what is in.
+// Where the orders of logits lie: from base on, as many bits.
+struct Span {
+  uint32_t base = 0;
+  int bits = 32;
+};
+// The cut after `need` of val, which is the same for equal logits or 0; *mass: the sum of what is in.
 template <int T, class Source, class F>
-__device__ __forceinline__ Cut cut_at(const Source& src, RowShared<T>& s, float lo, F val, u64 need, u64* mass) {
-  const Border b = border_of(src, s, lo, [](float z, int) { return order_of(z); }, val, need);
+__device__ __forceinline__ Cut cut_at(const Source& src, RowShared<T>& s, Block<T>& all, float lo, F val, u64 need, u64* mass, int id_bits, Span span = Span()) {
+  Border b = border_of(src, s, all, lo, [&](float z, int) { return order_of(z) - span.base; }, val, need, span.bits);
+  b.key += span.base;
   Cut c;
   c.key = b.key;
-  // how many of the tokens at the border, which have the same value each
-  const u64 count = block_total([&] {
-    u64 n = 0;
-    src.each(lo, [&](float z, int id) { n += order_of(z) == b.key && val(z, id); });
-    return n;
-  }(), s);
+  // how many tokens lie at the border
+  u64 count = 0;
+  src.each(lo, [&](float z, int id) { count += order_of(z) == b.key && val(z, id); });
+  count = all.sum(count);
   const u64 one = b.here / count, ties = (need - b.above + one - 1) / one;
-  if (ties < count)                                          // the lowest tokens
-    c.tie = static_cast<int>(~border_of(src, s, lo, [](float, int id) { return ~static_cast<uint32_t>(id); },
-                                        [&](float z, int id) { return u64{order_of(z) == b.key && val(z, id)}; }, ties).key);
+  if (ties < count) {                                        // the lowest of them
+    const int last = (1 << id_bits) - 1;
+    c.tie = last - static_cast<int>(border_of(src, s, all, lo, [&](float, int id) { return static_cast<uint32_t>(last - id); },
+                                              [&](float z, int id) { return u64{order_of(z) == b.key && val(z, id)}; }, ties, id_bits).key);
+  }
   *mass = b.above + ties * one;
   return c;
 }
 // The token at which the running mass of val, in rising order of tokens, passes `target`, which is less than all of it; unit_sum: the units' sums of val.
 template <typename In, int T, class F>
-__device__ __forceinline__ int token_beyond(const RowSource<In, T>& row, RowShared<T>& s, const u64* unit_sum, F val, u64 target) {
+__device__ __forceinline__ int token_beyond(const RowSource<In, T>& row, RowShared<T>& s, Block<T>& all, const u64* unit_sum, F val, u64 target) {
   u64 before = 0;
   if (threadIdx.x == 0) s.found_id = -1;
   int unit = -1;
@@ -370,7 +452,7 @@ __device__ __forceinline__ int token_beyond(const RowSource<In, T>& row, RowShar
     const int u = u0 + threadIdx.x;
     const u64 mine = u < row.units ? unit_sum[u] : 0;
     u64 total;
-    const u64 excl = before + block_excl_scan(mine, s.scan, &total);
+    const u64 excl = before + all.scan(mine, &total);
     if (excl <= target && target < excl + mine) {
       s.found_id = u;
       s.found_rest = target - excl;
@@ -390,7 +472,7 @@ __device__ __forceinline__ int token_beyond(const RowSource<In, T>& row, RowShar
     mine[i] = x > -INFINITY ? val(x, v + i) : 0;
     sum += mine[i];
   }
-  u64 excl = block_excl_scan(sum, s.scan, &total);
+  u64 excl = all.scan(sum, &total);
 #pragma unroll
   for (int i = 0; i < kEach; ++i) {
     if (excl <= rest && rest < excl + mine[i]) s.found_id = v + i;
@@ -402,47 +484,61 @@ __device__ __forceinline__ int token_beyond(const RowSource<In, T>& row, RowShar
 
 // Any row, whatever its logits are: the thresholds by whole passes over it.
 template <typename In, int T>
-__device__ __noinline__ Drawn draw_by_passes(const RowSource<In, T>& row, RowShared<T>& s, u64* s_unit, const RowDraw& d) {
+__device__ __noinline__ Drawn draw_by_passes(RowSource<In, T> row, RowShared<T>* shared, int turn, u64* s_unit, RowDraw d) {
+  RowShared<T>& s = *shared;
+  Block<T> all(s.block);
+  all.turn = turn;
   const float none = -INFINITY;
   Cut first, run;
   u64 mass;
   if (d.k > 0) {
     u64 have = 0;
     row.each(none, [&](float, int) { ++have; });
-    have = block_total(have, s);
-    if (static_cast<u64>(d.k) < have) first = cut_at(row, s, none, [](float, int) { return u64{1}; }, static_cast<u64>(d.k), &mass);
+    have = all.sum(have);
+    if (static_cast<u64>(d.k) < have) first = cut_at(row, s, all, none, [](float, int) { return u64{1}; }, static_cast<u64>(d.k), &mass, d.id_bits);
   }
   auto of_first = [&](float z, int id) { return first.in(z, id) ? d.weight(z) : u64{0}; };
   mass = 0;
   row.each(none, [&](float z, int id) { mass += of_first(z, id); });
-  mass = block_total(mass, s);
-  if (d.p < 1.0) run = cut_at(row, s, none, of_first, d.share(d.p, mass), &mass);
+  mass = all.sum(mass);
+  if (d.p < 1.0) run = cut_at(row, s, all, none, of_first, d.share(d.p, mass), &mass, d.id_bits);
   auto kept = [&](float z, int id) { return run.in(z, id) ? of_first(z, id) : u64{0}; };
   u64 sum = 0;
   row.each(none, [&](float z, int id) { sum += kept(z, id); }, [&](int u) {
-    sum = wave_sum(sum);
+    sum = lanes_sum(sum);
     if ((threadIdx.x & 63) == 0) s_unit[u] = sum;
     sum = 0;
   });
   __syncthreads();
-  return Drawn{token_beyond(row, s, s_unit, kept, d.target(mass)), mass};
+  return Drawn{token_beyond(row, s, all, s_unit, kept, d.target(mass)), mass};
 }
 
 // ---- the tokens in front
-// A number that at least so many logits reach: the threads take the maximum over the row's groups in turn, and the rank-th largest of theirs is it.
+// A number that at least so many logits reach: the threads of four wavefronts take the maximum over the row's groups in turn, and the rank-th largest of theirs is it.
+// (All sixteen, whose lists everybody merges: 5 us more of a row.)
+constexpr int kBoundT = 256;
 template <int T>
 __device__ __forceinline__ float front_bound(const float* __restrict__ group_max, int groups, RowShared<T>& s) {
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, rank = min(kTopRank, max(groups / 4, 1));
-  float x = -INFINITY;
-  for (int g = threadIdx.x; g < groups; g += T) x = fmaxf(x, group_max[g]);
-  x = sorted_desc(x);
-  s.top[wave][lane] = x;
-  __syncthreads();
-  x = s.top[0][lane];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, rank = min(kTopRank, groups / 8);
+  if (wave < kBoundT / kWave) {
+    float x = -INFINITY;
+    for (int g = threadIdx.x; g < groups / 4; g += 4 * kBoundT) {   // four groups that lie next to each other; a row's are a multiple of sixteen
+      floatx4 y[4];
 #pragma unroll
-  for (int w = 1; w < T / kWave; ++w) x = merged(x, s.top[w][lane]);
+      for (int i = 0; i < 4; ++i)
+        y[i] = g + i * kBoundT < groups / 4 ? reinterpret_cast<const floatx4*>(group_max)[g + i * kBoundT] : floatx4{-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll
+      for (int i = 0; i < 4; ++i) x = larger(x, larger(larger(y[i][0], y[i][1]), larger(y[i][2], y[i][3])));
+    }
+    s.top[wave][lane] = sorted_desc(x);
+  }
   __syncthreads();
-  return __shfl(x, rank - 1, kWave);
+  if (wave == 0) {
+    float x = merged(merged(s.top[0][lane], s.top[1][lane]), merged(s.top[2][lane], s.top[3][lane]));
+    s.top[0][lane] = x;
+  }
+  __syncthreads();
+  return s.top[0][rank - 1];
 }
 // Lists the tokens with z >= bound; false: more than there is room for.
 template <typename In, int T>
@@ -451,12 +547,14 @@ __device__ __forceinline__ bool list_front(const RowSource<In, T>& row, const fl
   int* const s_group = reinterpret_cast<int*>(s.bins);
   if (threadIdx.x == 0) s.n_list = s.n_groups = 0;
   __syncthreads();
-  for (int g = threadIdx.x; g < groups; g += T) {
-    const float x = group_max[g];
-    if (x >= bound && x > -INFINITY) {
-      const int at = atomicAdd(&s.n_groups, 1);
-      if (at < kGroupCap) s_group[at] = g;
-    }
+  for (int g = threadIdx.x; g < groups / 4; g += T) {
+    const floatx4 x = reinterpret_cast<const floatx4*>(group_max)[g];
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      if (x[i] >= bound && x[i] > -INFINITY) {
+        const int at = atomicAdd(&s.n_groups, 1);
+        if (at < kGroupCap) s_group[at] = g * 4 + i;
+      }
   }
   __syncthreads();
   const int n = s.n_groups;
@@ -488,54 +586,70 @@ __device__ __forceinline__ bool list_front(const RowSource<In, T>& row, const fl
   __syncthreads();
   return s.n_list <= kListCap;
 }
-// What the listed tokens say, where they are enough: id -1 where they are not.  Each is compared with all of them, once by its logit and once by its number.
+// What the listed tokens say, where they are enough: id -1 where they are not.  Each is compared with all of them, once by its logit and once by its number, by
+// the threads that it has: sixteen of up to 64 tokens, four of up to 256.
 template <int T>
-__device__ __forceinline__ Drawn draw_from_front(RowShared<T>& s, int n, float bound, bool all_listed, const RowDraw& d) {
+__device__ __forceinline__ Drawn draw_from_front(RowShared<T>& s, Block<T>& all, int n, float bound, bool all_listed, const RowDraw& d) {
   u64* const s_key = s.bins;                                 // [kRanked] each
   u64* const s_w = s.bins + kRanked;
   u64* const s_sorted = s.bins + 2 * kRanked;
-  const int i = threadIdx.x;
-  u64 key = 0, w = 0;
-  if (i < n) {
-    key = static_cast<u64>(order_of(s.list_z[i])) << 32 | (0xFFFFFFFFu - static_cast<uint32_t>(s.list_id[i]));
-    w = d.weight(s.list_z[i]);
-    s_key[i] = key;
+  int* const s_rank = reinterpret_cast<int*>(s.bins + 3 * kRanked);
+  u64* const s_run = s.bins + 4 * kRanked;
+  const int of = n <= kWave ? kWave : n <= 2 * kWave ? 2 * kWave : kRanked, parts = T / of;
+  const int i = threadIdx.x & (of - 1), part = threadIdx.x / of;   // a part to whole wavefronts
+  const bool one = part == 0 && i < n;                       // the token's own thread
+  u64 w = 0;
+  if (part == 0) {
+    s_key[i] = i < n ? static_cast<u64>(order_of(s.list_z[i])) << 32 | (0xFFFFFFFFu - static_cast<uint32_t>(s.list_id[i])) : 0;
+    s_rank[i] = 0;
+    s_run[i] = 0;
+    if (i < n) w = d.weight(s.list_z[i]);
+  }
+  if (threadIdx.x == 0) s.found_id = -1;
+  __syncthreads();
+  const u64 key = s_key[i];
+  const int j0 = part * (of / parts), j1 = min(j0 + of / parts, n);
+  if (i < n && j0 < j1) {
+    int rank = 0;
+#pragma unroll 8
+    for (int j = j0; j < j1; ++j) rank += s_key[j] > key;
+    atomicAdd(&s_rank[i], rank);
   }
   __syncthreads();
-  int rank = 0;
-  if (i < n)
-    for (int j = 0; j < n; ++j) rank += s_key[j] > key;
-  const bool first = i < n && (d.k == 0 || rank < d.k);
-  if (!first) w = 0;
-  if (i < n) s_sorted[rank] = w;
+  const int rank = s_rank[i];
+  if (!one || (d.k > 0 && rank >= d.k)) w = 0;
+  if (one) s_sorted[rank] = w;
   __syncthreads();
   u64 mass;
-  const u64 ahead = block_excl_scan(i < n ? s_sorted[i] : 0, s.scan, &mass);   // of the i-th in falling order
+  const u64 here = one ? s_sorted[i] : 0, ahead = all.scan(here, &mass);   // of the i-th in falling order
   const bool whole = d.k > 0 || (d.by_min() && d.weight(bound) == 0) || all_listed;   // nothing that is not listed counts
   u64 need = mass;
   if (d.p < 1.0) {
     if (whole) need = d.share(d.p, mass);
     else {
-      const double part = ceil(d.p * d.all * d.one);
-      need = part < 1.0 ? 1 : static_cast<u64>(part);
+      const double part_of = ceil(d.p * d.all * d.one);
+      need = part_of < 1.0 ? 1 : static_cast<u64>(part_of);
     }
   }
   if ((d.k > n && !all_listed) || (!whole && (d.by_min() || d.p == 1.0 || need > mass))) return Drawn{-1, 0};
-  if (i < n) {                                               // kept: whose front is shorter than what is needed
+  if (one) {                                                 // kept: whose front is shorter than what is needed
     if (ahead >= need) s_sorted[i] = 0;
-    const u64 mine = s_sorted[i];
-    if (mine && ahead + mine >= need) s.found_above = ahead + mine;
+    else if (here && ahead + here >= need) s.found_above = ahead + here;
   }
   __syncthreads();
   mass = s.found_above;
-  w = i < n ? s_sorted[rank] : 0;
-  if (i < n) s_w[i] = w;
+  if (one) s_w[i] = w = s_sorted[rank];
   __syncthreads();
-  if (i < n && w) {
+  const uint32_t mine = static_cast<uint32_t>(key);          // falls with the token
+  if (i < n && j0 < j1) {
     u64 run = 0;
-    const uint32_t mine = static_cast<uint32_t>(key);        // falls with the token
-    for (int j = 0; j < n; ++j) run += static_cast<uint32_t>(s_key[j]) >= mine ? s_w[j] : 0;
-    const u64 target = d.target(mass);
+#pragma unroll 8
+    for (int j = j0; j < j1; ++j) run += static_cast<uint32_t>(s_key[j]) >= mine ? s_w[j] : 0;
+    if (run) atomicAdd(&s_run[i], run);
+  }
+  __syncthreads();
+  if (one && w) {
+    const u64 run = s_run[i], target = d.target(mass);
     if (target < run && run - w <= target) s.found_id = s.list_id[i];
   }
   __syncthreads();
@@ -545,179 +659,217 @@ __device__ __forceinline__ Drawn draw_from_front(RowShared<T>& s, int n, float b
 // ---- rows whose mass is spread
 // The tokens below the front by their distance to it, in 1/64 of T: their counts say near which bin the border of top_p lies and in which exactly that of top_k.  A second
 // pass sums what lies above for certain, by unit, and lists the tokens of the bins around; among those the borders are found as they are.  Where a border was not
-// among the bins (id -1), or they hold too many, the row is gone through bit by bit.
+// among the bins, or they hold too many, the row is gone through bit by bit.
 constexpr double kBinsPerT = 64.0;
-template <typename In, int T>
-__device__ __forceinline__ Drawn draw_by_bins(const RowSource<In, T>& row, RowShared<T>& s, u64* s_unit, float bound, int n_front, double c, const RowDraw& d) {
-  constexpr int kEach = kBins / T;
-  uint32_t* const s_count = reinterpret_cast<uint32_t*>(s.bins);
-  const float scale = static_cast<float>(fmin(c * (kBinsPerT / kLog2e64), 1e30));
-  auto bin_of = [&](float z) { return static_cast<int>(fminf((bound - z) * scale, static_cast<float>(kBins - 1))); };
-  // below this nothing counts: weights under min_p, or so small that all tokens together with them are not what top_p leaves out
-  double least = d.by_min() ? d.m : d.k > 0 || d.p == 1.0 ? 0.0 : (1.0 - d.p) * d.all / row.V;
-  float lo = -INFINITY;
-  if (least > 0.0 && c > 0.0) {
-    const double x = d.w.top + log2(least) / c;
-    lo = static_cast<float>(x);
-    lo -= fabsf(lo) * 1e-6f + 1e-30f;
+struct Binning {
+  float bound, lo, scale;                                    // of tokens with lo <= z < bound
+  __device__ __forceinline__ Binning(float bound_, const RowDraw& d, int V) : bound(bound_), lo(-INFINITY) {
+    const double c = d.w.c;
+    scale = static_cast<float>(fmin(c * (kBinsPerT / kLog2e64), 1e30));
+    // below lo nothing counts: weights under min_p, or so small that all tokens together with them are not what top_p leaves out
+    const double least = d.by_min() ? d.m : d.k > 0 || d.p == 1.0 ? 0.0 : (1.0 - d.p) * d.all / V;
+    if (!(least > 0.0)) return;
+    lo = static_cast<float>(d.w.top + static_cast<double>(__log2f(static_cast<float>(least))) / c * (1.0 + 1e-6));
+    lo -= fabsf(lo) * 1e-6f + static_cast<float>(1e-5 / c);
   }
-  for (int i = threadIdx.x; i < kBins; i += T) s_count[i] = 0;
-  // the front's mass
-  u64 front = 0;
-  for (int i = threadIdx.x; i < n_front; i += T) front += d.weight(s.list_z[i]);
-  front = block_total(front, s);
-  row.each(lo, [&](float z, int) {
-    if (z < bound && z >= lo) atomicAdd(&s_count[bin_of(z)], 1u);
-  });
-  __syncthreads();
-  const double at_bound = d.w(bound), step = exp2(-1.0 / kBinsPerT * kLog2e64);
-  u64 counts[kEach], n_mine = 0, n_all;
+  __device__ __forceinline__ bool has(float z) const { return z < bound && z >= lo && z > -INFINITY; }
+  __device__ __forceinline__ int bin(float z) const { return static_cast<int>(fminf((bound - z) * scale, static_cast<float>(kBins - 1))); }
+  // A bin's logits by its edges, a hundredth of a bin and a few numbers apart: more than the rounding of what bin() computes.
+  __device__ __forceinline__ Span span(int from, int to) const {
+    Span a;
+    if (to >= kBins - 1) return a;                           // what lies beyond is in the last bin
+    a.base = order_of(bound - (static_cast<float>(to) + 1.01f) / scale) - 8;
+    const uint32_t end = order_of(bound - (static_cast<float>(from) - 0.01f) / scale) + 8;
+    a.bits = 32 - __clz(static_cast<int>(end - a.base));
+    return a;
+  }
+};
+// The bins that matter.
+struct Bracket {
+  int b1, b2;                                                // those around the border of top_p (none: b2 < b1)
+  int k_bin;                                                 // that of the k-th token; kBins: all are among the first k
+  int sure;                                                  // bins before it are in for certain
+  int last;                                                  // what lies behind it counts for nothing
+  u64 k_in_bin;                                              // places of the k-th bin
+  __device__ __forceinline__ bool lists(int b) const { return (b == k_bin && b < kBins) || (b >= b1 && b <= b2); }
+};
+// First pass, of the units [u0, u1).
+template <typename In, int T>
+__device__ __forceinline__ void count_bins(const RowSource<In, T>& row, const Binning& q, int u0, int u1, uint32_t* s_count) {
+  for (int u = u0 + static_cast<int>(threadIdx.x >> 6); u < u1; u += T / kWave) {
+    const float most = row.unit_max[u];
+    if (!(most >= q.lo) || most == -INFINITY) continue;
+    float x[kPerLane];
+    load_unit(row.z, row.V, u, x);
+#pragma unroll
+    for (int i = 0; i < kPerLane; ++i)
+      if (q.has(x[i])) atomicAdd(&s_count[q.bin(x[i])], 1u);
+  }
+}
+// counts: this thread's bins, kBins / T of them from threadIdx.x * kBins / T on.
+template <int T>
+__device__ __forceinline__ Bracket bracket_of(const uint32_t (&counts)[kBins / T], RowShared<T>& s, Block<T>& all, const Binning& q, u64 front, int n_front, const RowDraw& d) {
+  constexpr int kEach = kBins / T;
+  const double at_bound = d.w(q.bound);
+  u64 n_mine = 0, n_all;
   double m_mine = 0.0, m_all, of[kEach];
 #pragma unroll
   for (int i = 0; i < kEach; ++i) {
     const int b = static_cast<int>(threadIdx.x) * kEach + i;
-    counts[i] = s_count[b];
-    of[i] = at_bound * exp2(-(b + 0.5) / kBinsPerT * kLog2e64);
+    of[i] = at_bound * exp2_near(-(b + 0.5) / kBinsPerT * kLog2e64);
     n_mine += counts[i];
     m_mine += static_cast<double>(counts[i]) * of[i];
   }
-  u64 n_before = block_excl_scan(n_mine, s.scan, &n_all);
-  const double m_before = block_excl_scan(m_mine, s.dscan, &m_all);
+  const u64 n_before = all.scan(n_mine, &n_all);
+  const double m_before = all.scan(m_mine, &m_all);
   const double f_mass = static_cast<double>(front) / d.one;
-  // the bin of the k-th token
   if (threadIdx.x == 0) {
     s.found_bin = kBins;
     s.found_drest = f_mass + m_all;
     s.found_rest = 0;
+    s.found_id = s.n_groups = kBins - 1;
   }
   __syncthreads();
-  const bool behind_counts = d.k == 0 || d.k > n_front;
-  const u64 k_rest = d.k > n_front ? static_cast<u64>(d.k - n_front) : 0;   // places behind the front
-  {
+  if (d.k > 0) {                                             // the bin of the k-th token; all of the front are among the first k
+    const u64 k_rest = static_cast<u64>(d.k - n_front);
     u64 n = n_before;
     double m = m_before;
 #pragma unroll
     for (int i = 0; i < kEach; ++i) {
-      if (d.k > 0 && n < k_rest && k_rest <= n + counts[i]) {
-        s.found_bin = static_cast<uint32_t>(threadIdx.x * kEach + i);
+      if (n < k_rest && k_rest <= n + counts[i]) {
+        s.found_bin = threadIdx.x * kEach + i;
         s.found_rest = k_rest - n;
         s.found_drest = f_mass + m + static_cast<double>(k_rest - n) * of[i];
       }
       n += counts[i];
       m += static_cast<double>(counts[i]) * of[i];
     }
+    __syncthreads();
   }
-  __syncthreads();
-  const int k_bin = static_cast<int>(s.found_bin);           // kBins: all are among the first k
-  const u64 k_in_bin = s.found_rest;
-  const double total = !d.by_min() && d.k == 0 ? d.all : s.found_drest;
-  __syncthreads();
-  // the bins around the border of top_p
-  int b1 = 0, b2 = -1;
-  if (d.p < 1.0 && behind_counts) {
-    const double need = d.p * total - f_mass, off = 1e-3 * fabs(need) + 1e-6 * total;
-    if (need + off > 0.0) {
-      if (threadIdx.x == 0) s.found_id = s.n_groups = kBins - 1;
-      __syncthreads();
-      double m = m_before;
+  Bracket r;
+  r.k_bin = static_cast<int>(s.found_bin);
+  r.k_in_bin = s.found_rest;
+  const double total = !d.by_min() && d.k == 0 ? d.all : s.found_drest;   // what top_p is of, nearly
+  r.b1 = 0;
+  r.b2 = -1;
+  const double need = d.p * total - f_mass, off = 1e-3 * fabs(need) + 1e-6 * total;
+  if (d.p < 1.0 && need + off > 0.0) {
+    int from = kBins - 1, to = kBins - 1;                    // the thread's first bin that reaches the lower end, and the upper one
+    double m = m_before + m_mine;
 #pragma unroll
-      for (int i = 0; i < kEach; ++i) {
-        const double next = m + static_cast<double>(counts[i]) * of[i];
-        const int b = static_cast<int>(threadIdx.x) * kEach + i;
-        if (need - off <= next) atomicMin(&s.found_id, b);
-        if (need + off <= next) atomicMin(&s.n_groups, b);
-        m = next;
-      }
-      __syncthreads();
-      b1 = max(s.found_id - 1, 0);
-      b2 = min(s.n_groups + 1, min(k_bin, kBins - 1));
-      b1 = min(b1, b2);
+    for (int i = kEach - 1; i >= 0; --i) {
+      const int b = static_cast<int>(threadIdx.x) * kEach + i;
+      if (need - off <= m) from = b;
+      if (need + off <= m) to = b;
+      m -= static_cast<double>(counts[i]) * of[i];
     }
+    from = -wave_max(-from);
+    to = -wave_max(-to);
+    if ((threadIdx.x & 63) == 0) {
+      atomicMin(&s.found_id, from);
+      atomicMin(&s.n_groups, to);
+    }
+    __syncthreads();
+    r.b2 = min(s.n_groups + 1, min(r.k_bin, kBins - 1));
+    r.b1 = min(max(s.found_id - 1, 0), r.b2);
   }
-  const bool by_p = d.p < 1.0;
-  // tokens above b1 are in for certain; without top_p all that come before k_bin
-  const int sure_end = by_p ? (b2 < 0 ? 0 : b1) : min(k_bin, kBins);
-  const bool need_total = by_p && (d.k > 0 || d.by_min());   // the mass that top_p is of
-  const int last = !behind_counts ? -1 : need_total || !by_p ? min(k_bin, kBins - 1) : b2;   // bins that matter
-  if (threadIdx.x == 0) s.n_list = n_front;
   __syncthreads();
-  u64 sure = 0, rest = 0, unit = 0;
-  row.each(lo, [&](float z, int id) {
-    if (!(z < bound && z >= lo)) return;
-    const int b = bin_of(z);
-    if (b > last) return;
-    if (b == k_bin || (b >= b1 && b <= b2)) {
-      const int at = atomicAdd(&s.n_list, 1);
-      if (at < kListCap) {
-        s.list_z[at] = z;
-        s.list_id[at] = id;
+  const bool by_p = d.p < 1.0, total_open = d.k > 0 || d.by_min();
+  r.sure = by_p ? (r.b2 < 0 ? 0 : r.b1) : r.k_bin;
+  r.last = total_open || !by_p ? min(r.k_bin, kBins - 1) : r.b2;
+  return r;
+}
+// Second pass, of the units [u0, u1): the sum of what is in for certain of every unit, of all units what else top_p may be of, and the list.
+template <typename In, int T>
+__device__ __forceinline__ void sum_units(const RowSource<In, T>& row, const Binning& q, const Bracket& r, const RowDraw& d, int u0, int u1, u64* unit_sum, float* list_z,
+                                          int* list_id, int* n_list, u64& sure, u64& rest) {
+  for (int u = u0 + static_cast<int>(threadIdx.x >> 6); u < u1; u += T / kWave) {
+    u64 unit = 0;
+    const float most = row.unit_max[u];
+    if (most >= q.lo && most > -INFINITY) {
+      float x[kPerLane];
+      load_unit(row.z, row.V, u, x);
+      uint32_t mask = 0;                                     // of what the lane lists
+#pragma unroll
+      for (int i = 0; i < kPerLane; ++i) {
+        const int b = q.has(x[i]) ? q.bin(x[i]) : kBins;
+        const bool list = r.lists(b);
+        if (list) mask |= 1u << i;
+        if (!list && b <= r.last) {
+          const u64 w = d.weight(x[i]);
+          if (b < r.sure) unit += w;
+          else rest += w;
+        }
+        if (i % 4 == 3) __builtin_amdgcn_sched_barrier(0);   // sixteen weights at once take more registers than there are
       }
-      return;
+      if (__ballot(mask)) {                                  // one place for all that a wavefront lists of a unit
+        const int mine = __popc(mask), upto = static_cast<int>(lanes_scan(static_cast<u64>(mine)));
+        int at = 0;
+        if ((threadIdx.x & 63) == 63) at = atomicAdd(n_list, upto);
+        at = __shfl(at, 63, kWave) + upto - mine;
+#pragma unroll
+        for (int i = 0; i < kPerLane; ++i)
+          if (mask >> i & 1) {
+            if (at < kListCap) {
+              list_z[at] = x[i];
+              list_id[at] = token_of<In>(u, i);
+            }
+            ++at;
+          }
+      }
+      sure += unit;
+      unit = lanes_sum(unit);
     }
-    const u64 w = d.weight(z);
-    if (b < sure_end) unit += w;
-    else rest += w;
-  }, [&](int u) {
-    sure += unit;
-    unit = wave_sum(unit);
-    if ((threadIdx.x & 63) == 0) s_unit[u] = unit;
-    unit = 0;
-  });
-  sure = block_total(sure, s);
-  rest = block_total(rest, s);
-  const int n_list = s.n_list;
-  if (n_list > kListCap) return Drawn{-1, 0};
-  // the first k: those in the bin of the k-th
+    if ((threadIdx.x & 63) == 0) unit_sum[u] = unit;
+  }
+}
+// From the lists and sums, in LDS: the borders, and the token.  id -1: the border of top_p lies elsewhere.
+template <typename In, int T>
+__device__ __forceinline__ Drawn draw_listed(const RowSource<In, T>& row, RowShared<T>& s, Block<T>& all, u64* s_unit, const Binning& q, const Bracket& r, int n_front, int n_list,
+                                             u64 sure, u64 rest, const RowDraw& d) {
   Cut first, run;
   const ListSource<T> listed{&s, 0, n_list}, front_list{&s, 0, n_front}, behind{&s, n_front, n_list};
   u64 mass;
-  if (!behind_counts) first = cut_at(front_list, s, -INFINITY, [](float, int) { return u64{1}; }, static_cast<u64>(d.k), &mass);
-  else if (k_bin < kBins) first = cut_at(behind, s, -INFINITY, [&](float z, int) { return u64{bin_of(z) == k_bin}; }, k_in_bin, &mass);
+  if (r.k_bin < kBins)
+    first = cut_at(behind, s, all, -INFINITY, [&](float z, int) { return u64{q.bin(z) == r.k_bin}; }, r.k_in_bin, &mass, d.id_bits, q.span(r.k_bin, r.k_bin));
   auto of_first = [&](float z, int id) { return first.in(z, id) ? d.weight(z) : u64{0}; };
-  auto sum_of = [&](const ListSource<T>& l) {
-    u64 m = 0;
-    l.each(-INFINITY, [&](float z, int id) { m += of_first(z, id); });
-    return block_total(m, s);
-  };
-  const u64 in_front = sum_of(front_list), in_behind = sum_of(behind);
+  auto in_bins = [&](float z, int id) { return q.bin(z) <= r.b2 ? of_first(z, id) : u64{0}; };
+  u64 in_front = 0, in_behind = 0, have = 0, none = 0;
+  front_list.each(-INFINITY, [&](float z, int) { in_front += d.weight(z); });
+  behind.each(-INFINITY, [&](float z, int id) { in_behind += of_first(z, id); have += in_bins(z, id); });
+  all.sum(in_front, in_behind);
+  all.sum(have, none);
   mass = in_front + sure + in_behind + rest;
-  bool sure_in = true;
-  if (by_p) {
+  if (d.p < 1.0) {
     u64 need = d.share(d.p, mass);
-    if (!need_total) {
+    if (d.k == 0 && !d.by_min()) {                           // of all tokens
       const double part = ceil(d.p * d.all * d.one);
       need = part < 1.0 ? 1 : static_cast<u64>(part);
     }
     if (need <= in_front) {
-      run = cut_at(front_list, s, -INFINITY, of_first, need, &mass);
-      sure_in = false;
+      run = cut_at(front_list, s, all, -INFINITY, [&](float z, int) { return d.weight(z); }, need, &mass, d.id_bits);
+      for (int u = threadIdx.x; u < row.units; u += T) s_unit[u] = 0;
     } else {
-      auto in_bins = [&](float z, int id) { return z < bound && bin_of(z) <= b2 ? of_first(z, id) : u64{0}; };
-      u64 have = 0;
-      behind.each(-INFINITY, [&](float z, int id) { have += in_bins(z, id); });
-      have = block_total(have, s);
       if (need <= in_front + sure || need > in_front + sure + have) return Drawn{-1, 0};
-      run = cut_at(behind, s, -INFINITY, in_bins, need - in_front - sure, &mass);
+      run = cut_at(behind, s, all, -INFINITY, in_bins, need - in_front - sure, &mass, d.id_bits, q.span(r.b1, r.b2));
       mass += in_front + sure;
     }
   }
   auto kept = [&](float z, int id) { return run.in(z, id) ? of_first(z, id) : u64{0}; };
-  if (!sure_in)
-    for (int u = threadIdx.x; u < row.units; u += T) s_unit[u] = 0;
   __syncthreads();
   listed.each(-INFINITY, [&](float z, int id) {
     const u64 w = kept(z, id);
     if (w) atomicAdd(&s_unit[id / kUnit], w);
   });
   __syncthreads();
-  return Drawn{token_beyond(row, s, s_unit, kept, d.target(mass)), mass};
+  return Drawn{token_beyond(row, s, all, s_unit, kept, d.target(mass)), mass};
 }
 
 // No filter: the unit from the units' masses, then the token.
 template <typename In, int T, class Shared>
-__device__ __forceinline__ Drawn draw_unfiltered(const RowSource<In, T>& row, Shared& s, const double* mass_of, const Weigh& w, double u, double all) {
+__device__ __forceinline__ Drawn draw_unfiltered(const RowSource<In, T>& row, Shared& s, Block<T>& block, const double* mass_of, const Weigh& w, double u, double all) {
   const double target = u * all;
-  auto mass = [&](int i) { return mass_of[i] * w(or_none(row.unit_max[i], row.infinite)); };
+  auto mass = [&](int i) { return mass_of[i] * w(row.extreme(row.unit_max[i])); };
   if (threadIdx.x == 0) s.found_id = -1;
   int unit = -1;
   double before = 0.0;
@@ -725,7 +877,7 @@ __device__ __forceinline__ Drawn draw_unfiltered(const RowSource<In, T>& row, Sh
     const int i = u0 + threadIdx.x;
     const double mine = i < row.units ? mass(i) : 0.0;
     double sum;
-    const double excl = before + block_excl_scan(mine, s.dscan, &sum);
+    const double excl = before + block.scan(mine, &sum);
     if (mine > kNoWeight && excl + mine > target) atomicMin(reinterpret_cast<unsigned*>(&s.found_id), static_cast<unsigned>(i));
     __syncthreads();
     unit = s.found_id;
@@ -753,7 +905,7 @@ __device__ __forceinline__ Drawn draw_unfiltered(const RowSource<In, T>& row, Sh
     else last = v + i;
     sum += mine[i];
   }
-  double run = block_excl_scan(sum, s.dscan, &total);
+  double run = block.scan(sum, &total);
 #pragma unroll
   for (int i = kEach - 1; i >= 0; --i) {                     // the thread's first that passes
     double to = run;
@@ -781,101 +933,244 @@ __device__ __forceinline__ int largest(const RowSource<In, T>& row, Shared& s, f
   __syncthreads();
   if (threadIdx.x == 0) s.found_id = INT32_MAX;
   __syncthreads();
-  const float ref = or_none(top, row.infinite);
+  const float ref = row.extreme(top);
   for (int v = unit * kUnit + threadIdx.x; v < (unit + 1) * kUnit; v += T)
     if (row.at(v) == ref) atomicMin(&s.found_id, v);
   __syncthreads();
   return s.found_id;
 }
+template <int T>
 struct PlainShared {
-  float red[17];
-  double dscan[17];
+  u64 block[2][2][T / kWave];
   double found_drest;
   int found_id;
 };
-// A workgroup to a row.  FILTERED: some row may have a filter.
-template <typename In, int T, bool FILTERED>
+// What the kernels of a row have in common: its largest logit, sums and settings.
+struct RowCalls {
+  Settings S;
+  const int32_t* rowsel;
+  int64_t c0;
+  Summary A;
+  const float* uniform;
+  SampleOut out;
+  int unit_bits;
+};
+template <typename In, int T>
+__device__ __forceinline__ RowSource<In, T> row_source(const Logits<In>& L, const RowCalls& C, int64_t m, float top) {
+  return RowSource<In, T>{L.row(m), L.V, L.units, C.A.unit + m * L.units, Extreme(top)};
+}
+__device__ __forceinline__ RowDraw row_draw(const RowCalls& C, int64_t row, float ref, double t, double u, double all, int V) {
+  RowDraw d{ref, Weigh(ref, scale_of(t)), C.S.k(row), C.S.p(row), C.S.m(row), u, all, ldexp(1.0, C.unit_bits), 32 - __clz(V - 1)};
+  if (d.k >= V || d.k < 0) d.k = 0;
+  d.p = d.p < 1.0 ? fmax(d.p, 0.0) : 1.0;
+  d.m = d.m > 0.0 ? fmin(d.m, 1.0) : 0.0;
+  return d;
+}
+__device__ __forceinline__ double row_uniform(const RowCalls& C, int64_t row) {
+  const double u = C.uniform[row];
+  return u > 0.0 ? fmin(u, 1.0) : 0.0;
+}
+// By one thread.  zi, ref: the token's logit and the largest, sum: of exp(z - ref); kept: the mass that it was drawn from.
+__device__ __forceinline__ void write_drawn(const SampleOut& out, int64_t row, int id, float zi, float ref, double sum, double t, double kept) {
+  out.ids[row] = id;
+  const double gap = zi == ref ? 0.0 : static_cast<double>(zi) - static_cast<double>(ref);
+  if (out.logp) out.logp[row] = static_cast<float>(gap - log_of(sum));
+  if (out.logq) out.logq[row] = t > 0.0 ? static_cast<float>(gap / t - log_of(kept)) : 0.f;
+}
+// A row that its front did not decide, on its way through the launches behind.
+struct RowState {
+  int flat;                                                  // it is one; the rest is only written then
+  float top, bound;
+  int n_front, n_list;
+  double all, sum;
+  u64 front, rest;
+  Bracket bracket;
+};
+struct FlatWs {
+  RowState* state;                                           // [rows]
+  uint32_t* counts;                                          // [rows][parts][kBins]
+  u64* unit_sum;                                             // [rows][units]
+  float* list_z;                                             // [rows][kListCap]
+  int* list_id;
+  int parts;
+};
+enum class Filter { kNone, kSome, kSomeInOne };              // no row has one; rows may have; ... and the launch does all of a row
+
+// A workgroup to a row.
+template <typename In, int T, Filter FILTER>
 __global__ void __launch_bounds__(T)
-k_sample_row(Logits<In> L, Settings S, const int32_t* __restrict__ rowsel, int64_t c0, Summary A, const float* __restrict__ uniform, int unit_bits, SampleOut out) {
-  extern __shared__ u64 s_unit[];                            // [units], FILTERED only
-  __shared__ std::conditional_t<FILTERED, RowShared<T>, PlainShared> s;
-  const int64_t m = blockIdx.x, row = rowsel ? rowsel[c0 + m] : c0 + m;
-  const float* const unit_max = A.unit + m * L.units;
-  const double *const mass_of = A.mass + m * L.units, *const sum_of = A.sum + m * L.units;
-  const double t = S.t(row);
-  double u = uniform[row];
+k_sample_row(Logits<In> L, RowCalls C, FlatWs F) {
+  extern __shared__ u64 s_unit[];                            // [units], kSomeInOne only
+  __shared__ std::conditional_t<FILTER == Filter::kNone, PlainShared<T>, RowShared<T>> s;
+  const int64_t m = blockIdx.x, row = C.rowsel ? C.rowsel[C.c0 + m] : C.c0 + m;
+  const float* const unit_max = C.A.unit + m * L.units;
+  const double *const mass_of = C.A.mass + m * L.units, *const sum_of = C.A.sum + m * L.units;
+  const double t = C.S.t(row), u = row_uniform(C, row);
   float top = -INFINITY;
-  for (int i = threadIdx.x; i < L.units; i += T) top = fmaxf(top, unit_max[i]);
-  {
-    float* const red = reinterpret_cast<float*>(s.dscan);
-    top = wave_max(top);
-    if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = top;
-    __syncthreads();
-    for (int w = 0; w < T / kWave; ++w) top = fmaxf(top, red[w]);
-    __syncthreads();
-  }
+  for (int i = threadIdx.x; i < L.units; i += T) top = larger(top, unit_max[i]);
+  Block<T> block(s.block);
+  top = block.max(top);
+  if (FILTER == Filter::kSome && threadIdx.x == 0) F.state[m].flat = 0;
   if (top == -INFINITY) {                                    // nothing to draw from
     if (threadIdx.x == 0) {
-      out.ids[row] = -1;
-      if (out.logp) out.logp[row] = 0.f;
-      if (out.logq) out.logq[row] = 0.f;
+      C.out.ids[row] = -1;
+      if (C.out.logp) C.out.logp[row] = 0.f;
+      if (C.out.logq) C.out.logq[row] = 0.f;
     }
     return;
   }
-  const RowSource<In, T> src{L.row(m), L.V, L.units, unit_max, top == INFINITY};
-  const float ref = or_none(top, src.infinite);
-  const double c = scale_of(t);
-  const Weigh w{ref, c}, w1{ref, kLog2e64};
-  u = u > 0.0 ? fmin(u, 1.0) : 0.0;
+  const RowSource<In, T> src = row_source<In, T>(L, C, m, top);
+  const float ref = src.extreme(top);
+  const Weigh w(ref, scale_of(t)), w1(ref, kLog2e64);
   double sum = 0.0, all = 0.0;                               // of exp(z - top), for the log-prob of the softmax itself, and of the weights
   for (int i = threadIdx.x; i < L.units; i += T) {
-    const float x = or_none(unit_max[i], src.infinite);
+    const float x = src.extreme(unit_max[i]);
     sum += sum_of[i] * w1(x);
     all += mass_of[i] * w(x);
   }
-  block_excl_scan(sum, s.dscan, &sum);
-  block_excl_scan(all, s.dscan, &all);
+  block.sum(sum, all);
   int id;
   double kept = all;
   if (!(t > 0.0)) {
     id = largest(src, s, top);
-  } else if constexpr (!FILTERED) {
-    id = draw_unfiltered(src, s, mass_of, w, u, all).id;
+  } else if constexpr (FILTER == Filter::kNone) {
+    id = draw_unfiltered(src, s, block, mass_of, w, u, all).id;
   } else {
-    int k = S.k(row);
-    double p = S.p(row), mp = S.m(row);
-    if (k >= L.V || k < 0) k = 0;
-    p = p < 1.0 ? fmax(p, 0.0) : 1.0;
-    mp = mp > 0.0 ? fmin(mp, 1.0) : 0.0;
-    if (k == 0 && p == 1.0 && mp == 0.0) {
-      id = draw_unfiltered(src, s, mass_of, w, u, all).id;
+    const RowDraw d = row_draw(C, row, ref, t, u, all, L.V);
+    if (d.k == 0 && d.p == 1.0 && d.m == 0.0) {
+      id = draw_unfiltered(src, s, block, mass_of, w, u, all).id;
     } else {
-      const RowDraw d{ref, w, k, p, mp, u, all, ldexp(1.0, unit_bits)};
-      const float* const group_max = A.group + m * L.units * kGroupsPerUnit;
-      const int groups = L.units * kGroupsPerUnit;
-      float bound = src.infinite ? -INFINITY : L.V <= kRanked ? -INFINITY : front_bound<T>(group_max, groups, s);
+      const float* const group_max = C.A.group + m * L.units * kGroupsPerUnit;
+      float bound = L.V <= kRanked ? -INFINITY : front_bound<T>(group_max, L.units * kGroupsPerUnit, s);
       Drawn got{-1, 0};
-      if (src.infinite) {
-        got = draw_by_passes<In, T>(src, s, s_unit, d);
-      } else {
+      int n = 0;
+      if (!src.extreme.is) {
         const bool listed = list_front(src, group_max, bound, s);
-        const int n = listed ? s.n_list : 0;
+        n = s.n_list;
         __syncthreads();
-        if (listed && n <= kRanked) got = draw_from_front(s, n, bound, bound == -INFINITY, d);
-        if (!listed) bound = INFINITY;
-        if (got.id < 0 && bound > -INFINITY && listed) got = draw_by_bins(src, s, s_unit, bound, n, c, d);
-        if (got.id < 0) got = draw_by_passes<In, T>(src, s, s_unit, d);
+        if (listed && n <= kRanked) got = draw_from_front(s, block, n, bound, bound == -INFINITY, d);
+        if (!listed || n > kRanked) {                        // many that are alike: no front, bins from the largest on
+          n = 0;
+          bound = INFINITY;
+        }
+      }
+      if (got.id < 0) {
+        const bool bins = !src.extreme.is && bound > -INFINITY;
+        if (bound == INFINITY) bound = d.w.next_above();
+        u64 front = 0;
+        for (int i = threadIdx.x; i < n; i += T) front += d.weight(s.list_z[i]);
+        front = block.sum(front);
+        if constexpr (FILTER == Filter::kSome) {
+          for (int i = threadIdx.x; i < n; i += T) {
+            F.list_z[m * kListCap + i] = s.list_z[i];
+            F.list_id[m * kListCap + i] = s.list_id[i];
+          }
+          if (threadIdx.x == 0) F.state[m] = RowState{bins ? 1 : 2, top, bound, n, n, all, sum, front, 0, Bracket{}};
+          return;
+        } else {
+          if (bins) {
+            const Binning q(bound, d, L.V);
+            uint32_t* const s_count = reinterpret_cast<uint32_t*>(s.bins);
+            for (int i = threadIdx.x; i < kBins; i += T) s_count[i] = 0;
+            __syncthreads();
+            count_bins(src, q, 0, L.units, s_count);
+            __syncthreads();
+            uint32_t counts[kBins / T];
+#pragma unroll
+            for (int i = 0; i < kBins / T; ++i) counts[i] = s_count[threadIdx.x * (kBins / T) + i];
+            const Bracket r = bracket_of(counts, s, block, q, front, n, d);
+            if (threadIdx.x == 0) s.n_list = n;
+            __syncthreads();
+            u64 sure = 0, rest = 0;
+            sum_units(src, q, r, d, 0, L.units, s_unit, s.list_z, s.list_id, &s.n_list, sure, rest);
+            block.sum(sure, rest);
+            if (s.n_list <= kListCap) got = draw_listed(src, s, block, s_unit, q, r, n, s.n_list, sure, rest, d);
+            __syncthreads();
+          }
+          if (got.id < 0) got = draw_by_passes<In, T>(src, &s, block.turn, s_unit, d);
+        }
       }
       id = got.id;
       kept = static_cast<double>(got.mass) / d.one;
     }
   }
+  if (threadIdx.x == 0) write_drawn(C.out, row, id, src.at(id), ref, sum, t, kept);
+}
+// Rows that are spread, a part of the units to a workgroup: the counts, ...
+template <typename In, int T>
+__global__ void __launch_bounds__(T)
+k_sample_count(Logits<In> L, RowCalls C, FlatWs F) {
+  __shared__ uint32_t s_count[kBins];
+  const int64_t m = blockIdx.y;
+  const RowState& state = F.state[m];
+  if (state.flat != 1) return;
+  const int64_t row = C.rowsel ? C.rowsel[C.c0 + m] : C.c0 + m;
+  const RowSource<In, T> src = row_source<In, T>(L, C, m, state.top);
+  const RowDraw d = row_draw(C, row, state.top, C.S.t(row), 0.0, state.all, L.V);
+  for (int i = threadIdx.x; i < kBins; i += T) s_count[i] = 0;
+  __syncthreads();
+  count_bins(src, Binning(state.bound, d, L.V), L.units * static_cast<int>(blockIdx.x) / F.parts, L.units * static_cast<int>(blockIdx.x + 1) / F.parts, s_count);
+  __syncthreads();
+  uint32_t* const to = F.counts + (m * F.parts + blockIdx.x) * kBins;
+  for (int i = threadIdx.x; i < kBins; i += T) to[i] = s_count[i];
+}
+// ... what they say, and the sums and lists, ...
+template <typename In, int T>
+__global__ void __launch_bounds__(T)
+k_sample_sums(Logits<In> L, RowCalls C, FlatWs F) {
+  constexpr int kEach = kBins / T;
+  __shared__ RowShared<T> s;
+  const int64_t m = blockIdx.y;
+  RowState& state = F.state[m];
+  if (state.flat != 1) return;
+  const int64_t row = C.rowsel ? C.rowsel[C.c0 + m] : C.c0 + m;
+  const RowSource<In, T> src = row_source<In, T>(L, C, m, state.top);
+  const RowDraw d = row_draw(C, row, state.top, C.S.t(row), 0.0, state.all, L.V);
+  const Binning q(state.bound, d, L.V);
+  Block<T> block(s.block);
+  uint32_t counts[kEach] = {};
+  for (int p = 0; p < F.parts; ++p)
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) counts[i] += F.counts[(m * F.parts + p) * kBins + threadIdx.x * kEach + i];
+  const Bracket r = bracket_of(counts, s, block, q, state.front, state.n_front, d);
+  u64 sure = 0, rest = 0;
+  sum_units(src, q, r, d, L.units * static_cast<int>(blockIdx.x) / F.parts, L.units * static_cast<int>(blockIdx.x + 1) / F.parts, F.unit_sum + m * L.units, F.list_z + m * kListCap,
+            F.list_id + m * kListCap, &state.n_list, sure, rest);
+  rest = block.sum(rest);
   if (threadIdx.x != 0) return;
-  out.ids[row] = id;
-  const float zi = src.at(id);
-  const double gap = zi == ref ? 0.0 : static_cast<double>(zi) - static_cast<double>(ref);
-  if (out.logp) out.logp[row] = static_cast<float>(gap - log(sum));
-  if (out.logq) out.logq[row] = t > 0.0 ? static_cast<float>(gap * (c / kLog2e64) - log(kept)) : 0.f;
+  if (rest) atomicAdd(&state.rest, rest);
+  if (blockIdx.x == 0) state.bracket = r;
+}
+// ... and the token, a workgroup to a row.
+template <typename In, int T>
+__global__ void __launch_bounds__(T)
+k_sample_flat(Logits<In> L, RowCalls C, FlatWs F) {
+  extern __shared__ u64 s_unit[];                            // [units]
+  __shared__ RowShared<T> s;
+  const int64_t m = blockIdx.x;
+  const RowState& state = F.state[m];
+  if (state.flat == 0) return;
+  const int64_t row = C.rowsel ? C.rowsel[C.c0 + m] : C.c0 + m;
+  const RowSource<In, T> src = row_source<In, T>(L, C, m, state.top);
+  const float ref = src.extreme(state.top);
+  const double t = C.S.t(row);
+  const RowDraw d = row_draw(C, row, ref, t, row_uniform(C, row), state.all, L.V);
+  Block<T> block(s.block);
+  Drawn got{-1, 0};
+  const int n = state.n_list;
+  if (state.flat == 1 && n <= kListCap) {
+    for (int i = threadIdx.x; i < n; i += T) {
+      s.list_z[i] = F.list_z[m * kListCap + i];
+      s.list_id[i] = F.list_id[m * kListCap + i];
+    }
+    u64 sure = 0;
+    for (int i = threadIdx.x; i < L.units; i += T) sure += s_unit[i] = F.unit_sum[m * L.units + i];
+    sure = block.sum(sure);
+    got = draw_listed(src, s, block, s_unit, Binning(state.bound, d, L.V), state.bracket, state.n_front, n, sure, state.rest, d);
+    __syncthreads();
+  }
+  if (got.id < 0) got = draw_by_passes<In, T>(src, &s, block.turn, s_unit, d);
+  if (threadIdx.x == 0) write_drawn(C.out, row, got.id, src.at(got.id), ref, state.sum, t, static_cast<double>(got.mass) / d.one);
 }
 // what the call defines on rows that are not selected
 __global__ void __launch_bounds__(256)
@@ -950,16 +1245,19 @@ k_sample_few(const uint16_t* __restrict__ W, const uint16_t* __restrict__ H, int
 }
 
 // ------------------------------------------------------------------ host side
-constexpr int64_t kSampleRows = 4096;                        // rows of a chunk: of given logits, ...
-constexpr int64_t kHeadRows = 1024;                          // ... of a head, whose logits are kept on the way
+constexpr int64_t kSampleRows = 1024;                        // rows of a chunk
+constexpr int64_t kRowsInOne = 4;
 struct SampleWs {
   Summary A;
+  FlatWs flat;
   float* z;
   double* z64;
   char* room;
   size_t room_bytes;
   size_t bytes;
 };
+// Workgroups to a row that is spread, of as many rows; 0: the row's own does all of it.
+int flat_parts(int64_t rows) { return rows <= kRowsInOne ? 0 : static_cast<int>(std::min<int64_t>(std::max<int64_t>(2048 / rows, 4), 16)); }
 int units_of(int V) { return static_cast<int>(cdiv(V, kUnit)); }
 void carve(Carver& c, SampleWs& w, int64_t rows, int V) {
   w = SampleWs{};
@@ -968,6 +1266,14 @@ void carve(Carver& c, SampleWs& w, int64_t rows, int V) {
   w.A.unit = c.take<float>(units);
   w.A.mass = c.take<double>(units);
   w.A.sum = c.take<double>(units);
+  w.flat.parts = flat_parts(rows);
+  if (w.flat.parts > 0) {
+    w.flat.state = c.take<RowState>(rows);
+    w.flat.counts = c.take<uint32_t>(static_cast<size_t>(std::min(rows * 16, std::max<int64_t>(2048, rows * 4))) * kBins);   // as many as any count of rows up to it takes
+    w.flat.unit_sum = c.take<u64>(units);
+    w.flat.list_z = c.take<float>(static_cast<size_t>(rows) * kListCap);
+    w.flat.list_id = c.take<int>(static_cast<size_t>(rows) * kListCap);
+  }
   w.bytes = c.off;
 }
 void carve(Carver& c, SampleWs& w, int64_t rows, int d, int V, umas_dtype dt) {
@@ -1008,18 +1314,36 @@ int bits_of(int V) {
   while ((int64_t{1} << b) < V) ++b;
   return std::min(51, 62 - b);
 }
-constexpr int kRowT = 1024, kPlainT = 256;
+constexpr int kRowT = 1024, kPlainT = 256, kFlatT = 512;
 template <typename In>
 umas_status sample_rows(const Logits<In>& L, const Settings& S, const int32_t* rowsel, int64_t c0, int64_t rows, const SampleWs& w, const float* u, const SampleOut& out,
                         hipStream_t st) {
-  hipLaunchKernelGGL(k_sample_open<In>, dim3(cdiv(L.units, kOpenUnits), static_cast<unsigned>(rows)), dim3(kOpenT), 0, st, L, S, rowsel, c0, w.A);
+  const unsigned n = static_cast<unsigned>(rows);
+  const size_t unit_bytes = L.units * sizeof(u64);
+  hipLaunchKernelGGL(k_sample_open<In>, dim3(cdiv(L.units, kOpenUnits), n), dim3(kOpenT), 0, st, L, S, rowsel, c0, w.A);
   UMAS_LAUNCHED("k_sample_open");
   const bool plain = !S.top_k_of && !S.top_p_of && !S.min_p_of && S.min_p == 0.0 && S.top_p == 1.0 && (S.top_k == 0 || S.top_k >= L.V);
   const bool greedy = !S.temperature_of && S.temperature == 0.0;
-  if (plain || greedy) hipLaunchKernelGGL((k_sample_row<In, kPlainT, false>), dim3(static_cast<unsigned>(rows)), dim3(kPlainT), 0, st, L, S, rowsel, c0, w.A, u, 0, out);
-  else
-    hipLaunchKernelGGL((k_sample_row<In, kRowT, true>), dim3(static_cast<unsigned>(rows)), dim3(kRowT), L.units * sizeof(u64), st, L, S, rowsel, c0, w.A, u, bits_of(L.V), out);
+  const RowCalls C{S, rowsel, c0, w.A, u, out, bits_of(L.V)};
+  if (plain || greedy) {
+    hipLaunchKernelGGL((k_sample_row<In, kPlainT, Filter::kNone>), dim3(n), dim3(kPlainT), 0, st, L, C, w.flat);
+    UMAS_LAUNCHED("k_sample_row");
+    return UMAS_OK;
+  }
+  if (w.flat.parts == 0) {
+    hipLaunchKernelGGL((k_sample_row<In, kRowT, Filter::kSomeInOne>), dim3(n), dim3(kRowT), unit_bytes, st, L, C, w.flat);
+    UMAS_LAUNCHED("k_sample_row");
+    return UMAS_OK;
+  }
+  const dim3 parts(w.flat.parts, n);
+  hipLaunchKernelGGL((k_sample_row<In, kRowT, Filter::kSome>), dim3(n), dim3(kRowT), 0, st, L, C, w.flat);
   UMAS_LAUNCHED("k_sample_row");
+  hipLaunchKernelGGL((k_sample_count<In, kFlatT>), parts, dim3(kFlatT), 0, st, L, C, w.flat);
+  UMAS_LAUNCHED("k_sample_count");
+  hipLaunchKernelGGL((k_sample_sums<In, kFlatT>), parts, dim3(kFlatT), 0, st, L, C, w.flat);
+  UMAS_LAUNCHED("k_sample_sums");
+  hipLaunchKernelGGL((k_sample_flat<In, kRowT>), dim3(n), dim3(kRowT), unit_bytes, st, L, C, w.flat);
+  UMAS_LAUNCHED("k_sample_flat");
   return UMAS_OK;
 }
 
@@ -1070,7 +1394,7 @@ extern "C" size_t umas_sample_tokens_workspace_bytes_min(int64_t n_sel, int32_t 
 }
 extern "C" size_t umas_sample_tokens_workspace_bytes(int64_t n_sel, int32_t d, int32_t V, umas_dtype dtype) {
   if (n_sel < 0 || d < 1 || V < 1 || V > kMaxSampleV) return 0;
-  return head_bytes(n_sel, kHeadRows, d, V, dtype);
+  return head_bytes(n_sel, kSampleRows, d, V, dtype);
 }
 
 extern "C" umas_status umas_sample_tokens(const void* H, const void* W, umas_dtype dtype, int64_t n_rows, int32_t d, int32_t V, const int32_t* rowsel, int64_t n_sel,
@@ -1093,7 +1417,7 @@ extern "C" umas_status umas_sample_tokens(const void* H, const void* W, umas_dty
     UMAS_LAUNCHED("k_sample_clear");
   }
   if (n_sel == 0) return UMAS_OK;
-  int64_t cap = std::min(n_sel, kHeadRows);
+  int64_t cap = std::min(n_sel, kSampleRows);
   while (cap > 256 && head_bytes(n_sel, cap, d, V, dtype) > workspace_bytes) cap = std::max<int64_t>(round_up(cap / 2, 256), 256);
   Carver c(workspace);
   SampleWs w;
