@@ -41,8 +41,8 @@ struct Weigh {
   __device__ __forceinline__ Weigh(float largest, double c_) : top(largest) {
     const uint32_t u = __float_as_uint(largest);             // the next number below it
     const float below = largest == 0.f ? __uint_as_float(0x80000001u) : __uint_as_float(largest > 0.f ? u - 1 : u + 1);
-    c = fmax(fmin(c_, 1000.0 / (top - static_cast<double>(below))), 1e-30);   // (a temperature without end: all are 1 but those of -infinity)
-    least = fminf(static_cast<float>(fmax(top - 1000.0 / c, -3e38)), below);
+    c = fmax(fmin(c_, static_cast<double>(1000.f * __builtin_amdgcn_rcpf(largest - below))), 1e-30);   // (a temperature without end: all are 1 but those of -infinity)
+    least = fminf(fmaxf(largest - 1000.f * __builtin_amdgcn_rcpf(static_cast<float>(fmin(c, 1e38))), -3e38f), below);
   }
   __device__ __forceinline__ float next_above() const {      // the largest logit's next number
     const float x = static_cast<float>(top);
@@ -70,7 +70,7 @@ constexpr double kLog2e64 = 1.4426950408889634074;
 // log x of 1 <= x: the float32 one and a step of Newton's, whose error is half the square of what that one is off by.  (The library's took 3 us of a row.)
 __device__ __forceinline__ double log_of(double x) {
   const float y = __logf(static_cast<float>(x));
-  return static_cast<double>(y) + (x * Weigh(0.f, kLog2e64)(-y) - 1.0);
+  return static_cast<double>(y) + (x * Weigh(0.f, kLog2e64)(-y) - 1.0);   // (the largest is 0, as y >= 0)
 }
 // 2^t, nearly: for estimates.
 __device__ __forceinline__ double exp2_near(double t) { return static_cast<double>(__builtin_amdgcn_exp2f(static_cast<float>(t))); }
@@ -101,7 +101,8 @@ struct Logits {
 // What the first launch leaves, per row.
 struct Summary {
   float *group, *unit;                                       // [rows][units * 16], [rows][units]: maxima; -infinity where nothing counts
-  double *mass, *sum;                                        // [rows][units]: sum of w at T and of exp(z - max) at 1, relative to the unit's maximum
+  float* ref;                                                // [rows][units]: what the sums are relative to, the larger maximum of two units
+  double *mass, *sum;                                        // [rows][units]: sum of w at T and of exp(z - ref) at 1
 };
 
 // ------------------------------------------------------------------ loads
@@ -123,91 +124,136 @@ __device__ __forceinline__ int token_of(int unit, int i) {    // of the lane's i
   return unit * kUnit + (i / kRun<In>) * (kRun<In> * kWave) + (threadIdx.x & 63) * kRun<In> + i % kRun<In>;
 }
 template <typename In>
-__device__ __forceinline__ void load_unit(const In* __restrict__ z, int V, int unit, float (&x)[kPerLane]) {
+__device__ __forceinline__ void load_unit(const In* __restrict__ z, int V, int unit, float (&x)[kPerLane]) {   // as they are, numbers or not
   typedef uint32_t u32x4a __attribute__((ext_vector_type(4), aligned(2)));
   constexpr int R = kRun<In>;
+  if ((unit + 1) * kUnit <= V) {
 #pragma unroll
-  for (int i = 0; i < kPerLane; i += R) {
-    const int v = token_of<In>(unit, i);
-    if (v + R <= V) {
+    for (int i = 0; i < kPerLane; i += R) {
+      const int v = token_of<In>(unit, i);
       if constexpr (std::is_same<In, double>::value) {
 #pragma unroll
-        for (int j = 0; j < R; ++j) x[i + j] = logit(z[v + j]);
+        for (int j = 0; j < R; ++j) x[i + j] = static_cast<float>(z[v + j]);
       } else {
         const u32x4a w = *reinterpret_cast<const u32x4a*>(z + v);
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
           if constexpr (R == 8) {
-            x[i + 2 * j] = logit(__uint_as_float(w[j] << 16));
-            x[i + 2 * j + 1] = logit(__uint_as_float(w[j] & 0xFFFF0000u));
+            x[i + 2 * j] = __uint_as_float(w[j] << 16);
+            x[i + 2 * j + 1] = __uint_as_float(w[j] & 0xFFFF0000u);
           } else {
-            x[i + j] = logit(__uint_as_float(w[j]));
+            x[i + j] = __uint_as_float(w[j]);
           }
         }
       }
-    } else {
-#pragma unroll
-      for (int j = 0; j < R; ++j) x[i + j] = v + j < V ? logit(z[v + j]) : -INFINITY;
     }
+    return;
+  }
+#pragma unroll
+  for (int i = 0; i < kPerLane; ++i) {
+    const int v = token_of<In>(unit, i);
+    x[i] = v < V ? logit(z[v]) : -INFINITY;
   }
 }
 
 // ------------------------------------------------------------------ first launch
-constexpr int kOpenT = 256, kOpenUnits = kOpenT / kWave;
+// A wavefront takes two units, whose largest logit is found and whose sums are exchanged together.
+constexpr int kOpenT = 256, kOpenPairs = kOpenT / kWave;
 template <typename In>
-__global__ void __launch_bounds__(kOpenT)
-k_sample_open(Logits<In> L, Settings S, const int32_t* __restrict__ rowsel, int64_t c0, Summary out) {
-  constexpr int R = kRun<In>, kLanes = kGroup / R;            // lanes to a group
-  const int lane = threadIdx.x & 63, unit = blockIdx.x * kOpenUnits + (threadIdx.x >> 6);
-  if (unit >= L.units) return;
-  const int64_t m = blockIdx.y, row = rowsel ? rowsel[c0 + m] : c0 + m;
-  float x[kPerLane];
-  load_unit(L.row(m), L.V, unit, x);
-  const int64_t at = m * L.units + unit;
+__device__ __forceinline__ float group_maxima(const float (&x)[kPerLane], float (&g)[kPerLane / kRun<In>]) {   // ... and the lane's
+  constexpr int R = kRun<In>;
   float top = -INFINITY;
 #pragma unroll
   for (int i = 0; i < kPerLane; i += R) {
-    float g = x[i];
+    float m = x[i];
 #pragma unroll
-    for (int j = 1; j < R; ++j) g = larger(g, x[i + j]);
-#pragma unroll
-    for (int s = 0; s < 4; ++s)
-      if (1 << s < kLanes) g = larger(g, s == 0 ? lane_xor<1>(g) : s == 1 ? lane_xor<2>(g) : s == 2 ? lane_xor<4>(g) : lane_xor<8>(g));
-    if (lane % kLanes == 0) out.group[at * kGroupsPerUnit + i / R * R + lane / kLanes] = g;
-    top = larger(top, g);
+    for (int j = 1; j < R; ++j) m = larger(m, x[i + j]);
+    m = larger(m, lane_xor<1>(m));
+    m = larger(m, lane_xor<2>(m));
+    m = larger(m, lane_xor<4>(m));
+    if constexpr (kGroup / R > 8) m = larger(m, lane_xor<8>(m));
+    g[i / R] = m;
+    top = larger(top, m);
   }
+  if constexpr (kGroup / R <= 8) top = larger(top, lane_xor<8>(top));
+  top = larger(top, lane_xor<16>(top));
+  return larger(top, lane_xor<32>(top));
+}
+// Of two numbers, summed over the wavefront: the first in the lower half's lanes, the second in the upper half's.
+__device__ __forceinline__ double halves_sum(double a, double b) {
+  const bool upper = threadIdx.x & 32;
+  const double mine = upper ? b : a, other = upper ? a : b;
+  double x = mine + bits_of(lane_xor<32>(bits_in(other)), double());
+  x += bits_of(lane_xor<1>(bits_in(x)), double());
+  x += bits_of(lane_xor<2>(bits_in(x)), double());
+  x += bits_of(lane_xor<4>(bits_in(x)), double());
+  x += bits_of(lane_xor<8>(bits_in(x)), double());
+  return x + bits_of(lane_xor<16>(bits_in(x)), double());
+}
+template <typename In>
+__global__ void __launch_bounds__(kOpenT, 8)
+k_sample_open(Logits<In> L, Settings S, const int32_t* __restrict__ rowsel, int64_t c0, Summary out) {
+  constexpr int R = kRun<In>, kLanes = kGroup / R;            // lanes to a group
+  const int lane = threadIdx.x & 63, u0 = 2 * (blockIdx.x * kOpenPairs + static_cast<int>(threadIdx.x >> 6));
+  if (u0 >= L.units) return;
+  const int64_t m = blockIdx.y, row = rowsel ? rowsel[c0 + m] : c0 + m;
+  float x[2][kPerLane], g[2][kPerLane / R], top[2];
+  load_unit(L.row(m), L.V, u0, x[0]);
+  load_unit(L.row(m), L.V, u0 + 1, x[1]);                    // of one that does not exist: nothing
 #pragma unroll
-  for (int s = 3; s < 6; ++s)
-    if (1 << s >= kLanes) top = larger(top, s == 3 ? lane_xor<8>(top) : s == 4 ? lane_xor<16>(top) : lane_xor<32>(top));
-  double mass = 0.0, sum = 0.0;
-  if (top > -INFINITY) {
+  for (int p = 0; p < 2; ++p) top[p] = group_maxima<In>(x[p], g[p]);
+  if (!(top[0] == top[0] && top[1] == top[1])) {             // some are no number: as if they were -infinity
+#pragma unroll
+    for (int p = 0; p < 2; ++p) {
+#pragma unroll
+      for (int i = 0; i < kPerLane; ++i) x[p][i] = logit(x[p][i]);
+      top[p] = group_maxima<In>(x[p], g[p]);
+    }
+  }
+  const int64_t at = m * L.units + u0;
+#pragma unroll
+  for (int p = 0; p < 2; ++p) {
+    if (u0 + p >= L.units) continue;
+#pragma unroll
+    for (int i = 0; i < kPerLane / R; ++i)
+      if (lane % kLanes == 0) out.group[(at + p) * kGroupsPerUnit + i * R + lane / kLanes] = g[p][i];
+  }
+  const float most = larger(top[0], top[1]);
+  double mass[2] = {0.0, 0.0}, sum[2] = {0.0, 0.0};
+  if (most > -INFINITY) {
     const double t = S.t(row);
     const bool drawn = t > 0.0;
-    const Extreme extreme(top);
+    const Extreme extreme(most);
     if (extreme.is)
 #pragma unroll
-      for (int i = 0; i < kPerLane; ++i) x[i] = extreme(x[i]);
-    const float ref = extreme(top);
-    if (drawn) {
-      const Weigh w{ref, scale_of(t)};
+      for (int p = 0; p < 2; ++p)
 #pragma unroll
-      for (int i = 0; i < kPerLane; ++i) mass += w(x[i]);
-      mass = lanes_sum(mass);
+        for (int i = 0; i < kPerLane; ++i) x[p][i] = extreme(x[p][i]);
+    const float ref = extreme(most);
+    if (drawn) {
+      const Weigh w(ref, scale_of(t));
+#pragma unroll
+      for (int p = 0; p < 2; ++p)
+#pragma unroll
+        for (int i = 0; i < kPerLane; ++i) mass[p] += w(x[p][i]);
+      mass[0] = halves_sum(mass[0], mass[1]);
     }
     if (drawn && t == 1.0) {
-      sum = mass;
+      sum[0] = mass[0];
     } else {
       constexpr float kLog2e = 1.44269504088896341f;
 #pragma unroll
-      for (int i = 0; i < kPerLane; ++i) sum += static_cast<double>(__builtin_amdgcn_exp2f((x[i] - ref) * kLog2e));
-      sum = lanes_sum(sum);
+      for (int p = 0; p < 2; ++p)
+#pragma unroll
+        for (int i = 0; i < kPerLane; ++i) sum[p] += static_cast<double>(__builtin_amdgcn_exp2f((x[p][i] - ref) * kLog2e));
+      sum[0] = halves_sum(sum[0], sum[1]);
     }
   }
-  if (lane == 0) {
-    out.unit[at] = top;
-    out.mass[at] = mass;
-    out.sum[at] = sum;
-  }
+  if (lane % 32 != 0 || u0 + lane / 32 >= L.units) return;
+  out.unit[at + lane / 32] = lane == 0 ? top[0] : top[1];
+  out.ref[at + lane / 32] = most;
+  out.mass[at + lane / 32] = mass[0];
+  out.sum[at + lane / 32] = sum[0];
 }
 
 // ------------------------------------------------------------------ second launch
@@ -294,7 +340,7 @@ struct RowSource {
   int V, units;
   const float* unit_max;                                     // of the row
   Extreme extreme;
-  __device__ __forceinline__ float at(int v) const { return v < V ? extreme(logit(z[v])) : -INFINITY; }
+  __device__ __forceinline__ float at(int v) const { return static_cast<unsigned>(v) < static_cast<unsigned>(V) ? extreme(logit(z[v])) : -INFINITY; }   // -1: no token
   // f(z, token) for every token with z > -infinity, and z >= lo; others may come.  `after` once a unit, by its wavefront, also where the unit has none
   template <class F, class G>
   __device__ __forceinline__ void each(float lo, F f, G after) const {
@@ -305,7 +351,7 @@ struct RowSource {
         load_unit(z, V, u, x);
 #pragma unroll
         for (int i = 0; i < kPerLane; ++i) {
-          const float zi = extreme(x[i]);
+          const float zi = extreme(logit(x[i]));
           if (zi > -INFINITY) f(zi, token_of<In>(u, i));
           if (i % 4 == 3) __builtin_amdgcn_sched_barrier(0);  // sixteen weights at once take more registers than there are
         }
@@ -707,8 +753,8 @@ __device__ __forceinline__ void count_bins(const RowSource<In, T>& row, const Bi
   }
 }
 // counts: this thread's bins, kBins / T of them from threadIdx.x * kBins / T on.
-template <int T>
-__device__ __forceinline__ Bracket bracket_of(const uint32_t (&counts)[kBins / T], RowShared<T>& s, Block<T>& all, const Binning& q, u64 front, int n_front, const RowDraw& d) {
+template <int T, class Shared>
+__device__ __forceinline__ Bracket bracket_of(const uint32_t (&counts)[kBins / T], Shared& s, Block<T>& all, const Binning& q, u64 front, int n_front, const RowDraw& d) {
   constexpr int kEach = kBins / T;
   const double at_bound = d.w(q.bound);
   u64 n_mine = 0, n_all;
@@ -865,11 +911,16 @@ __device__ __forceinline__ Drawn draw_listed(const RowSource<In, T>& row, RowSha
   return Drawn{token_beyond(row, s, all, s_unit, kept, d.target(mass)), mass};
 }
 
+// The least of the lanes' numbers that is not negative into *to, which all but the first such lane of a wavefront leave alone: numbers rise with the lanes.
+__device__ __forceinline__ void first_of(int* to, int mine) {
+  const u64 have = __ballot(mine >= 0);
+  if (have && (threadIdx.x & 63) == static_cast<unsigned>(__ffsll(static_cast<long long>(have)) - 1)) atomicMin(reinterpret_cast<unsigned*>(to), static_cast<unsigned>(mine));
+}
 // No filter: the unit from the units' masses, then the token.
 template <typename In, int T, class Shared>
-__device__ __forceinline__ Drawn draw_unfiltered(const RowSource<In, T>& row, Shared& s, Block<T>& block, const double* mass_of, const Weigh& w, double u, double all) {
+__device__ __forceinline__ Drawn draw_unfiltered(const RowSource<In, T>& row, Shared& s, Block<T>& block, const float* ref_of, const double* mass_of, const Weigh& w, double u, double all) {
   const double target = u * all;
-  auto mass = [&](int i) { return mass_of[i] * w(row.extreme(row.unit_max[i])); };
+  auto mass = [&](int i) { return mass_of[i] * w(row.extreme(ref_of[i])); };
   if (threadIdx.x == 0) s.found_id = -1;
   int unit = -1;
   double before = 0.0;
@@ -878,7 +929,7 @@ __device__ __forceinline__ Drawn draw_unfiltered(const RowSource<In, T>& row, Sh
     const double mine = i < row.units ? mass(i) : 0.0;
     double sum;
     const double excl = before + block.scan(mine, &sum);
-    if (mine > kNoWeight && excl + mine > target) atomicMin(reinterpret_cast<unsigned*>(&s.found_id), static_cast<unsigned>(i));
+    first_of(&s.found_id, mine > kNoWeight && excl + mine > target ? i : -1);
     __syncthreads();
     unit = s.found_id;
     if (i == unit) s.found_drest = target - excl;
@@ -906,18 +957,18 @@ __device__ __forceinline__ Drawn draw_unfiltered(const RowSource<In, T>& row, Sh
     sum += mine[i];
   }
   double run = block.scan(sum, &total);
+  int passes = -1;
 #pragma unroll
-  for (int i = kEach - 1; i >= 0; --i) {                     // the thread's first that passes
-    double to = run;
-#pragma unroll
-    for (int j = 0; j <= i; ++j) to += mine[j];
-    if (mine[i] > 0.0 && to > rest) atomicMin(reinterpret_cast<unsigned*>(&s.found_id), static_cast<unsigned>(v + i));
+  for (int i = 0; i < kEach; ++i) {
+    run += mine[i];
+    if (passes < 0 && mine[i] > 0.0 && run > rest) passes = v + i;
   }
+  first_of(&s.found_id, passes);
   __syncthreads();
   const int id = s.found_id;
   __syncthreads();
   if (id >= 0) return Drawn{id, 0};
-  if (last >= 0) atomicMax(&s.found_id, last);               // the unit's sum, added up in another order, ends above the target: its last token
+  if (last >= 0) atomicMax(&s.found_id, last);               // u = 1, or the unit's sum, added up in another order, ends above the target: its last token
   __syncthreads();
   return Drawn{s.found_id, 0};
 }
@@ -944,6 +995,14 @@ struct PlainShared {
   u64 block[2][2][T / kWave];
   double found_drest;
   int found_id;
+};
+template <int T>
+struct BinShared {
+  u64 block[2][2][T / kWave];
+  u64 found_rest;
+  double found_drest;
+  uint32_t found_bin;
+  int found_id, n_groups;
 };
 // What the kernels of a row have in common: its largest logit, sums and settings.
 struct RowCalls {
@@ -1004,6 +1063,7 @@ k_sample_row(Logits<In> L, RowCalls C, FlatWs F) {
   __shared__ std::conditional_t<FILTER == Filter::kNone, PlainShared<T>, RowShared<T>> s;
   const int64_t m = blockIdx.x, row = C.rowsel ? C.rowsel[C.c0 + m] : C.c0 + m;
   const float* const unit_max = C.A.unit + m * L.units;
+  const float* const ref_of = C.A.ref + m * L.units;
   const double *const mass_of = C.A.mass + m * L.units, *const sum_of = C.A.sum + m * L.units;
   const double t = C.S.t(row), u = row_uniform(C, row);
   float top = -INFINITY;
@@ -1024,7 +1084,7 @@ k_sample_row(Logits<In> L, RowCalls C, FlatWs F) {
   const Weigh w(ref, scale_of(t)), w1(ref, kLog2e64);
   double sum = 0.0, all = 0.0;                               // of exp(z - top), for the log-prob of the softmax itself, and of the weights
   for (int i = threadIdx.x; i < L.units; i += T) {
-    const float x = src.extreme(unit_max[i]);
+    const float x = src.extreme(ref_of[i]);
     sum += sum_of[i] * w1(x);
     all += mass_of[i] * w(x);
   }
@@ -1034,11 +1094,11 @@ k_sample_row(Logits<In> L, RowCalls C, FlatWs F) {
   if (!(t > 0.0)) {
     id = largest(src, s, top);
   } else if constexpr (FILTER == Filter::kNone) {
-    id = draw_unfiltered(src, s, block, mass_of, w, u, all).id;
+    id = draw_unfiltered(src, s, block, ref_of, mass_of, w, u, all).id;
   } else {
     const RowDraw d = row_draw(C, row, ref, t, u, all, L.V);
     if (d.k == 0 && d.p == 1.0 && d.m == 0.0) {
-      id = draw_unfiltered(src, s, block, mass_of, w, u, all).id;
+      id = draw_unfiltered(src, s, block, ref_of, mass_of, w, u, all).id;
     } else {
       const float* const group_max = C.A.group + m * L.units * kGroupsPerUnit;
       float bound = L.V <= kRanked ? -INFINITY : front_bound<T>(group_max, L.units * kGroupsPerUnit, s);
@@ -1078,7 +1138,7 @@ k_sample_row(Logits<In> L, RowCalls C, FlatWs F) {
             uint32_t counts[kBins / T];
 #pragma unroll
             for (int i = 0; i < kBins / T; ++i) counts[i] = s_count[threadIdx.x * (kBins / T) + i];
-            const Bracket r = bracket_of(counts, s, block, q, front, n, d);
+            const Bracket r = bracket_of<T>(counts, s, block, q, front, n, d);
             if (threadIdx.x == 0) s.n_list = n;
             __syncthreads();
             u64 sure = 0, rest = 0;
@@ -1096,30 +1156,12 @@ k_sample_row(Logits<In> L, RowCalls C, FlatWs F) {
   }
   if (threadIdx.x == 0) write_drawn(C.out, row, id, src.at(id), ref, sum, t, kept);
 }
-// Rows that are spread, a part of the units to a workgroup: the counts, ...
+// Rows that are spread, a part of the units to a workgroup: the counts, ...  (A row's last workgroup to find out what they say would need a fence, whose
+// writing back of the caches took the launch from 17 us to 165.)
 template <typename In, int T>
 __global__ void __launch_bounds__(T)
 k_sample_count(Logits<In> L, RowCalls C, FlatWs F) {
   __shared__ uint32_t s_count[kBins];
-  const int64_t m = blockIdx.y;
-  const RowState& state = F.state[m];
-  if (state.flat != 1) return;
-  const int64_t row = C.rowsel ? C.rowsel[C.c0 + m] : C.c0 + m;
-  const RowSource<In, T> src = row_source<In, T>(L, C, m, state.top);
-  const RowDraw d = row_draw(C, row, state.top, C.S.t(row), 0.0, state.all, L.V);
-  for (int i = threadIdx.x; i < kBins; i += T) s_count[i] = 0;
-  __syncthreads();
-  count_bins(src, Binning(state.bound, d, L.V), L.units * static_cast<int>(blockIdx.x) / F.parts, L.units * static_cast<int>(blockIdx.x + 1) / F.parts, s_count);
-  __syncthreads();
-  uint32_t* const to = F.counts + (m * F.parts + blockIdx.x) * kBins;
-  for (int i = threadIdx.x; i < kBins; i += T) to[i] = s_count[i];
-}
-// ... what they say, and the sums and lists, ...
-template <typename In, int T>
-__global__ void __launch_bounds__(T)
-k_sample_sums(Logits<In> L, RowCalls C, FlatWs F) {
-  constexpr int kEach = kBins / T;
-  __shared__ RowShared<T> s;
   const int64_t m = blockIdx.y;
   RowState& state = F.state[m];
   if (state.flat != 1) return;
@@ -1127,19 +1169,52 @@ k_sample_sums(Logits<In> L, RowCalls C, FlatWs F) {
   const RowSource<In, T> src = row_source<In, T>(L, C, m, state.top);
   const RowDraw d = row_draw(C, row, state.top, C.S.t(row), 0.0, state.all, L.V);
   const Binning q(state.bound, d, L.V);
-  Block<T> block(s.block);
+  for (int i = threadIdx.x; i < kBins; i += T) s_count[i] = 0;
+  __syncthreads();
+  count_bins(src, q, L.units * static_cast<int>(blockIdx.x) / F.parts, L.units * static_cast<int>(blockIdx.x + 1) / F.parts, s_count);
+  __syncthreads();
+  uint32_t* const to = F.counts + (m * F.parts + blockIdx.x) * kBins;
+  for (int i = threadIdx.x; i < kBins; i += T) to[i] = s_count[i];
+}
+// ... what they say, ...
+template <int T>
+__global__ void __launch_bounds__(T)
+k_sample_bracket(RowCalls C, FlatWs F, int V) {
+  constexpr int kEach = kBins / T;
+  __shared__ BinShared<T> s;
+  const int64_t m = blockIdx.x;
+  RowState& state = F.state[m];
+  if (state.flat != 1) return;
+  const int64_t row = C.rowsel ? C.rowsel[C.c0 + m] : C.c0 + m;
+  const RowDraw d = row_draw(C, row, state.top, C.S.t(row), 0.0, state.all, V);
+  const Binning q(state.bound, d, V);
   uint32_t counts[kEach] = {};
   for (int p = 0; p < F.parts; ++p)
 #pragma unroll
     for (int i = 0; i < kEach; ++i) counts[i] += F.counts[(m * F.parts + p) * kBins + threadIdx.x * kEach + i];
-  const Bracket r = bracket_of(counts, s, block, q, state.front, state.n_front, d);
+  Block<T> block(s.block);
+  const Bracket r = bracket_of<T>(counts, s, block, q, state.front, state.n_front, d);
+  if (threadIdx.x == 0) state.bracket = r;
+}
+// ... then the sums and lists, ...
+constexpr int kSumUnits = 16;                                // of a workgroup
+template <typename In, int T>
+__global__ void __launch_bounds__(T, 6)
+k_sample_sums(Logits<In> L, RowCalls C, FlatWs F) {
+  __shared__ u64 s_block[2][2][T / kWave];
+  const int64_t m = blockIdx.y;
+  RowState& state = F.state[m];
+  if (state.flat != 1) return;
+  const int64_t row = C.rowsel ? C.rowsel[C.c0 + m] : C.c0 + m;
+  const RowSource<In, T> src = row_source<In, T>(L, C, m, state.top);
+  const RowDraw d = row_draw(C, row, state.top, C.S.t(row), 0.0, state.all, L.V);
+  Block<T> block(s_block);
   u64 sure = 0, rest = 0;
-  sum_units(src, q, r, d, L.units * static_cast<int>(blockIdx.x) / F.parts, L.units * static_cast<int>(blockIdx.x + 1) / F.parts, F.unit_sum + m * L.units, F.list_z + m * kListCap,
-            F.list_id + m * kListCap, &state.n_list, sure, rest);
+  const int u0 = blockIdx.x * kSumUnits;
+  sum_units(src, Binning(state.bound, d, L.V), state.bracket, d, u0, min(u0 + kSumUnits, L.units), F.unit_sum + m * L.units, F.list_z + m * kListCap, F.list_id + m * kListCap,
+            &state.n_list, sure, rest);
   rest = block.sum(rest);
-  if (threadIdx.x != 0) return;
-  if (rest) atomicAdd(&state.rest, rest);
-  if (blockIdx.x == 0) state.bracket = r;
+  if (threadIdx.x == 0 && rest) atomicAdd(&state.rest, rest);
 }
 // ... and the token, a workgroup to a row.
 template <typename In, int T>
@@ -1264,6 +1339,7 @@ void carve(Carver& c, SampleWs& w, int64_t rows, int V) {
   const size_t units = static_cast<size_t>(rows) * units_of(V);
   w.A.group = c.take<float>(units * kGroupsPerUnit);
   w.A.unit = c.take<float>(units);
+  w.A.ref = c.take<float>(units);
   w.A.mass = c.take<double>(units);
   w.A.sum = c.take<double>(units);
   w.flat.parts = flat_parts(rows);
@@ -1320,7 +1396,7 @@ umas_status sample_rows(const Logits<In>& L, const Settings& S, const int32_t* r
                         hipStream_t st) {
   const unsigned n = static_cast<unsigned>(rows);
   const size_t unit_bytes = L.units * sizeof(u64);
-  hipLaunchKernelGGL(k_sample_open<In>, dim3(cdiv(L.units, kOpenUnits), n), dim3(kOpenT), 0, st, L, S, rowsel, c0, w.A);
+  hipLaunchKernelGGL(k_sample_open<In>, dim3(cdiv(L.units, 2 * kOpenPairs), n), dim3(kOpenT), 0, st, L, S, rowsel, c0, w.A);
   UMAS_LAUNCHED("k_sample_open");
   const bool plain = !S.top_k_of && !S.top_p_of && !S.min_p_of && S.min_p == 0.0 && S.top_p == 1.0 && (S.top_k == 0 || S.top_k >= L.V);
   const bool greedy = !S.temperature_of && S.temperature == 0.0;
@@ -1340,7 +1416,9 @@ umas_status sample_rows(const Logits<In>& L, const Settings& S, const int32_t* r
   UMAS_LAUNCHED("k_sample_row");
   hipLaunchKernelGGL((k_sample_count<In, kFlatT>), parts, dim3(kFlatT), 0, st, L, C, w.flat);
   UMAS_LAUNCHED("k_sample_count");
-  hipLaunchKernelGGL((k_sample_sums<In, kFlatT>), parts, dim3(kFlatT), 0, st, L, C, w.flat);
+  hipLaunchKernelGGL((k_sample_bracket<kFlatT>), dim3(n), dim3(kFlatT), 0, st, C, w.flat, L.V);
+  UMAS_LAUNCHED("k_sample_bracket");
+  hipLaunchKernelGGL((k_sample_sums<In, kFlatT>), dim3(cdiv(L.units, kSumUnits), n), dim3(kFlatT), 0, st, L, C, w.flat);
   UMAS_LAUNCHED("k_sample_sums");
   hipLaunchKernelGGL((k_sample_flat<In, kRowT>), dim3(n), dim3(kRowT), unit_bytes, st, L, C, w.flat);
   UMAS_LAUNCHED("k_sample_flat");
