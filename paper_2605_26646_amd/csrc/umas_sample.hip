@@ -192,9 +192,10 @@ __device__ __forceinline__ double halves_sum(double a, double b) {
 }
 template <typename In>
 __global__ void __launch_bounds__(kOpenT, 8)
-k_sample_open(Logits<In> L, Settings S, const int32_t* __restrict__ rowsel, int64_t c0, Summary out) {
+k_sample_open(Logits<In> L, Settings S, const int32_t* __restrict__ rowsel, int64_t c0, Summary out, int* __restrict__ count) {
   constexpr int R = kRun<In>, kLanes = kGroup / R;            // lanes to a group
   const int lane = threadIdx.x & 63, u0 = 2 * (blockIdx.x * kOpenPairs + static_cast<int>(threadIdx.x >> 6));
+  if (count && blockIdx.x == 0 && blockIdx.y == 0 && threadIdx.x == 0) *count = 0;
   if (u0 >= L.units) return;
   const int64_t m = blockIdx.y, row = rowsel ? rowsel[c0 + m] : c0 + m;
   float x[2][kPerLane], g[2][kPerLane / R], top[2];
@@ -257,9 +258,9 @@ k_sample_open(Logits<In> L, Settings S, const int32_t* __restrict__ rowsel, int6
 }
 
 // ------------------------------------------------------------------ second launch
-constexpr int kBins = 2048;
+constexpr int kBins = 2048, kCounts = 4096;                  // of eleven bits of a key, and of distances to the front
 constexpr int kTopRank = 64;
-constexpr int kListCap = 4096, kRanked = 256;                // tokens of a list, and of one that is ordered by comparing all with all
+constexpr int kListCap = 2048, kRanked = 256;                // tokens of a list, and of one that is ordered by comparing all with all
 constexpr int kGroupCap = 1024;
 // Sums and scans over a workgroup of T threads: what the wavefronts have goes through one of two buffers in turn, so that one barrier is enough.
 template <int T>
@@ -321,17 +322,43 @@ struct Block {
     return v;
   }
 };
-template <int T>
+// LIST: tokens that are listed; WEIGHTS: their weights beside them.
+template <int T, int LIST = kListCap, bool WEIGHTS = true>
 struct RowShared {
+  static constexpr int kList = LIST;
   u64 block[2][2][T / kWave];
   u64 bins[kBins];                                           // masses or counts
-  float list_z[kListCap];
-  int list_id[kListCap];
+  u64 list_w[WEIGHTS ? LIST : 1];
+  float list_z[LIST];
+  int list_id[LIST];
   float top[4][kWave];
   u64 found_above, found_here, found_rest;
   double found_drest;
   uint32_t found_bin;
   int found_id, n_list, n_groups;
+};
+// A row's settings and what the first launch says about it.
+struct RowDraw {
+  float top;
+  Weigh w;
+  int k;                                                     // 0: none
+  double p, m, u;                                            // p = 1, m = 0: none
+  double all;                                                // the mass of all tokens, in units of the largest weight
+  double one;                                                // 1 in units of the whole numbers
+  int id_bits;                                               // of a token's number
+  __device__ __forceinline__ bool by_min() const { return m > 0.0; }
+  // x * one, one at most 2^51, rounded to nearest by the addition of 2^52, whose bits are kNothing; of a weight that min_p does not leave nothing
+  static constexpr u64 kNothing = 0x4330000000000000ull;
+  __device__ __forceinline__ u64 bits(double x) const { return static_cast<u64>(__double_as_longlong(fma(x >= m ? x : 0.0, one, 4503599627370496.0))); }
+  __device__ __forceinline__ u64 weight(float z) const { return bits(w(z)) - kNothing; }
+  __device__ __forceinline__ u64 share(double part, u64 of) const {   // the least whole number that reaches part of a mass
+    const u64 n = static_cast<u64>(ceil(part * static_cast<double>(of)));
+    return n < 1 ? 1 : n > of ? of : n;
+  }
+  __device__ __forceinline__ u64 target(u64 mass) const {
+    const u64 t = static_cast<u64>(u * static_cast<double>(mass));
+    return t < mass ? t : mass - 1;
+  }
 };
 // The logits of a row of T threads, a unit to a wavefront at a time.
 template <typename In, int T>
@@ -341,9 +368,9 @@ struct RowSource {
   const float* unit_max;                                     // of the row
   Extreme extreme;
   __device__ __forceinline__ float at(int v) const { return static_cast<unsigned>(v) < static_cast<unsigned>(V) ? extreme(logit(z[v])) : -INFINITY; }   // -1: no token
-  // f(z, token) for every token with z > -infinity, and z >= lo; others may come.  `after` once a unit, by its wavefront, also where the unit has none
+  // f(z, token, weight()) for every token with z > -infinity, and z >= lo; others may come.  `after` once a unit, by its wavefront, also where the unit has none
   template <class F, class G>
-  __device__ __forceinline__ void each(float lo, F f, G after) const {
+  __device__ __forceinline__ void each(float lo, const RowDraw& d, F f, G after) const {
     for (int u = threadIdx.x >> 6; u < units; u += T / kWave) {
       const float top = unit_max[u];
       if ((extreme.is || top >= lo) && top > -INFINITY) {
@@ -352,7 +379,7 @@ struct RowSource {
 #pragma unroll
         for (int i = 0; i < kPerLane; ++i) {
           const float zi = extreme(logit(x[i]));
-          if (zi > -INFINITY) f(zi, token_of<In>(u, i));
+          if (zi > -INFINITY) f(zi, token_of<In>(u, i), [&] { return d.weight(zi); });
           if (i % 4 == 3) __builtin_amdgcn_sched_barrier(0);  // sixteen weights at once take more registers than there are
         }
       }
@@ -360,7 +387,7 @@ struct RowSource {
     }
   }
   template <class F>
-  __device__ __forceinline__ void each(float lo, F f) const { each(lo, f, [](int) {}); }
+  __device__ __forceinline__ void each(float lo, const RowDraw& d, F f) const { each(lo, d, f, [](int) {}); }
 };
 // Listed tokens [a, b).
 template <int T>
@@ -368,8 +395,8 @@ struct ListSource {
   const RowShared<T>* s;
   int a, b;
   template <class F>
-  __device__ __forceinline__ void each(float, F f) const {
-    for (int i = a + static_cast<int>(threadIdx.x); i < b; i += T) f(s->list_z[i], s->list_id[i]);
+  __device__ __forceinline__ void each(float, const RowDraw&, F f) const {
+    for (int i = a + static_cast<int>(threadIdx.x); i < b; i += T) f(s->list_z[i], s->list_id[i], [&] { return s->list_w[i]; });
   }
 };
 struct Border {
@@ -379,7 +406,7 @@ struct Border {
 // The key at which the sum of val over the keys in falling order reaches `need`, 1 <= need <= the sum over all; keys of `known` bits.  Eleven
 // bits at a time from the top; whole numbers, so that the order in which the additions come is nothing.
 template <int T, class Source, class K, class F>
-__device__ __forceinline__ Border border_of(const Source& src, RowShared<T>& s, Block<T>& all, float lo, K key_of, F val, u64 need, int known) {
+__device__ __forceinline__ Border border_of(const Source& src, RowShared<T>& s, Block<T>& all, float lo, const RowDraw& d, K key_of, F val, u64 need, int known) {
   constexpr int kEach = kBins / T;
   Border b{0, 0, 0};
 #pragma unroll 1
@@ -388,10 +415,10 @@ __device__ __forceinline__ Border border_of(const Source& src, RowShared<T>& s, 
     const uint32_t mask = (1u << (known - shift)) - 1;
     for (int i = threadIdx.x; i < kBins; i += T) s.bins[i] = 0;
     __syncthreads();
-    src.each(lo, [&](float z, int id) {
+    src.each(lo, d, [&](float z, int id, auto w) {
       const uint32_t key = key_of(z, id);
       if (known < 32 && (key ^ b.key) >> known) return;
-      const u64 v = val(z, id);
+      const u64 v = val(z, id, w);
       if (v) atomicAdd(&s.bins[(key >> shift) & mask], v);
     });
     __syncthreads();
@@ -424,32 +451,6 @@ struct SampleOut {
   int32_t* ids;
   float *logp, *logq;
 };
-// A row's settings and what the first launch says about it.
-struct RowDraw {
-  float top;
-  Weigh w;
-  int k;                                                     // 0: none
-  double p, m, u;                                            // p = 1, m = 0: none
-  double all;                                                // the mass of all tokens, in units of the largest weight
-  double one;                                                // 1 in units of the whole numbers
-  int id_bits;                                               // of a token's number
-  __device__ __forceinline__ bool by_min() const { return m > 0.0; }
-  __device__ __forceinline__ u64 whole(double x) const {     // x * one, one at most 2^51, rounded to nearest by the addition
-    return static_cast<u64>(__double_as_longlong(fma(x, one, 4503599627370496.0))) & ((u64{1} << 52) - 1);
-  }
-  __device__ __forceinline__ u64 weight(float z) const {     // of the tokens that min_p leaves
-    const double x = w(z);
-    return x >= m ? whole(x) : u64{0};
-  }
-  __device__ __forceinline__ u64 share(double part, u64 of) const {   // the least whole number that reaches part of a mass
-    const u64 n = static_cast<u64>(ceil(part * static_cast<double>(of)));
-    return n < 1 ? 1 : n > of ? of : n;
-  }
-  __device__ __forceinline__ u64 target(u64 mass) const {
-    const u64 t = static_cast<u64>(u * static_cast<double>(mass));
-    return t < mass ? t : mass - 1;
-  }
-};
 // Where what is kept ends: a token is in if its logit orders above the key, or at it with a token up to `tie`.
 struct Cut {
   uint32_t key = 0;
@@ -463,6 +464,7 @@ struct Drawn {
   int id;
   u64 mass;                                                  // the kept one
 };
+__device__ __forceinline__ float logit_at(uint32_t order) { return __uint_as_float(order & 0x80000000u ? order ^ 0x80000000u : ~order); }
 // Where the orders of logits lie: from base on, as many bits.
 struct Span {
   uint32_t base = 0;
@@ -470,20 +472,20 @@ struct Span {
 };
 // The cut after `need` of val, which is the same for equal logits or 0; *mass: the sum of what is in.
 template <int T, class Source, class F>
-__device__ __forceinline__ Cut cut_at(const Source& src, RowShared<T>& s, Block<T>& all, float lo, F val, u64 need, u64* mass, int id_bits, Span span = Span()) {
-  Border b = border_of(src, s, all, lo, [&](float z, int) { return order_of(z) - span.base; }, val, need, span.bits);
+__device__ __forceinline__ Cut cut_at(const Source& src, RowShared<T>& s, Block<T>& all, float lo, const RowDraw& d, F val, u64 need, u64* mass, Span span = Span()) {
+  Border b = border_of(src, s, all, lo, d, [&](float z, int) { return order_of(z) - span.base; }, val, need, span.bits);
   b.key += span.base;
   Cut c;
   c.key = b.key;
   // how many tokens lie at the border
   u64 count = 0;
-  src.each(lo, [&](float z, int id) { count += order_of(z) == b.key && val(z, id); });
+  src.each(lo, d, [&](float z, int id, auto w) { count += order_of(z) == b.key && val(z, id, w); });
   count = all.sum(count);
   const u64 one = b.here / count, ties = (need - b.above + one - 1) / one;
   if (ties < count) {                                        // the lowest of them
-    const int last = (1 << id_bits) - 1;
-    c.tie = last - static_cast<int>(border_of(src, s, all, lo, [&](float, int id) { return static_cast<uint32_t>(last - id); },
-                                              [&](float z, int id) { return u64{order_of(z) == b.key && val(z, id)}; }, ties, id_bits).key);
+    const int last = (1 << d.id_bits) - 1;
+    c.tie = last - static_cast<int>(border_of(src, s, all, lo, d, [&](float, int id) { return static_cast<uint32_t>(last - id); },
+                                              [&](float z, int id, auto w) { return u64{order_of(z) == b.key && val(z, id, w)}; }, ties, d.id_bits).key);
   }
   *mass = b.above + ties * one;
   return c;
@@ -537,34 +539,35 @@ __device__ __noinline__ Drawn draw_by_passes(RowSource<In, T> row, RowShared<T>*
   const float none = -INFINITY;
   Cut first, run;
   u64 mass;
+  auto one = [](float, int, auto) { return u64{1}; };
   if (d.k > 0) {
     u64 have = 0;
-    row.each(none, [&](float, int) { ++have; });
+    row.each(none, d, [&](float, int, auto) { ++have; });
     have = all.sum(have);
-    if (static_cast<u64>(d.k) < have) first = cut_at(row, s, all, none, [](float, int) { return u64{1}; }, static_cast<u64>(d.k), &mass, d.id_bits);
+    if (static_cast<u64>(d.k) < have) first = cut_at(row, s, all, none, d, one, static_cast<u64>(d.k), &mass);
   }
-  auto of_first = [&](float z, int id) { return first.in(z, id) ? d.weight(z) : u64{0}; };
+  auto of_first = [&](float z, int id, auto w) { return first.in(z, id) ? w() : u64{0}; };
   mass = 0;
-  row.each(none, [&](float z, int id) { mass += of_first(z, id); });
+  row.each(none, d, [&](float z, int id, auto w) { mass += of_first(z, id, w); });
   mass = all.sum(mass);
-  if (d.p < 1.0) run = cut_at(row, s, all, none, of_first, d.share(d.p, mass), &mass, d.id_bits);
-  auto kept = [&](float z, int id) { return run.in(z, id) ? of_first(z, id) : u64{0}; };
+  if (d.p < 1.0) run = cut_at(row, s, all, none, d, of_first, d.share(d.p, mass), &mass);
+  auto kept = [&](float z, int id, auto w) { return run.in(z, id) ? of_first(z, id, w) : u64{0}; };
   u64 sum = 0;
-  row.each(none, [&](float z, int id) { sum += kept(z, id); }, [&](int u) {
+  row.each(none, d, [&](float z, int id, auto w) { sum += kept(z, id, w); }, [&](int u) {
     sum = lanes_sum(sum);
     if ((threadIdx.x & 63) == 0) s_unit[u] = sum;
     sum = 0;
   });
   __syncthreads();
-  return Drawn{token_beyond(row, s, all, s_unit, kept, d.target(mass)), mass};
+  return Drawn{token_beyond(row, s, all, s_unit, [&](float z, int id) { return kept(z, id, [&] { return d.weight(z); }); }, d.target(mass)), mass};
 }
 
 // ---- the tokens in front
 // A number that at least so many logits reach: the threads of four wavefronts take the maximum over the row's groups in turn, and the rank-th largest of theirs is it.
 // (All sixteen, whose lists everybody merges: 5 us more of a row.)
 constexpr int kBoundT = 256;
-template <int T>
-__device__ __forceinline__ float front_bound(const float* __restrict__ group_max, int groups, RowShared<T>& s) {
+template <int T, class Shared>
+__device__ __forceinline__ float front_bound(const float* __restrict__ group_max, int groups, Shared& s) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, rank = min(kTopRank, groups / 8);
   if (wave < kBoundT / kWave) {
     float x = -INFINITY;
@@ -587,8 +590,8 @@ __device__ __forceinline__ float front_bound(const float* __restrict__ group_max
   return s.top[0][rank - 1];
 }
 // Lists the tokens with z >= bound; false: more than there is room for.
-template <typename In, int T>
-__device__ __forceinline__ bool list_front(const RowSource<In, T>& row, const float* __restrict__ group_max, float bound, RowShared<T>& s) {
+template <typename In, int T, class Shared>
+__device__ __forceinline__ bool list_front(const RowSource<In, T>& row, const float* __restrict__ group_max, float bound, Shared& s) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, groups = row.units * kGroupsPerUnit;
   int* const s_group = reinterpret_cast<int*>(s.bins);
   if (threadIdx.x == 0) s.n_list = s.n_groups = 0;
@@ -623,19 +626,19 @@ __device__ __forceinline__ bool list_front(const RowSource<In, T>& row, const fl
       int at = 0;
       if (lane == 0) at = atomicAdd(&s.n_list, __popcll(m));
       at = __shfl(at, 0, kWave) + __popcll(m & ((u64{1} << lane) - 1));
-      if (in && at < kListCap) {
+      if (in && at < Shared::kList) {
         s.list_z[at] = x[q];
         s.list_id[at] = id[q];
       }
     }
   }
   __syncthreads();
-  return s.n_list <= kListCap;
+  return s.n_list <= Shared::kList;
 }
 // What the listed tokens say, where they are enough: id -1 where they are not.  Each is compared with all of them, once by its logit and once by its number, by
 // the threads that it has: sixteen of up to 64 tokens, four of up to 256.
-template <int T>
-__device__ __forceinline__ Drawn draw_from_front(RowShared<T>& s, Block<T>& all, int n, float bound, bool all_listed, const RowDraw& d) {
+template <int T, class Shared>
+__device__ __forceinline__ Drawn draw_from_front(Shared& s, Block<T>& all, int n, float bound, bool all_listed, const RowDraw& d) {
   u64* const s_key = s.bins;                                 // [kRanked] each
   u64* const s_w = s.bins + kRanked;
   u64* const s_sorted = s.bins + 2 * kRanked;
@@ -703,15 +706,15 @@ __device__ __forceinline__ Drawn draw_from_front(RowShared<T>& s, Block<T>& all,
 }
 
 // ---- rows whose mass is spread
-// The tokens below the front by their distance to it, in 1/64 of T: their counts say near which bin the border of top_p lies and in which exactly that of top_k.  A second
+// The tokens below the front by their distance to it, in 1/128 of T, at most 1/128: their counts say near which bin the border of top_p lies and in which exactly that of top_k.  A second
 // pass sums what lies above for certain, by unit, and lists the tokens of the bins around; among those the borders are found as they are.  Where a border was not
 // among the bins, or they hold too many, the row is gone through bit by bit.
-constexpr double kBinsPerT = 64.0;
+constexpr float kCountsPerOne = 128.f;
 struct Binning {
-  float bound, lo, scale;                                    // of tokens with lo <= z < bound
+  float bound, lo, scale;                                    // of tokens with lo <= z < bound; bins to a difference of 1
   __device__ __forceinline__ Binning(float bound_, const RowDraw& d, int V) : bound(bound_), lo(-INFINITY) {
     const double c = d.w.c;
-    scale = static_cast<float>(fmin(c * (kBinsPerT / kLog2e64), 1e30));
+    scale = kCountsPerOne * fminf(static_cast<float>(c / kLog2e64), 1.f);
     // below lo nothing counts: weights under min_p, or so small that all tokens together with them are not what top_p leaves out
     const double least = d.by_min() ? d.m : d.k > 0 || d.p == 1.0 ? 0.0 : (1.0 - d.p) * d.all / V;
     if (!(least > 0.0)) return;
@@ -719,25 +722,33 @@ struct Binning {
     lo -= fabsf(lo) * 1e-6f + static_cast<float>(1e-5 / c);
   }
   __device__ __forceinline__ bool has(float z) const { return z < bound && z >= lo && z > -INFINITY; }
-  __device__ __forceinline__ int bin(float z) const { return static_cast<int>(fminf((bound - z) * scale, static_cast<float>(kBins - 1))); }
-  // A bin's logits by its edges, a hundredth of a bin and a few numbers apart: more than the rounding of what bin() computes.
-  __device__ __forceinline__ Span span(int from, int to) const {
-    Span a;
-    if (to >= kBins - 1) return a;                           // what lies beyond is in the last bin
-    a.base = order_of(bound - (static_cast<float>(to) + 1.01f) / scale) - 8;
-    const uint32_t end = order_of(bound - (static_cast<float>(from) - 0.01f) / scale) + 8;
-    a.bits = 32 - __clz(static_cast<int>(end - a.base));
-    return a;
+  __device__ __forceinline__ int bin(float z) const { return static_cast<int>(fminf((bound - z) * scale, static_cast<float>(kCounts - 1))); }
+  // The largest logit of the bins from b on: found by its bits, as what bin() rounds to is what counts.
+  __device__ __forceinline__ float edge(int b) const {
+    if (b >= kCounts) return -INFINITY;
+    uint32_t below = order_of(-INFINITY), above = order_of(bound);   // bin(below) >= b, and that of above is not (or is the bound)
+    while (above - below > 1) {
+      const uint32_t mid = below + (above - below) / 2;
+      if (bin(logit_at(mid)) >= b) below = mid;
+      else above = mid;
+    }
+    return logit_at(below);
   }
 };
-// The bins that matter.
+// What counts, between thresholds.
 struct Bracket {
-  int b1, b2;                                                // those around the border of top_p (none: b2 < b1)
-  int k_bin;                                                 // that of the k-th token; kBins: all are among the first k
-  int sure;                                                  // bins before it are in for certain
-  int last;                                                  // what lies behind it counts for nothing
-  u64 k_in_bin;                                              // places of the k-th bin
-  __device__ __forceinline__ bool lists(int b) const { return (b == k_bin && b < kBins) || (b >= b1 && b <= b2); }
+  float sure;                                                // above it tokens are in for certain
+  float list;                                                // from sure down to here, exclusive, lies the border of top_p
+  float k_from, k_to;                                        // from k_from down to k_to, exclusive, lies the k-th token (-infinity: all are among the first k)
+  float last;                                                // what is not above it counts for nothing
+  u64 k_in_bin;                                              // places from k_from down
+  __device__ __forceinline__ bool lists(float z) const { return (z <= sure && z > list) || (z <= k_from && z > k_to); }
+  __device__ __forceinline__ static Span span(float from, float to) {   // of the logits from `from` down to `to`, exclusive
+    Span a;
+    a.base = order_of(to) + 1;
+    a.bits = max(32 - __clz(static_cast<int>(order_of(from) - a.base)), 1);
+    return a;
+  }
 };
 // First pass, of the units [u0, u1).
 template <typename In, int T>
@@ -752,17 +763,17 @@ __device__ __forceinline__ void count_bins(const RowSource<In, T>& row, const Bi
       if (q.has(x[i])) atomicAdd(&s_count[q.bin(x[i])], 1u);
   }
 }
-// counts: this thread's bins, kBins / T of them from threadIdx.x * kBins / T on.
+// counts: this thread's bins, kCounts / T of them from threadIdx.x * kCounts / T on.
 template <int T, class Shared>
-__device__ __forceinline__ Bracket bracket_of(const uint32_t (&counts)[kBins / T], Shared& s, Block<T>& all, const Binning& q, u64 front, int n_front, const RowDraw& d) {
-  constexpr int kEach = kBins / T;
-  const double at_bound = d.w(q.bound);
+__device__ __forceinline__ Bracket bracket_of(const uint32_t (&counts)[kCounts / T], Shared& s, Block<T>& all, const Binning& q, u64 front, int n_front, const RowDraw& d) {
+  constexpr int kEach = kCounts / T;
+  const double at_bound = d.w(q.bound), per_bin = -d.w.c / q.scale;   // the power of 2 that a bin takes from a weight
   u64 n_mine = 0, n_all;
   double m_mine = 0.0, m_all, of[kEach];
 #pragma unroll
   for (int i = 0; i < kEach; ++i) {
     const int b = static_cast<int>(threadIdx.x) * kEach + i;
-    of[i] = at_bound * exp2_near(-(b + 0.5) / kBinsPerT * kLog2e64);
+    of[i] = at_bound * exp2_near((b + 0.5) * per_bin);
     n_mine += counts[i];
     m_mine += static_cast<double>(counts[i]) * of[i];
   }
@@ -770,10 +781,10 @@ __device__ __forceinline__ Bracket bracket_of(const uint32_t (&counts)[kBins / T
   const double m_before = all.scan(m_mine, &m_all);
   const double f_mass = static_cast<double>(front) / d.one;
   if (threadIdx.x == 0) {
-    s.found_bin = kBins;
+    s.found_bin = kCounts;
     s.found_drest = f_mass + m_all;
     s.found_rest = 0;
-    s.found_id = s.n_groups = kBins - 1;
+    s.found_id = s.n_groups = kCounts - 1;
   }
   __syncthreads();
   if (d.k > 0) {                                             // the bin of the k-th token; all of the front are among the first k
@@ -792,15 +803,12 @@ __device__ __forceinline__ Bracket bracket_of(const uint32_t (&counts)[kBins / T
     }
     __syncthreads();
   }
-  Bracket r;
-  r.k_bin = static_cast<int>(s.found_bin);
-  r.k_in_bin = s.found_rest;
+  const int k_bin = static_cast<int>(s.found_bin);
   const double total = !d.by_min() && d.k == 0 ? d.all : s.found_drest;   // what top_p is of, nearly
-  r.b1 = 0;
-  r.b2 = -1;
-  const double need = d.p * total - f_mass, off = 1e-3 * fabs(need) + 1e-6 * total;
+  int b1 = 0, b2 = -1;
+  const double need = d.p * total - f_mass, off = (1e-3 + per_bin * per_bin / 16) * fabs(need) + 1e-6 * total;   // (logits of a bin are not all in its middle)
   if (d.p < 1.0 && need + off > 0.0) {
-    int from = kBins - 1, to = kBins - 1;                    // the thread's first bin that reaches the lower end, and the upper one
+    int from = kCounts - 1, to = kCounts - 1;                    // the thread's first bin that reaches the lower end, and the upper one
     double m = m_before + m_mine;
 #pragma unroll
     for (int i = kEach - 1; i >= 0; --i) {
@@ -816,19 +824,30 @@ __device__ __forceinline__ Bracket bracket_of(const uint32_t (&counts)[kBins / T
       atomicMin(&s.n_groups, to);
     }
     __syncthreads();
-    r.b2 = min(s.n_groups + 1, min(r.k_bin, kBins - 1));
-    r.b1 = min(max(s.found_id - 1, 0), r.b2);
+    b2 = min(s.n_groups + 1, min(k_bin, kCounts - 1));
+    b1 = min(max(s.found_id - 1, 0), b2);
   }
-  __syncthreads();
+  // the thresholds, a lane to each
+  const int lane = threadIdx.x & 63, bin = lane == 0 ? b1 : lane == 1 ? b2 + 1 : lane == 2 ? k_bin : min(k_bin + 1, kCounts);
+  const float edge = q.edge(bin);
+  const float e1 = __shfl(edge, 0, kWave), e2 = __shfl(edge, 1, kWave);
+  Bracket r;
+  r.k_from = __shfl(edge, 2, kWave);
+  r.k_to = __shfl(edge, 3, kWave);
+  r.k_in_bin = s.found_rest;
   const bool by_p = d.p < 1.0, total_open = d.k > 0 || d.by_min();
-  r.sure = by_p ? (r.b2 < 0 ? 0 : r.b1) : r.k_bin;
-  r.last = total_open || !by_p ? min(r.k_bin, kBins - 1) : r.b2;
+  r.sure = !by_p ? r.k_from : b2 < 0 ? INFINITY : e1;
+  r.list = !by_p ? r.k_from : b2 < 0 ? INFINITY : e2;
+  r.last = total_open || !by_p ? r.k_to : r.list;
+  __syncthreads();
   return r;
 }
 // Second pass, of the units [u0, u1): the sum of what is in for certain of every unit, of all units what else top_p may be of, and the list.
+// The sums are of the bits of x + 2^52, x a weight as a whole number: without a mask, 2^52's own bits are taken off the sixteen at the end.
 template <typename In, int T>
 __device__ __forceinline__ void sum_units(const RowSource<In, T>& row, const Binning& q, const Bracket& r, const RowDraw& d, int u0, int u1, u64* unit_sum, float* list_z,
-                                          int* list_id, int* n_list, u64& sure, u64& rest) {
+                                          int* list_id, int* n_list, int room, u64& sure, u64& rest) {
+  const bool total_open = d.p < 1.0 && (d.k > 0 || d.by_min());
   for (int u = u0 + static_cast<int>(threadIdx.x >> 6); u < u1; u += T / kWave) {
     u64 unit = 0;
     const float most = row.unit_max[u];
@@ -838,16 +857,19 @@ __device__ __forceinline__ void sum_units(const RowSource<In, T>& row, const Bin
       uint32_t mask = 0;                                     // of what the lane lists
 #pragma unroll
       for (int i = 0; i < kPerLane; ++i) {
-        const int b = q.has(x[i]) ? q.bin(x[i]) : kBins;
-        const bool list = r.lists(b);
+        const bool has = q.has(x[i]), list = has && r.lists(x[i]);
         if (list) mask |= 1u << i;
-        if (!list && b <= r.last) {
-          const u64 w = d.weight(x[i]);
-          if (b < r.sure) unit += w;
-          else rest += w;
+        const float z = has && !list && x[i] > r.last ? x[i] : -INFINITY;   // a weight of nothing
+        if (!total_open) {
+          unit += d.bits(d.w(z > r.sure ? z : -INFINITY));
+        } else {
+          const u64 w = d.bits(d.w(z));
+          unit += z > r.sure ? w : RowDraw::kNothing;
+          rest += z > r.sure ? RowDraw::kNothing : w;
         }
-        if (i % 4 == 3) __builtin_amdgcn_sched_barrier(0);   // sixteen weights at once take more registers than there are
       }
+      unit -= kPerLane * RowDraw::kNothing;
+      if (total_open) rest -= kPerLane * RowDraw::kNothing;
       if (__ballot(mask)) {                                  // one place for all that a wavefront lists of a unit
         const int mine = __popc(mask), upto = static_cast<int>(lanes_scan(static_cast<u64>(mine)));
         int at = 0;
@@ -856,7 +878,7 @@ __device__ __forceinline__ void sum_units(const RowSource<In, T>& row, const Bin
 #pragma unroll
         for (int i = 0; i < kPerLane; ++i)
           if (mask >> i & 1) {
-            if (at < kListCap) {
+            if (at < room) {
               list_z[at] = x[i];
               list_id[at] = token_of<In>(u, i);
             }
@@ -875,16 +897,19 @@ __device__ __forceinline__ Drawn draw_listed(const RowSource<In, T>& row, RowSha
                                              u64 sure, u64 rest, const RowDraw& d) {
   Cut first, run;
   const ListSource<T> listed{&s, 0, n_list}, front_list{&s, 0, n_front}, behind{&s, n_front, n_list};
+  for (int i = threadIdx.x; i < n_list; i += T) s.list_w[i] = d.weight(s.list_z[i]);
+  __syncthreads();
   u64 mass;
-  if (r.k_bin < kBins)
-    first = cut_at(behind, s, all, -INFINITY, [&](float z, int) { return u64{q.bin(z) == r.k_bin}; }, r.k_in_bin, &mass, d.id_bits, q.span(r.k_bin, r.k_bin));
-  auto of_first = [&](float z, int id) { return first.in(z, id) ? d.weight(z) : u64{0}; };
-  auto in_bins = [&](float z, int id) { return q.bin(z) <= r.b2 ? of_first(z, id) : u64{0}; };
-  u64 in_front = 0, in_behind = 0, have = 0, none = 0;
-  front_list.each(-INFINITY, [&](float z, int) { in_front += d.weight(z); });
-  behind.each(-INFINITY, [&](float z, int id) { in_behind += of_first(z, id); have += in_bins(z, id); });
+  const float none = -INFINITY;
+  if (r.k_from > -INFINITY)
+    first = cut_at(behind, s, all, none, d, [&](float z, int, auto) { return u64{z <= r.k_from && z > r.k_to}; }, r.k_in_bin, &mass, Bracket::span(r.k_from, r.k_to));
+  auto of_first = [&](float z, int id, auto w) { return first.in(z, id) ? w() : u64{0}; };
+  auto in_bins = [&](float z, int id, auto w) { return z <= r.sure && z > r.list ? of_first(z, id, w) : u64{0}; };
+  u64 in_front = 0, in_behind = 0, have = 0, other = 0;
+  front_list.each(none, d, [&](float, int, auto w) { in_front += w(); });
+  behind.each(none, d, [&](float z, int id, auto w) { in_behind += of_first(z, id, w); have += in_bins(z, id, w); });
   all.sum(in_front, in_behind);
-  all.sum(have, none);
+  all.sum(have, other);
   mass = in_front + sure + in_behind + rest;
   if (d.p < 1.0) {
     u64 need = d.share(d.p, mass);
@@ -893,22 +918,22 @@ __device__ __forceinline__ Drawn draw_listed(const RowSource<In, T>& row, RowSha
       need = part < 1.0 ? 1 : static_cast<u64>(part);
     }
     if (need <= in_front) {
-      run = cut_at(front_list, s, all, -INFINITY, [&](float z, int) { return d.weight(z); }, need, &mass, d.id_bits);
+      run = cut_at(front_list, s, all, none, d, [](float, int, auto w) { return w(); }, need, &mass);
       for (int u = threadIdx.x; u < row.units; u += T) s_unit[u] = 0;
     } else {
       if (need <= in_front + sure || need > in_front + sure + have) return Drawn{-1, 0};
-      run = cut_at(behind, s, all, -INFINITY, in_bins, need - in_front - sure, &mass, d.id_bits, q.span(r.b1, r.b2));
+      run = cut_at(behind, s, all, none, d, in_bins, need - in_front - sure, &mass, Bracket::span(r.sure, r.list));
       mass += in_front + sure;
     }
   }
-  auto kept = [&](float z, int id) { return run.in(z, id) ? of_first(z, id) : u64{0}; };
+  auto kept = [&](float z, int id, auto w) { return run.in(z, id) ? of_first(z, id, w) : u64{0}; };
   __syncthreads();
-  listed.each(-INFINITY, [&](float z, int id) {
-    const u64 w = kept(z, id);
-    if (w) atomicAdd(&s_unit[id / kUnit], w);
+  listed.each(none, d, [&](float z, int id, auto w) {
+    const u64 x = kept(z, id, w);
+    if (x) atomicAdd(&s_unit[id / kUnit], x);
   });
   __syncthreads();
-  return Drawn{token_beyond(row, s, all, s_unit, kept, d.target(mass)), mass};
+  return Drawn{token_beyond(row, s, all, s_unit, [&](float z, int id) { return kept(z, id, [&] { return d.weight(z); }); }, d.target(mass)), mass};
 }
 
 // The least of the lanes' numbers that is not negative into *to, which all but the first such lane of a wavefront leave alone: numbers rise with the lanes.
@@ -1038,7 +1063,7 @@ __device__ __forceinline__ void write_drawn(const SampleOut& out, int64_t row, i
 }
 // A row that its front did not decide, on its way through the launches behind.
 struct RowState {
-  int flat;                                                  // it is one; the rest is only written then
+  int bins;                                                  // bins serve; else it is gone through bit by bit
   float top, bound;
   int n_front, n_list;
   double all, sum;
@@ -1046,8 +1071,10 @@ struct RowState {
   Bracket bracket;
 };
 struct FlatWs {
+  int* count;                                                // of such rows, cleared by the first launch
+  int* order;                                                // [rows]: their numbers, as they came
   RowState* state;                                           // [rows]
-  uint32_t* counts;                                          // [rows][parts][kBins]
+  uint32_t* counts;                                          // [rows][parts][kCounts]
   u64* unit_sum;                                             // [rows][units]
   float* list_z;                                             // [rows][kListCap]
   int* list_id;
@@ -1060,7 +1087,7 @@ template <typename In, int T, Filter FILTER>
 __global__ void __launch_bounds__(T)
 k_sample_row(Logits<In> L, RowCalls C, FlatWs F) {
   extern __shared__ u64 s_unit[];                            // [units], kSomeInOne only
-  __shared__ std::conditional_t<FILTER == Filter::kNone, PlainShared<T>, RowShared<T>> s;
+  __shared__ std::conditional_t<FILTER == Filter::kNone, PlainShared<T>, std::conditional_t<FILTER == Filter::kSome, RowShared<T, 4 * kRanked, false>, RowShared<T>>> s;
   const int64_t m = blockIdx.x, row = C.rowsel ? C.rowsel[C.c0 + m] : C.c0 + m;
   const float* const unit_max = C.A.unit + m * L.units;
   const float* const ref_of = C.A.ref + m * L.units;
@@ -1070,7 +1097,6 @@ k_sample_row(Logits<In> L, RowCalls C, FlatWs F) {
   for (int i = threadIdx.x; i < L.units; i += T) top = larger(top, unit_max[i]);
   Block<T> block(s.block);
   top = block.max(top);
-  if (FILTER == Filter::kSome && threadIdx.x == 0) F.state[m].flat = 0;
   if (top == -INFINITY) {                                    // nothing to draw from
     if (threadIdx.x == 0) {
       C.out.ids[row] = -1;
@@ -1125,24 +1151,27 @@ k_sample_row(Logits<In> L, RowCalls C, FlatWs F) {
             F.list_z[m * kListCap + i] = s.list_z[i];
             F.list_id[m * kListCap + i] = s.list_id[i];
           }
-          if (threadIdx.x == 0) F.state[m] = RowState{bins ? 1 : 2, top, bound, n, n, all, sum, front, 0, Bracket{}};
+          if (threadIdx.x == 0) {
+            F.order[atomicAdd(F.count, 1)] = static_cast<int>(m);
+            F.state[m] = RowState{bins ? 1 : 0, top, bound, n, n, all, sum, front, 0, Bracket{}};
+          }
           return;
         } else {
           if (bins) {
             const Binning q(bound, d, L.V);
             uint32_t* const s_count = reinterpret_cast<uint32_t*>(s.bins);
-            for (int i = threadIdx.x; i < kBins; i += T) s_count[i] = 0;
+            for (int i = threadIdx.x; i < kCounts; i += T) s_count[i] = 0;
             __syncthreads();
             count_bins(src, q, 0, L.units, s_count);
             __syncthreads();
-            uint32_t counts[kBins / T];
+            uint32_t counts[kCounts / T];
 #pragma unroll
-            for (int i = 0; i < kBins / T; ++i) counts[i] = s_count[threadIdx.x * (kBins / T) + i];
+            for (int i = 0; i < kCounts / T; ++i) counts[i] = s_count[threadIdx.x * (kCounts / T) + i];
             const Bracket r = bracket_of<T>(counts, s, block, q, front, n, d);
             if (threadIdx.x == 0) s.n_list = n;
             __syncthreads();
             u64 sure = 0, rest = 0;
-            sum_units(src, q, r, d, 0, L.units, s_unit, s.list_z, s.list_id, &s.n_list, sure, rest);
+            sum_units(src, q, r, d, 0, L.units, s_unit, s.list_z, s.list_id, &s.n_list, kListCap, sure, rest);
             block.sum(sure, rest);
             if (s.n_list <= kListCap) got = draw_listed(src, s, block, s_unit, q, r, n, s.n_list, sure, rest, d);
             __syncthreads();
@@ -1161,60 +1190,96 @@ k_sample_row(Logits<In> L, RowCalls C, FlatWs F) {
 template <typename In, int T>
 __global__ void __launch_bounds__(T)
 k_sample_count(Logits<In> L, RowCalls C, FlatWs F) {
-  __shared__ uint32_t s_count[kBins];
-  const int64_t m = blockIdx.y;
+  __shared__ uint32_t s_count[kCounts];
+  if (static_cast<int>(blockIdx.y) >= *F.count) return;
+  const int64_t m = F.order[blockIdx.y];
   RowState& state = F.state[m];
-  if (state.flat != 1) return;
+  if (!state.bins) return;
   const int64_t row = C.rowsel ? C.rowsel[C.c0 + m] : C.c0 + m;
   const RowSource<In, T> src = row_source<In, T>(L, C, m, state.top);
   const RowDraw d = row_draw(C, row, state.top, C.S.t(row), 0.0, state.all, L.V);
   const Binning q(state.bound, d, L.V);
-  for (int i = threadIdx.x; i < kBins; i += T) s_count[i] = 0;
+  for (int i = threadIdx.x; i < kCounts; i += T) s_count[i] = 0;
   __syncthreads();
   count_bins(src, q, L.units * static_cast<int>(blockIdx.x) / F.parts, L.units * static_cast<int>(blockIdx.x + 1) / F.parts, s_count);
   __syncthreads();
-  uint32_t* const to = F.counts + (m * F.parts + blockIdx.x) * kBins;
-  for (int i = threadIdx.x; i < kBins; i += T) to[i] = s_count[i];
+  uint32_t* const to = F.counts + (m * F.parts + blockIdx.x) * kCounts;
+  for (int i = threadIdx.x; i < kCounts; i += T) to[i] = s_count[i];
 }
 // ... what they say, ...
 template <int T>
 __global__ void __launch_bounds__(T)
 k_sample_bracket(RowCalls C, FlatWs F, int V) {
-  constexpr int kEach = kBins / T;
+  constexpr int kEach = kCounts / T;
   __shared__ BinShared<T> s;
-  const int64_t m = blockIdx.x;
+  if (static_cast<int>(blockIdx.x) >= *F.count) return;
+  const int64_t m = F.order[blockIdx.x];
   RowState& state = F.state[m];
-  if (state.flat != 1) return;
+  if (!state.bins) return;
   const int64_t row = C.rowsel ? C.rowsel[C.c0 + m] : C.c0 + m;
   const RowDraw d = row_draw(C, row, state.top, C.S.t(row), 0.0, state.all, V);
   const Binning q(state.bound, d, V);
   uint32_t counts[kEach] = {};
-  for (int p = 0; p < F.parts; ++p)
+  static_assert(kEach % 4 == 0, "sixteen bytes at a time");
+  constexpr int kAtOnce = 4;                                 // parts under way
+  for (int p = 0; p < F.parts; p += kAtOnce) {
+    uint4 x[kAtOnce][kEach / 4];
 #pragma unroll
-    for (int i = 0; i < kEach; ++i) counts[i] += F.counts[(m * F.parts + p) * kBins + threadIdx.x * kEach + i];
+    for (int b = 0; b < kAtOnce; ++b)
+#pragma unroll
+      for (int i = 0; i < kEach / 4; ++i)
+        x[b][i] = p + b < F.parts ? reinterpret_cast<const uint4*>(F.counts + (m * F.parts + p + b) * kCounts + threadIdx.x * kEach)[i] : make_uint4(0u, 0u, 0u, 0u);
+#pragma unroll
+    for (int b = 0; b < kAtOnce; ++b)
+#pragma unroll
+      for (int i = 0; i < kEach / 4; ++i) {
+        counts[4 * i] += x[b][i].x;
+        counts[4 * i + 1] += x[b][i].y;
+        counts[4 * i + 2] += x[b][i].z;
+        counts[4 * i + 3] += x[b][i].w;
+      }
+  }
   Block<T> block(s.block);
   const Bracket r = bracket_of<T>(counts, s, block, q, state.front, state.n_front, d);
   if (threadIdx.x == 0) state.bracket = r;
 }
 // ... then the sums and lists, ...
-constexpr int kSumUnits = 16;                                // of a workgroup
+constexpr int kSumUnits = 8, kSumList = 1024;               // of a workgroup
 template <typename In, int T>
-__global__ void __launch_bounds__(T, 6)
+__global__ void __launch_bounds__(T, 4)
 k_sample_sums(Logits<In> L, RowCalls C, FlatWs F) {
   __shared__ u64 s_block[2][2][T / kWave];
-  const int64_t m = blockIdx.y;
+  __shared__ float s_z[kSumList];
+  __shared__ int s_id[kSumList];
+  __shared__ int s_n, s_at;
+  if (static_cast<int>(blockIdx.y) >= *F.count) return;
+  const int64_t m = F.order[blockIdx.y];
   RowState& state = F.state[m];
-  if (state.flat != 1) return;
+  if (!state.bins) return;
   const int64_t row = C.rowsel ? C.rowsel[C.c0 + m] : C.c0 + m;
   const RowSource<In, T> src = row_source<In, T>(L, C, m, state.top);
   const RowDraw d = row_draw(C, row, state.top, C.S.t(row), 0.0, state.all, L.V);
   Block<T> block(s_block);
+  if (threadIdx.x == 0) s_n = 0;
+  __syncthreads();
   u64 sure = 0, rest = 0;
   const int u0 = blockIdx.x * kSumUnits;
-  sum_units(src, Binning(state.bound, d, L.V), state.bracket, d, u0, min(u0 + kSumUnits, L.units), F.unit_sum + m * L.units, F.list_z + m * kListCap, F.list_id + m * kListCap,
-            &state.n_list, sure, rest);
+  sum_units(src, Binning(state.bound, d, L.V), state.bracket, d, u0, min(u0 + kSumUnits, L.units), F.unit_sum + m * L.units, s_z, s_id, &s_n, kSumList, sure, rest);
   rest = block.sum(rest);
-  if (threadIdx.x == 0 && rest) atomicAdd(&state.rest, rest);
+  // the workgroup's list behind the others' (by every wavefront for itself it took twice the launch: all wait at one address)
+  const int n = s_n;
+  if (threadIdx.x == 0) {
+    s_at = n > 0 ? atomicAdd(&state.n_list, n <= kSumList ? n : kListCap + 1) : 0;   // more than there is room for: the row's list is full
+    if (rest) atomicAdd(&state.rest, rest);
+  }
+  __syncthreads();
+  for (int i = threadIdx.x; i < min(n, kSumList); i += T) {
+    const int at = s_at + i;
+    if (at < kListCap) {
+      F.list_z[m * kListCap + at] = s_z[i];
+      F.list_id[m * kListCap + at] = s_id[i];
+    }
+  }
 }
 // ... and the token, a workgroup to a row.
 template <typename In, int T>
@@ -1222,9 +1287,9 @@ __global__ void __launch_bounds__(T)
 k_sample_flat(Logits<In> L, RowCalls C, FlatWs F) {
   extern __shared__ u64 s_unit[];                            // [units]
   __shared__ RowShared<T> s;
-  const int64_t m = blockIdx.x;
+  if (static_cast<int>(blockIdx.x) >= *F.count) return;
+  const int64_t m = F.order[blockIdx.x];
   const RowState& state = F.state[m];
-  if (state.flat == 0) return;
   const int64_t row = C.rowsel ? C.rowsel[C.c0 + m] : C.c0 + m;
   const RowSource<In, T> src = row_source<In, T>(L, C, m, state.top);
   const float ref = src.extreme(state.top);
@@ -1233,7 +1298,7 @@ k_sample_flat(Logits<In> L, RowCalls C, FlatWs F) {
   Block<T> block(s.block);
   Drawn got{-1, 0};
   const int n = state.n_list;
-  if (state.flat == 1 && n <= kListCap) {
+  if (state.bins && n <= kListCap) {
     for (int i = threadIdx.x; i < n; i += T) {
       s.list_z[i] = F.list_z[m * kListCap + i];
       s.list_id[i] = F.list_id[m * kListCap + i];
@@ -1344,8 +1409,10 @@ void carve(Carver& c, SampleWs& w, int64_t rows, int V) {
   w.A.sum = c.take<double>(units);
   w.flat.parts = flat_parts(rows);
   if (w.flat.parts > 0) {
+    w.flat.count = c.take<int>(1);
+    w.flat.order = c.take<int>(rows);
     w.flat.state = c.take<RowState>(rows);
-    w.flat.counts = c.take<uint32_t>(static_cast<size_t>(std::min(rows * 16, std::max<int64_t>(2048, rows * 4))) * kBins);   // as many as any count of rows up to it takes
+    w.flat.counts = c.take<uint32_t>(static_cast<size_t>(std::min(rows * 16, std::max<int64_t>(2048, rows * 4))) * kCounts);   // as many as any count of rows up to it takes
     w.flat.unit_sum = c.take<u64>(units);
     w.flat.list_z = c.take<float>(static_cast<size_t>(rows) * kListCap);
     w.flat.list_id = c.take<int>(static_cast<size_t>(rows) * kListCap);
@@ -1390,13 +1457,13 @@ int bits_of(int V) {
   while ((int64_t{1} << b) < V) ++b;
   return std::min(51, 62 - b);
 }
-constexpr int kRowT = 1024, kPlainT = 256, kFlatT = 512;
+constexpr int kRowT = 1024, kOneT = 512, kPlainT = 256, kFlatT = 512, kSumT = 256;
 template <typename In>
 umas_status sample_rows(const Logits<In>& L, const Settings& S, const int32_t* rowsel, int64_t c0, int64_t rows, const SampleWs& w, const float* u, const SampleOut& out,
                         hipStream_t st) {
   const unsigned n = static_cast<unsigned>(rows);
   const size_t unit_bytes = L.units * sizeof(u64);
-  hipLaunchKernelGGL(k_sample_open<In>, dim3(cdiv(L.units, 2 * kOpenPairs), n), dim3(kOpenT), 0, st, L, S, rowsel, c0, w.A);
+  hipLaunchKernelGGL(k_sample_open<In>, dim3(cdiv(L.units, 2 * kOpenPairs), n), dim3(kOpenT), 0, st, L, S, rowsel, c0, w.A, w.flat.parts > 0 ? w.flat.count : nullptr);
   UMAS_LAUNCHED("k_sample_open");
   const bool plain = !S.top_k_of && !S.top_p_of && !S.min_p_of && S.min_p == 0.0 && S.top_p == 1.0 && (S.top_k == 0 || S.top_k >= L.V);
   const bool greedy = !S.temperature_of && S.temperature == 0.0;
@@ -1407,7 +1474,7 @@ umas_status sample_rows(const Logits<In>& L, const Settings& S, const int32_t* r
     return UMAS_OK;
   }
   if (w.flat.parts == 0) {
-    hipLaunchKernelGGL((k_sample_row<In, kRowT, Filter::kSomeInOne>), dim3(n), dim3(kRowT), unit_bytes, st, L, C, w.flat);
+    hipLaunchKernelGGL((k_sample_row<In, kOneT, Filter::kSomeInOne>), dim3(n), dim3(kOneT), unit_bytes, st, L, C, w.flat);
     UMAS_LAUNCHED("k_sample_row");
     return UMAS_OK;
   }
@@ -1418,9 +1485,9 @@ umas_status sample_rows(const Logits<In>& L, const Settings& S, const int32_t* r
   UMAS_LAUNCHED("k_sample_count");
   hipLaunchKernelGGL((k_sample_bracket<kFlatT>), dim3(n), dim3(kFlatT), 0, st, C, w.flat, L.V);
   UMAS_LAUNCHED("k_sample_bracket");
-  hipLaunchKernelGGL((k_sample_sums<In, kFlatT>), dim3(cdiv(L.units, kSumUnits), n), dim3(kFlatT), 0, st, L, C, w.flat);
+  hipLaunchKernelGGL((k_sample_sums<In, kSumT>), dim3(cdiv(L.units, kSumUnits), n), dim3(kSumT), 0, st, L, C, w.flat);
   UMAS_LAUNCHED("k_sample_sums");
-  hipLaunchKernelGGL((k_sample_flat<In, kRowT>), dim3(n), dim3(kRowT), unit_bytes, st, L, C, w.flat);
+  hipLaunchKernelGGL((k_sample_flat<In, kFlatT>), dim3(n), dim3(kFlatT), unit_bytes, st, L, C, w.flat);
   UMAS_LAUNCHED("k_sample_flat");
   return UMAS_OK;
 }
