@@ -179,8 +179,9 @@ k_rms_norm(NormArgs A) {
 }
 
 // ------------------------------------------------------------------ backward
-// T threads to a row at a time; they keep their columns' share of dg over all rows that they do.  A workgroup's shares meet in LDS, the workgroups' in
-// k_norm_gain, both in a fixed order.  A row whose dy is 0 throughout adds nothing, whatever it holds.
+// T threads to a row, up to two pieces each, so that a row, the next one on its way, and the columns' share of dg over all rows that the threads do stay in
+// registers at four wavefronts to a SIMD.  A workgroup's shares meet in LDS, the workgroups' in k_norm_gain, both in a fixed order.  A row whose dy is 0 throughout
+// adds nothing, whatever it holds.
 struct NormBackArgs {
   const void *dy, *hidden, *gain;
   const float* inv_rms;
@@ -190,64 +191,103 @@ struct NormBackArgs {
   void* dx;
   float* part;                                               // [gridDim.x][d]
 };
-template <typename E, int T, int NV>
-__global__ void __launch_bounds__(kNT)
-k_norm_back(NormBackArgs A) {
-  constexpr int N = Piece<E>::N, kRows = kNT / T;
-  __shared__ float s_red[kNT / kWave];
-  __shared__ float s_part[kRows == 1 ? 1 : kNT * 4];
-  const int t = threadIdx.x % T, pieces = (A.d + N - 1) / N;
-  float dg[NV][N];
+template <int T> constexpr int kBackT = T < 256 ? 256 : T;   // threads of a workgroup
+template <typename E, int NV, bool THROUGH>
+struct BackRow {
+  u32x4u y[NV], h[NV], th[THROUGH ? NV : 1];
+  float inv;
+  template <int T>
+  __device__ __forceinline__ void load(const NormBackArgs& A, int64_t row, int t, int pieces) {
+    const u32x4u none = {0u, 0u, 0u, 0u};
+    if (row >= A.n) {                                        // nothing to add, nothing to write
 #pragma unroll
-  for (int k = 0; k < NV; ++k)
-#pragma unroll
-    for (int i = 0; i < N; ++i) dg[k][i] = 0.f;
-  const u32x4u none = {0u, 0u, 0u, 0u};
-  for (int64_t row = static_cast<int64_t>(blockIdx.x) * kRows + threadIdx.x / T; row < A.n; row += static_cast<int64_t>(gridDim.x) * kRows) {
-    const E* const dy = static_cast<const E*>(A.dy) + row * A.d;
-    const E* const hidden = static_cast<const E*>(A.hidden) + row * A.d;
-    const E* const through = A.dhidden ? static_cast<const E*>(A.dhidden) + row * A.d : nullptr;
-    E* const dx = static_cast<E*>(A.dx) + row * A.d;
-    u32x4u y[NV], h[NV], th[NV];
+      for (int k = 0; k < NV; ++k) y[k] = none;
+      return;
+    }
+    const int64_t at = row * A.d;
 #pragma unroll
     for (int k = 0; k < NV; ++k) {
-      y[k] = t + k * T < pieces ? load_piece(dy, t + k * T, A.d) : none;
-      h[k] = t + k * T < pieces ? load_piece(hidden, t + k * T, A.d) : none;
-      if (through) th[k] = t + k * T < pieces ? load_piece(through, t + k * T, A.d) : none;
+      const int p = t + k * T;
+      const bool in = p < pieces;
+      y[k] = in ? load_piece(static_cast<const E*>(A.dy) + at, p, A.d) : none;
+      h[k] = in ? load_piece(static_cast<const E*>(A.hidden) + at, p, A.d) : none;
+      if constexpr (THROUGH) th[k] = in ? load_piece(static_cast<const E*>(A.dhidden) + at, p, A.d) : none;
     }
-    const float inv = A.inv_rms[row];
+    inv = A.inv_rms[row];
+  }
+};
+template <typename E, int T, int NV, bool THROUGH>
+__global__ void __launch_bounds__(kBackT<T>)
+k_norm_back(NormBackArgs A) {
+  constexpr int N = Piece<E>::N, B = kBackT<T>, kRows = B / T, kWaves = T / kWave;
+  __shared__ float2 s_red[2][B / kWave];
+  __shared__ float s_part[kRows == 1 ? 1 : B * 4];
+  const int t = threadIdx.x % T, slot = threadIdx.x / T, pieces = (A.d + N - 1) / N;
+  float dg[NV][N];
+  u32x4u gain[NV];
+#pragma unroll
+  for (int k = 0; k < NV; ++k) {
+    gain[k] = t + k * T < pieces ? load_piece(static_cast<const E*>(A.gain), t + k * T, A.d) : u32x4u{0u, 0u, 0u, 0u};
+#pragma unroll
+    for (int i = 0; i < N; ++i) dg[k][i] = 0.f;
+  }
+  const int64_t step = static_cast<int64_t>(gridDim.x) * kRows;
+  int64_t row = static_cast<int64_t>(blockIdx.x) * kRows + slot;
+  constexpr bool kAhead = T < 1024;                          // the next row on its way: of 1024 threads there are no registers for it
+  BackRow<E, NV, THROUGH> at, next;
+  if constexpr (kAhead) at.template load<T>(A, row, t, pieces);
+  int turn = 0;
+  for (int64_t first = static_cast<int64_t>(blockIdx.x) * kRows; first < A.n; first += step, row += step, turn ^= 1) {   // the workgroup's rows together
+    if constexpr (kAhead) next.template load<T>(A, row + step, t, pieces);
+    else at.template load<T>(A, row, t, pieces);
     float dot = 0.f, some = 0.f;
 #pragma unroll
     for (int k = 0; k < NV; ++k) {
       float a[N], b[N], g[N];
-      Piece<E>::unpack(y[k], a);
-      Piece<E>::unpack(h[k], b);
-      Piece<E>::unpack(t + k * T < pieces ? load_piece(static_cast<const E*>(A.gain), t + k * T, A.d) : none, g);
+      Piece<E>::unpack(at.y[k], a);
+      Piece<E>::unpack(at.h[k], b);
+      Piece<E>::unpack(gain[k], g);
 #pragma unroll
       for (int i = 0; i < N; ++i) {
         dot = fmaf(a[i] * g[i], b[i], dot);
         if (!(a[i] == 0.f)) some = 1.f;
       }
     }
-    dot = row_reduce<T>(dot, s_red, add);
-    some = row_reduce<T>(some, s_red, add);
-    const float m = dot * inv * inv / static_cast<float>(A.d);
+    dot = row_reduce<kWave>(dot, nullptr, add);
+    some = __ballot(some != 0.f) ? 1.f : 0.f;
+    if constexpr (T > kWave) {                               // one barrier a row: the next row's sums go to the other buffer
+      if ((threadIdx.x & 63) == 0) s_red[turn][threadIdx.x >> 6] = make_float2(dot, some);
+      __syncthreads();
+      dot = some = 0.f;
 #pragma unroll
-    for (int k = 0; k < NV; ++k) {
-      if (t + k * T >= pieces) continue;
-      float a[N], b[N], g[N], o[N];
-      Piece<E>::unpack(y[k], a);
-      Piece<E>::unpack(h[k], b);
-      Piece<E>::unpack(load_piece(static_cast<const E*>(A.gain), t + k * T, A.d), g);
-      if (through) Piece<E>::unpack(th[k], o);
-#pragma unroll
-      for (int i = 0; i < N; ++i) {
-        const float v = some != 0.f ? inv * (a[i] * g[i] - b[i] * m) : 0.f;
-        if (some != 0.f) dg[k][i] = fmaf(a[i], b[i] * inv, dg[k][i]);
-        o[i] = through ? o[i] + v : v;
+      for (int w = 0; w < kWaves; ++w) {
+        const float2 v = s_red[turn][slot * kWaves + w];
+        dot += v.x;
+        some += v.y;
       }
-      store_piece(dx, t + k * T, A.d, Piece<E>::pack(o));
     }
+    if (row < A.n) {
+      const float m = dot * at.inv * at.inv / static_cast<float>(A.d);
+      E* const dx = static_cast<E*>(A.dx) + row * A.d;
+#pragma unroll
+      for (int k = 0; k < NV; ++k) {
+        if (t + k * T >= pieces) continue;
+        float a[N], b[N], g[N], o[N];
+        Piece<E>::unpack(at.y[k], a);
+        Piece<E>::unpack(at.h[k], b);
+        Piece<E>::unpack(gain[k], g);
+        if constexpr (THROUGH) Piece<E>::unpack(at.th[k], o);
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+          const float v = some != 0.f ? at.inv * (a[i] * g[i] - b[i] * m) : 0.f;
+          if (some != 0.f) dg[k][i] = fmaf(a[i], b[i] * at.inv, dg[k][i]);
+          if constexpr (THROUGH) o[i] += v;
+          else o[i] = v;
+        }
+        store_piece(dx, t + k * T, A.d, Piece<E>::pack(o));
+      }
+    }
+    if constexpr (kAhead) at = next;
   }
   float* const part = A.part + static_cast<int64_t>(blockIdx.x) * A.d;
 #pragma unroll
@@ -276,29 +316,40 @@ k_norm_back(NormBackArgs A) {
     }
   }
 }
-// dg from the workgroups' shares: a workgroup to 64 columns, its wavefronts every sixteenth share, eight loads of a thread under way (with four wavefronts and
-// one load after the other the 1024 shares of 2048 columns took 95 us).
+// dg from the workgroups' shares: a workgroup to 64 columns, sixteen threads to a share, eight loads of a thread under way.
 constexpr int kGainT = 1024;
 __global__ void __launch_bounds__(kGainT)
 k_norm_gain(const float* __restrict__ part, int parts, int d, int accumulate, float* __restrict__ dgain) {
-  constexpr int kWaves = kGainT / kWave, kAtOnce = 8;
-  __shared__ float s[kGainT];
-  const int col = blockIdx.x * kWave + (threadIdx.x & 63), w = threadIdx.x >> 6;
-  float v = 0.f;
-  if (col < d)
-    for (int p = w; p < parts; p += kWaves * kAtOnce) {
-      float x[kAtOnce];
+  constexpr int kShares = kGainT / 16, kAtOnce = 8;
+  typedef float floatx4u __attribute__((ext_vector_type(4), aligned(4)));
+  __shared__ floatx4 s[kShares][16];
+  const int q = threadIdx.x & 15, w = threadIdx.x >> 4, col = blockIdx.x * kWave + q * 4;
+  floatx4 v = {0.f, 0.f, 0.f, 0.f};
+  for (int p = w; p < parts; p += kShares * kAtOnce) {
+    floatx4u x[kAtOnce];
 #pragma unroll
-      for (int i = 0; i < kAtOnce; ++i) x[i] = p + i * kWaves < parts ? part[static_cast<int64_t>(p + i * kWaves) * d + col] : 0.f;
-#pragma unroll
-      for (int i = 0; i < kAtOnce; ++i) v += x[i];
+    for (int i = 0; i < kAtOnce; ++i) {
+      const float* const from = part + static_cast<int64_t>(p + i * kShares) * d + col;
+      x[i] = floatx4u{0.f, 0.f, 0.f, 0.f};
+      if (p + i * kShares < parts) {
+        if (col + 4 <= d) x[i] = *reinterpret_cast<const floatx4u*>(from);
+        else
+          for (int j = 0; j < d - col; ++j) x[i][j] = from[j];
+      }
     }
-  s[threadIdx.x] = v;
-  __syncthreads();
-  if (w != 0 || col >= d) return;
 #pragma unroll
-  for (int k = 1; k < kWaves; ++k) v += s[k * kWave + threadIdx.x];
-  dgain[col] = accumulate ? dgain[col] + v : v;
+    for (int i = 0; i < kAtOnce; ++i) v += floatx4{x[i][0], x[i][1], x[i][2], x[i][3]};
+  }
+  s[w][q] = v;
+#pragma unroll
+  for (int o = kShares / 2; o > 0; o >>= 1) {
+    __syncthreads();
+    if (w < o) s[w][q] = v = v + s[w + o][q];
+  }
+  if (w != 0) return;
+#pragma unroll
+  for (int j = 0; j < 4; ++j)
+    if (col + j < d) dgain[col + j] = accumulate ? dgain[col + j] + v[j] : v[j];
 }
 
 // ------------------------------------------------------------------ host side
@@ -316,6 +367,20 @@ void with_width(int pieces, bool wide, Launch launch) {
   };
   if (wide || pieces > 8 * kWave) go(std::integral_constant<int, kNT>());
   else go(std::integral_constant<int, kWave>());
+}
+// ... of the backward pass: two pieces, from 2048 on (float32, 16 384 columns are 4096 pieces) four
+template <class Launch>
+void with_back(int pieces, Launch launch) {
+  auto go = [&](auto t, auto nv) { launch(t, nv); };
+  using One = std::integral_constant<int, 1>;
+  using Two = std::integral_constant<int, 2>;
+  if (pieces <= 64) go(std::integral_constant<int, 64>(), One());
+  else if (pieces <= 128) go(std::integral_constant<int, 64>(), Two());
+  else if (pieces <= 256) go(std::integral_constant<int, 128>(), Two());
+  else if (pieces <= 512) go(std::integral_constant<int, 256>(), Two());
+  else if (pieces <= 1024) go(std::integral_constant<int, 512>(), Two());
+  else if (pieces <= 2048) go(std::integral_constant<int, 1024>(), Two());
+  else go(std::integral_constant<int, 1024>(), std::integral_constant<int, 4>());
 }
 constexpr int64_t kWideRows = 2048;                          // up to so many rows a workgroup takes a row
 constexpr int kNormParts = 1024;                             // shares of dg at most
@@ -350,7 +415,15 @@ umas_status norm(const NormArgs& A, umas_dtype dt, hipStream_t st) {
   UMAS_LAUNCHED("k_rms_norm");
   return UMAS_OK;
 }
-int back_parts(int64_t n, int rows_at_once) { return static_cast<int>(std::min<int64_t>(cdiv(std::max<int64_t>(n, 1), rows_at_once), kNormParts)); }
+// Workgroups of the backward pass, each of which leaves a share of dg.  A row of 4 KB and more keeps enough loads under way for one to a compute unit, and every other one costs
+// its share: 39 224 bf16 rows of 2048 with 256, 512 and 1024 of them 116, 124 and 143 us, 20 000 of 4096 117, 125 and 144, 10 000 of 8192 127, 134 and 146, 2000 of 2048 13.2, 14.8 and 18.7;
+// shorter rows 30 000 of 512 33, 27.4 and 28, 100 000 of 256 83, 55 and 44.5; float32, whose rows of up to 16 KB want two, 10 000 of 2048 79, 65 and 69, 4000 of 8192
+// 105, 108.
+int back_parts(int64_t n, int rows_at_once, umas_dtype dt, int d) {
+  const int64_t bytes = static_cast<int64_t>(d) * (dt == UMAS_BF16 ? 2 : 4);
+  const int64_t most = bytes < 1024 ? 1024 : bytes < 4096 || (dt == UMAS_F32 && bytes <= 16384) ? 512 : 256;
+  return static_cast<int>(std::min<int64_t>(cdiv(std::max<int64_t>(n, 1), rows_at_once), most));
+}
 
 }  // namespace
 }  // namespace umas
@@ -395,9 +468,11 @@ extern "C" umas_status umas_rms_norm_bwd(const void* dy, const void* hidden, con
     NormBackArgs A{dy, hidden, gain, inv_rms, dhidden, n_rows, d, dx, static_cast<float*>(workspace)};
     auto run = [&](auto e) {
       using E = decltype(e);
-      with_width(static_cast<int>(cdiv(d, Piece<E>::N)), n_rows <= kWideRows, [&](auto t, auto nv) {
-        parts = back_parts(n_rows, kNT / decltype(t)::value);
-        hipLaunchKernelGGL((k_norm_back<E, decltype(t)::value, decltype(nv)::value>), dim3(parts), dim3(kNT), 0, st, A);
+      with_back(static_cast<int>(cdiv(d, Piece<E>::N)), [&](auto t, auto nv) {
+        constexpr int T = decltype(t)::value, NV = decltype(nv)::value;
+        parts = back_parts(n_rows, kBackT<T> / T, dtype, d);
+        if (dhidden) hipLaunchKernelGGL((k_norm_back<E, T, NV, true>), dim3(parts), dim3(kBackT<T>), 0, st, A);
+        else hipLaunchKernelGGL((k_norm_back<E, T, NV, false>), dim3(parts), dim3(kBackT<T>), 0, st, A);
       });
     };
     if (dtype == UMAS_BF16) run(uint16_t{});
