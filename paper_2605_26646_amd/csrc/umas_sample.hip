@@ -260,7 +260,7 @@ k_sample_open(Logits<In> L, Settings S, const int32_t* __restrict__ rowsel, int6
 // ------------------------------------------------------------------ second launch
 constexpr int kBins = 2048, kCounts = 4096;                  // of eleven bits of a key, and of distances to the front
 constexpr int kTopRank = 64;
-constexpr int kListCap = 2048, kRanked = 256;                // tokens of a list, and of one that is ordered by comparing all with all
+constexpr int kListCap = 4096, kRanked = 512;                // tokens of a list, and of one that is ordered by comparing all with all
 constexpr int kGroupCap = 1024;
 // Sums and scans over a workgroup of T threads: what the wavefronts have goes through one of two buffers in turn, so that one barrier is enough.
 template <int T>
@@ -322,16 +322,18 @@ struct Block {
     return v;
   }
 };
-// LIST: tokens that are listed; WEIGHTS: their weights beside them.
-template <int T, int LIST = kListCap, bool WEIGHTS = true>
+// LIST: tokens that are listed; ALL: with their weights, and the units' sums.
+template <int T, int LIST = kListCap, bool ALL = true>
 struct RowShared {
   static constexpr int kList = LIST;
   u64 block[2][2][T / kWave];
   u64 bins[kBins];                                           // masses or counts
-  u64 list_w[WEIGHTS ? LIST : 1];
+  u64 list_w[ALL ? LIST : 1];
+  u64 unit[ALL ? kMaxSampleV / kUnit : 1];
   float list_z[LIST];
   int list_id[LIST];
   float top[4][kWave];
+  int rank[kRanked];
   u64 found_above, found_here, found_rest;
   double found_drest;
   uint32_t found_bin;
@@ -589,9 +591,9 @@ __device__ __forceinline__ float front_bound(const float* __restrict__ group_max
   __syncthreads();
   return s.top[0][rank - 1];
 }
-// Lists the tokens with z >= bound; false: more than there is room for.
+// Lists the tokens with z >= bound; false: they lie in more than so many groups, or are more than there is room for.
 template <typename In, int T, class Shared>
-__device__ __forceinline__ bool list_front(const RowSource<In, T>& row, const float* __restrict__ group_max, float bound, Shared& s) {
+__device__ __forceinline__ bool list_front(const RowSource<In, T>& row, const float* __restrict__ group_max, float bound, int most_groups, Shared& s) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, groups = row.units * kGroupsPerUnit;
   int* const s_group = reinterpret_cast<int*>(s.bins);
   if (threadIdx.x == 0) s.n_list = s.n_groups = 0;
@@ -607,7 +609,7 @@ __device__ __forceinline__ bool list_front(const RowSource<In, T>& row, const fl
   }
   __syncthreads();
   const int n = s.n_groups;
-  if (n > kGroupCap) return false;
+  if (n > most_groups) return false;
   constexpr int kAtOnce = 4;
   for (int i = wave; i < n; i += T / kWave * kAtOnce) {
     float x[kAtOnce];
@@ -636,15 +638,16 @@ __device__ __forceinline__ bool list_front(const RowSource<In, T>& row, const fl
   return s.n_list <= Shared::kList;
 }
 // What the listed tokens say, where they are enough: id -1 where they are not.  Each is compared with all of them, once by its logit and once by its number, by
-// the threads that it has: sixteen of up to 64 tokens, four of up to 256.
+// the threads that it has: of 1024 sixteen for up to 64 tokens, two for up to 512.
 template <int T, class Shared>
 __device__ __forceinline__ Drawn draw_from_front(Shared& s, Block<T>& all, int n, float bound, bool all_listed, const RowDraw& d) {
   u64* const s_key = s.bins;                                 // [kRanked] each
   u64* const s_w = s.bins + kRanked;
   u64* const s_sorted = s.bins + 2 * kRanked;
-  int* const s_rank = reinterpret_cast<int*>(s.bins + 3 * kRanked);
-  u64* const s_run = s.bins + 4 * kRanked;
-  const int of = n <= kWave ? kWave : n <= 2 * kWave ? 2 * kWave : kRanked, parts = T / of;
+  u64* const s_run = s.bins + 3 * kRanked;
+  static_assert(4 * kRanked <= kBins && kRanked <= T, "a thread at the least to a token");
+  int* const s_rank = s.rank;
+  const int of = n <= kWave ? kWave : n <= 2 * kWave ? 2 * kWave : n <= 4 * kWave ? 4 * kWave : kRanked, parts = T / of;
   const int i = threadIdx.x & (of - 1), part = threadIdx.x / of;   // a part to whole wavefronts
   const bool one = part == 0 && i < n;                       // the token's own thread
   u64 w = 0;
@@ -717,9 +720,12 @@ struct Binning {
     scale = kCountsPerOne * fminf(static_cast<float>(c / kLog2e64), 1.f);
     // below lo nothing counts: weights under min_p, or so small that all tokens together with them are not what top_p leaves out
     const double least = d.by_min() ? d.m : d.k > 0 || d.p == 1.0 ? 0.0 : (1.0 - d.p) * d.all / V;
-    if (!(least > 0.0)) return;
-    lo = static_cast<float>(d.w.top + static_cast<double>(__log2f(static_cast<float>(least))) / c * (1.0 + 1e-6));
-    lo -= fabsf(lo) * 1e-6f + static_cast<float>(1e-5 / c);
+    if (least > 0.0) lo = least_logit(d, least);
+  }
+  // A logit that is below all whose weight is `least` or more, but not far.
+  __device__ __forceinline__ static float least_logit(const RowDraw& d, double least) {
+    const float z = static_cast<float>(d.w.top + static_cast<double>(__log2f(static_cast<float>(least))) / d.w.c * (1.0 + 1e-6));
+    return z - (fabsf(z) * 1e-6f + static_cast<float>(1e-5 / d.w.c));
   }
   __device__ __forceinline__ bool has(float z) const { return z < bound && z >= lo && z > -INFINITY; }
   __device__ __forceinline__ int bin(float z) const { return static_cast<int>(fminf((bound - z) * scale, static_cast<float>(kCounts - 1))); }
@@ -860,7 +866,10 @@ __device__ __forceinline__ void sum_units(const RowSource<In, T>& row, const Bin
         const bool has = q.has(x[i]), list = has && r.lists(x[i]);
         if (list) mask |= 1u << i;
         const float z = has && !list && x[i] > r.last ? x[i] : -INFINITY;   // a weight of nothing
-        if (!total_open) {
+        if (!__ballot(z > -INFINITY)) {
+          unit += RowDraw::kNothing;
+          if (total_open) rest += RowDraw::kNothing;
+        } else if (!total_open) {
           unit += d.bits(d.w(z > r.sure ? z : -INFINITY));
         } else {
           const u64 w = d.bits(d.w(z));
@@ -1086,8 +1095,7 @@ enum class Filter { kNone, kSome, kSomeInOne };              // no row has one; 
 template <typename In, int T, Filter FILTER>
 __global__ void __launch_bounds__(T)
 k_sample_row(Logits<In> L, RowCalls C, FlatWs F) {
-  extern __shared__ u64 s_unit[];                            // [units], kSomeInOne only
-  __shared__ std::conditional_t<FILTER == Filter::kNone, PlainShared<T>, std::conditional_t<FILTER == Filter::kSome, RowShared<T, 4 * kRanked, false>, RowShared<T>>> s;
+  __shared__ std::conditional_t<FILTER == Filter::kNone, PlainShared<T>, std::conditional_t<FILTER == Filter::kSome, RowShared<T, 2 * kRanked, false>, RowShared<T>>> s;
   const int64_t m = blockIdx.x, row = C.rowsel ? C.rowsel[C.c0 + m] : C.c0 + m;
   const float* const unit_max = C.A.unit + m * L.units;
   const float* const ref_of = C.A.ref + m * L.units;
@@ -1127,11 +1135,22 @@ k_sample_row(Logits<In> L, RowCalls C, FlatWs F) {
       id = draw_unfiltered(src, s, block, ref_of, mass_of, w, u, all).id;
     } else {
       const float* const group_max = C.A.group + m * L.units * kGroupsPerUnit;
-      float bound = L.V <= kRanked ? -INFINITY : front_bound<T>(group_max, L.units * kGroupsPerUnit, s);
+      float bound = -INFINITY;                               // up to as many as can be ordered: all of them
       Drawn got{-1, 0};
       int n = 0;
       if (!src.extreme.is) {
-        const bool listed = list_front(src, group_max, bound, s);
+        // under min_p what is not below its border is all that counts, where that is not too much
+        bool listed = false;
+        if (d.by_min()) {
+          const float least = Binning::least_logit(d, d.m);
+          listed = list_front(src, group_max, least, kRanked, s) && s.n_list <= kRanked;
+          __syncthreads();
+          if (listed) bound = least;
+        }
+        if (!listed) {
+          if (L.V > kRanked) bound = front_bound<T>(group_max, L.units * kGroupsPerUnit, s);
+          listed = list_front(src, group_max, bound, kGroupCap, s);
+        }
         n = s.n_list;
         __syncthreads();
         if (listed && n <= kRanked) got = draw_from_front(s, block, n, bound, bound == -INFINITY, d);
@@ -1171,12 +1190,12 @@ k_sample_row(Logits<In> L, RowCalls C, FlatWs F) {
             if (threadIdx.x == 0) s.n_list = n;
             __syncthreads();
             u64 sure = 0, rest = 0;
-            sum_units(src, q, r, d, 0, L.units, s_unit, s.list_z, s.list_id, &s.n_list, kListCap, sure, rest);
+            sum_units(src, q, r, d, 0, L.units, s.unit, s.list_z, s.list_id, &s.n_list, kListCap, sure, rest);
             block.sum(sure, rest);
-            if (s.n_list <= kListCap) got = draw_listed(src, s, block, s_unit, q, r, n, s.n_list, sure, rest, d);
+            if (s.n_list <= kListCap) got = draw_listed(src, s, block, s.unit, q, r, n, s.n_list, sure, rest, d);
             __syncthreads();
           }
-          if (got.id < 0) got = draw_by_passes<In, T>(src, &s, block.turn, s_unit, d);
+          if (got.id < 0) got = draw_by_passes<In, T>(src, &s, block.turn, s.unit, d);
         }
       }
       id = got.id;
@@ -1244,7 +1263,7 @@ k_sample_bracket(RowCalls C, FlatWs F, int V) {
   if (threadIdx.x == 0) state.bracket = r;
 }
 // ... then the sums and lists, ...
-constexpr int kSumUnits = 8, kSumList = 1024;               // of a workgroup
+constexpr int kSumUnits = 8, kSumList = 2048;               // of a workgroup
 template <typename In, int T>
 __global__ void __launch_bounds__(T, 4)
 k_sample_sums(Logits<In> L, RowCalls C, FlatWs F) {
@@ -1285,7 +1304,6 @@ k_sample_sums(Logits<In> L, RowCalls C, FlatWs F) {
 template <typename In, int T>
 __global__ void __launch_bounds__(T)
 k_sample_flat(Logits<In> L, RowCalls C, FlatWs F) {
-  extern __shared__ u64 s_unit[];                            // [units]
   __shared__ RowShared<T> s;
   if (static_cast<int>(blockIdx.x) >= *F.count) return;
   const int64_t m = F.order[blockIdx.x];
@@ -1304,12 +1322,12 @@ k_sample_flat(Logits<In> L, RowCalls C, FlatWs F) {
       s.list_id[i] = F.list_id[m * kListCap + i];
     }
     u64 sure = 0;
-    for (int i = threadIdx.x; i < L.units; i += T) sure += s_unit[i] = F.unit_sum[m * L.units + i];
+    for (int i = threadIdx.x; i < L.units; i += T) sure += s.unit[i] = F.unit_sum[m * L.units + i];
     sure = block.sum(sure);
-    got = draw_listed(src, s, block, s_unit, Binning(state.bound, d, L.V), state.bracket, state.n_front, n, sure, state.rest, d);
+    got = draw_listed(src, s, block, s.unit, Binning(state.bound, d, L.V), state.bracket, state.n_front, n, sure, state.rest, d);
     __syncthreads();
   }
-  if (got.id < 0) got = draw_by_passes<In, T>(src, &s, block.turn, s_unit, d);
+  if (got.id < 0) got = draw_by_passes<In, T>(src, &s, block.turn, s.unit, d);
   if (threadIdx.x == 0) write_drawn(C.out, row, got.id, src.at(got.id), ref, state.sum, t, static_cast<double>(got.mass) / d.one);
 }
 // what the call defines on rows that are not selected
@@ -1462,7 +1480,6 @@ template <typename In>
 umas_status sample_rows(const Logits<In>& L, const Settings& S, const int32_t* rowsel, int64_t c0, int64_t rows, const SampleWs& w, const float* u, const SampleOut& out,
                         hipStream_t st) {
   const unsigned n = static_cast<unsigned>(rows);
-  const size_t unit_bytes = L.units * sizeof(u64);
   hipLaunchKernelGGL(k_sample_open<In>, dim3(cdiv(L.units, 2 * kOpenPairs), n), dim3(kOpenT), 0, st, L, S, rowsel, c0, w.A, w.flat.parts > 0 ? w.flat.count : nullptr);
   UMAS_LAUNCHED("k_sample_open");
   const bool plain = !S.top_k_of && !S.top_p_of && !S.min_p_of && S.min_p == 0.0 && S.top_p == 1.0 && (S.top_k == 0 || S.top_k >= L.V);
@@ -1473,8 +1490,10 @@ umas_status sample_rows(const Logits<In>& L, const Settings& S, const int32_t* r
     UMAS_LAUNCHED("k_sample_row");
     return UMAS_OK;
   }
-  if (w.flat.parts == 0) {
-    hipLaunchKernelGGL((k_sample_row<In, kOneT, Filter::kSomeInOne>), dim3(n), dim3(kOneT), unit_bytes, st, L, C, w.flat);
+  // the front decides where it holds the first k, but for rows of many equal logits: no launches for others, which cost 4 us each where there is nothing for them to do
+  const bool decided = !S.top_k_of && S.top_k >= 1 && S.top_k <= std::min(kTopRank, L.units * kGroupsPerUnit / 8);
+  if (w.flat.parts == 0 || decided) {
+    hipLaunchKernelGGL((k_sample_row<In, kOneT, Filter::kSomeInOne>), dim3(n), dim3(kOneT), 0, st, L, C, w.flat);
     UMAS_LAUNCHED("k_sample_row");
     return UMAS_OK;
   }
@@ -1487,7 +1506,7 @@ umas_status sample_rows(const Logits<In>& L, const Settings& S, const int32_t* r
   UMAS_LAUNCHED("k_sample_bracket");
   hipLaunchKernelGGL((k_sample_sums<In, kSumT>), dim3(cdiv(L.units, kSumUnits), n), dim3(kSumT), 0, st, L, C, w.flat);
   UMAS_LAUNCHED("k_sample_sums");
-  hipLaunchKernelGGL((k_sample_flat<In, kFlatT>), dim3(n), dim3(kFlatT), unit_bytes, st, L, C, w.flat);
+  hipLaunchKernelGGL((k_sample_flat<In, kFlatT>), dim3(n), dim3(kFlatT), 0, st, L, C, w.flat);
   UMAS_LAUNCHED("k_sample_flat");
   return UMAS_OK;
 }
