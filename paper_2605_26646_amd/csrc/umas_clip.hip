@@ -263,7 +263,7 @@ extern "C" umas_status umas_clip_gradients(const umas_gradient* gradients, int32
   UMAS_REQUIRE(n >= 0, UMAS_EINVAL, "negative count of gradients");
   UMAS_REQUIRE(gradients || n == 0, UMAS_EINVAL, "gradients must not be NULL");
   UMAS_REQUIRE(max_norm > 0.0, UMAS_EINVAL, "max_norm must be positive");
-  UMAS_REQUIRE(stats, UMAS_EINVAL, "stats must not be NULL");
+  UMAS_REQUIRE(stats && reinterpret_cast<uintptr_t>(stats) % 8 == 0, UMAS_EINVAL, "stats must not be NULL, and 8-byte aligned");
   uint64_t chunks = 0;
   for (int32_t i = 0; i < n; ++i) {
     const umas_gradient& g = gradients[i];

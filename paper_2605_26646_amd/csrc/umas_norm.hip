@@ -93,86 +93,87 @@ k_rms_norm(NormArgs A) {
   constexpr int N = Piece<E>::N, kRows = kNT / T;
   __shared__ float s_red[kNT / kWave];
   const int t = threadIdx.x % T, pieces = (A.d + N - 1) / N;
-  const int64_t row = static_cast<int64_t>(blockIdx.x) * kRows + threadIdx.x / T;
-  if (row >= A.n) return;                                    // whole wavefronts; with T = kNT none
-  const E* const x = static_cast<const E*>(A.x) + row * A.d;
-  const E* const r = A.residual ? static_cast<const E*>(A.residual) + row * A.d : nullptr;
-  E* const hidden = A.hidden ? static_cast<E*>(A.hidden) + row * A.d : nullptr;
-  u32x4u v[NV], g[NV];
+  // a row to a workgroup or wavefront, and more only where there are more than a grid holds
+  for (int64_t row = static_cast<int64_t>(blockIdx.x) * kRows + threadIdx.x / T; row < A.n; row += static_cast<int64_t>(gridDim.x) * kRows) {
+    const E* const x = static_cast<const E*>(A.x) + row * A.d;
+    const E* const r = A.residual ? static_cast<const E*>(A.residual) + row * A.d : nullptr;
+    E* const hidden = A.hidden ? static_cast<E*>(A.hidden) + row * A.d : nullptr;
+    u32x4u v[NV], g[NV];
 #pragma unroll
-  for (int k = 0; k < NV; ++k) v[k] = t + k * T < pieces ? load_piece(x, t + k * T, A.d) : u32x4u{0u, 0u, 0u, 0u};
-  if (r) {
-    u32x4u w[NV];
+    for (int k = 0; k < NV; ++k) v[k] = t + k * T < pieces ? load_piece(x, t + k * T, A.d) : u32x4u{0u, 0u, 0u, 0u};
+    if (r) {
+      u32x4u w[NV];
 #pragma unroll
-    for (int k = 0; k < NV; ++k) w[k] = t + k * T < pieces ? load_piece(r, t + k * T, A.d) : u32x4u{0u, 0u, 0u, 0u};
+      for (int k = 0; k < NV; ++k) w[k] = t + k * T < pieces ? load_piece(r, t + k * T, A.d) : u32x4u{0u, 0u, 0u, 0u};
+#pragma unroll
+      for (int k = 0; k < NV; ++k) {
+        float a[N], b[N];
+        Piece<E>::unpack(v[k], a);
+        Piece<E>::unpack(w[k], b);
+#pragma unroll
+        for (int i = 0; i < N; ++i) a[i] += b[i];
+        v[k] = Piece<E>::pack(a);                              // the norm is of the sum as it is stored
+        if (hidden && t + k * T < pieces) store_piece(hidden, t + k * T, A.d, v[k]);
+      }
+    }
+#pragma unroll
+    for (int k = 0; k < NV; ++k) g[k] = t + k * T < pieces ? load_piece(static_cast<const E*>(A.gain), t + k * T, A.d) : u32x4u{0u, 0u, 0u, 0u};
+    float sum = 0.f;
 #pragma unroll
     for (int k = 0; k < NV; ++k) {
-      float a[N], b[N];
+      float a[N];
       Piece<E>::unpack(v[k], a);
-      Piece<E>::unpack(w[k], b);
 #pragma unroll
-      for (int i = 0; i < N; ++i) a[i] += b[i];
-      v[k] = Piece<E>::pack(a);                              // the norm is of the sum as it is stored
-      if (hidden && t + k * T < pieces) store_piece(hidden, t + k * T, A.d, v[k]);
+      for (int i = 0; i < N; ++i) sum = fmaf(a[i], a[i], sum);
     }
-  }
-#pragma unroll
-  for (int k = 0; k < NV; ++k) g[k] = t + k * T < pieces ? load_piece(static_cast<const E*>(A.gain), t + k * T, A.d) : u32x4u{0u, 0u, 0u, 0u};
-  float sum = 0.f;
-#pragma unroll
-  for (int k = 0; k < NV; ++k) {
-    float a[N];
-    Piece<E>::unpack(v[k], a);
-#pragma unroll
-    for (int i = 0; i < N; ++i) sum = fmaf(a[i], a[i], sum);
-  }
-  sum = row_reduce<T>(sum, s_red, add);
-  const float inv = 1.f / sqrtf(sum / static_cast<float>(A.d) + A.eps);
-  if (A.inv_rms && t == 0) A.inv_rms[row] = inv;
-  float c = 0.f;
-#pragma unroll
-  for (int k = 0; k < NV; ++k) {
-    float a[N], b[N];
-    Piece<E>::unpack(v[k], a);
-    Piece<E>::unpack(g[k], b);
-#pragma unroll
-    for (int i = 0; i < N; ++i) {
-      a[i] = a[i] * inv * b[i];
-      if constexpr (QUANT) c = most(c, fabsf(a[i]));
-    }
-    if constexpr (!QUANT)
-      if (t + k * T < pieces) store_piece(static_cast<E*>(A.y) + row * A.d, t + k * T, A.d, Piece<E>::pack(a));
-  }
-  if constexpr (QUANT) {
-    c = row_reduce<T>(c, s_red, most) / 448.f;
-    if (!(c > 0.f) && c == c) c = 1.f;                       // a row of zeros
-    if (t == 0) A.scale[row] = c;
-    uint8_t* const q = A.q + row * A.d;
+    sum = row_reduce<T>(sum, s_red, add);
+    const float inv = 1.f / sqrtf(sum / static_cast<float>(A.d) + A.eps);
+    if (A.inv_rms && t == 0) A.inv_rms[row] = inv;
+    float c = 0.f;
 #pragma unroll
     for (int k = 0; k < NV; ++k) {
-      if (t + k * T >= pieces) continue;
       float a[N], b[N];
       Piece<E>::unpack(v[k], a);
       Piece<E>::unpack(g[k], b);
 #pragma unroll
       for (int i = 0; i < N; ++i) {
-        a[i] = a[i] * inv * b[i] / c;
-        // the quotient of the largest one may round to just above 448; what is no number stays none
-        a[i] = a[i] > 448.f ? 448.f : a[i] < -448.f ? -448.f : a[i];
+        a[i] = a[i] * inv * b[i];
+        if constexpr (QUANT) c = most(c, fabsf(a[i]));
       }
-      uint32_t w[N / 4];
+      if constexpr (!QUANT)
+        if (t + k * T < pieces) store_piece(static_cast<E*>(A.y) + row * A.d, t + k * T, A.d, Piece<E>::pack(a));
+    }
+    if constexpr (QUANT) {
+      c = row_reduce<T>(c, s_red, most) / 448.f;
+      if (!(c > 0.f) && c == c) c = 1.f;                       // a row of zeros
+      if (t == 0) A.scale[row] = c;
+      uint8_t* const q = A.q + row * A.d;
 #pragma unroll
-      for (int i = 0; i < N / 4; ++i) {
-        int p = __builtin_amdgcn_cvt_pk_fp8_f32(a[4 * i], a[4 * i + 1], 0, false);
-        p = __builtin_amdgcn_cvt_pk_fp8_f32(a[4 * i + 2], a[4 * i + 3], p, true);
-        w[i] = static_cast<uint32_t>(p);
-      }
-      const int at = (t + k * T) * N;
-      if (std::is_same<E, uint16_t>::value) {
-        typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
-        if constexpr (N == 8) *reinterpret_cast<u32x2*>(q + at) = u32x2{w[0], w[1]};
-      } else {
-        for (int i = 0; i < 4 && at + i < A.d; ++i) q[at + i] = static_cast<uint8_t>(w[0] >> (8 * i));
+      for (int k = 0; k < NV; ++k) {
+        if (t + k * T >= pieces) continue;
+        float a[N], b[N];
+        Piece<E>::unpack(v[k], a);
+        Piece<E>::unpack(g[k], b);
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+          a[i] = a[i] * inv * b[i] / c;
+          // the quotient of the largest one may round to just above 448; what is no number stays none
+          a[i] = a[i] > 448.f ? 448.f : a[i] < -448.f ? -448.f : a[i];
+        }
+        uint32_t w[N / 4];
+#pragma unroll
+        for (int i = 0; i < N / 4; ++i) {
+          int p = __builtin_amdgcn_cvt_pk_fp8_f32(a[4 * i], a[4 * i + 1], 0, false);
+          p = __builtin_amdgcn_cvt_pk_fp8_f32(a[4 * i + 2], a[4 * i + 3], p, true);
+          w[i] = static_cast<uint32_t>(p);
+        }
+        const int at = (t + k * T) * N;
+        if (std::is_same<E, uint16_t>::value) {
+          typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+          if constexpr (N == 8) *reinterpret_cast<u32x2*>(q + at) = u32x2{w[0], w[1]};
+        } else {
+          for (int i = 0; i < 4 && at + i < A.d; ++i) q[at + i] = static_cast<uint8_t>(w[0] >> (8 * i));
+        }
       }
     }
   }
@@ -382,8 +383,9 @@ void with_back(int pieces, Launch launch) {
   else if (pieces <= 2048) go(std::integral_constant<int, 1024>(), Two());
   else go(std::integral_constant<int, 1024>(), std::integral_constant<int, 4>());
 }
+constexpr unsigned kNormGrid = 1u << 23;                     // threads of a launch are counted in 32 bits
 constexpr int64_t kWideRows = 2048;                          // up to so many rows a workgroup takes a row
-constexpr int kNormParts = 1024;                             // shares of dg at most
+constexpr int kNormParts = 1024;                             // shares of dg at most (back_parts)
 umas_status check_norm(umas_dtype dt, int64_t n, int d) {
   UMAS_REQUIRE(dt == UMAS_F32 || dt == UMAS_BF16, UMAS_EDTYPE, "dtype=%d is neither F32 nor BF16", static_cast<int>(dt));
   UMAS_REQUIRE(n >= 0, UMAS_EINVAL, "negative row count");
@@ -405,7 +407,7 @@ umas_status norm(const NormArgs& A, umas_dtype dt, hipStream_t st) {
   auto run = [&](auto e) {
     using E = decltype(e);
     with_width(static_cast<int>(cdiv(A.d, Piece<E>::N)), A.n <= kWideRows, [&](auto t, auto nv) {
-      const dim3 grid(cdiv(A.n, kNT / decltype(t)::value));
+      const dim3 grid(std::min(cdiv(A.n, kNT / decltype(t)::value), kNormGrid));
       if (A.q) hipLaunchKernelGGL((k_rms_norm<E, decltype(t)::value, decltype(nv)::value, true>), grid, dim3(kNT), 0, st, A);
       else hipLaunchKernelGGL((k_rms_norm<E, decltype(t)::value, decltype(nv)::value, false>), grid, dim3(kNT), 0, st, A);
     });
