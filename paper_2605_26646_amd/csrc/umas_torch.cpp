@@ -10,6 +10,7 @@
 #include <ATen/ops/empty.h>
 #include <ATen/ops/empty_like.h>
 #include <c10/core/TensorOptions.h>
+#include <c10/core/impl/DeviceGuardImplInterface.h>
 #include <torch/csrc/Exceptions.h>
 #include <torch/csrc/autograd/python_variable.h>
 
@@ -576,9 +577,9 @@ const at::Tensor& whole(PyObject* o, at::ScalarType type, int64_t n, const at::D
 void* whole_or_null(PyObject* o, at::ScalarType type, int64_t n, const at::Device& dev, const char* name) {
   return o == Py_None ? nullptr : whole(o, type, n, dev, name).data_ptr();
 }
-void on_a_gpu(const at::Tensor& t, const char* name) {
-  if (t.is_cuda()) return;
-  PyErr_Format(PyExc_ValueError, "%s and what goes with it must be on a GPU", name);
+void on_a_gpu(const at::Tensor& t, const char* name) {     // the one that the launches go to: their stream is of the current device
+  if (t.is_cuda() && t.device() == c10::impl::getDeviceGuardImpl(at::kCUDA)->getDevice()) return;
+  PyErr_Format(PyExc_ValueError, t.is_cuda() ? "%s and what goes with it must be on the current GPU" : "%s and what goes with it must be on a GPU", name);
   throw Failed();
 }
 void same_address(const char* a, const at::Tensor& x, const char* b, const at::Tensor& y) {   // two outputs of a call
@@ -682,6 +683,14 @@ struct DrawnOutputs {                                     // ids, logp, logq
     whole(logq.t, at::kFloat, n, dev, "logq");
     same_address("logp", logp.t, "logq", logq.t);
   }
+  void apart_from(const at::Tensor& u, PyObject* const* settings) const {   // temperature, top_k, top_p, min_p
+    for (const at::Tensor& o : {logp.t, logq.t}) {
+      same_address("u", u, "an output", o);
+      for (int i : {0, 2, 3})
+        if (THPVariable_Check(settings[i])) same_address("a setting", tensor(settings[i]), "an output", o);
+    }
+    if (THPVariable_Check(settings[1])) same_address("top_k", tensor(settings[1]), "ids", ids.t);
+  }
 };
 PyObject* sample_logits(PyObject* const* a) {             // logits, u, temperature, top_k, top_p, min_p, ids, logp, logq, workspace, stream
   const Rows z(a[0]);
@@ -693,6 +702,7 @@ PyObject* sample_logits(PyObject* const* a) {             // logits, u, temperat
   const at::Tensor& u = whole(a[1], at::kFloat, z.n, dev, "u");
   const umas_sampling s = sampling_of(a + 2, z.n, dev);
   const DrawnOutputs out(a + 6, z.n, dev);
+  out.apart_from(u, a + 2);
   const Output ws(a[9], [&] { return workspace(umas_sample_logits_workspace_bytes(z.n, z.d), dev); });
   in_reach(ws.t, dev, "workspace");
   on_a_gpu(z.t, "logits");
@@ -712,6 +722,7 @@ PyObject* sample_tokens(PyObject* const* a) {             // H, W, u, rowsel, te
   const at::Tensor& u = whole(a[2], at::kFloat, H.n, dev, "u");
   const umas_sampling s = sampling_of(a + 4, H.n, dev);
   const DrawnOutputs out(a + 8, H.n, dev);
+  out.apart_from(u, a + 4);
   const umas_dtype dt = static_cast<umas_dtype>(H.dt);
   const Output ws(a[11], [&] { return workspace(umas_sample_tokens_workspace_bytes(sel.n, H.d, V, dt), dev); });
   in_reach(ws.t, dev, "workspace");

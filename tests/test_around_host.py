@@ -241,3 +241,16 @@ def away(*shape, dtype=F):
 def test_an_array_of_another_device(lib, call, kw):
     with pytest.raises(ValueError, match="device"):
         call(**kw)
+
+
+@pytest.mark.parametrize("call", [native_logits, native_tokens])
+def test_draws_into_what_the_call_reads(lib, call):
+    one, whole = Z(6), Z(6, dtype=I)
+    for kw in (dict(u=one, logp=one), dict(u=one, logq=one), dict(temperature=one, logp=one), dict(top_p=one, logq=one), dict(min_p=one, logp=one), dict(top_k=whole, ids=whole)):
+        with pytest.raises(ValueError, match="different"):
+            call(**kw)
+
+
+def test_statistics_of_clipping_are_aligned(lib):
+    status, message = call_clip(lib, [], stats=260)
+    assert status == -1 and "8-byte" in message
