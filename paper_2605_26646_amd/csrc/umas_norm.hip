@@ -354,19 +354,24 @@ k_norm_gain(const float* __restrict__ part, int parts, int d, int accumulate, fl
 }
 
 // ------------------------------------------------------------------ host side
-// launch(T, NV): threads to a row and pieces to a thread
+// launch(T, NV): threads to a row and pieces to a thread.  One piece: a wavefront, whatever the number of rows (bf16, 512 columns with a residual: 2000 rows 4.3 us, by workgroups
+// 4.6, 40 000 rows 29 and 49).  Up to four: a workgroup while rows are few (2048 columns: 64 rows 4.3 and 4.2 us, in 8 bits 5.9 and 4.3; 1000 rows 5.0 and 4.6; 2000 as
+// fast; 4000 rows 10.9 and 13.0, 40 000 rows 113 and 115).  More: a workgroup (4096 columns: 500 rows 5.8 and 4.7 us, 8000 rows 45.6 and 41.3, in 8 bits 47.2 and 40.4).
+constexpr int64_t kWideRows = 2048;
 template <class Launch>
-void with_width(int pieces, bool wide, Launch launch) {
+void with_width(int pieces, int64_t rows, Launch launch) {
   auto go = [&](auto t) {
     constexpr int T = decltype(t)::value;
     const int nv = static_cast<int>(cdiv(pieces, T));
     if (nv <= 1) launch(t, std::integral_constant<int, 1>());
     else if (nv <= 2) launch(t, std::integral_constant<int, 2>());
     else if (nv <= 4) launch(t, std::integral_constant<int, 4>());
-    else if (nv <= 8) launch(t, std::integral_constant<int, 8>());
-    else launch(t, std::integral_constant<int, 16>());
+    else if constexpr (T == kNT) {
+      if (nv <= 8) launch(t, std::integral_constant<int, 8>());
+      else launch(t, std::integral_constant<int, 16>());
+    }
   };
-  if (wide || pieces > 8 * kWave) go(std::integral_constant<int, kNT>());
+  if (pieces > 4 * kWave || (pieces > kWave && rows <= kWideRows)) go(std::integral_constant<int, kNT>());
   else go(std::integral_constant<int, kWave>());
 }
 // ... of the backward pass: two pieces, from 2048 on (float32, 16 384 columns are 4096 pieces) four
@@ -384,7 +389,6 @@ void with_back(int pieces, Launch launch) {
   else go(std::integral_constant<int, 1024>(), std::integral_constant<int, 4>());
 }
 constexpr unsigned kNormGrid = 1u << 23;                     // threads of a launch are counted in 32 bits
-constexpr int64_t kWideRows = 2048;                          // up to so many rows a workgroup takes a row
 constexpr int kNormParts = 1024;                             // shares of dg at most (back_parts)
 umas_status check_norm(umas_dtype dt, int64_t n, int d) {
   UMAS_REQUIRE(dt == UMAS_F32 || dt == UMAS_BF16, UMAS_EDTYPE, "dtype=%d is neither F32 nor BF16", static_cast<int>(dt));
@@ -406,7 +410,7 @@ umas_status norm(const NormArgs& A, umas_dtype dt, hipStream_t st) {
   if (A.n == 0) return UMAS_OK;
   auto run = [&](auto e) {
     using E = decltype(e);
-    with_width(static_cast<int>(cdiv(A.d, Piece<E>::N)), A.n <= kWideRows, [&](auto t, auto nv) {
+    with_width(static_cast<int>(cdiv(A.d, Piece<E>::N)), A.n, [&](auto t, auto nv) {
       const dim3 grid(std::min(cdiv(A.n, kNT / decltype(t)::value), kNormGrid));
       if (A.q) hipLaunchKernelGGL((k_rms_norm<E, decltype(t)::value, decltype(nv)::value, true>), grid, dim3(kNT), 0, st, A);
       else hipLaunchKernelGGL((k_rms_norm<E, decltype(t)::value, decltype(nv)::value, false>), grid, dim3(kNT), 0, st, A);
