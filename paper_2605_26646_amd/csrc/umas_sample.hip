@@ -663,7 +663,10 @@ __device__ __forceinline__ Drawn draw_from_front(Shared& s, Block<T>& all, int n
     s_run[i] = 0;
     if (i < n) w = d.weight(s.list_z[i]);
   }
-  if (threadIdx.x == 0) s.found_id = -1;
+  if (threadIdx.x == 0) {
+    s.found_id = -1;
+    s.n_groups = 0;
+  }
   __syncthreads();
   const u64 key = s_key[i];
   const int j0 = part * (of / parts), j1 = min(j0 + of / parts, n);
@@ -699,6 +702,29 @@ __device__ __forceinline__ Drawn draw_from_front(Shared& s, Block<T>& all, int n
   if (one) s_w[i] = w = s_sorted[rank];
   __syncthreads();
   const uint32_t mine = static_cast<uint32_t>(key);          // falls with the token
+  if (of > 2 * kWave) {                                      // many: by runs of tokens first, then among those of the run
+    const u64 target = d.target(mass);
+    const int id = s.list_id[i], run = id >> max(d.id_bits - (of == kRanked ? 9 : 8), 0);
+    if (one && w) atomicAdd(&s_run[run], w);
+    __syncthreads();
+    u64 total;
+    const u64 in_run = part == 0 ? s_run[i] : 0, before = all.scan(in_run, &total);
+    if (before <= target && target < before + in_run) {
+      s.found_bin = i;
+      s.found_rest = before;
+    }
+    __syncthreads();
+    const bool member = one && w && run == static_cast<int>(s.found_bin);
+    if (member) s_rank[atomicAdd(&s.n_groups, 1)] = i;
+    __syncthreads();
+    if (member) {
+      u64 upto = s.found_rest;
+      for (int m = 0; m < s.n_groups; ++m) upto += static_cast<uint32_t>(s_key[s_rank[m]]) >= mine ? s_w[s_rank[m]] : 0;
+      if (target < upto && upto - w <= target) s.found_id = id;
+    }
+    __syncthreads();
+    return Drawn{s.found_id, mass};
+  }
   if (i < n && j0 < j1) {
     u64 run = 0;
 #pragma unroll 8
