@@ -522,7 +522,8 @@ umas_status umas_distill_fwd_bwd(const void* H, const void* W, umas_dtype dtype,
  *   hidden       DEVICE [n_rows, d]: s, what goes on past the norm; NULL exactly where residual is.  It may be x or residual themselves.
  *   y            DEVICE [n_rows, d]; may be x
  *   inv_rms      DEVICE float [n_rows]: i, for the backward pass; may be NULL
- * All arrays but inv_rms have the type dtype and are 16-byte aligned; 1 <= d <= 16384, a multiple of 8 for bf16.  Sums are float32.
+ * All arrays but inv_rms have the type dtype and are 16-byte aligned; 1 <= d <= 16384, a multiple of 8 for bf16.  Sums are float32.  But for what is
+ * said here, outputs overlap neither each other nor what is read; so in the calls below.
  *
  * umas_rms_norm_quantized leaves y in 8 bits instead: q = y / scale in e4m3 (4 bits of exponent, 3 of mantissa, no infinities, largest 448), rounded to
  * nearest, scale_i = max_j |y_ij| / 448 and 1 for a row of zeros; y is not rounded on the way.
@@ -551,8 +552,9 @@ umas_status umas_rms_norm_bwd(const void* dy, const void* hidden, const void* ga
  *   the first top_k (0, or V and more: all); of these those with w_v >= min_p; of these the shortest run from the front whose mass
  *   (sum of w) reaches top_p of the mass of them all (1: all).  The token is the first, in rising order, at which the running mass of
  *   what is kept passes u times the kept mass.
- * Logits of -infinity and those that are no number are never drawn and have no mass.  Masses are float64 or exact: tokens whose w is below 2^-39 to 2^-52
- * (2^-44 at 151 936 tokens) count as 0 where a filter is on.  The same inputs give the same token, whatever the other rows and the workspace are.
+ * Logits of -infinity and those that are no number are never drawn and have no mass.  Masses are float64, or where a filter is on whole numbers of 2^-s,
+ * s = min(51, 62 - log2 V rounded up) (2^-44 at 151 936 tokens): a w below half of that counts as 0 there.  A w itself is off by 2.2e-12 of its value at most.
+ * The same inputs give the same token, whatever the other rows and the workspace are.
  *   logits       DEVICE [n_rows, V] of the type dtype, row i at logits + i * row_stride, row_stride >= V, aligned to its type
  *   u            DEVICE float [n_rows], uniform on [0,1); below 0 or no number counts as 0, from 1 on the last kept token is drawn
  *   ids          DEVICE int32 [n_rows]; -1 for a row that has nothing to draw from
@@ -560,7 +562,8 @@ umas_status umas_rms_norm_bwd(const void* dy, const void* hidden, const void* ga
  *   logq         DEVICE float [n_rows] or NULL: log-probability of the token under what it was drawn from; 0 where id is -1
  * umas_sample_tokens takes the logits from a head, z = W h_i (float accumulate), for the selected rows; ids, logp and logq of other rows are -1, 0
  * and 0.  H, W, rowsel, n_sel, dtype and their limits as in umas_policy_logprobs; u and the settings of a row lie at its number in [0, n_rows).
- * The workspace bounds of how many rows logits are kept on the way, at least 256.  V <= UMAS_MAX_SAMPLE_V. */
+ * The workspace bounds of how many rows logits are kept on the way, at least 256.  V <= UMAS_MAX_SAMPLE_V.  ids, logp and logq overlap nothing that
+ * the call reads, u and the settings' arrays among it. */
 typedef struct umas_sampling {
   double temperature;            /* >= 0; 0: the largest logit, of equal ones the lowest token (top_k, top_p and min_p change nothing then) */
   double top_p;                  /* in [0,1] */
@@ -588,7 +591,7 @@ umas_status umas_sample_tokens(const void* H, const void* W, umas_dtype dtype, i
  *   gradients  HOST [n], read inside the call: arrays of any size, each of its own type, aligned to that; out is grad (in place; with c = 1 nothing is
  *              written) or another array of the same type and size.  No output may overlap anything else of the list (UMAS_EINVAL).
  *   max_norm   > 0; infinity: the norm alone
- *   stats      DEVICE umas_clip_stats
+ *   stats      DEVICE umas_clip_stats, 8-byte aligned, outside the arrays
  * The call may be recorded into a graph: the list travels with the launches. */
 typedef struct umas_gradient {
   const void* grad;

@@ -3,12 +3,18 @@
 //   w_v = exp((z_v - max z) / T);  tokens in falling order of z, equal ones in rising order;  the first k of them;  of these those with w >= min_p;  of these
 //   the shortest run from the front whose mass reaches top_p of theirs;  of what is kept, in rising order of tokens, the first whose running mass passes
 //   u times the kept mass
-// A uniform number may fall next to a border between two tokens, so masses are float64 or whole numbers: w in units of 2^-s, s = 62 - log2 V, at most 52, whose
-// sums are exact in any order (64-bit atomics in LDS give the same result whichever comes first).
+// A uniform number may fall next to a border between two tokens, so masses are float64 where nothing is filtered, and else whole numbers: w in units of 2^-s, s = min(51, 62 - log2 V),
+// whose sums are exact in any order (64-bit atomics in LDS give the same result whichever comes first).
 //
-// Two launches.  The first reads the logits once: maxima of groups of 64, and of units of 1024 the maximum, the mass at T and the sum of exponentials.  The second gives
-// a workgroup to a row.  Without filters the unit and then the token are found from the units' masses; thresholds are found by their bits, eleven at a time from
-// the top, with a histogram of counts or masses.
+// The first launch, k_sample_open, is the one pass over all logits: maxima of groups of 64, and of units of 1024 the maximum, the sum of exponentials and, where all tokens' mass decides,
+// that mass in float64.  From memory that is a read at 5.6 TB/s (400 float32 rows of 151 936: 43 us); where float64 exponentials count, they bound it (twelve float64 instructions a
+// logit of 5.4 cycles each: 777 float32 rows of 50 001 37 us, 156 MB at 4.2 TB/s).
+// The second, k_sample_row, gives a workgroup to a row.  Without filters the unit and then the token are found from the units' masses.  Else the front is listed: the tokens that the
+// 64th largest of the threads' group maxima bounds, or all that min_p leaves; up to 512 of them decide by themselves if nothing behind them can count (13 us for a row of 152 064, 14 for 256).
+// Rows that are spread, whose border lies behind the front, go through four more launches over the chip: counts of the tokens by their distance to the front (k_sample_count), from these the
+// thresholds between which a border lies (k_sample_bracket), the sums above and lists between them (k_sample_sums), and the border and token from those (k_sample_flat): 11, 9,
+// 32 and 21 us for what is spread among 256 rows.  Up to four rows do all of it in the second launch.  Where lists overflow, with floods of equal logits, thresholds are found bit by bit, eleven
+// at a time from the top, with a histogram of counts or masses (draw_by_passes): right for every row, and slow.
 #include <float.h>
 
 #include <algorithm>
@@ -227,7 +233,7 @@ k_sample_open(Logits<In> L, Settings S, const int32_t* __restrict__ rowsel, int6
   const float most = larger(top[0], top[1]);
   double mass[2] = {0.0, 0.0}, sum[2] = {0.0, 0.0};
   if (most > -INFINITY) {
-    // float64 exponentials only where they count: 256 bf16 rows of 152 064 with settings of their own @@
+    // float64 exponentials only where they count: 256 bf16 rows of 152 064 with settings of their own 40 -> 25.6 us, 400 float32 rows under min_p 53 -> 43
     const double t = S.t(row);
     const bool drawn = S.of_all(row, L.V);
     const Extreme extreme(most);
@@ -266,7 +272,7 @@ k_sample_open(Logits<In> L, Settings S, const int32_t* __restrict__ rowsel, int6
 // ------------------------------------------------------------------ second launch
 constexpr int kBins = 2048, kCounts = 4096;                  // of eleven bits of a key, and of distances to the front
 constexpr int kTopRank = 64;
-constexpr int kListCap = 4096, kRanked = 512;                // tokens of a list, and of one that is ordered by comparing all with all
+constexpr int kListCap = 4096, kRanked = 512, kCompared = 128;   // tokens of a list, of one that decides by itself, and of one that is ordered by comparing all with all
 constexpr int kGroupCap = 1024;
 // Sums and scans over a workgroup of T threads: what the wavefronts have goes through one of two buffers in turn, so that one barrier is enough.
 template <int T>
@@ -343,7 +349,7 @@ struct RowShared {
   u64 found_above, found_here, found_rest;
   double found_drest;
   uint32_t found_bin;
-  int found_id, n_list, n_groups;
+  int found_id, n_list, n_groups, n_members[3];
 };
 // A row's settings and what the first launch says about it.
 struct RowDraw {
@@ -643,17 +649,17 @@ __device__ __forceinline__ bool list_front(const RowSource<In, T>& row, const fl
   __syncthreads();
   return s.n_list <= Shared::kList;
 }
-// What the listed tokens say, where they are enough: id -1 where they are not.  Each is compared with all of them, once by its logit and once by its number, by
-// the threads that it has: of 1024 sixteen for up to 64 tokens, two for up to 512.
+// What the listed tokens say, where they are enough: id -1 where they are not.  Up to 128 tokens: each is compared with all of them, once by its logit and once by its number, by
+// the threads that it has: of 1024 sixteen for up to 64 tokens, eight for up to 128.
 template <int T, class Shared>
 __device__ __forceinline__ Drawn draw_from_front(Shared& s, Block<T>& all, int n, float bound, bool all_listed, const RowDraw& d) {
-  u64* const s_key = s.bins;                                 // [kRanked] each
-  u64* const s_w = s.bins + kRanked;
-  u64* const s_sorted = s.bins + 2 * kRanked;
-  u64* const s_run = s.bins + 3 * kRanked;
-  static_assert(4 * kRanked <= kBins && kRanked <= T, "a thread at the least to a token");
+  u64* const s_key = s.bins;                                 // [kCompared] each
+  u64* const s_w = s.bins + kCompared;
+  u64* const s_sorted = s.bins + 2 * kCompared;
+  u64* const s_run = s.bins + 3 * kCompared;
+  static_assert(4 * kCompared <= kBins && kCompared <= T, "a thread at the least to a token");
   int* const s_rank = s.rank;
-  const int of = n <= kWave ? kWave : n <= 2 * kWave ? 2 * kWave : n <= 4 * kWave ? 4 * kWave : kRanked, parts = T / of;
+  const int of = n <= kWave ? kWave : kCompared, parts = T / of;
   const int i = threadIdx.x & (of - 1), part = threadIdx.x / of;   // a part to whole wavefronts
   const bool one = part == 0 && i < n;                       // the token's own thread
   u64 w = 0;
@@ -663,10 +669,7 @@ __device__ __forceinline__ Drawn draw_from_front(Shared& s, Block<T>& all, int n
     s_run[i] = 0;
     if (i < n) w = d.weight(s.list_z[i]);
   }
-  if (threadIdx.x == 0) {
-    s.found_id = -1;
-    s.n_groups = 0;
-  }
+  if (threadIdx.x == 0) s.found_id = -1;
   __syncthreads();
   const u64 key = s_key[i];
   const int j0 = part * (of / parts), j1 = min(j0 + of / parts, n);
@@ -702,29 +705,6 @@ __device__ __forceinline__ Drawn draw_from_front(Shared& s, Block<T>& all, int n
   if (one) s_w[i] = w = s_sorted[rank];
   __syncthreads();
   const uint32_t mine = static_cast<uint32_t>(key);          // falls with the token
-  if (of > 2 * kWave) {                                      // many: by runs of tokens first, then among those of the run
-    const u64 target = d.target(mass);
-    const int id = s.list_id[i], run = id >> max(d.id_bits - (of == kRanked ? 9 : 8), 0);
-    if (one && w) atomicAdd(&s_run[run], w);
-    __syncthreads();
-    u64 total;
-    const u64 in_run = part == 0 ? s_run[i] : 0, before = all.scan(in_run, &total);
-    if (before <= target && target < before + in_run) {
-      s.found_bin = i;
-      s.found_rest = before;
-    }
-    __syncthreads();
-    const bool member = one && w && run == static_cast<int>(s.found_bin);
-    if (member) s_rank[atomicAdd(&s.n_groups, 1)] = i;
-    __syncthreads();
-    if (member) {
-      u64 upto = s.found_rest;
-      for (int m = 0; m < s.n_groups; ++m) upto += static_cast<uint32_t>(s_key[s_rank[m]]) >= mine ? s_w[s_rank[m]] : 0;
-      if (target < upto && upto - w <= target) s.found_id = id;
-    }
-    __syncthreads();
-    return Drawn{s.found_id, mass};
-  }
   if (i < n && j0 < j1) {
     u64 run = 0;
 #pragma unroll 8
@@ -735,6 +715,120 @@ __device__ __forceinline__ Drawn draw_from_front(Shared& s, Block<T>& all, int n
   if (one && w) {
     const u64 run = s_run[i], target = d.target(mass);
     if (target < run && run - w <= target) s.found_id = s.list_id[i];
+  }
+  __syncthreads();
+  return Drawn{s.found_id, mass};
+}
+// ... and up to 512: a border, or the token, is found among the sums of 512 runs of logits, or of tokens, and then among those of its run.  (Comparing all with all, a 400 rows' launch
+// with fronts of up to 512 took 48 us, the last step by runs 39; all by runs takes 4 us less of the call's 424.)
+template <int T, class Shared>
+__device__ __forceinline__ Drawn draw_from_long_front(Shared& s, Block<T>& all, int n, float bound, bool all_listed, const RowDraw& d) {
+  u64* const s_key = s.bins;                                 // [kRanked] each
+  u64* const s_w = s.bins + kRanked;
+  u64* const s_mass = s.bins + 2 * kRanked;
+  int* const s_member = reinterpret_cast<int*>(s.bins + 3 * kRanked);
+  int* const s_count = s.rank;
+  static_assert(4 * kRanked <= kBins && kRanked <= T, "a thread at the least to a token, and to a run");
+  const int i = threadIdx.x;
+  const bool one = i < n;
+  if (i < kRanked) s_count[i] = s_mass[i] = 0;
+  if (i < 3) s.n_members[i] = 0;
+  if (i == 0) {
+    s.found_id = -1;
+    s.found_here = 0;
+  }
+  __syncthreads();
+  const float z = one ? s.list_z[i] : 0.f, range = bound > -INFINITY ? d.top - bound : 40.f / static_cast<float>(d.w.c);
+  const int id = one ? s.list_id[i] : 0, run = static_cast<int>(fminf((d.top - z) * (kRanked / range), kRanked - 1.f));   // falling logits; what is no number is the last one's
+  const u64 key = static_cast<u64>(order_of(z)) << 32 | (0xFFFFFFFFu - static_cast<uint32_t>(id));
+  u64 w = one ? d.weight(z) : 0;
+  if (one) {
+    s_key[i] = key;
+    atomicAdd(&s_count[run], 1);
+    if (w) atomicAdd(&s_mass[run], w);
+  }
+  __syncthreads();
+  u64 mass, count, in_run = i < kRanked ? s_mass[i] : 0;
+  const u64 n_run = i < kRanked ? s_count[i] : 0, n_before = all.scan(n_run, &count), before = all.scan(in_run, &mass);
+  if (d.k > 0 && d.k < n) {
+    const u64 k = static_cast<u64>(d.k);
+    if (n_before < k && k <= n_before + n_run) {
+      s.found_bin = i;
+      s.found_rest = n_before;
+      s.found_above = before;
+    }
+    __syncthreads();
+    const int border = static_cast<int>(s.found_bin);
+    const bool member = one && run == border;
+    if (member) s_member[atomicAdd(&s.n_members[0], 1)] = i;
+    __syncthreads();
+    if (member) {
+      u64 rank = s.found_rest;
+      for (int m = 0; m < s.n_members[0]; ++m) rank += s_key[s_member[m]] > key;
+      if (rank >= k) w = 0;
+      else if (w) atomicAdd(&s.found_here, w);
+    } else if (run > border) {
+      w = 0;
+    }
+    __syncthreads();
+    in_run = i < border ? in_run : i == border ? s.found_here : 0;
+    mass = s.found_above + s.found_here;
+  }
+  const bool whole = d.k > 0 || (d.by_min() && d.weight(bound) == 0) || all_listed;   // nothing that is not listed counts
+  u64 need = mass;
+  if (d.p < 1.0) {
+    if (whole) need = d.share(d.p, mass);
+    else {
+      const double part_of = ceil(d.p * d.all * d.one);
+      need = part_of < 1.0 ? 1 : static_cast<u64>(part_of);
+    }
+  }
+  if ((d.k > n && !all_listed) || (!whole && (d.by_min() || d.p == 1.0 || need > mass))) return Drawn{-1, 0};
+  if (need < mass) {
+    if (before < need && need <= before + in_run) {
+      s.found_bin = i;
+      s.found_rest = before;
+    }
+    if (one) s_w[i] = w;
+    __syncthreads();
+    const int border = static_cast<int>(s.found_bin);
+    const bool member = one && w && run == border;
+    if (member) s_member[atomicAdd(&s.n_members[1], 1)] = i;
+    __syncthreads();
+    if (member) {
+      u64 ahead = s.found_rest;
+      for (int m = 0; m < s.n_members[1]; ++m) ahead += s_key[s_member[m]] > key ? s_w[s_member[m]] : 0;
+      if (ahead >= need) w = 0;
+      else if (ahead + w >= need) s.found_above = ahead + w;
+    } else if (run > border) {
+      w = 0;
+    }
+    __syncthreads();
+    mass = s.found_above;
+  }
+  // in rising order of tokens
+  if (i < kRanked) s_mass[i] = 0;
+  if (one) s_w[i] = w;
+  __syncthreads();
+  const u64 target = d.target(mass);
+  const int part = id >> max(d.id_bits - 9, 0);
+  static_assert(kRanked == 1 << 9, "runs of tokens");
+  if (w) atomicAdd(&s_mass[part], w);
+  __syncthreads();
+  u64 total;
+  const u64 in_part = i < kRanked ? s_mass[i] : 0, ahead = all.scan(in_part, &total);
+  if (ahead <= target && target < ahead + in_part) {
+    s.found_bin = i;
+    s.found_rest = ahead;
+  }
+  __syncthreads();
+  const bool member = w && part == static_cast<int>(s.found_bin);
+  if (member) s_member[atomicAdd(&s.n_members[2], 1)] = i;
+  __syncthreads();
+  if (member) {
+    u64 upto = s.found_rest;
+    for (int m = 0; m < s.n_members[2]; ++m) upto += static_cast<uint32_t>(s_key[s_member[m]]) >= static_cast<uint32_t>(key) ? s_w[s_member[m]] : 0;
+    if (target < upto && upto - w <= target) s.found_id = id;
   }
   __syncthreads();
   return Drawn{s.found_id, mass};
@@ -1185,7 +1279,8 @@ k_sample_row(Logits<In> L, RowCalls C, FlatWs F) {
         }
         n = s.n_list;
         __syncthreads();
-        if (listed && n <= kRanked) got = draw_from_front(s, block, n, bound, bound == -INFINITY, d);
+        if (listed && n <= kCompared) got = draw_from_front(s, block, n, bound, bound == -INFINITY, d);
+        else if (listed && n <= kRanked) got = draw_from_long_front(s, block, n, bound, bound == -INFINITY, d);
         if (!listed || n > kRanked) {                        // many that are alike: no front, bins from the largest on
           n = 0;
           bound = INFINITY;

@@ -43,7 +43,7 @@ def draw64(z, u, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0):
     last = torch.where(kept > 0, torch.arange(z.shape[1], device=z.device), 0).max(1).values
     ids = torch.minimum((run <= u.double()[:, None] * run[:, -1:]).sum(1), last)
     at = ids[:, None]
-    return ids, torch.log(p.gather(1, at)[:, 0] / p.sum(1)), torch.log(kept.gather(1, at)[:, 0] / run[:, -1]), (p / p.sum(1, keepdim=True) * ((z - top).abs() + 2)).sum(1)
+    return ids, torch.log(p.gather(1, at)[:, 0] / p.sum(1)), torch.log(kept.gather(1, at)[:, 0] / run[:, -1]), torch.where(p > 0, p / p.sum(1, keepdim=True) * ((z - top).abs() + 2), 0).sum(1)
 
 
 def check(z, u, got, **s):
@@ -82,6 +82,34 @@ def test_filters_that_end_far_behind_the_front(V, kind, dtype):
         check(z, u, got, **s)
         few = [umas.umas_sample_logits(z[a:a + 2], u[a:a + 2], **s) for a in range(0, n, 2)]
         assert same(got, [torch.cat(x) for x in zip(*few)]), s
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("kind", ["flat", "wide", "peaked", "ties", "equal", "rising", "two"])
+@pytest.mark.parametrize("V", [128, 129, 300, 511, 512, 513])
+def test_rows_of_as_many_tokens_as_one_list_holds(V, kind, dtype):
+    gen = torch.Generator("cuda").manual_seed(V + len(kind))
+    n = 12
+    z, u = logits_of(kind, n, V, dtype, gen), torch.rand(n, device="cuda", generator=gen)
+    z[3, :V // 3] = -math.inf
+    z[4, V // 4:] = torch.finfo(z.dtype).min
+    z[5, 2:] = -1e30
+    u[0], u[1] = 0.0, 1.0 - 2.0 ** -24
+    for s in (dict(top_k=1), dict(top_k=V // 2), dict(top_k=V - 1, top_p=0.9), dict(top_p=0.6), dict(top_p=0.999, min_p=0.1), dict(top_k=140, min_p=0.05, top_p=0.5, temperature=2.0),
+              dict(min_p=1.0), dict(top_p=0.0), dict(top_p=0.8, temperature=1e-3)):
+        got = umas.umas_sample_logits(z, u, **s)
+        check(z, u, got, **s)
+        assert same(got, [torch.cat(x) for x in zip(*[umas.umas_sample_logits(z[a:a + 3], u[a:a + 3], **s) for a in range(0, n, 3)])]), s
+
+
+@pytest.mark.parametrize("min_p", [0.3, 0.1, 0.03, 0.01])
+def test_some_hundreds_of_tokens_above_a_border_of_min_p(min_p):
+    gen = torch.Generator("cuda").manual_seed(5)
+    n, V = 48, 50000
+    z = torch.randn(n, V, device="cuda", generator=gen) * torch.linspace(0.3, 3, n, device="cuda")[:, None]
+    u = torch.rand(n, device="cuda", generator=gen)
+    for s in (dict(), dict(top_p=0.9), dict(top_k=200), dict(top_k=150, top_p=0.5)):
+        check(z, u, umas.umas_sample_logits(z, u, min_p=min_p, **s), min_p=min_p, **s)
 
 
 @pytest.mark.parametrize("n", [1, 6])
