@@ -1,10 +1,10 @@
 """One role's model taught by another's, then asked for tokens.
 
 Two roles share a workflow: a planner, whose model is the larger one, and a solver.  The rollout's tokens are routed to the two models; for the solver's
-tokens the planner's head leaves its largest logits (umas_top_logits).  The solver's projection and head are warmed up on the tokens the planner
-would have said (umas_cross_entropy_fwd_bwd), then follow the planner's distribution (umas_distill_fwd_bwd), in micro-batches of whole trajectories
-whose gradients add up.  At the end the solver answers one token at a time: its own largest logits, drawn from with their probabilities under the whole
-vocabulary.  Everything is synthetic: contexts are random vectors, the models are a projection and a head.
+tokens the planner's head leaves its largest logits (umas_top_logits).  The solver's projection, norm (umas_rms_norm, umas_rms_norm_bwd) and head are warmed
+up on the tokens the planner would have said (umas_cross_entropy_fwd_bwd), then follow the planner's distribution (umas_distill_fwd_bwd), in micro-batches
+of whole trajectories whose gradients add up and are clipped to a common norm (umas_clip_gradients).  At the end the solver answers: a token drawn under
+top-k and top-p (umas_sample_tokens).  Everything is synthetic: contexts are random vectors, the models are a projection, a norm and a head.
 
     python examples/teach_role.py [--steps 60] [--rows-per-turn 48] [--vocabulary 4000] [--top 32]
 """
@@ -39,28 +39,36 @@ def projected(x, A, W):
     return (x @ A).bfloat16(), W.bfloat16()
 
 
+def solver(x, A, gain, W):
+    """(hidden states, head, what the norm's backward pass needs)."""
+    h, Wb = projected(x, A, W)
+    H, h, inv_rms = umas.umas_rms_norm(h, gain.bfloat16())
+    return H, Wb, (h, gain.bfloat16(), inv_rms)
+
+
 def train(x, params, opt, parts, n_rows, teach):
-    """One step over all parts: dW adds up in float32, dH rows of the parts go to the projection.  Returns the loss of the step."""
-    A, W = params
-    H, Wb = projected(x, A, W)
+    """One step over all parts: dW and the gain's gradient add up in float32, dH rows of the parts go to the projection.  Returns the loss of the step."""
+    A, gain, W = params
+    H, Wb, behind = solver(x, *params)
     dW = torch.empty(W.shape, dtype=torch.float32, device="cuda")
-    A.grad, loss = torch.zeros_like(A), 0.0
+    A.grad, gain.grad, loss = torch.zeros_like(A), torch.zeros_like(gain), 0.0
     for i, rows in enumerate(parts):
         stats, _, dH, _ = teach(H, Wb, rows, accumulate_dW=i > 0, norm_rows=n_rows, dW=dW)
-        A.grad += x.t() @ dH.float()                 # rows of other parts are zeros
+        dh, _ = umas.umas_rms_norm_bwd(dH, *behind, accumulate_dgain=True, dgain=gain.grad)
+        A.grad += x.t() @ dh.float()                 # rows of other parts are zeros
         loss += float(umas.read_target_stats(stats)["loss"][0])
     W.grad = dW
+    umas.umas_clip_gradients([p.grad for p in params], 1.0)   # what is no number would scale nothing: read_clip_stats says so
     opt.step()
     return loss
 
 
 def answer(x, params, k, gen):
-    """The next token after one context, one of the k largest logits drawn in proportion to their probabilities, and its probability."""
-    H, Wb = projected(x, *params)
-    ids, logits, lse = umas.umas_top_logits(H, Wb, k)
-    p = torch.exp(logits[0] - lse[0])                # under the whole vocabulary
-    j = torch.multinomial(p, 1, generator=gen)[0]
-    return int(ids[0, j]), float(p[j])
+    """The next token after one context, drawn from the first of the k largest logits that hold 0.95 of their mass, and its probability under the whole vocabulary."""
+    H, Wb, _ = solver(x, *params)
+    u = torch.rand(len(x), device="cuda", generator=gen)
+    ids, logp, _ = umas.umas_sample_tokens(H, Wb, u, top_k=k, top_p=0.95)
+    return int(ids[0]), float(logp[0].exp())
 
 
 def main(argv=None):
@@ -87,14 +95,14 @@ def main(argv=None):
     H_t, W_t = projected(x, randn(context, 256) / context ** 0.5, randn(V, 256) * 0.35)
     top_ids, top_logits, lse_t = umas.umas_top_logits(H_t, W_t, k, rows)
 
-    params = [randn(context, 128) / context ** 0.5, 0.05 * randn(V, 128)]
+    params = [randn(context, 128) / context ** 0.5, torch.ones(128, device="cuda"), 0.05 * randn(V, 128)]
     opt = torch.optim.Adam(params, lr=1e-2)
     said = top_ids[:, 0].contiguous()                # -1 on rows that are not the model's own
     by_tokens = lambda H, W, r, **kw: umas.umas_cross_entropy_fwd_bwd(H, W, said, r, z_coef=1e-4, **kw)
     by_teacher = lambda H, W, r, **kw: umas.umas_distill_fwd_bwd(H, W, top_ids, top_logits, lse_t, r, **kw)
 
     def divergence():
-        H, Wb = projected(x, *params)
+        H, Wb, _ = solver(x, *params)
         stats, kl, _, _ = by_teacher(H, Wb, rows)
         ids, _, _ = umas.umas_top_logits(H, Wb, 1, rows)
         return float(umas.read_target_stats(stats)["loss"][0]), float((ids[rows.long(), 0] == said[rows.long()]).float().mean())
