@@ -854,7 +854,8 @@ struct Binning {
     return z - (fabsf(z) * 1e-6f + static_cast<float>(1e-5 / d.w.c));
   }
   __device__ __forceinline__ bool has(float z) const { return z < bound && z >= lo && z > -INFINITY; }
-  __device__ __forceinline__ int bin(float z) const { return static_cast<int>(fminf((bound - z) * scale, static_cast<float>(kCounts - 1))); }
+  __device__ __forceinline__ float place(float z) const { return fminf((bound - z) * scale, static_cast<float>(kCounts - 1)); }
+  __device__ __forceinline__ int bin(float z) const { return static_cast<int>(place(z)); }
   // The largest logit of the bins from b on: found by its bits, as what bin() rounds to is what counts.
   __device__ __forceinline__ float edge(int b) const {
     if (b >= kCounts) return -INFINITY;
@@ -882,9 +883,10 @@ struct Bracket {
     return a;
   }
 };
-// First pass, of the units [u0, u1).
+// First pass, of the units [u0, u1).  s_off: where in the bin, in 256ths, one of its tokens lies.  (Of bf16 logits a bin holds few values, at temperatures near 1 all in the same place
+// of theirs: with the bins' middles taken for it thresholds were half a bin off, and flat rows were gone through bit by bit, 64 of 152 064 under top_p 516 us in place of 99.)
 template <typename In, int T>
-__device__ __forceinline__ void count_bins(const RowSource<In, T>& row, const Binning& q, int u0, int u1, uint32_t* s_count) {
+__device__ __forceinline__ void count_bins(const RowSource<In, T>& row, const Binning& q, int u0, int u1, uint32_t* s_count, uint8_t* s_off) {
   for (int u = u0 + static_cast<int>(threadIdx.x >> 6); u < u1; u += T / kWave) {
     const float most = row.unit_max[u];
     if (!(most >= q.lo) || most == -INFINITY) continue;
@@ -892,12 +894,20 @@ __device__ __forceinline__ void count_bins(const RowSource<In, T>& row, const Bi
     load_unit(row.z, row.V, u, x);
 #pragma unroll
     for (int i = 0; i < kPerLane; ++i)
-      if (q.has(x[i])) atomicAdd(&s_count[q.bin(x[i])], 1u);
+      if (q.has(x[i])) {
+        const float at = q.place(x[i]);
+        const int b = static_cast<int>(at);
+        atomicAdd(&s_count[b], 1u);
+        s_off[b] = static_cast<uint8_t>((at - static_cast<float>(b)) * 256.f);   // whichever comes last
+      }
   }
 }
-// counts: this thread's bins, kCounts / T of them from threadIdx.x * kCounts / T on.
+// A bin of a part in 32 bits: fewer than 2^24 tokens, and their place.
+constexpr int kOffShift = 24;
+static_assert(kMaxSampleV < 1 << kOffShift, "a bin holds a vocabulary");
+// counts: this thread's bins, kCounts / T of them from threadIdx.x * kCounts / T on, and places: the sums of where their tokens lie.
 template <int T, class Shared>
-__device__ __forceinline__ Bracket bracket_of(const uint32_t (&counts)[kCounts / T], Shared& s, Block<T>& all, const Binning& q, u64 front, int n_front, const RowDraw& d) {
+__device__ __forceinline__ Bracket bracket_of(const uint32_t (&counts)[kCounts / T], const uint32_t (&places)[kCounts / T], Shared& s, Block<T>& all, const Binning& q, u64 front, int n_front, const RowDraw& d) {
   constexpr int kEach = kCounts / T;
   const double at_bound = d.w(q.bound), per_bin = -d.w.c / q.scale;   // the power of 2 that a bin takes from a weight
   u64 n_mine = 0, n_all;
@@ -905,7 +915,8 @@ __device__ __forceinline__ Bracket bracket_of(const uint32_t (&counts)[kCounts /
 #pragma unroll
   for (int i = 0; i < kEach; ++i) {
     const int b = static_cast<int>(threadIdx.x) * kEach + i;
-    of[i] = at_bound * exp2_near((b + 0.5) * per_bin);
+    const float place = (static_cast<float>(places[i]) * __builtin_amdgcn_rcpf(fmaxf(static_cast<float>(counts[i]), 1.f)) + 0.5f) * (1.f / 256);
+    of[i] = b < kCounts - 1 ? at_bound * exp2_near((b + static_cast<double>(place)) * per_bin) : 0.0;   // (what is further away, under a mask, weighs nothing, or the thresholds do not hold)
     n_mine += counts[i];
     m_mine += static_cast<double>(counts[i]) * of[i];
   }
@@ -935,10 +946,12 @@ __device__ __forceinline__ Bracket bracket_of(const uint32_t (&counts)[kCounts /
     }
     __syncthreads();
   }
-  const int k_bin = static_cast<int>(s.found_bin);
+  int k_bin = static_cast<int>(s.found_bin);
+  // the last bin holds all that is further away, a mask's lowest numbers among it: where that weighs nothing it does not matter which of it are among the first k
+  if (k_bin == kCounts - 1 && d.weight(q.edge(k_bin)) == 0) k_bin = kCounts;
   const double total = !d.by_min() && d.k == 0 ? d.all : s.found_drest;   // what top_p is of, nearly
   int b1 = 0, b2 = -1;
-  const double need = d.p * total - f_mass, off = (1e-3 + per_bin * per_bin / 16) * fabs(need) + 1e-6 * total;   // (logits of a bin are not all in its middle)
+  const double need = d.p * total - f_mass, off = (5e-4 + per_bin * per_bin / 16) * fabs(need) + 1e-6 * total;   // (logits of a bin are not all in one place)
   if (d.p < 1.0 && need + off > 0.0) {
     int from = kCounts - 1, to = kCounts - 1;                    // the thread's first bin that reaches the lower end, and the upper one
     double m = m_before + m_mine;
@@ -1306,14 +1319,21 @@ k_sample_row(Logits<In> L, RowCalls C, FlatWs F) {
           if (bins) {
             const Binning q(bound, d, L.V);
             uint32_t* const s_count = reinterpret_cast<uint32_t*>(s.bins);
+            uint8_t* const s_off = reinterpret_cast<uint8_t*>(s.list_w);
+            static_assert(kCounts * 4 <= sizeof(s.bins) && kCounts <= sizeof(s.list_w), "counts and places");
             for (int i = threadIdx.x; i < kCounts; i += T) s_count[i] = 0;
             __syncthreads();
-            count_bins(src, q, 0, L.units, s_count);
+            count_bins(src, q, 0, L.units, s_count, s_off);
             __syncthreads();
-            uint32_t counts[kCounts / T];
+            uint32_t counts[kCounts / T], places[kCounts / T];
 #pragma unroll
-            for (int i = 0; i < kCounts / T; ++i) counts[i] = s_count[threadIdx.x * (kCounts / T) + i];
-            const Bracket r = bracket_of<T>(counts, s, block, q, front, n, d);
+            for (int i = 0; i < kCounts / T; ++i) {
+              const int b = threadIdx.x * (kCounts / T) + i;
+              counts[i] = s_count[b];
+              places[i] = counts[i] ? counts[i] * s_off[b] : 0;
+            }
+            __syncthreads();
+            const Bracket r = bracket_of<T>(counts, places, s, block, q, front, n, d);
             if (threadIdx.x == 0) s.n_list = n;
             __syncthreads();
             u64 sure = 0, rest = 0;
@@ -1337,6 +1357,7 @@ template <typename In, int T>
 __global__ void __launch_bounds__(T)
 k_sample_count(Logits<In> L, RowCalls C, FlatWs F) {
   __shared__ uint32_t s_count[kCounts];
+  __shared__ uint8_t s_off[kCounts];
   if (static_cast<int>(blockIdx.y) >= *F.count) return;
   const int64_t m = F.order[blockIdx.y];
   RowState& state = F.state[m];
@@ -1347,10 +1368,10 @@ k_sample_count(Logits<In> L, RowCalls C, FlatWs F) {
   const Binning q(state.bound, d, L.V);
   for (int i = threadIdx.x; i < kCounts; i += T) s_count[i] = 0;
   __syncthreads();
-  count_bins(src, q, L.units * static_cast<int>(blockIdx.x) / F.parts, L.units * static_cast<int>(blockIdx.x + 1) / F.parts, s_count);
+  count_bins(src, q, L.units * static_cast<int>(blockIdx.x) / F.parts, L.units * static_cast<int>(blockIdx.x + 1) / F.parts, s_count, s_off);
   __syncthreads();
   uint32_t* const to = F.counts + (m * F.parts + blockIdx.x) * kCounts;
-  for (int i = threadIdx.x; i < kCounts; i += T) to[i] = s_count[i];
+  for (int i = threadIdx.x; i < kCounts; i += T) to[i] = s_count[i] ? s_count[i] | static_cast<uint32_t>(s_off[i]) << kOffShift : 0;
 }
 // ... what they say, ...
 template <int T>
@@ -1365,7 +1386,12 @@ k_sample_bracket(RowCalls C, FlatWs F, int V) {
   const int64_t row = C.rowsel ? C.rowsel[C.c0 + m] : C.c0 + m;
   const RowDraw d = row_draw(C, row, state.top, C.S.t(row), 0.0, state.all, V);
   const Binning q(state.bound, d, V);
-  uint32_t counts[kEach] = {};
+  uint32_t counts[kEach] = {}, places[kEach] = {};
+  auto take = [&](int i, uint32_t x) {
+    const uint32_t n = x & ((1u << kOffShift) - 1);
+    counts[i] += n;
+    places[i] += n * (x >> kOffShift);
+  };
   static_assert(kEach % 4 == 0, "sixteen bytes at a time");
   constexpr int kAtOnce = 4;                                 // parts under way
   for (int p = 0; p < F.parts; p += kAtOnce) {
@@ -1379,14 +1405,14 @@ k_sample_bracket(RowCalls C, FlatWs F, int V) {
     for (int b = 0; b < kAtOnce; ++b)
 #pragma unroll
       for (int i = 0; i < kEach / 4; ++i) {
-        counts[4 * i] += x[b][i].x;
-        counts[4 * i + 1] += x[b][i].y;
-        counts[4 * i + 2] += x[b][i].z;
-        counts[4 * i + 3] += x[b][i].w;
+        take(4 * i, x[b][i].x);
+        take(4 * i + 1, x[b][i].y);
+        take(4 * i + 2, x[b][i].z);
+        take(4 * i + 3, x[b][i].w);
       }
   }
   Block<T> block(s.block);
-  const Bracket r = bracket_of<T>(counts, s, block, q, state.front, state.n_front, d);
+  const Bracket r = bracket_of<T>(counts, places, s, block, q, state.front, state.n_front, d);
   if (threadIdx.x == 0) state.bracket = r;
 }
 // ... then the sums and lists, ...
