@@ -13,7 +13,7 @@
 // 64th largest of the threads' group maxima bounds, or all that min_p leaves; up to 512 of them decide by themselves if nothing behind them can count (13 us for a row of 152 064, 14 for 256).
 // Rows that are spread, whose border lies behind the front, go through four more launches over the chip: counts of the tokens by their distance to the front (k_sample_count), from these the
 // thresholds between which a border lies (k_sample_bracket), the sums above and lists between them (k_sample_sums), and the border and token from those (k_sample_flat): 11, 9,
-// 32 and 21 us for what is spread among 256 rows.  Up to four rows do all of it in the second launch.  Where lists overflow, with floods of equal logits, thresholds are found bit by bit, eleven
+// 32 and 21 us for what is spread among 256 rows.  A single row does all of it in the second launch.  Where lists overflow, with floods of equal logits, thresholds are found bit by bit, eleven
 // at a time from the top, with a histogram of counts or masses (draw_by_passes): right for every row, and slow.
 #include <float.h>
 
@@ -1557,7 +1557,9 @@ k_sample_few(const uint16_t* __restrict__ W, const uint16_t* __restrict__ H, int
 
 // ------------------------------------------------------------------ host side
 constexpr int64_t kSampleRows = 1024;                        // rows of a chunk
-constexpr int64_t kRowsInOne = 4;
+// A single row: its workgroup does all of it, 19 us in place of 24 of 152 064 logits where the front decides, 155 in place of 56 where it does not, which has to be so for one draw in
+// twenty to weigh as much.  Of four rows any may be spread: 156 and 58 us.
+constexpr int64_t kRowsInOne = 1;
 struct SampleWs {
   Summary A;
   FlatWs flat;

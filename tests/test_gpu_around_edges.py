@@ -72,7 +72,7 @@ FAR = [dict(top_p=0.9), dict(top_p=0.5, temperature=0.7), dict(top_p=0.99, tempe
 @pytest.mark.parametrize("kind", ["flat", "wide", "peaked", "ties", "equal", "rising", "falling", "two"])
 @pytest.mark.parametrize("V", [33001, 151936])
 def test_filters_that_end_far_behind_the_front(V, kind, dtype):
-    """Few rows (one launch does all of a row) and many (spread over the chip) give the same."""
+    """One row (whose workgroup does all of it), two and many (spread over the chip) give the same."""
     gen = torch.Generator("cuda").manual_seed(V + len(kind))
     n = 10
     z, u = logits_of(kind, n, V, dtype, gen), torch.rand(n, device="cuda", generator=gen)
@@ -80,8 +80,9 @@ def test_filters_that_end_far_behind_the_front(V, kind, dtype):
     for s in FAR + [dict()]:
         got = umas.umas_sample_logits(z, u, **s)
         check(z, u, got, **s)
-        few = [umas.umas_sample_logits(z[a:a + 2], u[a:a + 2], **s) for a in range(0, n, 2)]
-        assert same(got, [torch.cat(x) for x in zip(*few)]), s
+        for rows in (1, 2):
+            few = [umas.umas_sample_logits(z[a:a + rows], u[a:a + rows], **s) for a in range(0, n, rows)]
+            assert same(got, [torch.cat(x) for x in zip(*few)]), s
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
