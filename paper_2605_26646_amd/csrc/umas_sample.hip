@@ -12,8 +12,8 @@
 // The second, k_sample_row, gives a workgroup to a row.  Without filters the unit and then the token are found from the units' masses.  Else the front is listed: the tokens that the
 // 64th largest of the threads' group maxima bounds, or all that min_p leaves; up to 512 of them decide by themselves if nothing behind them can count (13 us for a row of 152 064, 14 for 256).
 // Rows that are spread, whose border lies behind the front, go through four more launches over the chip: counts of the tokens by their distance to the front (k_sample_count), from these the
-// thresholds between which a border lies (k_sample_bracket), the sums above and lists between them (k_sample_sums), and the border and token from those (k_sample_flat): 11, 9,
-// 32 and 21 us for what is spread among 256 rows.  A single row does all of it in the second launch.  Where lists overflow, with floods of equal logits, thresholds are found bit by bit, eleven
+// thresholds between which a border lies (k_sample_bracket), the sums above and lists between them (k_sample_sums), and the border and token from those (k_sample_flat): 13, 10,
+// 33 and 22 us for what is spread among 256 rows.  A single row does all of it in the second launch.  Where lists overflow, with floods of equal logits, thresholds are found bit by bit, eleven
 // at a time from the top, with a histogram of counts or masses (draw_by_passes): right for every row, and slow.
 #include <float.h>
 
