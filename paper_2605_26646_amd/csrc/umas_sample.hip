@@ -36,19 +36,25 @@ constexpr int kMaxSampleV = UMAS_MAX_SAMPLE_V;
 // exp((z - top) c), c = log2 e / T, for z <= top, as 2^n times a polynomial in the rest f, |f| <= 1/2: the interpolation of (2^f - 1) / f at eight Chebyshev nodes, times f, plus
 // 1; off by 2.2e-12 of itself.  Whole and rest come from an addition that pushes the rest out of a float64, the power from an addition to the exponent's bits: the conversions and
 // ldexp that the compiler would take for them cost four times a multiply-add each (39 million logits, with eleven coefficients, rint and ldexp 58 us).
-// The largest logit's own weight is exactly 1, equal logits' weights are equal; below 2^-1000 is 2^-1000: logits are held up to the one whose weight that is, in float32, which
-// costs a third of a float64 maximum.  (Where that one is not below the largest itself the temperature is so low that c may as well be what takes the next number
-// below the largest to 2^-1000.)
+// The largest logit's own weight is exactly 1, equal logits' weights are equal; below 2^-1000 is 2^-1000, nearly: logits are held up to the first float32 number whose weight is no
+// more than that, in float32, which costs a third of a float64 maximum.  (Where that one is not below the largest itself the temperature is so low that c may as well be what takes
+// the next number below the largest to 2^-1000.)  At low temperatures numbers that lie next to each other are hundreds of powers of two apart and that number's own power may be 2^-2000:
+// the power is held up as well, a whole number's maximum, or it would run over into the sign.
 // The maximum of two numbers in one instruction (fmaxf makes both quiet first).
 __device__ __forceinline__ float larger(float a, float b) { return __builtin_elementwise_maximum(a, b); }
+__device__ __forceinline__ float next_below(float x) {        // of a finite one
+  const uint32_t u = __float_as_uint(x);
+  return x == 0.f ? __uint_as_float(0x80000001u) : __uint_as_float(x > 0.f ? u - 1 : u + 1);
+}
 struct Weigh {
+  static constexpr int kLeastPower = -1000;
   double top, c;
   float least;
   __device__ __forceinline__ Weigh(float largest, double c_) : top(largest) {
-    const uint32_t u = __float_as_uint(largest);             // the next number below it
-    const float below = largest == 0.f ? __uint_as_float(0x80000001u) : __uint_as_float(largest > 0.f ? u - 1 : u + 1);
+    const float below = next_below(largest);
     c = fmax(fmin(c_, static_cast<double>(1000.f * __builtin_amdgcn_rcpf(largest - below))), 1e-30);   // (a temperature without end: all are 1 but those of -infinity)
     least = fminf(fmaxf(largest - 1000.f * __builtin_amdgcn_rcpf(static_cast<float>(fmin(c, 1e38))), -3e38f), below);
+    if ((static_cast<double>(least) - top) * c > kLeastPower) least = next_below(least);   // rounded towards the largest
   }
   __device__ __forceinline__ float next_above() const {      // the largest logit's next number
     const float x = static_cast<float>(top);
@@ -68,7 +74,8 @@ struct Weigh {
     p = fma(p, f, 0.24022650695888503);
     p = fma(p, f, 0.6931471805568324);
     p = fma(p, f, 1.0);
-    return __hiloint2double(__double2hiint(p) + (__double2loint(pushed) << 20), __double2loint(p));
+    const int power = max(__double2loint(pushed), kLeastPower);
+    return __hiloint2double(__double2hiint(p) + static_cast<int>(static_cast<uint32_t>(power) << 20), __double2loint(p));
   }
 };
 constexpr double kNoWeight = 1e-290;                          // what is no more than this is not drawn, u = 0 or not

@@ -1,0 +1,76 @@
+"""The draws, the norm and the clipping at the ends of what their numbers hold: temperatures close to 0, logits of many binades, borders on which sums that are
+taken in another order fall to the other side, infinite gains, factors below float32's normal numbers.
+
+Tolerances, from the arithmetic; f = 2^-24.
+  draws     as in check_draws: tokens are equal, logp and logq are off by what their sums are"""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+import paper_2605_26646_amd as umas
+from tests.test_gpu_around import DT, check_draws, device
+
+pytestmark = pytest.mark.gpu
+F = 2.0 ** -24
+
+
+# ------------------------------------------------------------------------------------------------ draws
+def close_logits(tops, V, dtype, rng):
+    """A row for each largest logit: it stands at up to three places, some of the numbers next below it at others, the rest is far below, masked by -infinity or by the
+    lowest number.  Every unit of 1024 tokens but the last starts with masked ones, and one holds nothing else."""
+    step = 1 if dtype == "f32" else 1 << 16                          # of float32's bits from one number to the next
+    z = np.empty((len(tops), V), np.float32)
+    for i, top in enumerate(np.float32(tops)):
+        z[i] = -np.inf if i % 2 else torch.finfo(DT[dtype]).min
+        some = rng.permutation(np.arange(V // 3, V))
+        z[i, some[:V // 4]] = top - np.abs(top) * (1 + rng.random(V // 4)) - 1
+        bits = np.full(V // 8, top, np.float32).view(np.int32)
+        below = rng.integers(1, 12, V // 8) * step
+        z[i, some[V // 4:V // 4 + V // 8]] = (bits + np.where(top > 0, -below, below)).astype(np.int32).view(np.float32)
+        z[i, some[-1 - i % 3:]] = top
+    return z
+
+
+def without_dust(z, t):
+    """Weights below 1e-290 count as none, which a float64 oracle holds on to down to 1e-323: tokens around there become -infinity."""
+    with np.errstate(over="ignore"):
+        gap = (z - z.max(1, keepdims=True)) / np.asarray(t, np.float64).reshape(-1, 1)
+    return np.where((gap < -600) & (gap > -780), -np.inf, z)
+
+
+TOPS = [s * 1.37 * 2.0 ** e for e in range(-3, 17) for s in (1, -1)] + [1.0, -2.0, 20.0, 2.0 ** 31 * 1.1, 2.0 ** 31 * 1.9, -(2.0 ** 32) * 0.7, 2.0 ** 40]
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("V", [7, 1100, 2100])
+def test_temperatures_close_to_0_beside_largest_logits_of_many_binades(V, dtype):
+    rng = np.random.default_rng([21, V])
+    n = len(TOPS)
+    _, rows = device(close_logits(TOPS, V, dtype, rng), dtype)
+    for t in [1.0] + [10.0 ** -e for e in range(3, 13)]:
+        t = float(np.float32(t * (1 + 0.5 * rng.random())))
+        z, zh = device(without_dust(rows, t), dtype)
+        for u in (np.zeros(n, np.float32), rng.random(n).astype(np.float32), np.full(n, 1 - F, np.float32)):
+            check_draws(zh, u, dict(temperature=t), umas.umas_sample_logits(z, torch.from_numpy(u).cuda(), temperature=t), V)
+        u = 0.01 + 0.98 * rng.random(n).astype(np.float32)
+        for s in (dict(top_p=0.7), dict(top_k=2), dict(min_p=0.5), dict(temperature=torch.full((n,), t, device="cuda"))):
+            plain = {k: v for k, v in s.items() if k != "temperature"}
+            check_draws(zh, u, dict(temperature=t, **plain), umas.umas_sample_logits(z, torch.from_numpy(u).cuda(), **{"temperature": t, **s}), V)
+
+
+def test_a_cold_draw_of_a_wide_vocabulary_is_the_largest_logit():
+    n, V = 40, 151936
+    gen = torch.Generator("cuda").manual_seed(3)
+    z, u = torch.randn(n, V, device="cuda", generator=gen) * 5, torch.rand(n, device="cuda", generator=gen)
+    best = z.max(1)
+    logp = torch.log_softmax(z.double(), 1).gather(1, best.indices[:, None])[:, 0]
+    for t in (1e-6, 1e-7, 1e-8, 1e-9, 1e-10):
+        for s in (dict(), dict(top_p=0.9)):
+            ids, got, logq = umas.umas_sample_logits(z, u, temperature=t, **s)
+            # the second largest logit is 1e-4 below and more, but for a chance of 1e-3 a row; that one is a draw between two
+            sure = z.topk(2, 1).values.diff(dim=1).abs()[:, 0] > 800 * t
+            assert sure.sum() > n // 2 and torch.equal(ids[sure], best.indices[sure].int()) and not logq[sure].any()
+            assert ((got.double() - logp)[sure].abs() <= 40 * 2.0 ** -22 + F * logp[sure].abs()).all()   # |x| + 2 <= 40 where p counts
+            assert (ids >= 0).all() and got.isfinite().all()
