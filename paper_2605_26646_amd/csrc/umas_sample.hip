@@ -656,10 +656,11 @@ __device__ __forceinline__ bool list_front(const RowSource<In, T>& row, const fl
   __syncthreads();
   return s.n_list <= Shared::kList;
 }
-// What the listed tokens say, where they are enough: id -1 where they are not.  Up to 128 tokens: each is compared with all of them, once by its logit and once by its number, by
+// What the listed tokens say, where they are enough: id -1 where they are not.  `complete`: no other token has a weight, so that a top_k beyond them keeps them all (24 rows of 152 064
+// under top_k 50 and min_p 0.05, of which few tokens are left, 15 us; gone through as if others might count 57).  Up to 128 tokens: each is compared with all of them, once by its logit and once by its number, by
 // the threads that it has: of 1024 sixteen for up to 64 tokens, eight for up to 128.
 template <int T, class Shared>
-__device__ __forceinline__ Drawn draw_from_front(Shared& s, Block<T>& all, int n, float bound, bool all_listed, const RowDraw& d) {
+__device__ __forceinline__ Drawn draw_from_front(Shared& s, Block<T>& all, int n, bool complete, const RowDraw& d) {
   u64* const s_key = s.bins;                                 // [kCompared] each
   u64* const s_w = s.bins + kCompared;
   u64* const s_sorted = s.bins + 2 * kCompared;
@@ -693,7 +694,7 @@ __device__ __forceinline__ Drawn draw_from_front(Shared& s, Block<T>& all, int n
   __syncthreads();
   u64 mass;
   const u64 here = one ? s_sorted[i] : 0, ahead = all.scan(here, &mass);   // of the i-th in falling order
-  const bool whole = d.k > 0 || (d.by_min() && d.weight(bound) == 0) || all_listed;   // nothing that is not listed counts
+  const bool whole = d.k > 0 || complete;                    // nothing that is not listed counts
   u64 need = mass;
   if (d.p < 1.0) {
     if (whole) need = d.share(d.p, mass);
@@ -702,7 +703,7 @@ __device__ __forceinline__ Drawn draw_from_front(Shared& s, Block<T>& all, int n
       need = part_of < 1.0 ? 1 : static_cast<u64>(part_of);
     }
   }
-  if ((d.k > n && !all_listed) || (!whole && (d.by_min() || d.p == 1.0 || need > mass))) return Drawn{-1, 0};
+  if ((d.k > n && !complete) || (!whole && (d.by_min() || d.p == 1.0 || need > mass))) return Drawn{-1, 0};
   if (one) {                                                 // kept: whose front is shorter than what is needed
     if (ahead >= need) s_sorted[i] = 0;
     else if (here && ahead + here >= need) s.found_above = ahead + here;
@@ -729,7 +730,7 @@ __device__ __forceinline__ Drawn draw_from_front(Shared& s, Block<T>& all, int n
 // ... and up to 512: a border, or the token, is found among the sums of 512 runs of logits, or of tokens, and then among those of its run.  (Comparing all with all, a 400 rows' launch
 // with fronts of up to 512 took 48 us, the last step by runs 39; all by runs takes 4 us less of the call's 424.)
 template <int T, class Shared>
-__device__ __forceinline__ Drawn draw_from_long_front(Shared& s, Block<T>& all, int n, float bound, bool all_listed, const RowDraw& d) {
+__device__ __forceinline__ Drawn draw_from_long_front(Shared& s, Block<T>& all, int n, float bound, bool complete, const RowDraw& d) {
   u64* const s_key = s.bins;                                 // [kRanked] each
   u64* const s_w = s.bins + kRanked;
   u64* const s_mass = s.bins + 2 * kRanked;
@@ -781,7 +782,7 @@ __device__ __forceinline__ Drawn draw_from_long_front(Shared& s, Block<T>& all, 
     in_run = i < border ? in_run : i == border ? s.found_here : 0;
     mass = s.found_above + s.found_here;
   }
-  const bool whole = d.k > 0 || (d.by_min() && d.weight(bound) == 0) || all_listed;   // nothing that is not listed counts
+  const bool whole = d.k > 0 || complete;                    // nothing that is not listed counts
   u64 need = mass;
   if (d.p < 1.0) {
     if (whole) need = d.share(d.p, mass);
@@ -790,7 +791,7 @@ __device__ __forceinline__ Drawn draw_from_long_front(Shared& s, Block<T>& all, 
       need = part_of < 1.0 ? 1 : static_cast<u64>(part_of);
     }
   }
-  if ((d.k > n && !all_listed) || (!whole && (d.by_min() || d.p == 1.0 || need > mass))) return Drawn{-1, 0};
+  if ((d.k > n && !complete) || (!whole && (d.by_min() || d.p == 1.0 || need > mass))) return Drawn{-1, 0};
   if (need < mass) {
     if (before < need && need <= before + in_run) {
       s.found_bin = i;
@@ -1299,8 +1300,9 @@ k_sample_row(Logits<In> L, RowCalls C, FlatWs F) {
         }
         n = s.n_list;
         __syncthreads();
-        if (listed && n <= kCompared) got = draw_from_front(s, block, n, bound, bound == -INFINITY, d);
-        else if (listed && n <= kRanked) got = draw_from_long_front(s, block, n, bound, bound == -INFINITY, d);
+        const bool complete = bound == -INFINITY || (d.by_min() && d.weight(bound) == 0);
+        if (listed && n <= kCompared) got = draw_from_front(s, block, n, complete, d);
+        else if (listed && n <= kRanked) got = draw_from_long_front(s, block, n, bound, complete, d);
         if (!listed || n > kRanked) {                        // many that are alike: no front, bins from the largest on
           n = 0;
           bound = INFINITY;

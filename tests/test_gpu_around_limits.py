@@ -11,6 +11,7 @@ import torch
 
 import paper_2605_26646_amd as umas
 from tests.test_gpu_around import DT, check_draws, device
+from tests.test_gpu_around_edges import check, same
 
 pytestmark = pytest.mark.gpu
 F = 2.0 ** -24
@@ -74,3 +75,28 @@ def test_a_cold_draw_of_a_wide_vocabulary_is_the_largest_logit():
             assert sure.sum() > n // 2 and torch.equal(ids[sure], best.indices[sure].int()) and not logq[sure].any()
             assert ((got.double() - logp)[sure].abs() <= 40 * 2.0 ** -22 + F * logp[sure].abs()).all()   # |x| + 2 <= 40 where p counts
             assert (ids >= 0).all() and got.isfinite().all()
+
+
+@pytest.mark.parametrize("scale,min_p,most", [(4.0, 0.05, 60), (1.0, 0.2, 500)])
+def test_rows_of_which_min_p_leaves_fewer_tokens_than_top_k(scale, min_p, most):
+    """They are decided by the list of what is left: no launch for spread rows gets one.  Its lists, 4096 places a row, are the last that lies in the workspace."""
+    n, V = 60, 50000
+    gen = torch.Generator("cuda").manual_seed(7)
+    z, u = torch.randn(n, V, device="cuda", generator=gen) * scale, torch.rand(n, device="cuda", generator=gen)
+    left = (z >= z.max(1, keepdim=True).values + math.log(min_p)).sum(1)
+    z, u = z[left <= most], u[left <= most]
+    n = len(z)
+    assert n >= 20
+    lib = umas.load_library()
+    ws = torch.full((lib.umas_sample_logits_workspace_bytes(n, V),), 0x5A, dtype=torch.uint8, device="cuda")
+    k = most + 1
+    for s in (dict(top_k=k), dict(top_k=k, top_p=0.8), dict(top_k=20000), dict(top_k=20000, top_p=0.8)):
+        got = umas.umas_sample_logits(z, u, min_p=min_p, workspace=ws, **s)
+        check(z, u, got, min_p=min_p, **s)
+        assert (ws[-n * 4096 * 4:] == 0x5A).all(), s
+        one = [umas.umas_sample_logits(z[i:i + 1], u[i:i + 1], min_p=min_p, **s) for i in range(n)]
+        assert same(got, [torch.cat(x) for x in zip(*one)]), s
+        k_of = torch.full((n,), s["top_k"], device="cuda", dtype=torch.int32)
+        assert same(got, umas.umas_sample_logits(z, u, **{**s, "top_k": k_of}, min_p=min_p, workspace=ws)) and (ws[-n * 4096 * 4:] == 0x5A).all(), s
+    if most <= 64:                                                   # a top_k that is held to be decided by the front, by one workgroup a row
+        check(z, u, umas.umas_sample_logits(z, u, min_p=min_p, top_k=64), min_p=min_p, top_k=64)
