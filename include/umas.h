@@ -553,7 +553,8 @@ umas_status umas_rms_norm_bwd(const void* dy, const void* hidden, const void* ga
  *   (sum of w) reaches top_p of the mass of them all (1: all).  The token is the first, in rising order, at which the running mass of
  *   what is kept passes u times the kept mass.
  * Logits of -infinity and those that are no number are never drawn and have no mass.  Masses are float64, or where a filter is on whole numbers of 2^-s,
- * s = min(51, 62 - log2 V rounded up) (2^-44 at 151 936 tokens): a w below half of that counts as 0 there.  A w itself is off by 2.2e-12 of its value at most,
+ * s = min(51, 62 - log2 V rounded up) (2^-44 at 151 936 tokens): a w below half of that counts as 0 there, but for the mass of all tokens that top_p is of where neither top_k nor min_p
+ * is on, which is float64.  A w itself is off by 2.2e-12 of its value at most,
  * and one below 1e-290 counts as 0; temperatures above 1.4e30 count as that.
  * The same inputs give the same token, whatever the other rows and the workspace are.
  *   logits       DEVICE [n_rows, V] of the type dtype, row i at logits + i * row_stride, row_stride >= V, aligned to its type

@@ -376,6 +376,14 @@ struct RowDraw {
     const u64 n = static_cast<u64>(ceil(part * static_cast<double>(of)));
     return n < 1 ? 1 : n > of ? of : n;
   }
+  // What the kept run has to reach, of whole numbers that add up to `mass`: top_p's part of them, or without top_k and min_p of all tokens' float64 mass.  (That is known before any
+  // whole number; it holds what rounds to none of them as well, so that the whole numbers may fall short of it.)  Every way to a row's token takes it from here.
+  __device__ __forceinline__ u64 needed(u64 mass) const {
+    if (!(p < 1.0)) return mass;
+    if (k > 0 || by_min()) return share(p, mass);
+    const double part = ceil(p * all * one);
+    return part < 1.0 ? 1 : static_cast<u64>(part);
+  }
   __device__ __forceinline__ u64 target(u64 mass) const {
     const u64 t = static_cast<u64>(u * static_cast<double>(mass));
     return t < mass ? t : mass - 1;
@@ -571,7 +579,7 @@ __device__ __noinline__ Drawn draw_by_passes(RowSource<In, T> row, RowShared<T>*
   mass = 0;
   row.each(none, d, [&](float z, int id, auto w) { mass += of_first(z, id, w); });
   mass = all.sum(mass);
-  if (d.p < 1.0) run = cut_at(row, s, all, none, d, of_first, d.share(d.p, mass), &mass);
+  if (d.p < 1.0) run = cut_at(row, s, all, none, d, of_first, min(d.needed(mass), mass), &mass);
   auto kept = [&](float z, int id, auto w) { return run.in(z, id) ? of_first(z, id, w) : u64{0}; };
   u64 sum = 0;
   row.each(none, d, [&](float z, int id, auto w) { sum += kept(z, id, w); }, [&](int u) {
@@ -695,14 +703,8 @@ __device__ __forceinline__ Drawn draw_from_front(Shared& s, Block<T>& all, int n
   u64 mass;
   const u64 here = one ? s_sorted[i] : 0, ahead = all.scan(here, &mass);   // of the i-th in falling order
   const bool whole = d.k > 0 || complete;                    // nothing that is not listed counts
-  u64 need = mass;
-  if (d.p < 1.0) {
-    if (whole) need = d.share(d.p, mass);
-    else {
-      const double part_of = ceil(d.p * d.all * d.one);
-      need = part_of < 1.0 ? 1 : static_cast<u64>(part_of);
-    }
-  }
+  u64 need = d.needed(mass);
+  if (whole) need = min(need, mass);
   if ((d.k > n && !complete) || (!whole && (d.by_min() || d.p == 1.0 || need > mass))) return Drawn{-1, 0};
   if (one) {                                                 // kept: whose front is shorter than what is needed
     if (ahead >= need) s_sorted[i] = 0;
@@ -783,14 +785,8 @@ __device__ __forceinline__ Drawn draw_from_long_front(Shared& s, Block<T>& all, 
     mass = s.found_above + s.found_here;
   }
   const bool whole = d.k > 0 || complete;                    // nothing that is not listed counts
-  u64 need = mass;
-  if (d.p < 1.0) {
-    if (whole) need = d.share(d.p, mass);
-    else {
-      const double part_of = ceil(d.p * d.all * d.one);
-      need = part_of < 1.0 ? 1 : static_cast<u64>(part_of);
-    }
-  }
+  u64 need = d.needed(mass);
+  if (whole) need = min(need, mass);
   if ((d.k > n && !complete) || (!whole && (d.by_min() || d.p == 1.0 || need > mass))) return Drawn{-1, 0};
   if (need < mass) {
     if (before < need && need <= before + in_run) {
@@ -906,7 +902,7 @@ __device__ __forceinline__ void count_bins(const RowSource<In, T>& row, const Bi
         const float at = q.place(x[i]);
         const int b = static_cast<int>(at);
         atomicAdd(&s_count[b], 1u);
-        s_off[b] = static_cast<uint8_t>((at - static_cast<float>(b)) * 256.f);   // whichever comes last
+        s_off[b] = static_cast<uint8_t>((at - static_cast<float>(b)) * 256.f);   // whichever comes last: thresholds may differ by it, the border that is found between them does not
       }
   }
 }
@@ -1068,11 +1064,7 @@ __device__ __forceinline__ Drawn draw_listed(const RowSource<In, T>& row, RowSha
   all.sum(have, other);
   mass = in_front + sure + in_behind + rest;
   if (d.p < 1.0) {
-    u64 need = d.share(d.p, mass);
-    if (d.k == 0 && !d.by_min()) {                           // of all tokens
-      const double part = ceil(d.p * d.all * d.one);
-      need = part < 1.0 ? 1 : static_cast<u64>(part);
-    }
+    const u64 need = d.needed(mass);
     if (need <= in_front) {
       run = cut_at(front_list, s, all, none, d, [](float, int, auto w) { return w(); }, need, &mass);
       for (int u = threadIdx.x; u < row.units; u += T) s_unit[u] = 0;

@@ -100,3 +100,22 @@ def test_rows_of_which_min_p_leaves_fewer_tokens_than_top_k(scale, min_p, most):
         assert same(got, umas.umas_sample_logits(z, u, **{**s, "top_k": k_of}, min_p=min_p, workspace=ws)) and (ws[-n * 4096 * 4:] == 0x5A).all(), s
     if most <= 64:                                                   # a top_k that is held to be decided by the front, by one workgroup a row
         check(z, u, umas.umas_sample_logits(z, u, min_p=min_p, top_k=64), min_p=min_p, top_k=64)
+
+
+@pytest.mark.parametrize("n", [1, 2, 5])
+def test_a_border_of_top_p_among_equal_logits_beside_weights_that_are_no_whole_number(n):
+    """One token of weight 1, 3000 equal ones of 64 units (2^-46 of it each), and 30 000 of 0.45 units, which count in the mass that top_p is of and else as nothing.  u = 1 draws the last token
+    that is kept: the border's.  A row alone lists the equal ones; among others a workgroup finds more of them than it has room for, and they are gone through by bits."""
+    V, at, many = 33001, 4096, 3000
+    z = torch.full((V,), -math.log(2) * (46 - math.log2(0.45)))
+    z[at:at + many] = -40 * math.log(2)
+    z[0] = 0
+    w = torch.exp(z.double())
+    assert abs(w[at] * 2.0 ** 46 - 64) < 1e-3 and 0.44 < w[1] * 2.0 ** 46 < 0.46
+    z, u = z.cuda().expand(n, V).contiguous(), torch.ones(n, device="cuda")
+    all_of = float(w.sum())
+    for reach, last in ((1 + 1500.5 * float(w[at]), at + 1500), (1 + 0.5 * float(w[at]), at), (1 + 2999.5 * float(w[at]), at + 2999),
+                        (all_of - 5000 * 2.0 ** -46, at + many - 1)):        # ... beyond all whole numbers: what has one is kept
+        ids, _, logq = umas.umas_sample_logits(z, u, top_p=reach / all_of)
+        assert ids.tolist() == [last] * n, (reach, ids.tolist())
+        assert (logq + 40 * math.log(2)).abs().max() <= 1e-5                 # 2 f of 28, and the mass, which is 1 to 3e-9
