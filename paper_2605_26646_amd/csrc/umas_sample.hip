@@ -87,6 +87,11 @@ __device__ __forceinline__ double log_of(double x) {
 }
 // 2^t, nearly: for estimates.
 __device__ __forceinline__ double exp2_near(double t) { return static_cast<double>(__builtin_amdgcn_exp2f(static_cast<float>(t))); }
+// Rounded by itself, where what it is added to may differ from one kernel to the next.
+__device__ __forceinline__ double product(double a, double b) {
+#pragma clang fp contract(off)
+  return a * b;
+}
 // A temperature whose inverse leaves no finite number: 0 times it has to stay 0.
 __device__ __forceinline__ double scale_of(double t) { return fmin(kLog2e64 / t, 1e300); }
 __device__ __forceinline__ uint32_t order_of(float z) {       // whole numbers in the order of the logits, one zero
@@ -281,7 +286,8 @@ constexpr int kBins = 2048, kCounts = 4096;                  // of eleven bits o
 constexpr int kTopRank = 64;
 constexpr int kListCap = 4096, kRanked = 512, kCompared = 128;   // tokens of a list, of one that decides by itself, and of one that is ordered by comparing all with all
 constexpr int kGroupCap = 1024;
-// Sums and scans over a workgroup of T threads: what the wavefronts have goes through one of two buffers in turn, so that one barrier is enough.
+// Sums and scans over a workgroup of T threads: what the wavefronts have goes through one of two buffers in turn, so that one barrier is enough.  Float64 numbers that are taken T at a time, in
+// their order, each time onto what there is so far, are added up in the same order whatever T is: one after the other the sums of 64.
 template <int T>
 struct Block {
   static constexpr int W = T / kWave;
@@ -289,14 +295,14 @@ struct Block {
   int turn = 0;
   __device__ __forceinline__ explicit Block(u64 (*b)[2][W]) : buf(b) {}
   template <class V>
-  __device__ __forceinline__ V scan(V v, V* total) {         // exclusive
+  __device__ __forceinline__ V scan(V v, V* total, V from = V()) {   // exclusive, from a number on, which *total has in it
     const int wave = threadIdx.x >> 6;
     const V incl = lanes_scan(v);
     u64(&to)[W] = buf[turn][0];
     turn ^= 1;
     if ((threadIdx.x & 63) == 63) to[wave] = bits_in(incl);
     __syncthreads();
-    V before = V(), all = V();
+    V before = from, all = from;
 #pragma unroll
     for (int w = 0; w < W; ++w) {
       const V x = umas::bits_of(to[w], V());
@@ -307,22 +313,27 @@ struct Block {
     return before + (incl - v);
   }
   template <class V>
-  __device__ __forceinline__ void sum(V& a, V& b) {
-    a = lanes_sum(a);
-    b = lanes_sum(b);
+  __device__ __forceinline__ void add(V& a, V& b, V x, V y) {   // all threads' x and y onto a and b
+    x = lanes_sum(x);
+    y = lanes_sum(y);
     u64(&to)[2][W] = buf[turn];
     turn ^= 1;
     if ((threadIdx.x & 63) == 0) {
-      to[0][threadIdx.x >> 6] = bits_in(a);
-      to[1][threadIdx.x >> 6] = bits_in(b);
+      to[0][threadIdx.x >> 6] = bits_in(x);
+      to[1][threadIdx.x >> 6] = bits_in(y);
     }
     __syncthreads();
-    a = b = V();
 #pragma unroll
     for (int w = 0; w < W; ++w) {
       a += umas::bits_of(to[0][w], V());
       b += umas::bits_of(to[1][w], V());
     }
+  }
+  template <class V>
+  __device__ __forceinline__ void sum(V& a, V& b) {
+    const V x = a, y = b;
+    a = b = V();
+    add(a, b, x, y);
   }
   template <class V>
   __device__ __forceinline__ V sum(V a) {
@@ -1089,24 +1100,24 @@ __device__ __forceinline__ void first_of(int* to, int mine) {
   const u64 have = __ballot(mine >= 0);
   if (have && (threadIdx.x & 63) == static_cast<unsigned>(__ffsll(static_cast<long long>(have)) - 1)) atomicMin(reinterpret_cast<unsigned*>(to), static_cast<unsigned>(mine));
 }
-// No filter: the unit from the units' masses, then the token.
+// No filter: the unit from the units' masses, then the token.  A row alone, or one whose settings lie in arrays, has another T than others: the sums' order does not depend on it.
 template <typename In, int T, class Shared>
 __device__ __forceinline__ Drawn draw_unfiltered(const RowSource<In, T>& row, Shared& s, Block<T>& block, const float* ref_of, const double* mass_of, const Weigh& w, double u, double all) {
-  const double target = u * all;
-  auto mass = [&](int i) { return mass_of[i] * w(row.extreme(ref_of[i])); };
+  const double target = product(u, all);
+  auto mass = [&](int i) { return product(mass_of[i], w(row.extreme(ref_of[i]))); };
   if (threadIdx.x == 0) s.found_id = -1;
   int unit = -1;
   double before = 0.0;
   for (int u0 = 0; u0 < row.units && unit < 0; u0 += T) {
     const int i = u0 + threadIdx.x;
     const double mine = i < row.units ? mass(i) : 0.0;
-    double sum;
-    const double excl = before + block.scan(mine, &sum);
+    double upto;
+    const double excl = block.scan(mine, &upto, before);
     first_of(&s.found_id, mine > kNoWeight && excl + mine > target ? i : -1);
     __syncthreads();
     unit = s.found_id;
     if (i == unit) s.found_drest = target - excl;
-    before += sum;
+    before = upto;
     __syncthreads();
   }
   double rest = INFINITY;                                    // u = 1: the last token that has a weight
@@ -1117,13 +1128,15 @@ __device__ __forceinline__ Drawn draw_unfiltered(const RowSource<In, T>& row, Sh
   }
   __syncthreads();
   if (threadIdx.x == 0) s.found_id = -1;
-  constexpr int kEach = kUnit / T;
+  constexpr int kEach = 4;                                   // by as many threads as that takes
+  static_assert(T >= kUnit / kEach, "a unit's tokens have their threads");
+  const bool has = threadIdx.x < kUnit / kEach;
   const int v = unit * kUnit + static_cast<int>(threadIdx.x) * kEach;
   double mine[kEach], sum = 0.0, total;
   int last = -1;
 #pragma unroll
   for (int i = 0; i < kEach; ++i) {
-    const float x = row.at(v + i);
+    const float x = has ? row.at(v + i) : -INFINITY;
     mine[i] = x > -INFINITY ? w(x) : 0.0;
     if (!(mine[i] > kNoWeight)) mine[i] = 0.0;
     else last = v + i;
@@ -1256,12 +1269,16 @@ k_sample_row(Logits<In> L, RowCalls C, FlatWs F) {
   const float ref = src.extreme(top);
   const Weigh w(ref, scale_of(t)), w1(ref, kLog2e64);
   double sum = 0.0, all = 0.0;                               // of exp(z - top), for the log-prob of the softmax itself, and of the weights
-  for (int i = threadIdx.x; i < L.units; i += T) {
-    const float x = src.extreme(ref_of[i]);
-    sum += sum_of[i] * w1(x);
-    all += mass_of[i] * w(x);
+  for (int u0 = 0; u0 < L.units; u0 += T) {
+    const int i = u0 + threadIdx.x;
+    double mine = 0.0, mass = 0.0;
+    if (i < L.units) {
+      const float x = src.extreme(ref_of[i]);
+      mine = product(sum_of[i], w1(x));
+      mass = product(mass_of[i], w(x));
+    }
+    block.add(sum, all, mine, mass);
   }
-  block.sum(sum, all);
   int id;
   double kept = all;
   if (!(t > 0.0)) {

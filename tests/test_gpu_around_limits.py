@@ -119,3 +119,22 @@ def test_a_border_of_top_p_among_equal_logits_beside_weights_that_are_no_whole_n
         ids, _, logq = umas.umas_sample_logits(z, u, top_p=reach / all_of)
         assert ids.tolist() == [last] * n, (reach, ids.tolist())
         assert (logq + 40 * math.log(2)).abs().max() <= 1e-5                 # 2 f of 28, and the mass, which is 1 to 3e-9
+
+
+@pytest.mark.parametrize("V", [1000, 1024, 5000, 600000])
+def test_borders_that_rounding_decides_fall_the_same_way_alone_and_among_others(V):
+    """A row of two or four equal parts: at u = 1/4, 1/2 and 3/4 the running mass and what it has to pass are the same number, but for the order of sums."""
+    n = 60 if V < 10000 else 12
+    gen = torch.Generator("cuda").manual_seed(V)
+    z = torch.cat([torch.randn(n // 2, V // p, device="cuda", generator=gen).repeat(1, p) for p in (2, 4)])
+    n = len(z)
+    for j, t in ((1, 1.0), (2, 0.7), (3, 1.9)):
+        u, t_of = torch.full((n,), j / 4, device="cuda"), torch.full((n,), t, device="cuda")
+        got = umas.umas_sample_logits(z, u, temperature=t_of)
+        one = [umas.umas_sample_logits(z[i:i + 1], u[i:i + 1], temperature=t_of[i:i + 1]) for i in range(n)]
+        assert same(got, [torch.cat(x) for x in zip(*one)]), t
+        assert same(got, umas.umas_sample_logits(z, u, temperature=float(t_of[0]))), t
+        k_of = torch.zeros(n, dtype=torch.int32, device="cuda")
+        assert same(got, umas.umas_sample_logits(z, u, temperature=float(t_of[0]), top_k=k_of)), t
+        rows = slice(0 if j == 2 else n // 2, n)                     # whose parts end there: the last token of one or the first of the next
+        assert ((got[0][rows].long() - V // 4 * j).abs() <= 1).all()
