@@ -528,7 +528,7 @@ umas_status umas_distill_fwd_bwd(const void* H, const void* W, umas_dtype dtype,
  * umas_rms_norm_quantized leaves y in 8 bits instead: q = y / scale in e4m3 (4 bits of exponent, 3 of mantissa, no infinities, largest 448), rounded to
  * nearest, scale_i = max_j |y_ij| / 448 and 1 for a row of zeros; y is not rounded on the way.
  *   q            DEVICE uint8 [n_rows, d], 16-byte aligned
- *   scale        DEVICE float [n_rows]; of a row that holds something that is no number, or an infinity, scale and q are no numbers either
+ *   scale        DEVICE float [n_rows]; of a row whose y holds something that is no number, or an infinity, scale and q are no numbers either
  *
  * Backward, a_j = dy_j gain_j:
  *   dx_j = i (a_j - s_j i^2/d sum_k a_k s_k) + dhidden_j;  dgain_j = sum over rows of dy_j s_j i

@@ -146,6 +146,7 @@ k_rms_norm(NormArgs A) {
     if constexpr (QUANT) {
       c = row_reduce<T>(c, s_red, most) / 448.f;
       if (!(c > 0.f) && c == c) c = 1.f;                       // a row of zeros
+      if (c == INFINITY) c = NAN;                              // an infinite gain, or a product beyond float32: no scale brings the row into 8 bits
       if (t == 0) A.scale[row] = c;
       uint8_t* const q = A.q + row * A.d;
 #pragma unroll

@@ -138,3 +138,21 @@ def test_borders_that_rounding_decides_fall_the_same_way_alone_and_among_others(
         assert same(got, umas.umas_sample_logits(z, u, temperature=float(t_of[0]), top_k=k_of)), t
         rows = slice(0 if j == 2 else n // 2, n)                     # whose parts end there: the last token of one or the first of the next
         assert ((got[0][rows].long() - V // 4 * j).abs() <= 1).all()
+
+
+# ------------------------------------------------------------------------------------------------ norm
+@pytest.mark.parametrize("dtype,d", [("bf16", 64), ("bf16", 4096), ("f32", 33), ("f32", 3000)])
+def test_a_row_whose_norm_is_infinite_in_places_is_no_number_in_8_bits(dtype, d):
+    for big in (math.inf, -math.inf, torch.finfo(DT[dtype]).max):      # the last: a normalised 2 times the largest number is beyond it
+        x = torch.randn(9, d, device="cuda").to(DT[dtype])
+        x[:, 3] = 0
+        x[::2, 3] = 2 * math.sqrt(d)                                   # normalised 1.7 to 2: sqrt(d (4 d) / (4 d + d))
+        gain = torch.ones(d, device="cuda").to(DT[dtype])
+        gain[3] = big
+        y = umas.umas_rms_norm(x, gain)[0]
+        q, scale, _, _ = umas.umas_rms_norm_quantized(x, gain)
+        assert y[::2, 3].isinf().all() and scale[::2].isnan().all() and q[::2].float().isnan().all()
+        if math.isfinite(big):
+            assert (scale[1::2] > 0).all() and scale.isfinite()[1::2].all() and q[1::2].float().isfinite().all()
+        else:
+            assert scale[1::2].isnan().all() and q[1::2].float().isnan().all()   # 0 times infinity
