@@ -526,7 +526,8 @@ umas_status umas_distill_fwd_bwd(const void* H, const void* W, umas_dtype dtype,
  * said here, outputs overlap neither each other nor what is read; so in the calls below.
  *
  * umas_rms_norm_quantized leaves y in 8 bits instead: q = y / scale in e4m3 (4 bits of exponent, 3 of mantissa, no infinities, largest 448), rounded to
- * nearest, scale_i = max_j |y_ij| / 448 and 1 for a row of zeros; y is not rounded on the way.
+ * nearest and to even, scale_i = max_j |y_ij| / 448 and 1 for a row of zeros; y is not rounded on the way, and of bf16 q is the quotient's nearest number
+ * itself, the same in any call.
  *   q            DEVICE uint8 [n_rows, d], 16-byte aligned
  *   scale        DEVICE float [n_rows]; of a row whose y holds something that is no number, or an infinity, scale and q are no numbers either
  *

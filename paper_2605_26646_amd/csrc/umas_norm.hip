@@ -1,7 +1,10 @@
 // Root-mean-square norm in front of a head: s = x + r, i = 1 / sqrt(mean s^2 + eps), y = s i g, and its backward pass.
 //
 //   forward   a row stays in registers between its sum of squares and what is written: one read of x and r, one write of s and y
-//   8 bits    c = max_j |y_j| / 448 (448 is the largest e4m3 number), q_j = e4m3(y_j / c): a second reduction over the same registers
+//   8 bits    c = max_j |y_j| / 448 (448 is the largest e4m3 number), q_j = e4m3(y_j / c): a second reduction over the same registers.  y_j / c = 448 s_j gain_j / max_k |s_k gain_k|
+//             does not depend on i, and is taken without it: of bf16 the products are exact, so that the quotient is rounded once to float32, and nothing that lies next to a border of
+//             e4m3 falls to the other side.  (About one in 2500 lies on one; with y_j and c themselves, both rounded, a fifth of
+//             these went to the uneven side, others with another number of rows.)
 //   backward  with a_j = dy_j g_j:  dx = i (a - s i^2/d sum_k a_k s_k) + ds,  dg = sum over rows of dy s i
 // All of it is bound by memory: four arrays of n d elements each way.
 #include <algorithm>
@@ -128,6 +131,8 @@ k_rms_norm(NormArgs A) {
     }
     sum = row_reduce<T>(sum, s_red, add);
     const float inv = 1.f / sqrtf(sum / static_cast<float>(A.d) + A.eps);
+    // in 8 bits, inv's power of 2 in its place, which rounds nothing and keeps products where y is
+    const float by = QUANT ? __uint_as_float(__float_as_uint(inv) & 0x7F800000u) : inv;
     if (A.inv_rms && t == 0) A.inv_rms[row] = inv;
     float c = 0.f;
 #pragma unroll
@@ -137,16 +142,20 @@ k_rms_norm(NormArgs A) {
       Piece<E>::unpack(g[k], b);
 #pragma unroll
       for (int i = 0; i < N; ++i) {
-        a[i] = a[i] * inv * b[i];
+        a[i] = a[i] * by * b[i];
         if constexpr (QUANT) c = most(c, fabsf(a[i]));
       }
       if constexpr (!QUANT)
         if (t + k * T < pieces) store_piece(static_cast<E*>(A.y) + row * A.d, t + k * T, A.d, Piece<E>::pack(a));
     }
     if constexpr (QUANT) {
-      c = row_reduce<T>(c, s_red, most) / 448.f;
-      if (!(c > 0.f) && c == c) c = 1.f;                       // a row of zeros
-      if (c == INFINITY) c = NAN;                              // an infinite gain, or a product beyond float32: no scale brings the row into 8 bits
+      float top = row_reduce<T>(c, s_red, most);
+      c = top > 0.f ? top * (inv / by) / 448.f : top;
+      if (c == 0.f) {                                          // a row of zeros
+        c = 1.f;
+        top = INFINITY;
+      }
+      if (c == INFINITY) c = top = NAN;                        // an infinite gain, or a product beyond float32: no scale brings the row into 8 bits
       if (t == 0) A.scale[row] = c;
       uint8_t* const q = A.q + row * A.d;
 #pragma unroll
@@ -157,9 +166,9 @@ k_rms_norm(NormArgs A) {
         Piece<E>::unpack(g[k], b);
 #pragma unroll
         for (int i = 0; i < N; ++i) {
-          a[i] = a[i] * inv * b[i] / c;
-          // the quotient of the largest one may round to just above 448; what is no number stays none
-          a[i] = a[i] > 448.f ? 448.f : a[i] < -448.f ? -448.f : a[i];
+          a[i] = a[i] * by * b[i] * 0.875f / top * 512.f;      // 448 = 7/8 of 512: nothing runs over, and of bf16 nothing rounds but the quotient
+          // of float32, 7/8 of the largest one may round up; what is no number stays none
+          if constexpr (std::is_same<E, float>::value) a[i] = a[i] > 448.f ? 448.f : a[i] < -448.f ? -448.f : a[i];
         }
         uint32_t w[N / 4];
 #pragma unroll

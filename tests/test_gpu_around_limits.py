@@ -156,3 +156,28 @@ def test_a_row_whose_norm_is_infinite_in_places_is_no_number_in_8_bits(dtype, d)
             assert (scale[1::2] > 0).all() and scale.isfinite()[1::2].all() and q[1::2].float().isfinite().all()
         else:
             assert scale[1::2].isnan().all() and q[1::2].float().isnan().all()   # 0 times infinity
+
+
+@pytest.mark.parametrize("d", [64, 512, 1024, 2048, 3584, 8192])
+def test_quotients_on_a_border_of_8_bits_go_to_the_even_side_in_any_call(d):
+    """448 s gain / max |s gain|: products of two bf16 numbers have 16 bits, so float64 has the quotient to 2^-53, and what lies on no border lies 2^-24 of itself and more from each."""
+    n = 2100                                                           # more rows than those that a workgroup each takes
+    torch.manual_seed(d)
+    x, r = torch.randn(n, d).bfloat16(), (torch.randn(n, d) * (0.5 + 4 * torch.rand(n, 1))).bfloat16()
+    gain = (1 + 0.3 * torch.randn(d)).bfloat16()
+    x, r, g = x.cuda(), r.cuda(), gain.cuda()
+    q, scale, hidden, inv = umas.umas_rms_norm_quantized(x, g, r)
+    t = hidden.cpu().double() * gain.double()
+    t = 448 * t / t.abs().max(1, keepdim=True).values
+    bits = torch.arange(127, dtype=torch.uint8)
+    value = bits.view(torch.float8_e4m3fn).double()
+    border = (value[1:] + value[:-1]) / 2
+    at = torch.bucketize(t.abs(), border)                              # the nearest one's bits; of what lies on a border the lower one's
+    on = border[at.clamp(max=125)] == t.abs()
+    assert on.sum() > n * d / 20000                                    # they do not lie there by chance alone
+    at = torch.where(on & (at % 2 == 1), at + 1, at)
+    got = q.cpu().view(torch.uint8)
+    assert torch.equal((got & 127).long(), at) and torch.equal((got & 127 != 0) & (got > 127), (at != 0) & (t < 0))
+    for rows in (1, 5, 300):
+        few = umas.umas_rms_norm_quantized(x[:rows], g, r[:rows])
+        assert torch.equal(few[0].view(torch.uint8), q[:rows].view(torch.uint8))
