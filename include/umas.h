@@ -590,7 +590,7 @@ umas_status umas_sample_tokens(const void* H, const void* W, umas_dtype dtype, i
 
 /* The global norm of a list of gradients, and clipping:
  *   N = sqrt(sum over all arrays of g^2);  c = max_norm / N where N > max_norm, else 1;  out = c g
- * Squares are summed in float64.  A norm that is no finite number scales nothing (c = 1): n_not_finite says that the step is to be left out.
+ * Squares are summed in float64, which holds the norm of any finite numbers.  One of numbers that are not scales nothing (c = 1): n_not_finite says that the step is to be left out.
  *   gradients  HOST [n], read inside the call: arrays of any size, each of its own type, aligned to that; out is grad (in place; with c = 1 nothing is
  *              written) or another array of the same type and size.  No output may overlap anything else of the list (UMAS_EINVAL).
  *   max_norm   > 0; infinity: the norm alone
@@ -603,8 +603,8 @@ typedef struct umas_gradient {
   int32_t dtype;                 /* umas_dtype */
 } umas_gradient;
 typedef struct umas_clip_stats {
-  float norm;
-  float scale;                   /* c */
+  float norm;                    /* infinite from 3.4e38 on */
+  float scale;                   /* c; out is as near to c g where float32 has no number for c */
   int64_t n_not_finite;          /* numbers that are infinite or none */
 } umas_clip_stats;
 size_t umas_clip_workspace_bytes(int32_t n);

@@ -138,13 +138,14 @@ k_clip_norm(const ClipArgs<Table> A) {
   for (int w = 0; w < kCT / kWave; ++w) { sum += s_sum[w]; b += s_bad[w]; }
   A.part[blockIdx.x] = ClipPart{sum, b};
 }
-template <typename E>
-__device__ __forceinline__ E scaled(float x, float c) {
-  if constexpr (std::is_same<E, uint16_t>::value) return f2bf(x * c);
-  else return x * c;
-}
-template <typename E>
-__device__ __forceinline__ void scale_chunk(const E* p, E* o, int64_t n, float c) {   // p may be o
+// c, in float64 where float32 has few bits for it or none (a norm of 1e38 and more, a max_norm of 1e-30)
+template <typename C>
+struct Factor {
+  C c;
+  __device__ __forceinline__ float operator()(float x) const { return static_cast<float>(x * c); }
+};
+template <typename E, class Times>
+__device__ __forceinline__ void scale_chunk(const E* p, E* o, int64_t n, Times times) {   // p may be o
   constexpr int N = 16 / sizeof(E);
   const int whole = static_cast<int>(n < kChunk ? n : kChunk) / N;
   for (int i = threadIdx.x; i < whole; i += kCT) {
@@ -153,14 +154,18 @@ __device__ __forceinline__ void scale_chunk(const E* p, E* o, int64_t n, float c
     u32x4u v;
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
-      if constexpr (sizeof(E) == 2) v[j] = pack_bf16x2(x[2 * j] * c, x[2 * j + 1] * c);
-      else v[j] = __float_as_uint(x[j] * c);
+      if constexpr (sizeof(E) == 2) v[j] = pack_bf16x2(times(x[2 * j]), times(x[2 * j + 1]));
+      else v[j] = __float_as_uint(times(x[j]));
     }
     __builtin_nontemporal_store(v, reinterpret_cast<u32x4u*>(o + i * N));
   }
   if (n >= kChunk) return;
   const int at = whole * N + threadIdx.x;
-  if (at < n) o[at] = scaled<E>(value_of(p[at]), c);
+  if (at < n) {
+    const float x = times(value_of(p[at]));
+    if constexpr (std::is_same<E, uint16_t>::value) o[at] = f2bf(x);
+    else o[at] = x;
+  }
 }
 template <class Table>
 __global__ void __launch_bounds__(kCT)
@@ -179,7 +184,8 @@ k_clip_scale(const ClipArgs<Table> A, int parts) {
   for (int w = 0; w < kCT / kWave; ++w) { sum += s_sum[w]; bad += s_bad[w]; }
   const double norm = sqrt(sum);
   // a norm that is no finite number scales nothing: the comparison is false for one that is none
-  const float c = norm > A.max_norm && norm < INFINITY ? static_cast<float>(A.max_norm / norm) : 1.f;
+  const double exact = norm > A.max_norm && norm < INFINITY ? A.max_norm / norm : 1.0;
+  const float c = static_cast<float>(exact);
   if (blockIdx.x == 0 && threadIdx.x == 0) *A.stats = umas_clip_stats{static_cast<float>(norm), c, bad};
   const ClipEntry* const e = A.entries();
   const unsigned wg = gridDim.x - 1 - blockIdx.x;            // from the end
@@ -189,8 +195,12 @@ k_clip_scale(const ClipArgs<Table> A, int parts) {
     while (e[at].first > k - 1) --at;
     if (c == 1.f && e[at].in == e[at].out) continue;         // as it is
     const int64_t off = static_cast<int64_t>(k - 1 - e[at].first) * kChunk, rest = e[at].n - off;
-    if (e[at].bf16) scale_chunk(static_cast<const uint16_t*>(e[at].in) + off, static_cast<uint16_t*>(e[at].out) + off, rest, c);
-    else scale_chunk(static_cast<const float*>(e[at].in) + off, static_cast<float*>(e[at].out) + off, rest, c);
+    auto scale = [&](auto times) {
+      if (e[at].bf16) scale_chunk(static_cast<const uint16_t*>(e[at].in) + off, static_cast<uint16_t*>(e[at].out) + off, rest, times);
+      else scale_chunk(static_cast<const float*>(e[at].in) + off, static_cast<float*>(e[at].out) + off, rest, times);
+    };
+    if (exact < 0x1p-100) scale(Factor<double>{exact});
+    else scale(Factor<float>{c});
   }
 }
 

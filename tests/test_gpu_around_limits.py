@@ -181,3 +181,24 @@ def test_quotients_on_a_border_of_8_bits_go_to_the_even_side_in_any_call(d):
     for rows in (1, 5, 300):
         few = umas.umas_rms_norm_quantized(x[:rows], g, r[:rows])
         assert torch.equal(few[0].view(torch.uint8), q[:rows].view(torch.uint8))
+
+
+# ------------------------------------------------------------------------------------------------ clipping
+@pytest.mark.parametrize("max_norm", [1.0, 1e-4, 1e-20, 1e-30])
+def test_factors_below_the_normal_numbers_of_32_bits(max_norm):
+    """Norms of 1e38 and more over a small bound: out is c g to 2 f and its rounding, whatever float32 has for c."""
+    for size, big in ((1, 3e38), (9001, 3e38), (20000, 1e37), (5000, 2e30)):
+        grads = [(big * (0.5 + 0.5 * torch.rand(size, device="cuda"))), -(big * (0.5 + 0.5 * torch.rand(size + 3, device="cuda"))).bfloat16(), torch.ones(5, device="cuda")]
+        norm = math.sqrt(sum(float(g.double().square().sum()) for g in grads))
+        c = max_norm / norm
+        out = [torch.full_like(g, 7) for g in grads]
+        stats, _ = umas.umas_clip_gradients(grads, max_norm, out=out)
+        s = umas.read_clip_stats(stats)[0]
+        assert s["n_not_finite"] == 0 and (s["norm"] == np.inf if norm > 3.5e38 else abs(s["norm"] / norm - 1) < 2 * F)
+        assert abs(float(s["scale"]) - c) <= 2 * F * c + 2.0 ** -149
+        for o, g in zip(out, grads):
+            want, u = g.double() * c, 2.0 ** -8 if g.dtype == torch.bfloat16 else 0.0
+            # half a step of the smallest numbers, which bf16's are of 2^-133
+            assert ((o.double() - want).abs() <= (u + 3 * F) * want.abs() + (2.0 ** -134 if u else 2.0 ** -150)).all(), (size, big)
+        umas.umas_clip_gradients(grads, max_norm)
+        assert same(grads, out)
