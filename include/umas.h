@@ -522,12 +522,13 @@ umas_status umas_distill_fwd_bwd(const void* H, const void* W, umas_dtype dtype,
  *   hidden       DEVICE [n_rows, d]: s, what goes on past the norm; NULL exactly where residual is.  It may be x or residual themselves.
  *   y            DEVICE [n_rows, d]; may be x
  *   inv_rms      DEVICE float [n_rows]: i, for the backward pass; may be NULL
- * All arrays but inv_rms have the type dtype and are 16-byte aligned; 1 <= d <= 16384, a multiple of 8 for bf16.  Sums are float32.  But for what is
- * said here, outputs overlap neither each other nor what is read; so in the calls below.
+ * All arrays but inv_rms have the type dtype and are 16-byte aligned; 1 <= d <= 16384, a multiple of 8 for bf16.  Sums are float32: a row
+ * whose sum of squares is beyond its largest number has i = 0, as one that holds an infinity.  But for what is said here, outputs overlap neither each other
+ * nor what is read; so in the calls below.
  *
  * umas_rms_norm_quantized leaves y in 8 bits instead: q = y / scale in e4m3 (4 bits of exponent, 3 of mantissa, no infinities, largest 448), rounded to
  * nearest and to even, scale_i = max_j |y_ij| / 448 and 1 for a row of zeros; y is not rounded on the way, and of bf16 q is the quotient's nearest number
- * itself, the same in any call.
+ * itself, the same in any call (where the row's largest |y| is not below 1e-30).
  *   q            DEVICE uint8 [n_rows, d], 16-byte aligned
  *   scale        DEVICE float [n_rows]; of a row whose y holds something that is no number, or an infinity, scale and q are no numbers either
  *
@@ -554,14 +555,16 @@ umas_status umas_rms_norm_bwd(const void* dy, const void* hidden, const void* ga
  *   (sum of w) reaches top_p of the mass of them all (1: all).  The token is the first, in rising order, at which the running mass of
  *   what is kept passes u times the kept mass.
  * Logits of -infinity and those that are no number are never drawn and have no mass.  Masses are float64, or where a filter is on whole numbers of 2^-s,
- * s = min(51, 62 - log2 V rounded up) (2^-44 at 151 936 tokens): a w below half of that counts as 0 there, but for the mass of all tokens that top_p is of where neither top_k nor min_p
- * is on, which is float64.  A w itself is off by 2.2e-12 of its value at most,
- * and one below 1e-290 counts as 0; temperatures above 1.4e30 count as that.
- * The same inputs give the same token, whatever the other rows and the workspace are.
+ * s = min(51, 62 - log2 V rounded up) (2^-44 at 151 936 tokens): a w below half of that counts as 0 there, but for the mass of all tokens, which top_p is
+ * of where neither top_k nor min_p is on: that is float64.  A w itself is off by 2.2e-12 of its value at most, and one below 1e-290 counts as 0;
+ * temperatures above 1.4e30 count as that.
+ * The same logits, u and settings give the same token, logp and logq, whatever the other rows and the workspace are.  (Of a head, the last bits of logits
+ * differ between calls of few selected rows, up to 64, and calls of more, which take the sums over d in another order.)
  *   logits       DEVICE [n_rows, V] of the type dtype, row i at logits + i * row_stride, row_stride >= V, aligned to its type
  *   u            DEVICE float [n_rows], uniform on [0,1); below 0 or no number counts as 0, from 1 on the last kept token is drawn
  *   ids          DEVICE int32 [n_rows]; -1 for a row that has nothing to draw from
- *   logp         DEVICE float [n_rows] or NULL: log softmax(z)[id], what umas_policy_logprobs gives; 0 where id is -1
+ *   logp         DEVICE float [n_rows] or NULL: log softmax(z)[id], what umas_policy_logprobs gives; 0 where id is -1.  Its sum is float64, of exponentials that are float32 but for
+ *                temperature 1 without top_k and min_p: off by some 2^-22 of the mean distance to the largest logit
  *   logq         DEVICE float [n_rows] or NULL: log-probability of the token under what it was drawn from; 0 where id is -1
  * umas_sample_tokens takes the logits from a head, z = W h_i (float accumulate), for the selected rows; ids, logp and logq of other rows are -1, 0
  * and 0.  H, W, rowsel, n_sel, dtype and their limits as in umas_policy_logprobs; u and the settings of a row lie at its number in [0, n_rows).
@@ -590,7 +593,8 @@ umas_status umas_sample_tokens(const void* H, const void* W, umas_dtype dtype, i
 
 /* The global norm of a list of gradients, and clipping:
  *   N = sqrt(sum over all arrays of g^2);  c = max_norm / N where N > max_norm, else 1;  out = c g
- * Squares are summed in float64, which holds the norm of any finite numbers.  One of numbers that are not scales nothing (c = 1): n_not_finite says that the step is to be left out.
+ * Squares are summed in float64, which holds the norm of any finite numbers.  One of numbers that are not scales nothing (c = 1): n_not_finite says that the
+ * step is to be left out.
  *   gradients  HOST [n], read inside the call: arrays of any size, each of its own type, aligned to that; out is grad (in place; with c = 1 nothing is
  *              written) or another array of the same type and size.  No output may overlap anything else of the list (UMAS_EINVAL).
  *   max_norm   > 0; infinity: the norm alone

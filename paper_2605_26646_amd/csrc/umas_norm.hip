@@ -364,9 +364,9 @@ k_norm_gain(const float* __restrict__ part, int parts, int d, int accumulate, fl
 }
 
 // ------------------------------------------------------------------ host side
-// launch(T, NV): threads to a row and pieces to a thread.  One piece: a wavefront, whatever the number of rows (bf16, 512 columns with a residual: 2000 rows 4.3 us, by workgroups
-// 4.6, 40 000 rows 29 and 49).  Up to four: a workgroup while rows are few (2048 columns: 64 rows 4.3 and 4.2 us, in 8 bits 5.9 and 4.3; 1000 rows 5.0 and 4.6; 2000 as
-// fast; 4000 rows 10.9 and 13.0, 40 000 rows 113 and 115).  More: a workgroup (4096 columns: 500 rows 5.8 and 4.7 us, 8000 rows 45.6 and 41.3, in 8 bits 47.2 and 40.4).
+// launch(T, NV): threads to a row and pieces to a thread.  One piece: a wavefront, whatever the number of rows (bf16, 512 columns with a residual: 2000 rows 3.2 us, by workgroups
+// 4.3, 40 000 rows 26 and 40).  Up to four: a workgroup while rows are few (2048 columns: 64 rows 3.3 and 2.9 us, in 8 bits 4.7 and 3.6; 1000 rows 4.5 and 4.2; 2000 as
+// fast; 4000 rows 11.0 and 12.9, 40 000 rows 113 and 116).  More: a workgroup (4096 columns: 500 rows 5.2 and 4.3 us, 8000 rows 39.2 and 40.3, in 8 bits 41.0 and 37.2).
 constexpr int64_t kWideRows = 2048;
 template <class Launch>
 void with_width(int pieces, int64_t rows, Launch launch) {

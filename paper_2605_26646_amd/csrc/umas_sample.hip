@@ -7,13 +7,13 @@
 // whose sums are exact in any order (64-bit atomics in LDS give the same result whichever comes first).
 //
 // The first launch, k_sample_open, is the one pass over all logits: maxima of groups of 64, and of units of 1024 the maximum, the sum of exponentials and, where all tokens' mass decides,
-// that mass in float64.  From memory that is a read at 5.6 TB/s (400 float32 rows of 151 936: 43 us); where float64 exponentials count, they bound it (twelve float64 instructions a
-// logit of 5.4 cycles each: 777 float32 rows of 50 001 37 us, 156 MB at 4.2 TB/s).
+// that mass in float64.  From memory that is a read at 5.6 TB/s (400 float32 rows of 151 936: 43 us); where float64 exponentials count, a wavefront first reads its
+// two units and then computes, one after the other: 777 float32 rows of 50 001 39 us, of which reading 156 MB is 25 and fifteen float64 instructions a logit, of 5.4 cycles each, are 20.
 // The second, k_sample_row, gives a workgroup to a row.  Without filters the unit and then the token are found from the units' masses.  Else the front is listed: the tokens that the
-// 64th largest of the threads' group maxima bounds, or all that min_p leaves; up to 512 of them decide by themselves if nothing behind them can count (13 us for a row of 152 064, 14 for 256).
+// 64th largest of the threads' group maxima bounds, or all that min_p leaves; up to 512 of them decide by themselves if nothing behind them can count (13 us for a row of 152 064, 14.5 for 256).
 // Rows that are spread, whose border lies behind the front, go through four more launches over the chip: counts of the tokens by their distance to the front (k_sample_count), from these the
-// thresholds between which a border lies (k_sample_bracket), the sums above and lists between them (k_sample_sums), and the border and token from those (k_sample_flat): 13, 10,
-// 33 and 22 us for what is spread among 256 rows.  A single row does all of it in the second launch.  Where lists overflow, with floods of equal logits, thresholds are found bit by bit, eleven
+// thresholds between which a border lies (k_sample_bracket), the sums above and lists between them (k_sample_sums), and the border and token from those (k_sample_flat): 11, 10,
+// 28 and 25 us for what is spread among 256 rows.  A single row does all of it in the second launch.  Where lists overflow, with floods of equal logits, thresholds are found bit by bit, eleven
 // at a time from the top, with a histogram of counts or masses (draw_by_passes): right for every row, and slow.
 #include <float.h>
 
@@ -1663,7 +1663,8 @@ umas_status sample_rows(const Logits<In>& L, const Settings& S, const int32_t* r
     UMAS_LAUNCHED("k_sample_row");
     return UMAS_OK;
   }
-  // the front decides where it holds the first k, but for rows of many equal logits: no launches for others, which cost 4 us each where there is nothing for them to do
+  // the front decides where it holds the first k, or all that min_p leaves, but for rows of many equal logits: no launches for others, which cost 4 us each where there is nothing for them to do
+  // (bf16 rows of 152 064 under top_k 20: 2 rows 18 us and with them 23.5, 24 rows 18.7 and 24.5, 256 rows 33 and 41, 1024 rows 116 and 124; float32 the same differences)
   const bool decided = !S.top_k_of && S.top_k >= 1 && S.top_k <= std::min(kTopRank, L.units * kGroupsPerUnit / 8);
   if (w.flat.parts == 0 || decided) {
     hipLaunchKernelGGL((k_sample_row<In, kOneT, Filter::kSomeInOne>), dim3(n), dim3(kOneT), 0, st, L, C, w.flat);
